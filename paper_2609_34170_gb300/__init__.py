@@ -13,5 +13,8 @@ from ._binding import (  # noqa: F401
     ravel_set_state, ravel_step_kernel_count, ravel_profile_step, ravel_gemm, ravel_gemm_noalloc,
     ravel_gemm_noalloc_status, ravel_debug_inject, RAVEL_FAULT_PREFIX_LEN, RAVEL_FAULT_WITHHOLD_ARRIVAL,
     ravel_status_string, ravel_last_error,
+    ravel_cache_create, ravel_cache_destroy, ravel_cache_reset, ravel_cache_append, ravel_cache_attend,
+    ravel_cache_evict, ravel_cache_read,
 )
+from .cache import ContextCache  # noqa: F401
 from .session import RollingSession  # noqa: F401

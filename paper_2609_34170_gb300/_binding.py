@@ -39,6 +39,11 @@ class RavelWeights(C.Structure):
                 + [(n, C.c_void_p) for n in ADAPTER_FIELDS])
 
 
+class RavelCacheConfig(C.Structure):
+    _fields_ = [(n, C.c_int) for n in (
+        "layers", "n_q_heads", "n_kv_heads", "head_dim", "max_tokens", "max_batch", "max_queries", "dtype")]
+
+
 class RavelError(RuntimeError):
     def __init__(self, status: int, msg: str):
         self.status = status
@@ -62,7 +67,7 @@ def load(path: str | None = None):
     if not os.path.exists(path):
         raise OSError(f"{path} is missing: build it with paper_2609_34170_gb300.build.build()")
     L = C.CDLL(path)
-    vp, i, pp = C.c_void_p, C.c_int, C.POINTER(C.c_void_p)
+    vp, i, ll, pp = C.c_void_p, C.c_int, C.c_longlong, C.POINTER(C.c_void_p)
     sig = {
         "ravel_create": (i, [C.POINTER(RavelConfig), C.POINTER(RavelWeights), i, pp]),
         "ravel_destroy": (None, [vp]),
@@ -85,6 +90,14 @@ def load(path: str | None = None):
         "ravel_debug_inject": (i, [vp, i, i, vp]),
         "ravel_status_string": (C.c_char_p, [i]),
         "ravel_last_error": (C.c_char_p, [vp]),
+        "ravel_cache_create": (i, [C.POINTER(RavelCacheConfig), i, pp]),
+        "ravel_cache_destroy": (None, [vp]),
+        "ravel_cache_reset": (i, [vp]),
+        "ravel_cache_append": (i, [vp, i, i, i, vp, vp, ll, ll, vp, vp, vp]),
+        "ravel_cache_attend": (i, [vp, i, i, i, vp, ll, ll, vp, ll, ll, vp, vp, i, i, i, i, C.c_float, vp, ll, i, vp]),
+        "ravel_cache_evict": (i, [vp, i, vp, i, i, vp, vp, ll, i, i, i, vp, vp, vp, vp]),
+        "ravel_cache_read": (i, [vp, i, i, i, vp, vp, vp, vp, vp]),
+        "ravel_cache_last_error": (C.c_char_p, [vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -286,3 +299,102 @@ def ravel_status_string(status: int) -> str:
 
 def ravel_last_error(h) -> str:
     return load().ravel_last_error(h).decode()
+
+
+# ---- the 8-bit context cache (include/ravel_cache.h)
+
+
+def _check_cache(c, status: int, what: str):
+    if status != 0:
+        raise RavelError(status, f"{what}: {load().ravel_cache_last_error(c).decode()}")
+
+
+def _strided(t, dtype, heads: int, head_dim: int, name: str):
+    """(address, robot stride, token stride) of a [B, n, heads, head_dim] CUDA
+    tensor whose heads are contiguous (columns of a projection's rows will do)."""
+    shape, stride = t.shape, t.stride()
+    if not t.is_cuda or t.dtype != dtype:
+        raise ValueError(f"{name} must be a CUDA tensor of dtype {dtype}, got {t.dtype} on {t.device}")
+    if len(shape) != 4 or shape[2] != heads or shape[3] != head_dim:
+        raise ValueError(f"{name} must be [batch, n, {heads}, {head_dim}], got {tuple(shape)}")
+    if (stride[3] != 1 and head_dim > 1) or (stride[2] != head_dim and heads > 1):
+        raise ValueError(f"{name}: the heads of a token must be contiguous")
+    return t.data_ptr(), stride[0], stride[1]
+
+
+def _ints(t, batch: int, name: str):
+    """Device pointer of an int32 CUDA tensor [batch] (or None)."""
+    if t is None:
+        return None
+    if t.dtype.itemsize != 4 or t.dtype.is_floating_point or not t.is_cuda or t.shape != (batch,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 CUDA tensor [{batch}]")
+    return t.data_ptr()
+
+
+def ravel_cache_create(layers: int, n_q_heads: int, n_kv_heads: int, head_dim: int, max_tokens: int, max_batch: int,
+                       max_queries: int, dtype: int = RAVEL_BF16, device: int = 0):
+    c = RavelCacheConfig(layers, n_q_heads, n_kv_heads, head_dim, max_tokens, max_batch, max_queries, dtype)
+    h = C.c_void_p()
+    st = load().ravel_cache_create(C.byref(c), device, C.byref(h))
+    if st != 0:
+        raise RavelError(st, "ravel_cache_create failed (see stderr)")
+    return h
+
+
+def ravel_cache_destroy(c):
+    load().ravel_cache_destroy(c)
+
+
+def ravel_cache_reset(c):
+    _check_cache(c, load().ravel_cache_reset(c), "ravel_cache_reset")
+
+
+def ravel_cache_append(c, layer: int, k, v, starts=None, counts=None, stream=None):
+    """k, v [B, n, Hkv, hd] with the same strides; see ravel_cache.h."""
+    B, n, heads, hd = k.shape
+    kp, rs, ts = _strided(k, k.dtype, heads, hd, "k")
+    vp, vrs, vts = _strided(v, k.dtype, heads, hd, "v")
+    if v.shape != k.shape or (vrs, vts) != (rs, ts):
+        raise ValueError("k and v must have the same shape and strides")
+    _check_cache(c, load().ravel_cache_append(c, layer, B, n, kp, vp, rs, ts, _ints(starts, B, "starts"),
+                                              _ints(counts, B, "counts"), _stream_ptr(stream)), "ravel_cache_append")
+
+
+def ravel_cache_attend(c, layer: int, q, out, lengths, counts, max_length: int, causal: bool = True, window: int = 0,
+                       sinks: int = 0, scale: float = 0.0, mass=None, add_mass: bool = False, stream=None):
+    """q, out [B, n, Hq, hd]; mass float32 [B, Hkv, >= max_length] or None; see ravel_cache.h."""
+    B, n, heads, hd = q.shape
+    qp, qrs, qts = _strided(q, q.dtype, heads, hd, "q")
+    op, ors, ots = _strided(out, q.dtype, heads, hd, "out")
+    if out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    if lengths is None:
+        raise ValueError("lengths must be a contiguous int32 CUDA tensor")
+    mp, ms = None, 0
+    if mass is not None:
+        import torch
+        mp, ms = _dptr(mass, torch.float32, "mass"), mass.shape[-1]
+    _check_cache(c, load().ravel_cache_attend(c, layer, B, n, qp, qrs, qts, op, ors, ots, _ints(lengths, B, "lengths"),
+                                              _ints(counts, B, "counts"), max_length, int(causal), window, sinks, scale,
+                                              mp, ms, int(add_mass), _stream_ptr(stream)), "ravel_cache_attend")
+
+
+def ravel_cache_evict(c, layer: int, to, to_layer: int, lengths, mass, keep: int, sinks: int, recent: int, new_lengths,
+                      index, new_mass=None, stream=None):
+    """mass float32 [B, Hkv, tokens]; index int32 [B, Hkv, keep]; see ravel_cache.h."""
+    import torch
+    B = mass.shape[0]
+    _check_cache(c, load().ravel_cache_evict(
+        c, layer, to, to_layer, B, _ints(lengths, B, "lengths"), _dptr(mass, torch.float32, "mass"), mass.shape[-1], keep,
+        sinks, recent, _ints(new_lengths, B, "new_lengths"), _dptr(index, torch.int32, "index"),
+        _dptr(new_mass, torch.float32, "new_mass"), _stream_ptr(stream)), "ravel_cache_evict")
+
+
+def ravel_cache_read(c, layer: int, k, v, firsts=None, lengths=None, stream=None):
+    """k, v [B, Hkv, n, hd], contiguous, written; see ravel_cache.h."""
+    B, n = k.shape[0], k.shape[2]
+    if v.shape != k.shape or v.dtype != k.dtype:
+        raise ValueError("k and v must have the same shape and dtype")
+    _check_cache(c, load().ravel_cache_read(c, layer, B, n, _ints(firsts, B, "firsts"), _ints(lengths, B, "lengths"),
+                                            _dptr(k, name="k"), _dptr(v, name="v"), _stream_ptr(stream)),
+                 "ravel_cache_read")

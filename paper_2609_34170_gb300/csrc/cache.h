@@ -1,0 +1,84 @@
+// Internal launch API of the 8-bit context cache (host side).  Every launcher
+// enqueues on `st` and returns the launch's cudaError_t.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "kernels.h"
+
+namespace ravel {
+
+constexpr int kCacheBlock = 16;      // tokens that share an exponent
+constexpr int kCacheRound = 128;     // capacities are whole multiples of this, so that tiles stay inside
+constexpr int kCacheExpMin = -100;   // least exponent of a block
+
+// One layer of a cache: rows of hdp bytes, [B][Hkv][T][hdp], exponents
+// [B][Hkv][T / 16].  T: the capacity rounded up to kCacheRound.
+struct CacheLayer {
+  uint8_t *k, *v;
+  int8_t *ke, *ve;
+  int Hkv, hd, hdp, T;
+};
+
+struct AppendArgs {
+  CacheLayer c;
+  const void *k, *v;
+  long long robot, token;   // strides in elements
+  int batch, n, max_tokens;
+  const int *starts, *counts;
+  int vec;                  // rows are 16-byte aligned
+  int* err;
+};
+cudaError_t launch_cache_append(const AppendArgs& a, Dtype dt, cudaStream_t st);
+
+struct ReadArgs {
+  CacheLayer c;
+  int batch, n, max_tokens;
+  const int *firsts, *lengths;
+  void *k, *v;
+  int vec;
+  int* err;
+};
+cudaError_t launch_cache_read(const ReadArgs& a, Dtype dt, cudaStream_t st);
+
+struct EvictArgs {
+  CacheLayer from, to;
+  int batch, keep, sinks, recent, max_tokens;
+  const int* lengths;
+  const float* mass;
+  long long mass_stride;
+  int *new_lengths, *index;
+  float* new_mass;
+  int* err;
+};
+cudaError_t launch_cache_evict(const EvictArgs& a, cudaStream_t st);
+
+struct CacheAttnArgs {
+  CacheLayer c;
+  const void* q;
+  void* out;
+  long long q_robot, q_token, out_robot, out_token;
+  const int *lengths, *counts;
+  int batch, n, G, max_length;
+  int causal, window, sinks;
+  float scale_log2;         // softmax scale * log2(e)
+  float* mass;
+  long long mass_stride;
+  int mass_add;
+  int vec;                  // q rows are 16-byte aligned
+  int num_sms;
+  // workspace
+  float* part;              // [units * splits][16][hdp] normalised partial outputs
+  float2* part_ml;          // [units * splits][16] (max, sum)
+  unsigned* arrived;        // [units] splits that have finished (zero between launches)
+  float2* row_ml;           // [B][Hkv][n * G] (max, 1 / sum), written where mass is wanted
+  int* err;
+  // chosen by the launcher
+  int row_tiles, splits;
+};
+constexpr int kCacheSplitCtas = 608;   // row tiles x splits of a launch that splits the tokens
+cudaError_t launch_cache_attend(const CacheAttnArgs& a, Dtype dt, cudaStream_t st);
+cudaError_t init_cache_kernels();
+
+}  // namespace ravel

@@ -1,0 +1,690 @@
+// Attention over the 8-bit context cache for few query rows (single tokens,
+// short runs of queries) and in fp32, and the attention mass of its tokens.
+//
+// Rows: query i, head g of a KV head's group is row r = i * G + g; a CTA owns a
+// tile of 16 rows of one (robot, KV head) and a share (split) of the tokens
+// that the tile sees; its warps take turns at units of 16 * NT tokens, each
+// with its own running maximum, sum and output, which are joined in shared
+// memory and then across the splits.
+//
+// What bounds it is the cache's bytes: 16 query rows against a token cost one
+// m16n8k16 row of MMAs whatever the group's size, so a token's time does not
+// depend on G.  These MMAs take their operands from registers: the codes go
+// from global memory to registers and are widened there (e4m3 -> f16 is exact),
+// in an order of dims and tokens that makes every load 16 bytes: within an MMA
+// the dims of q k (and the tokens of p v) may come in any order that both
+// operands share.  tcgen05 would want the widened codes in shared memory first
+// and 128 rows to work on.
+//
+// Numbers: q is scaled by a power of two per row to a maximum in [2^14, 2^15) and
+// held in f16 -- exactly for bf16 inputs (8 significant bits; what lies 2^38
+// below the row's largest is dropped), in two f16 pieces for fp32 ones (23
+// bits).  Products with the codes are exact in the tensor core's fp32 sums;
+// block exponents and row scales are applied to the sums in fp32.  P is scaled
+// to a maximum of 2^15 and multiplied by 2^(ve - E), E the largest value
+// exponent of the blocks that the row sees: one f16 piece (11 bits) for bf16
+// results, two for fp32 ones; what lies 2^39 below the largest is dropped.
+// Maxima, sums and outputs are fp32.
+#include "cache.cuh"
+#include "launch.h"
+#include "tc_common.cuh"
+
+namespace ravel {
+namespace {
+
+constexpr int RW = 4;             // warps of a CTA
+constexpr float kPExp = 15.f;     // P's largest value is 2^kPExp
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], const uint4& a, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, "
+      "%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// What a tile of rows sees: tokens [0, sink) and [from, to) in units, and the
+// numbers that decide single tokens.
+struct Sight {
+  int len, count;     // the robot's tokens and queries
+  int p0;             // position of query 0 (len - count)
+  int sink_units, from, units;   // unit t is t < sink_units ? t : t - sink_units + from
+};
+
+struct RowMask {
+  int hi, lo, sinks;   // sees j < hi and (j >= lo or j < sinks)
+  __device__ __forceinline__ bool sees(int j) const { return j < hi && (j >= lo || j < sinks); }
+};
+
+__device__ __forceinline__ RowMask row_mask(const CacheAttnArgs& a, const Sight& s, int r) {
+  RowMask m;
+  const int i = r / a.G;
+  m.sinks = a.sinks;
+  m.lo = 0;
+  if (i >= s.count) m.hi = 0;
+  else if (!a.causal) m.hi = s.len;
+  else {
+    m.hi = s.p0 + i + 1;
+    if (a.window > 0) m.lo = max(0, m.hi - a.window);
+  }
+  return m;
+}
+
+// The robot's length and count, checked; a robot out of range sees nothing.
+__device__ __forceinline__ bool robot_sight(const CacheAttnArgs& a, int b, Sight& s) {
+  s.len = a.lengths[b];
+  s.count = a.counts ? a.counts[b] : a.n;
+  const bool ok = s.len >= 0 && s.len <= a.max_length && s.count >= 0 && s.count <= a.n &&
+                  (!a.causal || s.count <= s.len);
+  if (!ok) s.len = s.count = 0;
+  s.p0 = s.len - s.count;
+  return ok;
+}
+
+// Units of `U` tokens that rows r0 .. r1 (r0 < count * G) see between them.
+__device__ __forceinline__ void tile_sight(const CacheAttnArgs& a, Sight& s, int r0, int r1, int U) {
+  const RowMask first = row_mask(a, s, r0), last = row_mask(a, s, min(r1, s.count * a.G - 1));
+  s.from = first.lo / U;
+  s.sink_units = a.window > 0 ? min((a.sinks + U - 1) / U, s.from) : 0;
+  s.units = s.sink_units + (last.hi + U - 1) / U - s.from;
+}
+
+// Query rows r0 .. r0 + 15 into shared memory as the A fragments of the MMAs:
+// word (piece, k-step, lane) holds rows lane / 4 and + 8, dims 64 j + 16 (lane % 4)
+// + 4 s + 0 .. 3 of k-step 4 j + s.  Rows that do not exist are zeros.  fac[r]:
+// 2^exponent taken out of the row, times the softmax scale.
+template <int HDP, int NP, typename T, int THREADS>
+__device__ __forceinline__ void stage_q(const CacheAttnArgs& a, const Sight& s, int b, int h, int r0, uint32_t* frag,
+                                        float* fac) {
+  constexpr int TPR = HDP / 16;   // threads per row
+  for (int w = threadIdx.x; w < 16 * TPR; w += THREADS) {
+    const int lr = w / TPR, d = (w % TPR) * 16, r = r0 + lr;
+    float x[16];
+    const int i = r / a.G;
+    if (i < s.count && d < a.c.hd) {
+      const T* row = (const T*)a.q + (size_t)((long long)b * a.q_robot + (long long)i * a.q_token) +
+                     (size_t)(h * a.G + r % a.G) * a.c.hd;
+      load16(row, d, a.c.hd, a.vec, x);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 16; ++q) x[q] = 0.f;
+    }
+    uint32_t top = 0u;   // bits of the largest magnitude: NaN counts as larger than all
+#pragma unroll
+    for (int q = 0; q < 16; ++q) top = max(top, __float_as_uint(x[q]) & 0x7fffffffu);
+    // the row's threads lie in one warp, TPR of them (4, 8, 12 or 16), at a multiple of 4
+    // lanes but not always aligned to TPR: the maximum goes through shared memory
+    atomicMax((unsigned*)&fac[lr], top);
+  }
+  __syncthreads();
+  for (int w = threadIdx.x; w < 16 * TPR; w += THREADS) {
+    const int lr = w / TPR, d = (w % TPR) * 16, r = r0 + lr;
+    float x[16];
+    const int i = r / a.G;
+    if (i < s.count && d < a.c.hd) {
+      const T* row = (const T*)a.q + (size_t)((long long)b * a.q_robot + (long long)i * a.q_token) +
+                     (size_t)(h * a.G + r % a.G) * a.c.hd;
+      load16(row, d, a.c.hd, a.vec, x);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 16; ++q) x[q] = 0.f;
+    }
+    const uint32_t top = ((const unsigned*)fac)[lr];
+    // factor 2^(14 - exponent), at most 2^126 (rows below 2^-112 keep fewer bits)
+    const int e = min(14 - ((int)(top >> 23) - 127), 126);
+    const bool bad = top >= 0x7f800000u;
+    const float f = bad ? __int_as_float(0x7fffffff) : exp2i(e);
+    // dims d .. d + 15 are k-steps 4 j + 0 .. 3 of lane (4 (row % 8) + c)
+    const int j = d / 64, c = (d / 16) % 4, lane = (lr & 7) * 4 + c;
+#pragma unroll
+    for (int s4 = 0; s4 < 4; ++s4) {
+      const float y0 = x[4 * s4] * f, y1 = x[4 * s4 + 1] * f, y2 = x[4 * s4 + 2] * f, y3 = x[4 * s4 + 3] * f;
+      uint32_t lo = pack_f16x2(y0, y1), hi = pack_f16x2(y2, y3);
+      // fragment registers: a0 (row, dims 0 1), a1 (row + 8, 0 1), a2 (row, 2 3), a3 (row + 8, 2 3)
+      uint32_t* at = frag + ((4 * j + s4) * 32 + lane) * 4 + (lr >> 3);
+      at[0] = lo;
+      at[2] = hi;
+      if (NP == 2) {
+        at += HDP / 16 * 128;
+        at[0] = pack_f16x2(y0 - f16lo(lo), y1 - f16hi(lo));
+        at[2] = pack_f16x2(y2 - f16lo(hi), y3 - f16hi(hi));
+      }
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x < 16) {
+    const uint32_t top = ((const unsigned*)fac)[threadIdx.x];
+    const int e = min(14 - ((int)(top >> 23) - 127), 126);
+    fac[threadIdx.x] = exp2i(-max(e, -126)) * a.scale_log2;   // (e >= -114 for finite rows)
+  }
+  __syncthreads();
+}
+
+// S of the block of 16 tokens whose key rows begin at `k`: s[hh][.] covers
+// tokens 8 hh + 2 c, + 1 for rows g and g + 8.
+template <int HDP>
+struct KeyRegs {
+  uint4 w[2][HDP / 64];   // tokens g and g + 8: 16 bytes at 64 j + 16 c
+  __device__ __forceinline__ void load(const uint8_t* k, int g, int c) {
+#pragma unroll
+    for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+      for (int j = 0; j < HDP / 64; ++j)
+        w[hh][j] = __ldg((const uint4*)(k + (size_t)(g + 8 * hh) * HDP + 64 * j + 16 * c));
+  }
+};
+
+template <int HDP>
+struct ValueRegs {
+  uint32_t w[4][HDP / 32];   // tokens 2 c, 2 c + 1, 2 c + 8, 2 c + 9
+  __device__ __forceinline__ void load(const uint8_t* v, int g, int c) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const uint8_t* row = v + (size_t)(2 * c + (t & 1) + 4 * (t & 2)) * HDP;
+#pragma unroll
+      for (int j = 0; j < HDP / 128; ++j) {
+        const uint4 x = __ldg((const uint4*)(row + 128 * j + 16 * g));
+        w[t][4 * j] = x.x;
+        w[t][4 * j + 1] = x.y;
+        w[t][4 * j + 2] = x.z;
+        w[t][4 * j + 3] = x.w;
+      }
+      if (HDP % 128) {
+        const uint2 x = __ldg((const uint2*)(row + HDP / 128 * 128 + 8 * g));
+        w[t][HDP / 32 - 2] = x.x;
+        w[t][HDP / 32 - 1] = x.y;
+      }
+    }
+  }
+  // dim of column n of MMA tile (word wi, byte i)
+  static __device__ __forceinline__ int dim(int wi, int i, int n) {
+    return wi < HDP / 128 * 4 ? wi / 4 * 128 + 16 * n + wi % 4 * 4 + i
+                              : HDP / 128 * 128 + 8 * n + (wi - HDP / 128 * 4) * 4 + i;
+  }
+};
+
+template <int HDP, int NP, typename T>
+__global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(CacheAttnArgs a) {
+  constexpr int NT = HDP == 64 ? 4 : (HDP == 128 ? 2 : 1);   // blocks of 16 tokens per unit
+  constexpr int U = 16 * NT, KS = HDP / 16;
+  extern __shared__ __align__(16) uint8_t smem[];
+  uint32_t* frag = (uint32_t*)smem;                  // [NP][KS][32][4]
+  float* joint = (float*)(smem + NP * KS * 512);     // [RW][16][HDP] outputs of the warps
+  __shared__ float fac[16];
+  __shared__ float2 warp_ml[RW][16], split_w[16];
+  __shared__ unsigned last;
+
+  const int b = blockIdx.z, h = blockIdx.y, tile = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+  const CacheLayer& L = a.c;
+  const int r0 = tile * 16, rows = min(16, a.n * a.G - r0);
+  const size_t head = (size_t)b * L.Hkv + h;
+  Sight s;
+  if (!robot_sight(a, b, s) && threadIdx.x == 0 && blockIdx.x == 0 && h == 0) raise_error(a.err, ERR_SHAPE);
+  T* out0 = (T*)a.out + (size_t)((long long)b * a.out_robot) + (size_t)h * a.G * L.hd;
+  auto out_row = [&](int r) { return out0 + (size_t)((long long)(r / a.G) * a.out_token) + (size_t)(r % a.G) * L.hd; };
+  if (r0 >= s.count * a.G || s.len == 0) {   // nothing to see: zeros
+    if (split == 0)
+      for (int w = threadIdx.x; w < rows * L.hd; w += RW * 32) out_row(r0 + w / L.hd)[w % L.hd] = from_f32<T>(0.f);
+    if (split == 0 && a.mass && threadIdx.x < rows)
+      a.row_ml[head * a.n * a.G + r0 + threadIdx.x] = make_float2(0.f, 0.f);
+    return;
+  }
+  tile_sight(a, s, r0, r0 + 15, U);
+  const int u0 = (int)((long long)s.units * split / a.splits), u1 = (int)((long long)s.units * (split + 1) / a.splits);
+
+  if (threadIdx.x < 16) fac[threadIdx.x] = 0.f;
+  __syncthreads();
+  stage_q<HDP, NP, T, RW * 32>(a, s, b, h, r0, frag, fac);
+  const RowMask mk[2] = {row_mask(a, s, r0 + g), row_mask(a, s, r0 + g + 8)};
+  const float rf[2] = {fac[g], fac[g + 8]};
+  // tokens that every row that exists sees: [full_lo, full_hi) and below a.sinks
+  const RowMask first = row_mask(a, s, r0), lastm = row_mask(a, s, min(r0 + 15, s.count * a.G - 1));
+  const int full_hi = first.hi, full_lo = lastm.lo;
+
+  const uint8_t *K = L.k + head * L.T * HDP, *V = L.v + head * L.T * HDP;
+  const int8_t *KE = L.ke + head * (L.T / 16), *VE = L.ve + head * (L.T / 16);
+
+  float o[HDP / 8][4];
+#pragma unroll
+  for (int t = 0; t < HDP / 8; ++t)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) o[t][q] = 0.f;
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  int E[2] = {-127, -127};
+
+  KeyRegs<HDP> kr[NT];
+  ValueRegs<HDP> vr[NT];
+  auto unit_token = [&](int u) { return (u < s.sink_units ? u : u - s.sink_units + s.from) * U; };
+  int u = u0 + warp;
+  if (u < u1) {
+    const int j0 = unit_token(u);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) kr[t].load(K + (size_t)(j0 + 16 * t) * HDP, g, c);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) vr[t].load(V + (size_t)(j0 + 16 * t) * HDP, g, c);
+  }
+  for (; u < u1; u += RW) {
+    const int j0 = unit_token(u);
+    float kf[NT];
+    int ve[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      kf[t] = exp2i(KE[j0 / 16 + t]);
+      ve[t] = VE[j0 / 16 + t];
+    }
+    float sc[NT][2][4];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) sc[t][hh][q] = 0.f;
+#pragma unroll
+    for (int j = 0; j < HDP / 64; ++j) {
+#pragma unroll
+      for (int s4 = 0; s4 < 4; ++s4) {
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+          const uint4 qa = *(const uint4*)(frag + ((p * KS + 4 * j + s4) * 32 + lane) * 4);
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) {
+              const uint4 kw = kr[t].w[hh][j];
+              const uint32_t w = s4 == 0 ? kw.x : (s4 == 1 ? kw.y : (s4 == 2 ? kw.z : kw.w));
+              mma_f16(sc[t][hh], qa, e4m3_lo(w), e4m3_hi(w));
+            }
+        }
+      }
+    }
+    const int un = u + RW;
+    const int jn = un < u1 ? unit_token(un) : 0;
+    if (un < u1) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) kr[t].load(K + (size_t)(jn + 16 * t) * HDP, g, c);
+    }
+    // scores in the log2 domain; hidden ones -inf
+    const bool full = j0 + U <= full_hi && (j0 >= full_lo || j0 + U <= a.sinks);
+    bool seen[NT][2];   // the row sees something of the block
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      seen[t][0] = seen[t][1] = full;
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) sc[t][hh][q] *= rf[q >> 1] * kf[t];
+      if (!full) {
+        const int jb = j0 + 16 * t;
+#pragma unroll
+        for (int rr = 0; rr < 2; ++rr)
+          seen[t][rr] = jb < mk[rr].hi && (jb + 16 > mk[rr].lo || jb < mk[rr].sinks);
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            if (!mk[q >> 1].sees(jb + 8 * hh + 2 * c + (q & 1))) sc[t][hh][q] = -INFINITY;
+      }
+    }
+    float alpha[2], mu[2];
+    int En[2];
+#pragma unroll
+    for (int rr = 0; rr < 2; ++rr) {
+      float mx = -INFINITY;
+      En[rr] = E[rr];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) mx = fmaxf(mx, fmaxf(sc[t][hh][2 * rr], sc[t][hh][2 * rr + 1]));
+        if (seen[t][rr]) En[rr] = max(En[rr], ve[t]);
+      }
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+      const float mn = fmaxf(m[rr], mx);
+      mu[rr] = mn == -INFINITY ? 0.f : mn;
+      alpha[rr] = m[rr] == -INFINITY ? 0.f : exp2f(m[rr] - mu[rr]);
+      m[rr] = mn;
+    }
+    // (a factor is 1 in most units: the maximum settles early)
+    if (__any_sync(0xffffffffu, alpha[0] != 1.f || alpha[1] != 1.f || En[0] != E[0] || En[1] != E[1])) {
+      const float f0 = alpha[0] * exp2i(max(E[0] - En[0], -126)), f1 = alpha[1] * exp2i(max(E[1] - En[1], -126));
+      l[0] *= alpha[0];
+      l[1] *= alpha[1];
+#pragma unroll
+      for (int t = 0; t < HDP / 8; ++t) {
+        o[t][0] *= f0;
+        o[t][1] *= f0;
+        o[t][2] *= f1;
+        o[t][3] *= f1;
+      }
+      E[0] = En[0];
+      E[1] = En[1];
+    }
+    const float nb[2] = {kPExp - mu[0], kPExp - mu[1]};
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      uint4 pa[NP];
+      {
+        float p[2][4];
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            p[hh][q] = NP == 2 ? exp2f(sc[t][hh][q] + nb[q >> 1]) : fast_exp2(sc[t][hh][q] + nb[q >> 1]);
+            l[q >> 1] += p[hh][q];
+          }
+        const float f0 = exp2i(max(ve[t] - E[0], -126)), f1 = exp2i(max(ve[t] - E[1], -126));
+        // (a block that the row does not see may have a larger exponent than E: its p are 0)
+        const float g0 = seen[t][0] ? f0 : 0.f, g1 = seen[t][1] ? f1 : 0.f;
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+          p[hh][0] *= g0;
+          p[hh][1] *= g0;
+          p[hh][2] *= g1;
+          p[hh][3] *= g1;
+        }
+        pa[0] = make_uint4(pack_f16x2(p[0][0], p[0][1]), pack_f16x2(p[0][2], p[0][3]), pack_f16x2(p[1][0], p[1][1]),
+                           pack_f16x2(p[1][2], p[1][3]));
+        if (NP == 2)
+          pa[NP - 1] = make_uint4(pack_f16x2(p[0][0] - f16lo(pa[0].x), p[0][1] - f16hi(pa[0].x)),
+                                  pack_f16x2(p[0][2] - f16lo(pa[0].y), p[0][3] - f16hi(pa[0].y)),
+                                  pack_f16x2(p[1][0] - f16lo(pa[0].z), p[1][1] - f16hi(pa[0].z)),
+                                  pack_f16x2(p[1][2] - f16lo(pa[0].w), p[1][3] - f16hi(pa[0].w)));
+      }
+#pragma unroll
+      for (int wi = 0; wi < HDP / 32; ++wi) {
+        // bytes i of two tokens' words side by side
+        const uint32_t x0 = __byte_perm(vr[t].w[0][wi], vr[t].w[1][wi], 0x5140);
+        const uint32_t y0 = __byte_perm(vr[t].w[0][wi], vr[t].w[1][wi], 0x7362);
+        const uint32_t x1 = __byte_perm(vr[t].w[2][wi], vr[t].w[3][wi], 0x5140);
+        const uint32_t y1 = __byte_perm(vr[t].w[2][wi], vr[t].w[3][wi], 0x7362);
+        const uint32_t b0[4] = {e4m3_lo(x0), e4m3_hi(x0), e4m3_lo(y0), e4m3_hi(y0)};
+        const uint32_t b1[4] = {e4m3_lo(x1), e4m3_hi(x1), e4m3_lo(y1), e4m3_hi(y1)};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int p = 0; p < NP; ++p) mma_f16(o[4 * wi + i], pa[p], b0[i], b1[i]);
+      }
+    }
+    if (un < u1) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) vr[t].load(V + (size_t)(jn + 16 * t) * HDP, g, c);
+    }
+  }
+
+  // ---- join the warps: outputs normalised by their own sums, then weighted
+#pragma unroll
+  for (int rr = 0; rr < 2; ++rr) {
+    l[rr] += __shfl_xor_sync(0xffffffffu, l[rr], 1);
+    l[rr] += __shfl_xor_sync(0xffffffffu, l[rr], 2);
+    // (units that every query sees are not masked: a row without a query stops here)
+    const bool real = mk[rr].hi > 0;
+    if (!real) {
+      l[rr] = 0.f;
+      m[rr] = -INFINITY;
+    }
+    const bool has = !(l[rr] <= 0.f);   // (a sum that is not a number stays one)
+    const float f = has ? 1.f / l[rr] : 0.f;
+    const float e2 = exp2i(max(E[rr], -126));
+    const int row = g + 8 * rr;
+    if (c == 0) warp_ml[warp][row] = make_float2(m[rr], l[rr]);
+    float* dst = joint + ((size_t)warp * 16 + row) * HDP;
+    if (row < rows) {
+#pragma unroll
+      for (int wi = 0; wi < HDP / 32; ++wi)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int q = 0; q < 2; ++q)
+            dst[ValueRegs<HDP>::dim(wi, i, 2 * c + q)] = real ? o[4 * wi + i][2 * rr + q] * f * e2 : 0.f;
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x < 16) {   // the warps' weights, in place of (m, l)
+    const int row = threadIdx.x;
+    float M = -INFINITY, S = 0.f;
+#pragma unroll
+    for (int w = 0; w < RW; ++w) M = fmaxf(M, warp_ml[w][row].x);
+#pragma unroll
+    for (int w = 0; w < RW; ++w) {
+      const float2 x = warp_ml[w][row];
+      // a NaN sum has no maximum of its own: it counts as it is
+      const float wt = x.y != x.y ? x.y : (x.x == -INFINITY ? 0.f : exp2f(x.x - M) * x.y);
+      warp_ml[w][row].x = wt;
+      S += wt;
+    }
+    const float inv = !(S <= 0.f) ? 1.f / S : 0.f;
+#pragma unroll
+    for (int w = 0; w < RW; ++w) warp_ml[w][row].x *= inv;
+    split_w[row] = make_float2(M, S);
+  }
+  __syncthreads();
+  auto joined = [&](int row, int d) {
+    float acc = 0.f;
+#pragma unroll
+    for (int w = 0; w < RW; ++w) {
+      const float wt = warp_ml[w][row].x;
+      acc += wt != 0.f ? wt * joint[((size_t)w * 16 + row) * HDP + d] : 0.f;
+    }
+    return acc;
+  };
+  if (a.splits == 1) {
+    for (int w = threadIdx.x; w < rows * L.hd; w += RW * 32) {
+      const int row = w / L.hd, d = w % L.hd;
+      out_row(r0 + row)[d] = from_f32<T>(joined(row, d));
+    }
+    if (a.mass && threadIdx.x < rows) {
+      const float2 x = split_w[threadIdx.x];
+      a.row_ml[head * a.n * a.G + r0 + threadIdx.x] = make_float2(x.x == -INFINITY ? 0.f : x.x, !(x.y <= 0.f) ? 1.f / x.y : 0.f);
+    }
+    return;
+  }
+  const size_t unit = head * a.row_tiles + tile;
+  float* part = a.part + (unit * a.splits + split) * 16 * HDP;
+  for (int w = threadIdx.x; w < rows * HDP; w += RW * 32) __stcg(part + w, joined(w / HDP, w % HDP));
+  if (threadIdx.x < rows) __stcg(a.part_ml + (unit * a.splits + split) * 16 + threadIdx.x, split_w[threadIdx.x]);
+  // the last split to arrive joins them all, in their order
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) last = atomicInc(a.arrived + unit, (unsigned)a.splits - 1u) == (unsigned)a.splits - 1u;
+  __syncthreads();
+  if (!last) return;
+  __threadfence();
+  float* wts = joint;   // [splits][16]
+  if (threadIdx.x < 16 && (int)threadIdx.x < rows) {
+    const int row = threadIdx.x;
+    const float2* ml = a.part_ml + unit * a.splits * 16 + row;
+    float M = -INFINITY, S = 0.f;
+    for (int q = 0; q < a.splits; ++q) M = fmaxf(M, __ldcg(ml + q * 16).x);
+    for (int q = 0; q < a.splits; ++q) {
+      const float2 x = __ldcg(ml + q * 16);
+      const float wt = x.y != x.y ? x.y : (x.x == -INFINITY ? 0.f : exp2f(x.x - M) * x.y);
+      wts[q * 16 + row] = wt;
+      S += wt;
+    }
+    const float inv = !(S <= 0.f) ? 1.f / S : 0.f;
+    for (int q = 0; q < a.splits; ++q) wts[q * 16 + row] *= inv;
+    if (a.mass) a.row_ml[head * a.n * a.G + r0 + row] = make_float2(M == -INFINITY ? 0.f : M, inv);
+  }
+  __syncthreads();
+  const float* p0 = a.part + unit * a.splits * 16 * HDP;
+  for (int w = threadIdx.x; w < rows * (HDP / 4); w += RW * 32) {
+    const int row = w / (HDP / 4), d = w % (HDP / 4) * 4;
+    if (d >= L.hd) continue;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int q = 0; q < a.splits; ++q) {
+      const float4 x = __ldcg((const float4*)(p0 + ((size_t)q * 16 + row) * HDP + d));
+      const float wt = wts[q * 16 + row];   // (0 times an empty split's zeros)
+      acc.x += wt * x.x;
+      acc.y += wt * x.y;
+      acc.z += wt * x.z;
+      acc.w += wt * x.w;
+    }
+    T* dst = out_row(r0 + row) + d;   // hd is a multiple of 8
+    dst[0] = from_f32<T>(acc.x);
+    dst[1] = from_f32<T>(acc.y);
+    dst[2] = from_f32<T>(acc.z);
+    dst[3] = from_f32<T>(acc.w);
+  }
+}
+
+// Attention mass: token j's softmax weights summed over the rows of its KV
+// head, from the rows' (max, 1 / sum) that the attention left behind.  A warp
+// owns a block of 16 tokens, keeps its widened key fragments in registers and
+// walks the rows' tiles; sums are fp32 in a fixed order.
+template <int HDP, int NP, typename T>
+__global__ void __launch_bounds__(RW * 32) cache_mass_kernel(CacheAttnArgs a) {
+  constexpr int KS = HDP / 16;
+  extern __shared__ __align__(16) uint8_t smem[];
+  uint32_t* frag = (uint32_t*)smem;   // [NP][KS][32][4]
+  __shared__ float fac[16];
+  const int b = blockIdx.z, h = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int g = lane >> 2, c = lane & 3;
+  const CacheLayer& L = a.c;
+  const size_t head = (size_t)b * L.Hkv + h;
+  Sight s;
+  robot_sight(a, b, s);
+  const int j0 = (blockIdx.x * RW + warp) * 16, jc0 = blockIdx.x * RW * 16, jc1 = jc0 + RW * 16;
+  float* mass = a.mass + head * a.mass_stride;
+  float acc[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
+  // (uniform in the CTA) queries that can see a token of the CTA's
+  int i0 = 0, i1 = jc0 < s.len ? s.count : 0;
+  if (a.causal) {
+    i0 = max(0, jc0 - s.p0);
+    if (a.window > 0 && jc0 >= a.sinks) i1 = min(i1, jc1 - 1 + a.window - s.p0);
+  }
+  if (i0 < i1) {
+    uint32_t kb[2][KS][2];
+    {
+      KeyRegs<HDP> kr;
+      kr.load(L.k + (head * L.T + min(j0, L.T - 16)) * HDP, g, c);
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+        for (int j = 0; j < HDP / 64; ++j) {
+          const uint32_t w[4] = {kr.w[hh][j].x, kr.w[hh][j].y, kr.w[hh][j].z, kr.w[hh][j].w};
+#pragma unroll
+          for (int s4 = 0; s4 < 4; ++s4) {
+            kb[hh][4 * j + s4][0] = e4m3_lo(w[s4]);
+            kb[hh][4 * j + s4][1] = e4m3_hi(w[s4]);
+          }
+        }
+    }
+    const float kf = exp2i(L.ke[head * (L.T / 16) + min(j0, L.T - 16) / 16]);
+    const float2* ml = a.row_ml + head * a.n * a.G;
+    for (int r0 = i0 * a.G / 16 * 16; r0 < i1 * a.G; r0 += 16) {
+      __syncthreads();
+      if (threadIdx.x < 16) fac[threadIdx.x] = 0.f;
+      __syncthreads();
+      stage_q<HDP, NP, T, RW * 32>(a, s, b, h, r0, frag, fac);
+      float sc[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const uint4 qa = *(const uint4*)(frag + ((p * KS + ks) * 32 + lane) * 4);
+#pragma unroll
+          for (int hh = 0; hh < 2; ++hh) mma_f16(sc[hh], qa, kb[hh][ks][0], kb[hh][ks][1]);
+        }
+#pragma unroll
+      for (int rr = 0; rr < 2; ++rr) {
+        const int r = r0 + g + 8 * rr;
+        const RowMask mk = row_mask(a, s, r);
+        const float2 x = r < a.n * a.G ? ml[r] : make_float2(0.f, 0.f);
+        const float f = fac[g + 8 * rr] * kf;
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+          for (int q = 0; q < 2; ++q)
+            if (mk.sees(j0 + 8 * hh + 2 * c + q))
+              acc[hh][q] += exp2f(fmaf(sc[hh][2 * rr + q], f, kPExp - x.x)) * x.y;
+      }
+    }
+  }
+#pragma unroll
+  for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      float v = acc[hh][q];
+      v += __shfl_xor_sync(0xffffffffu, v, 4);
+      v += __shfl_xor_sync(0xffffffffu, v, 8);
+      v += __shfl_xor_sync(0xffffffffu, v, 16);
+      const int j = j0 + 8 * hh + 2 * c + q;
+      if (g == 0 && j < a.max_length) {
+        if (!a.mass_add) mass[j] = v;
+        else if (j < s.len) mass[j] += v;
+      }
+    }
+}
+
+template <int HDP, int NP>
+constexpr int frag_bytes() { return NP * (HDP / 16) * 512; }
+
+template <int HDP, int NP>
+constexpr int rows_smem() { return frag_bytes<HDP, NP>() + RW * 16 * HDP * 4; }
+
+template <int HDP, int NP, typename T>
+cudaError_t launch_rows(CacheAttnArgs a, cudaStream_t st) {
+  constexpr int U = HDP == 64 ? 64 : (HDP == 128 ? 32 : 16);
+  a.row_tiles = (a.n * a.G + 15) / 16;
+  const long long tiles = (long long)a.row_tiles * a.c.Hkv * a.batch;
+  // tokens that a row tile sees at most, in units
+  long long seen = a.max_length;
+  if (a.window > 0) seen = min(seen, (long long)a.window + a.sinks + 15 / a.G + 1 + 2 * U);
+  const int units = (int)((seen + U - 1) / U);
+  a.splits = 1;
+  if (tiles < 2 * a.num_sms) {
+    // two CTAs per SM, each warp with a unit at least
+    // (and no more splits than the joining CTA has weights for in shared memory)
+    const long long most = min(min((long long)kCacheSplitCtas, 2ll * a.num_sms) / tiles, (long long)RW * HDP);
+    a.splits = (int)max(1ll, min(most, (long long)(units + RW - 1) / RW));
+  }
+  cache_rows_kernel<HDP, NP, T><<<dim3(a.row_tiles * a.splits, a.c.Hkv, a.batch), RW * 32, rows_smem<HDP, NP>(), st>>>(a);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess || !a.mass || a.max_length == 0) return e;
+  cache_mass_kernel<HDP, NP, T>
+      <<<dim3((a.max_length + RW * 16 - 1) / (RW * 16), a.c.Hkv, a.batch), RW * 32, frag_bytes<HDP, NP>(), st>>>(a);
+  return cudaGetLastError();
+}
+
+template <int HDP>
+cudaError_t launch_hd(const CacheAttnArgs& a, Dtype dt, cudaStream_t st) {
+  return dt == DT_BF16 ? launch_rows<HDP, 1, bf16>(a, st) : launch_rows<HDP, 2, float>(a, st);
+}
+
+template <int HDP>
+cudaError_t init_hd() {
+  cudaError_t e = cudaFuncSetAttribute(cache_rows_kernel<HDP, 1, bf16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       rows_smem<HDP, 1>());
+  if (e != cudaSuccess) return e;
+  return cudaFuncSetAttribute(cache_rows_kernel<HDP, 2, float>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              rows_smem<HDP, 2>());
+}
+
+}  // namespace
+
+cudaError_t launch_cache_attend(const CacheAttnArgs& a, Dtype dt, cudaStream_t st) {
+  switch (a.c.hdp) {
+    case 64: return launch_hd<64>(a, dt, st);
+    case 128: return launch_hd<128>(a, dt, st);
+    case 192: return launch_hd<192>(a, dt, st);
+    default: return launch_hd<256>(a, dt, st);
+  }
+}
+
+cudaError_t init_cache_kernels() {
+  cudaError_t e = init_hd<64>();
+  if (e == cudaSuccess) e = init_hd<128>();
+  if (e == cudaSuccess) e = init_hd<192>();
+  if (e == cudaSuccess) e = init_hd<256>();
+  return e;
+}
+
+}  // namespace ravel

@@ -1,0 +1,327 @@
+// Storing into the 8-bit context cache, reading it back and eviction by
+// attention mass.
+#include "cache.cuh"
+
+namespace ravel {
+namespace {
+
+// One block of 16 tokens of one robot and KV head, keys and values: thread t
+// holds 16 values of each of token t / (hdp / 16) of the block.  `fresh` tokens
+// bring new values in kx / vx; `stay` tokens are in the cache already, under
+// the exponents ke_old / ve_old, and are rounded again where those rise.
+struct BlockShared {
+  int bad[kCacheBlock];      // the token has a value that is not finite
+  uint32_t kmax, vmax;       // bits of the largest finite magnitudes
+};
+
+__device__ __forceinline__ bool finite_f(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
+
+__device__ __forceinline__ void store_block(BlockShared& s, float* kx, float* vx, bool fresh, bool stay,
+                                            bool has_old, int token, const CacheLayer& c, size_t row, size_t block,
+                                            int d) {
+  if (threadIdx.x < kCacheBlock) s.bad[threadIdx.x] = 0;
+  if (threadIdx.x == kCacheBlock) s.kmax = s.vmax = 0u;
+  const int ke_old = has_old ? c.ke[block] : kCacheExpMin, ve_old = has_old ? c.ve[block] : kCacheExpMin;
+  __syncthreads();
+  float km = 0.f, vm = 0.f;
+  if (fresh) {
+    bool ok = true;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      ok = ok && finite_f(kx[i]) && finite_f(vx[i]);
+      km = fmaxf(km, fabsf(kx[i]));
+      vm = fmaxf(vm, fabsf(vx[i]));
+    }
+    if (!ok) s.bad[token] = 1;
+  }
+  __syncthreads();
+  const bool bad = s.bad[token] != 0;
+  uint32_t kb = __float_as_uint(fresh && !bad ? km : 0.f), vb = __float_as_uint(fresh && !bad ? vm : 0.f);
+  kb = __reduce_max_sync(0xffffffffu, kb);
+  vb = __reduce_max_sync(0xffffffffu, vb);
+  if ((threadIdx.x & 31) == 0) {
+    atomicMax(&s.kmax, kb);
+    atomicMax(&s.vmax, vb);
+  }
+  __syncthreads();
+  const int ke = max(block_exponent(s.kmax), ke_old), ve = max(block_exponent(s.vmax), ve_old);
+  uint4 *kd = (uint4*)(c.k + row + d), *vd = (uint4*)(c.v + row + d);
+  if (fresh) {
+    const uint32_t nan4 = 0x7f7f7f7fu;
+    *kd = bad ? make_uint4(nan4, nan4, nan4, nan4) : f32_to_e4m3x16(kx, exp2i(-ke));
+    *vd = bad ? make_uint4(0u, 0u, 0u, 0u) : f32_to_e4m3x16(vx, exp2i(-ve));
+  } else if (stay) {
+    float x[16];
+    if (ke != ke_old) {
+      e4m3x16_to_f32(*kd, exp2i(max(ke_old - ke, -126)), x);   // (below 2^-126 all round to zero anyway)
+      *kd = f32_to_e4m3x16(x, 1.f);
+    }
+    if (ve != ve_old) {
+      e4m3x16_to_f32(*vd, exp2i(max(ve_old - ve, -126)), x);
+      *vd = f32_to_e4m3x16(x, 1.f);
+    }
+  }
+  if (threadIdx.x == 0) {
+    c.ke[block] = (int8_t)ke;
+    c.ve[block] = (int8_t)ve;
+  }
+}
+
+// Bandwidth-bound for prompts, a launch's latency for single tokens.  A CTA per
+// block: its exponent needs the whole block's maximum before the first value
+// is rounded, and 16 tokens x 16 values per thread hold it in registers, so
+// the inputs are read once.
+template <typename T>
+__global__ void __launch_bounds__(256) cache_append_kernel(AppendArgs a) {
+  __shared__ BlockShared s;
+  const CacheLayer& c = a.c;
+  const int b = blockIdx.z, h = blockIdx.y;
+  const int start = a.starts ? a.starts[b] : 0, count = a.counts ? a.counts[b] : a.n;
+  if (start < 0 || count < 0 || count > a.n || start > a.max_tokens - count) {
+    if (threadIdx.x == 0 && blockIdx.x == 0 && h == 0) raise_error(a.err, ERR_SHAPE);
+    return;
+  }
+  const int blk = start / kCacheBlock + blockIdx.x, end = start + count;
+  if (count == 0 || blk * kCacheBlock >= end) return;
+  const int tpt = c.hdp / 16;   // threads per token
+  const int token = threadIdx.x / tpt, d = (threadIdx.x % tpt) * 16;
+  const int pos = blk * kCacheBlock + token;
+  const bool fresh = pos >= start && pos < end, stay = pos < start;
+  float kx[16], vx[16];
+  if (fresh) {
+    const size_t at = (size_t)((long long)b * a.robot + (long long)(pos - start) * a.token) + (size_t)h * c.hd;
+    load16((const T*)a.k + at, d, c.hd, a.vec, kx);
+    load16((const T*)a.v + at, d, c.hd, a.vec, vx);
+  }
+  const size_t head = (size_t)b * c.Hkv + h;
+  store_block(s, kx, vx, fresh, stay, blk * kCacheBlock < start, token, c, (head * c.T + pos) * c.hdp,
+              head * (c.T / kCacheBlock) + blk, d);
+}
+
+template <typename T>
+__device__ __forceinline__ void store16(T* row, int d, int hd, int vec, const float* x) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int d8 = d + 8 * h;
+    if (d8 >= hd) break;
+    T y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = from_f32<T>(x[8 * h + i]);
+    if (vec) {
+      constexpr int NV = 8 * sizeof(T) / 16;
+      uint4 w[NV];
+      memcpy(w, y, sizeof y);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) *((uint4*)(row + d8) + i) = w[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) row[d8 + i] = y[i];
+    }
+  }
+}
+
+// Bandwidth-bound: a thread takes 16 values of a token's key row and of its value row.
+template <typename T>
+__global__ void __launch_bounds__(256) cache_read_kernel(ReadArgs a) {
+  const CacheLayer& c = a.c;
+  const int b = blockIdx.z, h = blockIdx.y;
+  const int tpt = c.hdp / 16;
+  const long long idx = (long long)blockIdx.x * 256 + threadIdx.x;
+  const int i = (int)(idx / tpt), d = (int)(idx % tpt) * 16;
+  if (i >= a.n || d >= c.hd) return;
+  const int first = a.firsts ? a.firsts[b] : 0;
+  const int length = a.lengths ? a.lengths[b] : a.max_tokens;
+  const bool bad = first < 0 || length < 0 || length > a.max_tokens;
+  if (bad && idx == 0 && h == 0) raise_error(a.err, ERR_SHAPE);
+  const size_t head = (size_t)b * c.Hkv + h;
+  float k[16], v[16];
+  if (!bad && i < length - first) {
+    const int pos = first + i;
+    const size_t row = (head * c.T + pos) * c.hdp + d, block = head * (c.T / kCacheBlock) + pos / kCacheBlock;
+    const uint4 kw = *(const uint4*)(c.k + row), vw = *(const uint4*)(c.v + row);
+    e4m3x16_to_f32(kw, exp2i(c.ke[block]), k);
+    e4m3x16_to_f32(vw, exp2i(c.ve[block]), v);
+  } else {
+#pragma unroll
+    for (int q = 0; q < 16; ++q) k[q] = v[q] = 0.f;
+  }
+  const size_t out = (head * a.n + i) * c.hd;
+  store16((T*)a.k + out, d, c.hd, a.vec, k);
+  store16((T*)a.v + out, d, c.hd, a.vec, v);
+}
+
+// ---- eviction ---------------------------------------------------------------
+
+constexpr int kSelThreads = 1024;
+
+// Order of masses as unsigned integers: ascending, -0 = +0, NaN above all.
+__device__ __forceinline__ uint32_t mass_key(float x) {
+  const uint32_t u = __float_as_uint(x + 0.f);
+  if ((u & 0x7fffffffu) > 0x7f800000u) return 0xffffffffu;
+  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+
+// The tokens that one (robot, KV head) keeps: the key of the last one in by a
+// radix selection over the middle's masses (four histograms of 8 bits), then
+// one ordered pass that gives each kept token its place.  Ties go to the
+// earlier tokens.  No order of arrival enters the result: the histograms count.
+__global__ void __launch_bounds__(kSelThreads) cache_select_kernel(EvictArgs a) {
+  __shared__ unsigned hist[256];
+  __shared__ uint32_t sel_bin, sel_left;
+  __shared__ unsigned totals[2][32];
+  const int h = blockIdx.x, b = blockIdx.y, Hkv = a.from.Hkv;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  int len = a.lengths[b];
+  if (len < 0 || len > a.max_tokens || len > a.mass_stride) {
+    if (tid == 0 && h == 0) raise_error(a.err, ERR_SHAPE);
+    len = 0;
+  }
+  const int kept = min(len, a.keep);
+  const size_t head = (size_t)b * Hkv + h;
+  const float* mass = a.mass + head * a.mass_stride;
+  int* index = a.index + head * a.keep;
+  float* nm = a.new_mass ? a.new_mass + head * a.keep : nullptr;
+  if (tid == 0 && h == 0) a.new_lengths[b] = kept;
+  for (int i = kept + tid; i < a.keep; i += kSelThreads) {
+    index[i] = -1;
+    if (nm) nm[i] = 0.f;
+  }
+  if (len <= a.keep) {
+    for (int i = tid; i < kept; i += kSelThreads) {
+      index[i] = i;
+      if (nm) nm[i] = mass[i];
+    }
+    return;
+  }
+  const int lo = a.sinks, hi = len - a.recent;   // the middle, longer than what stays of it
+  uint32_t left = (uint32_t)(a.keep - a.sinks - a.recent);
+  uint32_t prefix = 0xffffffffu;   // (nothing of the middle stays: no key is above, no tie taken)
+  if (left > 0) {
+    prefix = 0u;
+    uint32_t mask = 0u;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+      if (tid < 256) hist[tid] = 0u;
+      __syncthreads();
+      for (int j = lo + tid; j < hi; j += kSelThreads) {
+        const uint32_t key = mass_key(mass[j]);
+        if ((key & mask) == prefix) atomicAdd(&hist[(key >> shift) & 255u], 1u);
+      }
+      __syncthreads();
+      if (warp == 0) {
+        // lane i holds bins 255 - 8i .. 248 - 8i, from the heaviest down
+        unsigned n[8], sum = 0;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          n[q] = hist[255 - 8 * lane - q];
+          sum += n[q];
+        }
+        unsigned before = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const unsigned up = __shfl_up_sync(0xffffffffu, before, o);
+          if (lane >= o) before += up;
+        }
+        before -= sum;   // tokens in heavier lanes' bins
+        if (before < left && before + sum >= left) {
+          bool found = false;
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            if (!found && before + n[q] >= left) {
+              sel_bin = (uint32_t)(255 - 8 * lane - q);
+              sel_left = left - before;
+              found = true;
+            }
+            before += n[q];
+          }
+        }
+      }
+      __syncthreads();
+      prefix |= sel_bin << shift;
+      mask |= 255u << shift;
+      left = sel_left;
+    }
+  }
+  // kept before j: those surely in (heavier, first, last) and as many ties as still fit
+  unsigned sure = 0, ties = 0;
+  int buf = 0;
+  for (int base = 0; base < len; base += kSelThreads, buf ^= 1) {
+    const int j = base + tid;
+    const float m = j < len ? mass[j] : 0.f;
+    const uint32_t key = mass_key(m);
+    const bool always = j < len && (j < lo || j >= hi), mid = j >= lo && j < hi;
+    const bool in = always || (mid && key > prefix), tie = mid && key == prefix;
+    const unsigned bi = __ballot_sync(0xffffffffu, in), bt = __ballot_sync(0xffffffffu, tie);
+    if (lane == 0) totals[buf][warp] = __popc(bi) | __popc(bt) << 16;
+    __syncthreads();
+    const unsigned own = totals[buf][lane];
+    unsigned pre = own;   // both counts in one word: at most 1024 each
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const unsigned up = __shfl_up_sync(0xffffffffu, pre, o);
+      if (lane >= o) pre += up;
+    }
+    const unsigned all = __shfl_sync(0xffffffffu, pre, 31);
+    const unsigned warps = __shfl_sync(0xffffffffu, pre - own, warp);
+    const unsigned below = (1u << lane) - 1u;
+    const unsigned s0 = sure + (warps & 0xffffu) + __popc(bi & below), t0 = ties + (warps >> 16) + __popc(bt & below);
+    if (in || (tie && t0 < left)) {
+      const unsigned at = s0 + min(t0, left);
+      index[at] = j;
+      if (nm) nm[at] = m;
+    }
+    sure += all & 0xffffu;
+    ties += all >> 16;
+  }
+}
+
+// The kept rows into the other cache: a CTA per block of 16, as in append.
+__global__ void __launch_bounds__(256) cache_move_kernel(EvictArgs a) {
+  __shared__ BlockShared s;
+  const CacheLayer &from = a.from, &to = a.to;
+  const int b = blockIdx.z, h = blockIdx.y;
+  const int kept = a.new_lengths[b];
+  if ((int)blockIdx.x * kCacheBlock >= kept) return;
+  const int tpt = to.hdp / 16;
+  const int token = threadIdx.x / tpt, d = (threadIdx.x % tpt) * 16;
+  const int pos = blockIdx.x * kCacheBlock + token;
+  const size_t head = (size_t)b * to.Hkv + h;
+  float kx[16], vx[16];
+  const bool fresh = pos < kept;
+  if (fresh) {
+    const int j = a.index[head * a.keep + pos];
+    const size_t row = (head * from.T + j) * from.hdp + d, block = head * (from.T / kCacheBlock) + j / kCacheBlock;
+    const uint4 kw = *(const uint4*)(from.k + row), vw = *(const uint4*)(from.v + row);
+    e4m3x16_to_f32(kw, exp2i(from.ke[block]), kx);
+    e4m3x16_to_f32(vw, exp2i(from.ve[block]), vx);
+  }
+  store_block(s, kx, vx, fresh, false, false, token, to, (head * to.T + pos) * to.hdp,
+              head * (to.T / kCacheBlock) + blockIdx.x, d);
+}
+
+}  // namespace
+
+cudaError_t launch_cache_append(const AppendArgs& a, Dtype dt, cudaStream_t st) {
+  // a start inside a block needs one block more
+  const dim3 grid((a.n + 2 * kCacheBlock - 2) / kCacheBlock, a.c.Hkv, a.batch);
+  if (dt == DT_BF16) cache_append_kernel<bf16><<<grid, a.c.hdp, 0, st>>>(a);
+  else cache_append_kernel<float><<<grid, a.c.hdp, 0, st>>>(a);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_cache_read(const ReadArgs& a, Dtype dt, cudaStream_t st) {
+  const dim3 grid((unsigned)(((long long)a.n * (a.c.hdp / 16) + 255) / 256), a.c.Hkv, a.batch);
+  if (dt == DT_BF16) cache_read_kernel<bf16><<<grid, 256, 0, st>>>(a);
+  else cache_read_kernel<float><<<grid, 256, 0, st>>>(a);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_cache_evict(const EvictArgs& a, cudaStream_t st) {
+  cache_select_kernel<<<dim3(a.from.Hkv, a.batch), kSelThreads, 0, st>>>(a);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  const dim3 grid((a.keep + kCacheBlock - 1) / kCacheBlock, a.to.Hkv, a.batch);
+  cache_move_kernel<<<grid, a.to.hdp, 0, st>>>(a);
+  return cudaGetLastError();
+}
+
+}  // namespace ravel

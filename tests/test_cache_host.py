@@ -1,0 +1,83 @@
+"""The 8-bit context cache without a GPU: the fp64 reference against torch's
+e4m3, its invariants, and what the library refuses before touching a device."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+from oracle import cache as ref
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2609_34170_gb300 import build, load
+    build.build()
+    return load()
+
+
+def test_reference_rounds_as_e4m3():
+    codes = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).double().numpy()
+    codes = codes[np.isfinite(codes)]
+    np.testing.assert_array_equal(ref.e4m3(codes), codes)
+    x = np.random.default_rng(0).uniform(-448, 448, 20000) * 2.0 ** np.random.default_rng(1).integers(-18, 1, 20000)
+    x = np.concatenate([x.astype(np.float32), (codes[:-1] + codes[1:]) / 2]).astype(np.float32)   # and ties
+    np.testing.assert_array_equal(ref.e4m3(x), torch.from_numpy(x).to(torch.float8_e4m3fn).double().numpy())
+
+
+def test_reference_exponent_is_the_smallest_that_fits():
+    for top in [448.0, np.nextafter(448.0, 500), 1.75, 1.7500001, 1e-30, 3e38, 2.0 ** -92 * 1.75]:
+        e = ref.exponent(top)
+        assert top <= 448 * 2.0 ** e and (e == ref.E_MIN or top > 448 * 2.0 ** (e - 1))
+    assert ref.exponent(0.0) == ref.exponent(1e-40) == ref.E_MIN
+
+
+def test_reference_append_in_pieces_holds_the_same_where_exponents_rise():
+    """Values stored token by token differ from those stored at once by no more
+    than a second rounding: half a step of the final grid's smallest."""
+    rng = np.random.default_rng(2)
+    k = rng.standard_normal((1, 16, 1, 8)) * 2.0 ** np.arange(16)[None, :, None, None]
+    one, many = ref.Held(1, 1, 16, 8), ref.Held(1, 1, 16, 8)
+    one.append(k, k, [0], [16])
+    for i in range(16):
+        many.append(k[:, i:i + 1], k[:, i:i + 1], [i], [1])
+    assert one.ke[0, 0, 0] == many.ke[0, 0, 0]
+    step = 2.0 ** (one.ke[0, 0, 0] - 9)
+    rel = np.abs(one.k - k.transpose(0, 2, 1, 3)).max()
+    assert np.abs(one.k - many.k).max() <= np.maximum(step, rel)
+
+
+def test_create_refuses_bad_shapes_without_a_gpu(lib):
+    from paper_2609_34170_gb300 import RavelError, ravel_cache_create
+    good = dict(layers=1, n_q_heads=4, n_kv_heads=2, head_dim=64, max_tokens=32, max_batch=1, max_queries=1)
+    for bad in (dict(layers=0), dict(n_q_heads=3), dict(head_dim=12), dict(head_dim=264), dict(max_tokens=0),
+                dict(max_batch=0), dict(max_queries=0), dict(dtype=2), dict(max_batch=65536), dict(n_kv_heads=0),
+                dict(max_tokens=(1 << 30) + 1), dict(max_queries=1 << 30)):
+        with pytest.raises(RavelError) as ei:
+            ravel_cache_create(**{**good, **bad})
+        assert ei.value.status == 2
+    with pytest.raises(ValueError):
+        from paper_2609_34170_gb300 import ContextCache
+        ContextCache(layers=1, n_q_heads=1, n_kv_heads=1, head_dim=64, max_tokens=16, dtype="fp16")
+
+
+def test_null_arguments_are_refused(lib):
+    assert lib.ravel_cache_create(None, 0, None) == 1
+    assert lib.ravel_cache_append(None, 0, 1, 1, None, None, 0, 0, None, None, None) == 1
+    assert lib.ravel_cache_attend(None, 0, 1, 1, None, 0, 0, None, 0, 0, None, None, 0, 1, 0, 0, 0.0, None, 0, 0, None) == 1
+    assert lib.ravel_cache_evict(None, 0, None, 0, 1, None, None, 0, 1, 0, 0, None, None, None, None) == 1
+    assert lib.ravel_cache_read(None, 0, 1, 1, None, None, None, None, None) == 1
+    assert lib.ravel_cache_reset(None) == 1
+    assert lib.ravel_cache_last_error(None) == b""
+    lib.ravel_cache_destroy(None)
+
+
+def test_binding_refuses_tensors_of_the_wrong_kind(lib):
+    from paper_2609_34170_gb300 import ravel_cache_append, ravel_cache_attend
+    handle = C.c_void_p()
+    k = torch.zeros((1, 2, 1, 64), dtype=torch.bfloat16)
+    with pytest.raises(ValueError):   # not on a GPU
+        ravel_cache_append(handle, 0, k, k)
+    with pytest.raises(ValueError):
+        ravel_cache_attend(handle, 0, k, k, None, None, 2)
