@@ -69,16 +69,19 @@ struct CacheAttnArgs {
   int vec;                  // q rows are 16-byte aligned
   int num_sms;
   // workspace
-  float* part;              // [units * splits][16][hdp] normalised partial outputs
-  float2* part_ml;          // [units * splits][16] (max, sum)
+  float* part;              // [units * splits][rows of a tile x hdp] normalised partial outputs
+  float2* part_ml;          // [units * splits][rows of a tile] (max, sum)
   unsigned* arrived;        // [units] splits that have finished (zero between launches)
-  float2* row_ml;           // [B][Hkv][n * G] (max, 1 / sum), written where mass is wanted
+  float2* row_ml;           // [B][Hkv][n * G] see row_weight, written where mass is wanted
   int* err;
   // chosen by the launcher
   int row_tiles, splits;
 };
-constexpr int kCacheSplitCtas = 608;   // row tiles x splits of a launch that splits the tokens
+constexpr int kCacheSplitCtas = 608;   // row tiles (of 16) x splits of a launch that splits the tokens
+constexpr int kCacheTcRows = 128;      // rows of a tile on the tensor cores: at most one such tile x split per SM
 cudaError_t launch_cache_attend(const CacheAttnArgs& a, Dtype dt, cudaStream_t st);
+cudaError_t launch_cache_attend_tc(const CacheAttnArgs& a, cudaStream_t st);   // bf16; not the mass
 cudaError_t init_cache_kernels();
+cudaError_t init_cache_tc_kernels();
 
 }  // namespace ravel

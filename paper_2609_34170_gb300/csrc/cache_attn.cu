@@ -21,13 +21,14 @@
 // below the row's largest is dropped), in two f16 pieces for fp32 ones (23
 // bits).  Products with the codes are exact in the tensor core's fp32 sums;
 // block exponents and row scales are applied to the sums in fp32.  P is scaled
-// to a maximum of 2^15 and multiplied by 2^(ve - E), E the largest value
-// exponent of the blocks that the row sees: one f16 piece (11 bits) for bf16
-// results, two for fp32 ones; what lies 2^39 below the largest is dropped.
-// Maxima, sums and outputs are fp32.
-#include "cache.cuh"
-#include "launch.h"
-#include "tc_common.cuh"
+// times 2^ve of its block, relative to the largest such product of the row,
+// scaled to at most 2^15: one f16 piece (11 bits) for bf16 results, two for fp32
+// ones; what contributes less than 2^-39 of the largest is dropped.  The sum of P
+// itself takes 2^ve out again, per block.  Both references (the row's largest
+// score, and its largest score + ve) are rounded up to integers in the log2
+// domain, so that every change of reference is an exact power of two.  Maxima,
+// sums and outputs are fp32.
+#include "cache_attn.cuh"
 
 namespace ravel {
 namespace {
@@ -41,58 +42,6 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint4& a, uint32_t 
       "%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
-}
-
-__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-
-// What a tile of rows sees: tokens [0, sink) and [from, to) in units, and the
-// numbers that decide single tokens.
-struct Sight {
-  int len, count;     // the robot's tokens and queries
-  int p0;             // position of query 0 (len - count)
-  int sink_units, from, units;   // unit t is t < sink_units ? t : t - sink_units + from
-};
-
-struct RowMask {
-  int hi, lo, sinks;   // sees j < hi and (j >= lo or j < sinks)
-  __device__ __forceinline__ bool sees(int j) const { return j < hi && (j >= lo || j < sinks); }
-};
-
-__device__ __forceinline__ RowMask row_mask(const CacheAttnArgs& a, const Sight& s, int r) {
-  RowMask m;
-  const int i = r / a.G;
-  m.sinks = a.sinks;
-  m.lo = 0;
-  if (i >= s.count) m.hi = 0;
-  else if (!a.causal) m.hi = s.len;
-  else {
-    m.hi = s.p0 + i + 1;
-    if (a.window > 0) m.lo = max(0, m.hi - a.window);
-  }
-  return m;
-}
-
-// The robot's length and count, checked; a robot out of range sees nothing.
-__device__ __forceinline__ bool robot_sight(const CacheAttnArgs& a, int b, Sight& s) {
-  s.len = a.lengths[b];
-  s.count = a.counts ? a.counts[b] : a.n;
-  const bool ok = s.len >= 0 && s.len <= a.max_length && s.count >= 0 && s.count <= a.n &&
-                  (!a.causal || s.count <= s.len);
-  if (!ok) s.len = s.count = 0;
-  s.p0 = s.len - s.count;
-  return ok;
-}
-
-// Units of `U` tokens that rows r0 .. r1 (r0 < count * G) see between them.
-__device__ __forceinline__ void tile_sight(const CacheAttnArgs& a, Sight& s, int r0, int r1, int U) {
-  const RowMask first = row_mask(a, s, r0), last = row_mask(a, s, min(r1, s.count * a.G - 1));
-  s.from = first.lo / U;
-  s.sink_units = a.window > 0 ? min((a.sinks + U - 1) / U, s.from) : 0;
-  s.units = s.sink_units + (last.hi + U - 1) / U - s.from;
 }
 
 // Query rows r0 .. r0 + 15 into shared memory as the A fragments of the MMAs:
@@ -256,8 +205,7 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(CacheAttnArgs a)
   for (int t = 0; t < HDP / 8; ++t)
 #pragma unroll
     for (int q = 0; q < 4; ++q) o[t][q] = 0.f;
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-  int E[2] = {-127, -127};
+  float m[2] = {-INFINITY, -INFINITY}, W[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 
   KeyRegs<HDP> kr[NT];
   ValueRegs<HDP> vr[NT];
@@ -312,10 +260,8 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(CacheAttnArgs a)
     }
     // scores in the log2 domain; hidden ones -inf
     const bool full = j0 + U <= full_hi && (j0 >= full_lo || j0 + U <= a.sinks);
-    bool seen[NT][2];   // the row sees something of the block
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      seen[t][0] = seen[t][1] = full;
 #pragma unroll
       for (int hh = 0; hh < 2; ++hh)
 #pragma unroll
@@ -323,71 +269,68 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(CacheAttnArgs a)
       if (!full) {
         const int jb = j0 + 16 * t;
 #pragma unroll
-        for (int rr = 0; rr < 2; ++rr)
-          seen[t][rr] = jb < mk[rr].hi && (jb + 16 > mk[rr].lo || jb < mk[rr].sinks);
-#pragma unroll
         for (int hh = 0; hh < 2; ++hh)
 #pragma unroll
           for (int q = 0; q < 4; ++q)
             if (!mk[q >> 1].sees(jb + 8 * hh + 2 * c + (q & 1))) sc[t][hh][q] = -INFINITY;
       }
     }
-    float alpha[2], mu[2];
-    int En[2];
+    float mu[2], wu[2];   // the references, 0 while the row has seen nothing
+    bool same = true;
+    float fl[2], fo[2];
 #pragma unroll
     for (int rr = 0; rr < 2; ++rr) {
-      float mx = -INFINITY;
-      En[rr] = E[rr];
+      float mx = -INFINITY, wx = -INFINITY;
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-#pragma unroll
-        for (int hh = 0; hh < 2; ++hh) mx = fmaxf(mx, fmaxf(sc[t][hh][2 * rr], sc[t][hh][2 * rr + 1]));
-        if (seen[t][rr]) En[rr] = max(En[rr], ve[t]);
+        const float x = fmaxf(fmaxf(sc[t][0][2 * rr], sc[t][0][2 * rr + 1]), fmaxf(sc[t][1][2 * rr], sc[t][1][2 * rr + 1]));
+        mx = fmaxf(mx, x);
+        wx = fmaxf(wx, x + (float)ve[t]);
       }
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-      const float mn = fmaxf(m[rr], mx);
+#pragma unroll
+      for (int o2 = 1; o2 <= 2; o2 <<= 1) {
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o2));
+        wx = fmaxf(wx, __shfl_xor_sync(0xffffffffu, wx, o2));
+      }
+      const float mn = fmaxf(m[rr], ceilf(mx)), wn = fmaxf(W[rr], ceilf(wx));
       mu[rr] = mn == -INFINITY ? 0.f : mn;
-      alpha[rr] = m[rr] == -INFINITY ? 0.f : exp2f(m[rr] - mu[rr]);
+      wu[rr] = wn == -INFINITY ? 0.f : wn;
+      same = same && mn == m[rr] && wn == W[rr];
+      fl[rr] = pow2f_down(m[rr] - mu[rr]);
+      fo[rr] = pow2f_down(W[rr] - wu[rr]);
       m[rr] = mn;
+      W[rr] = wn;
     }
-    // (a factor is 1 in most units: the maximum settles early)
-    if (__any_sync(0xffffffffu, alpha[0] != 1.f || alpha[1] != 1.f || En[0] != E[0] || En[1] != E[1])) {
-      const float f0 = alpha[0] * exp2i(max(E[0] - En[0], -126)), f1 = alpha[1] * exp2i(max(E[1] - En[1], -126));
-      l[0] *= alpha[0];
-      l[1] *= alpha[1];
+    // (most units change nothing: the maxima settle early)
+    if (__any_sync(0xffffffffu, !same)) {
+      l[0] *= fl[0];
+      l[1] *= fl[1];
 #pragma unroll
       for (int t = 0; t < HDP / 8; ++t) {
-        o[t][0] *= f0;
-        o[t][1] *= f0;
-        o[t][2] *= f1;
-        o[t][3] *= f1;
+        o[t][0] *= fo[0];
+        o[t][1] *= fo[0];
+        o[t][2] *= fo[1];
+        o[t][3] *= fo[1];
       }
-      E[0] = En[0];
-      E[1] = En[1];
     }
-    const float nb[2] = {kPExp - mu[0], kPExp - mu[1]};
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       uint4 pa[NP];
       {
         float p[2][4];
 #pragma unroll
-        for (int hh = 0; hh < 2; ++hh)
+        for (int rr = 0; rr < 2; ++rr) {
+          const float vf = fmaxf((float)ve[t], wu[rr] - mu[rr] - kVeBelow);
+          const float nb = kPExp + vf - wu[rr];
+          float sum = 0.f;
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            p[hh][q] = NP == 2 ? exp2f(sc[t][hh][q] + nb[q >> 1]) : fast_exp2(sc[t][hh][q] + nb[q >> 1]);
-            l[q >> 1] += p[hh][q];
-          }
-        const float f0 = exp2i(max(ve[t] - E[0], -126)), f1 = exp2i(max(ve[t] - E[1], -126));
-        // (a block that the row does not see may have a larger exponent than E: its p are 0)
-        const float g0 = seen[t][0] ? f0 : 0.f, g1 = seen[t][1] ? f1 : 0.f;
+          for (int hh = 0; hh < 2; ++hh)
 #pragma unroll
-        for (int hh = 0; hh < 2; ++hh) {
-          p[hh][0] *= g0;
-          p[hh][1] *= g0;
-          p[hh][2] *= g1;
-          p[hh][3] *= g1;
+            for (int q = 2 * rr; q < 2 * rr + 2; ++q) {
+              p[hh][q] = NP == 2 ? exp2f(sc[t][hh][q] + nb) : fast_exp2(sc[t][hh][q] + nb);
+              sum += p[hh][q];
+            }
+          l[rr] = fmaf(sum, pow2f(wu[rr] - mu[rr] - vf), l[rr]);
         }
         pa[0] = make_uint4(pack_f16x2(p[0][0], p[0][1]), pack_f16x2(p[0][2], p[0][3]), pack_f16x2(p[1][0], p[1][1]),
                            pack_f16x2(p[1][2], p[1][3]));
@@ -431,7 +374,7 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(CacheAttnArgs a)
     }
     const bool has = !(l[rr] <= 0.f);   // (a sum that is not a number stays one)
     const float f = has ? 1.f / l[rr] : 0.f;
-    const float e2 = exp2i(max(E[rr], -126));
+    const float e2 = real ? pow2f(W[rr] - m[rr]) : 0.f;
     const int row = g + 8 * rr;
     if (c == 0) warp_ml[warp][row] = make_float2(m[rr], l[rr]);
     float* dst = joint + ((size_t)warp * 16 + row) * HDP;
@@ -481,7 +424,7 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(CacheAttnArgs a)
     }
     if (a.mass && threadIdx.x < rows) {
       const float2 x = split_w[threadIdx.x];
-      a.row_ml[head * a.n * a.G + r0 + threadIdx.x] = make_float2(x.x == -INFINITY ? 0.f : x.x, !(x.y <= 0.f) ? 1.f / x.y : 0.f);
+      a.row_ml[head * a.n * a.G + r0 + threadIdx.x] = row_weight(x.x, x.y, kPExp);
     }
     return;
   }
@@ -510,7 +453,7 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(CacheAttnArgs a)
     }
     const float inv = !(S <= 0.f) ? 1.f / S : 0.f;
     for (int q = 0; q < a.splits; ++q) wts[q * 16 + row] *= inv;
-    if (a.mass) a.row_ml[head * a.n * a.G + r0 + row] = make_float2(M == -INFINITY ? 0.f : M, inv);
+    if (a.mass) a.row_ml[head * a.n * a.G + r0 + row] = row_weight(M, S, kPExp);
   }
   __syncthreads();
   const float* p0 = a.part + unit * a.splits * 16 * HDP;
@@ -604,7 +547,7 @@ __global__ void __launch_bounds__(RW * 32) cache_mass_kernel(CacheAttnArgs a) {
 #pragma unroll
           for (int q = 0; q < 2; ++q)
             if (mk.sees(j0 + 8 * hh + 2 * c + q))
-              acc[hh][q] += exp2f(fmaf(sc[hh][2 * rr + q], f, kPExp - x.x)) * x.y;
+              acc[hh][q] += exp2f(fmaf(sc[hh][2 * rr + q], f, -x.x)) * x.y;
       }
     }
   }
@@ -646,8 +589,13 @@ cudaError_t launch_rows(CacheAttnArgs a, cudaStream_t st) {
     const long long most = min(min((long long)kCacheSplitCtas, 2ll * a.num_sms) / tiles, (long long)RW * HDP);
     a.splits = (int)max(1ll, min(most, (long long)(units + RW - 1) / RW));
   }
-  cache_rows_kernel<HDP, NP, T><<<dim3(a.row_tiles * a.splits, a.c.Hkv, a.batch), RW * 32, rows_smem<HDP, NP>(), st>>>(a);
-  cudaError_t e = cudaGetLastError();
+  cudaError_t e;
+  if (NP == 1 && a.n * a.G > 16) {
+    e = launch_cache_attend_tc(a, st);
+  } else {
+    cache_rows_kernel<HDP, NP, T><<<dim3(a.row_tiles * a.splits, a.c.Hkv, a.batch), RW * 32, rows_smem<HDP, NP>(), st>>>(a);
+    e = cudaGetLastError();
+  }
   if (e != cudaSuccess || !a.mass || a.max_length == 0) return e;
   cache_mass_kernel<HDP, NP, T>
       <<<dim3((a.max_length + RW * 16 - 1) / (RW * 16), a.c.Hkv, a.batch), RW * 32, frag_bytes<HDP, NP>(), st>>>(a);

@@ -2,6 +2,7 @@
 // implements the C ABI of ravel_cache.h.
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
 #include <new>
@@ -128,8 +129,10 @@ ravel_status ravel_cache_create(const ravel_cache_config* cfg, int device, ravel
   get(&c->v, c->rows * cfg->layers);
   get(&c->ke, c->blocks * cfg->layers);
   get(&c->ve, c->blocks * cfg->layers);
-  get(&c->part, sizeof(float) * kCacheSplitCtas * 16 * c->hdp);
-  get(&c->part_ml, sizeof(float2) * kCacheSplitCtas * 16);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&c->num_sms, cudaDevAttrMultiProcessorCount, device);
+  const size_t part_rows = std::max((size_t)kCacheSplitCtas * 16, (size_t)c->num_sms * kCacheTcRows);
+  get(&c->part, sizeof(float) * part_rows * c->hdp);
+  get(&c->part_ml, sizeof(float2) * part_rows);
   get(&c->arrived, sizeof(unsigned) * kCacheSplitCtas);
   get(&c->row_ml, sizeof(float2) * cfg->max_batch * (size_t)cfg->n_q_heads * cfg->max_queries);
   get(&c->err, sizeof(ErrorWord));
@@ -140,8 +143,8 @@ ravel_status ravel_cache_create(const ravel_cache_config* cfg, int device, ravel
     if (e == cudaSuccess) *c->err_host = 0;
     if (e == cudaSuccess) e = cudaHostGetDevicePointer((void**)&w.mirror, c->err_host, 0);
     if (e == cudaSuccess) e = cudaMemcpy(c->err, &w, sizeof w, cudaMemcpyHostToDevice);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&c->num_sms, cudaDevAttrMultiProcessorCount, device);
     if (e == cudaSuccess) e = init_cache_kernels();
+    if (e == cudaSuccess) e = init_cache_tc_kernels();
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
   }
   if (e != cudaSuccess) {
