@@ -6,8 +6,9 @@
 //   S = Q K^T        tcgen05.mma kind::f16, M = 128, N = 128, into TMEM
 //   P = 2^(S - m)    softmax warps: TMEM -> registers -> f16 P over S in TMEM
 //   O += P V         tcgen05.mma, M = 128, N = head dim, 16 tokens at a time
-// Warp roles (416 threads): warps 0-7 softmax and epilogue, two threads per row;
-// warps 8, 9 widen K, warps 10, 11 widen V; warp 12 TMEM and MMAs.
+// Warp roles (640 threads): warps 0-7 Q, softmax and epilogue, two threads per row;
+// warps 8-11 widen K, warps 12-15 widen V; warp 16 TMEM and MMAs (17-19 idle, so
+// that registers can be moved between whole warpgroups).
 //
 // The codes go from global memory through the widening warps' registers into
 // shared memory as f16 (e4m3 -> f16 is exact), in the 128-byte swizzled layout
@@ -26,16 +27,18 @@
 #include <algorithm>
 
 #include "cache_attn.cuh"
+#include "launch.h"
 
 namespace ravel {
 namespace {
 
-constexpr int TCT = 416;
+constexpr int TCT = 640;
 constexpr int BM = 128, BT = 128;              // rows, tokens of a tile
 constexpr uint32_t QB = BM * 128;              // bytes of a 64-dim block of Q
 constexpr uint32_t KU = BT * 128;              // bytes of a K unit: 128 tokens x 64 dims
 constexpr uint32_t VB = 64 * 128;              // bytes of a 64-dim block of a V half
 constexpr float kTcShift = 7.f;                // P's largest value is 2^kTcShift (times 2^8 while lazy)
+constexpr int kTcCluster = 8;                  // splits that are a cluster
 constexpr uint32_t kPolls = 1u << 25;          // polls without progress: seconds
 
 template <int NB> struct TcShape {
@@ -61,6 +64,27 @@ __device__ __forceinline__ void widen(uint4 w, uint32_t lo, uint32_t hi) {
   sts_u4(hi, make_uint4(e4m3_lo(w.z), e4m3_hi(w.z), e4m3_lo(w.w), e4m3_hi(w.w)));
 }
 
+// Registers of a warpgroup: launched with 96 each (640 x 96 = 61440); softmax
+// 2 x 128 x 144, widening 2 x 128 x 80, the rest 128 x 24: 60416.
+template <int N>
+__device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
+__device__ __forceinline__ void store_bf16x8(bf16* dst, uint4 w, bool wide) {
+  if (wide) {
+    *(uint4*)dst = w;
+  } else {
+    bf16 y[8];
+    memcpy(y, &w, 16);
+#pragma unroll
+    for (int z = 0; z < 8; ++z) dst[z] = y[z];
+  }
+}
+
+// codes: read once by this CTA, by others of the same (robot, KV head) from L2
+__device__ __forceinline__ uint4 ldg_codes(const uint8_t* p) { return __ldg((const uint4*)p); }
+
 // A warp's writes to shared memory become visible to the tensor core: one arrival per warp.
 __device__ __forceinline__ void written(uint64_t* bar) {
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -82,13 +106,14 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(CacheAttnArgs a) {
   uint64_t* s_full = v_empty + VS;   // [2]
   uint64_t* p_full = s_full + 2;     // [2]
   uint64_t* pv_done = p_full + 2;    // [2]
-  uint64_t* ended = pv_done + 2;
+  uint64_t* q_full = pv_done + 2;
+  uint64_t* ended = q_full + 1;
   uint32_t* tmem_slot = (uint32_t*)(ended + 1);
   int* abort_flag = (int*)(tmem_slot + 1);
   int* last_flag = abort_flag + 1;
   uint32_t* row_top = (uint32_t*)(tail + 512);    // [128] bits of the rows' largest |q|
   float2* xm = (float2*)(tail + 1024);            // [2][128] row maxima, then sums, of the two halves
-  static_assert((2 * 8 + 2 * 4 + 7) * 8 + 12 <= 512, "barriers");
+  static_assert((2 * 8 + 2 * 4 + 8) * 8 + 12 <= 512, "barriers");
 
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int b = blockIdx.z, h = blockIdx.y, split = blockIdx.x % a.splits;
@@ -121,11 +146,11 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(CacheAttnArgs a) {
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < KS; ++i) {
-      mbar_init(&k_full[i], 2);
+      mbar_init(&k_full[i], 4);
       mbar_init(&k_empty[i], 1);
     }
     for (int i = 0; i < VS; ++i) {
-      mbar_init(&v_full[i], 2);
+      mbar_init(&v_full[i], 4);
       mbar_init(&v_empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -133,72 +158,15 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(CacheAttnArgs a) {
       mbar_init(&p_full[i], 256);
       mbar_init(&pv_done[i], 1);
     }
+    mbar_init(q_full, 8);
     mbar_init(ended, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (threadIdx.x < BM) row_top[threadIdx.x] = 0u;
-  if (warp == 12) {
+  if (warp == 16) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
-  cta_sync();
-  {
-    // Q: the rows' 16-dim pieces, loaded once, scaled by their row's power of two
-    constexpr int PIECES = BM * 4 * NB, PER = (PIECES + TCT - 1) / TCT;
-    uint4 raw[PER][2];
-#pragma unroll
-    for (int p = 0; p < PER; ++p) {
-      const int x = threadIdx.x + p * TCT;
-      const int r = x / (4 * NB), d = x % (4 * NB) * 16, i = (r0 + r) / a.G;
-      raw[p][0] = raw[p][1] = make_uint4(0u, 0u, 0u, 0u);
-      if (x < PIECES && i < s.count) {
-        const bf16* row = (const bf16*)a.q + (size_t)((long long)b * a.q_robot + (long long)i * a.q_token) +
-                          (size_t)(h * a.G + (r0 + r) % a.G) * L.hd + d;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          if (d + 8 * e >= L.hd) continue;
-          if (a.vec) {
-            raw[p][e] = __ldg((const uint4*)row + e);
-          } else {
-            bf16 y[8];
-#pragma unroll
-            for (int z = 0; z < 8; ++z) y[z] = row[8 * e + z];
-            memcpy(&raw[p][e], y, 16);
-          }
-        }
-        uint32_t top = 0u;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const uint32_t u[4] = {raw[p][e].x, raw[p][e].y, raw[p][e].z, raw[p][e].w};
-#pragma unroll
-          for (int z = 0; z < 4; ++z) top = max(top, max((u[z] & 0x7fffu) << 16, u[z] & 0x7fff0000u));
-        }
-        atomicMax(&row_top[r], top);
-      }
-    }
-    cta_sync();
-#pragma unroll
-    for (int p = 0; p < PER; ++p) {
-      const int x = threadIdx.x + p * TCT;
-      if (x < PIECES) {
-        const int r = x / (4 * NB), c = x % (4 * NB);
-        const uint32_t top = row_top[r];
-        const float f = top >= 0x7f800000u ? __int_as_float(0x7fffffff) : exp2i(min(14 - ((int)(top >> 23) - 127), 126));
-        const uint32_t at = q0 + (uint32_t)(c / 4) * QB + (uint32_t)r * 128u;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const uint32_t u[4] = {raw[p][e].x, raw[p][e].y, raw[p][e].z, raw[p][e].w};
-          uint32_t w[4];
-#pragma unroll
-          for (int z = 0; z < 4; ++z)
-            w[z] = pack_f16x2(__uint_as_float(u[z] << 16) * f, __uint_as_float(u[z] & 0xffff0000u) * f);
-          sts_u4(at + (uint32_t)((((c & 3) * 2 + e) ^ (r & 7)) * 16), make_uint4(w[0], w[1], w[2], w[3]));
-        }
-      }
-    }
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   tc_fence_before();
   cta_sync();
@@ -206,97 +174,126 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(CacheAttnArgs a) {
   const uint32_t tmem = *tmem_slot;
   constexpr uint32_t o_col = 2 * BT;
 
-  if (warp == 8 || warp == 9) {
-    // ---- K: units of 64 dims, the next one's codes in flight
-    const int ct = threadIdx.x - 8 * 32;
-    const uint8_t* src = L.k + head * L.T * HDP + (size_t)(ct >> 2) * HDP + 16 * (ct & 3);
+  if (warp >= 8 && warp < 16) {
+    regs_down<80>();
+    // ---- widening: K in units of 64 dims (warps 8-11), V in halves of 64 tokens (12-15),
+    // thread ct: 16 codes at dim 16 (ct % 4) of rows ct / 4, ct / 4 + 32, ...; the codes of
+    // the next two steps are in flight (a step's latency is several times its work)
+    const bool is_k = warp < 12;
+    const int ct = (threadIdx.x - 256) & 127;
+    const uint8_t* src = (is_k ? L.k : L.v) + head * L.T * HDP + (size_t)(ct >> 2) * HDP + 16 * (ct & 3);
     const uint32_t sw = (uint32_t)(ct >> 2) & 7u, row = (uint32_t)(ct >> 2) * 128u;
     const uint32_t lo = row + ((((uint32_t)ct & 3u) * 2u) ^ sw) * 16u, hi = row + ((((uint32_t)ct & 3u) * 2u + 1u) ^ sw) * 16u;
-    uint4 cur[8], nxt[8];
-    auto load = [&](uint4* x, int t, int blk) {
-      const uint8_t* at = src + (size_t)tile_token(t) * HDP + 64 * blk;
-#pragma unroll
-      for (int y = 0; y < 8; ++y) x[y] = __ldg((const uint4*)(at + (size_t)(16 * y) * HDP));
-    };
-    int slot = 0, t = t0, blk = 0;
+    int slot = 0;
     uint32_t ph = 1;
     bool ok = true;
-    if (n > 0) load(nxt, t, 0);
-    while (ok && t < t1) {
+    if (is_k) {
+      uint4 x0[4], x1[4], x2[4];
+      int t = t0, blk = 0;   // the unit to load next
+      auto load = [&](uint4(&x)[4]) {
+        if (t >= t1) return;
+        const uint8_t* at = src + (size_t)tile_token(t) * HDP + 64 * blk;
 #pragma unroll
-      for (int y = 0; y < 8; ++y) cur[y] = nxt[y];
-      if (++blk == NB) {
-        blk = 0;
-        ++t;
-      }
-      if (t < t1) load(nxt, t, blk);
-      ok = mbar_wait_warp(&k_empty[slot], ph);
-      const uint32_t to = k0 + (uint32_t)slot * KU;
-#pragma unroll
-      for (int y = 0; y < 8; ++y) widen(cur[y], to + lo + 2048u * y, to + hi + 2048u * y);
-      written(&k_full[slot]);
-      if (++slot == KS) {
-        slot = 0;
-        ph ^= 1u;
-      }
-    }
-    if (!ok && lane == 0) *abort_flag = 1;
-  } else if (warp == 10 || warp == 11) {
-    // ---- V: halves of 64 tokens, in steps of SB blocks of 64 dims
-    constexpr int SB = NB == 3 ? 1 : (NB == 1 ? 1 : 2), STEPS = NB / SB;
-    const int ct = threadIdx.x - 10 * 32;
-    const uint8_t* src = L.v + head * L.T * HDP + (size_t)(ct >> 2) * HDP + 16 * (ct & 3);
-    const uint32_t sw = (uint32_t)(ct >> 2) & 7u, row = (uint32_t)(ct >> 2) * 128u;
-    const uint32_t lo = row + ((((uint32_t)ct & 3u) * 2u) ^ sw) * 16u, hi = row + ((((uint32_t)ct & 3u) * 2u + 1u) ^ sw) * 16u;
-    uint4 cur[4 * SB], nxt[4 * SB];
-    auto load = [&](uint4* x, int t, int half, int step) {
-      const uint8_t* at = src + (size_t)(tile_token(t) + 64 * half) * HDP + 64 * SB * step;
-#pragma unroll
-      for (int y = 0; y < 4; ++y)
-#pragma unroll
-        for (int z = 0; z < SB; ++z) x[SB * y + z] = __ldg((const uint4*)(at + (size_t)(16 * y) * HDP + 64 * z));
-    };
-    int slot = 0, t = t0, half = 0, step = 0;
-    uint32_t ph = 1;
-    bool ok = true;
-    if (n > 0) load(nxt, t, 0, 0);
-    while (ok && t < t1) {
-#pragma unroll
-      for (int y = 0; y < 4 * SB; ++y) cur[y] = nxt[y];
-      const int now = step;
-      if (++step == STEPS) {
-        step = 0;
-        if (half == 0 && keys_of(tile_token(t)) > 64) {
-          half = 1;
-        } else {
-          half = 0;
+        for (int y = 0; y < 4; ++y) x[y] = ldg_codes(at + (size_t)(32 * y) * HDP);
+        if (++blk == NB) {
+          blk = 0;
           ++t;
         }
-      }
-      if (t < t1) load(nxt, t, half, step);
-      if (now == 0) ok = mbar_wait_warp(&v_empty[slot], ph);
-      const uint32_t to = v0 + (uint32_t)slot * VH + (uint32_t)(now * SB) * VB;
+      };
+      auto put = [&](const uint4(&x)[4]) {
+        ok = mbar_wait_warp(&k_empty[slot], ph);
+        const uint32_t to = k0 + (uint32_t)slot * KU;
 #pragma unroll
-      for (int y = 0; y < 4; ++y)
-#pragma unroll
-        for (int z = 0; z < SB; ++z) widen(cur[SB * y + z], to + lo + 2048u * y + VB * z, to + hi + 2048u * y + VB * z);
-      if (now == STEPS - 1) {
-        written(&v_full[slot]);
-        if (++slot == VS) {
+        for (int y = 0; y < 4; ++y) widen(x[y], to + lo + 4096u * y, to + hi + 4096u * y);
+        written(&k_full[slot]);
+        if (++slot == KS) {
           slot = 0;
           ph ^= 1u;
         }
+      };
+      load(x0);
+      load(x1);
+      int left = n * NB;
+      while (left > 0) {
+        load(x2);
+        put(x0);
+        if (!ok || --left == 0) break;
+        load(x0);
+        put(x1);
+        if (!ok || --left == 0) break;
+        load(x1);
+        put(x2);
+        if (!ok) break;
+        --left;
+      }
+    } else {
+      // a step: two blocks of 64 dims of a half (one, where their number is odd)
+      constexpr int SB = NB % 2 ? 1 : 2, STEPS = NB / SB;
+      uint4 x0[2 * SB], x1[2 * SB], x2[2 * SB];
+      int t = t0, half = 0, step = 0;   // the step to load next
+      auto load = [&](uint4(&x)[2 * SB]) {
+        if (t >= t1) return;
+        const int j0 = tile_token(t);
+        const uint8_t* at = src + (size_t)(j0 + 64 * half) * HDP + 64 * SB * step;
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+          for (int z = 0; z < SB; ++z) x[SB * y + z] = ldg_codes(at + (size_t)(32 * y) * HDP + 64 * z);
+        if (++step == STEPS) {
+          step = 0;
+          if (half == 0 && keys_of(j0) > 64) {
+            half = 1;
+          } else {
+            half = 0;
+            ++t;
+          }
+        }
+      };
+      int now = 0;
+      auto put = [&](const uint4(&x)[2 * SB]) {
+        if (now == 0) ok = mbar_wait_warp(&v_empty[slot], ph);
+        const uint32_t to = v0 + (uint32_t)slot * VH + (uint32_t)(now * SB) * VB;
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+          for (int z = 0; z < SB; ++z) widen(x[SB * y + z], to + lo + 4096u * y + VB * z, to + hi + 4096u * y + VB * z);
+        if (++now == STEPS) {
+          now = 0;
+          written(&v_full[slot]);
+          if (++slot == VS) {
+            slot = 0;
+            ph ^= 1u;
+          }
+        }
+      };
+      int left = 0;
+      for (int q = t0; q < t1; ++q) left += keys_of(tile_token(q)) > 64 ? 2 * STEPS : STEPS;
+      load(x0);
+      load(x1);
+      while (left > 0) {
+        load(x2);
+        put(x0);
+        if (!ok || --left == 0) break;
+        load(x0);
+        put(x1);
+        if (!ok || --left == 0) break;
+        load(x1);
+        put(x2);
+        if (!ok) break;
+        --left;
       }
     }
     if (!ok && lane == 0) *abort_flag = 1;
-  } else if (warp == 12) {
+  } else if (warp >= 16) {
+    regs_down<24>();
+    if (warp == 16) {
     // ---- MMAs: S of the next tile as soon as its K is there, P V of the oldest whose P is
     const uint32_t el = elect_one();
     const uint32_t idesc_s = idesc_f16(BM, BT), idesc_o = idesc_f16(BM, HDP) | (1u << 16);
     const uint64_t qd0 = sw128_desc(q0), kd0 = sw128_desc(k0), vd0 = sw128_mn_desc(v0, VB);
     int ns = 0, i = 0, sk = 0, sv = 0;
     uint32_t phk = 0, phv = 0, spins = 0;
-    bool ok = true;
+    bool ok = mbar_wait_warp(q_full, 0);
     while (ok && i < n) {
       bool progress = false;
       if (ns < n && ns <= i + 1 && mbar_test_warp(&k_full[sk], phk)) {
@@ -354,7 +351,59 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(CacheAttnArgs a) {
       if (lane == 0) *abort_flag = 1;
     }
     __syncwarp();
+    }
   } else {
+    regs_up<144>();
+    // ---- Q: rows of 8 NB lanes with 8 dims each, scaled by their power of two
+    {
+      constexpr int LPR = 8 * NB, RPW = 32 / LPR, PASS = 16 / RPW, AHEAD = PASS < 8 ? PASS : 8;
+      const int sub = lane / LPR, dl = lane % LPR;
+      const bool on = sub < RPW && 8 * dl < L.hd;
+      for (int p0 = 0; p0 < PASS; p0 += AHEAD) {
+        uint4 x[AHEAD];
+#pragma unroll
+        for (int p = 0; p < AHEAD; ++p) {
+          const int r = r0 + warp * 16 + (p0 + p) * RPW + sub, i = r / a.G;
+          x[p] = make_uint4(0u, 0u, 0u, 0u);
+          if (on && i < s.count) {
+            const bf16* at = (const bf16*)a.q + (size_t)((long long)b * a.q_robot + (long long)i * a.q_token) +
+                             (size_t)(h * a.G + r % a.G) * L.hd + 8 * dl;
+            if (a.vec) {
+              x[p] = __ldg((const uint4*)at);
+            } else {
+              bf16 y[8];
+#pragma unroll
+              for (int z = 0; z < 8; ++z) y[z] = at[z];
+              memcpy(&x[p], y, 16);
+            }
+          }
+        }
+#pragma unroll
+        for (int p = 0; p < AHEAD; ++p) {
+          const uint32_t u[4] = {x[p].x, x[p].y, x[p].z, x[p].w};
+          uint32_t top = 0u;   // bits of the largest magnitude: NaN counts as larger than all
+#pragma unroll
+          for (int z = 0; z < 4; ++z) top = max(top, max((u[z] & 0x7fffu) << 16, u[z] & 0x7fff0000u));
+          if (RPW == 1) {
+            top = __reduce_max_sync(0xffffffffu, top);
+          } else {
+#pragma unroll
+            for (int o = 1; o < LPR; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+          }
+          const float f = top >= 0x7f800000u ? __int_as_float(0x7fffffff) : exp2i(min(14 - ((int)(top >> 23) - 127), 126));
+          uint32_t w[4];
+#pragma unroll
+          for (int z = 0; z < 4; ++z)
+            w[z] = pack_f16x2(__uint_as_float(u[z] << 16) * f, __uint_as_float(u[z] & 0xffff0000u) * f);
+          const int lr = warp * 16 + (p0 + p) * RPW + sub;
+          if (sub < RPW) sts_u4(q0 + (uint32_t)(dl >> 3) * QB + (uint32_t)lr * 128u + (uint32_t)(((dl & 7) ^ (lr & 7)) * 16),
+                                make_uint4(w[0], w[1], w[2], w[3]));
+          if (sub < RPW && dl == 0) row_top[lr] = top;
+        }
+      }
+      written(q_full);
+      asm volatile("bar.sync 5, 256;" ::: "memory");   // row_top
+    }
     // ---- softmax and epilogue: row r (TMEM lane r), tokens 64 hf .. of each tile
     const int q4 = warp & 3, hf = warp >> 2, r = q4 * 32 + lane;
     auto pair_bar = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory"); };   // warps w and w + 4
@@ -484,82 +533,94 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(CacheAttnArgs a) {
         }
       }
       asm volatile("bar.sync 5, 256;" ::: "memory");
-      const int per = L.hd / 8;   // 16-byte pieces of a row
+      // a warp per row: 16-byte pieces
       const bool wide = ((uintptr_t)a.out | (uintptr_t)(a.out_robot * 2) | (uintptr_t)(a.out_token * 2)) % 16 == 0;
-      for (int x = threadIdx.x; x < rows * per; x += 256) {
-        const int rr = x / per, c = x % per;
-        const uint4 w = *(const uint4*)(smem + (size_t)(c >> 3) * QB + (size_t)rr * 128 + (((c & 7) ^ (rr & 7)) * 16));
-        bf16* dst = out_row(r0 + rr) + 8 * c;
-        if (wide) {
-          *(uint4*)dst = w;
-        } else {
-          bf16 y[8];
-          memcpy(y, &w, 16);
-#pragma unroll
-          for (int z = 0; z < 8; ++z) dst[z] = y[z];
+      for (int rr = warp; rr < rows; rr += 8) {
+        bf16* dst = out_row(r0 + rr) + 8 * lane;
+        if (8 * lane < L.hd) {
+          const uint4 w = *(const uint4*)(smem + (size_t)(lane >> 3) * QB + (size_t)rr * 128 + (((lane & 7) ^ (rr & 7)) * 16));
+          store_bf16x8(dst, w, wide);
         }
       }
     } else {
-      // partial [d / 4][row][4], normalised, with its (max, sum); the last split joins them in order
+      // partial [row][d], normalised, with its (max, sum)
       const size_t unit = head * a.row_tiles + tile, at = unit * a.splits + split;
-      float* part = a.part + at * BM * HDP;
+      float* part = a.part + (at * BM + r) * HDP;
       for (int cb = 32 * hf; cb < HDP; cb += 64) {
         uint32_t raw[32];
         tmem_ld32_async(lane_base + o_col + cb, raw);
         tmem_wait_ld();
         tmem_reg_fence16(raw);
         tmem_reg_fence16(raw + 16);
+        if (r < rows) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q)
-          __stcg((float4*)(part + ((size_t)(cb / 4 + q) * BM + r) * 4),
-                 real ? make_float4(__uint_as_float(raw[4 * q]) * inv, __uint_as_float(raw[4 * q + 1]) * inv,
-                                    __uint_as_float(raw[4 * q + 2]) * inv, __uint_as_float(raw[4 * q + 3]) * inv)
-                      : make_float4(0.f, 0.f, 0.f, 0.f));
+          for (int q = 0; q < 8; ++q)
+            __stcg((float4*)(part + cb + 4 * q),
+                   real ? make_float4(__uint_as_float(raw[4 * q]) * inv, __uint_as_float(raw[4 * q + 1]) * inv,
+                                      __uint_as_float(raw[4 * q + 2]) * inv, __uint_as_float(raw[4 * q + 3]) * inv)
+                        : make_float4(0.f, 0.f, 0.f, 0.f));
+        }
       }
       if (hf == 0) __stcg(a.part_ml + at * BM + r, make_float2(m_out, l_out));
       __threadfence();
-      asm volatile("bar.sync 5, 256;" ::: "memory");
-      if (threadIdx.x == 0) *last_flag = atomicInc(a.arrived + unit, (unsigned)a.splits - 1u) == (unsigned)a.splits - 1u;
-      asm volatile("bar.sync 5, 256;" ::: "memory");
-      if (*last_flag) {
-        __threadfence();
-        const float2* ml = a.part_ml + unit * a.splits * BM + r;
-        float M = -INFINITY, S = 0.f;
-        for (int q = 0; q < a.splits; ++q) M = fmaxf(M, __ldcg(ml + q * BM).x);
-        for (int q = 0; q < a.splits; ++q) {
-          const float2 x = __ldcg(ml + q * BM);
-          S += x.y != x.y ? x.y : (x.x == -INFINITY ? 0.f : exp2f(x.x - M) * x.y);
-        }
-        const float si = !(S <= 0.f) ? 1.f / S : 0.f;
-        if (a.mass && hf == 0 && r < rows) a.row_ml[head * a.n * a.G + r0 + r] = row_weight(M, S, kTcShift);
-        const float* p0 = a.part + unit * a.splits * BM * HDP;
-        bf16* dst = out_row(r0 + min(r, rows - 1));
-        for (int d4 = hf; d4 < L.hd / 4; d4 += 2) {
-          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      // the splits' partials joined in their order: up to 8 splits are a cluster, each of
+      // which joins a share of the rows once all have stored; of more, the last to arrive
+      // joins all rows
+      int ra = 0, rb = rows;
+      if (a.splits <= kTcCluster) {
+        cluster_sync();   // (the other roles arrive below)
+        const int share = (rows + a.splits - 1) / a.splits;
+        ra = split * share;
+        rb = min(rows, ra + share);
+      } else {
+        asm volatile("bar.sync 5, 256;" ::: "memory");
+        if (threadIdx.x == 0) *last_flag = atomicInc(a.arrived + unit, (unsigned)a.splits - 1u) == (unsigned)a.splits - 1u;
+        asm volatile("bar.sync 5, 256;" ::: "memory");
+        if (!*last_flag) rb = 0;
+      }
+      __threadfence();
+      {
+        const bool wide = ((uintptr_t)a.out | (uintptr_t)(a.out_robot * 2) | (uintptr_t)(a.out_token * 2)) % 16 == 0;
+        for (int rr = ra + warp; rr < rb; rr += 8) {
+          const float2* ml = a.part_ml + unit * a.splits * BM + rr;
+          const float* p0 = a.part + (unit * a.splits * BM + rr) * HDP + 8 * lane;
+          const bool on = 8 * lane < L.hd;
+          float M = -INFINITY, S = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+          for (int q = 0; q < a.splits; ++q) M = fmaxf(M, __ldcg(ml + q * BM).x);
+  #pragma unroll 4
           for (int q = 0; q < a.splits; ++q) {
             const float2 x = __ldcg(ml + q * BM);
-            const float wt = (x.y != x.y ? x.y : (x.x == -INFINITY ? 0.f : exp2f(x.x - M) * x.y)) * si;
-            const float4 y = __ldcg((const float4*)(p0 + (size_t)q * BM * HDP + ((size_t)d4 * BM + r) * 4));
-            acc.x += wt * y.x;
-            acc.y += wt * y.y;
-            acc.z += wt * y.z;
-            acc.w += wt * y.w;
+            const float wt = x.y != x.y ? x.y : (x.x == -INFINITY ? 0.f : exp2f(x.x - M) * x.y);
+            S += wt;
+            if (on) {
+              const float4* y = (const float4*)(p0 + (size_t)q * BM * HDP);
+              const float4 y0 = __ldcg(y), y1 = __ldcg(y + 1);
+              acc[0] = fmaf(wt, y0.x, acc[0]);
+              acc[1] = fmaf(wt, y0.y, acc[1]);
+              acc[2] = fmaf(wt, y0.z, acc[2]);
+              acc[3] = fmaf(wt, y0.w, acc[3]);
+              acc[4] = fmaf(wt, y1.x, acc[4]);
+              acc[5] = fmaf(wt, y1.y, acc[5]);
+              acc[6] = fmaf(wt, y1.z, acc[6]);
+              acc[7] = fmaf(wt, y1.w, acc[7]);
+            }
           }
-          if (r < rows) {
-            bf16* o = dst + 4 * d4;
-            o[0] = __float2bfloat16_rn(acc.x);
-            o[1] = __float2bfloat16_rn(acc.y);
-            o[2] = __float2bfloat16_rn(acc.z);
-            o[3] = __float2bfloat16_rn(acc.w);
-          }
+          const float si = !(S <= 0.f) ? 1.f / S : 0.f;
+          if (a.mass && lane == 0) a.row_ml[head * a.n * a.G + r0 + rr] = row_weight(M, S, kTcShift);
+          if (on)
+            store_bf16x8(out_row(r0 + rr) + 8 * lane,
+                         make_uint4(pack_bf16x2(acc[0] * si, acc[1] * si), pack_bf16x2(acc[2] * si, acc[3] * si),
+                                    pack_bf16x2(acc[4] * si, acc[5] * si), pack_bf16x2(acc[6] * si, acc[7] * si)),
+                         wide);
         }
       }
     }
   }
+  if (warp >= 8 && a.splits > 1 && a.splits <= kTcCluster) cluster_sync();
   tc_fence_before();
   cta_sync();
   if (*abort_flag && threadIdx.x == 0) raise_error(a.err, ERR_TIMEOUT);
-  if (warp == 12)
+  if (warp == 16)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
 }
 
@@ -571,8 +632,8 @@ cudaError_t launch_nb(CacheAttnArgs a, cudaStream_t st) {
   if (a.window > 0) seen = std::min(seen, (long long)a.window + a.sinks + BM / a.G + 1 + 2 * BT);
   const long long units = (seen + BT - 1) / BT;
   a.splits = (int)std::max(1ll, std::min((long long)a.num_sms / tiles, units));
-  cache_tc_kernel<NB><<<dim3(a.row_tiles * a.splits, a.c.Hkv, a.batch), TCT, TcShape<NB>::bytes, st>>>(a);
-  return cudaGetLastError();
+  return launch_kernel_cluster(cache_tc_kernel<NB>, dim3(a.row_tiles * a.splits, a.c.Hkv, a.batch), dim3(TCT),
+                               TcShape<NB>::bytes, st, dim3(a.splits <= kTcCluster ? a.splits : 1, 1, 1), a);
 }
 
 template <int NB>
