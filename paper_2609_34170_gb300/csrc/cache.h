@@ -68,6 +68,7 @@ struct CacheAttnArgs {
   int mass_add;
   int vec;                  // q rows are 16-byte aligned
   int num_sms;
+  const int* clusters;      // clusters of that many (up to 8) tensor-core CTAs that the device holds at once
   // workspace
   float* part;              // [units * splits][rows of a tile x hdp] normalised partial outputs
   float2* part_ml;          // [units * splits][rows of a tile] (max, sum)
@@ -82,6 +83,6 @@ constexpr int kCacheTcRows = 128;      // rows of a tile on the tensor cores: at
 cudaError_t launch_cache_attend(const CacheAttnArgs& a, Dtype dt, cudaStream_t st);
 cudaError_t launch_cache_attend_tc(const CacheAttnArgs& a, cudaStream_t st);   // bf16; not the mass
 cudaError_t init_cache_kernels();
-cudaError_t init_cache_tc_kernels();
+cudaError_t init_cache_tc_kernels(int hdp, int* clusters);   // clusters: [9]
 
 }  // namespace ravel

@@ -7,14 +7,17 @@
 //   P = 2^(S - m)    softmax warps: TMEM -> registers -> f16 P over S in TMEM
 //   O += P V         tcgen05.mma, M = 128, N = head dim, 16 tokens at a time
 // Warp roles (640 threads): warps 0-7 Q, softmax and epilogue, two threads per row;
-// warps 8-11 widen K, warps 12-15 widen V; warp 16 TMEM and MMAs (17-19 idle, so
-// that registers can be moved between whole warpgroups).
+// warps 8-11 widen K, warps 12-15 widen V; warp 16 TMEM and MMAs; warps 17, 18 load
+// the codes of K and V (19 idle, so that registers move between whole warpgroups).
 //
-// The codes go from global memory through the widening warps' registers into
-// shared memory as f16 (e4m3 -> f16 is exact), in the 128-byte swizzled layout
-// that a TMA load of f16 rows would leave: K in units of 64 head dims (16 KB),
-// V in halves of 64 tokens, each in a ring of its own with its own producers, so
-// that neither waits for the other's slots.  Feeding the codes as kind::f8f6f4
+// The codes come by TMA and are widened in shared memory to f16 (e4m3 -> f16 is
+// exact), into the 128-byte swizzled layout that a TMA load of f16 rows would
+// leave: K in units of 64 head dims (16 KB), V in halves of 64 tokens, each in
+// rings of its own with its own warps, so that neither waits for the other's
+// slots.  (With the codes loaded to registers by the widening warps themselves a
+// unit took a load's latency, 900 cycles of the 512 that the MMAs of four units
+// leave each: the proxy fence that ends a unit waits for the loads in flight.)
+// Feeding the codes as kind::f8f6f4
 // operands instead would need Q and P in 8 bits too: two pieces of each keep
 // bf16's precision and cost what one f16 MMA does, but 2^-9 is the least P that
 // e4m3 holds, and a long flat tail of smaller ones carries weight.
@@ -24,6 +27,9 @@
 // most 2^7 of the reference, 2^15 while a grown one waits for its rescaling of O
 // (only growth by more than 2^8 rescales); what contributes less than 2^-31 of the
 // row's largest is dropped.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
 #include <algorithm>
 
 #include "cache_attn.cuh"
@@ -36,18 +42,34 @@ constexpr int TCT = 640;
 constexpr int BM = 128, BT = 128;              // rows, tokens of a tile
 constexpr uint32_t QB = BM * 128;              // bytes of a 64-dim block of Q
 constexpr uint32_t KU = BT * 128;              // bytes of a K unit: 128 tokens x 64 dims
+constexpr uint32_t CB = 64 * 64;                // bytes of a slot of codes: 64 tokens x 64 dims
 constexpr uint32_t VB = 64 * 128;              // bytes of a 64-dim block of a V half
 constexpr float kTcShift = 7.f;                // P's largest value is 2^kTcShift (times 2^8 while lazy)
 constexpr int kTcCluster = 8;                  // splits that are a cluster
 constexpr uint32_t kPolls = 1u << 25;          // polls without progress: seconds
 
 template <int NB> struct TcShape {
-  // shared memory at NB blocks of 64 head dims: Q NB x 16 KB, then the rings
-  static constexpr int KS = NB == 4 ? 4 : (NB == 3 ? 5 : 2 * NB);
-  static constexpr int VS = NB == 4 ? 3 : 4;
-  static constexpr uint32_t bytes = NB * QB + KS * KU + VS * NB * VB + 3072;
+  // shared memory at NB blocks of 64 head dims: Q, the rings of widened K units and V
+  // halves, the rings of codes, barriers and row data
+  static constexpr int KS = 4;
+  static constexpr int VS = NB >= 3 ? 2 : 4;
+  // a multiple of the 4 warps that widen them: each slot is then waited for by one warp, in
+  // order.  (Loads may complete out of order; a warp that waits for a slot's next phase while
+  // another's load into it is still on its way would take the phase before for it.)
+  static constexpr int CS = NB == 4 ? 4 : 8;
+  static_assert(CS % 4 == 0, "widening warps");
+  static constexpr uint32_t ring = KS * KU + VS * NB * VB + 2 * CS * CB;
+  static constexpr uint32_t bytes = NB * QB + ring + 3072;
+  static_assert(bytes <= 227 * 1024, "shared memory");
+  // a row of the fp32 output that splits exchange (over the rings): 16 bytes more than
+  // the dims, so that rows written by neighbouring lanes fall on different banks
+  static constexpr uint32_t xrow = NB * 64 * 4 + 16;
+  static_assert(BM * xrow <= ring && BM * 4 * 256 <= ring && BM * 4 * 8 <= NB * QB, "exchange");
 };
-static_assert(TcShape<4>::bytes <= 227 * 1024 && TcShape<3>::bytes <= 227 * 1024, "shared memory");
+
+struct TcMaps {
+  CUtensorMap k, v;   // a layer's codes [B Hkv T][hdp] in boxes of 64 dims x 64 rows
+};
 
 // f16 A and B, fp32 D
 __device__ __forceinline__ uint32_t idesc_f16(int m, int n) {
@@ -82,8 +104,31 @@ __device__ __forceinline__ void store_bf16x8(bf16* dst, uint4 w, bool wide) {
   }
 }
 
-// codes: read once by this CTA, by others of the same (robot, KV head) from L2
-__device__ __forceinline__ uint4 ldg_codes(const uint8_t* p) { return __ldg((const uint4*)p); }
+// eight bf16 at any alignment
+__device__ __noinline__ uint4 ldg_bf16x8(const bf16* p) {
+  bf16 y[8];
+#pragma unroll
+  for (int z = 0; z < 8; ++z) y[z] = p[z];
+  uint4 w;
+  memcpy(&w, y, 16);
+  return w;
+}
+
+__device__ __forceinline__ uint4 lds_codes(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t a) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ float2 ld_cluster_f2(uint32_t a) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a));
+  return v;
+}
 
 // A warp's writes to shared memory become visible to the tensor core: one arrival per warp.
 __device__ __forceinline__ void written(uint64_t* bar) {
@@ -93,17 +138,19 @@ __device__ __forceinline__ void written(uint64_t* bar) {
 }
 
 template <int NB>
-__global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(CacheAttnArgs a) {
-  constexpr int HDP = 64 * NB, KS = TcShape<NB>::KS, VS = TcShape<NB>::VS;
+__global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant__ TcMaps maps, CacheAttnArgs a) {
+  constexpr int HDP = 64 * NB, KS = TcShape<NB>::KS, VS = TcShape<NB>::VS, CS = TcShape<NB>::CS;
   constexpr uint32_t VH = NB * VB;   // bytes of a V half
   extern __shared__ __align__(1024) uint8_t smem[];
-  const uint32_t q0 = smem_u32(smem), k0 = q0 + NB * QB, v0 = k0 + KS * KU;
-  uint8_t* tail = smem + NB * QB + KS * KU + VS * VH;
+  const uint32_t q0 = smem_u32(smem), k0 = q0 + NB * QB, v0 = k0 + KS * KU, ck0 = v0 + VS * VH, cv0 = ck0 + CS * CB;
+  uint8_t* tail = smem + NB * QB + TcShape<NB>::ring;
   uint64_t* k_full = (uint64_t*)tail;
   uint64_t* k_empty = k_full + KS;
   uint64_t* v_full = k_empty + KS;
   uint64_t* v_empty = v_full + VS;
-  uint64_t* s_full = v_empty + VS;   // [2]
+  uint64_t* c_full = v_empty + VS;   // [2 CS] codes of K, then of V
+  uint64_t* c_empty = c_full + 2 * CS;
+  uint64_t* s_full = c_empty + 2 * CS;   // [2]
   uint64_t* p_full = s_full + 2;     // [2]
   uint64_t* pv_done = p_full + 2;    // [2]
   uint64_t* q_full = pv_done + 2;
@@ -111,9 +158,10 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(CacheAttnArgs a) {
   uint32_t* tmem_slot = (uint32_t*)(ended + 1);
   int* abort_flag = (int*)(tmem_slot + 1);
   int* last_flag = abort_flag + 1;
+  int* c_issued = last_flag + 1;     // [2] loads of codes issued, K and V
   uint32_t* row_top = (uint32_t*)(tail + 512);    // [128] bits of the rows' largest |q|
   float2* xm = (float2*)(tail + 1024);            // [2][128] row maxima, then sums, of the two halves
-  static_assert((2 * 8 + 2 * 4 + 8) * 8 + 12 <= 512, "barriers");
+  static_assert((2 * KS + 2 * VS + 4 * CS + 8) * 8 + 20 <= 512, "barriers");
 
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int b = blockIdx.z, h = blockIdx.y, split = blockIdx.x % a.splits;
@@ -128,7 +176,10 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(CacheAttnArgs a) {
   }
   if (!robot_sight(a, b, s) && threadIdx.x == 0 && blockIdx.x == 0 && h == 0) raise_error(a.err, ERR_SHAPE);
   bf16* out0 = (bf16*)a.out + (size_t)((long long)b * a.out_robot) + (size_t)h * a.G * L.hd;
-  auto out_row = [&](int r) { return out0 + (size_t)((long long)(r / a.G) * a.out_token) + (size_t)(r % a.G) * L.hd; };
+  auto out_row = [&](int r) {
+    const uint32_t i = (uint32_t)r / (uint32_t)a.G;
+    return out0 + (size_t)((long long)i * a.out_token) + (size_t)((uint32_t)r - i * (uint32_t)a.G) * L.hd;
+  };
   if (r0 >= s.count * a.G || s.len == 0) {   // nothing to see: zeros
     if (split == 0)
       for (int w = threadIdx.x; w < rows * L.hd; w += TCT) out_row(r0 + w / L.hd)[w % L.hd] = __float2bfloat16_rn(0.f);
@@ -146,14 +197,19 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(CacheAttnArgs a) {
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < KS; ++i) {
-      mbar_init(&k_full[i], 4);
+      mbar_init(&k_full[i], 2);   // its steps
       mbar_init(&k_empty[i], 1);
     }
     for (int i = 0; i < VS; ++i) {
-      mbar_init(&v_full[i], 4);
+      mbar_init(&v_full[i], NB);
       mbar_init(&v_empty[i], 1);
     }
+    for (int i = 0; i < 2 * CS; ++i) {
+      mbar_init(&c_full[i], 1);
+      mbar_init(&c_empty[i], 1);
+    }
     for (int i = 0; i < 2; ++i) {
+      c_issued[i] = 0;
       mbar_init(&s_full[i], 1);
       mbar_init(&p_full[i], 256);
       mbar_init(&pv_done[i], 1);
@@ -168,6 +224,22 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(CacheAttnArgs a) {
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  // Q: rows of 8 NB lanes with 8 dims each, 16 rows per softmax warp; on their way while
+  // TMEM and barriers are set up
+  constexpr int LPR = 8 * NB, RPW = 32 / LPR, PASS = 16 / RPW;
+  const int q_sub = lane / LPR, q_dl = lane % LPR;
+  uint4 qx[PASS];
+  if (warp < 8) {
+    const bool on = q_sub < RPW && 8 * q_dl < L.hd;
+    const bf16* base = (const bf16*)a.q + (size_t)((long long)b * a.q_robot) + (size_t)h * a.G * L.hd + 8 * q_dl;
+#pragma unroll
+    for (int p = 0; p < PASS; ++p) {
+      const uint32_t r = (uint32_t)(r0 + warp * 16 + p * RPW + q_sub), i = r / (uint32_t)a.G;
+      const bf16* at = base + (size_t)((long long)i * a.q_token) + (size_t)(r - i * a.G) * L.hd;
+      qx[p] = make_uint4(0u, 0u, 0u, 0u);
+      if (on && (int)i < s.count) qx[p] = a.vec ? __ldg((const uint4*)at) : ldg_bf16x8(at);
+    }
+  }
   tc_fence_before();
   cta_sync();
   tc_fence_after();
@@ -176,112 +248,37 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(CacheAttnArgs a) {
 
   if (warp >= 8 && warp < 16) {
     regs_down<80>();
-    // ---- widening: K in units of 64 dims (warps 8-11), V in halves of 64 tokens (12-15),
-    // thread ct: 16 codes at dim 16 (ct % 4) of rows ct / 4, ct / 4 + 32, ...; the codes of
-    // the next two steps are in flight (a step's latency is several times its work)
+    // ---- widening: K in units of 64 dims (warps 8-11), V in halves of 64 tokens (12-15), in
+    // steps of 64 tokens x 64 dims.  A warp takes every fourth step as a whole, so that the
+    // waits, the proxy fence and the shared-memory latency of one lie beside the work on the
+    // others (a unit by four warps together took 750 cycles, little of it work).
     const bool is_k = warp < 12;
-    const int ct = (threadIdx.x - 256) & 127;
-    const uint8_t* src = (is_k ? L.k : L.v) + head * L.T * HDP + (size_t)(ct >> 2) * HDP + 16 * (ct & 3);
-    const uint32_t sw = (uint32_t)(ct >> 2) & 7u, row = (uint32_t)(ct >> 2) * 128u;
-    const uint32_t lo = row + ((((uint32_t)ct & 3u) * 2u) ^ sw) * 16u, hi = row + ((((uint32_t)ct & 3u) * 2u + 1u) ^ sw) * 16u;
-    int slot = 0;
-    uint32_t ph = 1;
+    // lane: 16 codes at dim 16 (lane % 4) of rows lane / 4, lane / 4 + 8, ...
+    const uint32_t sw = (uint32_t)(lane >> 2), row = (uint32_t)(lane >> 2) * 128u;
+    const uint32_t lo = row + ((((uint32_t)lane & 3u) * 2u) ^ sw) * 16u, hi = row + ((((uint32_t)lane & 3u) * 2u + 1u) ^ sw) * 16u;
+    const uint32_t codes = (is_k ? ck0 : cv0) + 16u * lane;
+    uint64_t *cf = c_full + (is_k ? 0 : CS), *ce = c_empty + (is_k ? 0 : CS);
+    // a unit of K takes 2 steps, a half of V NB; every tile but the last has two halves
+    const int per = is_k ? 2 : NB, ring = is_k ? KS : VS;
+    const int steps = is_k ? n * NB * 2 : (n > 0 ? (2 * n - (keys_of(tile_token(t1 - 1)) > 64 ? 0 : 1)) * NB : 0);
+    const uint32_t to0 = (is_k ? k0 : v0), slot_bytes = is_k ? KU : VH;
+    uint64_t *full = is_k ? k_full : v_full, *empty = is_k ? k_empty : v_empty;
     bool ok = true;
-    if (is_k) {
-      uint4 x0[4], x1[4], x2[4];
-      int t = t0, blk = 0;   // the unit to load next
-      auto load = [&](uint4(&x)[4]) {
-        if (t >= t1) return;
-        const uint8_t* at = src + (size_t)tile_token(t) * HDP + 64 * blk;
+    for (int u = warp & 3; u < steps; u += 4) {
+      const int cs = u % CS, item = u / per, slot = item % ring;
+      ok = mbar_wait_warp(&cf[cs], (uint32_t)(u / CS) & 1u);
+      if (!ok) break;
+      uint4 x[8];
 #pragma unroll
-        for (int y = 0; y < 4; ++y) x[y] = ldg_codes(at + (size_t)(32 * y) * HDP);
-        if (++blk == NB) {
-          blk = 0;
-          ++t;
-        }
-      };
-      auto put = [&](const uint4(&x)[4]) {
-        ok = mbar_wait_warp(&k_empty[slot], ph);
-        const uint32_t to = k0 + (uint32_t)slot * KU;
+      for (int y = 0; y < 8; ++y) x[y] = lds_codes(codes + (uint32_t)cs * CB + 512u * y);
+      ok = mbar_wait_warp(&empty[slot], ((uint32_t)(item / ring) & 1u) ^ 1u);
+      if (!ok) break;
+      __syncwarp();   // every lane has its codes
+      if (lane == 0) mbar_arrive(&ce[cs]);
+      const uint32_t to = to0 + (uint32_t)slot * slot_bytes + (uint32_t)(u % per) * VB;
 #pragma unroll
-        for (int y = 0; y < 4; ++y) widen(x[y], to + lo + 4096u * y, to + hi + 4096u * y);
-        written(&k_full[slot]);
-        if (++slot == KS) {
-          slot = 0;
-          ph ^= 1u;
-        }
-      };
-      load(x0);
-      load(x1);
-      int left = n * NB;
-      while (left > 0) {
-        load(x2);
-        put(x0);
-        if (!ok || --left == 0) break;
-        load(x0);
-        put(x1);
-        if (!ok || --left == 0) break;
-        load(x1);
-        put(x2);
-        if (!ok) break;
-        --left;
-      }
-    } else {
-      // a step: two blocks of 64 dims of a half (one, where their number is odd)
-      constexpr int SB = NB % 2 ? 1 : 2, STEPS = NB / SB;
-      uint4 x0[2 * SB], x1[2 * SB], x2[2 * SB];
-      int t = t0, half = 0, step = 0;   // the step to load next
-      auto load = [&](uint4(&x)[2 * SB]) {
-        if (t >= t1) return;
-        const int j0 = tile_token(t);
-        const uint8_t* at = src + (size_t)(j0 + 64 * half) * HDP + 64 * SB * step;
-#pragma unroll
-        for (int y = 0; y < 2; ++y)
-#pragma unroll
-          for (int z = 0; z < SB; ++z) x[SB * y + z] = ldg_codes(at + (size_t)(32 * y) * HDP + 64 * z);
-        if (++step == STEPS) {
-          step = 0;
-          if (half == 0 && keys_of(j0) > 64) {
-            half = 1;
-          } else {
-            half = 0;
-            ++t;
-          }
-        }
-      };
-      int now = 0;
-      auto put = [&](const uint4(&x)[2 * SB]) {
-        if (now == 0) ok = mbar_wait_warp(&v_empty[slot], ph);
-        const uint32_t to = v0 + (uint32_t)slot * VH + (uint32_t)(now * SB) * VB;
-#pragma unroll
-        for (int y = 0; y < 2; ++y)
-#pragma unroll
-          for (int z = 0; z < SB; ++z) widen(x[SB * y + z], to + lo + 4096u * y + VB * z, to + hi + 4096u * y + VB * z);
-        if (++now == STEPS) {
-          now = 0;
-          written(&v_full[slot]);
-          if (++slot == VS) {
-            slot = 0;
-            ph ^= 1u;
-          }
-        }
-      };
-      int left = 0;
-      for (int q = t0; q < t1; ++q) left += keys_of(tile_token(q)) > 64 ? 2 * STEPS : STEPS;
-      load(x0);
-      load(x1);
-      while (left > 0) {
-        load(x2);
-        put(x0);
-        if (!ok || --left == 0) break;
-        load(x0);
-        put(x1);
-        if (!ok || --left == 0) break;
-        load(x1);
-        put(x2);
-        if (!ok) break;
-        --left;
-      }
+      for (int y = 0; y < 8; ++y) widen(x[y], to + lo + 1024u * y, to + hi + 1024u * y);
+      written(&full[slot]);
     }
     if (!ok && lane == 0) *abort_flag = 1;
   } else if (warp >= 16) {
@@ -351,59 +348,69 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(CacheAttnArgs a) {
       if (lane == 0) *abort_flag = 1;
     }
     __syncwarp();
+    } else if (warp < 19) {
+      // ---- the codes' loads
+      const uint32_t el = elect_one();
+      const bool is_k = warp == 17;
+      const uint32_t to = is_k ? ck0 : cv0;
+      uint64_t *cf = c_full + (is_k ? 0 : CS), *ce = c_empty + (is_k ? 0 : CS);
+      uint64_t pol;
+      asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(pol));
+      const int y0 = (int)(head * L.T);
+      int slot = 0, issued = 0;
+      uint32_t ph = 1;
+      bool ok = true;
+      for (int t = t0; ok && t < t1; ++t) {
+        const int j0 = tile_token(t), steps = NB * (is_k || keys_of(j0) > 64 ? 2 : 1);
+        for (int q = 0; q < steps; ++q) {
+          ok = mbar_wait_warp(&ce[slot], ph);
+          if (!ok) break;
+          // K: the unit's two halves of 64 tokens; V: the half's blocks of 64 dims
+          const int half = is_k ? q & 1 : q / NB, blk = is_k ? q >> 1 : q % NB;
+          mbar_expect_tx_el(&cf[slot], CB, el);
+          tma_load_2d_el(is_k ? &maps.k : &maps.v, smem_u32(&cf[slot]), to + (uint32_t)slot * CB, 64 * blk, y0 + j0 + 64 * half,
+                         pol, el);
+          ++issued;
+          if (++slot == CS) {
+            slot = 0;
+            ph ^= 1u;
+          }
+        }
+      }
+      if (lane == 0) {
+        c_issued[is_k ? 0 : 1] = issued;
+        if (!ok) *abort_flag = 1;
+      }
+      __syncwarp();
     }
   } else {
     regs_up<144>();
-    // ---- Q: rows of 8 NB lanes with 8 dims each, scaled by their power of two
-    {
-      constexpr int LPR = 8 * NB, RPW = 32 / LPR, PASS = 16 / RPW, AHEAD = PASS < 8 ? PASS : 8;
-      const int sub = lane / LPR, dl = lane % LPR;
-      const bool on = sub < RPW && 8 * dl < L.hd;
-      for (int p0 = 0; p0 < PASS; p0 += AHEAD) {
-        uint4 x[AHEAD];
+    // ---- Q, scaled by the rows' powers of two
 #pragma unroll
-        for (int p = 0; p < AHEAD; ++p) {
-          const int r = r0 + warp * 16 + (p0 + p) * RPW + sub, i = r / a.G;
-          x[p] = make_uint4(0u, 0u, 0u, 0u);
-          if (on && i < s.count) {
-            const bf16* at = (const bf16*)a.q + (size_t)((long long)b * a.q_robot + (long long)i * a.q_token) +
-                             (size_t)(h * a.G + r % a.G) * L.hd + 8 * dl;
-            if (a.vec) {
-              x[p] = __ldg((const uint4*)at);
-            } else {
-              bf16 y[8];
+    for (int p = 0; p < PASS; ++p) {
+      const uint32_t u[4] = {qx[p].x, qx[p].y, qx[p].z, qx[p].w};
+      uint32_t top = 0u;   // bits of the largest magnitude: NaN counts as larger than all
 #pragma unroll
-              for (int z = 0; z < 8; ++z) y[z] = at[z];
-              memcpy(&x[p], y, 16);
-            }
-          }
-        }
+      for (int z = 0; z < 4; ++z) top = max(top, max((u[z] & 0x7fffu) << 16, u[z] & 0x7fff0000u));
+      if (RPW == 1) {
+        top = __reduce_max_sync(0xffffffffu, top);
+      } else {
 #pragma unroll
-        for (int p = 0; p < AHEAD; ++p) {
-          const uint32_t u[4] = {x[p].x, x[p].y, x[p].z, x[p].w};
-          uint32_t top = 0u;   // bits of the largest magnitude: NaN counts as larger than all
-#pragma unroll
-          for (int z = 0; z < 4; ++z) top = max(top, max((u[z] & 0x7fffu) << 16, u[z] & 0x7fff0000u));
-          if (RPW == 1) {
-            top = __reduce_max_sync(0xffffffffu, top);
-          } else {
-#pragma unroll
-            for (int o = 1; o < LPR; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-          }
-          const float f = top >= 0x7f800000u ? __int_as_float(0x7fffffff) : exp2i(min(14 - ((int)(top >> 23) - 127), 126));
-          uint32_t w[4];
-#pragma unroll
-          for (int z = 0; z < 4; ++z)
-            w[z] = pack_f16x2(__uint_as_float(u[z] << 16) * f, __uint_as_float(u[z] & 0xffff0000u) * f);
-          const int lr = warp * 16 + (p0 + p) * RPW + sub;
-          if (sub < RPW) sts_u4(q0 + (uint32_t)(dl >> 3) * QB + (uint32_t)lr * 128u + (uint32_t)(((dl & 7) ^ (lr & 7)) * 16),
-                                make_uint4(w[0], w[1], w[2], w[3]));
-          if (sub < RPW && dl == 0) row_top[lr] = top;
-        }
+        for (int o = 1; o < LPR; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
       }
-      written(q_full);
-      asm volatile("bar.sync 5, 256;" ::: "memory");   // row_top
+      const float f = top >= 0x7f800000u ? __int_as_float(0x7fffffff) : exp2i(min(14 - ((int)(top >> 23) - 127), 126));
+      uint32_t w[4];
+#pragma unroll
+      for (int z = 0; z < 4; ++z) w[z] = pack_f16x2(__uint_as_float(u[z] << 16) * f, __uint_as_float(u[z] & 0xffff0000u) * f);
+      const int lr = warp * 16 + p * RPW + q_sub;
+      if (q_sub < RPW) {
+        sts_u4(q0 + (uint32_t)(q_dl >> 3) * QB + (uint32_t)lr * 128u + (uint32_t)(((q_dl & 7) ^ (lr & 7)) * 16),
+               make_uint4(w[0], w[1], w[2], w[3]));
+        if (q_dl == 0) row_top[lr] = top;
+      }
     }
+    written(q_full);
+    asm volatile("bar.sync 5, 256;" ::: "memory");   // row_top
     // ---- softmax and epilogue: row r (TMEM lane r), tokens 64 hf .. of each tile
     const int q4 = warp & 3, hf = warp >> 2, r = q4 * 32 + lane;
     auto pair_bar = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory"); };   // warps w and w + 4
@@ -535,93 +542,137 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(CacheAttnArgs a) {
       asm volatile("bar.sync 5, 256;" ::: "memory");
       // a warp per row: 16-byte pieces
       const bool wide = ((uintptr_t)a.out | (uintptr_t)(a.out_robot * 2) | (uintptr_t)(a.out_token * 2)) % 16 == 0;
+#pragma unroll 4
       for (int rr = warp; rr < rows; rr += 8) {
         bf16* dst = out_row(r0 + rr) + 8 * lane;
-        if (8 * lane < L.hd) {
-          const uint4 w = *(const uint4*)(smem + (size_t)(lane >> 3) * QB + (size_t)rr * 128 + (((lane & 7) ^ (rr & 7)) * 16));
-          store_bf16x8(dst, w, wide);
-        }
+        if (8 * lane < L.hd) store_bf16x8(dst, lds_codes(q0 + (uint32_t)(lane >> 3) * QB + (uint32_t)rr * 128u + (uint32_t)(((lane & 7) ^ (rr & 7)) * 16)), wide);
       }
     } else {
-      // partial [row][d], normalised, with its (max, sum)
-      const size_t unit = head * a.row_tiles + tile, at = unit * a.splits + split;
-      float* part = a.part + (at * BM + r) * HDP;
+      // normalised partials, joined in the splits' order: up to 8 splits are a cluster, whose
+      // CTAs read a share of the rows each from one another's shared memory; of more, which
+      // store to L2, the last to arrive joins all rows
+      const bool cluster = a.splits <= kTcCluster;
+      const size_t unit = head * a.row_tiles + tile;
+      constexpr uint32_t XR = TcShape<NB>::xrow;
       for (int cb = 32 * hf; cb < HDP; cb += 64) {
         uint32_t raw[32];
         tmem_ld32_async(lane_base + o_col + cb, raw);
         tmem_wait_ld();
         tmem_reg_fence16(raw);
         tmem_reg_fence16(raw + 16);
-        if (r < rows) {
+#pragma unroll
+        for (int q = 0; q < 32; ++q) raw[q] = real ? __float_as_uint(__uint_as_float(raw[q]) * inv) : 0u;
+        if (cluster) {
 #pragma unroll
           for (int q = 0; q < 8; ++q)
-            __stcg((float4*)(part + cb + 4 * q),
-                   real ? make_float4(__uint_as_float(raw[4 * q]) * inv, __uint_as_float(raw[4 * q + 1]) * inv,
-                                      __uint_as_float(raw[4 * q + 2]) * inv, __uint_as_float(raw[4 * q + 3]) * inv)
-                        : make_float4(0.f, 0.f, 0.f, 0.f));
+            sts_u4(k0 + (uint32_t)r * XR + 4u * (cb + 4 * q), make_uint4(raw[4 * q], raw[4 * q + 1], raw[4 * q + 2], raw[4 * q + 3]));
+        } else if (r < rows) {
+          uint4* part = (uint4*)(a.part + ((unit * a.splits + split) * BM + r) * HDP + cb);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) __stcg(part + q, make_uint4(raw[4 * q], raw[4 * q + 1], raw[4 * q + 2], raw[4 * q + 3]));
         }
       }
-      if (hf == 0) __stcg(a.part_ml + at * BM + r, make_float2(m_out, l_out));
-      __threadfence();
-      // the splits' partials joined in their order: up to 8 splits are a cluster, each of
-      // which joins a share of the rows once all have stored; of more, the last to arrive
-      // joins all rows
       int ra = 0, rb = rows;
-      if (a.splits <= kTcCluster) {
+      if (cluster) {
+        pair_bar();   // (both halves have read the sums)
+        if (hf == 0) xm[r] = make_float2(m_out, l_out);
         cluster_sync();   // (the other roles arrive below)
         const int share = (rows + a.splits - 1) / a.splits;
         ra = split * share;
         rb = min(rows, ra + share);
       } else {
+        if (hf == 0) __stcg(a.part_ml + (unit * a.splits + split) * BM + r, make_float2(m_out, l_out));
+        __threadfence();
         asm volatile("bar.sync 5, 256;" ::: "memory");
         if (threadIdx.x == 0) *last_flag = atomicInc(a.arrived + unit, (unsigned)a.splits - 1u) == (unsigned)a.splits - 1u;
         asm volatile("bar.sync 5, 256;" ::: "memory");
         if (!*last_flag) rb = 0;
+        __threadfence();
       }
-      __threadfence();
-      {
-        const bool wide = ((uintptr_t)a.out | (uintptr_t)(a.out_robot * 2) | (uintptr_t)(a.out_token * 2)) % 16 == 0;
+      const bool wide = ((uintptr_t)a.out | (uintptr_t)(a.out_robot * 2) | (uintptr_t)(a.out_token * 2)) % 16 == 0;
+      // the splits' weights per row, [splits][128], into Q's place (every S has completed)
+      // or, where they may be many, the rings' ...
+      float* wts = (float*)(smem + (cluster ? 0 : NB * QB));
+      for (int rr = ra + threadIdx.x; rr < rb; rr += 256) {
+        const uint32_t xml = smem_u32(xm) + 8u * rr;
+        const float2* ml = a.part_ml + unit * a.splits * BM + rr;
+        float M = -INFINITY, S = 0.f;
+        for (int q = 0; q < a.splits; ++q)
+          M = fmaxf(M, cluster ? ld_cluster_f2(mapa_shared(xml, (uint32_t)q)).x : __ldcg(ml + q * BM).x);
+        for (int q = 0; q < a.splits; ++q) {
+          const float2 x = cluster ? ld_cluster_f2(mapa_shared(xml, (uint32_t)q)) : __ldcg(ml + q * BM);
+          const float wt = x.y != x.y ? x.y : (x.x == -INFINITY ? 0.f : exp2f(x.x - M) * x.y);
+          wts[q * BM + rr] = wt;
+          S += wt;
+        }
+        const float si = !(S <= 0.f) ? 1.f / S : 0.f;
+        for (int q = 0; q < a.splits; ++q) wts[q * BM + rr] *= si;
+        if (a.mass) a.row_ml[head * a.n * a.G + r0 + rr] = row_weight(M, S, kTcShift);
+      }
+      asm volatile("bar.sync 5, 256;" ::: "memory");
+      // ... then a warp per row
+      if (8 * lane < L.hd) {
+#pragma unroll 2
         for (int rr = ra + warp; rr < rb; rr += 8) {
-          const float2* ml = a.part_ml + unit * a.splits * BM + rr;
           const float* p0 = a.part + (unit * a.splits * BM + rr) * HDP + 8 * lane;
-          const bool on = 8 * lane < L.hd;
-          float M = -INFINITY, S = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-          for (int q = 0; q < a.splits; ++q) M = fmaxf(M, __ldcg(ml + q * BM).x);
-  #pragma unroll 4
+          float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
           for (int q = 0; q < a.splits; ++q) {
-            const float2 x = __ldcg(ml + q * BM);
-            const float wt = x.y != x.y ? x.y : (x.x == -INFINITY ? 0.f : exp2f(x.x - M) * x.y);
-            S += wt;
-            if (on) {
+            const float wt = wts[q * BM + rr];
+            float4 y0, y1;
+            if (cluster) {
+              const uint32_t at = mapa_shared(k0 + (uint32_t)rr * XR + 32u * lane, (uint32_t)q);
+              y0 = ld_cluster_f4(at);
+              y1 = ld_cluster_f4(at + 16);
+            } else {
               const float4* y = (const float4*)(p0 + (size_t)q * BM * HDP);
-              const float4 y0 = __ldcg(y), y1 = __ldcg(y + 1);
-              acc[0] = fmaf(wt, y0.x, acc[0]);
-              acc[1] = fmaf(wt, y0.y, acc[1]);
-              acc[2] = fmaf(wt, y0.z, acc[2]);
-              acc[3] = fmaf(wt, y0.w, acc[3]);
-              acc[4] = fmaf(wt, y1.x, acc[4]);
-              acc[5] = fmaf(wt, y1.y, acc[5]);
-              acc[6] = fmaf(wt, y1.z, acc[6]);
-              acc[7] = fmaf(wt, y1.w, acc[7]);
+              y0 = __ldcg(y);
+              y1 = __ldcg(y + 1);
             }
+            acc[0] = fmaf(wt, y0.x, acc[0]);
+            acc[1] = fmaf(wt, y0.y, acc[1]);
+            acc[2] = fmaf(wt, y0.z, acc[2]);
+            acc[3] = fmaf(wt, y0.w, acc[3]);
+            acc[4] = fmaf(wt, y1.x, acc[4]);
+            acc[5] = fmaf(wt, y1.y, acc[5]);
+            acc[6] = fmaf(wt, y1.z, acc[6]);
+            acc[7] = fmaf(wt, y1.w, acc[7]);
           }
-          const float si = !(S <= 0.f) ? 1.f / S : 0.f;
-          if (a.mass && lane == 0) a.row_ml[head * a.n * a.G + r0 + rr] = row_weight(M, S, kTcShift);
-          if (on)
-            store_bf16x8(out_row(r0 + rr) + 8 * lane,
-                         make_uint4(pack_bf16x2(acc[0] * si, acc[1] * si), pack_bf16x2(acc[2] * si, acc[3] * si),
-                                    pack_bf16x2(acc[4] * si, acc[5] * si), pack_bf16x2(acc[6] * si, acc[7] * si)),
-                         wide);
+          store_bf16x8(out_row(r0 + rr) + 8 * lane,
+                       make_uint4(pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3]), pack_bf16x2(acc[4], acc[5]),
+                                  pack_bf16x2(acc[6], acc[7])),
+                       wide);
         }
       }
+      if (cluster) cluster_sync();   // nobody leaves while its rows are read
     }
   }
-  if (warp >= 8 && a.splits > 1 && a.splits <= kTcCluster) cluster_sync();
+  if (warp >= 8 && a.splits > 1 && a.splits <= kTcCluster) {
+    cluster_sync();
+    cluster_sync();
+  }
   tc_fence_before();
   cta_sync();
-  if (*abort_flag && threadIdx.x == 0) raise_error(a.err, ERR_TIMEOUT);
+  if (*abort_flag && threadIdx.x == 0) {
+    // loads still on their way, at most the last CS, land before the shared memory goes away
+    for (int q = 0; q < 2; ++q)
+      for (int i = max(0, c_issued[q] - CS); i < c_issued[q]; ++i) mbar_wait(&c_full[q * CS + i % CS], (uint32_t)(i / CS) & 1u);
+    raise_error(a.err, ERR_TIMEOUT);
+  }
   if (warp == 16)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+}
+
+PFN_cuTensorMapEncodeTiled_v12000 g_enc = nullptr;
+
+cudaError_t encode_codes(CUtensorMap* m, const uint8_t* base, const CacheLayer& c, int batch) {
+  cuuint64_t dims[2] = {(cuuint64_t)c.hdp, (cuuint64_t)batch * c.Hkv * c.T};
+  cuuint64_t strides[1] = {(cuuint64_t)c.hdp};
+  cuuint32_t box[2] = {64u, 64u}, estr[2] = {1, 1};
+  const CUresult r = g_enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(base), dims, strides, box, estr,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
 template <int NB>
@@ -630,15 +681,39 @@ cudaError_t launch_nb(CacheAttnArgs a, cudaStream_t st) {
   const long long tiles = (long long)a.row_tiles * a.c.Hkv * a.batch;
   long long seen = a.max_length;
   if (a.window > 0) seen = std::min(seen, (long long)a.window + a.sinks + BM / a.G + 1 + 2 * BT);
-  const long long units = (seen + BT - 1) / BT;
-  a.splits = (int)std::max(1ll, std::min((long long)a.num_sms / tiles, units));
+  const int units = (int)((seen + BT - 1) / BT);
+  // As many splits as the SMs hold, as a cluster if that many clusters fit on the
+  // device at once, and no more than shorten the longest one.
+  int splits = (int)std::max(1ll, std::min(std::min((long long)a.num_sms / tiles, (long long)units), 256ll));
+  if (splits <= kTcCluster)
+    while (splits > 1 && a.clusters[splits] < tiles) --splits;
+  if (splits > 1) splits = (units + (units + splits - 1) / splits - 1) / ((units + splits - 1) / splits);
+  a.splits = splits;
+  TcMaps maps;
+  cudaError_t e = encode_codes(&maps.k, a.c.k, a.c, a.batch);
+  if (e == cudaSuccess) e = encode_codes(&maps.v, a.c.v, a.c, a.batch);
+  if (e != cudaSuccess) return e;
   return launch_kernel_cluster(cache_tc_kernel<NB>, dim3(a.row_tiles * a.splits, a.c.Hkv, a.batch), dim3(TCT),
-                               TcShape<NB>::bytes, st, dim3(a.splits <= kTcCluster ? a.splits : 1, 1, 1), a);
+                               TcShape<NB>::bytes, st, dim3(a.splits <= kTcCluster ? a.splits : 1, 1, 1), maps, a);
 }
 
 template <int NB>
-cudaError_t init_nb() {
-  return cudaFuncSetAttribute(cache_tc_kernel<NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcShape<NB>::bytes);
+cudaError_t init_nb(int* clusters) {
+  cudaError_t e = cudaFuncSetAttribute(cache_tc_kernel<NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcShape<NB>::bytes);
+  for (int s = 2; s <= kTcCluster && e == cudaSuccess; ++s) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr;
+    cfg.gridDim = dim3(s);
+    cfg.blockDim = dim3(TCT);
+    cfg.dynamicSmemBytes = TcShape<NB>::bytes;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = s;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    e = cudaOccupancyMaxActiveClusters(&clusters[s], cache_tc_kernel<NB>, &cfg);
+  }
+  return e;
 }
 
 }  // namespace
@@ -652,12 +727,21 @@ cudaError_t launch_cache_attend_tc(const CacheAttnArgs& a, cudaStream_t st) {
   }
 }
 
-cudaError_t init_cache_tc_kernels() {
-  cudaError_t e = init_nb<1>();
-  if (e == cudaSuccess) e = init_nb<2>();
-  if (e == cudaSuccess) e = init_nb<3>();
-  if (e == cudaSuccess) e = init_nb<4>();
-  return e;
+cudaError_t init_cache_tc_kernels(int hdp, int* clusters) {
+  if (!g_enc) {
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q);
+    if (e != cudaSuccess) return e;
+    if (q != cudaDriverEntryPointSuccess || !fn) return cudaErrorSymbolNotFound;
+    g_enc = (PFN_cuTensorMapEncodeTiled_v12000)fn;
+  }
+  switch (hdp) {
+    case 64: return init_nb<1>(clusters);
+    case 128: return init_nb<2>(clusters);
+    case 192: return init_nb<3>(clusters);
+    default: return init_nb<4>(clusters);
+  }
 }
 
 }  // namespace ravel

@@ -18,7 +18,7 @@ struct ravel_cache_ctx {
   ravel_cache_config cfg{};
   Dtype dt = DT_F32;
   size_t esize = 4;
-  int device = 0, num_sms = 0;
+  int device = 0, num_sms = 0, clusters[9] = {};
   int hdp = 0, T = 0;            // held row bytes; capacity rounded up
   size_t rows = 0, blocks = 0;   // per layer: bytes of K (or V), exponents
   uint8_t *k = nullptr, *v = nullptr;
@@ -79,7 +79,9 @@ const char* config_fault(const ravel_cache_config& c) {
   if (c.head_dim < 8 || c.head_dim % 8 || c.head_dim > 256) return "head_dim must be a multiple of 8, at most 256";
   if (c.dtype != RAVEL_FP32 && c.dtype != RAVEL_BF16) return "unknown dtype";
   if (c.n_kv_heads > 65535 || c.max_batch > 65535) return "at most 65535 KV heads and robots";
-  if (c.max_tokens > (1 << 30)) return "max_tokens must be at most 2^30";
+  // (rows of a layer are counted in 32 bits; the product of three 32-bit sizes could pass 64)
+  if ((double)c.max_batch * c.n_kv_heads * ((double)c.max_tokens + kCacheRound) > 2147483647.0)
+    return "max_batch * n_kv_heads * max_tokens must be below 2^31";
   if ((long long)c.max_queries * c.n_q_heads > (1 << 30)) return "max_queries * n_q_heads must be at most 2^30";
   return nullptr;
 }
@@ -144,7 +146,7 @@ ravel_status ravel_cache_create(const ravel_cache_config* cfg, int device, ravel
     if (e == cudaSuccess) e = cudaHostGetDevicePointer((void**)&w.mirror, c->err_host, 0);
     if (e == cudaSuccess) e = cudaMemcpy(c->err, &w, sizeof w, cudaMemcpyHostToDevice);
     if (e == cudaSuccess) e = init_cache_kernels();
-    if (e == cudaSuccess) e = init_cache_tc_kernels();
+    if (e == cudaSuccess) e = init_cache_tc_kernels(c->hdp, c->clusters);
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
   }
   if (e != cudaSuccess) {
@@ -233,6 +235,7 @@ ravel_status ravel_cache_attend(ravel_cache_t* c, int layer, int batch, int n, c
   a.mass_add = mass_add;
   a.vec = aligned16(q, q_robot_stride, q_token_stride, c->esize);
   a.num_sms = c->num_sms;
+  a.clusters = c->clusters;
   a.part = c->part;
   a.part_ml = c->part_ml;
   a.arrived = c->arrived;
