@@ -77,6 +77,7 @@ struct CacheAttnArgs {
   int* err;
   // chosen by the launcher
   int row_tiles, splits;
+  int group;                // tensor cores: (robot, KV head) pairs walked together
 };
 constexpr int kCacheSplitCtas = 608;   // row tiles (of 16) x splits of a launch that splits the tokens
 constexpr int kCacheTcRows = 128;      // rows of a tile on the tensor cores: at most one such tile x split per SM

@@ -1,26 +1,29 @@
 // Attention over the 8-bit context cache for many query rows (an expert's slots,
 // prompts), bf16, on the 5th-generation tensor cores.
 //
-// A CTA owns 128 rows (row r = query * G + head of the group) of one (robot, KV
-// head) and a share (split) of the 128-token tiles that they see:
+// An item is 128 rows (row r = query * G + head of the group) of one (robot, KV
+// head) and a share (split) of the 128-token tiles that they see; CTAs, one per SM,
+// walk the items of their launch:
 //   S = Q K^T        tcgen05.mma kind::f16, M = 128, N = 128, into TMEM
 //   P = 2^(S - m)    softmax warps: TMEM -> registers -> f16 P over S in TMEM
 //   O += P V         tcgen05.mma, M = 128, N = head dim, 16 tokens at a time
-// Warp roles (640 threads): warps 0-7 Q, softmax and epilogue, two threads per row;
-// warps 8-11 widen K, warps 12-15 widen V; warp 16 TMEM and MMAs; warps 17, 18 load
-// the codes of K and V (19 idle, so that registers move between whole warpgroups).
+// Warp roles (640 threads): warps 0-7 softmax and output, two threads per row; warps
+// 8-11 widen K and lay out Q, warps 12-15 widen V; warp 16 TMEM and MMAs; warps 17, 18
+// load the codes of K and V (19 idle, so that registers move between whole
+// warpgroups).  Every role walks the items on its own, so that one item's output
+// lies beside the next one's Q, K and first scores.
 //
 // The codes come by TMA and are widened in shared memory to f16 (e4m3 -> f16 is
 // exact), into the 128-byte swizzled layout that a TMA load of f16 rows would
 // leave: K in units of 64 head dims (16 KB), V in halves of 64 tokens, each in
 // rings of its own with its own warps, so that neither waits for the other's
 // slots.  (With the codes loaded to registers by the widening warps themselves a
-// unit took a load's latency, 900 cycles of the 512 that the MMAs of four units
-// leave each: the proxy fence that ends a unit waits for the loads in flight.)
-// Feeding the codes as kind::f8f6f4
-// operands instead would need Q and P in 8 bits too: two pieces of each keep
-// bf16's precision and cost what one f16 MMA does, but 2^-9 is the least P that
-// e4m3 holds, and a long flat tail of smaller ones carries weight.
+// unit took a load's latency, 900 cycles where the MMAs of one take 512: the proxy
+// fence that ends a unit waits for the loads in flight.)
+// Feeding the codes as kind::f8f6f4 operands instead would need Q and P in 8 bits
+// too: two pieces of each keep bf16's precision and cost what one f16 MMA does, but
+// 2^-9 is the least P that e4m3 holds, and a long flat tail of smaller ones carries
+// weight.
 //
 // Numbers as in the kernel for few rows: q in f16 under a power of two per row
 // (exact for bf16), block exponents of K on the scores, those of V on P.  P is at
@@ -42,7 +45,7 @@ constexpr int TCT = 640;
 constexpr int BM = 128, BT = 128;              // rows, tokens of a tile
 constexpr uint32_t QB = BM * 128;              // bytes of a 64-dim block of Q
 constexpr uint32_t KU = BT * 128;              // bytes of a K unit: 128 tokens x 64 dims
-constexpr uint32_t CB = 64 * 64;                // bytes of a slot of codes: 64 tokens x 64 dims
+constexpr uint32_t CB = 64 * 64;               // bytes of a slot of codes: 64 tokens x 64 dims
 constexpr uint32_t VB = 64 * 128;              // bytes of a 64-dim block of a V half
 constexpr float kTcShift = 7.f;                // P's largest value is 2^kTcShift (times 2^8 while lazy)
 constexpr int kTcCluster = 8;                  // splits that are a cluster
@@ -50,16 +53,18 @@ constexpr uint32_t kPolls = 1u << 25;          // polls without progress: second
 
 template <int NB> struct TcShape {
   // shared memory at NB blocks of 64 head dims: Q, the rings of widened K units and V
-  // halves, the rings of codes, barriers and row data
-  static constexpr int KS = 4;
-  static constexpr int VS = NB >= 3 ? 2 : 4;
-  // a multiple of the 4 warps that widen them: each slot is then waited for by one warp, in
-  // order.  (Loads may complete out of order; a warp that waits for a slot's next phase while
-  // another's load into it is still on its way would take the phase before for it.)
-  static constexpr int CS = NB == 4 ? 4 : 8;
-  static_assert(CS % 4 == 0, "widening warps");
-  static constexpr uint32_t ring = KS * KU + VS * NB * VB + 2 * CS * CB;
-  static constexpr uint32_t bytes = NB * QB + ring + 3072;
+  // halves, the rings of codes, the output's staging, barriers and row data
+  static constexpr int KS = NB == 4 ? 2 : (NB == 3 ? 3 : 4);
+  static constexpr int VS = NB >= 3 ? 2 : (NB == 2 ? 3 : 4);
+  // codes: multiples of the 4 warps that widen them: each slot is then waited for by one
+  // warp, in order.  (Loads may complete out of order; a warp that waits for a slot's next
+  // phase while another's load into it is still on its way would take the phase before for
+  // it.)
+  static constexpr int CK = 8, CV = NB == 4 ? 4 : 8;
+  static_assert(CK % 4 == 0 && CV % 4 == 0, "widening warps");
+  static constexpr uint32_t ring = KS * KU + VS * NB * VB + (CK + CV) * CB;
+  static constexpr uint32_t stage = 8 * 2048;   // 32 rows x 32 columns of bf16 per softmax warp
+  static constexpr uint32_t bytes = NB * QB + ring + stage + 3072;
   static_assert(bytes <= 227 * 1024, "shared memory");
   // a row of the fp32 output that splits exchange (over the rings): 16 bytes more than
   // the dims, so that rows written by neighbouring lanes fall on different banks
@@ -79,42 +84,7 @@ __device__ __forceinline__ uint32_t idesc_f16(int m, int n) {
 __device__ __forceinline__ void sts_u4(uint32_t a, uint4 v) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
-
-// 16 codes -> two 16-byte pieces of f16
-__device__ __forceinline__ void widen(uint4 w, uint32_t lo, uint32_t hi) {
-  sts_u4(lo, make_uint4(e4m3_lo(w.x), e4m3_hi(w.x), e4m3_lo(w.y), e4m3_hi(w.y)));
-  sts_u4(hi, make_uint4(e4m3_lo(w.z), e4m3_hi(w.z), e4m3_lo(w.w), e4m3_hi(w.w)));
-}
-
-// Registers of a warpgroup: launched with 96 each (640 x 96 = 61440); softmax
-// 2 x 128 x 144, widening 2 x 128 x 80, the rest 128 x 24: 60416.
-template <int N>
-__device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N>
-__device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-
-__device__ __forceinline__ void store_bf16x8(bf16* dst, uint4 w, bool wide) {
-  if (wide) {
-    *(uint4*)dst = w;
-  } else {
-    bf16 y[8];
-    memcpy(y, &w, 16);
-#pragma unroll
-    for (int z = 0; z < 8; ++z) dst[z] = y[z];
-  }
-}
-
-// eight bf16 at any alignment
-__device__ __noinline__ uint4 ldg_bf16x8(const bf16* p) {
-  bf16 y[8];
-#pragma unroll
-  for (int z = 0; z < 8; ++z) y[z] = p[z];
-  uint4 w;
-  memcpy(&w, y, 16);
-  return w;
-}
-
-__device__ __forceinline__ uint4 lds_codes(uint32_t a) {
+__device__ __forceinline__ uint4 lds_u4(uint32_t a) {
   uint4 v;
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
   return v;
@@ -130,6 +100,30 @@ __device__ __forceinline__ float2 ld_cluster_f2(uint32_t a) {
   return v;
 }
 
+// 16 codes -> two 16-byte pieces of f16
+__device__ __forceinline__ void widen(uint4 w, uint32_t lo, uint32_t hi) {
+  sts_u4(lo, make_uint4(e4m3_lo(w.x), e4m3_hi(w.x), e4m3_lo(w.y), e4m3_hi(w.y)));
+  sts_u4(hi, make_uint4(e4m3_lo(w.z), e4m3_hi(w.z), e4m3_lo(w.w), e4m3_hi(w.w)));
+}
+
+__device__ __forceinline__ void store_bf16x8(bf16* dst, uint4 w, bool wide) {
+  if (wide) {
+    *(uint4*)dst = w;
+  } else {
+    bf16 y[8];
+    memcpy(y, &w, 16);
+#pragma unroll
+    for (int z = 0; z < 8; ++z) dst[z] = y[z];
+  }
+}
+
+// Registers of a warpgroup: launched with 96 each (640 x 96 = 61440); softmax
+// 2 x 128 x 136, widening 2 x 128 x 80, the rest 128 x 48: 61440.
+template <int N>
+__device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
 // A warp's writes to shared memory become visible to the tensor core: one arrival per warp.
 __device__ __forceinline__ void written(uint64_t* bar) {
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -137,76 +131,105 @@ __device__ __forceinline__ void written(uint64_t* bar) {
   if ((threadIdx.x & 31) == 0) mbar_arrive(bar);
 }
 
+// Item w of a launch: its (robot, KV head), row tile, split, and the tiles of tokens
+// that it walks.
+struct Item {
+  int head, b, h, tile, split;
+  Sight s;
+  bool ok, live;     // the robot's numbers are in range; some row sees something
+  int t0, n;         // tiles t0 .. t0 + n - 1 of the sight's units
+  int hi;            // tokens from here on are nobody's
+  __device__ __forceinline__ int token(int i) const {
+    const int t = t0 + i;
+    return (t < s.sink_units ? t : t - s.sink_units + s.from) * BT;
+  }
+  // tokens of tile i that exist for these rows, in groups of 16
+  __device__ __forceinline__ int groups(int i) const { return (min(BT, hi - token(i)) + 15) >> 4; }
+  __device__ __forceinline__ int halves() const { return n == 0 ? 0 : 2 * n - (groups(n - 1) > 4 ? 0 : 1); }
+};
+
+// Items are ordered by groups of a.group (robot, KV head) pairs whose caches stay in L2
+// together, within a group by row tile from the last one on (causal: the longest first,
+// so that the CTAs' shares even out), then by split.
+__device__ __forceinline__ Item item_of(const CacheAttnArgs& a, int w) {
+  Item it;
+  const uint32_t x = (uint32_t)w / (uint32_t)a.splits, per = (uint32_t)(a.group * a.row_tiles);
+  it.split = w - (int)x * a.splits;
+  const uint32_t gi = x / per, rem = x - gi * per;
+  const uint32_t pairs = (uint32_t)min(a.group, a.batch * a.c.Hkv - (int)gi * a.group), row = rem / pairs;
+  it.tile = a.row_tiles - 1 - (int)row;
+  it.head = (int)(gi * a.group + rem - row * pairs);
+  it.b = (int)((uint32_t)it.head / (uint32_t)a.c.Hkv);
+  it.h = it.head - it.b * a.c.Hkv;
+  it.ok = robot_sight(a, it.b, it.s);
+  it.live = it.tile * BM < it.s.count * a.G && it.s.len > 0;
+  it.t0 = it.n = it.hi = 0;
+  if (it.live) {
+    tile_sight(a, it.s, it.tile * BM, it.tile * BM + BM - 1, BT);
+    it.hi = row_mask(a, it.s, min(it.tile * BM + BM, it.s.count * a.G) - 1).hi;
+    it.t0 = (int)((long long)it.s.units * it.split / a.splits);
+    it.n = (int)((long long)it.s.units * (it.split + 1) / a.splits) - it.t0;
+  }
+  return it;
+}
+
 template <int NB>
 __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant__ TcMaps maps, CacheAttnArgs a) {
-  constexpr int HDP = 64 * NB, KS = TcShape<NB>::KS, VS = TcShape<NB>::VS, CS = TcShape<NB>::CS;
+  using Shape = TcShape<NB>;
+  constexpr int HDP = 64 * NB, KS = Shape::KS, VS = Shape::VS, CK = Shape::CK, CV = Shape::CV;
   constexpr uint32_t VH = NB * VB;   // bytes of a V half
   extern __shared__ __align__(1024) uint8_t smem[];
-  const uint32_t q0 = smem_u32(smem), k0 = q0 + NB * QB, v0 = k0 + KS * KU, ck0 = v0 + VS * VH, cv0 = ck0 + CS * CB;
-  uint8_t* tail = smem + NB * QB + TcShape<NB>::ring;
+  const uint32_t q0 = smem_u32(smem), k0 = q0 + NB * QB, v0 = k0 + KS * KU, ck0 = v0 + VS * VH, cv0 = ck0 + CK * CB,
+                 st0 = cv0 + CV * CB;
+  uint8_t* tail = smem + NB * QB + Shape::ring + Shape::stage;
   uint64_t* k_full = (uint64_t*)tail;
   uint64_t* k_empty = k_full + KS;
   uint64_t* v_full = k_empty + KS;
   uint64_t* v_empty = v_full + VS;
-  uint64_t* c_full = v_empty + VS;   // [2 CS] codes of K, then of V
-  uint64_t* c_empty = c_full + 2 * CS;
-  uint64_t* s_full = c_empty + 2 * CS;   // [2]
-  uint64_t* p_full = s_full + 2;     // [2]
-  uint64_t* pv_done = p_full + 2;    // [2]
-  uint64_t* q_full = pv_done + 2;
-  uint64_t* ended = q_full + 1;
+  uint64_t* ck_full = v_empty + VS;
+  uint64_t* ck_empty = ck_full + CK;
+  uint64_t* cv_full = ck_empty + CK;
+  uint64_t* cv_empty = cv_full + CV;
+  uint64_t* s_full = cv_empty + CV;   // [2]
+  uint64_t* p_full = s_full + 2;      // [2]
+  uint64_t* pv_done = p_full + 2;     // [2]
+  uint64_t* q_full = pv_done + 2;     // an item's Q is laid out ...
+  uint64_t* q_empty = q_full + 1;     // ... and its last S has completed
+  uint64_t* o_free = q_empty + 1;     // an item's output has been read
+  uint64_t* ended = o_free + 1;
   uint32_t* tmem_slot = (uint32_t*)(ended + 1);
   int* abort_flag = (int*)(tmem_slot + 1);
   int* last_flag = abort_flag + 1;
-  int* c_issued = last_flag + 1;     // [2] loads of codes issued, K and V
-  uint32_t* row_top = (uint32_t*)(tail + 512);    // [128] bits of the rows' largest |q|
+  int* c_issued = last_flag + 1;                  // [2] loads of codes issued, K and V
+  // exponent bits of the rows' largest |q|, [4][128], by item: S runs up to two tiles, so up
+  // to two items, ahead of the softmax, and Q one more
+  uint8_t* row_exp = tail + 512;
   float2* xm = (float2*)(tail + 1024);            // [2][128] row maxima, then sums, of the two halves
-  static_assert((2 * KS + 2 * VS + 4 * CS + 8) * 8 + 20 <= 512, "barriers");
+  static_assert((2 * KS + 2 * VS + 2 * CK + 2 * CV + 10) * 8 + 20 <= 512, "barriers");
 
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-  const int b = blockIdx.z, h = blockIdx.y, split = blockIdx.x % a.splits;
-  const int tile = a.row_tiles - 1 - (int)blockIdx.x / a.splits;   // (causal: the longest first)
   const CacheLayer& L = a.c;
-  const int r0 = tile * BM, rows = min(BM, a.n * a.G - r0);
-  const size_t head = (size_t)b * L.Hkv + h;
-  Sight s;
+  const int items = a.row_tiles * a.splits * L.Hkv * a.batch;
   if (q0 & 1023u) {   // (the swizzled layouts count on it)
     if (threadIdx.x == 0) raise_error(a.err, ERR_SHAPE);
     return;
   }
-  if (!robot_sight(a, b, s) && threadIdx.x == 0 && blockIdx.x == 0 && h == 0) raise_error(a.err, ERR_SHAPE);
-  bf16* out0 = (bf16*)a.out + (size_t)((long long)b * a.out_robot) + (size_t)h * a.G * L.hd;
-  auto out_row = [&](int r) {
-    const uint32_t i = (uint32_t)r / (uint32_t)a.G;
-    return out0 + (size_t)((long long)i * a.out_token) + (size_t)((uint32_t)r - i * (uint32_t)a.G) * L.hd;
-  };
-  if (r0 >= s.count * a.G || s.len == 0) {   // nothing to see: zeros
-    if (split == 0)
-      for (int w = threadIdx.x; w < rows * L.hd; w += TCT) out_row(r0 + w / L.hd)[w % L.hd] = __float2bfloat16_rn(0.f);
-    if (split == 0 && a.mass && threadIdx.x < rows)
-      a.row_ml[head * a.n * a.G + r0 + threadIdx.x] = make_float2(0.f, 0.f);
-    return;
-  }
-  tile_sight(a, s, r0, r0 + BM - 1, BT);
-  const int t0 = (int)((long long)s.units * split / a.splits), t1 = (int)((long long)s.units * (split + 1) / a.splits);
-  const int n = t1 - t0;
-  const RowMask firstm = row_mask(a, s, r0), lastm = row_mask(a, s, min(r0 + BM, s.count * a.G) - 1);
-  // first token of tile t, and how many of its tokens exist for these rows
-  auto tile_token = [&](int t) { return (t < s.sink_units ? t : t - s.sink_units + s.from) * BT; };
-  auto keys_of = [&](int j0) { return min(BT, lastm.hi - j0); };
-
   if (threadIdx.x == 0) {
     for (int i = 0; i < KS; ++i) {
-      mbar_init(&k_full[i], 2);   // its steps
+      mbar_init(&k_full[i], 2);   // the steps of a unit
       mbar_init(&k_empty[i], 1);
     }
     for (int i = 0; i < VS; ++i) {
-      mbar_init(&v_full[i], NB);
+      mbar_init(&v_full[i], NB);   // ... of a half
       mbar_init(&v_empty[i], 1);
     }
-    for (int i = 0; i < 2 * CS; ++i) {
-      mbar_init(&c_full[i], 1);
-      mbar_init(&c_empty[i], 1);
+    for (int i = 0; i < CK; ++i) {
+      mbar_init(&ck_full[i], 1);
+      mbar_init(&ck_empty[i], 1);
+    }
+    for (int i = 0; i < CV; ++i) {
+      mbar_init(&cv_full[i], 1);
+      mbar_init(&cv_empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
       c_issued[i] = 0;
@@ -214,7 +237,9 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
       mbar_init(&p_full[i], 256);
       mbar_init(&pv_done[i], 1);
     }
-    mbar_init(q_full, 8);
+    mbar_init(q_full, 4);
+    mbar_init(q_empty, 1);
+    mbar_init(o_free, 8);
     mbar_init(ended, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -223,22 +248,6 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
-  // Q: rows of 8 NB lanes with 8 dims each, 16 rows per softmax warp; on their way while
-  // TMEM and barriers are set up
-  constexpr int LPR = 8 * NB, RPW = 32 / LPR, PASS = 16 / RPW;
-  const int q_sub = lane / LPR, q_dl = lane % LPR;
-  uint4 qx[PASS];
-  if (warp < 8) {
-    const bool on = q_sub < RPW && 8 * q_dl < L.hd;
-    const bf16* base = (const bf16*)a.q + (size_t)((long long)b * a.q_robot) + (size_t)h * a.G * L.hd + 8 * q_dl;
-#pragma unroll
-    for (int p = 0; p < PASS; ++p) {
-      const uint32_t r = (uint32_t)(r0 + warp * 16 + p * RPW + q_sub), i = r / (uint32_t)a.G;
-      const bf16* at = base + (size_t)((long long)i * a.q_token) + (size_t)(r - i * a.G) * L.hd;
-      qx[p] = make_uint4(0u, 0u, 0u, 0u);
-      if (on && (int)i < s.count) qx[p] = a.vec ? __ldg((const uint4*)at) : ldg_bf16x8(at);
-    }
   }
   tc_fence_before();
   cta_sync();
@@ -256,124 +265,220 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
     // lane: 16 codes at dim 16 (lane % 4) of rows lane / 4, lane / 4 + 8, ...
     const uint32_t sw = (uint32_t)(lane >> 2), row = (uint32_t)(lane >> 2) * 128u;
     const uint32_t lo = row + ((((uint32_t)lane & 3u) * 2u) ^ sw) * 16u, hi = row + ((((uint32_t)lane & 3u) * 2u + 1u) ^ sw) * 16u;
-    const uint32_t codes = (is_k ? ck0 : cv0) + 16u * lane;
-    uint64_t *cf = c_full + (is_k ? 0 : CS), *ce = c_empty + (is_k ? 0 : CS);
-    // a unit of K takes 2 steps, a half of V NB; every tile but the last has two halves
-    const int per = is_k ? 2 : NB, ring = is_k ? KS : VS;
-    const int steps = is_k ? n * NB * 2 : (n > 0 ? (2 * n - (keys_of(tile_token(t1 - 1)) > 64 ? 0 : 1)) * NB : 0);
-    const uint32_t to0 = (is_k ? k0 : v0), slot_bytes = is_k ? KU : VH;
+    uint64_t *cf = is_k ? ck_full : cv_full, *ce = is_k ? ck_empty : cv_empty;
     uint64_t *full = is_k ? k_full : v_full, *empty = is_k ? k_empty : v_empty;
+    const uint32_t codes = (is_k ? ck0 : cv0) + 16u * lane, to0 = is_k ? k0 : v0, slot_bytes = is_k ? KU : VH;
+    const int per = is_k ? 2 : NB, ring = is_k ? KS : VS, cring = is_k ? CK : CV;
+    int u = warp & 3, end = 0, qi = 0;   // this warp's next step, the steps so far, the items with Q so far
     bool ok = true;
-    for (int u = warp & 3; u < steps; u += 4) {
-      const int cs = u % CS, item = u / per, slot = item % ring;
-      ok = mbar_wait_warp(&cf[cs], (uint32_t)(u / CS) & 1u);
-      if (!ok) break;
-      uint4 x[8];
+    for (int w = blockIdx.x; ok && w < items; w += gridDim.x) {
+      const Item it = item_of(a, w);
+      if (it.n == 0) continue;
+      if (is_k) {
+        // Q, scaled by the rows' powers of two: 32 rows per warp, 8 NB lanes with 8 dims each
+        // to a row; a batch of loads is on its way while the Q before is still in use
+        constexpr int LPR = 8 * NB, RPW = 32 / LPR, PASS = 32 / RPW;
+        const int sub = lane / LPR, dl = lane % LPR;
+        const bool on = sub < RPW && 8 * dl < L.hd;
+        const bf16* base = (const bf16*)a.q + (size_t)((long long)it.b * a.q_robot) + (size_t)it.h * a.G * L.hd + 8 * dl;
+#pragma unroll 1
+        for (int p0 = 0; p0 < PASS; p0 += 8) {
+          uint4 x[8];
 #pragma unroll
-      for (int y = 0; y < 8; ++y) x[y] = lds_codes(codes + (uint32_t)cs * CB + 512u * y);
-      ok = mbar_wait_warp(&empty[slot], ((uint32_t)(item / ring) & 1u) ^ 1u);
-      if (!ok) break;
-      __syncwarp();   // every lane has its codes
-      if (lane == 0) mbar_arrive(&ce[cs]);
-      const uint32_t to = to0 + (uint32_t)slot * slot_bytes + (uint32_t)(u % per) * VB;
+          for (int p = 0; p < 8; ++p) {
+            const uint32_t r = (uint32_t)(it.tile * BM + (warp - 8) * 32 + (p0 + p) * RPW + sub), i = r / (uint32_t)a.G;
+            const bf16* at = base + (size_t)((long long)i * a.q_token) + (size_t)(r - i * a.G) * L.hd;
+            x[p] = make_uint4(0u, 0u, 0u, 0u);
+            if (on && (int)i < it.s.count) {
+              if (a.vec) {
+                x[p] = __ldg((const uint4*)at);
+              } else {
+                bf16 y[8];
 #pragma unroll
-      for (int y = 0; y < 8; ++y) widen(x[y], to + lo + 1024u * y, to + hi + 1024u * y);
-      written(&full[slot]);
+                for (int z = 0; z < 8; ++z) y[z] = at[z];
+                memcpy(&x[p], y, 16);
+              }
+            }
+          }
+          if (p0 == 0 && qi > 0) {
+            ok = mbar_wait_warp(q_empty, (uint32_t)(qi - 1) & 1u);
+            if (!ok) break;
+          }
+#pragma unroll
+          for (int p = 0; p < 8; ++p) {
+            const uint32_t y[4] = {x[p].x, x[p].y, x[p].z, x[p].w};
+            uint32_t top = 0u;   // bits of the largest magnitude: NaN counts as larger than all
+#pragma unroll
+            for (int z = 0; z < 4; ++z) top = max(top, max((y[z] & 0x7fffu) << 16, y[z] & 0x7fff0000u));
+            if (RPW == 1) {
+              top = __reduce_max_sync(0xffffffffu, top);
+            } else {
+#pragma unroll
+              for (int o = 1; o < LPR; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+            }
+            const float f = top >= 0x7f800000u ? __int_as_float(0x7fffffff) : exp2i(min(14 - ((int)(top >> 23) - 127), 126));
+            uint32_t o4[4];
+#pragma unroll
+            for (int z = 0; z < 4; ++z) o4[z] = pack_f16x2(__uint_as_float(y[z] << 16) * f, __uint_as_float(y[z] & 0xffff0000u) * f);
+            const int lr = (warp - 8) * 32 + (p0 + p) * RPW + sub;
+            if (sub < RPW) {
+              sts_u4(q0 + (uint32_t)(dl >> 3) * QB + (uint32_t)lr * 128u + (uint32_t)(((dl & 7) ^ (lr & 7)) * 16),
+                     make_uint4(o4[0], o4[1], o4[2], o4[3]));
+              if (dl == 0) row_exp[(qi & 3) * BM + lr] = (uint8_t)(top >> 23);
+            }
+          }
+        }
+        if (!ok) break;
+        written(q_full);
+        ++qi;
+      }
+      end += is_k ? it.n * NB * 2 : it.halves() * NB;
+      for (; u < end; u += 4) {
+        const int cs = u % cring, part = u / per, slot = part % ring;
+        ok = mbar_wait_warp(&cf[cs], (uint32_t)(u / cring) & 1u);
+        if (!ok) break;
+        uint4 x[8];
+#pragma unroll
+        for (int y = 0; y < 8; ++y) x[y] = lds_u4(codes + (uint32_t)cs * CB + 512u * y);
+        ok = mbar_wait_warp(&empty[slot], ((uint32_t)(part / ring) & 1u) ^ 1u);
+        if (!ok) break;
+        __syncwarp();   // every lane has its codes
+        if (lane == 0) mbar_arrive(&ce[cs]);
+        const uint32_t to = to0 + (uint32_t)slot * slot_bytes + (uint32_t)(u % per) * VB;
+#pragma unroll
+        for (int y = 0; y < 8; ++y) widen(x[y], to + lo + 1024u * y, to + hi + 1024u * y);
+        written(&full[slot]);
+      }
     }
     if (!ok && lane == 0) *abort_flag = 1;
   } else if (warp >= 16) {
-    regs_down<24>();
+    regs_down<48>();
     if (warp == 16) {
-    // ---- MMAs: S of the next tile as soon as its K is there, P V of the oldest whose P is
-    const uint32_t el = elect_one();
-    const uint32_t idesc_s = idesc_f16(BM, BT), idesc_o = idesc_f16(BM, HDP) | (1u << 16);
-    const uint64_t qd0 = sw128_desc(q0), kd0 = sw128_desc(k0), vd0 = sw128_mn_desc(v0, VB);
-    int ns = 0, i = 0, sk = 0, sv = 0;
-    uint32_t phk = 0, phv = 0, spins = 0;
-    bool ok = mbar_wait_warp(q_full, 0);
-    while (ok && i < n) {
-      bool progress = false;
-      if (ns < n && ns <= i + 1 && mbar_test_warp(&k_full[sk], phk)) {
-        const uint32_t sd = tmem + (uint32_t)(ns & 1) * BT;
-        uint64_t ad = qd0;
-#pragma unroll 1
-        for (int blk = 0; blk < NB; ++blk, ad += QB >> 4) {
-          if (blk) ok = mbar_wait_warp(&k_full[sk], phk);
-          if (!ok) break;
-          tc_fence_after();
-          const uint64_t bd = kd0 + (uint32_t)sk * (KU >> 4);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) umma_bf16(sd, ad + 2 * k, bd + 2 * k, idesc_s, (blk > 0 || k > 0) ? 1u : 0u, el);
-          umma_commit(&k_empty[sk], el);
-          if (++sk == KS) {
-            sk = 0;
-            phk ^= 1u;
-          }
+      // ---- MMAs: S of the next tile as soon as its K is there, P V of the oldest whose P is;
+      // S runs at most one tile ahead, into the next item where this one ends
+      const uint32_t el = elect_one();
+      const uint32_t idesc_s = idesc_f16(BM, BT), idesc_o = idesc_f16(BM, HDP) | (1u << 16);
+      const uint64_t qd0 = sw128_desc(q0), kd0 = sw128_desc(k0), vd0 = sw128_mn_desc(v0, VB);
+      // the next item with tiles from w on: its tiles, and the last one's groups of 16 tokens
+      auto next = [&](int& w, int& n, int& last) {
+        n = 0;
+        for (; w < items; w += gridDim.x) {
+          const Item it = item_of(a, w);
+          if (it.n == 0) continue;
+          n = it.n;
+          last = it.groups(n - 1);
+          w += gridDim.x;
+          return;
         }
-        if (!ok) break;
-        umma_commit(&s_full[ns & 1], el);
-        ++ns;
-        progress = true;
-      }
-      if (i < ns && mbar_test_warp(&p_full[i & 1], (uint32_t)(i >> 1) & 1u) && mbar_test_warp(&v_full[sv], phv)) {
-        const uint32_t pa = tmem + (uint32_t)(i & 1) * BT;
-        const int groups = (keys_of(tile_token(t0 + i)) + 15) >> 4;
+      };
+      int ws = blockIdx.x, wp = blockIdx.x;           // the cursors' next items
+      int sn = 0, pn = 0, s_last = 0, last = 0;       // tiles of S's and P V's items
+      int si = 0, pi = 0, sq = 0, pq = 0;             // tiles done of them; items begun
+      int gs = 0, gp = 0;                             // tiles in all
+      int sk = 0, sv = 0;
+      uint32_t phk = 0, phv = 0, spins = 0;
+      bool ok = true;
+      next(ws, sn, s_last);
+      next(wp, pn, last);
+      while (ok && pn > 0) {
+        bool progress = false;
+        if (sn > 0 && gs <= gp + 1 && (si > 0 || mbar_test_warp(q_full, (uint32_t)sq & 1u)) && mbar_test_warp(&k_full[sk], phk)) {
+          const uint32_t sd = tmem + (uint32_t)(gs & 1) * BT;
+          uint64_t ad = qd0;
 #pragma unroll 1
-        for (int hv = 0; 4 * hv < groups; ++hv) {
-          if (hv) ok = mbar_wait_warp(&v_full[sv], phv);
-          if (!ok) break;
-          tc_fence_after();
-          const uint64_t bd = vd0 + (uint32_t)sv * (VH >> 4);
+          for (int blk = 0; blk < NB; ++blk, ad += QB >> 4) {
+            if (blk) ok = mbar_wait_warp(&k_full[sk], phk);
+            if (!ok) break;
+            tc_fence_after();
+            const uint64_t bd = kd0 + (uint32_t)sk * (KU >> 4);
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (4 * hv + k < groups)
-              umma_bf16_ts(tmem + o_col, pa + 8 * (4 * hv + k), bd + 128 * k, idesc_o, (i + hv + k > 0) ? 1u : 0u, el);
-          umma_commit(&v_empty[sv], el);
-          if (++sv == VS) {
-            sv = 0;
-            phv ^= 1u;
+            for (int k = 0; k < 4; ++k) umma_bf16(sd, ad + 2 * k, bd + 2 * k, idesc_s, (blk > 0 || k > 0) ? 1u : 0u, el);
+            umma_commit(&k_empty[sk], el);
+            if (++sk == KS) {
+              sk = 0;
+              phk ^= 1u;
+            }
           }
+          if (!ok) break;
+          umma_commit(&s_full[gs & 1], el);
+          ++gs;
+          if (++si == sn) {
+            umma_commit(q_empty, el);
+            si = 0;
+            ++sq;
+            next(ws, sn, s_last);
+          }
+          progress = true;
         }
-        if (!ok) break;
-        umma_commit(&pv_done[i & 1], el);
-        ++i;
-        progress = true;
+        if (gp < gs && mbar_test_warp(&p_full[gp & 1], (uint32_t)(gp >> 1) & 1u) && mbar_test_warp(&v_full[sv], phv) &&
+            (pi > 0 || pq == 0 || mbar_test_warp(o_free, (uint32_t)(pq - 1) & 1u))) {
+          const uint32_t pa = tmem + (uint32_t)(gp & 1) * BT;
+          const int groups = pi + 1 < pn ? BT / 16 : last;
+#pragma unroll 1
+          for (int hv = 0; 4 * hv < groups; ++hv) {
+            if (hv) ok = mbar_wait_warp(&v_full[sv], phv);
+            if (!ok) break;
+            tc_fence_after();
+            const uint64_t bd = vd0 + (uint32_t)sv * (VH >> 4);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (4 * hv + k < groups)
+                umma_bf16_ts(tmem + o_col, pa + 8 * (4 * hv + k), bd + 128 * k, idesc_o, (pi + hv + k > 0) ? 1u : 0u, el);
+            umma_commit(&v_empty[sv], el);
+            if (++sv == VS) {
+              sv = 0;
+              phv ^= 1u;
+            }
+          }
+          if (!ok) break;
+          umma_commit(&pv_done[gp & 1], el);
+          ++gp;
+          if (++pi == pn) {
+            pi = 0;
+            ++pq;
+            next(wp, pn, last);
+          }
+          progress = true;
+        }
+        spins = progress ? 0u : spins + 1u;
+        if (spins > kPolls) ok = false;
       }
-      spins = progress ? 0u : spins + 1u;
-      if (spins > kPolls) ok = false;
-    }
-    if (!ok) {   // what was issued ends before the TMEM goes away
-      umma_commit(ended, el);
-      mbar_wait_warp(ended, 0);
-      if (lane == 0) *abort_flag = 1;
-    }
-    __syncwarp();
+      if (!ok) {   // what was issued ends before the TMEM goes away
+        umma_commit(ended, el);
+        mbar_wait_warp(ended, 0);
+        if (lane == 0) *abort_flag = 1;
+      }
+      __syncwarp();
     } else if (warp < 19) {
       // ---- the codes' loads
       const uint32_t el = elect_one();
       const bool is_k = warp == 17;
       const uint32_t to = is_k ? ck0 : cv0;
-      uint64_t *cf = c_full + (is_k ? 0 : CS), *ce = c_empty + (is_k ? 0 : CS);
+      const int ring = is_k ? CK : CV;
+      uint64_t *cf = is_k ? ck_full : cv_full, *ce = is_k ? ck_empty : cv_empty;
       uint64_t pol;
       asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(pol));
-      const int y0 = (int)(head * L.T);
       int slot = 0, issued = 0;
       uint32_t ph = 1;
       bool ok = true;
-      for (int t = t0; ok && t < t1; ++t) {
-        const int j0 = tile_token(t), steps = NB * (is_k || keys_of(j0) > 64 ? 2 : 1);
-        for (int q = 0; q < steps; ++q) {
-          ok = mbar_wait_warp(&ce[slot], ph);
-          if (!ok) break;
-          // K: the unit's two halves of 64 tokens; V: the half's blocks of 64 dims
-          const int half = is_k ? q & 1 : q / NB, blk = is_k ? q >> 1 : q % NB;
-          mbar_expect_tx_el(&cf[slot], CB, el);
-          tma_load_2d_el(is_k ? &maps.k : &maps.v, smem_u32(&cf[slot]), to + (uint32_t)slot * CB, 64 * blk, y0 + j0 + 64 * half,
-                         pol, el);
-          ++issued;
-          if (++slot == CS) {
-            slot = 0;
-            ph ^= 1u;
+      for (int w = blockIdx.x; ok && w < items; w += gridDim.x) {
+        const Item it = item_of(a, w);
+        const int y0 = it.head * L.T;
+        // K: a tile's units, each two halves of 64 tokens; V: its halves, each NB blocks of 64 dims
+        const int halves = it.halves();
+        for (int i = 0; ok && i < it.n; ++i) {
+          const int j0 = y0 + it.token(i), steps = NB * (is_k ? 2 : min(2, halves - 2 * i));
+          for (int q = 0; q < steps; ++q) {
+            ok = mbar_wait_warp(&ce[slot], ph);
+            if (!ok) break;
+            const int half = is_k ? q & 1 : q / NB, blk = is_k ? q >> 1 : q % NB;
+            mbar_expect_tx_el(&cf[slot], CB, el);
+            tma_load_2d_el(is_k ? &maps.k : &maps.v, smem_u32(&cf[slot]), to + (uint32_t)slot * CB, 64 * blk, j0 + 64 * half, pol, el);
+            ++issued;
+            if (++slot == ring) {
+              slot = 0;
+              ph ^= 1u;
+            }
           }
         }
       }
@@ -384,176 +489,184 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
       __syncwarp();
     }
   } else {
-    regs_up<144>();
-    // ---- Q, scaled by the rows' powers of two
-#pragma unroll
-    for (int p = 0; p < PASS; ++p) {
-      const uint32_t u[4] = {qx[p].x, qx[p].y, qx[p].z, qx[p].w};
-      uint32_t top = 0u;   // bits of the largest magnitude: NaN counts as larger than all
-#pragma unroll
-      for (int z = 0; z < 4; ++z) top = max(top, max((u[z] & 0x7fffu) << 16, u[z] & 0x7fff0000u));
-      if (RPW == 1) {
-        top = __reduce_max_sync(0xffffffffu, top);
-      } else {
-#pragma unroll
-        for (int o = 1; o < LPR; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-      }
-      const float f = top >= 0x7f800000u ? __int_as_float(0x7fffffff) : exp2i(min(14 - ((int)(top >> 23) - 127), 126));
-      uint32_t w[4];
-#pragma unroll
-      for (int z = 0; z < 4; ++z) w[z] = pack_f16x2(__uint_as_float(u[z] << 16) * f, __uint_as_float(u[z] & 0xffff0000u) * f);
-      const int lr = warp * 16 + p * RPW + q_sub;
-      if (q_sub < RPW) {
-        sts_u4(q0 + (uint32_t)(q_dl >> 3) * QB + (uint32_t)lr * 128u + (uint32_t)(((q_dl & 7) ^ (lr & 7)) * 16),
-               make_uint4(w[0], w[1], w[2], w[3]));
-        if (q_dl == 0) row_top[lr] = top;
-      }
-    }
-    written(q_full);
-    asm volatile("bar.sync 5, 256;" ::: "memory");   // row_top
-    // ---- softmax and epilogue: row r (TMEM lane r), tokens 64 hf .. of each tile
+    regs_up<136>();
+    // ---- softmax and output: row r (TMEM lane r), tokens 64 hf .. of each tile
     const int q4 = warp & 3, hf = warp >> 2, r = q4 * 32 + lane;
     auto pair_bar = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory"); };   // warps w and w + 4
     const uint32_t lane_base = tmem + ((uint32_t)(q4 * 32) << 16);
-    const RowMask mk = row_mask(a, s, r0 + r);
-    // (rows whose largest |q| is below 2^-112 keep fewer bits; -e >= -126)
-    const float rf = exp2i(-min(14 - ((int)(row_top[r] >> 23) - 127), 126)) * a.scale_log2;
-    const int8_t *KE = L.ke + head * (L.T / 16), *VE = L.ve + head * (L.T / 16);
-    // references in the log2 domain, integral: m of the row's sum, W of O (largest score + value exponent)
-    float m = -INFINITY, W = -INFINITY, l = 0.f;
-    bool ok = true;
-    for (int i = 0; i < n; ++i) {
-      const int j0 = tile_token(t0 + i);
-      // exponents of this half's four blocks
-      const uint32_t kes = *(const uint32_t*)(KE + j0 / 16 + 4 * hf), ves = *(const uint32_t*)(VE + j0 / 16 + 4 * hf);
-      const bool full = j0 + BT <= firstm.hi && (j0 >= lastm.lo || j0 + BT <= a.sinks);
-      if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&s_full[i & 1], (uint32_t)(i >> 1) & 1u));
-      tc_fence_after();
-      float sc[64];
-      {
-        uint32_t raw[64];
-        const uint32_t srow = lane_base + (uint32_t)(i & 1) * BT + 64 * hf;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) tmem_ld16_async(srow + 16 * q, raw + 16 * q);
-        tmem_wait_ld();
-#pragma unroll
-        for (int q = 0; q < 4; ++q) tmem_reg_fence16(raw + 16 * q);
-#pragma unroll
-        for (int k = 0; k < 64; ++k) sc[k] = __uint_as_float(raw[k]);
+    const bool wide = ((uintptr_t)a.out | (uintptr_t)(a.out_robot * 2) | (uintptr_t)(a.out_token * 2)) % 16 == 0;
+    bool ok = true;   // (after a wait that ran out the loops go on without waiting, so that pairs meet at every barrier)
+    int gt = 0, qi = 0;   // tiles and items with Q so far
+    for (int w = blockIdx.x; w < items; w += gridDim.x) {
+      const Item it = item_of(a, w);
+      const int r0 = it.tile * BM, rows = min(BM, a.n * a.G - r0), n = it.n;
+      const size_t head = it.head;
+      bf16* out0 = (bf16*)a.out + (size_t)((long long)it.b * a.out_robot) + (size_t)it.h * a.G * L.hd;
+      auto out_row = [&](int lr) {
+        const uint32_t x = (uint32_t)(r0 + lr), i = x / (uint32_t)a.G;
+        return out0 + (size_t)((long long)i * a.out_token) + (size_t)(x - i * (uint32_t)a.G) * L.hd;
+      };
+      if (!it.ok && it.tile == 0 && it.h == 0 && it.split == 0 && threadIdx.x == 0) raise_error(a.err, ERR_SHAPE);
+      if (!it.live) {   // nothing to see: zeros
+        if (it.split == 0) {
+          for (int x = threadIdx.x; x < rows * L.hd; x += 256) out_row(x / L.hd)[x % L.hd] = __float2bfloat16_rn(0.f);
+          if (a.mass && (int)threadIdx.x < rows) a.row_ml[head * a.n * a.G + r0 + threadIdx.x] = make_float2(0.f, 0.f);
+        }
+        continue;
       }
-      if (!full) {
-        const int jh = j0 + 64 * hf;
-#pragma unroll
-        for (int k = 0; k < 64; ++k) sc[k] = mk.sees(jh + k) ? sc[k] : -INFINITY;
-      }
-      float f[4], mx = -INFINITY, wx = -INFINITY;
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        // (not 0, which times a hidden score's -inf would not be a number)
-        f[t] = fmaxf(rf * exp2i((int)(int8_t)(kes >> (8 * t))), 1e-37f);
-        float m4[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          m4[e] = fmaxf(fmaxf(sc[16 * t + 4 * e], sc[16 * t + 4 * e + 1]), fmaxf(sc[16 * t + 4 * e + 2], sc[16 * t + 4 * e + 3]));
-        const float x = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * f[t];
-        mx = fmaxf(mx, x);
-        wx = fmaxf(wx, x + (float)(int8_t)(ves >> (8 * t)));
-      }
-      // (past the first barrier both halves have read their scores, past the second the maxima)
-      xm[hf * 128 + r] = make_float2(mx, wx);
-      pair_bar();
-      const float2 x0 = xm[r], x1 = xm[128 + r];
-      pair_bar();
-      const float mn = fmaxf(m, ceilf(fmaxf(x0.x, x1.x))), wn = fmaxf(W, ceilf(fmaxf(x0.y, x1.y)));
-      const float mu = mn == -INFINITY ? 0.f : mn;
-      l *= pow2f_down(m - mu);
-      m = mn;
-      const bool need = wn > W + 8.f;
-      if (i > 0 && __any_sync(0xffffffffu, need)) {
-        // O holds P V of every earlier tile before it is rescaled
-        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&pv_done[(i - 1) & 1], (uint32_t)((i - 1) >> 1) & 1u));
+      const RowMask mk = row_mask(a, it.s, r0 + r);
+      const RowMask firstm = row_mask(a, it.s, r0), lastm = row_mask(a, it.s, min(r0 + BM, it.s.count * a.G) - 1);
+      float rf = 0.f;
+      const int8_t *KE = L.ke + head * (L.T / 16), *VE = L.ve + head * (L.T / 16);
+      // references in the log2 domain, integral: m of the row's sum, W of O (largest score + value exponent)
+      float m = -INFINITY, W = -INFINITY, l = 0.f;
+      for (int i = 0; i < n; ++i, ++gt) {
+        const int j0 = it.token(i);
+        // exponents of this half's four blocks
+        const uint32_t kes = *(const uint32_t*)(KE + j0 / 16 + 4 * hf), ves = *(const uint32_t*)(VE + j0 / 16 + 4 * hf);
+        const bool full = j0 + BT <= firstm.hi && (j0 >= lastm.lo || j0 + BT <= a.sinks);
+        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&s_full[gt & 1], (uint32_t)(gt >> 1) & 1u));
         tc_fence_after();
-        const float alpha = need ? pow2f_down(W - wn) : 1.f;
-        for (int cb = 16 * hf; cb < HDP; cb += 32) {
-          float o[16];
-          tmem_ld16(lane_base + o_col + cb, o);
+        if (i == 0) {   // (S needed Q: it is there.  Rows whose largest |q| is below 2^-112 keep fewer bits; -e >= -126)
+          rf = exp2i(-min(14 - ((int)row_exp[(qi & 3) * BM + r] - 127), 126)) * a.scale_log2;
+          ++qi;
+        }
+        float sc[64];
+        {
+          uint32_t raw[64];
+          const uint32_t srow = lane_base + (uint32_t)(gt & 1) * BT + 64 * hf;
 #pragma unroll
-          for (int q = 0; q < 16; ++q) o[q] *= alpha;
-          tmem_st16(lane_base + o_col + cb, o);
+          for (int q = 0; q < 4; ++q) tmem_ld16_async(srow + 16 * q, raw + 16 * q);
+          tmem_wait_ld();
+#pragma unroll
+          for (int q = 0; q < 4; ++q) tmem_reg_fence16(raw + 16 * q);
+#pragma unroll
+          for (int k = 0; k < 64; ++k) sc[k] = __uint_as_float(raw[k]);
+        }
+        if (!full) {
+          const int jh = j0 + 64 * hf;
+#pragma unroll
+          for (int k = 0; k < 64; ++k) sc[k] = mk.sees(jh + k) ? sc[k] : -INFINITY;
+        }
+        float f[4], mx = -INFINITY, wx = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          // (not 0, which times a hidden score's -inf would not be a number)
+          f[t] = fmaxf(rf * exp2i((int)(int8_t)(kes >> (8 * t))), 1e-37f);
+          float m4[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            m4[e] = fmaxf(fmaxf(sc[16 * t + 4 * e], sc[16 * t + 4 * e + 1]), fmaxf(sc[16 * t + 4 * e + 2], sc[16 * t + 4 * e + 3]));
+          const float x = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * f[t];
+          mx = fmaxf(mx, x);
+          wx = fmaxf(wx, x + (float)(int8_t)(ves >> (8 * t)));
+        }
+        // (past the first barrier both halves have read their scores, past the second the maxima)
+        xm[hf * 128 + r] = make_float2(mx, wx);
+        pair_bar();
+        const float2 x0 = xm[r], x1 = xm[128 + r];
+        pair_bar();
+        const float mn = fmaxf(m, ceilf(fmaxf(x0.x, x1.x))), wn = fmaxf(W, ceilf(fmaxf(x0.y, x1.y)));
+        const float mu = mn == -INFINITY ? 0.f : mn;
+        l *= pow2f_down(m - mu);
+        m = mn;
+        const bool need = wn > W + 8.f;
+        if (i > 0 && __any_sync(0xffffffffu, need)) {
+          // O holds P V of every earlier tile before it is rescaled
+          if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&pv_done[(gt - 1) & 1], (uint32_t)((gt - 1) >> 1) & 1u));
+          tc_fence_after();
+          const float alpha = need ? pow2f_down(W - wn) : 1.f;
+          for (int cb = 16 * hf; cb < HDP; cb += 32) {
+            float o[16];
+            tmem_ld16(lane_base + o_col + cb, o);
+#pragma unroll
+            for (int q = 0; q < 16; ++q) o[q] *= alpha;
+            tmem_st16(lane_base + o_col + cb, o);
+          }
+          tmem_wait_st();
+        }
+        if (need) W = wn;
+        const float wu = W == -INFINITY ? 0.f : W;
+        const uint32_t prow = lane_base + (uint32_t)(gt & 1) * BT + 32 * hf;
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2) {
+          uint32_t wd[16];
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const int blk = 2 * h2 + t;
+            // the value exponent goes into that of P and out of the block's sum again
+            const float vf = fmaxf((float)(int8_t)(ves >> (8 * blk)), wu - mu - kVeBelow), nbt = kTcShift + vf - wu;
+            float e[16];
+#pragma unroll
+            for (int q = 0; q < 16; ++q) e[q] = fast_exp2(fmaf(sc[16 * blk + q], f[blk], nbt));
+            float s4[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) s4[q] = (e[4 * q] + e[4 * q + 1]) + (e[4 * q + 2] + e[4 * q + 3]);
+            l = fmaf((s4[0] + s4[1]) + (s4[2] + s4[3]), pow2f(wu - mu - vf), l);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) wd[8 * t + q] = pack_f16x2(e[2 * q], e[2 * q + 1]);
+          }
+          tmem_st16u(prow + 16 * h2, wd);
         }
         tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(&p_full[gt & 1]);
       }
-      if (need) W = wn;
-      const float wu = W == -INFINITY ? 0.f : W;
-      const uint32_t prow = lane_base + (uint32_t)(i & 1) * BT + 32 * hf;
+      if (ok && n > 0) {
+        ok = __all_sync(0xffffffffu, mbar_wait(&pv_done[(gt - 1) & 1], (uint32_t)((gt - 1) >> 1) & 1u));
+        tc_fence_after();
+      }
+      xm[hf * 128 + r].x = l;
+      pair_bar();
+      l = xm[r].x + xm[128 + r].x;
+      pair_bar();
+      const bool real = mk.hi > 0 && n > 0 && !(l <= 0.f);   // (a sum that is not a number stays one)
+      const float inv = real ? pow2f(W - m) / l : 0.f;
+      const float m_out = real ? m : -INFINITY, l_out = real ? l : 0.f;
+      if (a.splits == 1) {
+        if (a.mass && hf == 0 && r < rows) a.row_ml[head * a.n * a.G + r0 + r] = row_weight(m_out, l_out, kTcShift);
+        // O / l as bf16, 32 columns at a time: through the warp's own staging, from where four
+        // lanes store 64 bytes of a row
+        const uint32_t stg = st0 + 2048u * warp;
+        bf16* dst[4];
 #pragma unroll
-      for (int h2 = 0; h2 < 2; ++h2) {
-        uint32_t w[16];
+        for (int z = 0; z < 4; ++z) dst[z] = out_row(min(q4 * 32 + (lane >> 2) + 8 * z, rows - 1)) + 8 * (lane & 3);
+        for (int cb = 32 * hf; cb < HDP; cb += 64) {   // (the halves take alternate columns)
+          uint32_t raw[32];
+          tmem_ld32_async(lane_base + o_col + cb, raw);
+          tmem_wait_ld();
+          tmem_reg_fence16(raw);
+          tmem_reg_fence16(raw + 16);
+          if (cb + 64 >= HDP) {   // the last of O: the next item's may begin
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(o_free);
+          }
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const int blk = 2 * h2 + t;
-          const float vf = fmaxf((float)(int8_t)(ves >> (8 * blk)), wu - mu - kVeBelow), nbt = kTcShift + vf - wu;
-          float e[16];
+          for (int q = 0; q < 4; ++q) {
+            uint32_t wd[4];
 #pragma unroll
-          for (int q = 0; q < 16; ++q) e[q] = fast_exp2(fmaf(sc[16 * blk + q], f[blk], nbt));
-          float s4[4];
+            for (int z = 0; z < 4; ++z)
+              wd[z] = real ? pack_bf16x2(__uint_as_float(raw[8 * q + 2 * z]) * inv, __uint_as_float(raw[8 * q + 2 * z + 1]) * inv) : 0u;
+            sts_u4(stg + 64u * lane + (uint32_t)((q ^ ((lane >> 1) & 3)) * 16), make_uint4(wd[0], wd[1], wd[2], wd[3]));
+          }
+          __syncwarp();
 #pragma unroll
-          for (int q = 0; q < 4; ++q) s4[q] = (e[4 * q] + e[4 * q + 1]) + (e[4 * q + 2] + e[4 * q + 3]);
-          l = fmaf((s4[0] + s4[1]) + (s4[2] + s4[3]), pow2f(wu - mu - vf), l);
-#pragma unroll
-          for (int q = 0; q < 8; ++q) w[8 * t + q] = pack_f16x2(e[2 * q], e[2 * q + 1]);
+          for (int z = 0; z < 4; ++z) {
+            const int lr = (lane >> 2) + 8 * z;
+            const uint4 x = lds_u4(stg + 64u * lr + (uint32_t)(((lane & 3) ^ ((lr >> 1) & 3)) * 16));
+            if (q4 * 32 + lr < rows && cb + 8 * (lane & 3) < L.hd) store_bf16x8(dst[z] + cb, x, wide);
+          }
+          __syncwarp();
         }
-        tmem_st16u(prow + 16 * h2, w);
+        continue;
       }
-      tmem_wait_st();
-      tc_fence_before();
-      mbar_arrive(&p_full[i & 1]);
-    }
-    if (ok && n > 0) {
-      ok = __all_sync(0xffffffffu, mbar_wait(&pv_done[(n - 1) & 1], (uint32_t)((n - 1) >> 1) & 1u));
-      tc_fence_after();
-    }
-    if (!ok && lane == 0) *abort_flag = 1;
-    xm[hf * 128 + r].x = l;
-    pair_bar();
-    l = xm[r].x + xm[128 + r].x;
-    const bool real = mk.hi > 0 && n > 0 && !(l <= 0.f);   // (a sum that is not a number stays one)
-    const float inv = real ? pow2f(W - m) / l : 0.f;
-    const float m_out = real ? m : -INFINITY, l_out = real ? l : 0.f;
-    if (a.splits == 1) {
-      if (a.mass && hf == 0 && r < rows) a.row_ml[head * a.n * a.G + r0 + r] = row_weight(m_out, l_out, kTcShift);
-      // O / l as bf16 into Q's place (every S has completed), from where whole rows go out
-      for (int cb = 32 * hf; cb < HDP; cb += 64) {
-        uint32_t raw[32];
-        tmem_ld32_async(lane_base + o_col + cb, raw);
-        tmem_wait_ld();
-        tmem_reg_fence16(raw);
-        tmem_reg_fence16(raw + 16);
-        const uint32_t at = q0 + (uint32_t)(cb >> 6) * QB + (uint32_t)r * 128u;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          uint32_t w[4];
-#pragma unroll
-          for (int z = 0; z < 4; ++z)
-            w[z] = real ? pack_bf16x2(__uint_as_float(raw[8 * q + 2 * z]) * inv, __uint_as_float(raw[8 * q + 2 * z + 1]) * inv) : 0u;
-          sts_u4(at + (uint32_t)(((((cb & 32) >> 3) + q) ^ (r & 7)) * 16), make_uint4(w[0], w[1], w[2], w[3]));
-        }
-      }
-      asm volatile("bar.sync 5, 256;" ::: "memory");
-      // a warp per row: 16-byte pieces
-      const bool wide = ((uintptr_t)a.out | (uintptr_t)(a.out_robot * 2) | (uintptr_t)(a.out_token * 2)) % 16 == 0;
-#pragma unroll 4
-      for (int rr = warp; rr < rows; rr += 8) {
-        bf16* dst = out_row(r0 + rr) + 8 * lane;
-        if (8 * lane < L.hd) store_bf16x8(dst, lds_codes(q0 + (uint32_t)(lane >> 3) * QB + (uint32_t)rr * 128u + (uint32_t)(((lane & 7) ^ (rr & 7)) * 16)), wide);
-      }
-    } else {
-      // normalised partials, joined in the splits' order: up to 8 splits are a cluster, whose
-      // CTAs read a share of the rows each from one another's shared memory; of more, which
-      // store to L2, the last to arrive joins all rows
+      // splits (one item per CTA): normalised partials, joined in the splits' order: up to 8
+      // splits are a cluster, whose CTAs read a share of the rows each from one another's
+      // shared memory; of more, which store to L2, the last to arrive joins all rows
       const bool cluster = a.splits <= kTcCluster;
-      const size_t unit = head * a.row_tiles + tile;
-      constexpr uint32_t XR = TcShape<NB>::xrow;
+      const size_t unit = head * a.row_tiles + it.tile;
+      constexpr uint32_t XR = Shape::xrow;
       for (int cb = 32 * hf; cb < HDP; cb += 64) {
         uint32_t raw[32];
         tmem_ld32_async(lane_base + o_col + cb, raw);
@@ -567,21 +680,20 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
           for (int q = 0; q < 8; ++q)
             sts_u4(k0 + (uint32_t)r * XR + 4u * (cb + 4 * q), make_uint4(raw[4 * q], raw[4 * q + 1], raw[4 * q + 2], raw[4 * q + 3]));
         } else if (r < rows) {
-          uint4* part = (uint4*)(a.part + ((unit * a.splits + split) * BM + r) * HDP + cb);
+          uint4* part = (uint4*)(a.part + ((unit * a.splits + it.split) * BM + r) * HDP + cb);
 #pragma unroll
           for (int q = 0; q < 8; ++q) __stcg(part + q, make_uint4(raw[4 * q], raw[4 * q + 1], raw[4 * q + 2], raw[4 * q + 3]));
         }
       }
       int ra = 0, rb = rows;
       if (cluster) {
-        pair_bar();   // (both halves have read the sums)
         if (hf == 0) xm[r] = make_float2(m_out, l_out);
         cluster_sync();   // (the other roles arrive below)
         const int share = (rows + a.splits - 1) / a.splits;
-        ra = split * share;
+        ra = it.split * share;
         rb = min(rows, ra + share);
       } else {
-        if (hf == 0) __stcg(a.part_ml + (unit * a.splits + split) * BM + r, make_float2(m_out, l_out));
+        if (hf == 0) __stcg(a.part_ml + (unit * a.splits + it.split) * BM + r, make_float2(m_out, l_out));
         __threadfence();
         asm volatile("bar.sync 5, 256;" ::: "memory");
         if (threadIdx.x == 0) *last_flag = atomicInc(a.arrived + unit, (unsigned)a.splits - 1u) == (unsigned)a.splits - 1u;
@@ -589,7 +701,6 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
         if (!*last_flag) rb = 0;
         __threadfence();
       }
-      const bool wide = ((uintptr_t)a.out | (uintptr_t)(a.out_robot * 2) | (uintptr_t)(a.out_token * 2)) % 16 == 0;
       // the splits' weights per row, [splits][128], into Q's place (every S has completed)
       // or, where they may be many, the rings' ...
       float* wts = (float*)(smem + (cluster ? 0 : NB * QB));
@@ -605,8 +716,8 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
           wts[q * BM + rr] = wt;
           S += wt;
         }
-        const float si = !(S <= 0.f) ? 1.f / S : 0.f;
-        for (int q = 0; q < a.splits; ++q) wts[q * BM + rr] *= si;
+        const float sv = !(S <= 0.f) ? 1.f / S : 0.f;
+        for (int q = 0; q < a.splits; ++q) wts[q * BM + rr] *= sv;
         if (a.mass) a.row_ml[head * a.n * a.G + r0 + rr] = row_weight(M, S, kTcShift);
       }
       asm volatile("bar.sync 5, 256;" ::: "memory");
@@ -638,7 +749,7 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
             acc[6] = fmaf(wt, y1.z, acc[6]);
             acc[7] = fmaf(wt, y1.w, acc[7]);
           }
-          store_bf16x8(out_row(r0 + rr) + 8 * lane,
+          store_bf16x8(out_row(rr) + 8 * lane,
                        make_uint4(pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3]), pack_bf16x2(acc[4], acc[5]),
                                   pack_bf16x2(acc[6], acc[7])),
                        wide);
@@ -646,17 +757,18 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
       }
       if (cluster) cluster_sync();   // nobody leaves while its rows are read
     }
+    if (!ok && lane == 0) *abort_flag = 1;
   }
-  if (warp >= 8 && a.splits > 1 && a.splits <= kTcCluster) {
+  if (warp >= 8 && a.splits > 1 && a.splits <= kTcCluster && item_of(a, blockIdx.x).live) {
     cluster_sync();
     cluster_sync();
   }
   tc_fence_before();
   cta_sync();
   if (*abort_flag && threadIdx.x == 0) {
-    // loads still on their way, at most the last CS, land before the shared memory goes away
-    for (int q = 0; q < 2; ++q)
-      for (int i = max(0, c_issued[q] - CS); i < c_issued[q]; ++i) mbar_wait(&c_full[q * CS + i % CS], (uint32_t)(i / CS) & 1u);
+    // loads still on their way, at most a ring of them, land before the shared memory goes away
+    for (int i = max(0, c_issued[0] - CK); i < c_issued[0]; ++i) mbar_wait(&ck_full[i % CK], (uint32_t)(i / CK) & 1u);
+    for (int i = max(0, c_issued[1] - CV); i < c_issued[1]; ++i) mbar_wait(&cv_full[i % CV], (uint32_t)(i / CV) & 1u);
     raise_error(a.err, ERR_TIMEOUT);
   }
   if (warp == 16)
@@ -693,8 +805,14 @@ cudaError_t launch_nb(CacheAttnArgs a, cudaStream_t st) {
   cudaError_t e = encode_codes(&maps.k, a.c.k, a.c, a.batch);
   if (e == cudaSuccess) e = encode_codes(&maps.v, a.c.v, a.c, a.batch);
   if (e != cudaSuccess) return e;
-  return launch_kernel_cluster(cache_tc_kernel<NB>, dim3(a.row_tiles * a.splits, a.c.Hkv, a.batch), dim3(TCT),
-                               TcShape<NB>::bytes, st, dim3(a.splits <= kTcCluster ? a.splits : 1, 1, 1), maps, a);
+  // causal prompts: pairs whose caches take 48 MB together (beside the queries, in an L2 of 129)
+  const long long pairs = (long long)a.c.Hkv * a.batch;
+  a.group = 1;
+  if (a.causal && !a.window) a.group = (int)std::min(pairs, std::max(1ll, (48ll << 20) / (2ll * a.max_length * a.c.hdp + 1)));
+  if (tiles * a.splits > 0x7fffffffll) return cudaErrorInvalidValue;
+  const unsigned grid = a.splits == 1 ? (unsigned)std::min(tiles, (long long)a.num_sms) : (unsigned)(tiles * a.splits);
+  return launch_kernel_cluster(cache_tc_kernel<NB>, dim3(grid), dim3(TCT), TcShape<NB>::bytes, st,
+                               dim3(a.splits <= kTcCluster ? a.splits : 1, 1, 1), maps, a);
 }
 
 template <int NB>
