@@ -24,6 +24,10 @@ struct Sight {
 struct RowMask {
   int hi, lo, sinks;   // sees j < hi and (j >= lo or j < sinks)
   __device__ __forceinline__ bool sees(int j) const { return j < hi && (j >= lo || j < sinks); }
+  // tokens j .. j + 31 that it sees
+  __device__ __forceinline__ uint32_t bits(int j) const { return below(hi - j) & (~below(lo - j) | below(sinks - j)); }
+  // the lowest x bits
+  static __device__ __forceinline__ uint32_t below(int x) { return x <= 0 ? 0u : (x >= 32 ? 0xffffffffu : (1u << x) - 1u); }
 };
 
 __device__ __forceinline__ RowMask row_mask(const CacheAttnArgs& a, const Sight& s, int r) {

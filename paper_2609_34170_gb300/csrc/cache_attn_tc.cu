@@ -4,32 +4,33 @@
 // An item is 128 rows (row r = query * G + head of the group) of one (robot, KV
 // head) and a share (split) of the 128-token tiles that they see; CTAs, one per SM,
 // walk the items of their launch:
-//   S = Q K^T        tcgen05.mma kind::f16, M = 128, N = 128, into TMEM
+//   S = Q K^T        tcgen05.mma kind::f8f6f4, M = 128, N = 128, into TMEM: the codes
+//                    of K as they are, Q in two e4m3 pieces
 //   P = 2^(S - m)    softmax warps: TMEM -> registers -> f16 P over S in TMEM
-//   O += P V         tcgen05.mma, M = 128, N = head dim, 16 tokens at a time
+//   O += P V         tcgen05.mma kind::f16, M = 128, N = head dim, 16 tokens at a time
 // Warp roles (640 threads): warps 0-7 softmax and output, two threads per row; warps
-// 8-11 widen K and lay out Q, warps 12-15 widen V; warp 16 TMEM and MMAs; warps 17, 18
-// load the codes of K and V (19 idle, so that registers move between whole
-// warpgroups).  Every role walks the items on its own, so that one item's output
-// lies beside the next one's Q, K and first scores.
+// 8-11 lay out Q, warps 12-15 widen V; warp 16 TMEM and MMAs; warps 17, 18 load the
+// codes of K and V (19 idle, so that registers move between whole warpgroups).
+// Every role walks the items on its own, so that one item's output lies beside the
+// next one's Q, K and first scores.
 //
-// The codes come by TMA and are widened in shared memory to f16 (e4m3 -> f16 is
-// exact), into the 128-byte swizzled layout that a TMA load of f16 rows would
-// leave: K in units of 64 head dims (16 KB), V in halves of 64 tokens, each in
-// rings of its own with its own warps, so that neither waits for the other's
-// slots.  (With the codes loaded to registers by the widening warps themselves a
-// unit took a load's latency, 900 cycles where the MMAs of one take 512: the proxy
-// fence that ends a unit waits for the loads in flight.)
-// Feeding the codes as kind::f8f6f4 operands instead would need Q and P in 8 bits
-// too: two pieces of each keep bf16's precision and cost what one f16 MMA does, but
-// 2^-9 is the least P that e4m3 holds, and a long flat tail of smaller ones carries
-// weight.
+// What bounds it at head dim 256 is shared memory: per tile (2048 cycles of MMA) its
+// 128 bytes a cycle carry 192 KB of MMA operands, and every code that is widened to
+// f16 costs 4 bytes more of TMA, reading and writing.  So K is not widened: bf16's 8
+// significant bits are two e4m3 pieces of 4 (a rounded one and the rest, exactly,
+// down to 2^-18 of the row's largest), whose two MMAs at twice the rate cost what
+// one in f16 does.  V is: 2^-9 is the least P that e4m3 holds, and a long flat tail
+// of smaller ones carries weight.  The codes of V come by TMA and are widened in
+// shared memory to f16 (exact), into the 128-byte swizzled layout of a TMA load of
+// f16 rows.  (Widening K as well, in units of 64 head dims, 448 KB a tile, took 3600
+// to 4400 cycles; with the codes loaded to registers by the widening warps a step
+// took a load's latency, as the proxy fence that ends it waits for the loads in
+// flight.)
 //
-// Numbers as in the kernel for few rows: q in f16 under a power of two per row
-// (exact for bf16), block exponents of K on the scores, those of V on P.  P is at
-// most 2^7 of the reference, 2^15 while a grown one waits for its rescaling of O
-// (only growth by more than 2^8 rescales); what contributes less than 2^-31 of the
-// row's largest is dropped.
+// Numbers as in the kernel for few rows: a power of two per row of Q, block exponents
+// of K on the scores, those of V on P.  P is at most 2^7 of the reference, 2^15 while
+// a grown one waits for its rescaling of O (only growth by more than 2^8 rescales);
+// what contributes less than 2^-31 of the row's largest is dropped.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -43,40 +44,56 @@ namespace {
 
 constexpr int TCT = 640;
 constexpr int BM = 128, BT = 128;              // rows, tokens of a tile
-constexpr uint32_t QB = BM * 128;              // bytes of a 64-dim block of Q
-constexpr uint32_t KU = BT * 128;              // bytes of a K unit: 128 tokens x 64 dims
-constexpr uint32_t CB = 64 * 64;               // bytes of a slot of codes: 64 tokens x 64 dims
+constexpr uint32_t QB = BM * 64;               // bytes of a 64-dim block of a piece of Q
+constexpr uint32_t KU = BT * 64;               // bytes of a K unit: 128 tokens x 64 dims
+constexpr uint32_t CB = 64 * 64;               // bytes of a slot of V's codes: 64 tokens x 64 dims
 constexpr uint32_t VB = 64 * 128;              // bytes of a 64-dim block of a V half
+constexpr int kQExp = 7;                        // Q's largest magnitude per row is below 2^(kQExp + 1)
 constexpr float kTcShift = 7.f;                // P's largest value is 2^kTcShift (times 2^8 while lazy)
 constexpr int kTcCluster = 8;                  // splits that are a cluster
-constexpr uint32_t kPolls = 1u << 25;          // polls without progress: seconds
 
 template <int NB> struct TcShape {
-  // shared memory at NB blocks of 64 head dims: Q, the rings of widened K units and V
-  // halves, the rings of codes, the output's staging, barriers and row data
-  static constexpr int KS = NB == 4 ? 2 : (NB == 3 ? 3 : 4);
-  static constexpr int VS = NB >= 3 ? 2 : (NB == 2 ? 3 : 4);
-  // codes: multiples of the 4 warps that widen them: each slot is then waited for by one
-  // warp, in order.  (Loads may complete out of order; a warp that waits for a slot's next
-  // phase while another's load into it is still on its way would take the phase before for
-  // it.)
-  static constexpr int CK = 8, CV = NB == 4 ? 4 : 8;
-  static_assert(CK % 4 == 0 && CV % 4 == 0, "widening warps");
-  static constexpr uint32_t ring = KS * KU + VS * NB * VB + (CK + CV) * CB;
-  static constexpr uint32_t stage = 8 * 2048;   // 32 rows x 32 columns of bf16 per softmax warp
-  static constexpr uint32_t bytes = NB * QB + ring + stage + 3072;
+  // shared memory at NB blocks of 64 head dims: Q's pieces, the rings of K units, of widened
+  // V halves and of V's codes, barriers and row data
+  static constexpr int KS = NB == 4 ? 4 : 8;
+  static constexpr int VS = NB >= 3 ? 3 : (NB == 2 ? 4 : 8);
+  // a multiple of the 8 warps that widen them: each slot is then waited for by one warp, in
+  // order.  (Loads may complete out of order; a warp that waits for a slot's next phase while
+  // another's load into it is still on its way would take the phase before for it.)
+  static constexpr int CV = 8;
+  static_assert(CV % 8 == 0, "widening warps");
+  static constexpr uint32_t q_bytes = 2 * NB * QB;
+  static constexpr uint32_t ring = KS * KU + VS * NB * VB + CV * CB;
+  static constexpr uint32_t bytes = q_bytes + ring + 3072;
   static_assert(bytes <= 227 * 1024, "shared memory");
   // a row of the fp32 output that splits exchange (over the rings): 16 bytes more than
   // the dims, so that rows written by neighbouring lanes fall on different banks
   static constexpr uint32_t xrow = NB * 64 * 4 + 16;
-  static_assert(BM * xrow <= ring && BM * 4 * 256 <= ring && BM * 4 * 8 <= NB * QB, "exchange");
+  static_assert(BM * xrow <= ring && BM * 4 * 256 <= ring && BM * 4 * 8 <= q_bytes, "exchange");
 };
 
 struct TcMaps {
-  CUtensorMap k, v;   // a layer's codes [B Hkv T][hdp] in boxes of 64 dims x 64 rows
+  CUtensorMap k, v;   // a layer's codes [B Hkv T][hdp]: boxes of 64 dims x 128 rows (swizzled), x 64 rows
 };
 
-// f16 A and B, fp32 D
+// Shared-memory descriptor of a K-major tile of 64-byte rows, 64-byte swizzled: 8-row
+// groups 512 bytes apart.
+__device__ __forceinline__ uint64_t sw64_desc(uint32_t saddr) {
+  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(512 >> 4) << 32 | (uint64_t)1 << 46 |
+         (uint64_t)4 << 61;
+}
+
+// D += A B of e4m3 operands (K = 32), issued by the elected lane of a converged warp
+__device__ __forceinline__ void umma_e4m3(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc, uint32_t el) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(el));
+}
+
+// f16 A and B (kind::f16) or e4m3 ones (kind::f8f6f4), fp32 D
 __device__ __forceinline__ uint32_t idesc_f16(int m, int n) {
   return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
@@ -94,9 +111,9 @@ __device__ __forceinline__ float4 ld_cluster_f4(uint32_t a) {
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a));
   return v;
 }
-__device__ __forceinline__ float2 ld_cluster_f2(uint32_t a) {
-  float2 v;
-  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a));
+__device__ __forceinline__ float ld_cluster_f1(uint32_t a) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a));
   return v;
 }
 
@@ -104,6 +121,21 @@ __device__ __forceinline__ float2 ld_cluster_f2(uint32_t a) {
 __device__ __forceinline__ void widen(uint4 w, uint32_t lo, uint32_t hi) {
   sts_u4(lo, make_uint4(e4m3_lo(w.x), e4m3_hi(w.x), e4m3_lo(w.y), e4m3_hi(w.y)));
   sts_u4(hi, make_uint4(e4m3_lo(w.z), e4m3_hi(w.z), e4m3_lo(w.w), e4m3_hi(w.w)));
+}
+
+__device__ __forceinline__ void sts_u2(uint32_t a, uint32_t x, uint32_t y) {
+  asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(a), "r"(x), "r"(y) : "memory");
+}
+// two f16 -> two e4m3 (nearest, ties to even; NaN stays NaN), low halves first
+__device__ __forceinline__ uint32_t f16_to_e4m3(uint32_t h) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(h));
+  return r;
+}
+__device__ __forceinline__ uint32_t f16_sub(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
 }
 
 __device__ __forceinline__ void store_bf16x8(bf16* dst, uint4 w, bool wide) {
@@ -118,11 +150,32 @@ __device__ __forceinline__ void store_bf16x8(bf16* dst, uint4 w, bool wide) {
 }
 
 // Registers of a warpgroup: launched with 96 each (640 x 96 = 61440); softmax
-// 2 x 128 x 136, widening 2 x 128 x 80, the rest 128 x 48: 61440.
+// 2 x 128 x 136, Q and widening 2 x 128 x 80, the rest 128 x 48: 61440.
 template <int N>
 __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
 __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
+// Wait of a converged warp for a phase, bounded: 2^24 tries of 20 to 200 cycles each.  Four
+// instructions a try: twenty warps whose waits read the global timer between tries, as those
+// of kernels with fewer do, took over half of an SM's issue slots; tries with a time hint
+// sleep past the arrival.
+__device__ __forceinline__ bool wait_phase(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\t"
+      "mov.u32 n, 0;\n\t"
+      "TRY: mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "@p bra DONE;\n\t"
+      "add.u32 n, n, 1;\n\t"
+      "setp.lt.u32 q, n, 16777216;\n\t"
+      "@q bra TRY;\n\t"
+      "DONE: selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return __all_sync(0xffffffffu, ok != 0);
+}
 
 // A warp's writes to shared memory become visible to the tensor core: one arrival per warp.
 __device__ __forceinline__ void written(uint64_t* bar) {
@@ -173,22 +226,23 @@ __device__ __forceinline__ Item item_of(const CacheAttnArgs& a, int w) {
   return it;
 }
 
+// One value of a converged warp, so that the compiler knows it: the operands of the
+// asynchronous instructions then stay in uniform registers.
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+
 template <int NB>
 __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant__ TcMaps maps, CacheAttnArgs a) {
   using Shape = TcShape<NB>;
-  constexpr int HDP = 64 * NB, KS = Shape::KS, VS = Shape::VS, CK = Shape::CK, CV = Shape::CV;
+  constexpr int HDP = 64 * NB, KS = Shape::KS, VS = Shape::VS, CV = Shape::CV;
   constexpr uint32_t VH = NB * VB;   // bytes of a V half
   extern __shared__ __align__(1024) uint8_t smem[];
-  const uint32_t q0 = smem_u32(smem), k0 = q0 + NB * QB, v0 = k0 + KS * KU, ck0 = v0 + VS * VH, cv0 = ck0 + CK * CB,
-                 st0 = cv0 + CV * CB;
-  uint8_t* tail = smem + NB * QB + Shape::ring + Shape::stage;
+  const uint32_t q0 = smem_u32(smem), k0 = q0 + Shape::q_bytes, v0 = k0 + KS * KU, cv0 = v0 + VS * VH;
+  uint8_t* tail = smem + Shape::q_bytes + Shape::ring;
   uint64_t* k_full = (uint64_t*)tail;
   uint64_t* k_empty = k_full + KS;
   uint64_t* v_full = k_empty + KS;
   uint64_t* v_empty = v_full + VS;
-  uint64_t* ck_full = v_empty + VS;
-  uint64_t* ck_empty = ck_full + CK;
-  uint64_t* cv_full = ck_empty + CK;
+  uint64_t* cv_full = v_empty + VS;
   uint64_t* cv_empty = cv_full + CV;
   uint64_t* s_full = cv_empty + CV;   // [2]
   uint64_t* p_full = s_full + 2;      // [2]
@@ -200,12 +254,12 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
   uint32_t* tmem_slot = (uint32_t*)(ended + 1);
   int* abort_flag = (int*)(tmem_slot + 1);
   int* last_flag = abort_flag + 1;
-  int* c_issued = last_flag + 1;                  // [2] loads of codes issued, K and V
+  int* issued_flag = last_flag + 1;               // [2] loads of K and V issued
   // exponent bits of the rows' largest |q|, [4][128], by item: S runs up to two tiles, so up
   // to two items, ahead of the softmax, and Q one more
   uint8_t* row_exp = tail + 512;
-  float2* xm = (float2*)(tail + 1024);            // [2][128] row maxima, then sums, of the two halves
-  static_assert((2 * KS + 2 * VS + 2 * CK + 2 * CV + 10) * 8 + 20 <= 512, "barriers");
+  float2* xm = (float2*)(row_exp + 512);   // [2][128] row maxima, then sums, of the two halves
+  static_assert((2 * KS + 2 * VS + 2 * CV + 10) * 8 + 20 <= 512, "barriers");
 
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const CacheLayer& L = a.c;
@@ -216,23 +270,19 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
   }
   if (threadIdx.x == 0) {
     for (int i = 0; i < KS; ++i) {
-      mbar_init(&k_full[i], 2);   // the steps of a unit
+      mbar_init(&k_full[i], 1);
       mbar_init(&k_empty[i], 1);
     }
     for (int i = 0; i < VS; ++i) {
-      mbar_init(&v_full[i], NB);   // ... of a half
+      mbar_init(&v_full[i], NB);   // the steps of a half
       mbar_init(&v_empty[i], 1);
-    }
-    for (int i = 0; i < CK; ++i) {
-      mbar_init(&ck_full[i], 1);
-      mbar_init(&ck_empty[i], 1);
     }
     for (int i = 0; i < CV; ++i) {
       mbar_init(&cv_full[i], 1);
       mbar_init(&cv_empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
-      c_issued[i] = 0;
+      issued_flag[i] = 0;
       mbar_init(&s_full[i], 1);
       mbar_init(&p_full[i], 256);
       mbar_init(&pv_done[i], 1);
@@ -257,116 +307,156 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
 
   if (warp >= 8 && warp < 16) {
     regs_down<80>();
-    // ---- widening: K in units of 64 dims (warps 8-11), V in halves of 64 tokens (12-15), in
-    // steps of 64 tokens x 64 dims.  A warp takes every fourth step as a whole, so that the
-    // waits, the proxy fence and the shared-memory latency of one lie beside the work on the
-    // others (a unit by four warps together took 750 cycles, little of it work).
-    const bool is_k = warp < 12;
-    // lane: 16 codes at dim 16 (lane % 4) of rows lane / 4, lane / 4 + 8, ...
+    // ---- Q (warps 8-11) at an item's start, then, with warps 12-15, the widening of V.
+    // Q: 32 rows per warp, 8 NB lanes with 8 dims each to a row, scaled by the row's power
+    // of two to a largest magnitude in [2^7, 2^8), in two e4m3 pieces: y rounded and what is
+    // left.  A batch of 8 rows per pass is ready before Q's place is free.
+    constexpr int LPR = 8 * NB, RPW = 32 / LPR, PASS = 32 / RPW;
+    const int sub = lane / LPR < RPW ? lane / LPR : 0, dl = lane % LPR;
+    const bool mine = lane / LPR < RPW, on = mine && 8 * dl < L.hd;
+    const int row0 = (warp - 8) * 32 + sub;
+    int qi = 0;   // items so far
+    // V: halves of 64 tokens, in steps of 64 tokens x 64 dims.  A warp takes every eighth step
+    // as a whole, so that the waits, the proxy fence and the shared-memory latency of one lie
+    // beside the work on the others.  Lane: 16 codes at dim 16 (lane % 4) of rows lane / 4,
+    // lane / 4 + 8, ...
     const uint32_t sw = (uint32_t)(lane >> 2), row = (uint32_t)(lane >> 2) * 128u;
     const uint32_t lo = row + ((((uint32_t)lane & 3u) * 2u) ^ sw) * 16u, hi = row + ((((uint32_t)lane & 3u) * 2u + 1u) ^ sw) * 16u;
-    uint64_t *cf = is_k ? ck_full : cv_full, *ce = is_k ? ck_empty : cv_empty;
-    uint64_t *full = is_k ? k_full : v_full, *empty = is_k ? k_empty : v_empty;
-    const uint32_t codes = (is_k ? ck0 : cv0) + 16u * lane, to0 = is_k ? k0 : v0, slot_bytes = is_k ? KU : VH;
-    const int per = is_k ? 2 : NB, ring = is_k ? KS : VS, cring = is_k ? CK : CV;
-    int u = warp & 3, end = 0, qi = 0;   // this warp's next step, the steps so far, the items with Q so far
+    int u = warp - 8, end = 0;   // this warp's next step, the steps so far
     bool ok = true;
     for (int w = blockIdx.x; ok && w < items; w += gridDim.x) {
       const Item it = item_of(a, w);
       if (it.n == 0) continue;
-      if (is_k) {
-        // Q, scaled by the rows' powers of two: 32 rows per warp, 8 NB lanes with 8 dims each
-        // to a row; a batch of loads is on its way while the Q before is still in use
-        constexpr int LPR = 8 * NB, RPW = 32 / LPR, PASS = 32 / RPW;
-        const int sub = lane / LPR, dl = lane % LPR;
-        const bool on = sub < RPW && 8 * dl < L.hd;
-        const bf16* base = (const bf16*)a.q + (size_t)((long long)it.b * a.q_robot) + (size_t)it.h * a.G * L.hd + 8 * dl;
+      if (warp < 12) {
+        // (a row that does not exist reads the last one that does: loads without branches, the
+        // eight of a batch on their way together)
+        const uint32_t end_row = (uint32_t)(it.s.count * a.G);
+        const bf16* base = (const bf16*)a.q + (size_t)((long long)it.b * a.q_robot) + (size_t)it.h * a.G * L.hd + (on ? 8 * dl : 0);
+        uint32_t r = (uint32_t)(it.tile * BM + row0), i = r / (uint32_t)a.G, g = r - i * (uint32_t)a.G;
 #pragma unroll 1
         for (int p0 = 0; p0 < PASS; p0 += 8) {
           uint4 x[8];
+          uint32_t there = 0u;
+          const bf16* at[8];
 #pragma unroll
           for (int p = 0; p < 8; ++p) {
-            const uint32_t r = (uint32_t)(it.tile * BM + (warp - 8) * 32 + (p0 + p) * RPW + sub), i = r / (uint32_t)a.G;
-            const bf16* at = base + (size_t)((long long)i * a.q_token) + (size_t)(r - i * a.G) * L.hd;
-            x[p] = make_uint4(0u, 0u, 0u, 0u);
-            if (on && (int)i < it.s.count) {
-              if (a.vec) {
-                x[p] = __ldg((const uint4*)at);
-              } else {
-                bf16 y[8];
-#pragma unroll
-                for (int z = 0; z < 8; ++z) y[z] = at[z];
-                memcpy(&x[p], y, 16);
-              }
+            if (r < end_row) {
+              there |= on ? 1u << p : 0u;
+              at[p] = base + (size_t)((long long)i * a.q_token) + (size_t)g * L.hd;
+            } else {
+              at[p] = base;   // (row 0 of the tile's robot)
+            }
+            r += RPW;
+            g += RPW;
+            while (g >= (uint32_t)a.G) {
+              g -= (uint32_t)a.G;
+              ++i;
             }
           }
-          if (p0 == 0 && qi > 0) {
-            ok = mbar_wait_warp(q_empty, (uint32_t)(qi - 1) & 1u);
-            if (!ok) break;
+          if (a.vec) {
+#pragma unroll
+            for (int p = 0; p < 8; ++p) x[p] = __ldg((const uint4*)at[p]);
+          } else {
+#pragma unroll
+            for (int p = 0; p < 8; ++p) {
+              bf16 y[8];
+#pragma unroll
+              for (int z = 0; z < 8; ++z) y[z] = at[p][z];
+              memcpy(&x[p], y, 16);
+            }
           }
+          uint32_t exps[2] = {0u, 0u};   // the rows' exponent bits
 #pragma unroll
           for (int p = 0; p < 8; ++p) {
-            const uint32_t y[4] = {x[p].x, x[p].y, x[p].z, x[p].w};
-            uint32_t top = 0u;   // bits of the largest magnitude: NaN counts as larger than all
-#pragma unroll
-            for (int z = 0; z < 4; ++z) top = max(top, max((y[z] & 0x7fffu) << 16, y[z] & 0x7fff0000u));
+            const bool t = there >> p & 1u;
+            const uint32_t y[4] = {t ? x[p].x : 0u, t ? x[p].y : 0u, t ? x[p].z : 0u, t ? x[p].w : 0u};
+            // the largest magnitude's bits: NaN counts as larger than all
+            uint32_t top = __vmaxu2(__vmaxu2(y[0] & 0x7fff7fffu, y[1] & 0x7fff7fffu), __vmaxu2(y[2] & 0x7fff7fffu, y[3] & 0x7fff7fffu));
+            top = max(top >> 16, top & 0xffffu);
             if (RPW == 1) {
               top = __reduce_max_sync(0xffffffffu, top);
             } else {
 #pragma unroll
               for (int o = 1; o < LPR; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
             }
-            const float f = top >= 0x7f800000u ? __int_as_float(0x7fffffff) : exp2i(min(14 - ((int)(top >> 23) - 127), 126));
-            uint32_t o4[4];
+            const int e = (int)(top >> 7);
+            const float f = e == 255 ? __int_as_float(0x7fffffff) : exp2i(min(kQExp + 127 - e, 126));
+            uint32_t hi[2], lo[2];
 #pragma unroll
-            for (int z = 0; z < 4; ++z) o4[z] = pack_f16x2(__uint_as_float(y[z] << 16) * f, __uint_as_float(y[z] & 0xffff0000u) * f);
-            const int lr = (warp - 8) * 32 + (p0 + p) * RPW + sub;
-            if (sub < RPW) {
-              sts_u4(q0 + (uint32_t)(dl >> 3) * QB + (uint32_t)lr * 128u + (uint32_t)(((dl & 7) ^ (lr & 7)) * 16),
-                     make_uint4(o4[0], o4[1], o4[2], o4[3]));
-              if (dl == 0) row_exp[(qi & 3) * BM + lr] = (uint8_t)(top >> 23);
+            for (int z = 0; z < 2; ++z) {
+              const uint32_t h0 = pack_f16x2(__uint_as_float(y[2 * z] << 16) * f, __uint_as_float(y[2 * z] & 0xffff0000u) * f);
+              const uint32_t h1 = pack_f16x2(__uint_as_float(y[2 * z + 1] << 16) * f, __uint_as_float(y[2 * z + 1] & 0xffff0000u) * f);
+              hi[z] = f16_to_e4m3(h0) | f16_to_e4m3(h1) << 16;
+              lo[z] = f16_to_e4m3(f16_sub(h0, e4m3_lo(hi[z]))) | f16_to_e4m3(f16_sub(h1, e4m3_hi(hi[z]))) << 16;
+            }
+            x[p] = make_uint4(hi[0], hi[1], lo[0], lo[1]);
+            exps[p >> 2] |= (uint32_t)e << (8 * (p & 3));
+          }
+          if (p0 == 0 && qi > 0) {
+            ok = wait_phase(q_empty, (uint32_t)(qi - 1) & 1u);
+            if (!ok) break;
+          }
+#pragma unroll
+          for (int p = 0; p < 8; ++p) {
+            const int lr = row0 + (p0 + p) * RPW;
+            if (mine) {
+              const uint32_t to = q0 + (uint32_t)(dl >> 3) * QB + (uint32_t)lr * 64u +
+                                  (uint32_t)((((dl >> 1) & 3) ^ ((lr >> 1) & 3)) * 16 + (dl & 1) * 8);
+              sts_u2(to, x[p].x, x[p].y);
+              sts_u2(to + NB * QB, x[p].z, x[p].w);
+              if (dl == 0) row_exp[(qi & 3) * BM + lr] = (uint8_t)(exps[p >> 2] >> (8 * (p & 3)));
             }
           }
         }
         if (!ok) break;
         written(q_full);
         ++qi;
+        // the next item's Q comes to L2 meanwhile: lane's row
+        if (w + (int)gridDim.x < items) {
+          const Item nx = item_of(a, w + gridDim.x);
+          const uint32_t r2 = (uint32_t)(nx.tile * BM + (warp - 8) * 32 + lane), i2 = r2 / (uint32_t)a.G;
+          if (nx.n > 0 && r2 < (uint32_t)(nx.s.count * a.G)) {
+            const char* at = (const char*)((const bf16*)a.q + (size_t)((long long)nx.b * a.q_robot + (long long)i2 * a.q_token) +
+                                           (size_t)(nx.h * a.G + (int)(r2 - i2 * a.G)) * L.hd);
+            for (int z = 0; z < 2 * L.hd; z += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(at + z));
+          }
+        }
       }
-      end += is_k ? it.n * NB * 2 : it.halves() * NB;
-      for (; u < end; u += 4) {
-        const int cs = u % cring, part = u / per, slot = part % ring;
-        ok = mbar_wait_warp(&cf[cs], (uint32_t)(u / cring) & 1u);
+      end += it.halves() * NB;
+      for (; u < end; u += 8) {
+        const int cs = u % CV, part = u / NB, slot = part % VS;
+        ok = wait_phase(&cv_full[cs], (uint32_t)(u / CV) & 1u);
         if (!ok) break;
         uint4 x[8];
 #pragma unroll
-        for (int y = 0; y < 8; ++y) x[y] = lds_u4(codes + (uint32_t)cs * CB + 512u * y);
-        ok = mbar_wait_warp(&empty[slot], ((uint32_t)(part / ring) & 1u) ^ 1u);
+        for (int y = 0; y < 8; ++y) x[y] = lds_u4(cv0 + (uint32_t)cs * CB + 16u * lane + 512u * y);
+        ok = wait_phase(&v_empty[slot], ((uint32_t)(part / VS) & 1u) ^ 1u);
         if (!ok) break;
         __syncwarp();   // every lane has its codes
-        if (lane == 0) mbar_arrive(&ce[cs]);
-        const uint32_t to = to0 + (uint32_t)slot * slot_bytes + (uint32_t)(u % per) * VB;
+        if (lane == 0) mbar_arrive(&cv_empty[cs]);
+        const uint32_t to = v0 + (uint32_t)slot * VH + (uint32_t)(u % NB) * VB;
 #pragma unroll
         for (int y = 0; y < 8; ++y) widen(x[y], to + lo + 1024u * y, to + hi + 1024u * y);
-        written(&full[slot]);
+        written(&v_full[slot]);
       }
     }
     if (!ok && lane == 0) *abort_flag = 1;
   } else if (warp >= 16) {
     regs_down<48>();
     if (warp == 16) {
-      // ---- MMAs: S of the next tile as soon as its K is there, P V of the oldest whose P is;
-      // S runs at most one tile ahead, into the next item where this one ends
+      // ---- MMAs, in the order S 0, S 1, P V 0, S 2, P V 1, S 3, ...: two tiles of scores in
+      // flight, into the next item where this one ends
       const uint32_t el = elect_one();
       const uint32_t idesc_s = idesc_f16(BM, BT), idesc_o = idesc_f16(BM, HDP) | (1u << 16);
-      const uint64_t qd0 = sw128_desc(q0), kd0 = sw128_desc(k0), vd0 = sw128_mn_desc(v0, VB);
+      const uint64_t qd0 = sw64_desc(q0), kd0 = sw64_desc(k0), vd0 = sw128_mn_desc(v0, VB);
       // the next item with tiles from w on: its tiles, and the last one's groups of 16 tokens
       auto next = [&](int& w, int& n, int& last) {
         n = 0;
         for (; w < items; w += gridDim.x) {
           const Item it = item_of(a, w);
-          if (it.n == 0) continue;
-          n = it.n;
-          last = it.groups(n - 1);
+          n = uniform(it.n);
+          if (n == 0) continue;
+          last = uniform(it.groups(n - 1));
           w += gridDim.x;
           return;
         }
@@ -376,23 +466,29 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
       int si = 0, pi = 0, sq = 0, pq = 0;             // tiles done of them; items begun
       int gs = 0, gp = 0;                             // tiles in all
       int sk = 0, sv = 0;
-      uint32_t phk = 0, phv = 0, spins = 0;
+      uint32_t phk = 0, phv = 0;
       bool ok = true;
       next(ws, sn, s_last);
-      next(wp, pn, last);
-      while (ok && pn > 0) {
-        bool progress = false;
-        if (sn > 0 && gs <= gp + 1 && (si > 0 || mbar_test_warp(q_full, (uint32_t)sq & 1u)) && mbar_test_warp(&k_full[sk], phk)) {
+      wp = ws;
+      pn = sn;
+      last = s_last;
+      while (pn > 0) {
+        while (sn > 0 && gs <= gp + 1) {
+          if (si == 0) {   // (P V of what is in flight does not wait for the next item's Q)
+            if (gs > gp && !mbar_test_warp(q_full, (uint32_t)sq & 1u)) break;
+            ok = wait_phase(q_full, (uint32_t)sq & 1u);
+          }
           const uint32_t sd = tmem + (uint32_t)(gs & 1) * BT;
           uint64_t ad = qd0;
 #pragma unroll 1
-          for (int blk = 0; blk < NB; ++blk, ad += QB >> 4) {
-            if (blk) ok = mbar_wait_warp(&k_full[sk], phk);
+          for (int blk = 0; ok && blk < NB; ++blk, ad += QB >> 4) {
+            ok = wait_phase(&k_full[sk], phk);
             if (!ok) break;
             tc_fence_after();
             const uint64_t bd = kd0 + (uint32_t)sk * (KU >> 4);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) umma_bf16(sd, ad + 2 * k, bd + 2 * k, idesc_s, (blk > 0 || k > 0) ? 1u : 0u, el);
+            for (int k = 0; k < 4; ++k)   // both pieces of Q
+              umma_e4m3(sd, ad + (k >> 1) * (NB * QB >> 4) + 2 * (k & 1), bd + 2 * (k & 1), idesc_s, (blk > 0 || k > 0) ? 1u : 0u, el);
             umma_commit(&k_empty[sk], el);
             if (++sk == KS) {
               sk = 0;
@@ -408,44 +504,40 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
             ++sq;
             next(ws, sn, s_last);
           }
-          progress = true;
         }
-        if (gp < gs && mbar_test_warp(&p_full[gp & 1], (uint32_t)(gp >> 1) & 1u) && mbar_test_warp(&v_full[sv], phv) &&
-            (pi > 0 || pq == 0 || mbar_test_warp(o_free, (uint32_t)(pq - 1) & 1u))) {
-          const uint32_t pa = tmem + (uint32_t)(gp & 1) * BT;
-          const int groups = pi + 1 < pn ? BT / 16 : last;
+        if (ok) ok = wait_phase(&p_full[gp & 1], (uint32_t)(gp >> 1) & 1u);
+        if (ok && pi == 0 && pq > 0) ok = wait_phase(o_free, (uint32_t)(pq - 1) & 1u);
+        if (!ok) break;
+        const uint32_t pa = tmem + (uint32_t)(gp & 1) * BT;
+        const int groups = pi + 1 < pn ? BT / 16 : last;
 #pragma unroll 1
-          for (int hv = 0; 4 * hv < groups; ++hv) {
-            if (hv) ok = mbar_wait_warp(&v_full[sv], phv);
-            if (!ok) break;
-            tc_fence_after();
-            const uint64_t bd = vd0 + (uint32_t)sv * (VH >> 4);
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              if (4 * hv + k < groups)
-                umma_bf16_ts(tmem + o_col, pa + 8 * (4 * hv + k), bd + 128 * k, idesc_o, (pi + hv + k > 0) ? 1u : 0u, el);
-            umma_commit(&v_empty[sv], el);
-            if (++sv == VS) {
-              sv = 0;
-              phv ^= 1u;
-            }
-          }
+        for (int hv = 0; 4 * hv < groups; ++hv) {
+          ok = wait_phase(&v_full[sv], phv);
           if (!ok) break;
-          umma_commit(&pv_done[gp & 1], el);
-          ++gp;
-          if (++pi == pn) {
-            pi = 0;
-            ++pq;
-            next(wp, pn, last);
+          tc_fence_after();
+          const uint64_t bd = vd0 + (uint32_t)sv * (VH >> 4);
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (4 * hv + k < groups)
+              umma_bf16_ts(tmem + o_col, pa + 8 * (4 * hv + k), bd + 128 * k, idesc_o, (pi + hv + k > 0) ? 1u : 0u, el);
+          umma_commit(&v_empty[sv], el);
+          if (++sv == VS) {
+            sv = 0;
+            phv ^= 1u;
           }
-          progress = true;
         }
-        spins = progress ? 0u : spins + 1u;
-        if (spins > kPolls) ok = false;
+        if (!ok) break;
+        umma_commit(&pv_done[gp & 1], el);
+        ++gp;
+        if (++pi == pn) {
+          pi = 0;
+          ++pq;
+          next(wp, pn, last);
+        }
       }
       if (!ok) {   // what was issued ends before the TMEM goes away
         umma_commit(ended, el);
-        mbar_wait_warp(ended, 0);
+        wait_phase(ended, 0);
         if (lane == 0) *abort_flag = 1;
       }
       __syncwarp();
@@ -453,9 +545,8 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
       // ---- the codes' loads
       const uint32_t el = elect_one();
       const bool is_k = warp == 17;
-      const uint32_t to = is_k ? ck0 : cv0;
-      const int ring = is_k ? CK : CV;
-      uint64_t *cf = is_k ? ck_full : cv_full, *ce = is_k ? ck_empty : cv_empty;
+      const int ring = is_k ? KS : CV;
+      uint64_t *full = is_k ? k_full : cv_full, *empty = is_k ? k_empty : cv_empty;
       uint64_t pol;
       asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(pol));
       int slot = 0, issued = 0;
@@ -463,17 +554,27 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
       bool ok = true;
       for (int w = blockIdx.x; ok && w < items; w += gridDim.x) {
         const Item it = item_of(a, w);
-        const int y0 = it.head * L.T;
-        // K: a tile's units, each two halves of 64 tokens; V: its halves, each NB blocks of 64 dims
-        const int halves = it.halves();
-        for (int i = 0; ok && i < it.n; ++i) {
-          const int j0 = y0 + it.token(i), steps = NB * (is_k ? 2 : min(2, halves - 2 * i));
+        const int y0 = it.head * L.T, n = uniform(it.n);
+        // a (robot, KV head)'s codes come to L2 as its first items begin, up to 256 KB of them
+        // (its row tiles ask for the same lines at the same time)
+        if (it.n > 0 && (it.tile & 7) == 0 && el) {
+          const size_t from = ((size_t)y0 + it.token(0)) * HDP;
+          prefetch_l2_bulk((is_k ? L.k : L.v) + from, (uint32_t)min((size_t)it.n * BT * HDP, (size_t)(256 << 10)));
+        }
+        // K: a tile's units of 64 dims; V: its halves of 64 tokens, each NB blocks of 64 dims
+        const int halves = uniform(it.halves());
+        for (int i = 0; ok && i < n; ++i) {
+          const int j0 = uniform(y0 + it.token(i)), steps = NB * (is_k ? 1 : min(2, halves - 2 * i));
           for (int q = 0; q < steps; ++q) {
-            ok = mbar_wait_warp(&ce[slot], ph);
+            ok = wait_phase(&empty[slot], ph);
             if (!ok) break;
-            const int half = is_k ? q & 1 : q / NB, blk = is_k ? q >> 1 : q % NB;
-            mbar_expect_tx_el(&cf[slot], CB, el);
-            tma_load_2d_el(is_k ? &maps.k : &maps.v, smem_u32(&cf[slot]), to + (uint32_t)slot * CB, 64 * blk, j0 + 64 * half, pol, el);
+            if (is_k) {
+              mbar_expect_tx_el(&full[slot], KU, el);
+              tma_load_2d_el(&maps.k, smem_u32(&full[slot]), k0 + (uint32_t)slot * KU, 64 * q, j0, pol, el);
+            } else {
+              mbar_expect_tx_el(&full[slot], CB, el);
+              tma_load_2d_el(&maps.v, smem_u32(&full[slot]), cv0 + (uint32_t)slot * CB, 64 * (q % NB), j0 + 64 * (q / NB), pol, el);
+            }
             ++issued;
             if (++slot == ring) {
               slot = 0;
@@ -483,7 +584,7 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
         }
       }
       if (lane == 0) {
-        c_issued[is_k ? 0 : 1] = issued;
+        issued_flag[is_k ? 0 : 1] = issued;
         if (!ok) *abort_flag = 1;
       }
       __syncwarp();
@@ -525,10 +626,10 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
         // exponents of this half's four blocks
         const uint32_t kes = *(const uint32_t*)(KE + j0 / 16 + 4 * hf), ves = *(const uint32_t*)(VE + j0 / 16 + 4 * hf);
         const bool full = j0 + BT <= firstm.hi && (j0 >= lastm.lo || j0 + BT <= a.sinks);
-        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&s_full[gt & 1], (uint32_t)(gt >> 1) & 1u));
+        if (ok) ok = wait_phase(&s_full[gt & 1], (uint32_t)(gt >> 1) & 1u);
         tc_fence_after();
         if (i == 0) {   // (S needed Q: it is there.  Rows whose largest |q| is below 2^-112 keep fewer bits; -e >= -126)
-          rf = exp2i(-min(14 - ((int)row_exp[(qi & 3) * BM + r] - 127), 126)) * a.scale_log2;
+          rf = exp2i(-min(kQExp + 127 - (int)row_exp[(qi & 3) * BM + r], 126)) * a.scale_log2;
           ++qi;
         }
         float sc[64];
@@ -544,9 +645,12 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
           for (int k = 0; k < 64; ++k) sc[k] = __uint_as_float(raw[k]);
         }
         if (!full) {
-          const int jh = j0 + 64 * hf;
 #pragma unroll
-          for (int k = 0; k < 64; ++k) sc[k] = mk.sees(jh + k) ? sc[k] : -INFINITY;
+          for (int k2 = 0; k2 < 64; k2 += 32) {
+            const uint32_t see = mk.bits(j0 + 64 * hf + k2);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) sc[k2 + k] = see >> k & 1u ? sc[k2 + k] : -INFINITY;
+          }
         }
         float f[4], mx = -INFINITY, wx = -INFINITY;
 #pragma unroll
@@ -573,9 +677,10 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
         const bool need = wn > W + 8.f;
         if (i > 0 && __any_sync(0xffffffffu, need)) {
           // O holds P V of every earlier tile before it is rescaled
-          if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&pv_done[(gt - 1) & 1], (uint32_t)((gt - 1) >> 1) & 1u));
+          if (ok) ok = wait_phase(&pv_done[(gt - 1) & 1], (uint32_t)((gt - 1) >> 1) & 1u);
           tc_fence_after();
           const float alpha = need ? pow2f_down(W - wn) : 1.f;
+#pragma unroll 1
           for (int cb = 16 * hf; cb < HDP; cb += 32) {
             float o[16];
             tmem_ld16(lane_base + o_col + cb, o);
@@ -613,25 +718,22 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
         mbar_arrive(&p_full[gt & 1]);
       }
       if (ok && n > 0) {
-        ok = __all_sync(0xffffffffu, mbar_wait(&pv_done[(gt - 1) & 1], (uint32_t)((gt - 1) >> 1) & 1u));
+        ok = wait_phase(&pv_done[(gt - 1) & 1], (uint32_t)((gt - 1) >> 1) & 1u);
         tc_fence_after();
       }
       xm[hf * 128 + r].x = l;
       pair_bar();
-      l = xm[r].x + xm[128 + r].x;
+      l = xm[r].x + xm[128 + r].x;   // (read before the next tile's first barrier)
       pair_bar();
       const bool real = mk.hi > 0 && n > 0 && !(l <= 0.f);   // (a sum that is not a number stays one)
       const float inv = real ? pow2f(W - m) / l : 0.f;
       const float m_out = real ? m : -INFINITY, l_out = real ? l : 0.f;
       if (a.splits == 1) {
         if (a.mass && hf == 0 && r < rows) a.row_ml[head * a.n * a.G + r0 + r] = row_weight(m_out, l_out, kTcShift);
-        // O / l as bf16, 32 columns at a time: through the warp's own staging, from where four
-        // lanes store 64 bytes of a row
-        const uint32_t stg = st0 + 2048u * warp;
-        bf16* dst[4];
-#pragma unroll
-        for (int z = 0; z < 4; ++z) dst[z] = out_row(min(q4 * 32 + (lane >> 2) + 8 * z, rows - 1)) + 8 * (lane & 3);
-        for (int cb = 32 * hf; cb < HDP; cb += 64) {   // (the halves take alternate columns)
+        // O / l as bf16, each thread's columns of its row
+        bf16* dst = out_row(min(r, rows - 1));
+#pragma unroll 1
+        for (int cb = 32 * hf; cb < HDP; cb += 64) {   // (the warpgroups take alternate columns)
           uint32_t raw[32];
           tmem_ld32_async(lane_base + o_col + cb, raw);
           tmem_wait_ld();
@@ -642,22 +744,15 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
             __syncwarp();
             if (lane == 0) mbar_arrive(o_free);
           }
+          uint32_t wd[16];
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            uint32_t wd[4];
+          for (int q = 0; q < 16; ++q)
+            wd[q] = real ? pack_bf16x2(__uint_as_float(raw[2 * q]) * inv, __uint_as_float(raw[2 * q + 1]) * inv) : 0u;
+          if (r < rows) {
 #pragma unroll
-            for (int z = 0; z < 4; ++z)
-              wd[z] = real ? pack_bf16x2(__uint_as_float(raw[8 * q + 2 * z]) * inv, __uint_as_float(raw[8 * q + 2 * z + 1]) * inv) : 0u;
-            sts_u4(stg + 64u * lane + (uint32_t)((q ^ ((lane >> 1) & 3)) * 16), make_uint4(wd[0], wd[1], wd[2], wd[3]));
+            for (int q = 0; q < 4; ++q)
+              if (cb + 8 * q < L.hd) store_bf16x8(dst + cb + 8 * q, make_uint4(wd[4 * q], wd[4 * q + 1], wd[4 * q + 2], wd[4 * q + 3]), wide);
           }
-          __syncwarp();
-#pragma unroll
-          for (int z = 0; z < 4; ++z) {
-            const int lr = (lane >> 2) + 8 * z;
-            const uint4 x = lds_u4(stg + 64u * lr + (uint32_t)(((lane & 3) ^ ((lr >> 1) & 3)) * 16));
-            if (q4 * 32 + lr < rows && cb + 8 * (lane & 3) < L.hd) store_bf16x8(dst[z] + cb, x, wide);
-          }
-          __syncwarp();
         }
         continue;
       }
@@ -667,6 +762,7 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
       const bool cluster = a.splits <= kTcCluster;
       const size_t unit = head * a.row_tiles + it.tile;
       constexpr uint32_t XR = Shape::xrow;
+#pragma unroll 1
       for (int cb = 32 * hf; cb < HDP; cb += 64) {
         uint32_t raw[32];
         tmem_ld32_async(lane_base + o_col + cb, raw);
@@ -687,7 +783,9 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
       }
       int ra = 0, rb = rows;
       if (cluster) {
-        if (hf == 0) xm[r] = make_float2(m_out, l_out);
+        if (hf == 0) {
+          xm[r] = make_float2(m_out, l_out);
+        }
         cluster_sync();   // (the other roles arrive below)
         const int share = (rows + a.splits - 1) / a.splits;
         ra = it.split * share;
@@ -703,15 +801,19 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
       }
       // the splits' weights per row, [splits][128], into Q's place (every S has completed)
       // or, where they may be many, the rings' ...
-      float* wts = (float*)(smem + (cluster ? 0 : NB * QB));
+      float* wts = (float*)(smem + (cluster ? 0 : Shape::q_bytes));
       for (int rr = ra + threadIdx.x; rr < rb; rr += 256) {
-        const uint32_t xml = smem_u32(xm) + 8u * rr;
         const float2* ml = a.part_ml + unit * a.splits * BM + rr;
+        const uint32_t xml = smem_u32(xm) + 8u * rr;
+        auto split_ml = [&](int q) {
+          if (!cluster) return __ldcg(ml + q * BM);
+          const uint32_t at = mapa_shared(xml, (uint32_t)q);
+          return make_float2(ld_cluster_f1(at), ld_cluster_f1(at + 4));
+        };
         float M = -INFINITY, S = 0.f;
-        for (int q = 0; q < a.splits; ++q)
-          M = fmaxf(M, cluster ? ld_cluster_f2(mapa_shared(xml, (uint32_t)q)).x : __ldcg(ml + q * BM).x);
+        for (int q = 0; q < a.splits; ++q) M = fmaxf(M, split_ml(q).x);
         for (int q = 0; q < a.splits; ++q) {
-          const float2 x = cluster ? ld_cluster_f2(mapa_shared(xml, (uint32_t)q)) : __ldcg(ml + q * BM);
+          const float2 x = split_ml(q);
           const float wt = x.y != x.y ? x.y : (x.x == -INFINITY ? 0.f : exp2f(x.x - M) * x.y);
           wts[q * BM + rr] = wt;
           S += wt;
@@ -767,8 +869,8 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
   cta_sync();
   if (*abort_flag && threadIdx.x == 0) {
     // loads still on their way, at most a ring of them, land before the shared memory goes away
-    for (int i = max(0, c_issued[0] - CK); i < c_issued[0]; ++i) mbar_wait(&ck_full[i % CK], (uint32_t)(i / CK) & 1u);
-    for (int i = max(0, c_issued[1] - CV); i < c_issued[1]; ++i) mbar_wait(&cv_full[i % CV], (uint32_t)(i / CV) & 1u);
+    for (int i = max(0, issued_flag[0] - KS); i < issued_flag[0]; ++i) mbar_wait(&k_full[i % KS], (uint32_t)(i / KS) & 1u);
+    for (int i = max(0, issued_flag[1] - CV); i < issued_flag[1]; ++i) mbar_wait(&cv_full[i % CV], (uint32_t)(i / CV) & 1u);
     raise_error(a.err, ERR_TIMEOUT);
   }
   if (warp == 16)
@@ -777,12 +879,12 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
 
 PFN_cuTensorMapEncodeTiled_v12000 g_enc = nullptr;
 
-cudaError_t encode_codes(CUtensorMap* m, const uint8_t* base, const CacheLayer& c, int batch) {
+cudaError_t encode_codes(CUtensorMap* m, const uint8_t* base, const CacheLayer& c, int batch, int box_rows, bool swizzle) {
   cuuint64_t dims[2] = {(cuuint64_t)c.hdp, (cuuint64_t)batch * c.Hkv * c.T};
   cuuint64_t strides[1] = {(cuuint64_t)c.hdp};
-  cuuint32_t box[2] = {64u, 64u}, estr[2] = {1, 1};
+  cuuint32_t box[2] = {64u, (cuuint32_t)box_rows}, estr[2] = {1, 1};
   const CUresult r = g_enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(base), dims, strides, box, estr,
-                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
@@ -802,8 +904,8 @@ cudaError_t launch_nb(CacheAttnArgs a, cudaStream_t st) {
   if (splits > 1) splits = (units + (units + splits - 1) / splits - 1) / ((units + splits - 1) / splits);
   a.splits = splits;
   TcMaps maps;
-  cudaError_t e = encode_codes(&maps.k, a.c.k, a.c, a.batch);
-  if (e == cudaSuccess) e = encode_codes(&maps.v, a.c.v, a.c, a.batch);
+  cudaError_t e = encode_codes(&maps.k, a.c.k, a.c, a.batch, BT, true);
+  if (e == cudaSuccess) e = encode_codes(&maps.v, a.c.v, a.c, a.batch, 64, false);
   if (e != cudaSuccess) return e;
   // causal prompts: pairs whose caches take 48 MB together (beside the queries, in an L2 of 129)
   const long long pairs = (long long)a.c.Hkv * a.batch;
