@@ -74,6 +74,7 @@ struct CacheAttnArgs {
   float2* part_ml;          // [units * splits][rows of a tile] (max, sum)
   unsigned* arrived;        // [units] splits that have finished (zero between launches)
   float2* row_ml;           // [B][Hkv][n * G] see row_weight, written where mass is wanted
+  uint8_t* q_ws;            // per SM, 128 bytes per row (of 128) and 64 dims: an item's laid out Q
   int* err;
   // chosen by the launcher
   int row_tiles, splits;

@@ -9,7 +9,7 @@
 //   P = 2^(S - m)    softmax warps: TMEM -> registers -> f16 P over S in TMEM
 //   O += P V         tcgen05.mma kind::f16, M = 128, N = head dim, 16 tokens at a time
 // Warp roles (640 threads): warps 0-7 softmax and output, two threads per row; warps
-// 8-11 lay out Q, warps 12-15 widen V; warp 16 TMEM and MMAs; warps 17, 18 load the
+// 8-11 lay out the next item's Q, warps 12-15 widen V; warp 16 TMEM and MMAs; warps 17, 18 load the
 // codes of K and V (19 idle, so that registers move between whole warpgroups).
 // Every role walks the items on its own, so that one item's output lies beside the
 // next one's Q, K and first scores.
@@ -57,11 +57,11 @@ template <int NB> struct TcShape {
   // V halves and of V's codes, barriers and row data
   static constexpr int KS = NB == 4 ? 4 : 8;
   static constexpr int VS = NB >= 3 ? 3 : (NB == 2 ? 4 : 8);
-  // a multiple of the 8 warps that widen them: each slot is then waited for by one warp, in
+  // a multiple of the 4 warps that widen them: each slot is then waited for by one warp, in
   // order.  (Loads may complete out of order; a warp that waits for a slot's next phase while
   // another's load into it is still on its way would take the phase before for it.)
   static constexpr int CV = 8;
-  static_assert(CV % 8 == 0, "widening warps");
+  static_assert(CV % 4 == 0, "widening warps");
   static constexpr uint32_t q_bytes = 2 * NB * QB;
   static constexpr uint32_t ring = KS * KU + VS * NB * VB + CV * CB;
   static constexpr uint32_t bytes = q_bytes + ring + 3072;
@@ -136,6 +136,13 @@ __device__ __forceinline__ uint32_t f16_sub(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
+}
+
+// 32 bytes, 32-byte aligned
+__device__ __forceinline__ void stg_u8(void* p, const uint32_t* w) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+               "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
 }
 
 __device__ __forceinline__ void store_bf16x8(bf16* dst, uint4 w, bool wide) {
@@ -250,16 +257,17 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
   uint64_t* q_full = pv_done + 2;     // an item's Q is laid out ...
   uint64_t* q_empty = q_full + 1;     // ... and its last S has completed
   uint64_t* o_free = q_empty + 1;     // an item's output has been read
-  uint64_t* ended = o_free + 1;
+  uint64_t* q_laid = o_free + 1;      // an item's Q is laid out in L2
+  uint64_t* ended = q_laid + 1;
   uint32_t* tmem_slot = (uint32_t*)(ended + 1);
   int* abort_flag = (int*)(tmem_slot + 1);
   int* last_flag = abort_flag + 1;
-  int* issued_flag = last_flag + 1;               // [2] loads of K and V issued
+  int* issued_flag = last_flag + 1;               // [3] loads of K, V and Q issued
   // exponent bits of the rows' largest |q|, [4][128], by item: S runs up to two tiles, so up
   // to two items, ahead of the softmax, and Q one more
   uint8_t* row_exp = tail + 512;
   float2* xm = (float2*)(row_exp + 512);   // [2][128] row maxima, then sums, of the two halves
-  static_assert((2 * KS + 2 * VS + 2 * CV + 10) * 8 + 20 <= 512, "barriers");
+  static_assert((2 * KS + 2 * VS + 2 * CV + 11) * 8 + 24 <= 512, "barriers");
 
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const CacheLayer& L = a.c;
@@ -287,8 +295,10 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
       mbar_init(&p_full[i], 256);
       mbar_init(&pv_done[i], 1);
     }
-    mbar_init(q_full, 4);
+    mbar_init(q_full, 1);
     mbar_init(q_empty, 1);
+    mbar_init(q_laid, 4);
+    issued_flag[2] = 0;
     mbar_init(o_free, 8);
     mbar_init(ended, 1);
     *abort_flag = 0;
@@ -305,125 +315,146 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
   const uint32_t tmem = *tmem_slot;
   constexpr uint32_t o_col = 2 * BT;
 
-  if (warp >= 8 && warp < 16) {
-    regs_down<80>();
-    // ---- Q (warps 8-11) at an item's start, then, with warps 12-15, the widening of V.
-    // Q: 32 rows per warp, 8 NB lanes with 8 dims each to a row, scaled by the row's power
-    // of two to a largest magnitude in [2^7, 2^8), in two e4m3 pieces: y rounded and what is
-    // left.  A batch of 8 rows per pass is ready before Q's place is free.
-    constexpr int LPR = 8 * NB, RPW = 32 / LPR, PASS = 32 / RPW;
+  // Q rows rb .. rb + 7 of an item (8 NB lanes with 8 dims each to a row), scaled by the row's
+  // power of two to a largest magnitude in [2^7, 2^8), in two e4m3 pieces: y rounded and what
+  // is left.  Into shared memory, or (to) the same layout in L2.
+  auto stage_q8 = [&](const Item& it, int rb, int qi, uint8_t* to) {
+    constexpr int LPR = 8 * NB, RPW = 32 / LPR, PASS = 8 / RPW;
     const int sub = lane / LPR < RPW ? lane / LPR : 0, dl = lane % LPR;
     const bool mine = lane / LPR < RPW, on = mine && 8 * dl < L.hd;
-    const int row0 = (warp - 8) * 32 + sub;
+    // (a row that does not exist reads the robot's first: loads without branches, all on
+    // their way together)
+    const uint32_t end_row = (uint32_t)(it.s.count * a.G);
+    const bf16* base = (const bf16*)a.q + (size_t)((long long)it.b * a.q_robot) + (size_t)it.h * a.G * L.hd + (on ? 8 * dl : 0);
+    uint32_t r = (uint32_t)(it.tile * BM + rb + sub), i = r / (uint32_t)a.G, g = r - i * (uint32_t)a.G, there = 0u;
+    uint4 x[PASS];
+    const bf16* at[PASS];
+#pragma unroll
+    for (int p = 0; p < PASS; ++p) {
+      at[p] = base;
+      if (r < end_row) {
+        there |= on ? 1u << p : 0u;
+        at[p] += (size_t)((long long)i * a.q_token) + (size_t)g * L.hd;
+      }
+      r += RPW;
+      g += RPW;
+      while (g >= (uint32_t)a.G) {
+        g -= (uint32_t)a.G;
+        ++i;
+      }
+    }
+    if (a.vec) {
+#pragma unroll
+      for (int p = 0; p < PASS; ++p) x[p] = __ldg((const uint4*)at[p]);
+    } else {
+#pragma unroll
+      for (int p = 0; p < PASS; ++p) {
+        bf16 y[8];
+#pragma unroll
+        for (int z = 0; z < 8; ++z) y[z] = at[p][z];
+        memcpy(&x[p], y, 16);
+      }
+    }
+#pragma unroll
+    for (int p = 0; p < PASS; ++p) {
+      const bool t = there >> p & 1u;
+      const uint32_t y[4] = {t ? x[p].x : 0u, t ? x[p].y : 0u, t ? x[p].z : 0u, t ? x[p].w : 0u};
+      // the largest magnitude's bits: NaN counts as larger than all
+      uint32_t top = __vmaxu2(__vmaxu2(y[0] & 0x7fff7fffu, y[1] & 0x7fff7fffu), __vmaxu2(y[2] & 0x7fff7fffu, y[3] & 0x7fff7fffu));
+      top = max(top >> 16, top & 0xffffu);
+      if (RPW == 1) {
+        top = __reduce_max_sync(0xffffffffu, top);
+      } else {
+#pragma unroll
+        for (int o = 1; o < LPR; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+      }
+      const int e = (int)(top >> 7);
+      const float f = e == 255 ? __int_as_float(0x7fffffff) : exp2i(min(kQExp + 127 - e, 126));
+      uint32_t hi[2], lo[2];
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const uint32_t h0 = pack_f16x2(__uint_as_float(y[2 * z] << 16) * f, __uint_as_float(y[2 * z] & 0xffff0000u) * f);
+        const uint32_t h1 = pack_f16x2(__uint_as_float(y[2 * z + 1] << 16) * f, __uint_as_float(y[2 * z + 1] & 0xffff0000u) * f);
+        hi[z] = f16_to_e4m3(h0) | f16_to_e4m3(h1) << 16;
+        lo[z] = f16_to_e4m3(f16_sub(h0, e4m3_lo(hi[z]))) | f16_to_e4m3(f16_sub(h1, e4m3_hi(hi[z]))) << 16;
+      }
+      const int lr = rb + p * RPW + sub;
+      if (mine) {
+        const uint32_t off = (uint32_t)(dl >> 3) * QB + (uint32_t)lr * 64u +
+                             (uint32_t)((((dl >> 1) & 3) ^ ((lr >> 1) & 3)) * 16 + (dl & 1) * 8);
+        if (to) {
+          *(uint2*)(to + off) = make_uint2(hi[0], hi[1]);
+          *(uint2*)(to + off + NB * QB) = make_uint2(lo[0], lo[1]);
+        } else {
+          sts_u2(q0 + off, hi[0], hi[1]);
+          sts_u2(q0 + off + NB * QB, lo[0], lo[1]);
+        }
+        if (dl == 0) row_exp[(qi & 3) * BM + lr] = (uint8_t)e;
+      }
+    }
+  };
+  // the first item's Q, by all warps that have nothing else to do yet
+  if (warp < 16) {
+    for (int w = blockIdx.x; w < items; w += gridDim.x) {
+      const Item it = item_of(a, w);
+      if (it.n == 0) continue;
+      stage_q8(it, 8 * warp, 0, nullptr);
+      break;
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    asm volatile("bar.arrive 6, 544;" ::: "memory");   // (with warp 16)
+  }
+
+  if (warp >= 8 && warp < 12) {
+    regs_down<80>();
+    // ---- Q of the items after the first: into the CTA's place in L2 while the item before is
+    // at work, from there into shared memory in one copy as soon as its last S has completed.
+    // (Into shared memory directly, at that time, the rows' 100 instructions each left the
+    // tensor core without Q for 15000 cycles an item.)
+    uint8_t* place = a.q_ws + (size_t)blockIdx.x * Shape::q_bytes;
     int qi = 0;   // items so far
-    // V: halves of 64 tokens, in steps of 64 tokens x 64 dims.  A warp takes every eighth step
+    bool ok = true;
+    for (int w = blockIdx.x; ok && w < items; w += gridDim.x) {
+      const Item it = item_of(a, w);
+      if (it.n == 0) continue;
+      if (qi > 0) {
+        if (qi > 1) ok = wait_phase(q_full, (uint32_t)qi & 1u);   // the item before's copy has been read
+        if (!ok) break;
+#pragma unroll 1
+        for (int rb = 0; rb < 32; rb += 8) stage_q8(it, (warp - 8) * 32 + rb, qi, place);
+        __threadfence();
+        asm volatile("fence.proxy.async;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(q_laid);
+        if (warp == 8) {
+          ok = wait_phase(q_laid, (uint32_t)(qi - 1) & 1u) && wait_phase(q_empty, (uint32_t)(qi - 1) & 1u);
+          if (ok && lane == 0) {
+            mbar_expect_tx(q_full, Shape::q_bytes);
+            asm volatile(
+                "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(q0),
+                "l"(place), "r"(Shape::q_bytes), "r"(smem_u32(q_full))
+                : "memory");
+            issued_flag[2] = qi;
+          }
+          __syncwarp();
+        }
+      }
+      ++qi;
+    }
+    if (!ok && lane == 0) *abort_flag = 1;
+  } else if (warp >= 12 && warp < 16) {
+    regs_down<80>();
+    // ---- widening of V: halves of 64 tokens, in steps of 64 tokens x 64 dims.  A warp takes every fourth step
     // as a whole, so that the waits, the proxy fence and the shared-memory latency of one lie
     // beside the work on the others.  Lane: 16 codes at dim 16 (lane % 4) of rows lane / 4,
     // lane / 4 + 8, ...
     const uint32_t sw = (uint32_t)(lane >> 2), row = (uint32_t)(lane >> 2) * 128u;
     const uint32_t lo = row + ((((uint32_t)lane & 3u) * 2u) ^ sw) * 16u, hi = row + ((((uint32_t)lane & 3u) * 2u + 1u) ^ sw) * 16u;
-    int u = warp - 8, end = 0;   // this warp's next step, the steps so far
+    int u = warp - 12, end = 0;   // this warp's next step, the steps so far
     bool ok = true;
     for (int w = blockIdx.x; ok && w < items; w += gridDim.x) {
-      const Item it = item_of(a, w);
-      if (it.n == 0) continue;
-      if (warp < 12) {
-        // (a row that does not exist reads the last one that does: loads without branches, the
-        // eight of a batch on their way together)
-        const uint32_t end_row = (uint32_t)(it.s.count * a.G);
-        const bf16* base = (const bf16*)a.q + (size_t)((long long)it.b * a.q_robot) + (size_t)it.h * a.G * L.hd + (on ? 8 * dl : 0);
-        uint32_t r = (uint32_t)(it.tile * BM + row0), i = r / (uint32_t)a.G, g = r - i * (uint32_t)a.G;
-#pragma unroll 1
-        for (int p0 = 0; p0 < PASS; p0 += 8) {
-          uint4 x[8];
-          uint32_t there = 0u;
-          const bf16* at[8];
-#pragma unroll
-          for (int p = 0; p < 8; ++p) {
-            if (r < end_row) {
-              there |= on ? 1u << p : 0u;
-              at[p] = base + (size_t)((long long)i * a.q_token) + (size_t)g * L.hd;
-            } else {
-              at[p] = base;   // (row 0 of the tile's robot)
-            }
-            r += RPW;
-            g += RPW;
-            while (g >= (uint32_t)a.G) {
-              g -= (uint32_t)a.G;
-              ++i;
-            }
-          }
-          if (a.vec) {
-#pragma unroll
-            for (int p = 0; p < 8; ++p) x[p] = __ldg((const uint4*)at[p]);
-          } else {
-#pragma unroll
-            for (int p = 0; p < 8; ++p) {
-              bf16 y[8];
-#pragma unroll
-              for (int z = 0; z < 8; ++z) y[z] = at[p][z];
-              memcpy(&x[p], y, 16);
-            }
-          }
-          uint32_t exps[2] = {0u, 0u};   // the rows' exponent bits
-#pragma unroll
-          for (int p = 0; p < 8; ++p) {
-            const bool t = there >> p & 1u;
-            const uint32_t y[4] = {t ? x[p].x : 0u, t ? x[p].y : 0u, t ? x[p].z : 0u, t ? x[p].w : 0u};
-            // the largest magnitude's bits: NaN counts as larger than all
-            uint32_t top = __vmaxu2(__vmaxu2(y[0] & 0x7fff7fffu, y[1] & 0x7fff7fffu), __vmaxu2(y[2] & 0x7fff7fffu, y[3] & 0x7fff7fffu));
-            top = max(top >> 16, top & 0xffffu);
-            if (RPW == 1) {
-              top = __reduce_max_sync(0xffffffffu, top);
-            } else {
-#pragma unroll
-              for (int o = 1; o < LPR; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-            }
-            const int e = (int)(top >> 7);
-            const float f = e == 255 ? __int_as_float(0x7fffffff) : exp2i(min(kQExp + 127 - e, 126));
-            uint32_t hi[2], lo[2];
-#pragma unroll
-            for (int z = 0; z < 2; ++z) {
-              const uint32_t h0 = pack_f16x2(__uint_as_float(y[2 * z] << 16) * f, __uint_as_float(y[2 * z] & 0xffff0000u) * f);
-              const uint32_t h1 = pack_f16x2(__uint_as_float(y[2 * z + 1] << 16) * f, __uint_as_float(y[2 * z + 1] & 0xffff0000u) * f);
-              hi[z] = f16_to_e4m3(h0) | f16_to_e4m3(h1) << 16;
-              lo[z] = f16_to_e4m3(f16_sub(h0, e4m3_lo(hi[z]))) | f16_to_e4m3(f16_sub(h1, e4m3_hi(hi[z]))) << 16;
-            }
-            x[p] = make_uint4(hi[0], hi[1], lo[0], lo[1]);
-            exps[p >> 2] |= (uint32_t)e << (8 * (p & 3));
-          }
-          if (p0 == 0 && qi > 0) {
-            ok = wait_phase(q_empty, (uint32_t)(qi - 1) & 1u);
-            if (!ok) break;
-          }
-#pragma unroll
-          for (int p = 0; p < 8; ++p) {
-            const int lr = row0 + (p0 + p) * RPW;
-            if (mine) {
-              const uint32_t to = q0 + (uint32_t)(dl >> 3) * QB + (uint32_t)lr * 64u +
-                                  (uint32_t)((((dl >> 1) & 3) ^ ((lr >> 1) & 3)) * 16 + (dl & 1) * 8);
-              sts_u2(to, x[p].x, x[p].y);
-              sts_u2(to + NB * QB, x[p].z, x[p].w);
-              if (dl == 0) row_exp[(qi & 3) * BM + lr] = (uint8_t)(exps[p >> 2] >> (8 * (p & 3)));
-            }
-          }
-        }
-        if (!ok) break;
-        written(q_full);
-        ++qi;
-        // the next item's Q comes to L2 meanwhile: lane's row
-        if (w + (int)gridDim.x < items) {
-          const Item nx = item_of(a, w + gridDim.x);
-          const uint32_t r2 = (uint32_t)(nx.tile * BM + (warp - 8) * 32 + lane), i2 = r2 / (uint32_t)a.G;
-          if (nx.n > 0 && r2 < (uint32_t)(nx.s.count * a.G)) {
-            const char* at = (const char*)((const bf16*)a.q + (size_t)((long long)nx.b * a.q_robot + (long long)i2 * a.q_token) +
-                                           (size_t)(nx.h * a.G + (int)(r2 - i2 * a.G)) * L.hd);
-            for (int z = 0; z < 2 * L.hd; z += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(at + z));
-          }
-        }
-      }
-      end += it.halves() * NB;
-      for (; u < end; u += 8) {
+      end += item_of(a, w).halves() * NB;
+      for (; u < end; u += 4) {
         const int cs = u % CV, part = u / NB, slot = part % VS;
         ok = wait_phase(&cv_full[cs], (uint32_t)(u / CV) & 1u);
         if (!ok) break;
@@ -468,6 +499,7 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
       int sk = 0, sv = 0;
       uint32_t phk = 0, phv = 0;
       bool ok = true;
+      asm volatile("bar.sync 6, 544;" ::: "memory");
       next(ws, sn, s_last);
       wp = ws;
       pn = sn;
@@ -475,8 +507,9 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
       while (pn > 0) {
         while (sn > 0 && gs <= gp + 1) {
           if (si == 0) {   // (P V of what is in flight does not wait for the next item's Q)
-            if (gs > gp && !mbar_test_warp(q_full, (uint32_t)sq & 1u)) break;
-            ok = wait_phase(q_full, (uint32_t)sq & 1u);
+            // (the first item's came through barrier 6)
+            if (sq > 0 && gs > gp && !mbar_test_warp(q_full, (uint32_t)(sq - 1) & 1u)) break;
+            if (sq > 0) ok = wait_phase(q_full, (uint32_t)(sq - 1) & 1u);
           }
           const uint32_t sd = tmem + (uint32_t)(gs & 1) * BT;
           uint64_t ad = qd0;
@@ -595,7 +628,8 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
     const int q4 = warp & 3, hf = warp >> 2, r = q4 * 32 + lane;
     auto pair_bar = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory"); };   // warps w and w + 4
     const uint32_t lane_base = tmem + ((uint32_t)(q4 * 32) << 16);
-    const bool wide = ((uintptr_t)a.out | (uintptr_t)(a.out_robot * 2) | (uintptr_t)(a.out_token * 2)) % 16 == 0;
+    const uintptr_t places = (uintptr_t)a.out | (uintptr_t)(a.out_robot * 2) | (uintptr_t)(a.out_token * 2);
+    const bool wide = places % 16 == 0, wider = (places | (uintptr_t)(L.hd * 2)) % 32 == 0;
     bool ok = true;   // (after a wait that ran out the loops go on without waiting, so that pairs meet at every barrier)
     int gt = 0, qi = 0;   // tiles and items with Q so far
     for (int w = blockIdx.x; w < items; w += gridDim.x) {
@@ -748,7 +782,12 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
 #pragma unroll
           for (int q = 0; q < 16; ++q)
             wd[q] = real ? pack_bf16x2(__uint_as_float(raw[2 * q]) * inv, __uint_as_float(raw[2 * q + 1]) * inv) : 0u;
-          if (r < rows) {
+          if (r >= rows) continue;
+          if (wider) {   // (half the requests of 16-byte stores, each to 32 rows)
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+              if (cb + 16 * q < L.hd) stg_u8(dst + cb + 16 * q, wd + 8 * q);
+          } else {
 #pragma unroll
             for (int q = 0; q < 4; ++q)
               if (cb + 8 * q < L.hd) store_bf16x8(dst + cb + 8 * q, make_uint4(wd[4 * q], wd[4 * q + 1], wd[4 * q + 2], wd[4 * q + 3]), wide);
@@ -870,6 +909,7 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
   if (*abort_flag && threadIdx.x == 0) {
     // loads still on their way, at most a ring of them, land before the shared memory goes away
     for (int i = max(0, issued_flag[0] - KS); i < issued_flag[0]; ++i) mbar_wait(&k_full[i % KS], (uint32_t)(i / KS) & 1u);
+    if (issued_flag[2] > 0) mbar_wait(q_full, (uint32_t)(issued_flag[2] - 1) & 1u);
     for (int i = max(0, issued_flag[1] - CV); i < issued_flag[1]; ++i) mbar_wait(&cv_full[i % CV], (uint32_t)(i / CV) & 1u);
     raise_error(a.err, ERR_TIMEOUT);
   }

@@ -26,6 +26,7 @@ struct ravel_cache_ctx {
   float* part = nullptr;
   float2 *part_ml = nullptr, *row_ml = nullptr;
   unsigned* arrived = nullptr;
+  uint8_t* q_ws = nullptr;
   ErrorWord* err = nullptr;
   int* err_host = nullptr;       // pinned, mapped: the error word's mirror
   std::vector<void*> allocs;
@@ -137,6 +138,7 @@ ravel_status ravel_cache_create(const ravel_cache_config* cfg, int device, ravel
   get(&c->part_ml, sizeof(float2) * part_rows);
   get(&c->arrived, sizeof(unsigned) * kCacheSplitCtas);
   get(&c->row_ml, sizeof(float2) * cfg->max_batch * (size_t)cfg->n_q_heads * cfg->max_queries);
+  get(&c->q_ws, (size_t)c->num_sms * kCacheTcRows * c->hdp * 2);
   get(&c->err, sizeof(ErrorWord));
   if (e == cudaSuccess) {
     what = "set-up";
@@ -240,6 +242,7 @@ ravel_status ravel_cache_attend(ravel_cache_t* c, int layer, int batch, int n, c
   a.part_ml = c->part_ml;
   a.arrived = c->arrived;
   a.row_ml = c->row_ml;
+  a.q_ws = c->q_ws;
   a.err = &c->err->bits;
   const cudaError_t e = launch_cache_attend(a, c->dt, (cudaStream_t)stream);
   return e == cudaSuccess ? RAVEL_OK : cuda_fail(c, e, "attend");
