@@ -74,16 +74,22 @@ struct CacheAttnArgs {
   float2* part_ml;          // [units * splits][rows of a tile] (max, sum)
   unsigned* arrived;        // [units] splits that have finished (zero between launches)
   float2* row_ml;           // [B][Hkv][n * G] see row_weight, written where mass is wanted
+  float* mass_ws;           // the mass's sums by chunk
+  size_t mass_ws_bytes;
   uint8_t* q_ws;            // per SM, 128 bytes per row (of 128) and 64 dims: an item's laid out Q
   int* err;
   // chosen by the launcher
   int row_tiles, splits;
+  long long mass_pitch;     // tokens of a chunk's sums
   int group;                // tensor cores: (robot, KV head) pairs walked together
 };
 constexpr int kCacheSplitCtas = 608;   // row tiles (of 16) x splits of a launch that splits the tokens
 constexpr int kCacheTcRows = 128;      // rows of a tile on the tensor cores: at most one such tile x split per SM
 cudaError_t launch_cache_attend(const CacheAttnArgs& a, Dtype dt, cudaStream_t st);
 cudaError_t launch_cache_attend_tc(const CacheAttnArgs& a, cudaStream_t st);   // bf16; not the mass
+cudaError_t launch_cache_mass_tc(CacheAttnArgs a, cudaStream_t st);   // bf16, after the attention
+size_t cache_mass_ws_bytes(int heads, int T, int num_sms);
+cudaError_t init_cache_mass_tc_kernels();
 cudaError_t init_cache_kernels();
 cudaError_t init_cache_tc_kernels(int hdp, int* clusters);   // clusters: [9]
 

@@ -597,6 +597,7 @@ cudaError_t launch_rows(CacheAttnArgs a, cudaStream_t st) {
     e = cudaGetLastError();
   }
   if (e != cudaSuccess || !a.mass || a.max_length == 0) return e;
+  if (NP == 1 && a.n * a.G > 16) return launch_cache_mass_tc(a, st);
   cache_mass_kernel<HDP, NP, T>
       <<<dim3((a.max_length + RW * 16 - 1) / (RW * 16), a.c.Hkv, a.batch), RW * 32, frag_bytes<HDP, NP>(), st>>>(a);
   return cudaGetLastError();

@@ -31,24 +31,17 @@
 // of K on the scores, those of V on P.  P is at most 2^7 of the reference, 2^15 while
 // a grown one waits for its rescaling of O (only growth by more than 2^8 rescales);
 // what contributes less than 2^-31 of the row's largest is dropped.
-#include <cuda.h>
-#include <cudaTypedefs.h>
-
 #include <algorithm>
 
-#include "cache_attn.cuh"
+#include "cache_tc.cuh"
 #include "launch.h"
 
 namespace ravel {
 namespace {
 
 constexpr int TCT = 640;
-constexpr int BM = 128, BT = 128;              // rows, tokens of a tile
-constexpr uint32_t QB = BM * 64;               // bytes of a 64-dim block of a piece of Q
-constexpr uint32_t KU = BT * 64;               // bytes of a K unit: 128 tokens x 64 dims
 constexpr uint32_t CB = 64 * 64;               // bytes of a slot of V's codes: 64 tokens x 64 dims
 constexpr uint32_t VB = 64 * 128;              // bytes of a 64-dim block of a V half
-constexpr int kQExp = 7;                        // Q's largest magnitude per row is below 2^(kQExp + 1)
 constexpr float kTcShift = 7.f;                // P's largest value is 2^kTcShift (times 2^8 while lazy)
 constexpr int kTcCluster = 8;                  // splits that are a cluster
 
@@ -76,36 +69,6 @@ struct TcMaps {
   CUtensorMap k, v;   // a layer's codes [B Hkv T][hdp]: boxes of 64 dims x 128 rows (swizzled), x 64 rows
 };
 
-// Shared-memory descriptor of a K-major tile of 64-byte rows, 64-byte swizzled: 8-row
-// groups 512 bytes apart.
-__device__ __forceinline__ uint64_t sw64_desc(uint32_t saddr) {
-  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(512 >> 4) << 32 | (uint64_t)1 << 46 |
-         (uint64_t)4 << 61;
-}
-
-// D += A B of e4m3 operands (K = 32), issued by the elected lane of a converged warp
-__device__ __forceinline__ void umma_e4m3(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc, uint32_t el) {
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
-      "setp.ne.b32 q, %5, 0;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(el));
-}
-
-// f16 A and B (kind::f16) or e4m3 ones (kind::f8f6f4), fp32 D
-__device__ __forceinline__ uint32_t idesc_f16(int m, int n) {
-  return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
-}
-
-__device__ __forceinline__ void sts_u4(uint32_t a, uint4 v) {
-  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-}
-__device__ __forceinline__ uint4 lds_u4(uint32_t a) {
-  uint4 v;
-  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
-  return v;
-}
 __device__ __forceinline__ float4 ld_cluster_f4(uint32_t a) {
   float4 v;
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a));
@@ -121,21 +84,6 @@ __device__ __forceinline__ float ld_cluster_f1(uint32_t a) {
 __device__ __forceinline__ void widen(uint4 w, uint32_t lo, uint32_t hi) {
   sts_u4(lo, make_uint4(e4m3_lo(w.x), e4m3_hi(w.x), e4m3_lo(w.y), e4m3_hi(w.y)));
   sts_u4(hi, make_uint4(e4m3_lo(w.z), e4m3_hi(w.z), e4m3_lo(w.w), e4m3_hi(w.w)));
-}
-
-__device__ __forceinline__ void sts_u2(uint32_t a, uint32_t x, uint32_t y) {
-  asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(a), "r"(x), "r"(y) : "memory");
-}
-// two f16 -> two e4m3 (nearest, ties to even; NaN stays NaN), low halves first
-__device__ __forceinline__ uint32_t f16_to_e4m3(uint32_t h) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(h));
-  return r;
-}
-__device__ __forceinline__ uint32_t f16_sub(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
 }
 
 // 32 bytes, 32-byte aligned
@@ -162,34 +110,6 @@ template <int N>
 __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
 __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-
-// Wait of a converged warp for a phase, bounded: 2^24 tries of 20 to 200 cycles each.  Four
-// instructions a try: twenty warps whose waits read the global timer between tries, as those
-// of kernels with fewer do, took over half of an SM's issue slots; tries with a time hint
-// sleep past the arrival.
-__device__ __forceinline__ bool wait_phase(uint64_t* bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\t"
-      "mov.u32 n, 0;\n\t"
-      "TRY: mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "@p bra DONE;\n\t"
-      "add.u32 n, n, 1;\n\t"
-      "setp.lt.u32 q, n, 16777216;\n\t"
-      "@q bra TRY;\n\t"
-      "DONE: selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(smem_u32(bar)), "r"(parity)
-      : "memory");
-  return __all_sync(0xffffffffu, ok != 0);
-}
-
-// A warp's writes to shared memory become visible to the tensor core: one arrival per warp.
-__device__ __forceinline__ void written(uint64_t* bar) {
-  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  __syncwarp();
-  if ((threadIdx.x & 31) == 0) mbar_arrive(bar);
-}
 
 // Item w of a launch: its (robot, KV head), row tile, split, and the tiles of tokens
 // that it walks.
@@ -232,10 +152,6 @@ __device__ __forceinline__ Item item_of(const CacheAttnArgs& a, int w) {
   }
   return it;
 }
-
-// One value of a converged warp, so that the compiler knows it: the operands of the
-// asynchronous instructions then stay in uniform registers.
-__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 
 template <int NB>
 __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant__ TcMaps maps, CacheAttnArgs a) {
@@ -315,90 +231,15 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
   const uint32_t tmem = *tmem_slot;
   constexpr uint32_t o_col = 2 * BT;
 
-  // Q rows rb .. rb + 7 of an item (8 NB lanes with 8 dims each to a row), scaled by the row's
-  // power of two to a largest magnitude in [2^7, 2^8), in two e4m3 pieces: y rounded and what
-  // is left.  Into shared memory, or (to) the same layout in L2.
-  auto stage_q8 = [&](const Item& it, int rb, int qi, uint8_t* to) {
-    constexpr int LPR = 8 * NB, RPW = 32 / LPR, PASS = 8 / RPW;
-    const int sub = lane / LPR < RPW ? lane / LPR : 0, dl = lane % LPR;
-    const bool mine = lane / LPR < RPW, on = mine && 8 * dl < L.hd;
-    // (a row that does not exist reads the robot's first: loads without branches, all on
-    // their way together)
-    const uint32_t end_row = (uint32_t)(it.s.count * a.G);
-    const bf16* base = (const bf16*)a.q + (size_t)((long long)it.b * a.q_robot) + (size_t)it.h * a.G * L.hd + (on ? 8 * dl : 0);
-    uint32_t r = (uint32_t)(it.tile * BM + rb + sub), i = r / (uint32_t)a.G, g = r - i * (uint32_t)a.G, there = 0u;
-    uint4 x[PASS];
-    const bf16* at[PASS];
-#pragma unroll
-    for (int p = 0; p < PASS; ++p) {
-      at[p] = base;
-      if (r < end_row) {
-        there |= on ? 1u << p : 0u;
-        at[p] += (size_t)((long long)i * a.q_token) + (size_t)g * L.hd;
-      }
-      r += RPW;
-      g += RPW;
-      while (g >= (uint32_t)a.G) {
-        g -= (uint32_t)a.G;
-        ++i;
-      }
-    }
-    if (a.vec) {
-#pragma unroll
-      for (int p = 0; p < PASS; ++p) x[p] = __ldg((const uint4*)at[p]);
-    } else {
-#pragma unroll
-      for (int p = 0; p < PASS; ++p) {
-        bf16 y[8];
-#pragma unroll
-        for (int z = 0; z < 8; ++z) y[z] = at[p][z];
-        memcpy(&x[p], y, 16);
-      }
-    }
-#pragma unroll
-    for (int p = 0; p < PASS; ++p) {
-      const bool t = there >> p & 1u;
-      const uint32_t y[4] = {t ? x[p].x : 0u, t ? x[p].y : 0u, t ? x[p].z : 0u, t ? x[p].w : 0u};
-      // the largest magnitude's bits: NaN counts as larger than all
-      uint32_t top = __vmaxu2(__vmaxu2(y[0] & 0x7fff7fffu, y[1] & 0x7fff7fffu), __vmaxu2(y[2] & 0x7fff7fffu, y[3] & 0x7fff7fffu));
-      top = max(top >> 16, top & 0xffffu);
-      if (RPW == 1) {
-        top = __reduce_max_sync(0xffffffffu, top);
-      } else {
-#pragma unroll
-        for (int o = 1; o < LPR; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-      }
-      const int e = (int)(top >> 7);
-      const float f = e == 255 ? __int_as_float(0x7fffffff) : exp2i(min(kQExp + 127 - e, 126));
-      uint32_t hi[2], lo[2];
-#pragma unroll
-      for (int z = 0; z < 2; ++z) {
-        const uint32_t h0 = pack_f16x2(__uint_as_float(y[2 * z] << 16) * f, __uint_as_float(y[2 * z] & 0xffff0000u) * f);
-        const uint32_t h1 = pack_f16x2(__uint_as_float(y[2 * z + 1] << 16) * f, __uint_as_float(y[2 * z + 1] & 0xffff0000u) * f);
-        hi[z] = f16_to_e4m3(h0) | f16_to_e4m3(h1) << 16;
-        lo[z] = f16_to_e4m3(f16_sub(h0, e4m3_lo(hi[z]))) | f16_to_e4m3(f16_sub(h1, e4m3_hi(hi[z]))) << 16;
-      }
-      const int lr = rb + p * RPW + sub;
-      if (mine) {
-        const uint32_t off = (uint32_t)(dl >> 3) * QB + (uint32_t)lr * 64u +
-                             (uint32_t)((((dl >> 1) & 3) ^ ((lr >> 1) & 3)) * 16 + (dl & 1) * 8);
-        if (to) {
-          *(uint2*)(to + off) = make_uint2(hi[0], hi[1]);
-          *(uint2*)(to + off + NB * QB) = make_uint2(lo[0], lo[1]);
-        } else {
-          sts_u2(q0 + off, hi[0], hi[1]);
-          sts_u2(q0 + off + NB * QB, lo[0], lo[1]);
-        }
-        if (dl == 0) row_exp[(qi & 3) * BM + lr] = (uint8_t)e;
-      }
-    }
+  auto stage = [&](const Item& it, int rb, int qi, uint8_t* to) {
+    stage_q8<NB>(a, it.s, it.b, it.h, it.tile * BM, rb, q0, to, [&](int lr, int e) { row_exp[(qi & 3) * BM + lr] = (uint8_t)e; });
   };
   // the first item's Q, by all warps that have nothing else to do yet
   if (warp < 16) {
     for (int w = blockIdx.x; w < items; w += gridDim.x) {
       const Item it = item_of(a, w);
       if (it.n == 0) continue;
-      stage_q8(it, 8 * warp, 0, nullptr);
+      stage(it, 8 * warp, 0, nullptr);
       break;
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -421,7 +262,7 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
         if (qi > 1) ok = wait_phase(q_full, (uint32_t)qi & 1u);   // the item before's copy has been read
         if (!ok) break;
 #pragma unroll 1
-        for (int rb = 0; rb < 32; rb += 8) stage_q8(it, (warp - 8) * 32 + rb, qi, place);
+        for (int rb = 0; rb < 32; rb += 8) stage(it, (warp - 8) * 32 + rb, qi, place);
         __threadfence();
         asm volatile("fence.proxy.async;" ::: "memory");
         __syncwarp();
@@ -662,8 +503,8 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
         const bool full = j0 + BT <= firstm.hi && (j0 >= lastm.lo || j0 + BT <= a.sinks);
         if (ok) ok = wait_phase(&s_full[gt & 1], (uint32_t)(gt >> 1) & 1u);
         tc_fence_after();
-        if (i == 0) {   // (S needed Q: it is there.  Rows whose largest |q| is below 2^-112 keep fewer bits; -e >= -126)
-          rf = exp2i(-min(kQExp + 127 - (int)row_exp[(qi & 3) * BM + r], 126)) * a.scale_log2;
+        if (i == 0) {   // (S needed Q: it is there)
+          rf = q_factor(row_exp[(qi & 3) * BM + r], a.scale_log2);
           ++qi;
         }
         float sc[64];
@@ -917,18 +758,6 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
 }
 
-PFN_cuTensorMapEncodeTiled_v12000 g_enc = nullptr;
-
-cudaError_t encode_codes(CUtensorMap* m, const uint8_t* base, const CacheLayer& c, int batch, int box_rows, bool swizzle) {
-  cuuint64_t dims[2] = {(cuuint64_t)c.hdp, (cuuint64_t)batch * c.Hkv * c.T};
-  cuuint64_t strides[1] = {(cuuint64_t)c.hdp};
-  cuuint32_t box[2] = {64u, (cuuint32_t)box_rows}, estr[2] = {1, 1};
-  const CUresult r = g_enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(base), dims, strides, box, estr,
-                           CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
-}
-
 template <int NB>
 cudaError_t launch_nb(CacheAttnArgs a, cudaStream_t st) {
   a.row_tiles = (a.n * a.G + BM - 1) / BM;
@@ -978,6 +807,30 @@ cudaError_t init_nb(int* clusters) {
 
 }  // namespace
 
+static PFN_cuTensorMapEncodeTiled_v12000 g_enc = nullptr;
+
+cudaError_t encode_codes(CUtensorMap* m, const uint8_t* base, const CacheLayer& c, int batch, int box_rows, bool swizzle) {
+  cuuint64_t dims[2] = {(cuuint64_t)c.hdp, (cuuint64_t)batch * c.Hkv * c.T};
+  cuuint64_t strides[1] = {(cuuint64_t)c.hdp};
+  cuuint32_t box[2] = {64u, (cuuint32_t)box_rows}, estr[2] = {1, 1};
+  const CUresult r = g_enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(base), dims, strides, box, estr,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+cudaError_t cache_tc_encoder() {
+  if (!g_enc) {
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q);
+    if (e != cudaSuccess) return e;
+    if (q != cudaDriverEntryPointSuccess || !fn) return cudaErrorSymbolNotFound;
+    g_enc = (PFN_cuTensorMapEncodeTiled_v12000)fn;
+  }
+  return cudaSuccess;
+}
+
 cudaError_t launch_cache_attend_tc(const CacheAttnArgs& a, cudaStream_t st) {
   switch (a.c.hdp) {
     case 64: return launch_nb<1>(a, st);
@@ -988,14 +841,8 @@ cudaError_t launch_cache_attend_tc(const CacheAttnArgs& a, cudaStream_t st) {
 }
 
 cudaError_t init_cache_tc_kernels(int hdp, int* clusters) {
-  if (!g_enc) {
-    void* fn = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q);
-    if (e != cudaSuccess) return e;
-    if (q != cudaDriverEntryPointSuccess || !fn) return cudaErrorSymbolNotFound;
-    g_enc = (PFN_cuTensorMapEncodeTiled_v12000)fn;
-  }
+  const cudaError_t e = cache_tc_encoder();
+  if (e != cudaSuccess) return e;
   switch (hdp) {
     case 64: return init_nb<1>(clusters);
     case 128: return init_nb<2>(clusters);

@@ -27,6 +27,8 @@ struct ravel_cache_ctx {
   float2 *part_ml = nullptr, *row_ml = nullptr;
   unsigned* arrived = nullptr;
   uint8_t* q_ws = nullptr;
+  float* mass_ws = nullptr;
+  size_t mass_ws_bytes = 0;
   ErrorWord* err = nullptr;
   int* err_host = nullptr;       // pinned, mapped: the error word's mirror
   std::vector<void*> allocs;
@@ -138,6 +140,10 @@ ravel_status ravel_cache_create(const ravel_cache_config* cfg, int device, ravel
   get(&c->part_ml, sizeof(float2) * part_rows);
   get(&c->arrived, sizeof(unsigned) * kCacheSplitCtas);
   get(&c->row_ml, sizeof(float2) * cfg->max_batch * (size_t)cfg->n_q_heads * cfg->max_queries);
+  if (c->dt == DT_BF16) {
+    c->mass_ws_bytes = cache_mass_ws_bytes((int)heads, c->T, c->num_sms);
+    get(&c->mass_ws, c->mass_ws_bytes);
+  }
   get(&c->q_ws, (size_t)c->num_sms * kCacheTcRows * c->hdp * 2);
   get(&c->err, sizeof(ErrorWord));
   if (e == cudaSuccess) {
@@ -149,6 +155,7 @@ ravel_status ravel_cache_create(const ravel_cache_config* cfg, int device, ravel
     if (e == cudaSuccess) e = cudaMemcpy(c->err, &w, sizeof w, cudaMemcpyHostToDevice);
     if (e == cudaSuccess) e = init_cache_kernels();
     if (e == cudaSuccess) e = init_cache_tc_kernels(c->hdp, c->clusters);
+    if (e == cudaSuccess) e = init_cache_mass_tc_kernels();
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
   }
   if (e != cudaSuccess) {
@@ -243,6 +250,8 @@ ravel_status ravel_cache_attend(ravel_cache_t* c, int layer, int batch, int n, c
   a.arrived = c->arrived;
   a.row_ml = c->row_ml;
   a.q_ws = c->q_ws;
+  a.mass_ws = c->mass_ws;
+  a.mass_ws_bytes = c->mass_ws_bytes;
   a.err = &c->err->bits;
   const cudaError_t e = launch_cache_attend(a, c->dt, (cudaStream_t)stream);
   return e == cudaSuccess ? RAVEL_OK : cuda_fail(c, e, "attend");
