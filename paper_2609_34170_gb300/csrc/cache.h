@@ -2,6 +2,7 @@
 // enqueues on `st` and returns the launch's cudaError_t.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -54,8 +55,16 @@ struct EvictArgs {
 };
 cudaError_t launch_cache_evict(const EvictArgs& a, cudaStream_t st);
 
+// A layer's codes as tensor maps (host memory): boxes for the tensor cores' tiles and for
+// the units of the kernel for few rows.
+struct CacheMaps {
+  CUtensorMap k_tc, v_tc, k_rows, v_rows;
+};
+cudaError_t encode_layer(CacheMaps* m, const CacheLayer& c, int batch);
+
 struct CacheAttnArgs {
   CacheLayer c;
+  const CacheMaps* maps;
   const void* q;
   void* out;
   long long q_robot, q_token, out_robot, out_token;
@@ -74,13 +83,14 @@ struct CacheAttnArgs {
   float2* part_ml;          // [units * splits][rows of a tile] (max, sum)
   unsigned* arrived;        // [units] splits that have finished (zero between launches)
   float2* row_ml;           // [B][Hkv][n * G] see row_weight, written where mass is wanted
-  float* mass_ws;           // the mass's sums by chunk
+  float* mass_ws;           // the mass's sums by chunk, or scores kept for it
   size_t mass_ws_bytes;
   uint8_t* q_ws;            // per SM, 128 bytes per row (of 128) and 64 dims: an item's laid out Q
   int* err;
   // chosen by the launcher
   int row_tiles, splits;
-  long long mass_pitch;     // tokens of a chunk's sums
+  long long mass_pitch;     // tokens of a chunk's sums, or of a row's scores
+  float* scores;            // few rows: scores kept for the mass, or null
   int group;                // tensor cores: (robot, KV head) pairs walked together
 };
 constexpr int kCacheSplitCtas = 608;   // row tiles (of 16) x splits of a launch that splits the tokens

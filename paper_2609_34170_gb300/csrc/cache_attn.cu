@@ -28,7 +28,8 @@
 // score, and its largest score + ve) are rounded up to integers in the log2
 // domain, so that every change of reference is an exact power of two.  Maxima,
 // sums and outputs are fp32.
-#include "cache_attn.cuh"
+#include "cache_tc.cuh"
+#include "launch.h"
 
 namespace ravel {
 namespace {
@@ -51,39 +52,35 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint4& a, uint32_t 
 template <int HDP, int NP, typename T, int THREADS>
 __device__ __forceinline__ void stage_q(const CacheAttnArgs& a, const Sight& s, int b, int h, int r0, uint32_t* frag,
                                         float* fac) {
-  constexpr int TPR = HDP / 16;   // threads per row
-  for (int w = threadIdx.x; w < 16 * TPR; w += THREADS) {
-    const int lr = w / TPR, d = (w % TPR) * 16, r = r0 + lr;
-    float x[16];
+  constexpr int TPR = HDP / 16, ITEMS = (16 * TPR + THREADS - 1) / THREADS;   // threads per row, rows' pieces per thread
+  float x[ITEMS][16];
+#pragma unroll
+  for (int z = 0; z < ITEMS; ++z) {
+    const int w = threadIdx.x + z * THREADS, lr = w / TPR, d = (w % TPR) * 16, r = r0 + lr;
     const int i = r / a.G;
-    if (i < s.count && d < a.c.hd) {
+    if (w < 16 * TPR && i < s.count && d < a.c.hd) {
       const T* row = (const T*)a.q + (size_t)((long long)b * a.q_robot + (long long)i * a.q_token) +
                      (size_t)(h * a.G + r % a.G) * a.c.hd;
-      load16(row, d, a.c.hd, a.vec, x);
+      load16(row, d, a.c.hd, a.vec, x[z]);
     } else {
 #pragma unroll
-      for (int q = 0; q < 16; ++q) x[q] = 0.f;
+      for (int q = 0; q < 16; ++q) x[z][q] = 0.f;
     }
+  }
+#pragma unroll
+  for (int z = 0; z < ITEMS; ++z) {
+    const int w = threadIdx.x + z * THREADS;
     uint32_t top = 0u;   // bits of the largest magnitude: NaN counts as larger than all
 #pragma unroll
-    for (int q = 0; q < 16; ++q) top = max(top, __float_as_uint(x[q]) & 0x7fffffffu);
-    // the row's threads lie in one warp, TPR of them (4, 8, 12 or 16), at a multiple of 4
-    // lanes but not always aligned to TPR: the maximum goes through shared memory
-    atomicMax((unsigned*)&fac[lr], top);
+    for (int q = 0; q < 16; ++q) top = max(top, __float_as_uint(x[z][q]) & 0x7fffffffu);
+    if (w < 16 * TPR) atomicMax((unsigned*)&fac[w / TPR], top);
   }
   __syncthreads();
-  for (int w = threadIdx.x; w < 16 * TPR; w += THREADS) {
-    const int lr = w / TPR, d = (w % TPR) * 16, r = r0 + lr;
-    float x[16];
-    const int i = r / a.G;
-    if (i < s.count && d < a.c.hd) {
-      const T* row = (const T*)a.q + (size_t)((long long)b * a.q_robot + (long long)i * a.q_token) +
-                     (size_t)(h * a.G + r % a.G) * a.c.hd;
-      load16(row, d, a.c.hd, a.vec, x);
-    } else {
 #pragma unroll
-      for (int q = 0; q < 16; ++q) x[q] = 0.f;
-    }
+  for (int z = 0; z < ITEMS; ++z) {
+    const int w = threadIdx.x + z * THREADS;
+    if (w >= 16 * TPR) break;
+    const int lr = w / TPR, d = (w % TPR) * 16;
     const uint32_t top = ((const unsigned*)fac)[lr];
     // factor 2^(14 - exponent), at most 2^126 (rows below 2^-112 keep fewer bits)
     const int e = min(14 - ((int)(top >> 23) - 127), 126);
@@ -93,7 +90,7 @@ __device__ __forceinline__ void stage_q(const CacheAttnArgs& a, const Sight& s, 
     const int j = d / 64, c = (d / 16) % 4, lane = (lr & 7) * 4 + c;
 #pragma unroll
     for (int s4 = 0; s4 < 4; ++s4) {
-      const float y0 = x[4 * s4] * f, y1 = x[4 * s4 + 1] * f, y2 = x[4 * s4 + 2] * f, y3 = x[4 * s4 + 3] * f;
+      const float y0 = x[z][4 * s4] * f, y1 = x[z][4 * s4 + 1] * f, y2 = x[z][4 * s4 + 2] * f, y3 = x[z][4 * s4 + 3] * f;
       uint32_t lo = pack_f16x2(y0, y1), hi = pack_f16x2(y2, y3);
       // fragment registers: a0 (row, dims 0 1), a1 (row + 8, 0 1), a2 (row, 2 3), a3 (row + 8, 2 3)
       uint32_t* at = frag + ((4 * j + s4) * 32 + lane) * 4 + (lr >> 3);
@@ -129,25 +126,53 @@ struct KeyRegs {
   }
 };
 
+// A warp's unit of 16 NT tokens in shared memory: boxes of IN dims x U tokens as TMA
+// swizzles them (16-byte pieces of a row permuted by the row), codes of K or of V.
 template <int HDP>
-struct ValueRegs {
-  uint32_t w[4][HDP / 32];   // tokens 2 c, 2 c + 1, 2 c + 8, 2 c + 9
-  __device__ __forceinline__ void load(const uint8_t* v, int g, int c) {
+struct Unit {
+  static constexpr int NT = HDP == 64 ? 4 : (HDP == 128 ? 2 : 1);   // blocks of 16 tokens
+  static constexpr int U = 16 * NT, IN = HDP % 128 ? 64 : 128, BOXES = HDP / IN;
+  static constexpr uint32_t bytes = U * HDP;
+  // byte of a token's row where 16-byte piece p (of HDP / 16) lies
+  static __device__ __forceinline__ uint32_t at(int row, int p) {
+    constexpr int PP = IN / 16;
+    const int q = p % PP;
+    return (uint32_t)(p / PP * U * IN + row * IN + ((IN == 128 ? q ^ (row & 7) : q ^ ((row >> 1) & 3)) * 16));
+  }
+};
+
+// Key fragments of a block of 16 tokens: tokens g and g + 8, dims 64 j + 16 c .. + 15.
+template <int HDP>
+struct KeyUnit {
+  uint4 w[2][HDP / 64];
+  __device__ __forceinline__ void load(uint32_t unit, int row0, int g, int c) {
+#pragma unroll
+    for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+      for (int j = 0; j < HDP / 64; ++j) w[hh][j] = lds_u4(unit + Unit<HDP>::at(row0 + g + 8 * hh, 4 * j + c));
+  }
+};
+
+// Value fragments: tokens 2 c, 2 c + 1, 2 c + 8, 2 c + 9, 16 dims of each 128 from 16 g on
+// (8 of a last 64 from 8 g on).
+template <int HDP>
+struct ValueUnit {
+  uint32_t w[4][HDP / 32];
+  __device__ __forceinline__ void load(uint32_t unit, int row0, int g, int c) {
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      const uint8_t* row = v + (size_t)(2 * c + (t & 1) + 4 * (t & 2)) * HDP;
+      const int row = row0 + 2 * c + (t & 1) + 4 * (t & 2);
 #pragma unroll
       for (int j = 0; j < HDP / 128; ++j) {
-        const uint4 x = __ldg((const uint4*)(row + 128 * j + 16 * g));
+        const uint4 x = lds_u4(unit + Unit<HDP>::at(row, 8 * j + g));
         w[t][4 * j] = x.x;
         w[t][4 * j + 1] = x.y;
         w[t][4 * j + 2] = x.z;
         w[t][4 * j + 3] = x.w;
       }
       if (HDP % 128) {
-        const uint2 x = __ldg((const uint2*)(row + HDP / 128 * 128 + 8 * g));
-        w[t][HDP / 32 - 2] = x.x;
-        w[t][HDP / 32 - 1] = x.y;
+        const uint32_t at = unit + Unit<HDP>::at(row, HDP / 128 * 8 + (g >> 1)) + 8u * (g & 1);
+        asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[t][HDP / 32 - 2]), "=r"(w[t][HDP / 32 - 1]) : "r"(at));
       }
     }
   }
@@ -158,22 +183,44 @@ struct ValueRegs {
   }
 };
 
+template <int HDP, int NP>
+struct RowsShape {
+  static constexpr int frag = NP * (HDP / 16) * 512;   // bytes of Q's fragments
+  // units in flight per warp, K and V (24 KB; fp32's take 16: its fragments are twice as many)
+  static constexpr int D = NP == 2 ? 2 : 3;
+  static constexpr int ring = RW * D * 2 * (int)Unit<HDP>::bytes;
+  static constexpr int join = (RW + 1) * 16 * HDP * 4;   // the warps' outputs and their sum, over the ring
+  static constexpr int bytes = frag + (ring > join ? ring : join);
+};
+
+struct RowsMaps {
+  CUtensorMap k, v;   // a layer's codes [B Hkv T][HDP] in boxes of Unit::IN dims x U rows, swizzled
+};
+
 template <int HDP, int NP, typename T>
-__global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(CacheAttnArgs a) {
-  constexpr int NT = HDP == 64 ? 4 : (HDP == 128 ? 2 : 1);   // blocks of 16 tokens per unit
-  constexpr int U = 16 * NT, KS = HDP / 16;
-  extern __shared__ __align__(16) uint8_t smem[];
-  uint32_t* frag = (uint32_t*)smem;                  // [NP][KS][32][4]
-  float* joint = (float*)(smem + NP * KS * 512);     // [RW][16][HDP] outputs of the warps
+__global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_constant__ RowsMaps maps, CacheAttnArgs a) {
+  using Un = Unit<HDP>;
+  using Shape = RowsShape<HDP, NP>;
+  constexpr int NT = Un::NT, U = Un::U, KS = HDP / 16, D = Shape::D;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  float* joint = (float*)smem;                          // [RW][16][HDP] outputs of the warps, over the ring
+  float* mine = joint + RW * 16 * HDP;                  // [16][HDP] their sum
+  uint32_t* frag = (uint32_t*)(smem + Shape::bytes - Shape::frag);   // [NP][KS][32][4]
   __shared__ float fac[16];
   __shared__ float2 warp_ml[RW][16], split_w[16];
   __shared__ unsigned last;
+  __shared__ uint64_t arrived[RW][D];
+  __shared__ float split_wt[8][16];
 
   const int b = blockIdx.z, h = blockIdx.y, tile = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
   const CacheLayer& L = a.c;
   const int r0 = tile * 16, rows = min(16, a.n * a.G - r0);
   const size_t head = (size_t)b * L.Hkv + h;
+  if (smem_u32(smem) & 1023u) {   // (the swizzled layouts count on it)
+    if (threadIdx.x == 0) raise_error(a.err, ERR_SHAPE);
+    return;
+  }
   Sight s;
   if (!robot_sight(a, b, s) && threadIdx.x == 0 && blockIdx.x == 0 && h == 0) raise_error(a.err, ERR_SHAPE);
   T* out0 = (T*)a.out + (size_t)((long long)b * a.out_robot) + (size_t)h * a.G * L.hd;
@@ -188,6 +235,28 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(CacheAttnArgs a)
   tile_sight(a, s, r0, r0 + 15, U);
   const int u0 = (int)((long long)s.units * split / a.splits), u1 = (int)((long long)s.units * (split + 1) / a.splits);
 
+  // each warp's ring of units: its own loads, which it alone waits for
+  const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * D) * 2u * Un::bytes;
+  auto unit_token = [&](int u) { return (u < s.sink_units ? u : u - s.sink_units + s.from) * U; };
+  uint64_t pol;
+  asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(pol));
+  auto fetch = [&](int u, int slot) {   // (lane 0)
+    const int row = (int)(head * L.T) + unit_token(u);
+    const uint32_t to = ring + (uint32_t)slot * 2u * Un::bytes, bar = smem_u32(&arrived[warp][slot]);
+    mbar_expect_tx(&arrived[warp][slot], 2u * Un::bytes);
+#pragma unroll
+    for (int x = 0; x < Un::BOXES; ++x) {
+      tma_load_2d_el(&maps.k, bar, to + (uint32_t)(x * U * Un::IN), x * Un::IN, row, pol, 1u);
+      tma_load_2d_el(&maps.v, bar, to + Un::bytes + (uint32_t)(x * U * Un::IN), x * Un::IN, row, pol, 1u);
+    }
+  };
+  if (lane == 0) {
+    for (int x = 0; x < D; ++x) mbar_init(&arrived[warp][x], 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    for (int x = 0; x < D; ++x)
+      if (u0 + warp + RW * x < u1) fetch(u0 + warp + RW * x, x);
+  }
   if (threadIdx.x < 16) fac[threadIdx.x] = 0.f;
   __syncthreads();
   stage_q<HDP, NP, T, RW * 32>(a, s, b, h, r0, frag, fac);
@@ -197,7 +266,6 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(CacheAttnArgs a)
   const RowMask first = row_mask(a, s, r0), lastm = row_mask(a, s, min(r0 + 15, s.count * a.G - 1));
   const int full_hi = first.hi, full_lo = lastm.lo;
 
-  const uint8_t *K = L.k + head * L.T * HDP, *V = L.v + head * L.T * HDP;
   const int8_t *KE = L.ke + head * (L.T / 16), *VE = L.ve + head * (L.T / 16);
 
   float o[HDP / 8][4];
@@ -207,26 +275,40 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(CacheAttnArgs a)
     for (int q = 0; q < 4; ++q) o[t][q] = 0.f;
   float m[2] = {-INFINITY, -INFINITY}, W[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 
-  KeyRegs<HDP> kr[NT];
-  ValueRegs<HDP> vr[NT];
-  auto unit_token = [&](int u) { return (u < s.sink_units ? u : u - s.sink_units + s.from) * U; };
+  // the exponents of a unit's blocks, one byte each
+  auto exps_of = [&](const int8_t* e, int j0) -> uint32_t {
+    if (NT == 4) return __ldg((const uint32_t*)(e + j0 / 16));
+    if (NT == 2) return __ldg((const uint16_t*)(e + j0 / 16));
+    return (uint8_t)__ldg(e + j0 / 16);
+  };
   int u = u0 + warp;
+  uint32_t kes = 0u, ves = 0u;
   if (u < u1) {
-    const int j0 = unit_token(u);
-#pragma unroll
-    for (int t = 0; t < NT; ++t) kr[t].load(K + (size_t)(j0 + 16 * t) * HDP, g, c);
-#pragma unroll
-    for (int t = 0; t < NT; ++t) vr[t].load(V + (size_t)(j0 + 16 * t) * HDP, g, c);
+    kes = exps_of(KE, unit_token(u));
+    ves = exps_of(VE, unit_token(u));
   }
+  int slot = 0;
+  uint32_t phase = 0u;
+  bool ok = true;
   for (; u < u1; u += RW) {
     const int j0 = unit_token(u);
+    const uint32_t unit = ring + (uint32_t)slot * 2u * Un::bytes;
     float kf[NT];
     int ve[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      kf[t] = exp2i(KE[j0 / 16 + t]);
-      ve[t] = VE[j0 / 16 + t];
+      kf[t] = exp2i((int)(int8_t)(kes >> (8 * t)));
+      ve[t] = (int)(int8_t)(ves >> (8 * t));
     }
+    const int un = u + RW;
+    if (un < u1) {
+      kes = exps_of(KE, unit_token(un));
+      ves = exps_of(VE, unit_token(un));
+    }
+    if (ok) ok = wait_phase(&arrived[warp][slot], phase);
+    KeyUnit<HDP> kr[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) kr[t].load(unit, 16 * t, g, c);
     float sc[NT][2][4];
 #pragma unroll
     for (int t = 0; t < NT; ++t)
@@ -252,12 +334,6 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(CacheAttnArgs a)
         }
       }
     }
-    const int un = u + RW;
-    const int jn = un < u1 ? unit_token(un) : 0;
-    if (un < u1) {
-#pragma unroll
-      for (int t = 0; t < NT; ++t) kr[t].load(K + (size_t)(jn + 16 * t) * HDP, g, c);
-    }
     // scores in the log2 domain; hidden ones -inf
     const bool full = j0 + U <= full_hi && (j0 >= full_lo || j0 + U <= a.sinks);
 #pragma unroll
@@ -274,6 +350,17 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(CacheAttnArgs a)
           for (int q = 0; q < 4; ++q)
             if (!mk[q >> 1].sees(jb + 8 * hh + 2 * c + (q & 1))) sc[t][hh][q] = -INFINITY;
       }
+    }
+    if (a.scores) {   // kept for the mass
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+          for (int rr = 0; rr < 2; ++rr)
+            if (g + 8 * rr < rows)
+              *(float2*)(a.scores + (head * a.n * a.G + r0 + g + 8 * rr) * a.mass_pitch + j0 + 16 * t + 8 * hh + 2 * c) =
+                  make_float2(sc[t][hh][2 * rr], sc[t][hh][2 * rr + 1]);
     }
     float mu[2], wu[2];   // the references, 0 while the row has seen nothing
     bool same = true;
@@ -340,13 +427,15 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(CacheAttnArgs a)
                                   pack_f16x2(p[1][0] - f16lo(pa[0].z), p[1][1] - f16hi(pa[0].z)),
                                   pack_f16x2(p[1][2] - f16lo(pa[0].w), p[1][3] - f16hi(pa[0].w)));
       }
+      ValueUnit<HDP> vr;
+      vr.load(unit + Un::bytes, 16 * t, g, c);
 #pragma unroll
       for (int wi = 0; wi < HDP / 32; ++wi) {
         // bytes i of two tokens' words side by side
-        const uint32_t x0 = __byte_perm(vr[t].w[0][wi], vr[t].w[1][wi], 0x5140);
-        const uint32_t y0 = __byte_perm(vr[t].w[0][wi], vr[t].w[1][wi], 0x7362);
-        const uint32_t x1 = __byte_perm(vr[t].w[2][wi], vr[t].w[3][wi], 0x5140);
-        const uint32_t y1 = __byte_perm(vr[t].w[2][wi], vr[t].w[3][wi], 0x7362);
+        const uint32_t x0 = __byte_perm(vr.w[0][wi], vr.w[1][wi], 0x5140);
+        const uint32_t y0 = __byte_perm(vr.w[0][wi], vr.w[1][wi], 0x7362);
+        const uint32_t x1 = __byte_perm(vr.w[2][wi], vr.w[3][wi], 0x5140);
+        const uint32_t y1 = __byte_perm(vr.w[2][wi], vr.w[3][wi], 0x7362);
         const uint32_t b0[4] = {e4m3_lo(x0), e4m3_hi(x0), e4m3_lo(y0), e4m3_hi(y0)};
         const uint32_t b1[4] = {e4m3_lo(x1), e4m3_hi(x1), e4m3_lo(y1), e4m3_hi(y1)};
 #pragma unroll
@@ -355,11 +444,19 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(CacheAttnArgs a)
           for (int p = 0; p < NP; ++p) mma_f16(o[4 * wi + i], pa[p], b0[i], b1[i]);
       }
     }
-    if (un < u1) {
-#pragma unroll
-      for (int t = 0; t < NT; ++t) vr[t].load(V + (size_t)(jn + 16 * t) * HDP, g, c);
+    // every lane has read the unit: the slot takes the one D turns on
+    __syncwarp();
+    if (lane == 0 && u + RW * D < u1) fetch(u + RW * D, slot);
+    if (++slot == D) {
+      slot = 0;
+      phase ^= 1u;
     }
   }
+  if (!ok) {   // loads still on their way land before the shared memory goes away
+    for (int x = 0; x < D; ++x) mbar_wait(&arrived[warp][x], phase ^ (x < slot ? 1u : 0u));
+    if (lane == 0) raise_error(a.err, ERR_TIMEOUT);
+  }
+  __syncthreads();   // the rings are read: the outputs go over them
 
   // ---- join the warps: outputs normalised by their own sums, then weighted
 #pragma unroll
@@ -385,7 +482,7 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(CacheAttnArgs a)
         for (int i = 0; i < 4; ++i)
 #pragma unroll
           for (int q = 0; q < 2; ++q)
-            dst[ValueRegs<HDP>::dim(wi, i, 2 * c + q)] = real ? o[4 * wi + i][2 * rr + q] * f * e2 : 0.f;
+            dst[ValueUnit<HDP>::dim(wi, i, 2 * c + q)] = real ? o[4 * wi + i][2 * rr + q] * f * e2 : 0.f;
     }
   }
   __syncthreads();
@@ -426,6 +523,50 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(CacheAttnArgs a)
       const float2 x = split_w[threadIdx.x];
       a.row_ml[head * a.n * a.G + r0 + threadIdx.x] = row_weight(x.x, x.y, kPExp);
     }
+    return;
+  }
+  if (a.splits <= 8) {
+    // the splits are a cluster: each CTA joins a share of the rows' columns from all of them
+    for (int w = threadIdx.x; w < rows * HDP; w += RW * 32) mine[w] = joined(w / HDP, w % HDP);
+    cluster_sync();
+    if ((int)threadIdx.x < rows) {
+      const uint32_t at = smem_u32(&split_w[threadIdx.x]);
+      float M = -INFINITY, S = 0.f;
+      for (int q = 0; q < a.splits; ++q) M = fmaxf(M, ld_cluster_f1(mapa_shared(at, (uint32_t)q)));
+      for (int q = 0; q < a.splits; ++q) {
+        const uint32_t from = mapa_shared(at, (uint32_t)q);
+        const float2 x = make_float2(ld_cluster_f1(from), ld_cluster_f1(from + 4));
+        const float wt = x.y != x.y ? x.y : (x.x == -INFINITY ? 0.f : exp2f(x.x - M) * x.y);
+        split_wt[q][threadIdx.x] = wt;
+        S += wt;
+      }
+      const float inv = !(S <= 0.f) ? 1.f / S : 0.f;
+      for (int q = 0; q < a.splits; ++q) split_wt[q][threadIdx.x] *= inv;
+      if (a.mass && split == 0) a.row_ml[head * a.n * a.G + r0 + threadIdx.x] = row_weight(M, S, kPExp);
+    }
+    __syncthreads();
+    const int pieces = rows * (HDP / 4), share = (pieces + a.splits - 1) / a.splits;
+    for (int w = split * share + threadIdx.x; w < min(pieces, (split + 1) * share); w += RW * 32) {
+      const int row = w / (HDP / 4), d = w % (HDP / 4) * 4;
+      if (d >= L.hd) continue;
+      const uint32_t at = smem_u32(mine + row * HDP + d);
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+      for (int q = 0; q < a.splits; ++q) {
+        const float4 x = ld_cluster_f4(mapa_shared(at, (uint32_t)q));
+        const float wt = split_wt[q][row];
+        acc.x += wt * x.x;
+        acc.y += wt * x.y;
+        acc.z += wt * x.z;
+        acc.w += wt * x.w;
+      }
+      T* dst = out_row(r0 + row) + d;   // hd is a multiple of 8
+      dst[0] = from_f32<T>(acc.x);
+      dst[1] = from_f32<T>(acc.y);
+      dst[2] = from_f32<T>(acc.z);
+      dst[3] = from_f32<T>(acc.w);
+    }
+    cluster_sync();   // nobody leaves while its rows are read
     return;
   }
   const size_t unit = head * a.row_tiles + tile;
@@ -485,7 +626,7 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(CacheAttnArgs a)
 template <int HDP, int NP, typename T>
 __global__ void __launch_bounds__(RW * 32) cache_mass_kernel(CacheAttnArgs a) {
   constexpr int KS = HDP / 16;
-  extern __shared__ __align__(16) uint8_t smem[];
+  extern __shared__ __align__(1024) uint8_t smem[];
   uint32_t* frag = (uint32_t*)smem;   // [NP][KS][32][4]
   __shared__ float fac[16];
   const int b = blockIdx.z, h = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -567,15 +708,45 @@ __global__ void __launch_bounds__(RW * 32) cache_mass_kernel(CacheAttnArgs a) {
     }
 }
 
+// The same from the scores that the attention kept: a thread per two tokens.
+__global__ void __launch_bounds__(256) cache_mass_scores_kernel(CacheAttnArgs a) {
+  const int j = (blockIdx.x * 256 + threadIdx.x) * 2;
+  if (j >= a.max_length) return;
+  const int b = blockIdx.z;
+  const size_t head = (size_t)b * a.c.Hkv + blockIdx.y;
+  Sight s;
+  robot_sight(a, b, s);
+  const float2* ml = a.row_ml + head * a.n * a.G;
+  const float* sc = a.scores + head * a.n * a.G * a.mass_pitch + j;
+  float v0 = 0.f, v1 = 0.f;
+  if (j < s.len)
+    for (int i = 0; i < s.count; ++i) {
+      const RowMask mk = row_mask(a, s, i * a.G);
+      const bool s0 = mk.sees(j), s1 = mk.sees(j + 1);
+      if (!s0 && !s1) continue;
+#pragma unroll 4
+      for (int g = 0; g < a.G; ++g) {
+        const float2 x = __ldcs((const float2*)(sc + (size_t)(i * a.G + g) * a.mass_pitch)), y = __ldg(ml + i * a.G + g);
+        v0 += s0 ? exp2f(x.x - y.x) * y.y : 0.f;
+        v1 += s1 ? exp2f(x.y - y.x) * y.y : 0.f;
+      }
+    }
+  float* mass = a.mass + head * a.mass_stride + j;
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+    if (j + e < a.max_length) {
+      const float v = e ? v1 : v0;
+      if (!a.mass_add) mass[e] = v;
+      else if (j + e < s.len) mass[e] += v;
+    }
+}
+
 template <int HDP, int NP>
 constexpr int frag_bytes() { return NP * (HDP / 16) * 512; }
 
-template <int HDP, int NP>
-constexpr int rows_smem() { return frag_bytes<HDP, NP>() + RW * 16 * HDP * 4; }
-
 template <int HDP, int NP, typename T>
 cudaError_t launch_rows(CacheAttnArgs a, cudaStream_t st) {
-  constexpr int U = HDP == 64 ? 64 : (HDP == 128 ? 32 : 16);
+  constexpr int U = Unit<HDP>::U;
   a.row_tiles = (a.n * a.G + 15) / 16;
   const long long tiles = (long long)a.row_tiles * a.c.Hkv * a.batch;
   // tokens that a row tile sees at most, in units
@@ -588,18 +759,30 @@ cudaError_t launch_rows(CacheAttnArgs a, cudaStream_t st) {
     // (and no more splits than the joining CTA has weights for in shared memory)
     const long long most = min(min((long long)kCacheSplitCtas, 2ll * a.num_sms) / tiles, (long long)RW * HDP);
     a.splits = (int)max(1ll, min(most, (long long)(units + RW - 1) / RW));
+    // up to 8 splits join in distributed shared memory, more through L2, which takes longer
+    // than two units more for each warp
+    if (a.splits > 8 && units <= 8 * RW * 3) a.splits = 8;
   }
+  // (every head's and row's scores, where the mass's workspace holds them)
+  a.mass_pitch = (a.max_length + 127) / 128 * 128;
+  const bool keep = a.mass && (NP == 2 || a.n * a.G <= 16) &&
+                    (double)a.batch * a.c.Hkv * a.n * a.G * a.mass_pitch * 4 <= (double)a.mass_ws_bytes;
+  a.scores = keep ? a.mass_ws : nullptr;
   cudaError_t e;
   if (NP == 1 && a.n * a.G > 16) {
     e = launch_cache_attend_tc(a, st);
   } else {
-    cache_rows_kernel<HDP, NP, T><<<dim3(a.row_tiles * a.splits, a.c.Hkv, a.batch), RW * 32, rows_smem<HDP, NP>(), st>>>(a);
-    e = cudaGetLastError();
+    const RowsMaps maps{a.maps->k_rows, a.maps->v_rows};
+    e = launch_kernel_cluster(cache_rows_kernel<HDP, NP, T>, dim3(a.row_tiles * a.splits, a.c.Hkv, a.batch), dim3(RW * 32),
+                              RowsShape<HDP, NP>::bytes, st, dim3(a.splits <= 8 ? a.splits : 1, 1, 1), maps, a);
   }
   if (e != cudaSuccess || !a.mass || a.max_length == 0) return e;
   if (NP == 1 && a.n * a.G > 16) return launch_cache_mass_tc(a, st);
-  cache_mass_kernel<HDP, NP, T>
-      <<<dim3((a.max_length + RW * 16 - 1) / (RW * 16), a.c.Hkv, a.batch), RW * 32, frag_bytes<HDP, NP>(), st>>>(a);
+  if (keep)
+    cache_mass_scores_kernel<<<dim3((a.max_length + 511) / 512, a.c.Hkv, a.batch), 256, 0, st>>>(a);
+  else
+    cache_mass_kernel<HDP, NP, T>
+        <<<dim3((a.max_length + RW * 16 - 1) / (RW * 16), a.c.Hkv, a.batch), RW * 32, frag_bytes<HDP, NP>(), st>>>(a);
   return cudaGetLastError();
 }
 
@@ -611,10 +794,10 @@ cudaError_t launch_hd(const CacheAttnArgs& a, Dtype dt, cudaStream_t st) {
 template <int HDP>
 cudaError_t init_hd() {
   cudaError_t e = cudaFuncSetAttribute(cache_rows_kernel<HDP, 1, bf16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       rows_smem<HDP, 1>());
+                                       RowsShape<HDP, 1>::bytes);
   if (e != cudaSuccess) return e;
   return cudaFuncSetAttribute(cache_rows_kernel<HDP, 2, float>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              rows_smem<HDP, 2>());
+                              RowsShape<HDP, 2>::bytes);
 }
 
 }  // namespace
@@ -626,6 +809,17 @@ cudaError_t launch_cache_attend(const CacheAttnArgs& a, Dtype dt, cudaStream_t s
     case 192: return launch_hd<192>(a, dt, st);
     default: return launch_hd<256>(a, dt, st);
   }
+}
+
+// The maps of a layer for every robot of the cache: boxes of the kernels' tiles.
+cudaError_t encode_layer(CacheMaps* m, const CacheLayer& c, int batch) {
+  const int unit = c.hdp == 64 ? 64 : (c.hdp == 128 ? 32 : 16), in = c.hdp % 128 ? 64 : 128;
+  cudaError_t e = cache_tc_encoder();
+  if (e == cudaSuccess) e = encode_codes(&m->k_tc, c.k, c, batch, 64, BT, true);
+  if (e == cudaSuccess) e = encode_codes(&m->v_tc, c.v, c, batch, 64, 64, false);
+  if (e == cudaSuccess) e = encode_codes(&m->k_rows, c.k, c, batch, in, unit, true);
+  if (e == cudaSuccess) e = encode_codes(&m->v_rows, c.v, c, batch, in, unit, true);
+  return e;
 }
 
 cudaError_t init_cache_kernels() {

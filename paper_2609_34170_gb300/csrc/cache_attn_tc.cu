@@ -69,17 +69,6 @@ struct TcMaps {
   CUtensorMap k, v;   // a layer's codes [B Hkv T][hdp]: boxes of 64 dims x 128 rows (swizzled), x 64 rows
 };
 
-__device__ __forceinline__ float4 ld_cluster_f4(uint32_t a) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a));
-  return v;
-}
-__device__ __forceinline__ float ld_cluster_f1(uint32_t a) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a));
-  return v;
-}
-
 // 16 codes -> two 16-byte pieces of f16
 __device__ __forceinline__ void widen(uint4 w, uint32_t lo, uint32_t hi) {
   sts_u4(lo, make_uint4(e4m3_lo(w.x), e4m3_hi(w.x), e4m3_lo(w.y), e4m3_hi(w.y)));
@@ -772,10 +761,7 @@ cudaError_t launch_nb(CacheAttnArgs a, cudaStream_t st) {
     while (splits > 1 && a.clusters[splits] < tiles) --splits;
   if (splits > 1) splits = (units + (units + splits - 1) / splits - 1) / ((units + splits - 1) / splits);
   a.splits = splits;
-  TcMaps maps;
-  cudaError_t e = encode_codes(&maps.k, a.c.k, a.c, a.batch, BT, true);
-  if (e == cudaSuccess) e = encode_codes(&maps.v, a.c.v, a.c, a.batch, 64, false);
-  if (e != cudaSuccess) return e;
+  const TcMaps maps{a.maps->k_tc, a.maps->v_tc};
   // causal prompts: pairs whose caches take 48 MB together (beside the queries, in an L2 of 129)
   const long long pairs = (long long)a.c.Hkv * a.batch;
   a.group = 1;
@@ -809,12 +795,13 @@ cudaError_t init_nb(int* clusters) {
 
 static PFN_cuTensorMapEncodeTiled_v12000 g_enc = nullptr;
 
-cudaError_t encode_codes(CUtensorMap* m, const uint8_t* base, const CacheLayer& c, int batch, int box_rows, bool swizzle) {
+cudaError_t encode_codes(CUtensorMap* m, const uint8_t* base, const CacheLayer& c, int batch, int in, int box_rows,
+                         bool swizzle) {
   cuuint64_t dims[2] = {(cuuint64_t)c.hdp, (cuuint64_t)batch * c.Hkv * c.T};
   cuuint64_t strides[1] = {(cuuint64_t)c.hdp};
-  cuuint32_t box[2] = {64u, (cuuint32_t)box_rows}, estr[2] = {1, 1};
+  cuuint32_t box[2] = {(cuuint32_t)in, (cuuint32_t)box_rows}, estr[2] = {1, 1};
   const CUresult r = g_enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(base), dims, strides, box, estr,
-                           CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, !swizzle ? CU_TENSOR_MAP_SWIZZLE_NONE : (in == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B), CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
@@ -841,8 +828,6 @@ cudaError_t launch_cache_attend_tc(const CacheAttnArgs& a, cudaStream_t st) {
 }
 
 cudaError_t init_cache_tc_kernels(int hdp, int* clusters) {
-  const cudaError_t e = cache_tc_encoder();
-  if (e != cudaSuccess) return e;
   switch (hdp) {
     case 64: return init_nb<1>(clusters);
     case 128: return init_nb<2>(clusters);

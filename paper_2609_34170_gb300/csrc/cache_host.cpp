@@ -32,6 +32,7 @@ struct ravel_cache_ctx {
   ErrorWord* err = nullptr;
   int* err_host = nullptr;       // pinned, mapped: the error word's mirror
   std::vector<void*> allocs;
+  std::vector<CacheMaps> maps;   // by layer
   std::string last_error;
 
   CacheLayer layer(int l) const {
@@ -126,6 +127,7 @@ ravel_status ravel_cache_create(const ravel_cache_config* cfg, int device, ravel
   };
   try {
     c->allocs.reserve(16);
+    c->maps.resize(cfg->layers);
   } catch (...) {
     delete c;
     return RAVEL_ENOMEM;
@@ -140,10 +142,8 @@ ravel_status ravel_cache_create(const ravel_cache_config* cfg, int device, ravel
   get(&c->part_ml, sizeof(float2) * part_rows);
   get(&c->arrived, sizeof(unsigned) * kCacheSplitCtas);
   get(&c->row_ml, sizeof(float2) * cfg->max_batch * (size_t)cfg->n_q_heads * cfg->max_queries);
-  if (c->dt == DT_BF16) {
-    c->mass_ws_bytes = cache_mass_ws_bytes((int)heads, c->T, c->num_sms);
-    get(&c->mass_ws, c->mass_ws_bytes);
-  }
+  c->mass_ws_bytes = cache_mass_ws_bytes((int)heads, c->T, c->num_sms);
+  get(&c->mass_ws, c->mass_ws_bytes);
   get(&c->q_ws, (size_t)c->num_sms * kCacheTcRows * c->hdp * 2);
   get(&c->err, sizeof(ErrorWord));
   if (e == cudaSuccess) {
@@ -153,6 +153,7 @@ ravel_status ravel_cache_create(const ravel_cache_config* cfg, int device, ravel
     if (e == cudaSuccess) *c->err_host = 0;
     if (e == cudaSuccess) e = cudaHostGetDevicePointer((void**)&w.mirror, c->err_host, 0);
     if (e == cudaSuccess) e = cudaMemcpy(c->err, &w, sizeof w, cudaMemcpyHostToDevice);
+    for (int l = 0; l < cfg->layers && e == cudaSuccess; ++l) e = encode_layer(&c->maps[l], c->layer(l), cfg->max_batch);
     if (e == cudaSuccess) e = init_cache_kernels();
     if (e == cudaSuccess) e = init_cache_tc_kernels(c->hdp, c->clusters);
     if (e == cudaSuccess) e = init_cache_mass_tc_kernels();
@@ -221,6 +222,7 @@ ravel_status ravel_cache_attend(ravel_cache_t* c, int layer, int batch, int n, c
   if (mass && mass_stride < max_length) return fail(c, RAVEL_ESHAPE, "attend: mass_stride below max_length");
   CacheAttnArgs a{};
   a.c = c->layer(layer);
+  a.maps = &c->maps[layer];
   a.q = q;
   a.out = out;
   a.q_robot = q_robot_stride;

@@ -291,9 +291,8 @@ cudaError_t launch_cache_mass_tc(CacheAttnArgs a, cudaStream_t st) {
   long long chunks = std::max(1ll, (a.num_sms + heads - 1) / heads);
   chunks = std::min(chunks, std::max(1ll, (long long)(a.mass_ws_bytes / (8ull * a.mass_pitch)) / heads));
   a.splits = (int)std::min(chunks, (long long)a.row_tiles);
-  MassMaps maps;
-  cudaError_t e = encode_codes(&maps.k, a.c.k, a.c, a.batch, BT, true);
-  if (e != cudaSuccess) return e;
+  const MassMaps maps{a.maps->k_tc};
+  cudaError_t e;
   switch (a.c.hdp) {
     case 64: e = launch_nb<1>(maps, a, st); break;
     case 128: e = launch_nb<2>(maps, a, st); break;
@@ -311,8 +310,7 @@ size_t cache_mass_ws_bytes(int heads, int T, int num_sms) {
 }
 
 cudaError_t init_cache_mass_tc_kernels() {
-  cudaError_t e = cache_tc_encoder();
-  if (e == cudaSuccess) e = init_nb<1>();
+  cudaError_t e = init_nb<1>();
   if (e == cudaSuccess) e = init_nb<2>();
   if (e == cudaSuccess) e = init_nb<3>();
   if (e == cudaSuccess) e = init_nb<4>();

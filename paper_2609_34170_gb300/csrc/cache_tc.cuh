@@ -182,8 +182,21 @@ __device__ __forceinline__ float q_factor(int e, float scale_log2) {
   return exp2i(-min(kQExp + 127 - e, 126)) * scale_log2;
 }
 
-// the encoder of tensor maps; a layer's codes [B Hkv T][hdp] in boxes of 64 dims x box_rows
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t a) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ float ld_cluster_f1(uint32_t a) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a));
+  return v;
+}
+
+// the encoder of tensor maps; a layer's codes [B Hkv T][hdp] in boxes of `in` dims x
+// box_rows, swizzled over rows of `in` bytes or not
 cudaError_t cache_tc_encoder();
-cudaError_t encode_codes(CUtensorMap* m, const uint8_t* base, const CacheLayer& c, int batch, int box_rows, bool swizzle);
+cudaError_t encode_codes(CUtensorMap* m, const uint8_t* base, const CacheLayer& c, int batch, int in, int box_rows,
+                         bool swizzle);
 
 }  // namespace ravel
