@@ -5,6 +5,10 @@ A robot's prompt goes in layer by layer (``append``, ``attend``), then its
 decoded tokens one by one; ``evict`` shrinks what is held to a budget, and
 ``read`` returns it in the layout of a layer of ``RollingSession.set_context``.
 Positions, lengths and counts are int32 CUDA tensors with one entry per robot.
+Every call is enqueued on ``stream`` (None: the current one of the cache's device).
+
+The calls look their arguments over and hand addresses to the library, nothing
+else: at one token the host takes as long as the GPU.
 """
 from __future__ import annotations
 
@@ -27,11 +31,14 @@ class ContextCache:
         self.dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
         self.handle = B.ravel_cache_create(layers, n_q_heads, n_kv_heads, head_dim, max_tokens, max_batch, max_queries,
                                            B.RAVEL_BF16 if dtype == "bf16" else B.RAVEL_FP32, device)
+        self._lib = B.load()
+        self._int32, self._float32 = torch.int32, torch.float32
 
-    def _of_dtype(self, t, heads, name):
-        if t.dtype != self.dtype or t.dim() != 4 or t.shape[2] != heads or t.shape[3] != self.head_dim:
-            raise ValueError(f"{name} must be [batch, n, {heads}, {self.head_dim}] of dtype {self.dtype}, "
-                             f"got {tuple(t.shape)} of {t.dtype}")
+    # -- arguments
+    def _stream(self, stream):
+        if stream is None:
+            return B.current_raw_stream(self.device.index)
+        return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
     def _empty(self, shape, dtype, stream):
         """A new tensor of the stream that is going to write it."""
@@ -43,11 +50,49 @@ class ContextCache:
         with t.cuda.stream(stream):
             return t.empty(shape, dtype=dtype, device=self.device)
 
+    def _rows(self, x, heads, name):
+        """Strides (robot, token) of a [batch, n, heads, head_dim] tensor whose heads are contiguous."""
+        shape = x.shape
+        if x.dtype is not self.dtype or len(shape) != 4 or shape[2] != heads or shape[3] != self.head_dim or \
+                x.get_device() != self.device.index:
+            raise ValueError(f"{name} must be [batch, n, {heads}, {self.head_dim}] of dtype {self.dtype} on {self.device}, "
+                             f"got {tuple(shape)} of {x.dtype} on {x.device}")
+        robot, token, head, dim = x.stride()
+        if dim != 1 or (head != self.head_dim and heads > 1):
+            raise ValueError(f"{name}: the heads of a token must be contiguous")
+        return robot, token
+
+    def _ints(self, x, batch, name):
+        """Address of an int32 tensor [batch], or None."""
+        if x is None:
+            return None
+        if x.dtype is not self._int32 or x.shape != (batch,) or x.get_device() != self.device.index or not x.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous int32 tensor [{batch}] on {self.device}")
+        return x.data_ptr()
+
+    def _mass(self, mass, batch):
+        """Address and length of a mass's rows."""
+        shape = mass.shape
+        if len(shape) != 3 or (batch is not None and shape[0] != batch) or shape[1] != self.n_kv_heads or \
+                mass.dtype is not self._float32 or mass.get_device() != self.device.index or not mass.is_contiguous():
+            raise ValueError(f"mass must be a contiguous float32 tensor [{'batch' if batch is None else batch}, "
+                             f"{self.n_kv_heads}, tokens] on {self.device}, got {tuple(shape)} of {mass.dtype}")
+        return mass.data_ptr(), shape[2]
+
+    # -- calls
     def append(self, layer: int, k, v, starts=None, counts=None, stream=None):
         """Store tokens k, v [B, n, Hkv, hd]: token i < counts[b] of robot b at
         position starts[b] + i (None: all n of them; from position 0)."""
-        self._of_dtype(k, self.n_kv_heads, "k")
-        B.ravel_cache_append(self.handle, layer, k, v, starts, counts, stream)
+        strides = self._rows(k, self.n_kv_heads, "k")
+        shape = k.shape
+        if v.shape != shape or self._rows(v, self.n_kv_heads, "v") != strides:
+            raise ValueError("k and v must have the same shape and strides")
+        batch, n = shape[0], shape[1]
+        status = self._lib.ravel_cache_append(self.handle, layer, batch, n, k.data_ptr(), v.data_ptr(), strides[0], strides[1],
+                                              self._ints(starts, batch, "starts"), self._ints(counts, batch, "counts"),
+                                              self._stream(stream))
+        if status:
+            B._check_cache(self.handle, status, "ravel_cache_append")
 
     def attend(self, layer: int, q, lengths, counts=None, causal: bool = True, window: int = 0, sinks: int = 0,
                scale: float = 0.0, max_length: int | None = None, out=None, mass=None, add_mass: bool = False, stream=None):
@@ -57,17 +102,25 @@ class ContextCache:
         `window` of those and the first `sinks`.  mass (float32 [B, Hkv, tokens]):
         receives, or with add_mass is increased by, the attention mass that each
         token drew.  max_length: a bound of the lengths, if one below the
-        cache's (or mass's) room is known; launches are planned for it."""
-        self._of_dtype(q, self.n_q_heads, "q")
-        if max_length is None:
-            max_length = self.max_tokens
-        if mass is not None:
-            if mass.dim() != 3 or mass.shape[:2] != (q.shape[0], self.n_kv_heads):
-                raise ValueError(f"mass must be [{q.shape[0]}, {self.n_kv_heads}, tokens], got {tuple(mass.shape)}")
+        cache's room is known; launches are planned for it."""
+        qr, qt = self._rows(q, self.n_q_heads, "q")
+        shape = q.shape
+        batch, n = shape[0], shape[1]
         if out is None:
-            out = self._empty(q.shape, q.dtype, stream)
-        B.ravel_cache_attend(self.handle, layer, q, out, lengths, counts, max_length, causal, window, sinks, scale, mass,
-                             add_mass, stream)
+            out = self._empty(shape, q.dtype, stream)
+        elif out.shape != shape:
+            raise ValueError("out must have q's shape")
+        outr, outt = self._rows(out, self.n_q_heads, "out")
+        if lengths is None:
+            raise ValueError("lengths must be given")
+        mass_at, mass_len = self._mass(mass, batch) if mass is not None else (None, 0)
+        status = self._lib.ravel_cache_attend(
+            self.handle, layer, batch, n, q.data_ptr(), qr, qt, out.data_ptr(), outr, outt,
+            self._ints(lengths, batch, "lengths"), self._ints(counts, batch, "counts"),
+            self.max_tokens if max_length is None else max_length, 1 if causal else 0, window, sinks, scale, mass_at, mass_len,
+            1 if add_mass else 0, self._stream(stream))
+        if status:
+            B._check_cache(self.handle, status, "ravel_cache_attend")
         return out
 
     def evict(self, layer: int, to: "ContextCache", to_layer: int, lengths, mass, keep: int, sinks: int = 0,
@@ -76,22 +129,28 @@ class ContextCache:
         to_layer of `to`: the first `sinks`, the last `recent`, and the heaviest
         of the rest by mass [B, Hkv, tokens].  Returns their number per robot
         [B], their positions [B, Hkv, keep] (then -1) and their mass (then 0)."""
-        t = self.torch
-        if mass.dim() != 3 or mass.shape[1] != self.n_kv_heads:
-            raise ValueError(f"mass must be [batch, {self.n_kv_heads}, tokens], got {tuple(mass.shape)}")
+        mass_at, mass_len = self._mass(mass, None)
         batch = mass.shape[0]
-        new_lengths = self._empty((batch,), t.int32, stream)
-        index = self._empty((batch, self.n_kv_heads, max(keep, 1)), t.int32, stream)
-        new_mass = self._empty(index.shape, t.float32, stream)
-        B.ravel_cache_evict(self.handle, layer, to.handle, to_layer, lengths, mass, keep, sinks, recent, new_lengths, index,
-                            new_mass, stream)
+        new_lengths = self._empty((batch,), self._int32, stream)
+        shape = (batch, self.n_kv_heads, max(keep, 1))
+        index, new_mass = self._empty(shape, self._int32, stream), self._empty(shape, self._float32, stream)
+        status = self._lib.ravel_cache_evict(self.handle, layer, to.handle, to_layer, batch, self._ints(lengths, batch, "lengths"),
+                                             mass_at, mass_len, keep, sinks, recent, new_lengths.data_ptr(), index.data_ptr(),
+                                             new_mass.data_ptr(), self._stream(stream))
+        if status:
+            B._check_cache(self.handle, status, "ravel_cache_evict")
         return new_lengths, index, new_mass
 
     def read(self, layer: int, batch: int, n: int, firsts=None, lengths=None, stream=None):
         """The values held of n tokens per robot from position firsts[b] on
         (None: 0), zeros from lengths[b] on: k, v [B, Hkv, n, hd]."""
-        k, v = (self._empty((batch, self.n_kv_heads, n, self.head_dim), self.dtype, stream) for _ in "kv")
-        B.ravel_cache_read(self.handle, layer, k, v, firsts, lengths, stream)
+        shape = (batch, self.n_kv_heads, n, self.head_dim)
+        k, v = self._empty(shape, self.dtype, stream), self._empty(shape, self.dtype, stream)
+        status = self._lib.ravel_cache_read(self.handle, layer, batch, n, self._ints(firsts, batch, "firsts"),
+                                            self._ints(lengths, batch, "lengths"), k.data_ptr(), v.data_ptr(),
+                                            self._stream(stream))
+        if status:
+            B._check_cache(self.handle, status, "ravel_cache_read")
         return k, v
 
     def reset(self):

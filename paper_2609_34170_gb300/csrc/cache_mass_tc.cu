@@ -255,15 +255,22 @@ __global__ void __launch_bounds__(MT, 1) cache_mass_tc_kernel(const __grid_const
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256u) : "memory");
 }
 
-// The chunks' sums, in their order.
+// The chunks' sums: eight threads per token, every eighth of them each, then in the
+// threads' order -- the same order in every call.
 __global__ void __launch_bounds__(256) cache_mass_sum_kernel(CacheAttnArgs a) {
-  const int j = blockIdx.x * 256 + threadIdx.x;
-  if (j >= a.max_length) return;
+  __shared__ float sums[8][32];
+  const int lane = threadIdx.x & 31, eighth = threadIdx.x >> 5, j = blockIdx.x * 32 + lane;
   const size_t head = (size_t)blockIdx.z * a.c.Hkv + blockIdx.y;
-  const float* part = a.mass_ws + head * a.splits * 2 * a.mass_pitch + j;
+  const float* part = a.mass_ws + head * a.splits * 2 * a.mass_pitch + j;   // (j < pitch, a multiple of 32)
   float v = 0.f;
 #pragma unroll 8
-  for (int c = 0; c < 2 * a.splits; ++c) v += __ldcg(part + (size_t)c * a.mass_pitch);
+  for (int c = eighth; c < 2 * a.splits; c += 8) v += __ldcg(part + (size_t)c * a.mass_pitch);
+  sums[eighth][lane] = v;
+  __syncthreads();
+  if (eighth || j >= a.max_length) return;
+  v = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v += sums[e][lane];
   float* mass = a.mass + head * a.mass_stride + j;
   if (!a.mass_add) *mass = v;
   else if (j < a.lengths[blockIdx.z]) *mass += v;
@@ -300,7 +307,7 @@ cudaError_t launch_cache_mass_tc(CacheAttnArgs a, cudaStream_t st) {
     default: e = launch_nb<4>(maps, a, st); break;
   }
   if (e != cudaSuccess) return e;
-  cache_mass_sum_kernel<<<dim3((a.max_length + 255) / 256, a.c.Hkv, a.batch), 256, 0, st>>>(a);
+  cache_mass_sum_kernel<<<dim3((a.max_length + 31) / 32, a.c.Hkv, a.batch), 256, 0, st>>>(a);
   return cudaGetLastError();
 }
 

@@ -1,6 +1,10 @@
 // Storing into the 8-bit context cache, reading it back and eviction by
 // attention mass.
+#include <algorithm>
+
 #include "cache.cuh"
+#include "launch.h"
+#include "tc_common.cuh"
 
 namespace ravel {
 namespace {
@@ -154,6 +158,12 @@ __global__ void __launch_bounds__(256) cache_read_kernel(ReadArgs a) {
 
 constexpr int kSelThreads = 1024;
 
+__device__ __forceinline__ unsigned ld_cluster_u1(uint32_t a) {
+  unsigned v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+
 // Order of masses as unsigned integers: ascending, -0 = +0, NaN above all.
 __device__ __forceinline__ uint32_t mass_key(float x) {
   const uint32_t u = __float_as_uint(x + 0.f);
@@ -161,19 +171,25 @@ __device__ __forceinline__ uint32_t mass_key(float x) {
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-// The tokens that one (robot, KV head) keeps: the key of the last one in by a
-// radix selection over the middle's masses (four histograms of 8 bits), then
-// one ordered pass that gives each kept token its place.  Ties go to the
-// earlier tokens.  No order of arrival enters the result: the histograms count.
-__global__ void __launch_bounds__(kSelThreads) cache_select_kernel(EvictArgs a) {
-  __shared__ unsigned hist[256];
+// The tokens that one (robot, KV head) keeps: the key of the last one in by a radix
+// selection over the middle's masses (four histograms of 8 bits), then one ordered
+// pass that gives each kept token its place.  Ties go to the earlier tokens.  No order
+// of arrival enters the result: the histograms count.
+//
+// A cluster per (robot, KV head), each of its CTAs with a run of the tokens; the
+// histograms and the counts are added up through distributed shared memory.  The
+// masses are read five times, from L2 after the first: one CTA took 66 us for 65537
+// tokens, 64 dependent turns of the loop per pass.
+__global__ void __launch_bounds__(kSelThreads) cache_select_kernel(EvictArgs a, int ctas) {
+  __shared__ unsigned hist[2][256], sums[256];
   __shared__ uint32_t sel_bin, sel_left;
   __shared__ unsigned totals[2][32];
-  const int h = blockIdx.x, b = blockIdx.y, Hkv = a.from.Hkv;
+  __shared__ unsigned kept_here[2], before_here[2];   // surely in, ties: of this CTA's run, of the runs before it
+  const int h = blockIdx.x / ctas, rank = blockIdx.x % ctas, b = blockIdx.y, Hkv = a.from.Hkv;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   int len = a.lengths[b];
   if (len < 0 || len > a.max_tokens || len > a.mass_stride) {
-    if (tid == 0 && h == 0) raise_error(a.err, ERR_SHAPE);
+    if (tid == 0 && blockIdx.x == 0) raise_error(a.err, ERR_SHAPE);
     len = 0;
   }
   const int kept = min(len, a.keep);
@@ -181,30 +197,48 @@ __global__ void __launch_bounds__(kSelThreads) cache_select_kernel(EvictArgs a) 
   const float* mass = a.mass + head * a.mass_stride;
   int* index = a.index + head * a.keep;
   float* nm = a.new_mass ? a.new_mass + head * a.keep : nullptr;
-  if (tid == 0 && h == 0) a.new_lengths[b] = kept;
-  for (int i = kept + tid; i < a.keep; i += kSelThreads) {
+  if (tid == 0 && blockIdx.x == 0) a.new_lengths[b] = kept;
+  for (int i = kept + rank * kSelThreads + tid; i < a.keep; i += ctas * kSelThreads) {
     index[i] = -1;
     if (nm) nm[i] = 0.f;
   }
-  if (len <= a.keep) {
-    for (int i = tid; i < kept; i += kSelThreads) {
+  if (len <= a.keep) {   // (all of the cluster)
+    for (int i = rank * kSelThreads + tid; i < kept; i += ctas * kSelThreads) {
       index[i] = i;
       if (nm) nm[i] = mass[i];
     }
     return;
   }
   const int lo = a.sinks, hi = len - a.recent;   // the middle, longer than what stays of it
+  const int run = ((len + ctas - 1) / ctas + kSelThreads - 1) / kSelThreads * kSelThreads;
+  const int r0 = min(rank * run, len), r1 = min(r0 + run, len);
+  const int m0 = max(lo, r0), m1 = min(hi, r1);   // the middle's part of this run
   uint32_t left = (uint32_t)(a.keep - a.sinks - a.recent);
   uint32_t prefix = 0xffffffffu;   // (nothing of the middle stays: no key is above, no tie taken)
   if (left > 0) {
     prefix = 0u;
     uint32_t mask = 0u;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) hist[tid] = 0u;
+    int buf = 0;
+    for (int shift = 24; shift >= 0; shift -= 8, buf ^= 1) {
+      // (two histograms in turn: a CTA may still read this one's while its neighbours are at the next)
+      if (tid < 256) hist[buf][tid] = 0u;
       __syncthreads();
-      for (int j = lo + tid; j < hi; j += kSelThreads) {
-        const uint32_t key = mass_key(mass[j]);
-        if ((key & mask) == prefix) atomicAdd(&hist[(key >> shift) & 255u], 1u);
+#pragma unroll 8
+      for (int j = m0 + tid; j < m1; j += kSelThreads) {
+        const uint32_t key = mass_key(__ldg(mass + j));
+        if ((key & mask) == prefix) atomicAdd(&hist[buf][(key >> shift) & 255u], 1u);
+      }
+      if (ctas > 1) cluster_sync();
+      else __syncthreads();
+      if (tid < 256) {
+        unsigned n = 0;
+        if (ctas > 1) {
+          const uint32_t at = smem_u32(&hist[buf][tid]);
+          for (int q = 0; q < ctas; ++q) n += ld_cluster_u1(mapa_shared(at, (uint32_t)q));
+        } else {
+          n = hist[buf][tid];
+        }
+        sums[tid] = n;
       }
       __syncthreads();
       if (warp == 0) {
@@ -212,7 +246,7 @@ __global__ void __launch_bounds__(kSelThreads) cache_select_kernel(EvictArgs a) 
         unsigned n[8], sum = 0;
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-          n[q] = hist[255 - 8 * lane - q];
+          n[q] = sums[255 - 8 * lane - q];
           sum += n[q];
         }
         unsigned before = sum;
@@ -241,15 +275,51 @@ __global__ void __launch_bounds__(kSelThreads) cache_select_kernel(EvictArgs a) 
       left = sel_left;
     }
   }
-  // kept before j: those surely in (heavier, first, last) and as many ties as still fit
-  unsigned sure = 0, ties = 0;
-  int buf = 0;
-  for (int base = 0; base < len; base += kSelThreads, buf ^= 1) {
-    const int j = base + tid;
-    const float m = j < len ? mass[j] : 0.f;
+  // which tokens are surely in (heavier, first, last), and which are ties
+  auto kind = [&](int j, float& m, bool& in, bool& tie) {
+    m = j < r1 ? __ldg(mass + j) : 0.f;
     const uint32_t key = mass_key(m);
-    const bool always = j < len && (j < lo || j >= hi), mid = j >= lo && j < hi;
-    const bool in = always || (mid && key > prefix), tie = mid && key == prefix;
+    const bool always = j < r1 && (j < lo || j >= hi), mid = j >= m0 && j < m1;
+    in = always || (mid && key > prefix);
+    tie = mid && key == prefix;
+  };
+  unsigned sure = 0, ties = 0;
+  if (ctas > 1) {   // of the runs before this one
+    if (tid < 2) kept_here[tid] = 0u;
+    __syncthreads();
+    unsigned n0 = 0, n1 = 0;
+#pragma unroll 4
+    for (int j = r0 + tid; j < r1; j += kSelThreads) {
+      float m;
+      bool in, tie;
+      kind(j, m, in, tie);
+      n0 += in;
+      n1 += tie;
+    }
+    n0 = __reduce_add_sync(0xffffffffu, n0);
+    n1 = __reduce_add_sync(0xffffffffu, n1);
+    if (lane == 0) {
+      atomicAdd(&kept_here[0], n0);
+      atomicAdd(&kept_here[1], n1);
+    }
+    cluster_sync();
+    if (tid < 2) {
+      unsigned n = 0;
+      for (int q = 0; q < rank; ++q) n += ld_cluster_u1(mapa_shared(smem_u32(&kept_here[tid]), (uint32_t)q));
+      before_here[tid] = n;
+    }
+    __syncthreads();
+    sure = before_here[0];
+    ties = before_here[1];
+  }
+  // kept before j: those surely in and as many ties as still fit
+  int buf = 0;
+#pragma unroll 4
+  for (int base = r0; base < r1; base += kSelThreads, buf ^= 1) {
+    const int j = base + tid;
+    float m;
+    bool in, tie;
+    kind(j, m, in, tie);
     const unsigned bi = __ballot_sync(0xffffffffu, in), bt = __ballot_sync(0xffffffffu, tie);
     if (lane == 0) totals[buf][warp] = __popc(bi) | __popc(bt) << 16;
     __syncthreads();
@@ -272,6 +342,7 @@ __global__ void __launch_bounds__(kSelThreads) cache_select_kernel(EvictArgs a) 
     sure += all & 0xffffu;
     ties += all >> 16;
   }
+  if (ctas > 1) cluster_sync();   // nobody leaves while its counts are read
 }
 
 // The kept rows into the other cache: a CTA per block of 16, as in append.
@@ -316,8 +387,10 @@ cudaError_t launch_cache_read(const ReadArgs& a, Dtype dt, cudaStream_t st) {
 }
 
 cudaError_t launch_cache_evict(const EvictArgs& a, cudaStream_t st) {
-  cache_select_kernel<<<dim3(a.from.Hkv, a.batch), kSelThreads, 0, st>>>(a);
-  cudaError_t e = cudaGetLastError();
+  // a CTA per 4096 tokens, up to a cluster of 8 (at 816 tokens a cluster's barriers take longer than they save)
+  const int ctas = (int)std::min(8ll, std::max(1ll, std::min((long long)a.max_tokens, a.mass_stride) / 4096));
+  cudaError_t e = launch_kernel_cluster(cache_select_kernel, dim3(a.from.Hkv * ctas, a.batch), dim3(kSelThreads), 0, st,
+                                        dim3(ctas, 1, 1), a, ctas);
   if (e != cudaSuccess) return e;
   const dim3 grid((a.keep + kCacheBlock - 1) / kCacheBlock, a.to.Hkv, a.batch);
   cache_move_kernel<<<grid, a.to.hdp, 0, st>>>(a);
