@@ -189,7 +189,11 @@ struct RowsShape {
   // units in flight per warp, K and V (24 KB; fp32's take 16: its fragments are twice as many)
   static constexpr int D = NP == 2 ? 2 : 3;
   static constexpr int ring = RW * D * 2 * (int)Unit<HDP>::bytes;
-  static constexpr int join = (RW + 1) * 16 * HDP * 4;   // the warps' outputs and their sum, over the ring
+  // the warps' outputs, over the ring: rows JS floats apart, four floats more per 32 dims, so
+  // that the 16-byte pieces of a store (two rows, every 32nd or 16th dim) fall on different banks
+  static constexpr int JS = HDP == 64 ? 72 : (HDP == 128 ? 144 : (HDP == 192 ? 240 : 304));
+  static __device__ __forceinline__ int pos(int row, int d) { return row * JS + d + (d >> 5) * 4; }
+  static constexpr int join = RW * 16 * JS * 4 + 16 * HDP * 4;   // and their sum
   static constexpr int bytes = frag + (ring > join ? ring : join);
 };
 
@@ -203,8 +207,8 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
   using Shape = RowsShape<HDP, NP>;
   constexpr int NT = Un::NT, U = Un::U, KS = HDP / 16, D = Shape::D;
   extern __shared__ __align__(1024) uint8_t smem[];
-  float* joint = (float*)smem;                          // [RW][16][HDP] outputs of the warps, over the ring
-  float* mine = joint + RW * 16 * HDP;                  // [16][HDP] their sum
+  float* joint = (float*)smem;                          // [RW][16][JS] outputs of the warps, over the ring
+  float* mine = joint + RW * 16 * Shape::JS;            // [16][HDP] their sum
   uint32_t* frag = (uint32_t*)(smem + Shape::bytes - Shape::frag);   // [NP][KS][32][4]
   __shared__ float fac[16];
   __shared__ float2 warp_ml[RW][16], split_w[16];
@@ -474,15 +478,19 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
     const float e2 = real ? pow2f(W[rr] - m[rr]) : 0.f;
     const int row = g + 8 * rr;
     if (c == 0) warp_ml[warp][row] = make_float2(m[rr], l[rr]);
-    float* dst = joint + ((size_t)warp * 16 + row) * HDP;
+    float* dst = joint + warp * 16 * Shape::JS;
     if (row < rows) {
 #pragma unroll
       for (int wi = 0; wi < HDP / 32; ++wi)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int q = 0; q < 2; ++q)
-            dst[ValueUnit<HDP>::dim(wi, i, 2 * c + q)] = real ? o[4 * wi + i][2 * rr + q] * f * e2 : 0.f;
+        for (int q = 0; q < 2; ++q) {
+          float4 x;   // four dims side by side
+          x.x = real ? o[4 * wi][2 * rr + q] * f * e2 : 0.f;
+          x.y = real ? o[4 * wi + 1][2 * rr + q] * f * e2 : 0.f;
+          x.z = real ? o[4 * wi + 2][2 * rr + q] * f * e2 : 0.f;
+          x.w = real ? o[4 * wi + 3][2 * rr + q] * f * e2 : 0.f;
+          *(float4*)(dst + Shape::pos(row, ValueUnit<HDP>::dim(wi, 0, 2 * c + q))) = x;
+        }
     }
   }
   __syncthreads();
@@ -510,7 +518,7 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
 #pragma unroll
     for (int w = 0; w < RW; ++w) {
       const float wt = warp_ml[w][row].x;
-      acc += wt != 0.f ? wt * joint[((size_t)w * 16 + row) * HDP + d] : 0.f;
+      acc += wt != 0.f ? wt * joint[w * 16 * Shape::JS + Shape::pos(row, d)] : 0.f;
     }
     return acc;
   };
@@ -531,17 +539,23 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
     cluster_sync();
     if ((int)threadIdx.x < rows) {
       const uint32_t at = smem_u32(&split_w[threadIdx.x]);
-      float M = -INFINITY, S = 0.f;
-      for (int q = 0; q < a.splits; ++q) M = fmaxf(M, ld_cluster_f1(mapa_shared(at, (uint32_t)q)));
-      for (int q = 0; q < a.splits; ++q) {
-        const uint32_t from = mapa_shared(at, (uint32_t)q);
-        const float2 x = make_float2(ld_cluster_f1(from), ld_cluster_f1(from + 4));
-        const float wt = x.y != x.y ? x.y : (x.x == -INFINITY ? 0.f : exp2f(x.x - M) * x.y);
-        split_wt[q][threadIdx.x] = wt;
-        S += wt;
+      float2 x[8];   // (all on their way together)
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const uint32_t from = mapa_shared(at, (uint32_t)min(q, a.splits - 1));
+        x[q] = make_float2(ld_cluster_f1(from), ld_cluster_f1(from + 4));
+      }
+      float M = -INFINITY, S = 0.f, wt[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) M = fmaxf(M, x[q].x);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        wt[q] = q >= a.splits ? 0.f : (x[q].y != x[q].y ? x[q].y : (x[q].x == -INFINITY ? 0.f : exp2f(x[q].x - M) * x[q].y));
+        S += wt[q];
       }
       const float inv = !(S <= 0.f) ? 1.f / S : 0.f;
-      for (int q = 0; q < a.splits; ++q) split_wt[q][threadIdx.x] *= inv;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) split_wt[q][threadIdx.x] = wt[q] * inv;
       if (a.mass && split == 0) a.row_ml[head * a.n * a.G + r0 + threadIdx.x] = row_weight(M, S, kPExp);
     }
     __syncthreads();
