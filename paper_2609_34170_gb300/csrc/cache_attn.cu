@@ -45,6 +45,15 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint4& a, uint32_t 
       : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
 }
 
+__device__ __forceinline__ uint32_t word(const uint4& x, int i) { return i == 0 ? x.x : (i == 1 ? x.y : (i == 2 ? x.z : x.w)); }
+
+// An 8 x 8 tile of 16-bit values, a row per four lanes, transposed across the warp.
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
 // Query rows r0 .. r0 + 15 into shared memory as the A fragments of the MMAs:
 // word (piece, k-step, lane) holds rows lane / 4 and + 8, dims 64 j + 16 (lane % 4)
 // + 4 s + 0 .. 3 of k-step 4 j + s.  Rows that do not exist are zeros.  fac[r]:
@@ -183,7 +192,7 @@ struct ValueUnit {
   }
 };
 
-template <int HDP, int NP>
+template <int HDP, int NP, int RT>
 struct RowsShape {
   static constexpr int frag = NP * (HDP / 16) * 512;   // bytes of Q's fragments
   // units in flight per warp, K and V (24 KB; fp32's take 16: its fragments are twice as many)
@@ -191,9 +200,10 @@ struct RowsShape {
   static constexpr int ring = RW * D * 2 * (int)Unit<HDP>::bytes;
   // the warps' outputs, over the ring: rows JS floats apart, four floats more per 32 dims, so
   // that the 16-byte pieces of a store (two rows, every 32nd or 16th dim) fall on different banks
-  static constexpr int JS = HDP == 64 ? 72 : (HDP == 128 ? 144 : (HDP == 192 ? 240 : 304));
+  static constexpr int JS = RT == 8 ? (HDP == 64 ? 84 : (HDP == 128 ? 148 : (HDP == 192 ? 228 : 292)))
+                                    : (HDP == 64 ? 72 : (HDP == 128 ? 144 : (HDP == 192 ? 240 : 304)));
   static __device__ __forceinline__ int pos(int row, int d) { return row * JS + d + (d >> 5) * 4; }
-  static constexpr int join = RW * 16 * JS * 4 + 16 * HDP * 4;   // and their sum
+  static constexpr int join = RW * RT * JS * 4 + RT * HDP * 4;   // and their sum
   static constexpr int bytes = frag + (ring > join ? ring : join);
 };
 
@@ -201,14 +211,14 @@ struct RowsMaps {
   CUtensorMap k, v;   // a layer's codes [B Hkv T][HDP] in boxes of Unit::IN dims x U rows, swizzled
 };
 
-template <int HDP, int NP, typename T>
+template <int HDP, int NP, int RT, typename T>
 __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_constant__ RowsMaps maps, CacheAttnArgs a) {
   using Un = Unit<HDP>;
-  using Shape = RowsShape<HDP, NP>;
+  using Shape = RowsShape<HDP, NP, RT>;
   constexpr int NT = Un::NT, U = Un::U, KS = HDP / 16, D = Shape::D;
   extern __shared__ __align__(1024) uint8_t smem[];
-  float* joint = (float*)smem;                          // [RW][16][JS] outputs of the warps, over the ring
-  float* mine = joint + RW * 16 * Shape::JS;            // [16][HDP] their sum
+  float* joint = (float*)smem;                          // [RW][RT][JS] outputs of the warps, over the ring
+  float* mine = joint + RW * RT * Shape::JS;            // [RT][HDP] their sum
   uint32_t* frag = (uint32_t*)(smem + Shape::bytes - Shape::frag);   // [NP][KS][32][4]
   __shared__ float fac[16];
   __shared__ float2 warp_ml[RW][16], split_w[16];
@@ -219,7 +229,7 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
   const int b = blockIdx.z, h = blockIdx.y, tile = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
   const CacheLayer& L = a.c;
-  const int r0 = tile * 16, rows = min(16, a.n * a.G - r0);
+  const int r0 = tile * RT, rows = min(RT, a.n * a.G - r0);
   const size_t head = (size_t)b * L.Hkv + h;
   if (smem_u32(smem) & 1023u) {   // (the swizzled layouts count on it)
     if (threadIdx.x == 0) raise_error(a.err, ERR_SHAPE);
@@ -236,7 +246,7 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
       a.row_ml[head * a.n * a.G + r0 + threadIdx.x] = make_float2(0.f, 0.f);
     return;
   }
-  tile_sight(a, s, r0, r0 + 15, U);
+  tile_sight(a, s, r0, r0 + RT - 1, U);
   const int u0 = (int)((long long)s.units * split / a.splits), u1 = (int)((long long)s.units * (split + 1) / a.splits);
 
   // each warp's ring of units: its own loads, which it alone waits for
@@ -264,19 +274,33 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
   if (threadIdx.x < 16) fac[threadIdx.x] = 0.f;
   __syncthreads();
   stage_q<HDP, NP, T, RW * 32>(a, s, b, h, r0, frag, fac);
-  const RowMask mk[2] = {row_mask(a, s, r0 + g), row_mask(a, s, r0 + g + 8)};
-  const float rf[2] = {fac[g], fac[g + 8]};
+  // this lane's two rows: scores of rows g, g + 8 by tokens 2 c, 2 c + 1, or (RT = 8) of tokens
+  // g, g + 8 by rows 2 c, 2 c + 1
+  const int row_of[2] = {RT == 8 ? 2 * c : g, RT == 8 ? 2 * c + 1 : g + 8};
+  const RowMask mk[2] = {row_mask(a, s, r0 + row_of[0]), row_mask(a, s, r0 + row_of[1])};
+  const float rf[2] = {fac[row_of[0]], fac[row_of[1]]};
   // tokens that every row that exists sees: [full_lo, full_hi) and below a.sinks
-  const RowMask first = row_mask(a, s, r0), lastm = row_mask(a, s, min(r0 + 15, s.count * a.G - 1));
+  const RowMask first = row_mask(a, s, r0), lastm = row_mask(a, s, min(r0 + RT - 1, s.count * a.G - 1));
   const int full_hi = first.hi, full_lo = lastm.lo;
 
   const int8_t *KE = L.ke + head * (L.T / 16), *VE = L.ve + head * (L.T / 16);
 
-  float o[HDP / 8][4];
+  // outputs: rows g, g + 8 by dims 2 c, 2 c + 1 of each 8, or (RT = 8) dims g, g + 8 of each 16 by
+  // rows 2 c, 2 c + 1
+  constexpr int OT = RT == 8 ? HDP / 16 : HDP / 8;
+  float o[OT][4];
 #pragma unroll
-  for (int t = 0; t < HDP / 8; ++t)
+  for (int t = 0; t < OT; ++t)
 #pragma unroll
     for (int q = 0; q < 4; ++q) o[t][q] = 0.f;
+  uint32_t qb[RT == 8 && NP == 1 ? KS : 1][2];   // RT = 8: Q's fragments as B operands
+  if (RT == 8 && NP == 1) {
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      qb[ks][0] = frag[(ks * 32 + lane) * 4];
+      qb[ks][1] = frag[(ks * 32 + lane) * 4 + 2];
+    }
+  }
   float m[2] = {-INFINITY, -INFINITY}, W[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 
   // the exponents of a unit's blocks, one byte each
@@ -313,31 +337,76 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
     KeyUnit<HDP> kr[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) kr[t].load(unit, 16 * t, g, c);
-    float sc[NT][2][4];
+    // sc[t][hh][rr][q]: this lane's row rr, token 8 hh + 2 c + q of block t, or (RT = 8, q = 0) token
+    // 8 hh + g.  Few rows take K as the MMAs' A operand, 16 tokens by 8 rows: half the MMAs.
+    constexpr int QN = RT == 8 ? 1 : 2;
+    float sc[NT][2][2][QN];
+    if constexpr (RT == 8) {
+      // (where a unit has few tiles of scores, each has AC accumulators in turn: an MMA waits
+      // for the one before it in its tile)
+      constexpr int AC = 4 / NT;
+      float sa[AC][NT][4];
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+      for (int x = 0; x < AC; ++x)
 #pragma unroll
-      for (int hh = 0; hh < 2; ++hh)
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) sc[t][hh][q] = 0.f;
+          for (int q = 0; q < 4; ++q) sa[x][t][q] = 0.f;
 #pragma unroll
-    for (int j = 0; j < HDP / 64; ++j) {
+      for (int j = 0; j < HDP / 64; ++j)
 #pragma unroll
-      for (int s4 = 0; s4 < 4; ++s4) {
+        for (int s4 = 0; s4 < 4; ++s4)
 #pragma unroll
-        for (int p = 0; p < NP; ++p) {
-          const uint4 qa = *(const uint4*)(frag + ((p * KS + 4 * j + s4) * 32 + lane) * 4);
+          for (int t = 0; t < NT; ++t) {
+            const uint32_t w0 = word(kr[t].w[0][j], s4), w1 = word(kr[t].w[1][j], s4);
+            const uint4 ka = make_uint4(e4m3_lo(w0), e4m3_lo(w1), e4m3_hi(w0), e4m3_hi(w1));
 #pragma unroll
-          for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int hh = 0; hh < 2; ++hh) {
-              const uint4 kw = kr[t].w[hh][j];
-              const uint32_t w = s4 == 0 ? kw.x : (s4 == 1 ? kw.y : (s4 == 2 ? kw.z : kw.w));
-              mma_f16(sc[t][hh], qa, e4m3_lo(w), e4m3_hi(w));
+            for (int p = 0; p < NP; ++p) {
+              const uint32_t* at = frag + ((p * KS + 4 * j + s4) * 32 + lane) * 4;
+              mma_f16(sa[s4 % AC][t], ka, NP == 1 ? qb[4 * j + s4][0] : at[0], NP == 1 ? qb[4 * j + s4][1] : at[2]);
             }
+          }
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          float x = sa[0][t][q];
+#pragma unroll
+          for (int y = 1; y < AC; ++y) x += sa[y][t][q];
+          sc[t][q >> 1][q & 1][0] = x;
         }
-      }
+    } else {
+      float sa[NT][2][4];
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) sa[t][hh][q] = 0.f;
+#pragma unroll
+      for (int j = 0; j < HDP / 64; ++j)
+#pragma unroll
+        for (int s4 = 0; s4 < 4; ++s4)
+#pragma unroll
+          for (int p = 0; p < NP; ++p) {
+            const uint4 qa = *(const uint4*)(frag + ((p * KS + 4 * j + s4) * 32 + lane) * 4);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+              for (int hh = 0; hh < 2; ++hh) {
+                const uint32_t w = word(kr[t].w[hh][j], s4);
+                mma_f16(sa[t][hh], qa, e4m3_lo(w), e4m3_hi(w));
+              }
+          }
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) sc[t][hh][q >> 1][(q & 1) % QN] = sa[t][hh][q];
     }
+    // token of sc[t][hh][.][q], from the block's first on
+    auto place = [&](int hh, int q) { return RT == 8 ? 8 * hh + g : 8 * hh + 2 * c + q; };
     // scores in the log2 domain; hidden ones -inf
     const bool full = j0 + U <= full_hi && (j0 >= full_lo || j0 + U <= a.sinks);
 #pragma unroll
@@ -345,15 +414,12 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
 #pragma unroll
       for (int hh = 0; hh < 2; ++hh)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) sc[t][hh][q] *= rf[q >> 1] * kf[t];
-      if (!full) {
-        const int jb = j0 + 16 * t;
+        for (int rr = 0; rr < 2; ++rr)
 #pragma unroll
-        for (int hh = 0; hh < 2; ++hh)
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            if (!mk[q >> 1].sees(jb + 8 * hh + 2 * c + (q & 1))) sc[t][hh][q] = -INFINITY;
-      }
+          for (int q = 0; q < QN; ++q) {
+            sc[t][hh][rr][q] *= rf[rr] * kf[t];
+            if (!full && !mk[rr].sees(j0 + 16 * t + place(hh, q))) sc[t][hh][rr][q] = -INFINITY;
+          }
     }
     if (a.scores) {   // kept for the mass
 #pragma unroll
@@ -362,9 +428,11 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
         for (int hh = 0; hh < 2; ++hh)
 #pragma unroll
           for (int rr = 0; rr < 2; ++rr)
-            if (g + 8 * rr < rows)
-              *(float2*)(a.scores + (head * a.n * a.G + r0 + g + 8 * rr) * a.mass_pitch + j0 + 16 * t + 8 * hh + 2 * c) =
-                  make_float2(sc[t][hh][2 * rr], sc[t][hh][2 * rr + 1]);
+            if (row_of[rr] < rows) {
+              float* to = a.scores + (head * a.n * a.G + r0 + row_of[rr]) * a.mass_pitch + j0 + 16 * t + place(hh, 0);
+              if (RT == 8) *to = sc[t][hh][rr][0];
+              else *(float2*)to = make_float2(sc[t][hh][rr][0], sc[t][hh][rr][QN - 1]);
+            }
     }
     float mu[2], wu[2];   // the references, 0 while the row has seen nothing
     bool same = true;
@@ -374,12 +442,14 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
       float mx = -INFINITY, wx = -INFINITY;
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const float x = fmaxf(fmaxf(sc[t][0][2 * rr], sc[t][0][2 * rr + 1]), fmaxf(sc[t][1][2 * rr], sc[t][1][2 * rr + 1]));
+        float x = fmaxf(sc[t][0][rr][0], sc[t][1][rr][0]);
+        if (QN == 2) x = fmaxf(x, fmaxf(sc[t][0][rr][QN - 1], sc[t][1][rr][QN - 1]));
         mx = fmaxf(mx, x);
         wx = fmaxf(wx, x + (float)ve[t]);
       }
+      // over the lanes that hold the row's other tokens
 #pragma unroll
-      for (int o2 = 1; o2 <= 2; o2 <<= 1) {
+      for (int o2 = RT == 8 ? 4 : 1; o2 <= (RT == 8 ? 16 : 2); o2 <<= 1) {
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o2));
         wx = fmaxf(wx, __shfl_xor_sync(0xffffffffu, wx, o2));
       }
@@ -397,55 +467,75 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
       l[0] *= fl[0];
       l[1] *= fl[1];
 #pragma unroll
-      for (int t = 0; t < HDP / 8; ++t) {
+      for (int t = 0; t < OT; ++t) {
         o[t][0] *= fo[0];
-        o[t][1] *= fo[0];
-        o[t][2] *= fo[1];
+        o[t][1] *= fo[RT == 8 ? 1 : 0];
+        o[t][2] *= fo[RT == 8 ? 0 : 1];
         o[t][3] *= fo[1];
       }
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      uint4 pa[NP];
-      {
-        float p[2][4];
+      float p[2][2][QN];   // [hh][rr][q]
 #pragma unroll
-        for (int rr = 0; rr < 2; ++rr) {
-          const float vf = fmaxf((float)ve[t], wu[rr] - mu[rr] - kVeBelow);
-          const float nb = kPExp + vf - wu[rr];
-          float sum = 0.f;
+      for (int rr = 0; rr < 2; ++rr) {
+        const float vf = fmaxf((float)ve[t], wu[rr] - mu[rr] - kVeBelow);
+        const float nb = kPExp + vf - wu[rr];
+        float sum = 0.f;
 #pragma unroll
-          for (int hh = 0; hh < 2; ++hh)
+        for (int hh = 0; hh < 2; ++hh)
 #pragma unroll
-            for (int q = 2 * rr; q < 2 * rr + 2; ++q) {
-              p[hh][q] = NP == 2 ? exp2f(sc[t][hh][q] + nb) : fast_exp2(sc[t][hh][q] + nb);
-              sum += p[hh][q];
-            }
-          l[rr] = fmaf(sum, pow2f(wu[rr] - mu[rr] - vf), l[rr]);
-        }
-        pa[0] = make_uint4(pack_f16x2(p[0][0], p[0][1]), pack_f16x2(p[0][2], p[0][3]), pack_f16x2(p[1][0], p[1][1]),
-                           pack_f16x2(p[1][2], p[1][3]));
-        if (NP == 2)
-          pa[NP - 1] = make_uint4(pack_f16x2(p[0][0] - f16lo(pa[0].x), p[0][1] - f16hi(pa[0].x)),
-                                  pack_f16x2(p[0][2] - f16lo(pa[0].y), p[0][3] - f16hi(pa[0].y)),
-                                  pack_f16x2(p[1][0] - f16lo(pa[0].z), p[1][1] - f16hi(pa[0].z)),
-                                  pack_f16x2(p[1][2] - f16lo(pa[0].w), p[1][3] - f16hi(pa[0].w)));
+          for (int q = 0; q < QN; ++q) {
+            p[hh][rr][q] = NP == 2 ? exp2f(sc[t][hh][rr][q] + nb) : fast_exp2(sc[t][hh][rr][q] + nb);
+            sum += p[hh][rr][q];
+          }
+        l[rr] = fmaf(sum, pow2f(wu[rr] - mu[rr] - vf), l[rr]);
       }
       ValueUnit<HDP> vr;
       vr.load(unit + Un::bytes, 16 * t, g, c);
+      if constexpr (RT == 8) {
+        // P as the B operand (tokens 2 c, 2 c + 1, row g): the 8 x 8 tiles of scores transposed
+        uint32_t pb[NP][2];
 #pragma unroll
-      for (int wi = 0; wi < HDP / 32; ++wi) {
-        // bytes i of two tokens' words side by side
-        const uint32_t x0 = __byte_perm(vr.w[0][wi], vr.w[1][wi], 0x5140);
-        const uint32_t y0 = __byte_perm(vr.w[0][wi], vr.w[1][wi], 0x7362);
-        const uint32_t x1 = __byte_perm(vr.w[2][wi], vr.w[3][wi], 0x5140);
-        const uint32_t y1 = __byte_perm(vr.w[2][wi], vr.w[3][wi], 0x7362);
-        const uint32_t b0[4] = {e4m3_lo(x0), e4m3_hi(x0), e4m3_lo(y0), e4m3_hi(y0)};
-        const uint32_t b1[4] = {e4m3_lo(x1), e4m3_hi(x1), e4m3_lo(y1), e4m3_hi(y1)};
+        for (int hh = 0; hh < 2; ++hh) {
+          const uint32_t x = pack_f16x2(p[hh][0][0], p[hh][1][0]);
+          pb[0][hh] = transpose8x8(x);
+          if (NP == 2) pb[NP - 1][hh] = transpose8x8(pack_f16x2(p[hh][0][0] - f16lo(x), p[hh][1][0] - f16hi(x)));
+        }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int wi = 0; wi < HDP / 32; ++wi) {
+          // bytes i of two tokens' words side by side: dims g (even i) and g + 8 (odd i) of a tile
+          const uint32_t x0 = __byte_perm(vr.w[0][wi], vr.w[1][wi], 0x5140), x1 = __byte_perm(vr.w[2][wi], vr.w[3][wi], 0x5140);
+          const uint32_t y0 = __byte_perm(vr.w[0][wi], vr.w[1][wi], 0x7362), y1 = __byte_perm(vr.w[2][wi], vr.w[3][wi], 0x7362);
+          const uint4 xa = make_uint4(e4m3_lo(x0), e4m3_hi(x0), e4m3_lo(x1), e4m3_hi(x1));
+          const uint4 ya = make_uint4(e4m3_lo(y0), e4m3_hi(y0), e4m3_lo(y1), e4m3_hi(y1));
 #pragma unroll
-          for (int p = 0; p < NP; ++p) mma_f16(o[4 * wi + i], pa[p], b0[i], b1[i]);
+          for (int z = 0; z < NP; ++z) {
+            mma_f16(o[2 * wi], xa, pb[z][0], pb[z][1]);
+            mma_f16(o[2 * wi + 1], ya, pb[z][0], pb[z][1]);
+          }
+        }
+      } else {
+        uint4 pa[NP];
+        pa[0] = make_uint4(pack_f16x2(p[0][0][0], p[0][0][QN - 1]), pack_f16x2(p[0][1][0], p[0][1][QN - 1]),
+                           pack_f16x2(p[1][0][0], p[1][0][QN - 1]), pack_f16x2(p[1][1][0], p[1][1][QN - 1]));
+        if (NP == 2)
+          pa[NP - 1] = make_uint4(pack_f16x2(p[0][0][0] - f16lo(pa[0].x), p[0][0][QN - 1] - f16hi(pa[0].x)),
+                                  pack_f16x2(p[0][1][0] - f16lo(pa[0].y), p[0][1][QN - 1] - f16hi(pa[0].y)),
+                                  pack_f16x2(p[1][0][0] - f16lo(pa[0].z), p[1][0][QN - 1] - f16hi(pa[0].z)),
+                                  pack_f16x2(p[1][1][0] - f16lo(pa[0].w), p[1][1][QN - 1] - f16hi(pa[0].w)));
+#pragma unroll
+        for (int wi = 0; wi < HDP / 32; ++wi) {
+          // bytes i of two tokens' words side by side
+          const uint32_t x0 = __byte_perm(vr.w[0][wi], vr.w[1][wi], 0x5140), y0 = __byte_perm(vr.w[0][wi], vr.w[1][wi], 0x7362);
+          const uint32_t x1 = __byte_perm(vr.w[2][wi], vr.w[3][wi], 0x5140), y1 = __byte_perm(vr.w[2][wi], vr.w[3][wi], 0x7362);
+          const uint32_t b0[4] = {e4m3_lo(x0), e4m3_hi(x0), e4m3_lo(y0), e4m3_hi(y0)};
+          const uint32_t b1[4] = {e4m3_lo(x1), e4m3_hi(x1), e4m3_lo(y1), e4m3_hi(y1)};
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int z = 0; z < NP; ++z) mma_f16(o[4 * wi + i], pa[z], b0[i], b1[i]);
+        }
       }
     }
     // every lane has read the unit: the slot takes the one D turns on
@@ -462,11 +552,12 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
   }
   __syncthreads();   // the rings are read: the outputs go over them
 
+  constexpr int QN2 = RT == 8 ? 1 : 2;
   // ---- join the warps: outputs normalised by their own sums, then weighted
 #pragma unroll
   for (int rr = 0; rr < 2; ++rr) {
-    l[rr] += __shfl_xor_sync(0xffffffffu, l[rr], 1);
-    l[rr] += __shfl_xor_sync(0xffffffffu, l[rr], 2);
+#pragma unroll
+    for (int o2 = RT == 8 ? 4 : 1; o2 <= (RT == 8 ? 16 : 2); o2 <<= 1) l[rr] += __shfl_xor_sync(0xffffffffu, l[rr], o2);
     // (units that every query sees are not masked: a row without a query stops here)
     const bool real = mk[rr].hi > 0;
     if (!real) {
@@ -476,25 +567,30 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
     const bool has = !(l[rr] <= 0.f);   // (a sum that is not a number stays one)
     const float f = has ? 1.f / l[rr] : 0.f;
     const float e2 = real ? pow2f(W[rr] - m[rr]) : 0.f;
-    const int row = g + 8 * rr;
-    if (c == 0) warp_ml[warp][row] = make_float2(m[rr], l[rr]);
-    float* dst = joint + warp * 16 * Shape::JS;
+    const int row = row_of[rr];
+    if (RT == 8 ? g == 0 : c == 0) warp_ml[warp][row] = make_float2(m[rr], l[rr]);
+    float* dst = joint + warp * RT * Shape::JS;
     if (row < rows) {
 #pragma unroll
       for (int wi = 0; wi < HDP / 32; ++wi)
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
+        for (int q = 0; q < QN2; ++q) {
           float4 x;   // four dims side by side
-          x.x = real ? o[4 * wi][2 * rr + q] * f * e2 : 0.f;
-          x.y = real ? o[4 * wi + 1][2 * rr + q] * f * e2 : 0.f;
-          x.z = real ? o[4 * wi + 2][2 * rr + q] * f * e2 : 0.f;
-          x.w = real ? o[4 * wi + 3][2 * rr + q] * f * e2 : 0.f;
-          *(float4*)(dst + Shape::pos(row, ValueUnit<HDP>::dim(wi, 0, 2 * c + q))) = x;
+          if (RT == 8)
+            x = make_float4(o[2 * wi % OT][rr], o[2 * wi % OT][2 + rr], o[(2 * wi + 1) % OT][rr], o[(2 * wi + 1) % OT][2 + rr]);
+          else
+            x = make_float4(o[4 * wi % OT][2 * rr + q], o[(4 * wi + 1) % OT][2 * rr + q], o[(4 * wi + 2) % OT][2 * rr + q],
+                            o[(4 * wi + 3) % OT][2 * rr + q]);
+          x.x = real ? x.x * f * e2 : 0.f;
+          x.y = real ? x.y * f * e2 : 0.f;
+          x.z = real ? x.z * f * e2 : 0.f;
+          x.w = real ? x.w * f * e2 : 0.f;
+          *(float4*)(dst + Shape::pos(row, ValueUnit<HDP>::dim(wi, 0, RT == 8 ? g : 2 * c + q))) = x;
         }
     }
   }
   __syncthreads();
-  if (threadIdx.x < 16) {   // the warps' weights, in place of (m, l)
+  if (threadIdx.x < RT) {   // the warps' weights, in place of (m, l)
     const int row = threadIdx.x;
     float M = -INFINITY, S = 0.f;
 #pragma unroll
@@ -518,7 +614,7 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
 #pragma unroll
     for (int w = 0; w < RW; ++w) {
       const float wt = warp_ml[w][row].x;
-      acc += wt != 0.f ? wt * joint[w * 16 * Shape::JS + Shape::pos(row, d)] : 0.f;
+      acc += wt != 0.f ? wt * joint[w * RT * Shape::JS + Shape::pos(row, d)] : 0.f;
     }
     return acc;
   };
@@ -761,7 +857,8 @@ constexpr int frag_bytes() { return NP * (HDP / 16) * 512; }
 template <int HDP, int NP, typename T>
 cudaError_t launch_rows(CacheAttnArgs a, cudaStream_t st) {
   constexpr int U = Unit<HDP>::U;
-  a.row_tiles = (a.n * a.G + 15) / 16;
+  const int RT = a.n * a.G <= 8 ? 8 : 16;   // rows of a tile
+  a.row_tiles = (a.n * a.G + RT - 1) / RT;
   const long long tiles = (long long)a.row_tiles * a.c.Hkv * a.batch;
   // tokens that a row tile sees at most, in units
   long long seen = a.max_length;
@@ -787,8 +884,11 @@ cudaError_t launch_rows(CacheAttnArgs a, cudaStream_t st) {
     e = launch_cache_attend_tc(a, st);
   } else {
     const RowsMaps maps{a.maps->k_rows, a.maps->v_rows};
-    e = launch_kernel_cluster(cache_rows_kernel<HDP, NP, T>, dim3(a.row_tiles * a.splits, a.c.Hkv, a.batch), dim3(RW * 32),
-                              RowsShape<HDP, NP>::bytes, st, dim3(a.splits <= 8 ? a.splits : 1, 1, 1), maps, a);
+    const dim3 grid(a.row_tiles * a.splits, a.c.Hkv, a.batch), cluster(a.splits <= 8 ? a.splits : 1, 1, 1);
+    e = RT == 8 ? launch_kernel_cluster(cache_rows_kernel<HDP, NP, 8, T>, grid, dim3(RW * 32), RowsShape<HDP, NP, 8>::bytes,
+                                        st, cluster, maps, a)
+                : launch_kernel_cluster(cache_rows_kernel<HDP, NP, 16, T>, grid, dim3(RW * 32), RowsShape<HDP, NP, 16>::bytes,
+                                        st, cluster, maps, a);
   }
   if (e != cudaSuccess || !a.mass || a.max_length == 0) return e;
   if (NP == 1 && a.n * a.G > 16) return launch_cache_mass_tc(a, st);
@@ -805,13 +905,19 @@ cudaError_t launch_hd(const CacheAttnArgs& a, Dtype dt, cudaStream_t st) {
   return dt == DT_BF16 ? launch_rows<HDP, 1, bf16>(a, st) : launch_rows<HDP, 2, float>(a, st);
 }
 
+template <int HDP, int NP, int RT, typename T>
+cudaError_t init_rows() {
+  return cudaFuncSetAttribute(cache_rows_kernel<HDP, NP, RT, T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              RowsShape<HDP, NP, RT>::bytes);
+}
+
 template <int HDP>
 cudaError_t init_hd() {
-  cudaError_t e = cudaFuncSetAttribute(cache_rows_kernel<HDP, 1, bf16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       RowsShape<HDP, 1>::bytes);
-  if (e != cudaSuccess) return e;
-  return cudaFuncSetAttribute(cache_rows_kernel<HDP, 2, float>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              RowsShape<HDP, 2>::bytes);
+  cudaError_t e = init_rows<HDP, 1, 8, bf16>();
+  if (e == cudaSuccess) e = init_rows<HDP, 1, 16, bf16>();
+  if (e == cudaSuccess) e = init_rows<HDP, 2, 8, float>();
+  if (e == cudaSuccess) e = init_rows<HDP, 2, 16, float>();
+  return e;
 }
 
 }  // namespace
