@@ -690,20 +690,23 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
   __syncthreads();
   if (!last) return;
   __threadfence();
-  float* wts = joint;   // [splits][16]
-  if (threadIdx.x < 16 && (int)threadIdx.x < rows) {
+  // the splits' (max, sum), all on their way together, then their weights in their place
+  float2* wts = (float2*)joint;   // [splits][16]
+  for (int w = threadIdx.x; w < a.splits * 16; w += RW * 32)
+    if (w % 16 < rows) wts[w] = __ldcg(a.part_ml + unit * a.splits * 16 + w);
+  __syncthreads();
+  if ((int)threadIdx.x < rows) {
     const int row = threadIdx.x;
-    const float2* ml = a.part_ml + unit * a.splits * 16 + row;
     float M = -INFINITY, S = 0.f;
-    for (int q = 0; q < a.splits; ++q) M = fmaxf(M, __ldcg(ml + q * 16).x);
+    for (int q = 0; q < a.splits; ++q) M = fmaxf(M, wts[q * 16 + row].x);
     for (int q = 0; q < a.splits; ++q) {
-      const float2 x = __ldcg(ml + q * 16);
+      const float2 x = wts[q * 16 + row];
       const float wt = x.y != x.y ? x.y : (x.x == -INFINITY ? 0.f : exp2f(x.x - M) * x.y);
-      wts[q * 16 + row] = wt;
+      wts[q * 16 + row].x = wt;
       S += wt;
     }
     const float inv = !(S <= 0.f) ? 1.f / S : 0.f;
-    for (int q = 0; q < a.splits; ++q) wts[q * 16 + row] *= inv;
+    for (int q = 0; q < a.splits; ++q) wts[q * 16 + row].x *= inv;
     if (a.mass) a.row_ml[head * a.n * a.G + r0 + row] = row_weight(M, S, kPExp);
   }
   __syncthreads();
@@ -715,7 +718,7 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
 #pragma unroll 8
     for (int q = 0; q < a.splits; ++q) {
       const float4 x = __ldcg((const float4*)(p0 + ((size_t)q * 16 + row) * HDP + d));
-      const float wt = wts[q * 16 + row];   // (0 times an empty split's zeros)
+      const float wt = wts[q * 16 + row].x;   // (0 times an empty split's zeros)
       acc.x += wt * x.x;
       acc.y += wt * x.y;
       acc.z += wt * x.z;
@@ -868,7 +871,7 @@ cudaError_t launch_rows(CacheAttnArgs a, cudaStream_t st) {
   if (tiles < 2 * a.num_sms) {
     // two CTAs per SM, each warp with a unit at least
     // (and no more splits than the joining CTA has weights for in shared memory)
-    const long long most = min(min((long long)kCacheSplitCtas, 2ll * a.num_sms) / tiles, (long long)RW * HDP);
+    const long long most = min(min((long long)kCacheSplitCtas, 2ll * a.num_sms) / tiles, (long long)RW * HDP / 2);
     a.splits = (int)max(1ll, min(most, (long long)(units + RW - 1) / RW));
     // up to 8 splits join in distributed shared memory, more through L2, which takes longer
     // than two units more for each warp
