@@ -58,9 +58,10 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
 // word (piece, k-step, lane) holds rows lane / 4 and + 8, dims 64 j + 16 (lane % 4)
 // + 4 s + 0 .. 3 of k-step 4 j + s.  Rows that do not exist are zeros.  fac[r]:
 // 2^exponent taken out of the row, times the softmax scale.
-template <int HDP, int NP, typename T, int THREADS>
+// after_loads is called with the loads on their way.
+template <int HDP, int NP, typename T, int THREADS, typename F>
 __device__ __forceinline__ void stage_q(const CacheAttnArgs& a, const Sight& s, int b, int h, int r0, uint32_t* frag,
-                                        float* fac) {
+                                        float* fac, F after_loads) {
   constexpr int TPR = HDP / 16, ITEMS = (16 * TPR + THREADS - 1) / THREADS;   // threads per row, rows' pieces per thread
   float x[ITEMS][16];
 #pragma unroll
@@ -76,6 +77,7 @@ __device__ __forceinline__ void stage_q(const CacheAttnArgs& a, const Sight& s, 
       for (int q = 0; q < 16; ++q) x[z][q] = 0.f;
     }
   }
+  after_loads();
 #pragma unroll
   for (int z = 0; z < ITEMS; ++z) {
     const int w = threadIdx.x + z * THREADS;
@@ -268,12 +270,16 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
     for (int x = 0; x < D; ++x) mbar_init(&arrived[warp][x], 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    for (int x = 0; x < D; ++x)
-      if (u0 + warp + RW * x < u1) fetch(u0 + warp + RW * x, x);
   }
   if (threadIdx.x < 16) fac[threadIdx.x] = 0.f;
   __syncthreads();
-  stage_q<HDP, NP, T, RW * 32>(a, s, b, h, r0, frag, fac);
+  // (Q's loads first: behind the first units of all CTAs, 29 MB, they took 5 us)
+  stage_q<HDP, NP, T, RW * 32>(a, s, b, h, r0, frag, fac, [&]() {
+    if (lane == 0)
+      for (int x = 0; x < D; ++x)
+        if (u0 + warp + RW * x < u1) fetch(u0 + warp + RW * x, x);
+    __syncwarp();
+  });
   // this lane's two rows: scores of rows g, g + 8 by tokens 2 c, 2 c + 1, or (RT = 8) of tokens
   // g, g + 8 by rows 2 c, 2 c + 1
   const int row_of[2] = {RT == 8 ? 2 * c : g, RT == 8 ? 2 * c + 1 : g + 8};
@@ -609,19 +615,30 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
     split_w[row] = make_float2(M, S);
   }
   __syncthreads();
-  auto joined = [&](int row, int d) {
-    float acc = 0.f;
+  auto joined = [&](int row, int d) {   // four dims from d on
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int w = 0; w < RW; ++w) {
       const float wt = warp_ml[w][row].x;
-      acc += wt != 0.f ? wt * joint[w * RT * Shape::JS + Shape::pos(row, d)] : 0.f;
+      const float4 x = *(const float4*)(joint + w * RT * Shape::JS + Shape::pos(row, d));
+      acc.x += wt != 0.f ? wt * x.x : 0.f;
+      acc.y += wt != 0.f ? wt * x.y : 0.f;
+      acc.z += wt != 0.f ? wt * x.z : 0.f;
+      acc.w += wt != 0.f ? wt * x.w : 0.f;
     }
     return acc;
   };
+  auto store4 = [&](int row, int d, const float4& x) {   // (hd is a multiple of 8)
+    T* dst = out_row(r0 + row) + d;
+    dst[0] = from_f32<T>(x.x);
+    dst[1] = from_f32<T>(x.y);
+    dst[2] = from_f32<T>(x.z);
+    dst[3] = from_f32<T>(x.w);
+  };
   if (a.splits == 1) {
-    for (int w = threadIdx.x; w < rows * L.hd; w += RW * 32) {
-      const int row = w / L.hd, d = w % L.hd;
-      out_row(r0 + row)[d] = from_f32<T>(joined(row, d));
+    for (int w = threadIdx.x; w < rows * (HDP / 4); w += RW * 32) {
+      const int row = w / (HDP / 4), d = w % (HDP / 4) * 4;
+      if (d < L.hd) store4(row, d, joined(row, d));
     }
     if (a.mass && threadIdx.x < rows) {
       const float2 x = split_w[threadIdx.x];
@@ -631,7 +648,7 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
   }
   if (a.splits <= 8) {
     // the splits are a cluster: each CTA joins a share of the rows' columns from all of them
-    for (int w = threadIdx.x; w < rows * HDP; w += RW * 32) mine[w] = joined(w / HDP, w % HDP);
+    for (int w = threadIdx.x; w < rows * (HDP / 4); w += RW * 32) ((float4*)mine)[w] = joined(w / (HDP / 4), w % (HDP / 4) * 4);
     cluster_sync();
     if ((int)threadIdx.x < rows) {
       const uint32_t at = smem_u32(&split_w[threadIdx.x]);
@@ -670,18 +687,14 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
         acc.z += wt * x.z;
         acc.w += wt * x.w;
       }
-      T* dst = out_row(r0 + row) + d;   // hd is a multiple of 8
-      dst[0] = from_f32<T>(acc.x);
-      dst[1] = from_f32<T>(acc.y);
-      dst[2] = from_f32<T>(acc.z);
-      dst[3] = from_f32<T>(acc.w);
+      store4(row, d, acc);
     }
     cluster_sync();   // nobody leaves while its rows are read
     return;
   }
   const size_t unit = head * a.row_tiles + tile;
   float* part = a.part + (unit * a.splits + split) * 16 * HDP;
-  for (int w = threadIdx.x; w < rows * HDP; w += RW * 32) __stcg(part + w, joined(w / HDP, w % HDP));
+  for (int w = threadIdx.x; w < rows * (HDP / 4); w += RW * 32) __stcg((float4*)part + w, joined(w / (HDP / 4), w % (HDP / 4) * 4));
   if (threadIdx.x < rows) __stcg(a.part_ml + (unit * a.splits + split) * 16 + threadIdx.x, split_w[threadIdx.x]);
   // the last split to arrive joins them all, in their order
   __threadfence();
@@ -724,11 +737,7 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
       acc.z += wt * x.z;
       acc.w += wt * x.w;
     }
-    T* dst = out_row(r0 + row) + d;   // hd is a multiple of 8
-    dst[0] = from_f32<T>(acc.x);
-    dst[1] = from_f32<T>(acc.y);
-    dst[2] = from_f32<T>(acc.z);
-    dst[3] = from_f32<T>(acc.w);
+    store4(row, d, acc);
   }
 }
 
@@ -780,7 +789,7 @@ __global__ void __launch_bounds__(RW * 32) cache_mass_kernel(CacheAttnArgs a) {
       __syncthreads();
       if (threadIdx.x < 16) fac[threadIdx.x] = 0.f;
       __syncthreads();
-      stage_q<HDP, NP, T, RW * 32>(a, s, b, h, r0, frag, fac);
+      stage_q<HDP, NP, T, RW * 32>(a, s, b, h, r0, frag, fac, []() {});
       float sc[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
       for (int p = 0; p < NP; ++p)
