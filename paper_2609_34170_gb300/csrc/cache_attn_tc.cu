@@ -293,12 +293,13 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
         for (int y = 0; y < 8; ++y) x[y] = lds_u4(cv0 + (uint32_t)cs * CB + 16u * lane + 512u * y);
         ok = wait_phase(&v_empty[slot], ((uint32_t)(part / VS) & 1u) ^ 1u);
         if (!ok) break;
-        __syncwarp();   // every lane has its codes
-        if (lane == 0) mbar_arrive(&cv_empty[cs]);
         const uint32_t to = v0 + (uint32_t)slot * VH + (uint32_t)(u % NB) * VB;
 #pragma unroll
         for (int y = 0; y < 8; ++y) widen(x[y], to + lo + 1024u * y, to + hi + 1024u * y);
         written(&v_full[slot]);
+        // the codes' slot is free only here, with their use: an arrival right behind the loads is
+        // seen before the loads are done when copies fill shared memory (the next item's Q)
+        if (lane == 0) mbar_arrive(&cv_empty[cs]);
       }
     }
     if (!ok && lane == 0) *abort_flag = 1;
@@ -612,15 +613,15 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
 #pragma unroll
           for (int q = 0; q < 16; ++q)
             wd[q] = real ? pack_bf16x2(__uint_as_float(raw[2 * q]) * inv, __uint_as_float(raw[2 * q + 1]) * inv) : 0u;
-          if (r >= rows) continue;
+          const int ends = r < rows ? L.hd : 0;
           if (wider) {   // (half the requests of 16-byte stores, each to 32 rows)
 #pragma unroll
             for (int q = 0; q < 2; ++q)
-              if (cb + 16 * q < L.hd) stg_u8(dst + cb + 16 * q, wd + 8 * q);
+              if (cb + 16 * q < ends) stg_u8(dst + cb + 16 * q, wd + 8 * q);
           } else {
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-              if (cb + 8 * q < L.hd) store_bf16x8(dst + cb + 8 * q, make_uint4(wd[4 * q], wd[4 * q + 1], wd[4 * q + 2], wd[4 * q + 3]), wide);
+              if (cb + 8 * q < ends) store_bf16x8(dst + cb + 8 * q, make_uint4(wd[4 * q], wd[4 * q + 1], wd[4 * q + 2], wd[4 * q + 3]), wide);
           }
         }
         continue;

@@ -283,6 +283,18 @@ def test_mass_adds_up_and_repeats_bit_for_bit():
         assert torch.equal(p.cache.attend(0, q, L, mass=m3), o1) and torch.equal(m3, m1)
 
 
+@pytest.mark.parametrize("layout,n,batch", [((8, 1, 256), 300, 16), ((8, 2, 128), 300, 10), ((8, 1, 64), 300, 16), ((8, 1, 192), 300, 16)])
+def test_prompts_of_many_robots_repeat_bit_for_bit(layout, n, batch):
+    # more row tiles than SMs: their second ones start while the first ones' output is written
+    p = Pair(layout, "bf16", n + 12, batch, queries=n, lengths=[n + 3 * (b % 5) for b in range(batch)], seed=21)
+    q = _rand((batch, n, layout[0], layout[2]), 22, "bf16", 2.0)
+    first, _ = check(p, n, q=q)
+    first = first.clone()
+    for _ in range(40):
+        out = p.cache.attend(0, q, _ints(p.lengths))
+        assert torch.equal(out, first)
+
+
 def test_other_streams_scales_and_bounds():
     p = Pair((16, 4, 64), "bf16", 300, 2, queries=2, lengths=[300, 200])
     q = _rand((2, 2, 16, 64), 5, "bf16")
