@@ -45,6 +45,13 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint4& a, uint32_t 
       : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
 }
 
+// fp32's sums over MMAs: the tensor core cuts its sums off rather than rounding them, and
+// over a long chain that adds up, so that each pair of pieces starts from zero.
+__device__ __forceinline__ void add4(float (&d)[4], const float (&x)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) d[i] += x[i];
+}
+
 __device__ __forceinline__ uint32_t word(const uint4& x, int i) { return i == 0 ? x.x : (i == 1 ? x.y : (i == 2 ? x.z : x.w)); }
 
 // An 8 x 8 tile of 16-bit values, a row per four lanes, transposed across the warp.
@@ -366,10 +373,16 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
           for (int t = 0; t < NT; ++t) {
             const uint32_t w0 = word(kr[t].w[0][j], s4), w1 = word(kr[t].w[1][j], s4);
             const uint4 ka = make_uint4(e4m3_lo(w0), e4m3_lo(w1), e4m3_hi(w0), e4m3_hi(w1));
+            if constexpr (NP == 1) {
+              mma_f16(sa[s4 % AC][t], ka, qb[4 * j + s4][0], qb[4 * j + s4][1]);
+            } else {
+              float x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int p = 0; p < NP; ++p) {
-              const uint32_t* at = frag + ((p * KS + 4 * j + s4) * 32 + lane) * 4;
-              mma_f16(sa[s4 % AC][t], ka, NP == 1 ? qb[4 * j + s4][0] : at[0], NP == 1 ? qb[4 * j + s4][1] : at[2]);
+              for (int p = NP - 1; p >= 0; --p) {
+                const uint32_t* at = frag + ((p * KS + 4 * j + s4) * 32 + lane) * 4;
+                mma_f16(x, ka, at[0], at[2]);
+              }
+              add4(sa[s4 % AC][t], x);
             }
           }
 #pragma unroll
@@ -392,18 +405,25 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
 #pragma unroll
       for (int j = 0; j < HDP / 64; ++j)
 #pragma unroll
-        for (int s4 = 0; s4 < 4; ++s4)
+        for (int s4 = 0; s4 < 4; ++s4) {
+          uint4 qa[NP];
 #pragma unroll
-          for (int p = 0; p < NP; ++p) {
-            const uint4 qa = *(const uint4*)(frag + ((p * KS + 4 * j + s4) * 32 + lane) * 4);
+          for (int p = 0; p < NP; ++p) qa[p] = *(const uint4*)(frag + ((p * KS + 4 * j + s4) * 32 + lane) * 4);
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+          for (int t = 0; t < NT; ++t)
 #pragma unroll
-              for (int hh = 0; hh < 2; ++hh) {
-                const uint32_t w = word(kr[t].w[hh][j], s4);
-                mma_f16(sa[t][hh], qa, e4m3_lo(w), e4m3_hi(w));
+            for (int hh = 0; hh < 2; ++hh) {
+              const uint32_t w = word(kr[t].w[hh][j], s4), k0 = e4m3_lo(w), k1 = e4m3_hi(w);
+              if constexpr (NP == 1) {
+                mma_f16(sa[t][hh], qa[0], k0, k1);
+              } else {
+                float x[4] = {0.f, 0.f, 0.f, 0.f};
+                mma_f16(x, qa[NP - 1], k0, k1);
+                mma_f16(x, qa[0], k0, k1);
+                add4(sa[t][hh], x);
               }
-          }
+            }
+        }
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -515,10 +535,18 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
           const uint32_t y0 = __byte_perm(vr.w[0][wi], vr.w[1][wi], 0x7362), y1 = __byte_perm(vr.w[2][wi], vr.w[3][wi], 0x7362);
           const uint4 xa = make_uint4(e4m3_lo(x0), e4m3_hi(x0), e4m3_lo(x1), e4m3_hi(x1));
           const uint4 ya = make_uint4(e4m3_lo(y0), e4m3_hi(y0), e4m3_lo(y1), e4m3_hi(y1));
+          if constexpr (NP == 1) {
+            mma_f16(o[2 * wi], xa, pb[0][0], pb[0][1]);
+            mma_f16(o[2 * wi + 1], ya, pb[0][0], pb[0][1]);
+          } else {
+            float x[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int z = 0; z < NP; ++z) {
-            mma_f16(o[2 * wi], xa, pb[z][0], pb[z][1]);
-            mma_f16(o[2 * wi + 1], ya, pb[z][0], pb[z][1]);
+            for (int z = NP - 1; z >= 0; --z) {
+              mma_f16(x, xa, pb[z][0], pb[z][1]);
+              mma_f16(y, ya, pb[z][0], pb[z][1]);
+            }
+            add4(o[2 * wi], x);
+            add4(o[2 * wi + 1], y);
           }
         }
       } else {
@@ -538,9 +566,16 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
           const uint32_t b0[4] = {e4m3_lo(x0), e4m3_hi(x0), e4m3_lo(y0), e4m3_hi(y0)};
           const uint32_t b1[4] = {e4m3_lo(x1), e4m3_hi(x1), e4m3_lo(y1), e4m3_hi(y1)};
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int z = 0; z < NP; ++z) mma_f16(o[4 * wi + i], pa[z], b0[i], b1[i]);
+          for (int i = 0; i < 4; ++i) {
+            if constexpr (NP == 1) {
+              mma_f16(o[4 * wi + i], pa[0], b0[i], b1[i]);
+            } else {
+              float x[4] = {0.f, 0.f, 0.f, 0.f};
+              mma_f16(x, pa[NP - 1], b0[i], b1[i]);
+              mma_f16(x, pa[0], b0[i], b1[i]);
+              add4(o[4 * wi + i], x);
+            }
+          }
         }
       }
     }
@@ -792,13 +827,22 @@ __global__ void __launch_bounds__(RW * 32) cache_mass_kernel(CacheAttnArgs a) {
       stage_q<HDP, NP, T, RW * 32>(a, s, b, h, r0, frag, fac, []() {});
       float sc[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-      for (int p = 0; p < NP; ++p)
+      for (int ks = 0; ks < KS; ++ks) {
+        uint4 qa[NP];
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          const uint4 qa = *(const uint4*)(frag + ((p * KS + ks) * 32 + lane) * 4);
+        for (int p = 0; p < NP; ++p) qa[p] = *(const uint4*)(frag + ((p * KS + ks) * 32 + lane) * 4);
 #pragma unroll
-          for (int hh = 0; hh < 2; ++hh) mma_f16(sc[hh], qa, kb[hh][ks][0], kb[hh][ks][1]);
+        for (int hh = 0; hh < 2; ++hh) {
+          if constexpr (NP == 1) {
+            mma_f16(sc[hh], qa[0], kb[hh][ks][0], kb[hh][ks][1]);
+          } else {
+            float x[4] = {0.f, 0.f, 0.f, 0.f};
+            mma_f16(x, qa[NP - 1], kb[hh][ks][0], kb[hh][ks][1]);
+            mma_f16(x, qa[0], kb[hh][ks][0], kb[hh][ks][1]);
+            add4(sc[hh], x);
+          }
         }
+      }
 #pragma unroll
       for (int rr = 0; rr < 2; ++rr) {
         const int r = r0 + g + 8 * rr;

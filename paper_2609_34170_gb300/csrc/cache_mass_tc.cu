@@ -26,7 +26,7 @@ constexpr int MT = 640;
 template <int NB> struct MassShape {
   static constexpr int KS = 8;                              // K units in flight
   static constexpr uint32_t q_bytes = 2 * NB * QB;          // a tile of rows in two pieces
-  static constexpr uint32_t bytes = 2 * q_bytes + KS * KU + 4096 + 512;
+  static constexpr uint32_t bytes = 2 * q_bytes + KS * KU + 4096 + 2048 + 512;
   static_assert(bytes <= 227 * 1024, "shared memory");
 };
 
@@ -41,10 +41,12 @@ __global__ void __launch_bounds__(MT, 1) cache_mass_tc_kernel(const __grid_const
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t q0 = smem_u32(smem), k0 = q0 + 2 * Shape::q_bytes;
   uint8_t* tail = smem + 2 * Shape::q_bytes + KS * KU;
-  // per row (factor, log2 y - x), [4][128] by row tile: Q is laid out up to two tiles ahead of
-  // the exponentials, which may be two tiles of scores behind the MMAs
+  // per row (factor, -x) and y, [4][128] by row tile: Q is laid out up to two tiles ahead of the
+  // exponentials, which may be two tiles of scores behind the MMAs.  (x is integral: the
+  // exponent s - x is rounded once, where log2 y - x would bring a row's own rounding into it.)
   float2* rowc = (float2*)tail;
-  uint64_t* k_full = (uint64_t*)(tail + 4096);
+  float* rowy = (float*)(tail + 4096);
+  uint64_t* k_full = (uint64_t*)(tail + 4096 + 2048);
   uint64_t* k_empty = k_full + KS;
   uint64_t* q_full = k_empty + KS;   // [2]
   uint64_t* q_empty = q_full + 2;    // [2]
@@ -117,7 +119,8 @@ __global__ void __launch_bounds__(MT, 1) cache_mass_tc_kernel(const __grid_const
         stage_q8<NB>(a, s, b, h, rt * BM, rb, q0 + (uint32_t)(m & 1) * Shape::q_bytes, nullptr, [&](int lr, int e) {
           const float2 x = rt * BM + lr < end_row ? ml[lr] : make_float2(0.f, 0.f);
           // (factors as in the attention: not 0, which times an infinite score would not be a number)
-          rowc[(m & 3) * BM + lr] = make_float2(q_factor(e, a.scale_log2), log2f(x.y) - x.x);
+          rowc[(m & 3) * BM + lr] = make_float2(q_factor(e, a.scale_log2), -x.x);
+          rowy[(m & 3) * BM + lr] = x.y;
         });
       written(&q_full[m & 1]);
     }
@@ -196,7 +199,7 @@ __global__ void __launch_bounds__(MT, 1) cache_mass_tc_kernel(const __grid_const
     for (int rt = rt0; rt < rt1; ++rt) {
       const Sight sg = sight_of(rt);
       const int m = rt - rt0, first = rt * BM + 64 * hf;
-      const uint32_t rc = smem_u32(rowc + (m & 3) * BM + 64 * hf);
+      const uint32_t rc = smem_u32(rowc + (m & 3) * BM + 64 * hf), ry = smem_u32(rowy + (m & 3) * BM + 64 * hf);
       for (int i = 0; i < sg.units; ++i, ++g) {
         const int j0 = token(sg, i), j = j0 + t;
         const float old = own[j0], kf = exp2i(KE[j / 16]);
@@ -221,12 +224,14 @@ __global__ void __launch_bounds__(MT, 1) cache_mass_tc_kernel(const __grid_const
           // (a hidden row's weight may not be a number: it is left out after the exponent)
           auto add = [&](auto hidden) {
 #pragma unroll
-            for (int k = 0; k < 32; k += 2) {
-              float4 x;
-              asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(rc + 256u * c + 8u * k));
-              const float e0 = fmaf(__uint_as_float(raw[k]) * kf, x.x, x.y), e1 = fmaf(__uint_as_float(raw[k + 1]) * kf, x.z, x.w);
-              sum[k & 3] += fast_exp2(hidden(k) ? -INFINITY : e0);
-              sum[(k & 3) + 1] += fast_exp2(hidden(k + 1) ? -INFINITY : e1);
+            for (int k = 0; k < 32; k += 4) {
+              const float4 y = lds_f4(ry + 128u * c + 4u * k), x0 = lds_f4(rc + 256u * c + 8u * k), x1 = lds_f4(rc + 256u * c + 8u * k + 16u);
+              const float ys[4] = {y.x, y.y, y.z, y.w}, fs[4] = {x0.x, x0.z, x1.x, x1.z}, cs[4] = {x0.y, x0.w, x1.y, x1.w};
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                const float e = fmaf(__uint_as_float(raw[k + q]) * kf, fs[q], cs[q]);
+                sum[q] = fmaf(fast_exp2(hidden(k + q) ? -INFINITY : e), hidden(k + q) ? 0.f : ys[q], sum[q]);
+              }
             }
           };
           if (full) {
