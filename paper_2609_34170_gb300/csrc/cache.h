@@ -62,6 +62,23 @@ struct CacheMaps {
 };
 cudaError_t encode_layer(CacheMaps* m, const CacheLayer& c, int batch);
 
+// Division by a number that stays the same over a launch, of n < 2^31: with 2^shift >= d and
+// mul = 2^(31 + shift) / d rounded up, whose excess times n stays below 2^(31 + shift), the
+// quotient is n * mul / 2^(31 + shift).  (An item of the prompts' kernel takes ten of them: as
+// divisions, one of 64 bits among them, 2000 cycles.)
+struct LaunchDiv {
+  uint32_t d, mul;
+  int shift;
+  LaunchDiv() : LaunchDiv(1) {}
+  explicit LaunchDiv(int by) : d((uint32_t)by), shift(0) {
+    while ((1ull << shift) < d) ++shift;
+    mul = (uint32_t)(((1ull << (31 + shift)) + d - 1) / d);
+  }
+#ifdef __CUDACC__
+  __device__ __forceinline__ uint32_t of(uint32_t n) const { return (uint32_t)((uint64_t)n * mul >> (31 + shift)); }
+#endif
+};
+
 struct CacheAttnArgs {
   CacheLayer c;
   const CacheMaps* maps;
@@ -70,6 +87,7 @@ struct CacheAttnArgs {
   long long q_robot, q_token, out_robot, out_token;
   const int *lengths, *counts;
   int batch, n, G, max_length;
+  LaunchDiv by_G, by_heads;   // by G, by the KV heads
   int causal, window, sinks;
   float scale_log2;         // softmax scale * log2(e)
   float* mass;
@@ -89,6 +107,7 @@ struct CacheAttnArgs {
   int* err;
   // chosen by the launcher
   int row_tiles, splits;
+  LaunchDiv by_splits, by_group, by_last, by_pairs;   // tensor cores: of items, see there
   long long mass_pitch;     // tokens of a chunk's sums, or of a row's scores
   float* scores;            // few rows: scores kept for the mass, or null
   int group;                // tensor cores: (robot, KV head) pairs walked together

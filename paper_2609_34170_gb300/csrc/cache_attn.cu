@@ -74,10 +74,10 @@ __device__ __forceinline__ void stage_q(const CacheAttnArgs& a, const Sight& s, 
 #pragma unroll
   for (int z = 0; z < ITEMS; ++z) {
     const int w = threadIdx.x + z * THREADS, lr = w / TPR, d = (w % TPR) * 16, r = r0 + lr;
-    const int i = r / a.G;
+    const int i = (int)a.by_G.of((uint32_t)r);
     if (w < 16 * TPR && i < s.count && d < a.c.hd) {
       const T* row = (const T*)a.q + (size_t)((long long)b * a.q_robot + (long long)i * a.q_token) +
-                     (size_t)(h * a.G + r % a.G) * a.c.hd;
+                     (size_t)(h * a.G + r - i * a.G) * a.c.hd;
       load16(row, d, a.c.hd, a.vec, x[z]);
     } else {
 #pragma unroll
@@ -247,7 +247,10 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
   Sight s;
   if (!robot_sight(a, b, s) && threadIdx.x == 0 && blockIdx.x == 0 && h == 0) raise_error(a.err, ERR_SHAPE);
   T* out0 = (T*)a.out + (size_t)((long long)b * a.out_robot) + (size_t)h * a.G * L.hd;
-  auto out_row = [&](int r) { return out0 + (size_t)((long long)(r / a.G) * a.out_token) + (size_t)(r % a.G) * L.hd; };
+  auto out_row = [&](int r) {
+    const int i = (int)a.by_G.of((uint32_t)r);
+    return out0 + (size_t)((long long)i * a.out_token) + (size_t)(r - i * a.G) * L.hd;
+  };
   if (r0 >= s.count * a.G || s.len == 0) {   // nothing to see: zeros
     if (split == 0)
       for (int w = threadIdx.x; w < rows * L.hd; w += RW * 32) out_row(r0 + w / L.hd)[w % L.hd] = from_f32<T>(0.f);

@@ -32,7 +32,7 @@ struct RowMask {
 
 __device__ __forceinline__ RowMask row_mask(const CacheAttnArgs& a, const Sight& s, int r) {
   RowMask m;
-  const int i = r / a.G;
+  const int i = (int)a.by_G.of((uint32_t)r);
   m.sinks = a.sinks;
   m.lo = 0;
   if (i >= s.count) m.hi = 0;

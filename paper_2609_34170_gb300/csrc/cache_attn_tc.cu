@@ -122,13 +122,14 @@ struct Item {
 // so that the CTAs' shares even out), then by split.
 __device__ __forceinline__ Item item_of(const CacheAttnArgs& a, int w) {
   Item it;
-  const uint32_t x = (uint32_t)w / (uint32_t)a.splits, per = (uint32_t)(a.group * a.row_tiles);
+  const uint32_t x = a.by_splits.of((uint32_t)w);
   it.split = w - (int)x * a.splits;
-  const uint32_t gi = x / per, rem = x - gi * per;
-  const uint32_t pairs = (uint32_t)min(a.group, a.batch * a.c.Hkv - (int)gi * a.group), row = rem / pairs;
+  const uint32_t gi = a.by_group.of(x), rem = x - gi * a.by_group.d;
+  const bool whole = ((int)gi + 1) * a.group <= a.batch * a.c.Hkv;
+  const uint32_t pairs = whole ? a.by_pairs.d : a.by_last.d, row = whole ? a.by_pairs.of(rem) : a.by_last.of(rem);
   it.tile = a.row_tiles - 1 - (int)row;
   it.head = (int)(gi * a.group + rem - row * pairs);
-  it.b = (int)((uint32_t)it.head / (uint32_t)a.c.Hkv);
+  it.b = (int)a.by_heads.of((uint32_t)it.head);
   it.h = it.head - it.b * a.c.Hkv;
   it.ok = robot_sight(a, it.b, it.s);
   it.live = it.tile * BM < it.s.count * a.G && it.s.len > 0;
@@ -136,8 +137,10 @@ __device__ __forceinline__ Item item_of(const CacheAttnArgs& a, int w) {
   if (it.live) {
     tile_sight(a, it.s, it.tile * BM, it.tile * BM + BM - 1, BT);
     it.hi = row_mask(a, it.s, min(it.tile * BM + BM, it.s.count * a.G) - 1).hi;
-    it.t0 = (int)((long long)it.s.units * it.split / a.splits);
-    it.n = (int)((long long)it.s.units * (it.split + 1) / a.splits) - it.t0;
+    // units * split / splits, and the same of the next split
+    const uint32_t each = a.by_splits.of((uint32_t)it.s.units), more = (uint32_t)it.s.units - each * a.by_splits.d;
+    it.t0 = (int)(each * it.split + a.by_splits.of(more * it.split));
+    it.n = (int)(each * (it.split + 1) + a.by_splits.of(more * (it.split + 1))) - it.t0;
   }
   return it;
 }
@@ -311,30 +314,32 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
       const uint32_t el = elect_one();
       const uint32_t idesc_s = idesc_f16(BM, BT), idesc_o = idesc_f16(BM, HDP) | (1u << 16);
       const uint64_t qd0 = sw64_desc(q0), kd0 = sw64_desc(k0), vd0 = sw128_mn_desc(v0, VB);
-      // the next item with tiles from w on: its tiles, and the last one's groups of 16 tokens
-      auto next = [&](int& w, int& n, int& last) {
-        n = 0;
-        for (; w < items; w += gridDim.x) {
-          const Item it = item_of(a, w);
-          n = uniform(it.n);
-          if (n == 0) continue;
-          last = uniform(it.groups(n - 1));
-          w += gridDim.x;
-          return;
+      // the items with tiles, in order: tiles and the last one's groups of 16 tokens, 0 behind the
+      // last item.  The next one is looked up while there is nothing to issue; lane q % 32 keeps
+      // item q's for P V, up to two items behind S.
+      int ws = blockIdx.x, ahead = 0, kept = 0;
+      bool looked = false;
+      auto look = [&]() {
+        ahead = 0;
+        looked = true;
+        for (; ws < items && ahead == 0; ws += gridDim.x) {
+          const Item it = item_of(a, ws);
+          const int n = uniform(it.n);
+          if (n > 0) ahead = n << 4 | uniform(it.groups(n - 1));
         }
       };
-      int ws = blockIdx.x, wp = blockIdx.x;           // the cursors' next items
-      int sn = 0, pn = 0, s_last = 0, last = 0;       // tiles of S's and P V's items
+      int sn = 0, pn = 0, last = 0;                   // tiles of S's and P V's items
       int si = 0, pi = 0, sq = 0, pq = 0;             // tiles done of them; items begun
       int gs = 0, gp = 0;                             // tiles in all
       int sk = 0, sv = 0;
       uint32_t phk = 0, phv = 0;
       bool ok = true;
       asm volatile("bar.sync 6, 544;" ::: "memory");
-      next(ws, sn, s_last);
-      wp = ws;
-      pn = sn;
-      last = s_last;
+      look();
+      looked = false;
+      kept = ahead;
+      sn = pn = ahead >> 4;
+      last = ahead & 15;
       while (pn > 0) {
         while (sn > 0 && gs <= gp + 1) {
           if (si == 0) {   // (P V of what is in flight does not wait for the next item's Q)
@@ -366,9 +371,13 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
             umma_commit(q_empty, el);
             si = 0;
             ++sq;
-            next(ws, sn, s_last);
+            if (!looked) look();
+            looked = false;
+            sn = ahead >> 4;
+            if (lane == (sq & 31)) kept = ahead;
           }
         }
+        if (!looked) look();
         if (ok) ok = wait_phase(&p_full[gp & 1], (uint32_t)(gp >> 1) & 1u);
         if (ok && pi == 0 && pq > 0) ok = wait_phase(o_free, (uint32_t)(pq - 1) & 1u);
         if (!ok) break;
@@ -396,7 +405,9 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
         if (++pi == pn) {
           pi = 0;
           ++pq;
-          next(wp, pn, last);
+          const int x = __shfl_sync(0xffffffffu, kept, pq & 31);   // (S has come to it)
+          pn = x >> 4;
+          last = x & 15;
         }
       }
       if (!ok) {   // what was issued ends before the TMEM goes away
@@ -463,13 +474,15 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
     const bool wide = places % 16 == 0, wider = (places | (uintptr_t)(L.hd * 2)) % 32 == 0;
     bool ok = true;   // (after a wait that ran out the loops go on without waiting, so that pairs meet at every barrier)
     int gt = 0, qi = 0;   // tiles and items with Q so far
+    Item coming = item_of(a, blockIdx.x);
     for (int w = blockIdx.x; w < items; w += gridDim.x) {
-      const Item it = item_of(a, w);
+      const Item it = coming;
+      const int after = min(w + (int)gridDim.x, items - 1);   // (looked up where the tensor core is waited for)
       const int r0 = it.tile * BM, rows = min(BM, a.n * a.G - r0), n = it.n;
       const size_t head = it.head;
       bf16* out0 = (bf16*)a.out + (size_t)((long long)it.b * a.out_robot) + (size_t)it.h * a.G * L.hd;
       auto out_row = [&](int lr) {
-        const uint32_t x = (uint32_t)(r0 + lr), i = x / (uint32_t)a.G;
+        const uint32_t x = (uint32_t)(r0 + lr), i = a.by_G.of(x);
         return out0 + (size_t)((long long)i * a.out_token) + (size_t)(x - i * (uint32_t)a.G) * L.hd;
       };
       if (!it.ok && it.tile == 0 && it.h == 0 && it.split == 0 && threadIdx.x == 0) raise_error(a.err, ERR_SHAPE);
@@ -478,6 +491,7 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
           for (int x = threadIdx.x; x < rows * L.hd; x += 256) out_row(x / L.hd)[x % L.hd] = __float2bfloat16_rn(0.f);
           if (a.mass && (int)threadIdx.x < rows) a.row_ml[head * a.n * a.G + r0 + threadIdx.x] = make_float2(0.f, 0.f);
         }
+        coming = item_of(a, after);
         continue;
       }
       const RowMask mk = row_mask(a, it.s, r0 + r);
@@ -582,6 +596,7 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
         tc_fence_before();
         mbar_arrive(&p_full[gt & 1]);
       }
+      coming = item_of(a, after);
       if (ok && n > 0) {
         ok = wait_phase(&pv_done[(gt - 1) & 1], (uint32_t)((gt - 1) >> 1) & 1u);
         tc_fence_after();
@@ -762,12 +777,16 @@ cudaError_t launch_nb(CacheAttnArgs a, cudaStream_t st) {
     while (splits > 1 && a.clusters[splits] < tiles) --splits;
   if (splits > 1) splits = (units + (units + splits - 1) / splits - 1) / ((units + splits - 1) / splits);
   a.splits = splits;
+  a.by_splits = LaunchDiv(splits);
   const TcMaps maps{a.maps->k_tc, a.maps->v_tc};
   // causal prompts: pairs whose caches take 48 MB together (beside the queries, in an L2 of 129)
   const long long pairs = (long long)a.c.Hkv * a.batch;
   a.group = 1;
   if (a.causal && !a.window) a.group = (int)std::min(pairs, std::max(1ll, (48ll << 20) / (2ll * a.max_length * a.c.hdp + 1)));
-  if (tiles * a.splits > 0x7fffffffll) return cudaErrorInvalidValue;
+  if (tiles * a.splits > 0x7fff0000ll) return cudaErrorInvalidValue;
+  a.by_group = LaunchDiv(a.group * a.row_tiles);
+  a.by_pairs = LaunchDiv(a.group);
+  a.by_last = LaunchDiv((int)std::max(1ll, pairs % a.group));
   const unsigned grid = a.splits == 1 ? (unsigned)std::min(tiles, (long long)a.num_sms) : (unsigned)(tiles * a.splits);
   return launch_kernel_cluster(cache_tc_kernel<NB>, dim3(grid), dim3(TCT), TcShape<NB>::bytes, st,
                                dim3(a.splits <= kTcCluster ? a.splits : 1, 1, 1), maps, a);

@@ -234,6 +234,8 @@ ravel_status ravel_cache_attend(ravel_cache_t* c, int layer, int batch, int n, c
   a.batch = batch;
   a.n = n;
   a.G = c->cfg.n_q_heads / c->cfg.n_kv_heads;
+  a.by_G = LaunchDiv(a.G);
+  a.by_heads = LaunchDiv(c->cfg.n_kv_heads);
   a.max_length = max_length;
   a.causal = causal;
   // (a window or sinks of the whole length hide nothing; bounded, positions stay in 32 bits)

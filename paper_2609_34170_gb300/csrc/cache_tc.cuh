@@ -113,7 +113,7 @@ __device__ __forceinline__ void stage_q8(const CacheAttnArgs& a, const Sight& s,
   // their way together)
   const uint32_t end_row = (uint32_t)(s.count * a.G);
   const bf16* base = (const bf16*)a.q + (size_t)((long long)b * a.q_robot) + (size_t)h * a.G * a.c.hd + (on ? 8 * dl : 0);
-  uint32_t r = (uint32_t)(r0 + rb + sub), i = r / (uint32_t)a.G, g = r - i * (uint32_t)a.G, there = 0u;
+  uint32_t r = (uint32_t)(r0 + rb + sub), i = a.by_G.of(r), g = r - i * (uint32_t)a.G, there = 0u;
   uint4 x[PASS];
   const bf16* at[PASS];
 #pragma unroll
