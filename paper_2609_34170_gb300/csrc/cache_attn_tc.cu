@@ -347,13 +347,20 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
             if (sq > 0 && gs > gp && !mbar_test_warp(q_full, (uint32_t)(sq - 1) & 1u)) break;
             if (sq > 0) ok = wait_phase(q_full, (uint32_t)(sq - 1) & 1u);
           }
+          if (ok) {   // the tile's K units
+            auto unit = [&](int x) { return sk + x < KS ? sk + x : sk + x - KS; };
+            auto par = [&](int x) { return sk + x < KS ? phk : phk ^ 1u; };
+            constexpr int u1 = NB > 1 ? 1 : 0, u2 = NB > 2 ? 2 : 0, u3 = NB > 3 ? 3 : 0;
+            ok = NB == 1 ? wait_phase(&k_full[sk], phk)
+                         : wait_phases(&k_full[sk], phk, &k_full[unit(u1)], par(u1), &k_full[unit(u2)], par(u2), &k_full[unit(u3)],
+                                       par(u3));
+          }
+          if (!ok) break;
+          tc_fence_after();
           const uint32_t sd = tmem + (uint32_t)(gs & 1) * BT;
           uint64_t ad = qd0;
 #pragma unroll 1
-          for (int blk = 0; ok && blk < NB; ++blk, ad += QB >> 4) {
-            ok = wait_phase(&k_full[sk], phk);
-            if (!ok) break;
-            tc_fence_after();
+          for (int blk = 0; blk < NB; ++blk, ad += QB >> 4) {
             const uint64_t bd = kd0 + (uint32_t)sk * (KU >> 4);
 #pragma unroll
             for (int k = 0; k < 4; ++k)   // both pieces of Q
@@ -364,7 +371,6 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
               phk ^= 1u;
             }
           }
-          if (!ok) break;
           umma_commit(&s_full[gs & 1], el);
           ++gs;
           if (++si == sn) {
@@ -378,21 +384,33 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
           }
         }
         if (!looked) look();
-        if (ok) ok = wait_phase(&p_full[gp & 1], (uint32_t)(gp >> 1) & 1u);
-        if (ok && pi == 0 && pq > 0) ok = wait_phase(o_free, (uint32_t)(pq - 1) & 1u);
-        if (!ok) break;
         const uint32_t pa = tmem + (uint32_t)(gp & 1) * BT;
         const int groups = pi + 1 < pn ? BT / 16 : last;
+        if (ok) {   // P, the first half of V (both, where several tiles' lie in the ring), a free O
+          const bool two = NB <= 2 && groups > 4, first = pi == 0 && pq > 0;
+          const int s = two ? (sv + 1 < VS ? sv + 1 : 0) : sv;
+          ok = wait_phases(&p_full[gp & 1], (uint32_t)(gp >> 1) & 1u, &v_full[sv], phv, &v_full[s], s < sv ? phv ^ 1u : phv,
+                           first ? o_free : &v_full[sv], first ? (uint32_t)(pq - 1) & 1u : phv);
+        }
+        if (!ok) break;
+        tc_fence_after();
 #pragma unroll 1
         for (int hv = 0; 4 * hv < groups; ++hv) {
-          ok = wait_phase(&v_full[sv], phv);
-          if (!ok) break;
-          tc_fence_after();
+          if (NB > 2 && hv > 0) {
+            ok = wait_phase(&v_full[sv], phv);
+            if (!ok) break;
+            tc_fence_after();
+          }
           const uint64_t bd = vd0 + (uint32_t)sv * (VH >> 4);
+          const uint32_t ph = pa + 32 * hv, more = pi + hv > 0 ? 1u : 0u;
+          if (groups >= 4 * hv + 4) {   // (a comparison and a branch per MMA take longer than the MMA)
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (4 * hv + k < groups)
-              umma_bf16_ts(tmem + o_col, pa + 8 * (4 * hv + k), bd + 128 * k, idesc_o, (pi + hv + k > 0) ? 1u : 0u, el);
+            for (int k = 0; k < 4; ++k) umma_bf16_ts(tmem + o_col, ph + 8 * k, bd + 128 * k, idesc_o, k > 0 ? 1u : more, el);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 3; ++k)
+              if (4 * hv + k < groups) umma_bf16_ts(tmem + o_col, ph + 8 * k, bd + 128 * k, idesc_o, k > 0 ? 1u : more, el);
+          }
           umma_commit(&v_empty[sv], el);
           if (++sv == VS) {
             sv = 0;

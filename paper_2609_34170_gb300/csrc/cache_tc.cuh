@@ -85,6 +85,33 @@ __device__ __forceinline__ bool wait_phase(uint64_t* bar, uint32_t parity) {
   return __all_sync(0xffffffffu, ok != 0);
 }
 
+// The same for up to four phases, tried side by side (a try's latency is most of a wait's for
+// what has arrived; one behind the other, four waits took 500 cycles).  All lanes wait for
+// the same barriers.
+__device__ __forceinline__ bool wait_phases(uint64_t* b0, uint32_t p0, uint64_t* b1, uint32_t p1, uint64_t* b2, uint32_t p2,
+                                            uint64_t* b3, uint32_t p3) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p, q, r, s, t;\n\t.reg .u32 n;\n\t"
+      "mov.u32 n, 0;\n\t"
+      "TRY: mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 r, [%3], %4;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 s, [%5], %6;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 t, [%7], %8;\n\t"
+      "and.pred p, p, r;\n\t"
+      "and.pred s, s, t;\n\t"
+      "and.pred p, p, s;\n\t"
+      "@p bra DONE;\n\t"
+      "add.u32 n, n, 1;\n\t"
+      "setp.lt.u32 q, n, 16777216;\n\t"
+      "@q bra TRY;\n\t"
+      "DONE: selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(b0)), "r"(p0), "r"(smem_u32(b1)), "r"(p1), "r"(smem_u32(b2)), "r"(p2), "r"(smem_u32(b3)), "r"(p3)
+      : "memory");
+  return __all_sync(0xffffffffu, ok != 0);
+}
+
 // A warp's writes to shared memory become visible to the tensor core: one arrival per warp.
 __device__ __forceinline__ void written(uint64_t* bar) {
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
