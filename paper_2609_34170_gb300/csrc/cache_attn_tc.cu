@@ -57,7 +57,9 @@ template <int NB> struct TcShape {
   static_assert(CV % 4 == 0, "widening warps");
   static constexpr uint32_t q_bytes = 2 * NB * QB;
   static constexpr uint32_t ring = KS * KU + VS * NB * VB + CV * CB;
-  static constexpr uint32_t bytes = q_bytes + ring + 3072;
+  // places for the halves' maxima: in turn where there is room, which saves a barrier a tile
+  static constexpr int XM = NB == 4 ? 1 : 2;
+  static constexpr uint32_t bytes = q_bytes + ring + 1024 + XM * 2048;
   static_assert(bytes <= 227 * 1024, "shared memory");
   // a row of the fp32 output that splits exchange (over the rings): 16 bytes more than
   // the dims, so that rows written by neighbouring lanes fall on different banks
@@ -174,7 +176,7 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
   // exponent bits of the rows' largest |q|, [4][128], by item: S runs up to two tiles, so up
   // to two items, ahead of the softmax, and Q one more
   uint8_t* row_exp = tail + 512;
-  float2* xm = (float2*)(row_exp + 512);   // [2][128] row maxima, then sums, of the two halves
+  float2* xm = (float2*)(row_exp + 512);   // [XM][2][128] row maxima, then sums, of the two halves
   static_assert((2 * KS + 2 * VS + 2 * CV + 11) * 8 + 24 <= 512, "barriers");
 
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
@@ -342,10 +344,10 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
       last = ahead & 15;
       while (pn > 0) {
         while (sn > 0 && gs <= gp + 1) {
-          if (si == 0) {   // (P V of what is in flight does not wait for the next item's Q)
-            // (the first item's came through barrier 6)
-            if (sq > 0 && gs > gp && !mbar_test_warp(q_full, (uint32_t)(sq - 1) & 1u)) break;
-            if (sq > 0) ok = wait_phase(q_full, (uint32_t)(sq - 1) & 1u);
+          if (si == 0) {
+            // an item's last P V goes first: its output is what the softmax does next
+            if (gs > gp) break;
+            if (sq > 0) ok = wait_phase(q_full, (uint32_t)(sq - 1) & 1u);   // (the first item's came through barrier 6)
           }
           if (ok) {   // the tile's K units
             auto unit = [&](int x) { return sk + x < KS ? sk + x : sk + x - KS; };
@@ -383,7 +385,7 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
             if (lane == (sq & 31)) kept = ahead;
           }
         }
-        if (!looked) look();
+        if (!looked && pi == 0) look();   // (the softmax is at the output of the item before)
         const uint32_t pa = tmem + (uint32_t)(gp & 1) * BT;
         const int groups = pi + 1 < pn ? BT / 16 : last;
         if (ok) {   // P, the first half of V (both, where several tiles' lie in the ring), a free O
@@ -562,11 +564,13 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
           mx = fmaxf(mx, x);
           wx = fmaxf(wx, x + (float)(int8_t)(ves >> (8 * t)));
         }
-        // (past the first barrier both halves have read their scores, past the second the maxima)
-        xm[hf * 128 + r] = make_float2(mx, wx);
+        // (past the barrier both halves have read their scores, past a second or the next tile's
+        // the maxima)
+        float2* xt = xm + (Shape::XM > 1 ? (gt & 1) * 256 : 0);
+        xt[hf * 128 + r] = make_float2(mx, wx);
         pair_bar();
-        const float2 x0 = xm[r], x1 = xm[128 + r];
-        pair_bar();
+        const float2 x0 = xt[r], x1 = xt[128 + r];
+        if (Shape::XM == 1) pair_bar();
         const float mn = fmaxf(m, ceilf(fmaxf(x0.x, x1.x))), wn = fmaxf(W, ceilf(fmaxf(x0.y, x1.y)));
         const float mu = mn == -INFINITY ? 0.f : mn;
         l *= pow2f_down(m - mu);
@@ -619,9 +623,10 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
         ok = wait_phase(&pv_done[(gt - 1) & 1], (uint32_t)((gt - 1) >> 1) & 1u);
         tc_fence_after();
       }
+      pair_bar();   // (the last tile's maxima are read)
       xm[hf * 128 + r].x = l;
       pair_bar();
-      l = xm[r].x + xm[128 + r].x;   // (read before the next tile's first barrier)
+      l = xm[r].x + xm[128 + r].x;
       pair_bar();
       const bool real = mk.hi > 0 && n > 0 && !(l <= 0.f);   // (a sum that is not a number stays one)
       const float inv = real ? pow2f(W - m) / l : 0.f;
