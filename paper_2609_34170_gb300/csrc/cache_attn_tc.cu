@@ -520,64 +520,72 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
       const int8_t *KE = L.ke + head * (L.T / 16), *VE = L.ve + head * (L.T / 16);
       // references in the log2 domain, integral: m of the row's sum, W of O (largest score + value exponent)
       float m = -INFINITY, W = -INFINITY, l = 0.f;
-      for (int i = 0; i < n; ++i, ++gt) {
-        const int j0 = it.token(i);
-        // exponents of this half's four blocks
-        const uint32_t kes = *(const uint32_t*)(KE + j0 / 16 + 4 * hf), ves = *(const uint32_t*)(VE + j0 / 16 + 4 * hf);
-        const bool full = j0 + BT <= firstm.hi && (j0 >= lastm.lo || j0 + BT <= a.sinks);
-        if (ok) ok = wait_phase(&s_full[gt & 1], (uint32_t)(gt >> 1) & 1u);
-        tc_fence_after();
-        if (i == 0) {   // (S needed Q: it is there)
-          rf = q_factor(row_exp[(qi & 3) * BM + r], a.scale_log2);
-          ++qi;
-        }
-        float sc[64];
-        {
-          uint32_t raw[64];
-          const uint32_t srow = lane_base + (uint32_t)(gt & 1) * BT + 64 * hf;
+      // 64 of a tile's scores from the row's column `at` on, token j the first; hidden ones -inf
+      auto scores = [&](uint32_t at, int j, bool full, float (&sc)[64]) {
+        uint32_t raw[64];
 #pragma unroll
-          for (int q = 0; q < 4; ++q) tmem_ld16_async(srow + 16 * q, raw + 16 * q);
-          tmem_wait_ld();
+        for (int q = 0; q < 64; q += 16) tmem_ld16_async(at + q, raw + q);
+        tmem_wait_ld();
 #pragma unroll
-          for (int q = 0; q < 4; ++q) tmem_reg_fence16(raw + 16 * q);
+        for (int q = 0; q < 64; q += 16) tmem_reg_fence16(raw + q);
 #pragma unroll
-          for (int k = 0; k < 64; ++k) sc[k] = __uint_as_float(raw[k]);
-        }
+        for (int k = 0; k < 64; ++k) sc[k] = __uint_as_float(raw[k]);
         if (!full) {
 #pragma unroll
           for (int k2 = 0; k2 < 64; k2 += 32) {
-            const uint32_t see = mk.bits(j0 + 64 * hf + k2);
+            const uint32_t see = mk.bits(j + k2);
 #pragma unroll
             for (int k = 0; k < 32; ++k) sc[k2 + k] = see >> k & 1u ? sc[k2 + k] : -INFINITY;
           }
         }
-        float f[4], mx = -INFINITY, wx = -INFINITY;
+      };
+      // a block's factor (not 0, which times a hidden score's -inf would not be a number)
+      auto factor = [&](uint32_t kes, int t) { return fmaxf(rf * exp2i((int)(int8_t)(kes >> (8 * t))), 1e-37f); };
+      // their largest score and largest score + value exponent
+      auto maxima = [&](const float (&sc)[64], uint32_t kes, uint32_t ves, float& mx, float& wx) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-          // (not 0, which times a hidden score's -inf would not be a number)
-          f[t] = fmaxf(rf * exp2i((int)(int8_t)(kes >> (8 * t))), 1e-37f);
-          float m4[4];
+          float m5[5];
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            m4[e] = fmaxf(fmaxf(sc[16 * t + 4 * e], sc[16 * t + 4 * e + 1]), fmaxf(sc[16 * t + 4 * e + 2], sc[16 * t + 4 * e + 3]));
-          const float x = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * f[t];
+          for (int e = 0; e < 5; ++e) m5[e] = max3(sc[16 * t + 3 * e], sc[16 * t + 3 * e + 1], sc[16 * t + 3 * e + 2]);
+          const float x = fmaxf(max3(m5[0], m5[1], m5[2]), max3(m5[3], m5[4], sc[16 * t + 15])) * factor(kes, t);
           mx = fmaxf(mx, x);
           wx = fmaxf(wx, x + (float)(int8_t)(ves >> (8 * t)));
         }
-        // (past the barrier both halves have read their scores, past a second or the next tile's
-        // the maxima)
-        float2* xt = xm + (Shape::XM > 1 ? (gt & 1) * 256 : 0);
-        xt[hf * 128 + r] = make_float2(mx, wx);
-        pair_bar();
-        const float2 x0 = xt[r], x1 = xt[128 + r];
-        if (Shape::XM == 1) pair_bar();
-        const float mn = fmaxf(m, ceilf(fmaxf(x0.x, x1.x))), wn = fmaxf(W, ceilf(fmaxf(x0.y, x1.y)));
-        const float mu = mn == -INFINITY ? 0.f : mn;
+      };
+      // their weights into P at `to`, and into the row's sum
+      auto weights = [&](const float (&sc)[64], uint32_t kes, uint32_t ves, float mu, float wu, uint32_t to) {
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2) {
+          uint32_t wd[16];
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const int blk = 2 * h2 + t;
+            // the value exponent goes into that of P and out of the block's sum again
+            const float vf = fmaxf((float)(int8_t)(ves >> (8 * blk)), wu - mu - kVeBelow), nbt = kTcShift + vf - wu;
+            const float f = factor(kes, blk);
+            float2 e[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+              e[q] = fma2(make_float2(sc[16 * blk + 2 * q], sc[16 * blk + 2 * q + 1]), make_float2(f, f), make_float2(nbt, nbt));
+              e[q] = make_float2(fast_exp2(e[q].x), fast_exp2(e[q].y));
+              wd[8 * t + q] = pack_f16x2(e[q].x, e[q].y);
+            }
+            const float2 s = add2(add2(add2(e[0], e[1]), add2(e[2], e[3])), add2(add2(e[4], e[5]), add2(e[6], e[7])));
+            l = fmaf(s.x + s.y, pow2f(wu - mu - vf), l);
+          }
+          tmem_st16u(to + 16 * h2, wd);
+        }
+      };
+      // new references; where W rises by much, O, which holds P V of every earlier tile once the
+      // last one's has completed, is rescaled
+      auto refer = [&](float mx, float wx, bool any, float& mu, float& wu) {
+        const float mn = fmaxf(m, ceilf(mx)), wn = fmaxf(W, ceilf(wx));
+        mu = mn == -INFINITY ? 0.f : mn;
         l *= pow2f_down(m - mu);
         m = mn;
         const bool need = wn > W + 8.f;
-        if (i > 0 && __any_sync(0xffffffffu, need)) {
-          // O holds P V of every earlier tile before it is rescaled
+        if (any && __any_sync(0xffffffffu, need)) {
           if (ok) ok = wait_phase(&pv_done[(gt - 1) & 1], (uint32_t)((gt - 1) >> 1) & 1u);
           tc_fence_after();
           const float alpha = need ? pow2f_down(W - wn) : 1.f;
@@ -592,32 +600,34 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
           tmem_wait_st();
         }
         if (need) W = wn;
-        const float wu = W == -INFINITY ? 0.f : W;
-        const uint32_t prow = lane_base + (uint32_t)(gt & 1) * BT + 32 * hf;
-#pragma unroll
-        for (int h2 = 0; h2 < 2; ++h2) {
-          uint32_t wd[16];
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            const int blk = 2 * h2 + t;
-            // the value exponent goes into that of P and out of the block's sum again
-            const float vf = fmaxf((float)(int8_t)(ves >> (8 * blk)), wu - mu - kVeBelow), nbt = kTcShift + vf - wu;
-            float e[16];
-#pragma unroll
-            for (int q = 0; q < 16; ++q) e[q] = fast_exp2(fmaf(sc[16 * blk + q], f[blk], nbt));
-            float s4[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) s4[q] = (e[4 * q] + e[4 * q + 1]) + (e[4 * q + 2] + e[4 * q + 3]);
-            l = fmaf((s4[0] + s4[1]) + (s4[2] + s4[3]), pow2f(wu - mu - vf), l);
-#pragma unroll
-            for (int q = 0; q < 8; ++q) wd[8 * t + q] = pack_f16x2(e[2 * q], e[2 * q + 1]);
-          }
-          tmem_st16u(prow + 16 * h2, wd);
-        }
+        wu = W == -INFINITY ? 0.f : W;
+      };
+      for (int i = 0; i < n; ++i, ++gt) {
+        const int j0 = it.token(i);
+        // exponents of this half's four blocks
+        const uint32_t kes = *(const uint32_t*)(KE + j0 / 16 + 4 * hf), ves = *(const uint32_t*)(VE + j0 / 16 + 4 * hf);
+        const bool full = j0 + BT <= firstm.hi && (j0 >= lastm.lo || j0 + BT <= a.sinks);
+        if (ok) ok = wait_phase(&s_full[gt & 1], (uint32_t)(gt >> 1) & 1u);
+        tc_fence_after();
+        if (i == 0) rf = q_factor(row_exp[(qi & 3) * BM + r], a.scale_log2);   // (S needed Q: it is there)
+        const uint32_t srow = lane_base + (uint32_t)(gt & 1) * BT;
+        float sc[64], mx = -INFINITY, wx = -INFINITY, mu, wu;
+        scores(srow + 64 * hf, j0 + 64 * hf, full, sc);
+        maxima(sc, kes, ves, mx, wx);
+        // (past the barrier both halves have read their scores, past a second or the next tile's
+        // the maxima)
+        float2* xt = xm + (Shape::XM > 1 ? (gt & 1) * 256 : 0);
+        xt[hf * 128 + r] = make_float2(mx, wx);
+        pair_bar();
+        const float2 x0 = xt[r], x1 = xt[128 + r];
+        if (Shape::XM == 1) pair_bar();
+        refer(fmaxf(x0.x, x1.x), fmaxf(x0.y, x1.y), i > 0, mu, wu);
+        weights(sc, kes, ves, mu, wu, srow + 32 * hf);
         tmem_wait_st();
         tc_fence_before();
         mbar_arrive(&p_full[gt & 1]);
       }
+      if (n > 0) ++qi;
       coming = item_of(a, after);
       if (ok && n > 0) {
         ok = wait_phase(&pv_done[(gt - 1) & 1], (uint32_t)((gt - 1) >> 1) & 1u);
@@ -630,6 +640,15 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
       pair_bar();
       const bool real = mk.hi > 0 && n > 0 && !(l <= 0.f);   // (a sum that is not a number stays one)
       const float inv = real ? pow2f(W - m) / l : 0.f;
+      // 32 of the row's outputs, normalised
+      auto output = [&](int cb, uint32_t (&raw)[32]) {
+        tmem_ld32_async(lane_base + o_col + cb, raw);
+        tmem_wait_ld();
+        tmem_reg_fence16(raw);
+        tmem_reg_fence16(raw + 16);
+#pragma unroll
+        for (int q = 0; q < 32; ++q) raw[q] = real ? __float_as_uint(__uint_as_float(raw[q]) * inv) : 0u;
+      };
       const float m_out = real ? m : -INFINITY, l_out = real ? l : 0.f;
       if (a.splits == 1) {
         if (a.mass && hf == 0 && r < rows) a.row_ml[head * a.n * a.G + r0 + r] = row_weight(m_out, l_out, kTcShift);
@@ -638,10 +657,7 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
 #pragma unroll 1
         for (int cb = 32 * hf; cb < HDP; cb += 64) {   // (the warpgroups take alternate columns)
           uint32_t raw[32];
-          tmem_ld32_async(lane_base + o_col + cb, raw);
-          tmem_wait_ld();
-          tmem_reg_fence16(raw);
-          tmem_reg_fence16(raw + 16);
+          output(cb, raw);
           if (cb + 64 >= HDP) {   // the last of O: the next item's may begin
             tc_fence_before();
             __syncwarp();
@@ -649,8 +665,7 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
           }
           uint32_t wd[16];
 #pragma unroll
-          for (int q = 0; q < 16; ++q)
-            wd[q] = real ? pack_bf16x2(__uint_as_float(raw[2 * q]) * inv, __uint_as_float(raw[2 * q + 1]) * inv) : 0u;
+          for (int q = 0; q < 16; ++q) wd[q] = pack_bf16x2(__uint_as_float(raw[2 * q]), __uint_as_float(raw[2 * q + 1]));
           const int ends = r < rows ? L.hd : 0;
           if (wider) {   // (half the requests of 16-byte stores, each to 32 rows)
 #pragma unroll
@@ -673,12 +688,7 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
 #pragma unroll 1
       for (int cb = 32 * hf; cb < HDP; cb += 64) {
         uint32_t raw[32];
-        tmem_ld32_async(lane_base + o_col + cb, raw);
-        tmem_wait_ld();
-        tmem_reg_fence16(raw);
-        tmem_reg_fence16(raw + 16);
-#pragma unroll
-        for (int q = 0; q < 32; ++q) raw[q] = real ? __float_as_uint(__uint_as_float(raw[q]) * inv) : 0u;
+        output(cb, raw);
         if (cluster) {
 #pragma unroll
           for (int q = 0; q < 8; ++q)

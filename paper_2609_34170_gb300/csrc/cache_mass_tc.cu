@@ -213,7 +213,7 @@ __global__ void __launch_bounds__(MT, 1) cache_mass_tc_kernel(const __grid_const
         const bool full = __all_sync(0xffffffffu, rlo <= 0 && rhi >= 64);
         if (ok) ok = wait_phase(&s_full[g & 1], (uint32_t)(g >> 1) & 1u);
         tc_fence_after();
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll 1
         for (int c = 0; c < 2; ++c) {
           uint32_t raw[32];
@@ -226,12 +226,15 @@ __global__ void __launch_bounds__(MT, 1) cache_mass_tc_kernel(const __grid_const
 #pragma unroll
             for (int k = 0; k < 32; k += 4) {
               const float4 y = lds_f4(ry + 128u * c + 4u * k), x0 = lds_f4(rc + 256u * c + 8u * k), x1 = lds_f4(rc + 256u * c + 8u * k + 16u);
-              const float ys[4] = {y.x, y.y, y.z, y.w}, fs[4] = {x0.x, x0.z, x1.x, x1.z}, cs[4] = {x0.y, x0.w, x1.y, x1.w};
-#pragma unroll
-              for (int q = 0; q < 4; ++q) {
-                const float e = fmaf(__uint_as_float(raw[k + q]) * kf, fs[q], cs[q]);
-                sum[q] = fmaf(fast_exp2(hidden(k + q) ? -INFINITY : e), hidden(k + q) ? 0.f : ys[q], sum[q]);
-              }
+              const float2 kf2 = make_float2(kf, kf), none = make_float2(0.f, 0.f);
+              const float2 a0 = fma2(make_float2(__uint_as_float(raw[k]), __uint_as_float(raw[k + 1])), kf2, none);
+              const float2 a1 = fma2(make_float2(__uint_as_float(raw[k + 2]), __uint_as_float(raw[k + 3])), kf2, none);
+              float2 e0 = fma2(a0, make_float2(x0.x, x0.z), make_float2(x0.y, x0.w));
+              float2 e1 = fma2(a1, make_float2(x1.x, x1.z), make_float2(x1.y, x1.w));
+              e0 = make_float2(fast_exp2(hidden(k) ? -INFINITY : e0.x), fast_exp2(hidden(k + 1) ? -INFINITY : e0.y));
+              e1 = make_float2(fast_exp2(hidden(k + 2) ? -INFINITY : e1.x), fast_exp2(hidden(k + 3) ? -INFINITY : e1.y));
+              sum[0] = fma2(e0, make_float2(hidden(k) ? 0.f : y.x, hidden(k + 1) ? 0.f : y.y), sum[0]);
+              sum[1] = fma2(e1, make_float2(hidden(k + 2) ? 0.f : y.z, hidden(k + 3) ? 0.f : y.w), sum[1]);
             }
           };
           if (full) {
@@ -244,7 +247,7 @@ __global__ void __launch_bounds__(MT, 1) cache_mass_tc_kernel(const __grid_const
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&s_free[g & 1]);
-        own[j0] = old + ((sum[0] + sum[1]) + (sum[2] + sum[3]));
+        own[j0] = old + ((sum[0].x + sum[0].y) + (sum[1].x + sum[1].y));
       }
     }
   }
