@@ -77,13 +77,6 @@ __device__ __forceinline__ void widen(uint4 w, uint32_t lo, uint32_t hi) {
   sts_u4(hi, make_uint4(e4m3_lo(w.z), e4m3_hi(w.z), e4m3_lo(w.w), e4m3_hi(w.w)));
 }
 
-// 32 bytes, 32-byte aligned
-__device__ __forceinline__ void stg_u8(void* p, const uint32_t* w) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
-               "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-               : "memory");
-}
-
 __device__ __forceinline__ void store_bf16x8(bf16* dst, uint4 w, bool wide) {
   if (wide) {
     *(uint4*)dst = w;
@@ -491,7 +484,7 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
     auto pair_bar = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory"); };   // warps w and w + 4
     const uint32_t lane_base = tmem + ((uint32_t)(q4 * 32) << 16);
     const uintptr_t places = (uintptr_t)a.out | (uintptr_t)(a.out_robot * 2) | (uintptr_t)(a.out_token * 2);
-    const bool wide = places % 16 == 0, wider = (places | (uintptr_t)(L.hd * 2)) % 32 == 0;
+    const bool wide = places % 16 == 0;
     bool ok = true;   // (after a wait that ran out the loops go on without waiting, so that pairs meet at every barrier)
     int gt = 0, qi = 0;   // tiles and items with Q so far
     Item coming = item_of(a, blockIdx.x);
@@ -653,7 +646,9 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
       if (a.splits == 1) {
         if (a.mass && hf == 0 && r < rows) a.row_ml[head * a.n * a.G + r0 + r] = row_weight(m_out, l_out, kTcShift);
         // O / l as bf16, each thread's columns of its row
-        bf16* dst = out_row(min(r, rows - 1));
+        bf16 *own = out_row(min(r, rows - 1)), *dst[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) dst[k] = out_row(min(q4 * 32 + (lane & ~3) + k, rows - 1)) + 8 * (lane & 3);
 #pragma unroll 1
         for (int cb = 32 * hf; cb < HDP; cb += 64) {   // (the warpgroups take alternate columns)
           uint32_t raw[32];
@@ -666,15 +661,27 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
           uint32_t wd[16];
 #pragma unroll
           for (int q = 0; q < 16; ++q) wd[q] = pack_bf16x2(__uint_as_float(raw[2 * q]), __uint_as_float(raw[2 * q + 1]));
-          const int ends = r < rows ? L.hd : 0;
-          if (wider) {   // (half the requests of 16-byte stores, each to 32 rows)
+          if (wide) {
+            // four lanes' rows turned into four pieces of a row each: stores of 8 rows x 64 bytes
+            auto turn = [&](uint32_t& a, uint32_t& b, int bit) {
+              const uint32_t got = __shfl_xor_sync(0xffffffffu, lane & bit ? a : b, bit);
+              (lane & bit ? a : b) = got;
+            };
 #pragma unroll
-            for (int q = 0; q < 2; ++q)
-              if (cb + 16 * q < ends) stg_u8(dst + cb + 16 * q, wd + 8 * q);
-          } else {
+            for (int q = 0; q < 4; ++q) {
+              turn(wd[q], wd[4 + q], 1);
+              turn(wd[8 + q], wd[12 + q], 1);
+              turn(wd[q], wd[8 + q], 2);
+              turn(wd[4 + q], wd[12 + q], 2);
+            }
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-              if (cb + 8 * q < ends) store_bf16x8(dst + cb + 8 * q, make_uint4(wd[4 * q], wd[4 * q + 1], wd[4 * q + 2], wd[4 * q + 3]), wide);
+            for (int k = 0; k < 4; ++k)
+              if (q4 * 32 + (lane & ~3) + k < rows && cb + 8 * (lane & 3) < L.hd)
+                *(uint4*)(dst[k] + cb) = make_uint4(wd[4 * k], wd[4 * k + 1], wd[4 * k + 2], wd[4 * k + 3]);
+          } else if (r < rows) {
+#pragma unroll
+            for (int q = 0; q < 32; ++q)
+              if (cb + q < L.hd) own[cb + q] = __ushort_as_bfloat16((unsigned short)(wd[q / 2] >> (16 * (q & 1))));
           }
         }
         continue;
