@@ -157,6 +157,7 @@ __global__ void __launch_bounds__(256) cache_read_kernel(ReadArgs a) {
 // ---- eviction ---------------------------------------------------------------
 
 constexpr int kSelThreads = 1024;
+constexpr int kSelCluster = 8;      // CTAs of a head at most
 
 __device__ __forceinline__ unsigned ld_cluster_u1(uint32_t a) {
   unsigned v;
@@ -172,7 +173,7 @@ __device__ __forceinline__ uint32_t mass_key(float x) {
 }
 
 // The tokens that one (robot, KV head) keeps: the key of the last one in by a radix
-// selection over the middle's masses (four histograms of 8 bits), then one ordered
+// selection over the middle's masses (up to four histograms of 8 bits), then one ordered
 // pass that gives each kept token its place.  Ties go to the earlier tokens.  No order
 // of arrival enters the result: the histograms count.
 //
@@ -182,7 +183,7 @@ __device__ __forceinline__ uint32_t mass_key(float x) {
 // tokens, 64 dependent turns of the loop per pass.
 __global__ void __launch_bounds__(kSelThreads) cache_select_kernel(EvictArgs a, int ctas) {
   __shared__ unsigned hist[2][256], sums[256];
-  __shared__ uint32_t sel_bin, sel_left;
+  __shared__ uint32_t sel_bin, sel_left, sel_all;
   __shared__ unsigned totals[2][32];
   __shared__ unsigned kept_here[2], before_here[2];   // surely in, ties: of this CTA's run, of the runs before it
   const int h = blockIdx.x / ctas, rank = blockIdx.x % ctas, b = blockIdx.y, Hkv = a.from.Hkv;
@@ -234,7 +235,11 @@ __global__ void __launch_bounds__(kSelThreads) cache_select_kernel(EvictArgs a, 
         unsigned n = 0;
         if (ctas > 1) {
           const uint32_t at = smem_u32(&hist[buf][tid]);
-          for (int q = 0; q < ctas; ++q) n += ld_cluster_u1(mapa_shared(at, (uint32_t)q));
+          unsigned x[kSelCluster];   // (all on their way together)
+#pragma unroll
+          for (int q = 0; q < kSelCluster; ++q) x[q] = ld_cluster_u1(mapa_shared(at, (uint32_t)min(q, ctas - 1)));
+#pragma unroll
+          for (int q = 0; q < kSelCluster; ++q) n += q < ctas ? x[q] : 0u;
         } else {
           n = hist[buf][tid];
         }
@@ -263,6 +268,7 @@ __global__ void __launch_bounds__(kSelThreads) cache_select_kernel(EvictArgs a, 
             if (!found && before + n[q] >= left) {
               sel_bin = (uint32_t)(255 - 8 * lane - q);
               sel_left = left - before;
+              sel_all = n[q];
               found = true;
             }
             before += n[q];
@@ -273,6 +279,11 @@ __global__ void __launch_bounds__(kSelThreads) cache_select_kernel(EvictArgs a, 
       prefix |= sel_bin << shift;
       mask |= 255u << shift;
       left = sel_left;
+      if (sel_all == left && prefix > 0u) {   // the whole bin stays: its least key, and no ties
+        --prefix;
+        left = 0;
+        break;
+      }
     }
   }
   // which tokens are surely in (heavier, first, last), and which are ties
@@ -304,8 +315,11 @@ __global__ void __launch_bounds__(kSelThreads) cache_select_kernel(EvictArgs a, 
     }
     cluster_sync();
     if (tid < 2) {
-      unsigned n = 0;
-      for (int q = 0; q < rank; ++q) n += ld_cluster_u1(mapa_shared(smem_u32(&kept_here[tid]), (uint32_t)q));
+      unsigned n = 0, x[kSelCluster];
+#pragma unroll
+      for (int q = 0; q < kSelCluster; ++q) x[q] = ld_cluster_u1(mapa_shared(smem_u32(&kept_here[tid]), (uint32_t)min(q, ctas - 1)));
+#pragma unroll
+      for (int q = 0; q < kSelCluster; ++q) n += q < rank ? x[q] : 0u;
       before_here[tid] = n;
     }
     __syncthreads();
@@ -388,7 +402,7 @@ cudaError_t launch_cache_read(const ReadArgs& a, Dtype dt, cudaStream_t st) {
 
 cudaError_t launch_cache_evict(const EvictArgs& a, cudaStream_t st) {
   // a CTA per 4096 tokens, up to a cluster of 8 (at 816 tokens a cluster's barriers take longer than they save)
-  const int ctas = (int)std::min(8ll, std::max(1ll, std::min((long long)a.max_tokens, a.mass_stride) / 4096));
+  const int ctas = (int)std::min((long long)kSelCluster, std::max(1ll, std::min((long long)a.max_tokens, a.mass_stride) / 4096));
   cudaError_t e = launch_kernel_cluster(cache_select_kernel, dim3(a.from.Hkv * ctas, a.batch), dim3(kSelThreads), 0, st,
                                         dim3(ctas, 1, 1), a, ctas);
   if (e != cudaSuccess) return e;
