@@ -2,19 +2,28 @@
 // short runs of queries) and in fp32, and the attention mass of its tokens.
 //
 // Rows: query i, head g of a KV head's group is row r = i * G + g; a CTA owns a
-// tile of 16 rows of one (robot, KV head) and a share (split) of the tokens
-// that the tile sees; its warps take turns at units of 16 * NT tokens, each
-// with its own running maximum, sum and output, which are joined in shared
-// memory and then across the splits.
+// tile of 8 rows (where a robot's query rows are no more) or 16 of one (robot, KV
+// head) and a share (split) of the tokens that the tile sees; its four warps take
+// turns at units of 16 * NT tokens, each with its own running maximum, sum and
+// output, which are joined in shared memory and then across the splits: up to 8 of
+// them as a cluster, through its shared memory, more through L2.
 //
-// What bounds it is the cache's bytes: 16 query rows against a token cost one
-// m16n8k16 row of MMAs whatever the group's size, so a token's time does not
-// depend on G.  These MMAs take their operands from registers: the codes go
-// from global memory to registers and are widened there (e4m3 -> f16 is exact),
-// in an order of dims and tokens that makes every load 16 bytes: within an MMA
-// the dims of q k (and the tokens of p v) may come in any order that both
-// operands share.  tcgen05 would want the widened codes in shared memory first
-// and 128 rows to work on.
+// What bounds it on long caches is the cache's bytes: 8 query rows against 16 tokens
+// cost one m16n8k16 MMA per 16 dims whatever the group's size, so a token's time does
+// not depend on G.  A warp's units (K and V of 16 to 64 tokens, 8 KB) come by TMA into
+// a ring of its own that nobody else waits for, three units ahead, 96 KB a CTA and
+// two CTAs an SM; loads to registers held half of that in flight (4 robots of 131071
+// tokens: 149 us, now 56).  From there the codes go to registers 16 bytes at a time
+// and are widened there (e4m3 -> f16 is exact): within an MMA the dims of q k (and the
+// tokens of p v) may come in any order that both operands share, so that no load is
+// narrower.  tcgen05 would want the widened codes in shared memory first and 128 rows
+// to work on.  Few rows take K as the A operand, 16 tokens by 8 rows, and P transposed
+// in registers: half the MMAs and exponentials of a tile of 16 rows that is half empty.
+//
+// Measured (one query per robot, bf16): one robot of 816 tokens, head dim 256: 10.0 us,
+// a chain of launch, Q, one unit per warp, two joins; 64 robots of 1024 to 2048: 18.6 us
+// for 50 MB (2.7 TB/s; a round of unequal robots); 4 robots of 131071, 4 heads of 64:
+// 56 us for 269 MB (4.8 TB/s).  3 robots, 37 queries, 301 tokens in fp32: 9.7 us.
 //
 // Numbers: q is scaled by a power of two per row to a maximum in [2^14, 2^15) and
 // held in f16 -- exactly for bf16 inputs (8 significant bits; what lies 2^38
@@ -782,7 +791,10 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
 // Attention mass: token j's softmax weights summed over the rows of its KV
 // head, from the rows' (max, 1 / sum) that the attention left behind.  A warp
 // owns a block of 16 tokens, keeps its widened key fragments in registers and
-// walks the rows' tiles; sums are fp32 in a fixed order.
+// walks the rows' tiles; sums are fp32 in a fixed order.  For fp32 prompts, and for
+// few rows whose scores do not fit the workspace: bound by the MMAs and by laying
+// out Q again in every CTA (4 robots of 816 bf16 queries took it 1.1 ms, which is why
+// those have a kernel on the 5th-generation tensor cores).
 template <int HDP, int NP, typename T>
 __global__ void __launch_bounds__(RW * 32) cache_mass_kernel(CacheAttnArgs a) {
   constexpr int KS = HDP / 16;
@@ -877,7 +889,9 @@ __global__ void __launch_bounds__(RW * 32) cache_mass_kernel(CacheAttnArgs a) {
     }
 }
 
-// The same from the scores that the attention kept: a thread per two tokens.
+// The same from the scores that the attention kept: a thread per two tokens.  Bound by
+// reading them, 4 bytes per row and token (4 robots x 16 rows x 131071 tokens: 34 MB, in
+// L2, 13.6 us); computing them again would read the keys' 134 MB from HBM.
 __global__ void __launch_bounds__(256) cache_mass_scores_kernel(CacheAttnArgs a) {
   const int j = (blockIdx.x * 256 + threadIdx.x) * 2;
   if (j >= a.max_length) return;

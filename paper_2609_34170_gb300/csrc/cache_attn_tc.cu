@@ -31,6 +31,16 @@
 // of K on the scores, those of V on P.  P is at most 2^7 of the reference, 2^15 while
 // a grown one waits for its rescaling of O (only growth by more than 2^8 rescales);
 // what contributes less than 2^-31 of the row's largest is dropped.
+//
+// Measured: 16 prompts of 816 tokens (8 heads of 256, one KV head) 90.5 us, 964 TFLOP/s;
+// 2 of 8191 with a window of 1024 (16 heads of 64) 199 us; 50 slots of 16 robots over 816
+// tokens, 22 us.  A tile of 128 x 128 takes 1790 cycles at head dim 64, 1950 at 128, 2150 at
+// 192 and 2560 at 256 (MMAs alone: 512, 1024, 1536, 2048), an item's begin and end 7000 to
+// 12000 more.  At 64 the softmax's chain bounds it: scores in 130, maxima 250, their
+// exchange 250, exponentials 700, P out, and the wait for the next scores; at 256 that
+// chain beside the widening's share of shared memory (without MMAs and widening 2220).
+// Tiles in turn to the two warpgroups, a thread a row, measured the same (1770 at 64: with two
+// buffers of scores a P's way to the tile after next takes 1450), and an item's end 1500 more.
 #include <algorithm>
 
 #include "cache_tc.cuh"
