@@ -253,6 +253,14 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
     if (threadIdx.x == 0) raise_error(a.err, ERR_SHAPE);
     return;
   }
+  pdl_trigger();
+  if (lane == 0) {
+    for (int x = 0; x < D; ++x) mbar_init(&arrived[warp][x], 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (threadIdx.x < 16) fac[threadIdx.x] = 0.f;
+  pdl_wait();   // (the launch before may still write what is read from here on)
   Sight s;
   if (!robot_sight(a, b, s) && threadIdx.x == 0 && blockIdx.x == 0 && h == 0) raise_error(a.err, ERR_SHAPE);
   T* out0 = (T*)a.out + (size_t)((long long)b * a.out_robot) + (size_t)h * a.G * L.hd;
@@ -285,12 +293,6 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
       tma_load_2d_el(&maps.v, bar, to + Un::bytes + (uint32_t)(x * U * Un::IN), x * Un::IN, row, pol, 1u);
     }
   };
-  if (lane == 0) {
-    for (int x = 0; x < D; ++x) mbar_init(&arrived[warp][x], 1);
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  }
-  if (threadIdx.x < 16) fac[threadIdx.x] = 0.f;
   __syncthreads();
   // (Q's loads first: behind the first units of all CTAs, 29 MB, they took 5 us)
   stage_q<HDP, NP, T, RW * 32>(a, s, b, h, r0, frag, fac, [&]() {
@@ -805,6 +807,8 @@ __global__ void __launch_bounds__(RW * 32) cache_mass_kernel(CacheAttnArgs a) {
   const int g = lane >> 2, c = lane & 3;
   const CacheLayer& L = a.c;
   const size_t head = (size_t)b * L.Hkv + h;
+  pdl_trigger();
+  pdl_wait();
   Sight s;
   robot_sight(a, b, s);
   const int j0 = (blockIdx.x * RW + warp) * 16, jc0 = blockIdx.x * RW * 16, jc1 = jc0 + RW * 16;
@@ -894,6 +898,8 @@ __global__ void __launch_bounds__(RW * 32) cache_mass_kernel(CacheAttnArgs a) {
 // L2, 13.6 us); computing them again would read the keys' 134 MB from HBM.
 __global__ void __launch_bounds__(256) cache_mass_scores_kernel(CacheAttnArgs a) {
   const int j = (blockIdx.x * 256 + threadIdx.x) * 2;
+  pdl_trigger();
+  pdl_wait();
   if (j >= a.max_length) return;
   const int b = blockIdx.z;
   const size_t head = (size_t)b * a.c.Hkv + blockIdx.y;
@@ -952,6 +958,7 @@ cudaError_t launch_rows(CacheAttnArgs a, cudaStream_t st) {
   const bool keep = a.mass && (NP == 2 || a.n * a.G <= 16) &&
                     (double)a.batch * a.c.Hkv * a.n * a.G * a.mass_pitch * 4 <= (double)a.mass_ws_bytes;
   a.scores = keep ? a.mass_ws : nullptr;
+  const Overlap overlap;
   cudaError_t e;
   if (NP == 1 && a.n * a.G > 16) {
     e = launch_cache_attend_tc(a, st);
@@ -966,11 +973,9 @@ cudaError_t launch_rows(CacheAttnArgs a, cudaStream_t st) {
   if (e != cudaSuccess || !a.mass || a.max_length == 0) return e;
   if (NP == 1 && a.n * a.G > 16) return launch_cache_mass_tc(a, st);
   if (keep)
-    cache_mass_scores_kernel<<<dim3((a.max_length + 511) / 512, a.c.Hkv, a.batch), 256, 0, st>>>(a);
-  else
-    cache_mass_kernel<HDP, NP, T>
-        <<<dim3((a.max_length + RW * 16 - 1) / (RW * 16), a.c.Hkv, a.batch), RW * 32, frag_bytes<HDP, NP>(), st>>>(a);
-  return cudaGetLastError();
+    return launch_kernel(cache_mass_scores_kernel, dim3((a.max_length + 511) / 512, a.c.Hkv, a.batch), dim3(256), 0, st, 1, a);
+  return launch_kernel(cache_mass_kernel<HDP, NP, T>, dim3((a.max_length + RW * 16 - 1) / (RW * 16), a.c.Hkv, a.batch),
+                       dim3(RW * 32), frag_bytes<HDP, NP>(), st, 1, a);
 }
 
 template <int HDP>

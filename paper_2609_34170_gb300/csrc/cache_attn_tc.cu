@@ -185,6 +185,7 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const CacheLayer& L = a.c;
   const int items = a.row_tiles * a.splits * L.Hkv * a.batch;
+  pdl_wait();   // (before any TMEM is taken: the launch before may still need it)
   if (q0 & 1023u) {   // (the swizzled layouts count on it)
     if (threadIdx.x == 0) raise_error(a.err, ERR_SHAPE);
     return;
@@ -225,6 +226,7 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
   tc_fence_before();
   cta_sync();
   tc_fence_after();
+  pdl_trigger();
   const uint32_t tmem = *tmem_slot;
   constexpr uint32_t o_col = 2 * BT;
 
@@ -838,6 +840,7 @@ cudaError_t launch_nb(CacheAttnArgs a, cudaStream_t st) {
   a.by_pairs = LaunchDiv(a.group);
   a.by_last = LaunchDiv((int)std::max(1ll, pairs % a.group));
   const unsigned grid = a.splits == 1 ? (unsigned)std::min(tiles, (long long)a.num_sms) : (unsigned)(tiles * a.splits);
+  const Overlap overlap;
   return launch_kernel_cluster(cache_tc_kernel<NB>, dim3(grid), dim3(TCT), TcShape<NB>::bytes, st,
                                dim3(a.splits <= kTcCluster ? a.splits : 1, 1, 1), maps, a);
 }

@@ -63,6 +63,7 @@ __global__ void __launch_bounds__(MT, 1) cache_mass_tc_kernel(const __grid_const
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const CacheLayer& L = a.c;
   const int chunk = blockIdx.x % a.splits, head = blockIdx.x / a.splits, b = head / L.Hkv, h = head % L.Hkv;
+  pdl_wait();   // (before any TMEM is taken)
   Sight s;
   robot_sight(a, b, s);   // (the attention before has reported what is out of range)
   const int end_row = s.count * a.G;
@@ -99,6 +100,7 @@ __global__ void __launch_bounds__(MT, 1) cache_mass_tc_kernel(const __grid_const
   tc_fence_before();
   cta_sync();
   tc_fence_after();
+  pdl_trigger();
   const uint32_t tmem = *tmem_slot;
   // tiles of tokens that row tile rt sees, and the first token of its i-th
   auto sight_of = [&](int rt) {
@@ -271,6 +273,8 @@ __global__ void __launch_bounds__(256) cache_mass_sum_kernel(CacheAttnArgs a) {
   __shared__ float sums[8][32];
   const int lane = threadIdx.x & 31, eighth = threadIdx.x >> 5, j = blockIdx.x * 32 + lane;
   const size_t head = (size_t)blockIdx.z * a.c.Hkv + blockIdx.y;
+  pdl_trigger();
+  pdl_wait();
   const float* part = a.mass_ws + head * a.splits * 2 * a.mass_pitch + j;   // (j < pitch, a multiple of 32)
   float v = 0.f;
 #pragma unroll 8
@@ -289,8 +293,7 @@ __global__ void __launch_bounds__(256) cache_mass_sum_kernel(CacheAttnArgs a) {
 template <int NB>
 cudaError_t launch_nb(const MassMaps& maps, const CacheAttnArgs& a, cudaStream_t st) {
   const unsigned units = (unsigned)((long long)a.batch * a.c.Hkv * a.splits);
-  cache_mass_tc_kernel<NB><<<units, MT, MassShape<NB>::bytes, st>>>(maps, a);
-  return cudaGetLastError();
+  return launch_kernel(cache_mass_tc_kernel<NB>, dim3(units), dim3(MT), MassShape<NB>::bytes, st, 1, maps, a);
 }
 
 template <int NB>
@@ -309,6 +312,7 @@ cudaError_t launch_cache_mass_tc(CacheAttnArgs a, cudaStream_t st) {
   chunks = std::min(chunks, std::max(1ll, (long long)(a.mass_ws_bytes / (8ull * a.mass_pitch)) / heads));
   a.splits = (int)std::min(chunks, (long long)a.row_tiles);
   const MassMaps maps{a.maps->k_tc};
+  const Overlap overlap;
   cudaError_t e;
   switch (a.c.hdp) {
     case 64: e = launch_nb<1>(maps, a, st); break;
@@ -317,8 +321,7 @@ cudaError_t launch_cache_mass_tc(CacheAttnArgs a, cudaStream_t st) {
     default: e = launch_nb<4>(maps, a, st); break;
   }
   if (e != cudaSuccess) return e;
-  cache_mass_sum_kernel<<<dim3((a.max_length + 31) / 32, a.c.Hkv, a.batch), 256, 0, st>>>(a);
-  return cudaGetLastError();
+  return launch_kernel(cache_mass_sum_kernel, dim3((a.max_length + 31) / 32, a.c.Hkv, a.batch), dim3(256), 0, st, 1, a);
 }
 
 size_t cache_mass_ws_bytes(int heads, int T, int num_sms) {

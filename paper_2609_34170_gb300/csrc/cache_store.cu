@@ -79,6 +79,8 @@ __device__ __forceinline__ void store_block(BlockShared& s, float* kx, float* vx
 template <typename T>
 __global__ void __launch_bounds__(256) cache_append_kernel(AppendArgs a) {
   __shared__ BlockShared s;
+  pdl_trigger();
+  pdl_wait();
   const CacheLayer& c = a.c;
   const int b = blockIdx.z, h = blockIdx.y;
   const int start = a.starts ? a.starts[b] : 0, count = a.counts ? a.counts[b] : a.n;
@@ -133,6 +135,8 @@ __global__ void __launch_bounds__(256) cache_read_kernel(ReadArgs a) {
   const int b = blockIdx.z, h = blockIdx.y;
   const int tpt = c.hdp / 16;
   const long long idx = (long long)blockIdx.x * 256 + threadIdx.x;
+  pdl_trigger();
+  pdl_wait();
   const int i = (int)(idx / tpt), d = (int)(idx % tpt) * 16;
   if (i >= a.n || d >= c.hd) return;
   const int first = a.firsts ? a.firsts[b] : 0;
@@ -192,6 +196,8 @@ __global__ void __launch_bounds__(kSelThreads) cache_select_kernel(EvictArgs a, 
   __shared__ unsigned kept_here[2], before_here[2];   // surely in, ties: of this CTA's run, of the runs before it
   const int h = blockIdx.x / ctas, rank = blockIdx.x % ctas, b = blockIdx.y, Hkv = a.from.Hkv;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  pdl_trigger();
+  pdl_wait();
   int len = a.lengths[b];
   if (len < 0 || len > a.max_tokens || len > a.mass_stride) {
     if (tid == 0 && blockIdx.x == 0) raise_error(a.err, ERR_SHAPE);
@@ -369,6 +375,8 @@ __global__ void __launch_bounds__(256) cache_move_kernel(EvictArgs a) {
   __shared__ BlockShared s;
   const CacheLayer &from = a.from, &to = a.to;
   const int b = blockIdx.z, h = blockIdx.y;
+  pdl_trigger();
+  pdl_wait();
   const int kept = a.new_lengths[b];
   if ((int)blockIdx.x * kCacheBlock >= kept) return;
   const int tpt = to.hdp / 16;
@@ -393,27 +401,25 @@ __global__ void __launch_bounds__(256) cache_move_kernel(EvictArgs a) {
 cudaError_t launch_cache_append(const AppendArgs& a, Dtype dt, cudaStream_t st) {
   // a start inside a block needs one block more
   const dim3 grid((a.n + 2 * kCacheBlock - 2) / kCacheBlock, a.c.Hkv, a.batch);
-  if (dt == DT_BF16) cache_append_kernel<bf16><<<grid, a.c.hdp, 0, st>>>(a);
-  else cache_append_kernel<float><<<grid, a.c.hdp, 0, st>>>(a);
-  return cudaGetLastError();
+  const Overlap overlap;
+  return launch_kernel(dt == DT_BF16 ? cache_append_kernel<bf16> : cache_append_kernel<float>, grid, dim3(a.c.hdp), 0, st, 1, a);
 }
 
 cudaError_t launch_cache_read(const ReadArgs& a, Dtype dt, cudaStream_t st) {
   const dim3 grid((unsigned)(((long long)a.n * (a.c.hdp / 16) + 255) / 256), a.c.Hkv, a.batch);
-  if (dt == DT_BF16) cache_read_kernel<bf16><<<grid, 256, 0, st>>>(a);
-  else cache_read_kernel<float><<<grid, 256, 0, st>>>(a);
-  return cudaGetLastError();
+  const Overlap overlap;
+  return launch_kernel(dt == DT_BF16 ? cache_read_kernel<bf16> : cache_read_kernel<float>, grid, dim3(256), 0, st, 1, a);
 }
 
 cudaError_t launch_cache_evict(const EvictArgs& a, cudaStream_t st) {
   // a CTA per 4096 tokens, up to a cluster of 8 (at 816 tokens a cluster's barriers take longer than they save)
   const int ctas = (int)std::min((long long)kSelCluster, std::max(1ll, std::min((long long)a.max_tokens, a.mass_stride) / 4096));
+  const Overlap overlap;
   cudaError_t e = launch_kernel_cluster(cache_select_kernel, dim3(a.from.Hkv * ctas, a.batch), dim3(kSelThreads), 0, st,
                                         dim3(ctas, 1, 1), a, ctas);
   if (e != cudaSuccess) return e;
   const dim3 grid((a.keep + kCacheBlock - 1) / kCacheBlock, a.to.Hkv, a.batch);
-  cache_move_kernel<<<grid, a.to.hdp, 0, st>>>(a);
-  return cudaGetLastError();
+  return launch_kernel(cache_move_kernel, grid, dim3(a.to.hdp), 0, st, 1, a);
 }
 
 }  // namespace ravel

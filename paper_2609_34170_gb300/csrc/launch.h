@@ -15,6 +15,13 @@ inline bool& pdl_enabled() {
   return on;
 }
 
+// The launches of a scope may overlap their predecessors.
+struct Overlap {
+  const bool was = pdl_enabled();
+  Overlap() { pdl_enabled() = true; }
+  ~Overlap() { pdl_enabled() = was; }
+};
+
 template <typename... KArgs, typename... Args>
 cudaError_t launch_kernel_cluster(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st,
                                   dim3 cluster, Args&&... args) {
