@@ -8,7 +8,7 @@
 //                    of K as they are, Q in two e4m3 pieces
 //   P = 2^(S - m)    softmax warps: TMEM -> registers -> f16 P over S in TMEM
 //   O += P V         tcgen05.mma kind::f16, M = 128, N = head dim, 16 tokens at a time
-// Warp roles (640 threads): warps 0-7 softmax and output, two threads per row; warps
+// Warp roles (640 threads): warps 0-7 softmax and output (see TcShape::own); warps
 // 8-11 lay out the next item's Q, warps 12-15 widen V; warp 16 TMEM and MMAs; warps 17, 18 load the
 // codes of K and V (19 idle, so that registers move between whole warpgroups).
 // Every role walks the items on its own, so that one item's output lies beside the
@@ -33,14 +33,13 @@
 // what contributes less than 2^-31 of the row's largest is dropped.
 //
 // Measured: 16 prompts of 816 tokens (8 heads of 256, one KV head) 90.5 us, 964 TFLOP/s;
-// 2 of 8191 with a window of 1024 (16 heads of 64) 199 us; 50 slots of 16 robots over 816
-// tokens, 22 us.  A tile of 128 x 128 takes 1790 cycles at head dim 64, 1950 at 128, 2150 at
-// 192 and 2560 at 256 (MMAs alone: 512, 1024, 1536, 2048), an item's begin and end 7000 to
-// 12000 more.  At 64 the softmax's chain bounds it: scores in 130, maxima 250, their
-// exchange 250, exponentials 700, P out, and the wait for the next scores; at 256 that
-// chain beside the widening's share of shared memory (without MMAs and widening 2220).
-// Tiles in turn to the two warpgroups, a thread a row, measured the same (1770 at 64: with two
-// buffers of scores a P's way to the tile after next takes 1450), and an item's end 1500 more.
+// 2 of 8191 with a window of 1024 (16 heads of 64) 202 us, without the window 424; 50 slots of
+// 16 robots over 816 tokens, 20 us.  A tile of 128 x 128 takes 1570 cycles at head dim 64, 1940
+// at 128, 2190 at 192 and 2550 at 256 (MMAs alone: 512, 1024, 1536, 2048), an item's begin and
+// end 7500 to 12000 more.  Up to 128 the softmax bounds it; of a tile that two threads a row
+// share, one after the other: scores in 130, maxima 250, their exchange 250, exponentials 700,
+// P out, the wait for the next scores; at 256 that chain beside the widening's share of
+// shared memory (without MMAs and widening 2220).
 #include <algorithm>
 
 #include "cache_tc.cuh"
@@ -65,11 +64,24 @@ template <int NB> struct TcShape {
   // another's load into it is still on its way would take the phase before for it.)
   static constexpr int CV = 8;
   static_assert(CV % 4 == 0, "widening warps");
+  // (a half's slot is waited for by whichever warp comes to it: one that has codes for it knows
+  // that the slot's half before has begun, which was past that wait)
+  static_assert(CV <= VS * NB, "widening ahead");
   static constexpr uint32_t q_bytes = 2 * NB * QB;
   static constexpr uint32_t ring = KS * KU + VS * NB * VB + CV * CB;
+  // Up to head dim 64 TMEM holds three tiles of scores and two outputs: each softmax
+  // warpgroup takes every second tile, a thread a row, with references and an output of its
+  // own, joined at the item's end, so that one's waits lie beside the other's work: 1570
+  // cycles a tile instead of 1780 (2 causal prompts of 8191: 424 us instead of 479; with a
+  // window of 1024, of whose ten tiles three are masked, twice then, no difference).  Beyond,
+  // both share a tile, two threads to a row: with the two buffers of scores that fit at 128,
+  // a P's way to the scores of the tile after next, 1450 cycles, ate the gain.
+  static constexpr bool own = NB == 1;
+  static constexpr int SB = own ? 3 : 2;   // buffers of scores
   // places for the halves' maxima: in turn where there is room, which saves a barrier a tile
   static constexpr int XM = NB == 4 ? 1 : 2;
-  static constexpr uint32_t bytes = q_bytes + ring + 1024 + XM * 2048;
+  static constexpr uint32_t bars = own ? 640 : 512;   // bytes of barriers and flags
+  static constexpr uint32_t bytes = q_bytes + ring + bars + 512 + XM * 2048;
   static_assert(bytes <= 227 * 1024, "shared memory");
   // a row of the fp32 output that splits exchange (over the rings): 16 bytes more than
   // the dims, so that rows written by neighbouring lanes fall on different banks
@@ -153,7 +165,7 @@ __device__ __forceinline__ Item item_of(const CacheAttnArgs& a, int w) {
 template <int NB>
 __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant__ TcMaps maps, CacheAttnArgs a) {
   using Shape = TcShape<NB>;
-  constexpr int HDP = 64 * NB, KS = Shape::KS, VS = Shape::VS, CV = Shape::CV;
+  constexpr int HDP = 64 * NB, KS = Shape::KS, VS = Shape::VS, CV = Shape::CV, SB = Shape::SB;
   constexpr uint32_t VH = NB * VB;   // bytes of a V half
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t q0 = smem_u32(smem), k0 = q0 + Shape::q_bytes, v0 = k0 + KS * KU, cv0 = v0 + VS * VH;
@@ -164,10 +176,10 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
   uint64_t* v_empty = v_full + VS;
   uint64_t* cv_full = v_empty + VS;
   uint64_t* cv_empty = cv_full + CV;
-  uint64_t* s_full = cv_empty + CV;   // [2]
-  uint64_t* p_full = s_full + 2;      // [2]
-  uint64_t* pv_done = p_full + 2;     // [2]
-  uint64_t* q_full = pv_done + 2;     // an item's Q is laid out ...
+  uint64_t* s_full = cv_empty + CV;   // [SB]
+  uint64_t* p_full = s_full + SB;     // [SB]
+  uint64_t* pv_done = p_full + SB;    // [SB]
+  uint64_t* q_full = pv_done + SB;    // an item's Q is laid out ...
   uint64_t* q_empty = q_full + 1;     // ... and its last S has completed
   uint64_t* o_free = q_empty + 1;     // an item's output has been read
   uint64_t* q_laid = o_free + 1;      // an item's Q is laid out in L2
@@ -178,9 +190,9 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
   int* issued_flag = last_flag + 1;               // [3] loads of K, V and Q issued
   // exponent bits of the rows' largest |q|, [4][128], by item: S runs up to two tiles, so up
   // to two items, ahead of the softmax, and Q one more
-  uint8_t* row_exp = tail + 512;
+  uint8_t* row_exp = tail + Shape::bars;
   float2* xm = (float2*)(row_exp + 512);   // [XM][2][128] row maxima, then sums, of the two halves
-  static_assert((2 * KS + 2 * VS + 2 * CV + 11) * 8 + 24 <= 512, "barriers");
+  static_assert((2 * KS + 2 * VS + 2 * CV + 3 * SB + 5) * 8 + 24 <= Shape::bars, "barriers");
 
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const CacheLayer& L = a.c;
@@ -203,10 +215,10 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
       mbar_init(&cv_full[i], 1);
       mbar_init(&cv_empty[i], 1);
     }
-    for (int i = 0; i < 2; ++i) {
-      issued_flag[i] = 0;
+    issued_flag[0] = issued_flag[1] = 0;
+    for (int i = 0; i < SB; ++i) {
       mbar_init(&s_full[i], 1);
-      mbar_init(&p_full[i], 256);
+      mbar_init(&p_full[i], Shape::own ? 128 : 256);
       mbar_init(&pv_done[i], 1);
     }
     mbar_init(q_full, 1);
@@ -228,7 +240,8 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
   tc_fence_after();
   pdl_trigger();
   const uint32_t tmem = *tmem_slot;
-  constexpr uint32_t o_col = 2 * BT;
+  constexpr uint32_t o_col = SB * BT;
+  static_assert(o_col + (Shape::own ? 2 : 1) * HDP <= 512, "TMEM");
 
   auto stage = [&](const Item& it, int rb, int qi, uint8_t* to) {
     stage_q8<NB>(a, it.s, it.b, it.h, it.tile * BM, rb, q0, to, [&](int lr, int e) { row_exp[(qi & 3) * BM + lr] = (uint8_t)e; });
@@ -338,8 +351,8 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
       int sn = 0, pn = 0, last = 0;                   // tiles of S's and P V's items
       int si = 0, pi = 0, sq = 0, pq = 0;             // tiles done of them; items begun
       int gs = 0, gp = 0;                             // tiles in all
-      int sk = 0, sv = 0;
-      uint32_t phk = 0, phv = 0;
+      int sk = 0, sv = 0, bs = 0, bp = 0;             // slots; buffers of scores
+      uint32_t phk = 0, phv = 0, php = 0;
       bool ok = true;
       asm volatile("bar.sync 6, 544;" ::: "memory");
       look();
@@ -348,7 +361,7 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
       sn = pn = ahead >> 4;
       last = ahead & 15;
       while (pn > 0) {
-        while (sn > 0 && gs <= gp + 1) {
+        while (sn > 0 && gs < gp + SB) {
           if (si == 0) {
             // an item's last P V goes first: its output is what the softmax does next
             if (gs > gp) break;
@@ -364,7 +377,7 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
           }
           if (!ok) break;
           tc_fence_after();
-          const uint32_t sd = tmem + (uint32_t)(gs & 1) * BT;
+          const uint32_t sd = tmem + (uint32_t)bs * BT;
           uint64_t ad = qd0;
 #pragma unroll 1
           for (int blk = 0; blk < NB; ++blk, ad += QB >> 4) {
@@ -378,8 +391,9 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
               phk ^= 1u;
             }
           }
-          umma_commit(&s_full[gs & 1], el);
+          umma_commit(&s_full[bs], el);
           ++gs;
+          if (++bs == SB) bs = 0;
           if (++si == sn) {
             umma_commit(q_empty, el);
             si = 0;
@@ -391,12 +405,12 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
           }
         }
         if (!looked && pi == 0) look();   // (the softmax is at the output of the item before)
-        const uint32_t pa = tmem + (uint32_t)(gp & 1) * BT;
+        const uint32_t pa = tmem + (uint32_t)bp * BT, od = tmem + o_col + (Shape::own ? (uint32_t)(gp & 1) * HDP : 0u);
         const int groups = pi + 1 < pn ? BT / 16 : last;
         if (ok) {   // P, the first half of V (both, where several tiles' lie in the ring), a free O
           const bool two = NB <= 2 && groups > 4, first = pi == 0 && pq > 0;
           const int s = two ? (sv + 1 < VS ? sv + 1 : 0) : sv;
-          ok = wait_phases(&p_full[gp & 1], (uint32_t)(gp >> 1) & 1u, &v_full[sv], phv, &v_full[s], s < sv ? phv ^ 1u : phv,
+          ok = wait_phases(&p_full[bp], php, &v_full[sv], phv, &v_full[s], s < sv ? phv ^ 1u : phv,
                            first ? o_free : &v_full[sv], first ? (uint32_t)(pq - 1) & 1u : phv);
         }
         if (!ok) break;
@@ -409,14 +423,14 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
             tc_fence_after();
           }
           const uint64_t bd = vd0 + (uint32_t)sv * (VH >> 4);
-          const uint32_t ph = pa + 32 * hv, more = pi + hv > 0 ? 1u : 0u;
+          const uint32_t ph = pa + 32 * hv, more = hv > 0 || pi > (Shape::own ? 1 : 0) ? 1u : 0u;
           if (groups >= 4 * hv + 4) {   // (a comparison and a branch per MMA take longer than the MMA)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) umma_bf16_ts(tmem + o_col, ph + 8 * k, bd + 128 * k, idesc_o, k > 0 ? 1u : more, el);
+            for (int k = 0; k < 4; ++k) umma_bf16_ts(od, ph + 8 * k, bd + 128 * k, idesc_o, k > 0 ? 1u : more, el);
           } else {
 #pragma unroll
             for (int k = 0; k < 3; ++k)
-              if (4 * hv + k < groups) umma_bf16_ts(tmem + o_col, ph + 8 * k, bd + 128 * k, idesc_o, k > 0 ? 1u : more, el);
+              if (4 * hv + k < groups) umma_bf16_ts(od, ph + 8 * k, bd + 128 * k, idesc_o, k > 0 ? 1u : more, el);
           }
           umma_commit(&v_empty[sv], el);
           if (++sv == VS) {
@@ -425,8 +439,12 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
           }
         }
         if (!ok) break;
-        umma_commit(&pv_done[gp & 1], el);
+        umma_commit(&pv_done[bp], el);
         ++gp;
+        if (++bp == SB) {
+          bp = 0;
+          php ^= 1u;
+        }
         if (++pi == pn) {
           pi = 0;
           ++pq;
@@ -582,77 +600,155 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
           tmem_st16u(to + 16 * h2, wd);
         }
       };
-      // new references; where W rises by much, O, which holds P V of every earlier tile once the
-      // last one's has completed, is rescaled
-      auto refer = [&](float mx, float wx, bool any, float& mu, float& wu) {
+      // new references; where W rises by much, O, which holds P V of the earlier tiles (or every
+      // second one) once that of tile g has completed, is rescaled
+      auto refer = [&](float mx, float wx, bool any, int g, float& mu, float& wu) {
         const float mn = fmaxf(m, ceilf(mx)), wn = fmaxf(W, ceilf(wx));
         mu = mn == -INFINITY ? 0.f : mn;
         l *= pow2f_down(m - mu);
         m = mn;
         const bool need = wn > W + 8.f;
         if (any && __any_sync(0xffffffffu, need)) {
-          if (ok) ok = wait_phase(&pv_done[(gt - 1) & 1], (uint32_t)((gt - 1) >> 1) & 1u);
+          if (ok) ok = wait_phase(&pv_done[g % SB], (uint32_t)(g / SB) & 1u);
           tc_fence_after();
           const float alpha = need ? pow2f_down(W - wn) : 1.f;
+          constexpr int NC = Shape::own ? 64 : 16;   // columns at a time (a shared tile's scores are held meanwhile)
 #pragma unroll 1
-          for (int cb = 16 * hf; cb < HDP; cb += 32) {
-            float o[16];
-            tmem_ld16(lane_base + o_col + cb, o);
+          for (int cb = Shape::own ? hf * HDP : 16 * hf; cb < (Shape::own ? (hf + 1) * HDP : HDP); cb += Shape::own ? NC : 32) {
+            uint32_t o[NC];
 #pragma unroll
-            for (int q = 0; q < 16; ++q) o[q] *= alpha;
-            tmem_st16(lane_base + o_col + cb, o);
+            for (int q = 0; q < NC; q += 16) tmem_ld16_async(lane_base + o_col + cb + q, o + q);
+            tmem_wait_ld();
+#pragma unroll
+            for (int q = 0; q < NC; q += 16) {
+              tmem_reg_fence16(o + q);
+#pragma unroll
+              for (int x = 0; x < 16; ++x) o[q + x] = __float_as_uint(__uint_as_float(o[q + x]) * alpha);
+              tmem_st16u(lane_base + o_col + cb + q, o + q);
+            }
           }
           tmem_wait_st();
         }
         if (need) W = wn;
         wu = W == -INFINITY ? 0.f : W;
       };
-      for (int i = 0; i < n; ++i, ++gt) {
-        const int j0 = it.token(i);
-        // exponents of this half's four blocks
-        const uint32_t kes = *(const uint32_t*)(KE + j0 / 16 + 4 * hf), ves = *(const uint32_t*)(VE + j0 / 16 + 4 * hf);
-        const bool full = j0 + BT <= firstm.hi && (j0 >= lastm.lo || j0 + BT <= a.sinks);
-        if (ok) ok = wait_phase(&s_full[gt & 1], (uint32_t)(gt >> 1) & 1u);
-        tc_fence_after();
-        if (i == 0) rf = q_factor(row_exp[(qi & 3) * BM + r], a.scale_log2);   // (S needed Q: it is there)
-        const uint32_t srow = lane_base + (uint32_t)(gt & 1) * BT;
-        float sc[64], mx = -INFINITY, wx = -INFINITY, mu, wu;
-        scores(srow + 64 * hf, j0 + 64 * hf, full, sc);
-        maxima(sc, kes, ves, mx, wx);
-        // (past the barrier both halves have read their scores, past a second or the next tile's
-        // the maxima)
-        float2* xt = xm + (Shape::XM > 1 ? (gt & 1) * 256 : 0);
-        xt[hf * 128 + r] = make_float2(mx, wx);
-        pair_bar();
-        const float2 x0 = xt[r], x1 = xt[128 + r];
-        if (Shape::XM == 1) pair_bar();
-        refer(fmaxf(x0.x, x1.x), fmaxf(x0.y, x1.y), i > 0, mu, wu);
-        weights(sc, kes, ves, mu, wu, srow + 32 * hf);
-        tmem_wait_st();
-        tc_fence_before();
-        mbar_arrive(&p_full[gt & 1]);
+      if constexpr (Shape::own) {
+        const int i0 = (gt ^ hf) & 1;   // this warpgroup's first tile
+#pragma unroll 1
+        for (int i = i0; i < n; i += 2) {
+          const int j0 = it.token(i), g = gt + i, bs = g % SB;
+          const uint2 ke = *(const uint2*)(KE + j0 / 16), ve = *(const uint2*)(VE + j0 / 16);   // exponents of its blocks
+          const bool full = j0 + BT <= firstm.hi && (j0 >= lastm.lo || j0 + BT <= a.sinks);
+          if (ok) ok = wait_phase(&s_full[bs], (uint32_t)(g / SB) & 1u);
+          tc_fence_after();
+          if (i == i0) rf = q_factor(row_exp[(qi & 3) * BM + r], a.scale_log2);   // (S needed Q: it is there)
+          const uint32_t srow = lane_base + (uint32_t)bs * BT;
+          float mx = -INFINITY, wx = -INFINITY, mu, wu;
+#pragma unroll 1
+          for (int c = 0; c < BT; c += 64) {
+            float sc[64];
+            scores(srow + c, j0 + c, full, sc);
+            maxima(sc, c ? ke.y : ke.x, c ? ve.y : ve.x, mx, wx);
+          }
+          refer(mx, wx, i >= 2, g - 2, mu, wu);
+          // (P goes over scores that have been read again by then)
+#pragma unroll 1
+          for (int c = 0; c < BT; c += 64) {
+            float sc[64];
+            scores(srow + c, j0 + c, full, sc);
+            weights(sc, c ? ke.y : ke.x, c ? ve.y : ve.x, mu, wu, srow + c / 2);
+          }
+          tmem_wait_st();
+          tc_fence_before();
+          mbar_arrive(&p_full[bs]);
+        }
+        gt += n;
+      } else {
+        for (int i = 0; i < n; ++i, ++gt) {
+          const int j0 = it.token(i);
+          // exponents of this half's four blocks
+          const uint32_t kes = *(const uint32_t*)(KE + j0 / 16 + 4 * hf), ves = *(const uint32_t*)(VE + j0 / 16 + 4 * hf);
+          const bool full = j0 + BT <= firstm.hi && (j0 >= lastm.lo || j0 + BT <= a.sinks);
+          if (ok) ok = wait_phase(&s_full[gt & 1], (uint32_t)(gt >> 1) & 1u);
+          tc_fence_after();
+          if (i == 0) rf = q_factor(row_exp[(qi & 3) * BM + r], a.scale_log2);   // (S needed Q: it is there)
+          const uint32_t srow = lane_base + (uint32_t)(gt & 1) * BT;
+          float sc[64], mx = -INFINITY, wx = -INFINITY, mu, wu;
+          scores(srow + 64 * hf, j0 + 64 * hf, full, sc);
+          maxima(sc, kes, ves, mx, wx);
+          // (past the barrier both halves have read their scores, past a second or the next tile's
+          // the maxima)
+          float2* xt = xm + (Shape::XM > 1 ? (gt & 1) * 256 : 0);
+          xt[hf * 128 + r] = make_float2(mx, wx);
+          pair_bar();
+          const float2 x0 = xt[r], x1 = xt[128 + r];
+          if (Shape::XM == 1) pair_bar();
+          refer(fmaxf(x0.x, x1.x), fmaxf(x0.y, x1.y), i > 0, gt - 1, mu, wu);
+          weights(sc, kes, ves, mu, wu, srow + 32 * hf);
+          tmem_wait_st();
+          tc_fence_before();
+          mbar_arrive(&p_full[gt & 1]);
+        }
       }
       if (n > 0) ++qi;
       coming = item_of(a, after);
       if (ok && n > 0) {
-        ok = wait_phase(&pv_done[(gt - 1) & 1], (uint32_t)((gt - 1) >> 1) & 1u);
+        ok = wait_phase(&pv_done[(gt - 1) % SB], (uint32_t)((gt - 1) / SB) & 1u);
         tc_fence_after();
       }
-      pair_bar();   // (the last tile's maxima are read)
-      xm[hf * 128 + r].x = l;
-      pair_bar();
-      l = xm[r].x + xm[128 + r].x;
+      float of[2] = {1.f, 0.f};   // what the warpgroups' outputs are scaled by
+      if constexpr (Shape::own) {
+        float* xw = (float*)(xm + 256);
+        xm[hf * 128 + r] = make_float2(m, l);
+        xw[hf * 128 + r] = W;
+        pair_bar();
+        const float2 x0 = xm[r], x1 = xm[128 + r];
+        const float w0 = xw[r], w1 = xw[128 + r];
+        m = fmaxf(x0.x, x1.x);
+        W = fmaxf(w0, w1);
+        const float mu = m == -INFINITY ? 0.f : m, wu = W == -INFINITY ? 0.f : W;
+        // (exact steps of powers of two, as between a row's references)
+        l = fmaf(x0.y, pow2f_down(x0.x - mu), x1.y * pow2f_down(x1.x - mu));
+        of[0] = pow2f_down(w0 - wu);
+        of[1] = pow2f_down(w1 - wu);
+      } else {
+        pair_bar();   // (the last tile's maxima are read)
+        xm[hf * 128 + r].x = l;
+        pair_bar();
+        l = xm[r].x + xm[128 + r].x;
+      }
       pair_bar();
       const bool real = mk.hi > 0 && n > 0 && !(l <= 0.f);   // (a sum that is not a number stays one)
       const float inv = real ? pow2f(W - m) / l : 0.f;
       // 32 of the row's outputs, normalised
       auto output = [&](int cb, uint32_t (&raw)[32]) {
-        tmem_ld32_async(lane_base + o_col + cb, raw);
-        tmem_wait_ld();
-        tmem_reg_fence16(raw);
-        tmem_reg_fence16(raw + 16);
+        if constexpr (!Shape::own) {
+          tmem_ld32_async(lane_base + o_col + cb, raw);
+          tmem_wait_ld();
+          tmem_reg_fence16(raw);
+          tmem_reg_fence16(raw + 16);
 #pragma unroll
-        for (int q = 0; q < 32; ++q) raw[q] = real ? __float_as_uint(__uint_as_float(raw[q]) * inv) : 0u;
+          for (int q = 0; q < 32; ++q) raw[q] = real ? __float_as_uint(__uint_as_float(raw[q]) * inv) : 0u;
+        } else {
+          // (of a single tile, one output has nothing of this item)
+          const int only = n == 1 ? (gt - 1) & 1 : 0;
+          const float f0 = n > 1 ? of[0] * inv : inv, f1 = of[1] * inv;
+#pragma unroll
+          for (int q16 = 0; q16 < 32; q16 += 16) {
+            uint32_t* x = raw + q16;
+            uint32_t y[16] = {};
+            tmem_ld16_async(lane_base + o_col + only * HDP + cb + q16, x);
+            if (n > 1) tmem_ld16_async(lane_base + o_col + HDP + cb + q16, y);
+            tmem_wait_ld();
+            tmem_reg_fence16(x);
+            tmem_reg_fence16(y);
+#pragma unroll
+            for (int q = 0; q < 16; ++q) {
+              const float z = __uint_as_float(x[q]) * f0;
+              x[q] = real ? __float_as_uint(n > 1 ? fmaf(__uint_as_float(y[q]), f1, z) : z) : 0u;
+            }
+          }
+        }
       };
       const float m_out = real ? m : -INFINITY, l_out = real ? l : 0.f;
       if (a.splits == 1) {
