@@ -58,7 +58,11 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint4& a, uint32_t 
 // over a long chain that adds up, so that each pair of pieces starts from zero.
 __device__ __forceinline__ void add4(float (&d)[4], const float (&x)[4]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) d[i] += x[i];
+  for (int i = 0; i < 4; i += 2) {
+    const float2 y = add2(make_float2(d[i], d[i + 1]), make_float2(x[i], x[i + 1]));
+    d[i] = y.x;
+    d[i + 1] = y.y;
+  }
 }
 
 __device__ __forceinline__ uint32_t word(const uint4& x, int i) { return i == 0 ? x.x : (i == 1 ? x.y : (i == 2 ? x.z : x.w)); }
