@@ -356,6 +356,68 @@ def test_eviction_from_long_caches():
     np.testing.assert_array_equal(_np(k), held.k[:, :, :keep])
 
 
+def _chain(cache, small, x, lengths, n):
+    """Append, attend with the mass, evict and read back, none of them waited for."""
+    cache.append(0, x["k"], x["v"])
+    out = cache.attend(0, x["q"], lengths, mass=x["mass"])
+    kept, index, mass = cache.evict(0, small, 0, lengths, x["mass"], 50, sinks=2, recent=5)
+    return (out, x["mass"]) + (kept, index, mass) + small.read(0, x["k"].shape[0], 50, lengths=kept)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("layout,n", [((8, 1, 256), 1), ((8, 1, 256), 40), ((16, 4, 64), 70)])
+def test_chained_calls_wait_for_each_other(layout, n, dtype):
+    # launches may start before the ones before them have ended: what one writes the next reads
+    from paper_2609_34170_gb300 import ContextCache
+    hq, hkv, hd = layout
+    batch, tokens = 5, 300
+    lengths = _ints([300, 200, 120, 299, 250])
+    xs = []
+    for i in range(6):
+        xs.append({"k": _rand((batch, tokens, hkv, hd), 50 + i, dtype), "v": _rand((batch, tokens, hkv, hd), 60 + i, dtype),
+                   "q": _rand((batch, n, hq, hd), 70 + i, dtype, 2.0), "mass": torch.zeros((batch, hkv, tokens), device="cuda")})
+    cache, small = ContextCache(1, hq, hkv, hd, tokens, batch, n, dtype), ContextCache(1, hq, hkv, hd, 64, batch, 1, dtype)
+    want = []
+    for x in xs:
+        got = _chain(cache, small, x, lengths, n)
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in got])
+    for x in xs:
+        x["mass"].fill_(-1.0)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = [_chain(cache, small, x, lengths, n) for x in xs]
+        for a, b in zip(got, want):
+            for t, w in zip(a, b):
+                assert torch.equal(t, w)
+
+
+@pytest.mark.parametrize("n", [1, 40])
+def test_calls_replay_from_a_graph(n):
+    from paper_2609_34170_gb300 import ContextCache
+    batch, tokens = 3, 200
+    cache, small = ContextCache(1, 8, 1, 256, tokens, batch, n), ContextCache(1, 8, 1, 256, 64, batch, 1)
+    lengths = _ints([200, 77, 150])
+    x = {"k": _rand((batch, tokens, 1, 256), 80, "bf16"), "v": _rand((batch, tokens, 1, 256), 81, "bf16"),
+         "q": _rand((batch, n, 8, 256), 82, "bf16", 2.0), "mass": torch.zeros((batch, 1, tokens), device="cuda")}
+    _chain(cache, small, x, lengths, n)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = _chain(cache, small, x, lengths, n)
+    for seed in (83, 93):
+        for i, name in enumerate(("k", "v", "q")):
+            x[name].copy_(_rand(x[name].shape, seed + i, "bf16"))
+        lengths.copy_(_ints([seed, 200, 60]))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in held]
+        want = _chain(cache, small, x, lengths, n)
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+
+
 def test_refusals():
     from paper_2609_34170_gb300 import ContextCache, RavelError
     p = Pair((4, 2, 64), "bf16", 64, 2, queries=4, lengths=[30, 20])
