@@ -217,6 +217,9 @@ struct ValueUnit {
 template <int HDP, int NP, int RT>
 struct RowsShape {
   static constexpr int frag = NP * (HDP / 16) * 512;   // bytes of Q's fragments
+  // bf16's few rows hold Q in registers: its place then takes what the splits send each other
+  static constexpr bool send = RT == 8 && NP == 1;
+  static constexpr int pad = send ? 128 : 0;           // (their shares are rounded up)
   // units in flight per warp, K and V (24 KB; fp32's take 16: its fragments are twice as many)
   static constexpr int D = NP == 2 ? 2 : 3;
   static constexpr int ring = RW * D * 2 * (int)Unit<HDP>::bytes;
@@ -226,7 +229,8 @@ struct RowsShape {
                                     : (HDP == 64 ? 72 : (HDP == 128 ? 144 : (HDP == 192 ? 240 : 304)));
   static __device__ __forceinline__ int pos(int row, int d) { return row * JS + d + (d >> 5) * 4; }
   static constexpr int join = RW * RT * JS * 4 + RT * HDP * 4;   // and their sum
-  static constexpr int bytes = frag + (ring > join ? ring : join);
+  static constexpr int bytes = frag + pad + (ring > join ? ring : join);
+  static_assert(!send || frag + pad >= RT * HDP * 4 + 7 * 16, "what the splits send");
 };
 
 struct RowsMaps {
@@ -241,12 +245,13 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
   extern __shared__ __align__(1024) uint8_t smem[];
   float* joint = (float*)smem;                          // [RW][RT][JS] outputs of the warps, over the ring
   float* mine = joint + RW * RT * Shape::JS;            // [RT][HDP] their sum
-  uint32_t* frag = (uint32_t*)(smem + Shape::bytes - Shape::frag);   // [NP][KS][32][4]
+  uint32_t* frag = (uint32_t*)(smem + Shape::bytes - Shape::pad - Shape::frag);   // [NP][KS][32][4]
   __shared__ float fac[16];
   __shared__ float2 warp_ml[RW][16], split_w[16];
   __shared__ unsigned last;
   __shared__ uint64_t arrived[RW][D];
   __shared__ float split_wt[8][16];
+  __shared__ float2 split_in[Shape::send ? 8 : 1][8];   // the splits' (max, sum)
 
   const int b = blockIdx.z, h = blockIdx.y, tile = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
@@ -332,6 +337,8 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
       qb[ks][1] = frag[(ks * 32 + lane) * 4 + 2];
     }
   }
+  const bool cluster = a.splits > 1 && a.splits <= 8;
+  if (Shape::send && cluster) cluster_arrive_release();   // (Q's place is free)
   float m[2] = {-INFINITY, -INFINITY}, W[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 
   // the exponents of a unit's blocks, one byte each
@@ -699,7 +706,54 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
     }
     return;
   }
-  if (a.splits <= 8) {
+  if (Shape::send && cluster) {
+    // the splits are a cluster: each CTA sends every other its share of the rows' columns and the
+    // rows' (max, sum), so that one barrier is all that they wait for (each reading its share
+    // from all took a remote read's latency twice and a barrier at the end more: 0.7 us)
+    const int pieces = rows * (HDP / 4), share = (pieces + a.splits - 1) / a.splits;
+    const uint32_t part_of = ((1u << 22) + share - 1) / share;   // (w / share for w < 8 share: the excess stays below 2^22)
+    const uint32_t in = smem_u32(frag);
+    cluster_wait_acquire();   // (everybody holds Q)
+    for (int w = threadIdx.x; w < pieces; w += RW * 32) {
+      const uint32_t to = (uint32_t)w * part_of >> 22;
+      st_cluster_f4(mapa_shared(in + 16u * (uint32_t)(split * share + w - (int)to * share), to),
+                    joined(w / (HDP / 4), w % (HDP / 4) * 4));
+    }
+    if ((int)threadIdx.x < 8 * a.splits)
+      st_cluster_f2(mapa_shared(smem_u32(&split_in[split][threadIdx.x % 8]), threadIdx.x / 8), split_w[threadIdx.x % 8]);
+    cluster_sync();
+    if ((int)threadIdx.x < rows) {
+      float M = -INFINITY, S = 0.f;
+      for (int q = 0; q < a.splits; ++q) M = fmaxf(M, split_in[q][threadIdx.x].x);
+      for (int q = 0; q < a.splits; ++q) {
+        const float2 x = split_in[q][threadIdx.x];
+        const float wt = x.y != x.y ? x.y : (x.x == -INFINITY ? 0.f : exp2f(x.x - M) * x.y);
+        split_wt[q][threadIdx.x] = wt;
+        S += wt;
+      }
+      const float inv = !(S <= 0.f) ? 1.f / S : 0.f;
+      for (int q = 0; q < a.splits; ++q) split_wt[q][threadIdx.x] *= inv;
+      if (a.mass && split == 0) a.row_ml[head * a.n * a.G + r0 + threadIdx.x] = row_weight(M, S, kPExp);
+    }
+    __syncthreads();
+    for (int w = split * share + threadIdx.x; w < min(pieces, (split + 1) * share); w += RW * 32) {
+      const int row = w / (HDP / 4), d = w % (HDP / 4) * 4;
+      if (d >= L.hd) continue;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+      for (int q = 0; q < a.splits; ++q) {
+        const float4 x = lds_f4(in + 16u * (uint32_t)(q * share + w - split * share));
+        const float wt = split_wt[q][row];
+        acc.x += wt * x.x;
+        acc.y += wt * x.y;
+        acc.z += wt * x.z;
+        acc.w += wt * x.w;
+      }
+      store4(row, d, acc);
+    }
+    return;
+  }
+  if (cluster) {
     // the splits are a cluster: each CTA joins a share of the rows' columns from all of them
     for (int w = threadIdx.x; w < rows * (HDP / 4); w += RW * 32) ((float4*)mine)[w] = joined(w / (HDP / 4), w % (HDP / 4) * 4);
     cluster_sync();
