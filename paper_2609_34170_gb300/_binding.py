@@ -304,12 +304,13 @@ def ravel_last_error(h) -> str:
 # ---- the 8-bit context cache (include/ravel_cache.h)
 
 
-def current_raw_stream(device: int) -> int:
-    """The current stream of a device.  (torch.cuda.current_stream makes an
-    object first: 3 us of a call's 13.)"""
+def current_stream_getter():
+    """A function of a device's index that gives its current stream as an
+    address.  (torch.cuda.current_stream makes an object first: 3 us of a call's
+    13.)"""
     import torch
     get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return get(device) if get is not None else torch.cuda.current_stream(device).cuda_stream
+    return get if get is not None else lambda device: torch.cuda.current_stream(device).cuda_stream
 
 
 def _check_cache(c, status: int, what: str):

@@ -33,11 +33,12 @@ class ContextCache:
                                            B.RAVEL_BF16 if dtype == "bf16" else B.RAVEL_FP32, device)
         self._lib = B.load()
         self._int32, self._float32 = torch.int32, torch.float32
+        self._index, self._current_stream = self.device.index, B.current_stream_getter()
 
     # -- arguments
     def _stream(self, stream):
         if stream is None:
-            return B.current_raw_stream(self.device.index)
+            return self._current_stream(self._index)
         return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
     def _empty(self, shape, dtype, stream):
@@ -54,7 +55,7 @@ class ContextCache:
         """Strides (robot, token) of a [batch, n, heads, head_dim] tensor whose heads are contiguous."""
         shape = x.shape
         if x.dtype is not self.dtype or len(shape) != 4 or shape[2] != heads or shape[3] != self.head_dim or \
-                x.get_device() != self.device.index:
+                x.get_device() != self._index:
             raise ValueError(f"{name} must be [batch, n, {heads}, {self.head_dim}] of dtype {self.dtype} on {self.device}, "
                              f"got {tuple(shape)} of {x.dtype} on {x.device}")
         robot, token, head, dim = x.stride()
@@ -66,7 +67,7 @@ class ContextCache:
         """Address of an int32 tensor [batch], or None."""
         if x is None:
             return None
-        if x.dtype is not self._int32 or x.shape != (batch,) or x.get_device() != self.device.index or not x.is_contiguous():
+        if x.dtype is not self._int32 or x.shape != (batch,) or x.get_device() != self._index or not x.is_contiguous():
             raise ValueError(f"{name} must be a contiguous int32 tensor [{batch}] on {self.device}")
         return x.data_ptr()
 
@@ -74,7 +75,7 @@ class ContextCache:
         """Address and length of a mass's rows."""
         shape = mass.shape
         if len(shape) != 3 or (batch is not None and shape[0] != batch) or shape[1] != self.n_kv_heads or \
-                mass.dtype is not self._float32 or mass.get_device() != self.device.index or not mass.is_contiguous():
+                mass.dtype is not self._float32 or mass.get_device() != self._index or not mass.is_contiguous():
             raise ValueError(f"mass must be a contiguous float32 tensor [{'batch' if batch is None else batch}, "
                              f"{self.n_kv_heads}, tokens] on {self.device}, got {tuple(shape)} of {mass.dtype}")
         return mass.data_ptr(), shape[2]
@@ -110,7 +111,10 @@ class ContextCache:
             out = self._empty(shape, q.dtype, stream)
         elif out.shape != shape:
             raise ValueError("out must have q's shape")
-        outr, outt = self._rows(out, self.n_q_heads, "out")
+        if out.dtype is q.dtype and out.stride() == q.stride() and out.get_device() == self._index:
+            outr, outt = qr, qt
+        else:
+            outr, outt = self._rows(out, self.n_q_heads, "out")
         if lengths is None:
             raise ValueError("lengths must be given")
         mass_at, mass_len = self._mass(mass, batch) if mass is not None else (None, 0)
