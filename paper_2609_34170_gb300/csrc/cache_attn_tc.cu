@@ -32,8 +32,8 @@
 // a grown one waits for its rescaling of O (only growth by more than 2^8 rescales);
 // what contributes less than 2^-31 of the row's largest is dropped.
 //
-// Measured: 16 prompts of 816 tokens (8 heads of 256, one KV head) 90.5 us, 964 TFLOP/s;
-// 2 of 8191 with a window of 1024 (16 heads of 64) 202 us, without the window 424; 50 slots of
+// Measured: 16 prompts of 816 tokens (8 heads of 256, one KV head) 88.5 us, 985 TFLOP/s;
+// 2 of 8191 with a window of 1024 (16 heads of 64) 193 us, without the window 426; 50 slots of
 // 16 robots over 816 tokens, 20 us.  A tile of 128 x 128 takes 1570 cycles at head dim 64, 1940
 // at 128, 2190 at 192 and 2550 at 256 (MMAs alone: 512, 1024, 1536, 2048), an item's begin and
 // end 7500 to 12000 more.  Up to 128 the softmax bounds it; of a tile that two threads a row
@@ -73,7 +73,7 @@ template <int NB> struct TcShape {
   // warpgroup takes every second tile, a thread a row, with references and an output of its
   // own, joined at the item's end, so that one's waits lie beside the other's work: 1570
   // cycles a tile instead of 1780 (2 causal prompts of 8191: 424 us instead of 479; with a
-  // window of 1024, of whose ten tiles three are masked, twice then, no difference).  Beyond,
+  // window of 1024, of whose ten tiles three are masked, twice then, 193 instead of 199).  Beyond,
   // both share a tile, two threads to a row: with the two buffers of scores that fit at 128,
   // a P's way to the scores of the tile after next, 1450 cycles, ate the gain.
   static constexpr bool own = NB == 1;
@@ -720,15 +720,20 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
       pair_bar();
       const bool real = mk.hi > 0 && n > 0 && !(l <= 0.f);   // (a sum that is not a number stays one)
       const float inv = real ? pow2f(W - m) / l : 0.f;
-      // 32 of the row's outputs, normalised
+      // 32 of the row's outputs, normalised (not numbers to go by where the row is not real)
       auto output = [&](int cb, uint32_t (&raw)[32]) {
+        auto times = [](uint32_t& a, uint32_t& b, float f) {
+          const float2 x = fma2(make_float2(__uint_as_float(a), __uint_as_float(b)), make_float2(f, f), make_float2(-0.f, -0.f));
+          a = __float_as_uint(x.x);
+          b = __float_as_uint(x.y);
+        };
         if constexpr (!Shape::own) {
           tmem_ld32_async(lane_base + o_col + cb, raw);
           tmem_wait_ld();
           tmem_reg_fence16(raw);
           tmem_reg_fence16(raw + 16);
 #pragma unroll
-          for (int q = 0; q < 32; ++q) raw[q] = real ? __float_as_uint(__uint_as_float(raw[q]) * inv) : 0u;
+          for (int q = 0; q < 32; q += 2) times(raw[q], raw[q + 1], inv);
         } else {
           // (of a single tile, one output has nothing of this item)
           const int only = n == 1 ? (gt - 1) & 1 : 0;
@@ -743,9 +748,14 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
             tmem_reg_fence16(x);
             tmem_reg_fence16(y);
 #pragma unroll
-            for (int q = 0; q < 16; ++q) {
-              const float z = __uint_as_float(x[q]) * f0;
-              x[q] = real ? __float_as_uint(n > 1 ? fmaf(__uint_as_float(y[q]), f1, z) : z) : 0u;
+            for (int q = 0; q < 16; q += 2) {
+              times(x[q], x[q + 1], f0);
+              if (n > 1) {
+                const float2 z = fma2(make_float2(__uint_as_float(y[q]), __uint_as_float(y[q + 1])), make_float2(f1, f1),
+                                      make_float2(__uint_as_float(x[q]), __uint_as_float(x[q + 1])));
+                x[q] = __float_as_uint(z.x);
+                x[q + 1] = __float_as_uint(z.y);
+              }
             }
           }
         }
@@ -768,7 +778,7 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
           }
           uint32_t wd[16];
 #pragma unroll
-          for (int q = 0; q < 16; ++q) wd[q] = pack_bf16x2(__uint_as_float(raw[2 * q]), __uint_as_float(raw[2 * q + 1]));
+          for (int q = 0; q < 16; ++q) wd[q] = real ? pack_bf16x2(__uint_as_float(raw[2 * q]), __uint_as_float(raw[2 * q + 1])) : 0u;
           if (wide) {
             // four lanes' rows turned into four pieces of a row each: stores of 8 rows x 64 bytes
             auto turn = [&](uint32_t& a, uint32_t& b, int bit) {
@@ -804,6 +814,8 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
       for (int cb = 32 * hf; cb < HDP; cb += 64) {
         uint32_t raw[32];
         output(cb, raw);
+#pragma unroll
+        for (int q = 0; q < 32; ++q) raw[q] = real ? raw[q] : 0u;
         if (cluster) {
 #pragma unroll
           for (int q = 0; q < 8; ++q)
