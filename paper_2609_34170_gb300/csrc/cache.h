@@ -110,6 +110,7 @@ struct CacheAttnArgs {
   LaunchDiv by_splits, by_group, by_last, by_pairs;   // tensor cores: of items, see there
   long long mass_pitch;     // tokens of a chunk's sums, or of a row's scores
   float* scores;            // few rows: scores kept for the mass, or null
+  int b0, i0, i1;           // few rows: this launch's first robot, its queries i0 .. i1 - 1
   int group;                // tensor cores: (robot, KV head) pairs walked together
 };
 constexpr int kCacheSplitCtas = 608;   // row tiles (of 16) x splits of a launch that splits the tokens
@@ -117,7 +118,8 @@ constexpr int kCacheTcRows = 128;      // rows of a tile on the tensor cores: at
 cudaError_t launch_cache_attend(const CacheAttnArgs& a, Dtype dt, cudaStream_t st);
 cudaError_t launch_cache_attend_tc(const CacheAttnArgs& a, cudaStream_t st);   // bf16; not the mass
 cudaError_t launch_cache_mass_tc(CacheAttnArgs a, cudaStream_t st);   // bf16, after the attention
-size_t cache_mass_ws_bytes(int heads, int T, int num_sms);
+// rows: query rows per KV head of which scores may be kept; G: query heads per KV head
+size_t cache_mass_ws_bytes(int heads, int Hkv, int G, long long rows, int T, int num_sms);
 cudaError_t init_cache_mass_tc_kernels();
 cudaError_t init_cache_kernels();
 cudaError_t init_cache_tc_kernels(int hdp, int* clusters);   // clusters: [9]

@@ -37,6 +37,8 @@
 // score, and its largest score + ve) are rounded up to integers in the log2
 // domain, so that every change of reference is an exact power of two.  Maxima,
 // sums and outputs are fp32.
+#include <algorithm>
+
 #include "cache_tc.cuh"
 #include "launch.h"
 
@@ -143,20 +145,6 @@ __device__ __forceinline__ void stage_q(const CacheAttnArgs& a, const Sight& s, 
   __syncthreads();
 }
 
-// S of the block of 16 tokens whose key rows begin at `k`: s[hh][.] covers
-// tokens 8 hh + 2 c, + 1 for rows g and g + 8.
-template <int HDP>
-struct KeyRegs {
-  uint4 w[2][HDP / 64];   // tokens g and g + 8: 16 bytes at 64 j + 16 c
-  __device__ __forceinline__ void load(const uint8_t* k, int g, int c) {
-#pragma unroll
-    for (int hh = 0; hh < 2; ++hh)
-#pragma unroll
-      for (int j = 0; j < HDP / 64; ++j)
-        w[hh][j] = __ldg((const uint4*)(k + (size_t)(g + 8 * hh) * HDP + 64 * j + 16 * c));
-  }
-};
-
 // A warp's unit of 16 NT tokens in shared memory: boxes of IN dims x U tokens as TMA
 // swizzles them (16-byte pieces of a row permuted by the row), codes of K or of V.
 template <int HDP>
@@ -253,11 +241,11 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
   __shared__ float split_wt[8][16];
   __shared__ float2 split_in[Shape::send ? 8 : 1][8];   // the splits' (max, sum)
 
-  const int b = blockIdx.z, h = blockIdx.y, tile = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
+  const int b = blockIdx.z + a.b0, h = blockIdx.y, tile = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
   const CacheLayer& L = a.c;
-  const int r0 = tile * RT, rows = min(RT, a.n * a.G - r0);
-  const size_t head = (size_t)b * L.Hkv + h;
+  const int r0 = a.i0 * a.G + tile * RT, rows = min(RT, a.i1 * a.G - r0);
+  const size_t head = (size_t)b * L.Hkv + h, here = (size_t)blockIdx.z * L.Hkv + h;   // (of the cache, of this launch)
   if (smem_u32(smem) & 1023u) {   // (the swizzled layouts count on it)
     if (threadIdx.x == 0) raise_error(a.err, ERR_SHAPE);
     return;
@@ -480,7 +468,7 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
 #pragma unroll
           for (int rr = 0; rr < 2; ++rr)
             if (row_of[rr] < rows) {
-              float* to = a.scores + (head * a.n * a.G + r0 + row_of[rr]) * a.mass_pitch + j0 + 16 * t + place(hh, 0);
+              float* to = a.scores + (here * (a.i1 - a.i0) * a.G + r0 - a.i0 * a.G + row_of[rr]) * a.mass_pitch + j0 + 16 * t + place(hh, 0);
               if (RT == 8) *to = sc[t][hh][rr][0];
               else *(float2*)to = make_float2(sc[t][hh][rr][0], sc[t][hh][rr][QN - 1]);
             }
@@ -799,7 +787,7 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
     cluster_sync();   // nobody leaves while its rows are read
     return;
   }
-  const size_t unit = head * a.row_tiles + tile;
+  const size_t unit = here * a.row_tiles + tile;
   float* part = a.part + (unit * a.splits + split) * 16 * HDP;
   for (int w = threadIdx.x; w < rows * (HDP / 4); w += RW * 32) __stcg((float4*)part + w, joined(w / (HDP / 4), w % (HDP / 4) * 4));
   if (threadIdx.x < rows) __stcg(a.part_ml + (unit * a.splits + split) * 16 + threadIdx.x, split_w[threadIdx.x]);
@@ -848,136 +836,45 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
   }
 }
 
-// Attention mass: token j's softmax weights summed over the rows of its KV
-// head, from the rows' (max, 1 / sum) that the attention left behind.  A warp
-// owns a block of 16 tokens, keeps its widened key fragments in registers and
-// walks the rows' tiles; sums are fp32 in a fixed order.  For fp32 prompts, and for
-// few rows whose scores do not fit the workspace: bound by the MMAs and by laying
-// out Q again in every CTA (4 robots of 816 bf16 queries took it 1.1 ms, which is why
-// those have a kernel on the 5th-generation tensor cores).
-template <int HDP, int NP, typename T>
-__global__ void __launch_bounds__(RW * 32) cache_mass_kernel(CacheAttnArgs a) {
-  constexpr int KS = HDP / 16;
-  extern __shared__ __align__(1024) uint8_t smem[];
-  uint32_t* frag = (uint32_t*)smem;   // [NP][KS][32][4]
-  __shared__ float fac[16];
-  const int b = blockIdx.z, h = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int g = lane >> 2, c = lane & 3;
-  const CacheLayer& L = a.c;
-  const size_t head = (size_t)b * L.Hkv + h;
-  pdl_trigger();
-  pdl_wait();
-  Sight s;
-  robot_sight(a, b, s);
-  const int j0 = (blockIdx.x * RW + warp) * 16, jc0 = blockIdx.x * RW * 16, jc1 = jc0 + RW * 16;
-  float* mass = a.mass + head * a.mass_stride;
-  float acc[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
-  // (uniform in the CTA) queries that can see a token of the CTA's
-  int i0 = 0, i1 = jc0 < s.len ? s.count : 0;
-  if (a.causal) {
-    i0 = max(0, jc0 - s.p0);
-    if (a.window > 0 && jc0 >= a.sinks) i1 = min(i1, jc1 - 1 + a.window - s.p0);
-  }
-  if (i0 < i1) {
-    uint32_t kb[2][KS][2];
-    {
-      KeyRegs<HDP> kr;
-      kr.load(L.k + (head * L.T + min(j0, L.T - 16)) * HDP, g, c);
-#pragma unroll
-      for (int hh = 0; hh < 2; ++hh)
-#pragma unroll
-        for (int j = 0; j < HDP / 64; ++j) {
-          const uint32_t w[4] = {kr.w[hh][j].x, kr.w[hh][j].y, kr.w[hh][j].z, kr.w[hh][j].w};
-#pragma unroll
-          for (int s4 = 0; s4 < 4; ++s4) {
-            kb[hh][4 * j + s4][0] = e4m3_lo(w[s4]);
-            kb[hh][4 * j + s4][1] = e4m3_hi(w[s4]);
-          }
-        }
-    }
-    const float kf = exp2i(L.ke[head * (L.T / 16) + min(j0, L.T - 16) / 16]);
-    const float2* ml = a.row_ml + head * a.n * a.G;
-    for (int r0 = i0 * a.G / 16 * 16; r0 < i1 * a.G; r0 += 16) {
-      __syncthreads();
-      if (threadIdx.x < 16) fac[threadIdx.x] = 0.f;
-      __syncthreads();
-      stage_q<HDP, NP, T, RW * 32>(a, s, b, h, r0, frag, fac, []() {});
-      float sc[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        uint4 qa[NP];
-#pragma unroll
-        for (int p = 0; p < NP; ++p) qa[p] = *(const uint4*)(frag + ((p * KS + ks) * 32 + lane) * 4);
-#pragma unroll
-        for (int hh = 0; hh < 2; ++hh) {
-          if constexpr (NP == 1) {
-            mma_f16(sc[hh], qa[0], kb[hh][ks][0], kb[hh][ks][1]);
-          } else {
-            float x[4] = {0.f, 0.f, 0.f, 0.f};
-            mma_f16(x, qa[NP - 1], kb[hh][ks][0], kb[hh][ks][1]);
-            mma_f16(x, qa[0], kb[hh][ks][0], kb[hh][ks][1]);
-            add4(sc[hh], x);
-          }
-        }
-      }
-#pragma unroll
-      for (int rr = 0; rr < 2; ++rr) {
-        const int r = r0 + g + 8 * rr;
-        const RowMask mk = row_mask(a, s, r);
-        const float2 x = r < a.n * a.G ? ml[r] : make_float2(0.f, 0.f);
-        const float f = fac[g + 8 * rr] * kf;
-#pragma unroll
-        for (int hh = 0; hh < 2; ++hh)
-#pragma unroll
-          for (int q = 0; q < 2; ++q)
-            if (mk.sees(j0 + 8 * hh + 2 * c + q))
-              acc[hh][q] += exp2f(fmaf(sc[hh][2 * rr + q], f, -x.x)) * x.y;
-      }
-    }
-  }
-#pragma unroll
-  for (int hh = 0; hh < 2; ++hh)
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      float v = acc[hh][q];
-      v += __shfl_xor_sync(0xffffffffu, v, 4);
-      v += __shfl_xor_sync(0xffffffffu, v, 8);
-      v += __shfl_xor_sync(0xffffffffu, v, 16);
-      const int j = j0 + 8 * hh + 2 * c + q;
-      if (g == 0 && j < a.max_length) {
-        if (!a.mass_add) mass[j] = v;
-        else if (j < s.len) mass[j] += v;
-      }
-    }
-}
-
-// The same from the scores that the attention kept: a thread per two tokens.  Bound by
+// Attention mass: token j's softmax weights summed over the rows of its KV head, from the
+// scores that the attention kept and the rows' (max, 1 / sum): a thread per two tokens
+// and, of many queries, every 8th, 16th or 64th of them, summed in a fixed order.  Bound by
 // reading them, 4 bytes per row and token (4 robots x 16 rows x 131071 tokens: 34 MB, in
 // L2, 13.6 us); computing them again would read the keys' 134 MB from HBM.
-__global__ void __launch_bounds__(256) cache_mass_scores_kernel(CacheAttnArgs a) {
-  const int j = (blockIdx.x * 256 + threadIdx.x) * 2;
+__global__ void __launch_bounds__(1024) cache_mass_scores_kernel(CacheAttnArgs a, int groups) {
+  __shared__ float2 sums[1024];
+  const int per = (int)blockDim.x / groups, group = threadIdx.x / per, at = threadIdx.x % per;
+  const int j = (blockIdx.x * per + at) * 2;
   pdl_trigger();
   pdl_wait();
-  if (j >= a.max_length) return;
-  const int b = blockIdx.z;
-  const size_t head = (size_t)b * a.c.Hkv + blockIdx.y;
+  const int b = blockIdx.z + a.b0;
+  const size_t head = (size_t)b * a.c.Hkv + blockIdx.y, here = (size_t)blockIdx.z * a.c.Hkv + blockIdx.y;
   Sight s;
   robot_sight(a, b, s);
   const float2* ml = a.row_ml + head * a.n * a.G;
-  const float* sc = a.scores + head * a.n * a.G * a.mass_pitch + j;
+  const float* sc = a.scores + here * (a.i1 - a.i0) * a.G * a.mass_pitch + j;
   float v0 = 0.f, v1 = 0.f;
   if (j < s.len)
-    for (int i = 0; i < s.count; ++i) {
+    for (int i = a.i0 + group; i < min(a.i1, s.count); i += groups) {
       const RowMask mk = row_mask(a, s, i * a.G);
       const bool s0 = mk.sees(j), s1 = mk.sees(j + 1);
       if (!s0 && !s1) continue;
 #pragma unroll 4
       for (int g = 0; g < a.G; ++g) {
-        const float2 x = __ldcs((const float2*)(sc + (size_t)(i * a.G + g) * a.mass_pitch)), y = __ldg(ml + i * a.G + g);
+        const float2 x = __ldcs((const float2*)(sc + (size_t)((i - a.i0) * a.G + g) * a.mass_pitch)), y = __ldg(ml + i * a.G + g);
         v0 += s0 ? exp2f(x.x - y.x) * y.y : 0.f;
         v1 += s1 ? exp2f(x.y - y.x) * y.y : 0.f;
       }
     }
+  if (groups > 1) {
+    sums[threadIdx.x] = make_float2(v0, v1);
+    __syncthreads();
+    if (group) return;
+    for (int q = 1; q < groups; ++q) {
+      v0 += sums[q * per + at].x;
+      v1 += sums[q * per + at].y;
+    }
+  }
   float* mass = a.mass + head * a.mass_stride + j;
 #pragma unroll
   for (int e = 0; e < 2; ++e)
@@ -988,15 +885,14 @@ __global__ void __launch_bounds__(256) cache_mass_scores_kernel(CacheAttnArgs a)
     }
 }
 
-template <int HDP, int NP>
-constexpr int frag_bytes() { return NP * (HDP / 16) * 512; }
-
+// One launch of the rows kernel, queries i0 .. i1 - 1 of `batch` robots from b0 on, and, where
+// the mass is wanted, one over the scores that it left.
 template <int HDP, int NP, typename T>
-cudaError_t launch_rows(CacheAttnArgs a, cudaStream_t st) {
+cudaError_t launch_part(CacheAttnArgs a, int batch, cudaStream_t st) {
   constexpr int U = Unit<HDP>::U;
-  const int RT = a.n * a.G <= 8 ? 8 : 16;   // rows of a tile
-  a.row_tiles = (a.n * a.G + RT - 1) / RT;
-  const long long tiles = (long long)a.row_tiles * a.c.Hkv * a.batch;
+  const int rows = (a.i1 - a.i0) * a.G, RT = rows <= 8 ? 8 : 16;   // rows of a tile
+  a.row_tiles = (rows + RT - 1) / RT;
+  const long long tiles = (long long)a.row_tiles * a.c.Hkv * batch;
   // tokens that a row tile sees at most, in units
   long long seen = a.max_length;
   if (a.window > 0) seen = min(seen, (long long)a.window + a.sinks + 15 / a.G + 1 + 2 * U);
@@ -1011,29 +907,57 @@ cudaError_t launch_rows(CacheAttnArgs a, cudaStream_t st) {
     // than two units more for each warp
     if (a.splits > 8 && units <= 8 * RW * 3) a.splits = 8;
   }
-  // (every head's and row's scores, where the mass's workspace holds them)
-  a.mass_pitch = (a.max_length + 127) / 128 * 128;
-  const bool keep = a.mass && (NP == 2 || a.n * a.G <= 16) &&
-                    (double)a.batch * a.c.Hkv * a.n * a.G * a.mass_pitch * 4 <= (double)a.mass_ws_bytes;
-  a.scores = keep ? a.mass_ws : nullptr;
+  const RowsMaps maps{a.maps->k_rows, a.maps->v_rows};
+  const dim3 grid(a.row_tiles * a.splits, a.c.Hkv, batch), cluster(a.splits <= 8 ? a.splits : 1, 1, 1);
+  const cudaError_t e =
+      RT == 8 ? launch_kernel_cluster(cache_rows_kernel<HDP, NP, 8, T>, grid, dim3(RW * 32), RowsShape<HDP, NP, 8>::bytes, st,
+                                      cluster, maps, a)
+              : launch_kernel_cluster(cache_rows_kernel<HDP, NP, 16, T>, grid, dim3(RW * 32), RowsShape<HDP, NP, 16>::bytes, st,
+                                      cluster, maps, a);
+  if (e != cudaSuccess || !a.scores) return e;
+  // groups of a token's queries, and with them threads: as many as the queries fill, 1024 where
+  // the tokens are few CTAs otherwise (1 robot's 816 queries and tokens, one KV head of fp32: 232
+  // us with 8 groups, 36 with 64; 26 robots' 23 queries, two heads of 1465 tokens: 10 and 19)
+  const int queries = a.i1 - a.i0;
+  const bool few = (long long)((a.max_length + 63) / 64) * a.c.Hkv * batch < 2 * a.num_sms;
+  const int groups = queries >= 64 ? 64 : (queries < 16 ? 1 : (few ? 16 : 8)), threads = groups >= 16 ? 1024 : 256;
+  const int tokens = 2 * threads / groups;
+  return launch_kernel(cache_mass_scores_kernel, dim3((a.max_length + tokens - 1) / tokens, a.c.Hkv, batch), dim3(threads), 0, st, 1,
+                       a, groups);
+}
+
+template <int HDP, int NP, typename T>
+cudaError_t launch_rows(CacheAttnArgs a, cudaStream_t st) {
   const Overlap overlap;
-  cudaError_t e;
+  const bool mass = a.mass && a.max_length > 0;
   if (NP == 1 && a.n * a.G > 16) {
-    e = launch_cache_attend_tc(a, st);
-  } else {
-    const RowsMaps maps{a.maps->k_rows, a.maps->v_rows};
-    const dim3 grid(a.row_tiles * a.splits, a.c.Hkv, a.batch), cluster(a.splits <= 8 ? a.splits : 1, 1, 1);
-    e = RT == 8 ? launch_kernel_cluster(cache_rows_kernel<HDP, NP, 8, T>, grid, dim3(RW * 32), RowsShape<HDP, NP, 8>::bytes,
-                                        st, cluster, maps, a)
-                : launch_kernel_cluster(cache_rows_kernel<HDP, NP, 16, T>, grid, dim3(RW * 32), RowsShape<HDP, NP, 16>::bytes,
-                                        st, cluster, maps, a);
+    const cudaError_t e = launch_cache_attend_tc(a, st);
+    return e != cudaSuccess || !mass ? e : launch_cache_mass_tc(a, st);
   }
-  if (e != cudaSuccess || !a.mass || a.max_length == 0) return e;
-  if (NP == 1 && a.n * a.G > 16) return launch_cache_mass_tc(a, st);
-  if (keep)
-    return launch_kernel(cache_mass_scores_kernel, dim3((a.max_length + 511) / 512, a.c.Hkv, a.batch), dim3(256), 0, st, 1, a);
-  return launch_kernel(cache_mass_kernel<HDP, NP, T>, dim3((a.max_length + RW * 16 - 1) / (RW * 16), a.c.Hkv, a.batch),
-                       dim3(RW * 32), frag_bytes<HDP, NP>(), st, 1, a);
+  // For the mass every row's scores are kept, of as many robots (or, of one robot, queries) at
+  // a time as the workspace holds: a query of one robot at least.  (Computing them again, from
+  // keys in registers with Q laid out in every CTA, took with the attention 879 us instead of 82
+  // for one robot's 816 queries and tokens, 8 heads of 256 on one in fp32, and 619 instead of
+  // 248 for 4 robots' 1024, 16 heads of 64 on 4.)
+  a.mass_pitch = (a.max_length + 127) / 128 * 128;
+  a.scores = mass ? a.mass_ws : nullptr;
+  int robots = a.batch, queries = a.n;
+  if (mass) {
+    const size_t query = (size_t)a.c.Hkv * a.G * a.mass_pitch * 4, fit = a.mass_ws_bytes / query;
+    if (fit == 0) return cudaErrorInvalidValue;
+    robots = (int)std::min<size_t>(a.batch, std::max<size_t>(1, fit / a.n));
+    if (robots == 1) queries = (int)std::min<size_t>(a.n, fit >= 16 ? fit / 16 * 16 : fit);
+  }
+  for (a.b0 = 0; a.b0 < a.batch; a.b0 += robots) {
+    CacheAttnArgs part = a;
+    for (part.i0 = 0; part.i0 < a.n; part.i0 = part.i1) {
+      part.i1 = min(a.n, part.i0 + queries);
+      part.mass_add = a.mass_add || part.i0 > 0;
+      const cudaError_t e = launch_part<HDP, NP, T>(part, min(robots, a.batch - a.b0), st);
+      if (e != cudaSuccess) return e;
+    }
+  }
+  return cudaSuccess;
 }
 
 template <int HDP>

@@ -142,7 +142,9 @@ ravel_status ravel_cache_create(const ravel_cache_config* cfg, int device, ravel
   get(&c->part_ml, sizeof(float2) * part_rows);
   get(&c->arrived, sizeof(unsigned) * kCacheSplitCtas);
   get(&c->row_ml, sizeof(float2) * cfg->max_batch * (size_t)cfg->n_q_heads * cfg->max_queries);
-  c->mass_ws_bytes = cache_mass_ws_bytes((int)heads, c->T, c->num_sms);
+  const int G = cfg->n_q_heads / cfg->n_kv_heads;
+  c->mass_ws_bytes = cache_mass_ws_bytes((int)heads, cfg->n_kv_heads, G, cfg->dtype == RAVEL_FP32 ? (long long)cfg->max_queries * G : 16,
+                                         c->T, c->num_sms);
   get(&c->mass_ws, c->mass_ws_bytes);
   get(&c->q_ws, (size_t)c->num_sms * kCacheTcRows * c->hdp * 2);
   get(&c->err, sizeof(ErrorWord));

@@ -324,9 +324,12 @@ cudaError_t launch_cache_mass_tc(CacheAttnArgs a, cudaStream_t st) {
   return launch_kernel(cache_mass_sum_kernel, dim3((a.max_length + 31) / 32, a.c.Hkv, a.batch), dim3(256), 0, st, 1, a);
 }
 
-size_t cache_mass_ws_bytes(int heads, int T, int num_sms) {
-  const size_t least = 8ull * heads * T, most = 8ull * ((size_t)heads + num_sms) * T;
-  return std::max(least, std::min(most, (size_t)64 << 20));
+size_t cache_mass_ws_bytes(int heads, int Hkv, int G, long long rows, int T, int num_sms) {
+  // a chunk per head, and the scores of a query; at best a chunk per SM and all scores, up to
+  // 64 MB, which stay in L2 until they are summed
+  const size_t least = std::max(8ull * heads * T, 4ull * Hkv * G * T);
+  const double most = std::max(8.0 * ((double)heads + num_sms) * T, 4.0 * heads * (double)rows * T);
+  return std::max(least, (size_t)std::min(most, 64.0 * (1 << 20)));
 }
 
 cudaError_t init_cache_mass_tc_kernels() {

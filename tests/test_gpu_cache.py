@@ -356,6 +356,20 @@ def test_eviction_from_long_caches():
     np.testing.assert_array_equal(_np(k), held.k[:, :, :keep])
 
 
+@pytest.mark.parametrize("layout,n,batch", [((16, 4, 64), 900, 3), ((3, 3, 40), 150, 130), ((16, 1, 64), 1100, 1)])
+def test_mass_whose_scores_come_in_parts(layout, n, batch):
+    # more scores than are kept at a time: some robots', then some queries'
+    p = Pair(layout, "fp32", n + 40, batch, queries=n, lengths=[n + 40 - 7 * (b % 5) for b in range(batch)], seed=41)
+    check(p, n, mass=True, counts=[n - b % 3 for b in range(batch)])
+    _, m = check(p, n, mass=True, causal=False, seed=9)
+    q = _rand((batch, n, layout[0], layout[2]), 9, "fp32", 2.0)
+    twice = m.clone()
+    p.cache.attend(0, q, _ints(p.lengths), causal=False, mass=twice, add_mass=True)
+    for b, length in enumerate(p.lengths):
+        torch.testing.assert_close(twice[b, :, :length], 2 * m[b, :, :length], rtol=2 ** -20, atol=0)
+        assert torch.equal(twice[b, :, length:], m[b, :, length:])
+
+
 def _chain(cache, small, x, lengths, n):
     """Append, attend with the mass, evict and read back, none of them waited for."""
     cache.append(0, x["k"], x["v"])
