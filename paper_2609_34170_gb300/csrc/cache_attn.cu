@@ -39,6 +39,7 @@
 // sums and outputs are fp32.
 #include <algorithm>
 
+#include "cache_index.h"
 #include "cache_tc.cuh"
 #include "launch.h"
 
@@ -343,7 +344,6 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
   }
   int slot = 0;
   uint32_t phase = 0u;
-  bool ok = true;
   for (; u < u1; u += RW) {
     const int j0 = unit_token(u);
     const uint32_t unit = ring + (uint32_t)slot * 2u * Un::bytes;
@@ -359,7 +359,14 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
       kes = exps_of(KE, unit_token(un));
       ves = exps_of(VE, unit_token(un));
     }
-    if (ok) ok = wait_phase(&arrived[warp][slot], phase);
+    if (!wait_phase(&arrived[warp][slot], phase)) {
+      // nothing is issued any more, and what is on its way lands before the shared memory is
+      // written by others or goes away
+      const LoadsLeft left = loads_left((u - u0 - warp) / RW, (u1 - u0 - warp + RW - 1) / RW, D);
+      for (int x = left.first; x < left.end; ++x) mbar_wait(&arrived[warp][x % D], load_parity(x, D));
+      if (lane == 0) raise_error(a.err, ERR_TIMEOUT);
+      break;
+    }
     KeyUnit<HDP> kr[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) kr[t].load(unit, 16 * t, g, c);
@@ -599,10 +606,6 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
       slot = 0;
       phase ^= 1u;
     }
-  }
-  if (!ok) {   // loads still on their way land before the shared memory goes away
-    for (int x = 0; x < D; ++x) mbar_wait(&arrived[warp][x], phase ^ (x < slot ? 1u : 0u));
-    if (lane == 0) raise_error(a.err, ERR_TIMEOUT);
   }
   __syncthreads();   // the rings are read: the outputs go over them
 
