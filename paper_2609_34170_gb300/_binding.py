@@ -318,26 +318,64 @@ def _check_cache(c, status: int, what: str):
         raise RavelError(status, f"{what}: {load().ravel_cache_last_error(c).decode()}")
 
 
-def _strided(t, dtype, heads: int, head_dim: int, name: str):
-    """(address, robot stride, token stride) of a [B, n, heads, head_dim] CUDA
-    tensor whose heads are contiguous (columns of a projection's rows will do)."""
-    shape, stride = t.shape, t.stride()
-    if not t.is_cuda or t.dtype != dtype:
-        raise ValueError(f"{name} must be a CUDA tensor of dtype {dtype}, got {t.dtype} on {t.device}")
-    if len(shape) != 4 or shape[2] != heads or shape[3] != head_dim:
-        raise ValueError(f"{name} must be [batch, n, {heads}, {head_dim}], got {tuple(shape)}")
-    if (stride[3] != 1 and head_dim > 1) or (stride[2] != head_dim and heads > 1):
-        raise ValueError(f"{name}: the heads of a token must be contiguous")
-    return t.data_ptr(), stride[0], stride[1]
+class CacheArguments:
+    """What the calls on a cache look over: types, shapes, strides and device of
+    their tensors.  (The library takes addresses: what does not fit is read or
+    written past its end.)"""
+
+    def __init__(self, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: int, device: int):
+        import torch
+        self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, n_kv_heads, head_dim
+        self.dtype = torch.bfloat16 if dtype == RAVEL_BF16 else torch.float32
+        self.int32, self.float32 = torch.int32, torch.float32
+        self.device = torch.device("cuda", device)
+        self.index = device
+
+    def rows(self, x, heads: int, name: str):
+        """Strides (robot, token) of a [batch, n, heads, head_dim] tensor whose heads are contiguous."""
+        shape = x.shape
+        if x.dtype is not self.dtype or len(shape) != 4 or shape[2] != heads or shape[3] != self.head_dim or \
+                x.get_device() != self.index:
+            raise ValueError(f"{name} must be [batch, n, {heads}, {self.head_dim}] of dtype {self.dtype} on {self.device}, "
+                             f"got {tuple(shape)} of {x.dtype} on {x.device}")
+        robot, token, head, dim = x.stride()
+        if dim != 1 or (head != self.head_dim and heads > 1):
+            raise ValueError(f"{name}: the heads of a token must be contiguous")
+        return robot, token
+
+    def ints(self, x, batch: int, name: str):
+        """Address of an int32 tensor [batch], or None."""
+        if x is None:
+            return None
+        if x.dtype is not self.int32 or x.shape != (batch,) or x.get_device() != self.index or not x.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous int32 tensor [{batch}] on {self.device}")
+        return x.data_ptr()
+
+    def mass(self, mass, batch):
+        """Address and length of a mass's rows."""
+        shape = mass.shape
+        if len(shape) != 3 or (batch is not None and shape[0] != batch) or shape[1] != self.n_kv_heads or \
+                mass.dtype is not self.float32 or mass.get_device() != self.index or not mass.is_contiguous():
+            raise ValueError(f"mass must be a contiguous float32 tensor [{'batch' if batch is None else batch}, "
+                             f"{self.n_kv_heads}, tokens] on {self.device}, got {tuple(shape)} of {mass.dtype}")
+        return mass.data_ptr(), shape[2]
+
+    def dense(self, x, shape: tuple, dtype, name: str):
+        """Address of a contiguous tensor of that shape, or None."""
+        if x is None:
+            return None
+        if x.dtype is not dtype or x.shape != shape or x.get_device() != self.index or not x.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous tensor {list(shape)} of dtype {dtype} on {self.device}, "
+                             f"got {tuple(x.shape)} of {x.dtype} on {x.device}")
+        return x.data_ptr()
 
 
-def _ints(t, batch: int, name: str):
-    """Device pointer of an int32 CUDA tensor [batch] (or None)."""
-    if t is None:
-        return None
-    if t.dtype.itemsize != 4 or t.dtype.is_floating_point or not t.is_cuda or t.shape != (batch,) or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 CUDA tensor [{batch}]")
-    return t.data_ptr()
+def _arguments(c) -> CacheArguments:
+    # (an attribute of the handle, not a class of its own, which ctypes takes 60 ns longer to pass)
+    a = getattr(c, "arguments", None)
+    if a is None:
+        raise ValueError("not a handle that ravel_cache_create returned")
+    return a
 
 
 def ravel_cache_create(layers: int, n_q_heads: int, n_kv_heads: int, head_dim: int, max_tokens: int, max_batch: int,
@@ -347,6 +385,7 @@ def ravel_cache_create(layers: int, n_q_heads: int, n_kv_heads: int, head_dim: i
     st = load().ravel_cache_create(C.byref(c), device, C.byref(h))
     if st != 0:
         raise RavelError(st, "ravel_cache_create failed (see stderr)")
+    h.arguments = CacheArguments(n_q_heads, n_kv_heads, head_dim, dtype, device)
     return h
 
 
@@ -360,50 +399,54 @@ def ravel_cache_reset(c):
 
 def ravel_cache_append(c, layer: int, k, v, starts=None, counts=None, stream=None):
     """k, v [B, n, Hkv, hd] with the same strides; see ravel_cache.h."""
-    B, n, heads, hd = k.shape
-    kp, rs, ts = _strided(k, k.dtype, heads, hd, "k")
-    vp, vrs, vts = _strided(v, k.dtype, heads, hd, "v")
-    if v.shape != k.shape or (vrs, vts) != (rs, ts):
+    a = _arguments(c)
+    rs, ts = a.rows(k, a.n_kv_heads, "k")
+    if v.shape != k.shape or a.rows(v, a.n_kv_heads, "v") != (rs, ts):
         raise ValueError("k and v must have the same shape and strides")
-    _check_cache(c, load().ravel_cache_append(c, layer, B, n, kp, vp, rs, ts, _ints(starts, B, "starts"),
-                                              _ints(counts, B, "counts"), _stream_ptr(stream)), "ravel_cache_append")
+    B, n = k.shape[:2]
+    _check_cache(c, load().ravel_cache_append(c, layer, B, n, k.data_ptr(), v.data_ptr(), rs, ts, a.ints(starts, B, "starts"),
+                                              a.ints(counts, B, "counts"), _stream_ptr(stream)), "ravel_cache_append")
 
 
 def ravel_cache_attend(c, layer: int, q, out, lengths, counts, max_length: int, causal: bool = True, window: int = 0,
                        sinks: int = 0, scale: float = 0.0, mass=None, add_mass: bool = False, stream=None):
     """q, out [B, n, Hq, hd]; mass float32 [B, Hkv, >= max_length] or None; see ravel_cache.h."""
-    B, n, heads, hd = q.shape
-    qp, qrs, qts = _strided(q, q.dtype, heads, hd, "q")
-    op, ors, ots = _strided(out, q.dtype, heads, hd, "out")
+    a = _arguments(c)
+    qrs, qts = a.rows(q, a.n_q_heads, "q")
+    ors, ots = a.rows(out, a.n_q_heads, "out")
     if out.shape != q.shape:
         raise ValueError("out must have q's shape")
+    B, n = q.shape[:2]
     if lengths is None:
         raise ValueError("lengths must be a contiguous int32 CUDA tensor")
-    mp, ms = None, 0
-    if mass is not None:
-        import torch
-        mp, ms = _dptr(mass, torch.float32, "mass"), mass.shape[-1]
-    _check_cache(c, load().ravel_cache_attend(c, layer, B, n, qp, qrs, qts, op, ors, ots, _ints(lengths, B, "lengths"),
-                                              _ints(counts, B, "counts"), max_length, int(causal), window, sinks, scale,
-                                              mp, ms, int(add_mass), _stream_ptr(stream)), "ravel_cache_attend")
+    mp, ms = a.mass(mass, B) if mass is not None else (None, 0)
+    _check_cache(c, load().ravel_cache_attend(c, layer, B, n, q.data_ptr(), qrs, qts, out.data_ptr(), ors, ots,
+                                              a.ints(lengths, B, "lengths"), a.ints(counts, B, "counts"), max_length,
+                                              int(causal), window, sinks, scale, mp, ms, int(add_mass), _stream_ptr(stream)),
+                 "ravel_cache_attend")
 
 
 def ravel_cache_evict(c, layer: int, to, to_layer: int, lengths, mass, keep: int, sinks: int, recent: int, new_lengths,
                       index, new_mass=None, stream=None):
-    """mass float32 [B, Hkv, tokens]; index int32 [B, Hkv, keep]; see ravel_cache.h."""
-    import torch
+    """mass float32 [B, Hkv, tokens]; index int32 and new_mass float32 [B, Hkv, keep]; see ravel_cache.h."""
+    a = _arguments(c)
+    _arguments(to)
+    mp, ms = a.mass(mass, None)
     B = mass.shape[0]
+    kept = (B, a.n_kv_heads, keep)
     _check_cache(c, load().ravel_cache_evict(
-        c, layer, to, to_layer, B, _ints(lengths, B, "lengths"), _dptr(mass, torch.float32, "mass"), mass.shape[-1], keep,
-        sinks, recent, _ints(new_lengths, B, "new_lengths"), _dptr(index, torch.int32, "index"),
-        _dptr(new_mass, torch.float32, "new_mass"), _stream_ptr(stream)), "ravel_cache_evict")
+        c, layer, to, to_layer, B, a.ints(lengths, B, "lengths"), mp, ms, keep, sinks, recent,
+        a.ints(new_lengths, B, "new_lengths"), a.dense(index, kept, a.int32, "index"),
+        a.dense(new_mass, kept, a.float32, "new_mass"), _stream_ptr(stream)), "ravel_cache_evict")
 
 
 def ravel_cache_read(c, layer: int, k, v, firsts=None, lengths=None, stream=None):
     """k, v [B, Hkv, n, hd], contiguous, written; see ravel_cache.h."""
+    a = _arguments(c)
+    if len(k.shape) != 4:
+        raise ValueError(f"k must be [batch, {a.n_kv_heads}, n, {a.head_dim}], got {tuple(k.shape)}")
     B, n = k.shape[0], k.shape[2]
-    if v.shape != k.shape or v.dtype != k.dtype:
-        raise ValueError("k and v must have the same shape and dtype")
-    _check_cache(c, load().ravel_cache_read(c, layer, B, n, _ints(firsts, B, "firsts"), _ints(lengths, B, "lengths"),
-                                            _dptr(k, name="k"), _dptr(v, name="v"), _stream_ptr(stream)),
-                 "ravel_cache_read")
+    held = (B, a.n_kv_heads, n, a.head_dim)
+    _check_cache(c, load().ravel_cache_read(c, layer, B, n, a.ints(firsts, B, "firsts"), a.ints(lengths, B, "lengths"),
+                                            a.dense(k, held, a.dtype, "k"), a.dense(v, held, a.dtype, "v"),
+                                            _stream_ptr(stream)), "ravel_cache_read")

@@ -32,6 +32,8 @@ class ContextCache:
         self.handle = B.ravel_cache_create(layers, n_q_heads, n_kv_heads, head_dim, max_tokens, max_batch, max_queries,
                                            B.RAVEL_BF16 if dtype == "bf16" else B.RAVEL_FP32, device)
         self._lib = B.load()
+        arguments = self.handle.arguments
+        self._rows, self._ints, self._mass = arguments.rows, arguments.ints, arguments.mass
         self._int32, self._float32 = torch.int32, torch.float32
         self._index, self._current_stream = self.device.index, B.current_stream_getter()
 
@@ -50,35 +52,6 @@ class ContextCache:
             stream = t.cuda.ExternalStream(int(stream), device=self.device)
         with t.cuda.stream(stream):
             return t.empty(shape, dtype=dtype, device=self.device)
-
-    def _rows(self, x, heads, name):
-        """Strides (robot, token) of a [batch, n, heads, head_dim] tensor whose heads are contiguous."""
-        shape = x.shape
-        if x.dtype is not self.dtype or len(shape) != 4 or shape[2] != heads or shape[3] != self.head_dim or \
-                x.get_device() != self._index:
-            raise ValueError(f"{name} must be [batch, n, {heads}, {self.head_dim}] of dtype {self.dtype} on {self.device}, "
-                             f"got {tuple(shape)} of {x.dtype} on {x.device}")
-        robot, token, head, dim = x.stride()
-        if dim != 1 or (head != self.head_dim and heads > 1):
-            raise ValueError(f"{name}: the heads of a token must be contiguous")
-        return robot, token
-
-    def _ints(self, x, batch, name):
-        """Address of an int32 tensor [batch], or None."""
-        if x is None:
-            return None
-        if x.dtype is not self._int32 or x.shape != (batch,) or x.get_device() != self._index or not x.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous int32 tensor [{batch}] on {self.device}")
-        return x.data_ptr()
-
-    def _mass(self, mass, batch):
-        """Address and length of a mass's rows."""
-        shape = mass.shape
-        if len(shape) != 3 or (batch is not None and shape[0] != batch) or shape[1] != self.n_kv_heads or \
-                mass.dtype is not self._float32 or mass.get_device() != self._index or not mass.is_contiguous():
-            raise ValueError(f"mass must be a contiguous float32 tensor [{'batch' if batch is None else batch}, "
-                             f"{self.n_kv_heads}, tokens] on {self.device}, got {tuple(shape)} of {mass.dtype}")
-        return mass.data_ptr(), shape[2]
 
     # -- calls
     def append(self, layer: int, k, v, starts=None, counts=None, stream=None):

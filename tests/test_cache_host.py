@@ -81,3 +81,94 @@ def test_binding_refuses_tensors_of_the_wrong_kind(lib):
         ravel_cache_append(handle, 0, k, k)
     with pytest.raises(ValueError):
         ravel_cache_attend(handle, 0, k, k, None, None, 2)
+
+
+class _Gpu:
+    """Stands in for a CUDA tensor: all that the calls look at, none of the memory."""
+    is_cuda = True
+
+    def __init__(self, shape, dtype, stride=None, device=0):
+        self.shape, self.dtype, self.device, self._device = torch.Size(shape), dtype, torch.device("cuda", device), device
+        dense = [1]
+        for n in reversed(shape[1:]):
+            dense.insert(0, dense[0] * n)
+        self._stride = tuple(stride or dense)
+        self._dense = self._stride == tuple(dense)
+
+    def stride(self):
+        return self._stride
+
+    def get_device(self):
+        return self._device
+
+    def is_contiguous(self):
+        return self._dense
+
+    def data_ptr(self):
+        return 256
+
+
+def test_calls_on_a_handle_check_their_tensors_against_the_cache(lib):
+    """What does not fit the cache would be read or written past its end: it is
+    refused before the library is called (whose refusal of the null handle is a
+    RavelError)."""
+    import paper_2609_34170_gb300 as pkg
+    from paper_2609_34170_gb300 import _binding as B
+    c, to = C.c_void_p(), C.c_void_p()
+    for h in (c, to):
+        h.arguments = B.CacheArguments(n_q_heads=4, n_kv_heads=2, head_dim=64, dtype=B.RAVEL_BF16, device=0)
+    b16, f32, i32, u32 = torch.bfloat16, torch.float32, torch.int32, torch.uint32
+    k, q, ints = _Gpu((3, 5, 2, 64), b16), _Gpu((3, 5, 4, 64), b16), _Gpu((3,), i32)
+    mass, held = _Gpu((3, 2, 40), f32), _Gpu((3, 2, 9, 64), b16)
+    index, new_mass = _Gpu((3, 2, 8), i32), _Gpu((3, 2, 8), f32)
+
+    def append(h=c, k=k, v=None, starts=None, counts=None):
+        pkg.ravel_cache_append(h, 0, k, v or k, starts, counts, stream=0)
+
+    def attend(h=c, q=q, out=None, lengths=ints, counts=None, mass=None):
+        pkg.ravel_cache_attend(h, 0, q, out or q, lengths, counts, 40, mass=mass, stream=0)
+
+    def evict(h=c, to=to, lengths=ints, mass=mass, new_lengths=ints, index=index, new_mass=new_mass):
+        pkg.ravel_cache_evict(h, 0, to, 0, lengths, mass, 8, 1, 1, new_lengths, index, new_mass, stream=0)
+
+    def read(h=c, k=held, v=None, firsts=None, lengths=None):
+        pkg.ravel_cache_read(h, 0, k, v or k, firsts, lengths, stream=0)
+
+    for call in (append, attend, evict, read):   # what fits goes to the library
+        with pytest.raises(B.RavelError) as ei:
+            call()
+        assert ei.value.status == 1
+        with pytest.raises(ValueError):
+            call(h=C.c_void_p())
+    wrong_ints = [_Gpu((2,), i32), _Gpu((3,), u32), _Gpu((3,), f32), _Gpu((3,), i32, (2,)), _Gpu((3,), i32, device=1)]
+    for bad in (_Gpu((3, 5, 2, 64), f32), _Gpu((3, 5, 1, 64), b16), _Gpu((3, 5, 2, 32), b16), _Gpu((3, 5, 128), b16),
+                _Gpu((3, 5, 2, 64), b16, device=1), _Gpu((3, 5, 2, 64), b16, (640, 64, 320, 1))):
+        for args in (dict(k=bad), dict(v=bad)):
+            with pytest.raises(ValueError):
+                append(**args)
+    for bad in (_Gpu((3, 5, 4, 64), f32), _Gpu((3, 5, 3, 64), b16), _Gpu((3, 5, 4, 72), b16), _Gpu((3, 5, 4, 64), b16, device=1)):
+        for args in (dict(q=bad), dict(out=bad)):
+            with pytest.raises(ValueError):
+                attend(**args)
+    for bad in (_Gpu((2, 2, 40), f32), _Gpu((3, 1, 40), f32), _Gpu((3, 2, 40), b16), _Gpu((6, 40), f32),
+                _Gpu((3, 2, 40), f32, (160, 80, 2))):
+        with pytest.raises(ValueError):
+            attend(mass=bad)
+        with pytest.raises(ValueError):
+            evict(mass=bad)
+    for bad in (_Gpu((3, 2, 7), i32), _Gpu((3, 1, 8), i32), _Gpu((3, 2, 8), f32), _Gpu((2, 2, 8), i32)):
+        with pytest.raises(ValueError):
+            evict(index=bad)
+    for bad in (_Gpu((3, 2, 7), f32), _Gpu((3, 2, 8), i32)):
+        with pytest.raises(ValueError):
+            evict(new_mass=bad)
+    for bad in (_Gpu((3, 2, 9, 64), f32), _Gpu((3, 1, 9, 64), b16), _Gpu((3, 2, 9, 32), b16), _Gpu((3, 2, 576), b16)):
+        for args in (dict(k=bad), dict(v=bad)):
+            with pytest.raises(ValueError):
+                read(**args)
+    for bad in wrong_ints:
+        for call, names in ((append, ("starts", "counts")), (attend, ("lengths", "counts")), (evict, ("lengths", "new_lengths")),
+                            (read, ("firsts", "lengths"))):
+            for name in names:
+                with pytest.raises(ValueError):
+                    call(**{name: bad})

@@ -492,3 +492,31 @@ def test_refusals():
     refused(7, lambda: c.read(0, 2, 4))
     c.reset()
     assert torch.equal(c.attend(0, q, L), want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_calls_on_a_handle_do_what_the_class_does(dtype):
+    import paper_2609_34170_gb300 as pkg
+    batch, n, hq, hkv, hd, keep = 2, 21, 6, 2, 40, 13
+    k, v = _rand((batch, 30, hkv, hd), 1, dtype), _rand((batch, 30, hkv, hd), 2, dtype)
+    q, lengths = _rand((batch, n, hq, hd), 3, dtype, 2.0), _ints([30, 22])
+    cache, small = (pkg.ContextCache(2, hq, hkv, hd, t, batch, n, dtype) for t in (40, keep))
+    cache.append(1, k, v, counts=lengths)
+    mass = torch.zeros((batch, hkv, 40), device="cuda")
+    want = [cache.attend(1, q, lengths, window=9, sinks=2, mass=mass), mass]
+    want += cache.evict(1, small, 0, lengths, mass, keep, 2, 3)
+    want += small.read(0, batch, keep, lengths=want[2])
+    kind = pkg.RAVEL_BF16 if dtype == "bf16" else pkg.RAVEL_FP32
+    c, to = (pkg.ravel_cache_create(2, hq, hkv, hd, t, batch, n, kind) for t in (40, keep))
+    try:
+        got = [torch.empty_like(t) for t in want]
+        pkg.ravel_cache_append(c, 1, k, v, counts=lengths)
+        pkg.ravel_cache_attend(c, 1, q, got[0], lengths, None, 40, window=9, sinks=2, mass=got[1])
+        pkg.ravel_cache_evict(c, 1, to, 0, lengths, got[1], keep, 2, 3, got[2], got[3], got[4])
+        pkg.ravel_cache_read(to, 0, got[5], got[6], lengths=got[2])
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+    finally:
+        torch.cuda.synchronize()
+        pkg.ravel_cache_destroy(c)
+        pkg.ravel_cache_destroy(to)
