@@ -67,6 +67,37 @@ __device__ __forceinline__ uint4 f32_to_e4m3x16(const float* x, float scale) {
   return make_uint4(u[0], u[1], u[2], u[3]);
 }
 
+// What the launch before wrote, or other CTAs of this one, is read by plain loads or by these:
+// launches overlap, so that no tensor is read-only for as long as a kernel lives, and a load
+// of the read-only path (or one that the compiler takes for a pure function) might be older
+// than the wait in front of it (volatile statements stay in their order, the wait's among them).
+// l2: past the L1; once: read only once; kept: read by many warps of a CTA
+__device__ __forceinline__ float ld_l2(const float* p) {
+  float v;
+  asm volatile("ld.global.cg.f32 %0, [%1];" : "=f"(v) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ float2 ld_l2(const float2* p) {
+  float2 v;
+  asm volatile("ld.global.cg.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ float4 ld_l2(const float4* p) {
+  float4 v;
+  asm volatile("ld.global.cg.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ float2 ld_once(const float2* p) {
+  float2 v;
+  asm volatile("ld.global.cs.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ float2 ld_kept(const float2* p) {
+  float2 v;
+  asm volatile("ld.global.L1::evict_last.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "l"(p));
+  return v;
+}
+
 // 16 values of a row from dim d on (zeros from hd on; hd is a multiple of 8)
 template <typename T>
 __device__ __forceinline__ void load16(const T* row, int d, int hd, int vec, float* x) {
@@ -80,7 +111,7 @@ __device__ __forceinline__ void load16(const T* row, int d, int hd, int vec, flo
       constexpr int NV = 8 * sizeof(T) / 16;
       uint4 w[NV];
 #pragma unroll
-      for (int i = 0; i < NV; ++i) w[i] = __ldg((const uint4*)(row + d8) + i);
+      for (int i = 0; i < NV; ++i) w[i] = *((const uint4*)(row + d8) + i);
       const T* p = (const T*)w;
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[8 * h + i] = to_f32(p[i]);

@@ -332,9 +332,9 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
 
   // the exponents of a unit's blocks, one byte each
   auto exps_of = [&](const int8_t* e, int j0) -> uint32_t {
-    if (NT == 4) return __ldg((const uint32_t*)(e + j0 / 16));
-    if (NT == 2) return __ldg((const uint16_t*)(e + j0 / 16));
-    return (uint8_t)__ldg(e + j0 / 16);
+    if (NT == 4) return *(const uint32_t*)(e + j0 / 16);
+    if (NT == 2) return *(const uint16_t*)(e + j0 / 16);
+    return (uint8_t)e[j0 / 16];
   };
   int u = u0 + warp;
   uint32_t kes = 0u, ves = 0u;
@@ -804,7 +804,7 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
   // the splits' (max, sum), all on their way together, then their weights in their place
   float2* wts = (float2*)joint;   // [splits][16]
   for (int w = threadIdx.x; w < a.splits * 16; w += RW * 32)
-    if (w % 16 < rows) wts[w] = __ldcg(a.part_ml + unit * a.splits * 16 + w);
+    if (w % 16 < rows) wts[w] = ld_l2(a.part_ml + unit * a.splits * 16 + w);
   __syncthreads();
   if ((int)threadIdx.x < rows) {
     const int row = threadIdx.x;
@@ -828,7 +828,7 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 8
     for (int q = 0; q < a.splits; ++q) {
-      const float4 x = __ldcg((const float4*)(p0 + ((size_t)q * 16 + row) * HDP + d));
+      const float4 x = ld_l2((const float4*)(p0 + ((size_t)q * 16 + row) * HDP + d));
       const float wt = wts[q * 16 + row].x;   // (0 times an empty split's zeros)
       acc.x += wt * x.x;
       acc.y += wt * x.y;
@@ -864,7 +864,7 @@ __global__ void __launch_bounds__(1024) cache_mass_scores_kernel(CacheAttnArgs a
       if (!s0 && !s1) continue;
 #pragma unroll 4
       for (int g = 0; g < a.G; ++g) {
-        const float2 x = __ldcs((const float2*)(sc + (size_t)((i - a.i0) * a.G + g) * a.mass_pitch)), y = __ldg(ml + i * a.G + g);
+        const float2 x = ld_once((const float2*)(sc + (size_t)((i - a.i0) * a.G + g) * a.mass_pitch)), y = ld_kept(ml + i * a.G + g);
         v0 += s0 ? exp2f(x.x - y.x) * y.y : 0.f;
         v1 += s1 ? exp2f(x.y - y.x) * y.y : 0.f;
       }

@@ -851,7 +851,7 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
         const float2* ml = a.part_ml + unit * a.splits * BM + rr;
         const uint32_t xml = smem_u32(xm) + 8u * rr;
         auto split_ml = [&](int q) {
-          if (!cluster) return __ldcg(ml + q * BM);
+          if (!cluster) return ld_l2(ml + q * BM);
           const uint32_t at = mapa_shared(xml, (uint32_t)q);
           return make_float2(ld_cluster_f1(at), ld_cluster_f1(at + 4));
         };
@@ -884,8 +884,8 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
               y1 = ld_cluster_f4(at + 16);
             } else {
               const float4* y = (const float4*)(p0 + (size_t)q * BM * HDP);
-              y0 = __ldcg(y);
-              y1 = __ldcg(y + 1);
+              y0 = ld_l2(y);
+              y1 = ld_l2(y + 1);
             }
             acc[0] = fmaf(wt, y0.x, acc[0]);
             acc[1] = fmaf(wt, y0.y, acc[1]);

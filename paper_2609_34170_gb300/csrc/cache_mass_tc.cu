@@ -278,7 +278,7 @@ __global__ void __launch_bounds__(256) cache_mass_sum_kernel(CacheAttnArgs a) {
   const float* part = a.mass_ws + head * a.splits * 2 * a.mass_pitch + j;   // (j < pitch, a multiple of 32)
   float v = 0.f;
 #pragma unroll 8
-  for (int c = eighth; c < 2 * a.splits; c += 8) v += __ldcg(part + (size_t)c * a.mass_pitch);
+  for (int c = eighth; c < 2 * a.splits; c += 8) v += ld_l2(part + (size_t)c * a.mass_pitch);
   sums[eighth][lane] = v;
   __syncthreads();
   if (eighth || j >= a.max_length) return;

@@ -234,11 +234,19 @@ __global__ void __launch_bounds__(kSelThreads) cache_select_kernel(EvictArgs a, 
       // (two histograms in turn: a CTA may still read this one's while its neighbours are at the next)
       if (tid < 256) hist[buf][tid] = 0u;
       __syncthreads();
-#pragma unroll 8
-      for (int j = m0 + tid; j < m1; j += kSelThreads) {
-        const uint32_t key = mass_key(__ldg(mass + j));
+      auto count = [&](float m) {
+        const uint32_t key = mass_key(m);
         if ((key & mask) == prefix) atomicAdd(&hist[buf][(key >> shift) & 255u], 1u);
+      };
+      int j = m0 + tid;
+      for (; j + 7 * kSelThreads < m1; j += 8 * kSelThreads) {
+        float x[8];   // (all on their way together)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) x[q] = mass[j + q * kSelThreads];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) count(x[q]);
       }
+      for (; j < m1; j += kSelThreads) count(mass[j]);
       if (ctas > 1) cluster_sync();
       else __syncthreads();
       if (tid < 256) {
@@ -297,8 +305,8 @@ __global__ void __launch_bounds__(kSelThreads) cache_select_kernel(EvictArgs a, 
     }
   }
   // which tokens are surely in (heavier, first, last), and which are ties
-  auto kind = [&](int j, float& m, bool& in, bool& tie) {
-    m = j < r1 ? __ldg(mass + j) : 0.f;
+  auto load = [&](int j) { return j < r1 ? mass[j] : 0.f; };
+  auto kind = [&](int j, float m, bool& in, bool& tie) {
     const uint32_t key = mass_key(m);
     const bool always = j < r1 && (j < lo || j >= hi), mid = j >= m0 && j < m1;
     in = always || (mid && key > prefix);
@@ -311,9 +319,8 @@ __global__ void __launch_bounds__(kSelThreads) cache_select_kernel(EvictArgs a, 
     unsigned n0 = 0, n1 = 0;
 #pragma unroll 4
     for (int j = r0 + tid; j < r1; j += kSelThreads) {
-      float m;
       bool in, tie;
-      kind(j, m, in, tie);
+      kind(j, load(j), in, tie);
       n0 += in;
       n1 += tie;
     }
@@ -338,10 +345,7 @@ __global__ void __launch_bounds__(kSelThreads) cache_select_kernel(EvictArgs a, 
   }
   // kept before j: those surely in and as many ties as still fit
   int buf = 0;
-#pragma unroll 4
-  for (int base = r0; base < r1; base += kSelThreads, buf ^= 1) {
-    const int j = base + tid;
-    float m;
+  auto place = [&](int j, float m) {   // (every thread; j from r1 on: nothing)
     bool in, tie;
     kind(j, m, in, tie);
     const unsigned bi = __ballot_sync(0xffffffffu, in), bt = __ballot_sync(0xffffffffu, tie);
@@ -365,7 +369,17 @@ __global__ void __launch_bounds__(kSelThreads) cache_select_kernel(EvictArgs a, 
     }
     sure += all & 0xffffu;
     ties += all >> 16;
+    buf ^= 1;
+  };
+  int base = r0;
+  for (; base + 3 * kSelThreads < r1; base += 4 * kSelThreads) {
+    float m[4];   // (loads ahead of the turns' barriers)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) m[q] = load(base + q * kSelThreads + tid);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) place(base + q * kSelThreads + tid, m[q]);
   }
+  for (; base < r1; base += kSelThreads) place(base + tid, load(base + tid));
   if (ctas > 1) cluster_sync();   // nobody leaves while its counts are read
 }
 

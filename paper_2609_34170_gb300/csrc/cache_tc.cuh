@@ -183,7 +183,7 @@ __device__ __forceinline__ void stage_q8(const CacheAttnArgs& a, const Sight& s,
   }
   if (a.vec) {
 #pragma unroll
-    for (int p = 0; p < PASS; ++p) x[p] = __ldg((const uint4*)at[p]);
+    for (int p = 0; p < PASS; ++p) x[p] = *(const uint4*)at[p];
   } else {
 #pragma unroll
     for (int p = 0; p < PASS; ++p) {

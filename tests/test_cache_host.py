@@ -172,3 +172,23 @@ def test_calls_on_a_handle_check_their_tensors_against_the_cache(lib):
             for name in names:
                 with pytest.raises(ValueError):
                     call(**{name: bad})
+
+
+def test_kernels_that_overlap_their_predecessors_read_nothing_as_constant():
+    """The cache's launches start before the ones before them end, which may write
+    what they read: no load may take the read-only path or pass the wait in front
+    of it (those of the read-only kind, restrict pointers, loads that the compiler
+    takes for pure functions)."""
+    import glob
+    import os
+
+    from paper_2609_34170_gb300.build import CSRC
+    files = glob.glob(os.path.join(CSRC, "cache*.cu*"))
+    assert len(files) >= 6
+    for path in files:
+        with open(path) as f:
+            text = f.read()
+        for word in ("__ldg(", "__ldcg(", "__ldcs(", "__ldca(", "ld.global.nc", "__restrict__"):
+            assert word not in text, (os.path.basename(path), word)
+        for line in text.splitlines():
+            assert "ld.global" not in line or "asm volatile" in line, line
