@@ -49,7 +49,7 @@ typedef struct {
   int n_q_heads;    /* Hq, a multiple of n_kv_heads */
   int n_kv_heads;   /* Hkv */
   int head_dim;     /* hd, a multiple of 8, at most 256 (rows are held in 64, 128, 192 or 256 bytes) */
-  int max_tokens;   /* tokens per robot */
+  int max_tokens;   /* tokens per robot; max_batch * n_kv_heads * max_tokens is below 2^31 - 2^16 */
   int max_batch;    /* robots */
   int max_queries;  /* largest n of ravel_cache_attend */
   int dtype;        /* RAVEL_BF16 or RAVEL_FP32: type of the keys, values, queries and outputs of every call.

@@ -83,9 +83,10 @@ const char* config_fault(const ravel_cache_config& c) {
   if (c.head_dim < 8 || c.head_dim % 8 || c.head_dim > 256) return "head_dim must be a multiple of 8, at most 256";
   if (c.dtype != RAVEL_FP32 && c.dtype != RAVEL_BF16) return "unknown dtype";
   if (c.n_kv_heads > 65535 || c.max_batch > 65535) return "at most 65535 KV heads and robots";
-  // (rows of a layer are counted in 32 bits; the product of three 32-bit sizes could pass 64)
-  if ((double)c.max_batch * c.n_kv_heads * ((double)c.max_tokens + kCacheRound) > 2147483647.0)
-    return "max_batch * n_kv_heads * max_tokens must be below 2^31";
+  // (rows of a layer are counted in 32 bits, and what a CTA steps past the last one as well; the
+  // product of three 32-bit sizes could pass 64)
+  if ((double)c.max_batch * c.n_kv_heads * ((double)c.max_tokens + kCacheRound) > 2147483648.0 - 65536.0)
+    return "max_batch * n_kv_heads * max_tokens must be below 2^31 - 2^16";
   if ((long long)c.max_queries * c.n_q_heads > (1 << 30)) return "max_queries * n_q_heads must be at most 2^30";
   return nullptr;
 }

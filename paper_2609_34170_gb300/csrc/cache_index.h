@@ -24,4 +24,25 @@ RAVEL_HD LoadsLeft loads_left(int at, int loads, int slots) {
   return LoadsLeft{at, at + slots < loads ? at + slots : loads};
 }
 
+// Of the 64 rows from `first` on, those that see token j: lo .. hi - 1 of them (lo may be -1, for
+// "all from before").  Row r is query r / G at position p0 + r / G of a robot with `len` tokens
+// and rows below end_row.  A window reaches as far as the tokens do, so that its end may pass 32
+// bits.
+struct RowsThatSee {
+  int lo, hi;
+};
+RAVEL_HD RowsThatSee rows_that_see(int j, int len, int p0, int G, int end_row, int causal, int window, int sinks, int first) {
+  long long lo = 0, hi = j < len ? end_row : 0;
+  if (causal) {
+    lo = ((long long)j - p0) * G;
+    if (window > 0 && j >= sinks) {
+      const long long behind = ((long long)j + window - p0) * G;
+      hi = behind < hi ? behind : hi;
+    }
+  }
+  lo -= first;
+  hi -= first;
+  return RowsThatSee{(int)(lo < -1 ? -1 : (lo > 64 ? 64 : lo)), (int)(hi < 0 ? 0 : (hi > 64 ? 64 : hi))};
+}
+
 }  // namespace ravel

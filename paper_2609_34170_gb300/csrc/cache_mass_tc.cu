@@ -17,6 +17,7 @@
 // beside 38 for the attention.
 #include <algorithm>
 
+#include "cache_index.h"
 #include "cache_tc.cuh"
 #include "launch.h"
 
@@ -71,7 +72,7 @@ __global__ void __launch_bounds__(MT, 1) cache_mass_tc_kernel(const __grid_const
   const int rt0 = (int)((long long)a.row_tiles * chunk / a.splits);
   const int rt1 = s.len == 0 ? rt0 : min((int)((long long)a.row_tiles * (chunk + 1) / a.splits), (end_row + BM - 1) / BM);
   float* part = a.mass_ws + (size_t)blockIdx.x * 2 * a.mass_pitch;
-  for (int x = threadIdx.x; x < 2 * a.mass_pitch; x += MT) part[x] = 0.f;
+  for (long long x = threadIdx.x; x < 2 * a.mass_pitch; x += MT) part[x] = 0.f;
   if (rt0 >= rt1) return;
   if (q0 & 1023u) {   // (the swizzled layouts count on it)
     if (threadIdx.x == 0) raise_error(a.err, ERR_SHAPE);
@@ -207,14 +208,8 @@ __global__ void __launch_bounds__(MT, 1) cache_mass_tc_kernel(const __grid_const
       for (int i = 0; i < sg.units; ++i, ++g) {
         const int j0 = token(sg, i), j = j0 + t;
         const float old = own[j0], kf = exp2i(KE[j / 16]);
-        // the rows of this half that see the token: lo .. hi - 1
-        long long lo = 0, hi = j < s.len ? end_row : 0;
-        if (a.causal) {
-          lo = (long long)(j - s.p0) * a.G;
-          if (a.window > 0 && j >= a.sinks) hi = min(hi, (long long)(j + a.window - s.p0) * a.G);
-        }
-        const int rlo = (int)max(lo - first, -1ll), rhi = (int)max(min(hi - first, 64ll), 0ll);
-        const bool full = __all_sync(0xffffffffu, rlo <= 0 && rhi >= 64);
+        const RowsThatSee rows = rows_that_see(j, s.len, s.p0, a.G, end_row, a.causal, a.window, a.sinks, first);
+        const bool full = __all_sync(0xffffffffu, rows.lo <= 0 && rows.hi >= 64);
         if (ok) ok = wait_phase(&s_full[g & 1], (uint32_t)(g >> 1) & 1u);
         tc_fence_after();
         float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
@@ -244,7 +239,7 @@ __global__ void __launch_bounds__(MT, 1) cache_mass_tc_kernel(const __grid_const
           if (full) {
             add([](int) { return false; });
           } else {
-            const uint32_t see = RowMask::below(rhi - 32 * c) & ~RowMask::below(rlo - 32 * c);
+            const uint32_t see = RowMask::below(rows.hi - 32 * c) & ~RowMask::below(rows.lo - 32 * c);
             add([see](int k) { return (see & (1u << k)) == 0u; });
           }
         }

@@ -192,3 +192,15 @@ def test_kernels_that_overlap_their_predecessors_read_nothing_as_constant():
             assert word not in text, (os.path.basename(path), word)
         for line in text.splitlines():
             assert "ld.global" not in line or "asm volatile" in line, line
+
+
+def test_create_refuses_positions_that_could_pass_32_bits(lib):
+    """A CTA steps up to 2^14 tokens past the last one."""
+    from paper_2609_34170_gb300 import RavelError, ravel_cache_create
+    for batch, heads in ((1, 1), (2, 4)):
+        most = (2 ** 31 - 2 ** 16) // (batch * heads) - 128
+        for tokens in (most + 1, most + 2 ** 15 // (batch * heads), 2 ** 31 // (batch * heads) - 129):
+            with pytest.raises(RavelError) as ei:
+                ravel_cache_create(layers=1, n_q_heads=4, n_kv_heads=heads, head_dim=64, max_tokens=tokens, max_batch=batch,
+                                   max_queries=1)
+            assert ei.value.status == 2

@@ -82,3 +82,47 @@ def test_the_kernel_for_few_rows_issues_nothing_after_a_wait_ran_out():
     wait, issue = body.index("if (!wait_phase(&arrived[warp][slot], phase))"), body.index("fetch(u + RW * D, slot)")
     drain = body.index("loads_left((u - u0 - warp) / RW")
     assert wait < drain < body.index("break;", drain) < issue and body.count("wait_phase(") == 1
+
+
+# Against each row's own definition, in 64 bits.
+ROWS = r"""
+struct Case { int len, count, G, causal, window, sinks; };
+int main() {
+  const int big = 2147483647 - 65536 - 128, half = 1 << 30;
+  const Case cases[] = {
+      {300, 200, 8, 1, 0, 0}, {300, 300, 1, 1, 50, 4}, {300, 40, 20, 0, 0, 0}, {130, 130, 3, 1, 1, 0}, {130, 7, 64, 1, 130, 9},
+      {half + 5, 300, 4, 1, half, 4}, {big, 200, 8, 1, big, 0}, {big, 129, 1, 1, big - 1, 4}, {big, 1, 1000, 1, 3, big},
+      {big, 1, half, 1, big, 0}, {2 * (half / 2) + 77, 64, 16, 1, half / 2 + 9, 20}, {big, 300, 2, 0, 0, 0}};
+  srand(1);
+  long long checks = 0;
+  for (const Case& c : cases) {
+    const int p0 = c.len - c.count, end_row = c.count * c.G;
+    for (int t = 0; t < 4000; ++t) {
+      // tokens at the ends, at the window's edges and anywhere (up to the end of the last tile)
+      const int near = rand() % 300 - 150;
+      long long jj = t % 5 == 0 ? near : t % 5 == 1 ? (long long)c.len + near : t % 5 == 2 ? (long long)p0 + near
+                   : t % 5 == 3 ? (long long)p0 - c.window + near : (long long)rand() % c.len;
+      if (jj < 0 || jj >= (long long)c.len + 127) continue;
+      const int j = (int)jj, first = end_row > 64 ? rand() % end_row / 64 * 64 : 0;
+      const RowsThatSee got = rows_that_see(j, c.len, p0, c.G, end_row, c.causal, c.window, c.sinks, first);
+      if (got.lo < -1 || got.lo > 64 || got.hi < 0 || got.hi > 64) return printf("range"), 1;
+      for (int k = 0; k < 64; ++k) {
+        const long long r = (long long)first + k, p = p0 + r / c.G;
+        bool see = r < end_row && j < c.len;
+        if (c.causal) see = see && j <= p && (c.window == 0 || j > p - c.window || j < c.sinks);
+        if (see != (k >= got.lo && k < got.hi)) {
+          printf("len %d count %d G %d window %d sinks %d: token %d row %lld\n", c.len, c.count, c.G, c.window, c.sinks, j, r);
+          return 1;
+        }
+        ++checks;
+      }
+    }
+  }
+  printf("%lld\n", checks);
+  return 0;
+}
+"""
+
+
+def test_rows_that_see_a_token_at_any_position(run):
+    assert int(run(ROWS)[0]) > 1000000
