@@ -42,6 +42,7 @@
 // shared memory (without MMAs and widening 2220).
 #include <algorithm>
 
+#include "cache_index.h"
 #include "cache_tc.cuh"
 #include "launch.h"
 
@@ -126,8 +127,7 @@ struct Item {
   int t0, n;         // tiles t0 .. t0 + n - 1 of the sight's units
   int hi;            // tokens from here on are nobody's
   __device__ __forceinline__ int token(int i) const {
-    const int t = t0 + i;
-    return (t < s.sink_units ? t : t - s.sink_units + s.from) * BT;
+    return unit_place(t0 + i, s.sink_units, s.from) * BT;
   }
   // tokens of tile i that exist for these rows, in groups of 16
   __device__ __forceinline__ int groups(int i) const { return (min(BT, hi - token(i)) + 15) >> 4; }
@@ -474,10 +474,12 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
         const Item it = item_of(a, w);
         const int y0 = it.head * L.T, n = uniform(it.n);
         // a (robot, KV head)'s codes come to L2 as its first items begin, up to 256 KB of them
-        // (its row tiles ask for the same lines at the same time)
+        // (its row tiles ask for the same lines at the same time); of a window behind sinks the
+        // longer of the two, as a rule the window
         if (it.n > 0 && (it.tile & 7) == 0 && el) {
-          const size_t from = ((size_t)y0 + it.token(0)) * HDP;
-          prefetch_l2_bulk((is_k ? L.k : L.v) + from, (uint32_t)min((size_t)it.n * BT * HDP, (size_t)(256 << 10)));
+          const UnitRun run = longest_run(it.t0, it.n, it.s.sink_units, it.s.from);
+          const size_t from = ((size_t)y0 + (size_t)run.at * BT) * HDP;
+          prefetch_l2_bulk((is_k ? L.k : L.v) + from, (uint32_t)min((size_t)run.units * BT * HDP, (size_t)(256 << 10)));
         }
         // K: a tile's units of 64 dims; V: its halves of 64 tokens, each NB blocks of 64 dims
         const int halves = uniform(it.halves());

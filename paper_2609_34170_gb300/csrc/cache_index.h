@@ -45,4 +45,17 @@ RAVEL_HD RowsThatSee rows_that_see(int j, int len, int p0, int G, int end_row, i
   return RowsThatSee{(int)(lo < -1 ? -1 : (lo > 64 ? 64 : lo)), (int)(hi < 0 ? 0 : (hi > 64 ? 64 : hi))};
 }
 
+// Unit t of what a tile of rows sees: the first sink_units, then the window's from unit `from` on.
+RAVEL_HD int unit_place(int t, int sink_units, int from) { return t < sink_units ? t : t - sink_units + from; }
+
+// The longest run of neighbours among units t0 .. t0 + n - 1: where it begins and its units.
+struct UnitRun {
+  int at, units;
+};
+RAVEL_HD UnitRun longest_run(int t0, int n, int sink_units, int from) {
+  if (sink_units == from) return UnitRun{t0, n};   // (no gap between the sinks and the window)
+  const int sinks = sink_units <= t0 ? 0 : (sink_units - t0 < n ? sink_units - t0 : n);
+  return sinks > n - sinks ? UnitRun{t0, sinks} : UnitRun{unit_place(t0 + sinks, sink_units, from), n - sinks};
+}
+
 }  // namespace ravel

@@ -126,3 +126,42 @@ int main() {
 
 def test_rows_that_see_a_token_at_any_position(run):
     assert int(run(ROWS)[0]) > 1000000
+
+
+# What is prefetched is what is read: the longest run of the units that an item walks.
+RUN = r"""
+int main() {
+  int cases = 0;
+  for (int from = 0; from < 9; ++from)
+    for (int sinks = 0; sinks <= from; ++sinks)
+      for (int window = 0; window < 6; ++window)
+        for (int t0 = 0; t0 < sinks + window; ++t0)
+          for (int n = 1; t0 + n <= sinks + window; ++n) {
+            int best = 0, begin = 0;
+            for (int i = 0; i < n; ++i) {
+              const int at = unit_place(t0 + i, sinks, from);
+              if (at != (t0 + i < sinks ? t0 + i : from + t0 + i - sinks)) return printf("place"), 1;
+              if (i == 0 || at != unit_place(t0 + i - 1, sinks, from) + 1) begin = i;
+              best = i - begin + 1 > best ? i - begin + 1 : best;
+            }
+            const UnitRun run = longest_run(t0, n, sinks, from);
+            bool found = false;
+            for (int i = 0; i + run.units <= n; ++i) {
+              bool same = true;
+              for (int k = 0; k < run.units; ++k) same = same && unit_place(t0 + i + k, sinks, from) == run.at + k;
+              found = found || same;
+            }
+            if (run.units != best || !found) {
+              printf("sinks %d from %d t0 %d n %d: %d units at %d, longest %d\n", sinks, from, t0, n, run.units, run.at, best);
+              return 1;
+            }
+            ++cases;
+          }
+  printf("%d\n", cases);
+  return 0;
+}
+"""
+
+
+def test_the_longest_run_of_an_items_units(run):
+    assert int(run(RUN)[0]) > 500
