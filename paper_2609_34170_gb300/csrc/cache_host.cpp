@@ -52,6 +52,7 @@ ravel_status fail(ravel_cache_t* c, ravel_status s, const char* msg) {
 
 ravel_status cuda_fail(ravel_cache_t* c, cudaError_t e, const char* what) {
   char buf[160];
+  cudaGetLastError();   // (reported here: the step's launches ask for the last error)
   snprintf(buf, sizeof buf, "%s: %s", what, cudaGetErrorString(e));
   return fail(c, e == cudaErrorMemoryAllocation ? RAVEL_ENOMEM : RAVEL_ECUDA, buf);
 }
@@ -165,6 +166,7 @@ ravel_status ravel_cache_create(const ravel_cache_config* cfg, int device, ravel
   if (e != cudaSuccess) {
     fprintf(stderr, "ravel_cache_create: %s: %s\n", what, cudaGetErrorString(e));
     ravel_cache_destroy(c);
+    cudaGetLastError();   // (as in cuda_fail)
     return e == cudaErrorMemoryAllocation ? RAVEL_ENOMEM : RAVEL_ECUDA;
   }
   *out = c;

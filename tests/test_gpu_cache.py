@@ -520,3 +520,24 @@ def test_calls_on_a_handle_do_what_the_class_does(dtype):
         torch.cuda.synchronize()
         pkg.ravel_cache_destroy(c)
         pkg.ravel_cache_destroy(to)
+
+
+def test_a_cache_refused_for_want_of_memory_leaves_the_library_usable():
+    """The runtime keeps a failed call's error until it is asked for; the step's launches ask."""
+    import synth
+    from paper_2609_34170_gb300 import ContextCache, RavelError
+    from tests._harness import Case, check_step, gpu_session
+    case = Case(synth.ExpertConfig(layers=1, width=192, n_q_heads=6, n_kv_heads=2, head_dim=40, mlp_dim=320, slots=7, action_dim=5,
+                                   prefix=45, fop_tokens=3, batch=2, dtype="bf16"))
+    session = gpu_session(case)
+    for turn in range(2):
+        with pytest.raises(RavelError) as ei:
+            ContextCache(1024, 8, 4, 256, 1 << 20, 4)      # 1 TB of keys
+        assert ei.value.status == 3
+        session.reset(case.seeds)
+        if turn:                                           # (the session came with one)
+            session.set_context(case.k, case.v, case.P)
+        check_step(case, session)
+    session.close()
+    p = Pair((8, 2, 64), "bf16", 64, 2, queries=4, lengths=[30, 20])
+    check(p, 4, mass=True)
