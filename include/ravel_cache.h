@@ -13,7 +13,8 @@
  *    values: the smallest e >= -100 for which the largest magnitude stored is
  *    at most 448 * 2^e.  A value x is held as x / 2^e rounded to e4m3 (nearest,
  *    ties to even); a power of two costs the format no precision and makes
- *    the division exact.
+ *    the division exact.  (Values above 248 * 2^120 = 3.3e38 are held as 2^128,
+ *    which ravel_cache_read returns as infinity.)
  *  - Tokens that arrive in a block behind others never lower its e.  Where it
  *    rises, the tokens already there are rounded again.
  *  - A token that has a value that is not finite, in its key or its value row,

@@ -39,10 +39,10 @@ __device__ __forceinline__ float f16hi(uint32_t h) {
 // 2^e for -126 <= e <= 127
 __device__ __forceinline__ float exp2i(int e) { return __int_as_float((e + 127) << 23); }
 
-// The smallest e >= kCacheExpMin with x <= 448 * 2^e = 1.75 * 2^(e + 8), from the
+// The smallest e >= kCacheExpMin with x * 2^up <= 448 * 2^e = 1.75 * 2^(e + 8), from the
 // bits of a finite x >= 0: exact.
-__device__ __forceinline__ int block_exponent(uint32_t bits) {
-  const int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+__device__ __forceinline__ int block_exponent(uint32_t bits, int up) {
+  const int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0) + up;
   return max(e, kCacheExpMin);
 }
 

@@ -12,7 +12,8 @@ namespace {
 // One block of 16 tokens of one robot and KV head, keys and values: thread t
 // holds 16 values of each of token t / (hdp / 16) of the block.  `fresh` tokens
 // bring new values in kx / vx; `stay` tokens are in the cache already, under
-// the exponents ke_old / ve_old, and are rounded again where those rise.
+// the exponents ke_old / ve_old, and are rounded again where those rise.  kx / vx are the new
+// values times 2^-UP.
 struct BlockShared {
   int bad[kCacheBlock];      // the token has a value that is not finite
   uint32_t kmax, vmax;       // bits of the largest finite magnitudes
@@ -20,6 +21,7 @@ struct BlockShared {
 
 __device__ __forceinline__ bool finite_f(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
 
+template <int UP>
 __device__ __forceinline__ void store_block(BlockShared& s, float* kx, float* vx, bool fresh, bool stay,
                                             bool has_old, int token, const CacheLayer& c, size_t row, size_t block,
                                             int d) {
@@ -48,12 +50,12 @@ __device__ __forceinline__ void store_block(BlockShared& s, float* kx, float* vx
     atomicMax(&s.vmax, vb);
   }
   __syncthreads();
-  const int ke = max(block_exponent(s.kmax), ke_old), ve = max(block_exponent(s.vmax), ve_old);
+  const int ke = max(block_exponent(s.kmax, UP), ke_old), ve = max(block_exponent(s.vmax, UP), ve_old);
   uint4 *kd = (uint4*)(c.k + row + d), *vd = (uint4*)(c.v + row + d);
   if (fresh) {
     const uint32_t nan4 = 0x7f7f7f7fu;
-    *kd = bad ? make_uint4(nan4, nan4, nan4, nan4) : f32_to_e4m3x16(kx, exp2i(-ke));
-    *vd = bad ? make_uint4(0u, 0u, 0u, 0u) : f32_to_e4m3x16(vx, exp2i(-ve));
+    *kd = bad ? make_uint4(nan4, nan4, nan4, nan4) : f32_to_e4m3x16(kx, exp2i(UP - ke));
+    *vd = bad ? make_uint4(0u, 0u, 0u, 0u) : f32_to_e4m3x16(vx, exp2i(UP - ve));
   } else if (stay) {
     float x[16];
     if (ke != ke_old) {
@@ -101,7 +103,7 @@ __global__ void __launch_bounds__(256) cache_append_kernel(AppendArgs a) {
     load16((const T*)a.v + at, d, c.hd, a.vec, vx);
   }
   const size_t head = (size_t)b * c.Hkv + h;
-  store_block(s, kx, vx, fresh, stay, blk * kCacheBlock < start, token, c, (head * c.T + pos) * c.hdp,
+  store_block<0>(s, kx, vx, fresh, stay, blk * kCacheBlock < start, token, c, (head * c.T + pos) * c.hdp,
               head * (c.T / kCacheBlock) + blk, d);
 }
 
@@ -383,6 +385,10 @@ __global__ void __launch_bounds__(kSelThreads) cache_select_kernel(EvictArgs a, 
   if (ctas > 1) cluster_sync();   // nobody leaves while its counts are read
 }
 
+// Values on their way from cache to cache are 2^kMoveUp below what they stand for: a finite one
+// near fp32's largest is held as 2^128, which fp32 is not.
+constexpr int kMoveUp = 8;
+
 // The kept rows into the other cache: a CTA per block of 16, as in append.  Bound by the
 // dependent loads (index, block exponent, row): 256 of 816 tokens of 64 robots 8.2 us for 17 MB.
 __global__ void __launch_bounds__(256) cache_move_kernel(EvictArgs a) {
@@ -403,10 +409,10 @@ __global__ void __launch_bounds__(256) cache_move_kernel(EvictArgs a) {
     const int j = a.index[head * a.keep + pos];
     const size_t row = (head * from.T + j) * from.hdp + d, block = head * (from.T / kCacheBlock) + j / kCacheBlock;
     const uint4 kw = *(const uint4*)(from.k + row), vw = *(const uint4*)(from.v + row);
-    e4m3x16_to_f32(kw, exp2i(from.ke[block]), kx);
-    e4m3x16_to_f32(vw, exp2i(from.ve[block]), vx);
+    e4m3x16_to_f32(kw, exp2i(from.ke[block] - kMoveUp), kx);
+    e4m3x16_to_f32(vw, exp2i(from.ve[block] - kMoveUp), vx);
   }
-  store_block(s, kx, vx, fresh, false, false, token, to, (head * to.T + pos) * to.hdp,
+  store_block<kMoveUp>(s, kx, vx, fresh, false, false, token, to, (head * to.T + pos) * to.hdp,
               head * (to.T / kCacheBlock) + blockIdx.x, d);
 }
 

@@ -541,3 +541,30 @@ def test_a_cache_refused_for_want_of_memory_leaves_the_library_usable():
     session.close()
     p = Pair((8, 2, 64), "bf16", 64, 2, queries=4, lengths=[30, 20])
     check(p, 4, mass=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_eviction_keeps_the_largest_finite_values(dtype):
+    """What is held as 2^128, which neither type has, is no infinity on its way to another cache."""
+    from paper_2609_34170_gb300 import ContextCache
+    info = torch.finfo(_dt(dtype))
+    p = Pair((2, 2, 24), dtype, 64, 1)
+    k, v = _rand((1, 60, 2, 24), 1, dtype), _rand((1, 60, 2, 24), 2, dtype)
+    k[0, 3, 0, 5] = info.min
+    k[0, 40, 1, 0] = info.max
+    v[0, 3, 1, 7], v[0, 21, 0, 2] = info.max, 3.2e38
+    v[0, 22, 0, 1], k[0, 23, 0, 0] = info.tiny, 2.0 ** -100
+    p.cache.append(0, k, v)
+    p.held.append(_np(k), _np(v), [0], [60])
+    mass = np.random.default_rng(3).random((1, 2, 64)).astype(np.float32)
+    mass[:, :, [3, 21, 22, 23, 40]] = 2.0
+    cache, held, lengths = p.cache, p.held, [60]
+    for keep in (37, 17):         # out of the first cache, and out of the second again
+        to = ContextCache(1, 2, 2, 24, keep, 1, 1, dtype)
+        got = cache.evict(0, to, 0, _ints(lengths), torch.from_numpy(mass).cuda(), keep, 2, 3)
+        lengths, index, mass64, held = ref.evict(held, lengths, mass, keep, 2, 3)
+        np.testing.assert_array_equal(got[1].cpu().numpy(), index)
+        for g, w in zip(to.read(0, 1, keep, lengths=got[0]), (held.k, held.v)):
+            with np.errstate(over="ignore"):
+                np.testing.assert_array_equal(_np(g), w[:, :, :keep].astype(np.float32).astype(np.float64))
+        cache, mass, lengths = to, mass64.astype(np.float32), list(lengths)
