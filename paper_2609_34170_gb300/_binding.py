@@ -332,7 +332,8 @@ class CacheArguments:
         self.index = device
 
     def rows(self, x, heads: int, name: str):
-        """Strides (robot, token) of a [batch, n, heads, head_dim] tensor whose heads are contiguous."""
+        """Strides (robot, token) of a [batch, n, heads, head_dim] tensor whose heads are
+        contiguous; 0 where there is one robot or one token, whose stride means nothing."""
         shape = x.shape
         if x.dtype is not self.dtype or len(shape) != 4 or shape[2] != heads or shape[3] != self.head_dim or \
                 x.get_device() != self.index:
@@ -341,7 +342,7 @@ class CacheArguments:
         robot, token, head, dim = x.stride()
         if dim != 1 or (head != self.head_dim and heads > 1):
             raise ValueError(f"{name}: the heads of a token must be contiguous")
-        return robot, token
+        return robot if shape[0] > 1 else 0, token if shape[1] > 1 else 0
 
     def ints(self, x, batch: int, name: str):
         """Address of an int32 tensor [batch], or None."""

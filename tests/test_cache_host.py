@@ -204,3 +204,22 @@ def test_create_refuses_positions_that_could_pass_32_bits(lib):
                 ravel_cache_create(layers=1, n_q_heads=4, n_kv_heads=heads, head_dim=64, max_tokens=tokens, max_batch=batch,
                                    max_queries=1)
             assert ei.value.status == 2
+
+
+def test_strides_of_a_single_robot_or_token_mean_nothing(lib):
+    import paper_2609_34170_gb300 as pkg
+    from paper_2609_34170_gb300 import _binding as B
+    c = C.c_void_p()
+    c.arguments = B.CacheArguments(n_q_heads=4, n_kv_heads=2, head_dim=64, dtype=B.RAVEL_BF16, device=0)
+
+    def append(shape, k_stride, v_stride):
+        pkg.ravel_cache_append(c, 0, _Gpu(shape, torch.bfloat16, k_stride), _Gpu(shape, torch.bfloat16, v_stride), stream=0)
+
+    for shape, k, v in (((1, 1, 2, 64), (128, 128, 64, 1), (512, 512, 64, 1)), ((1, 5, 2, 64), (640, 512, 64, 1), (9999, 512, 64, 1)),
+                        ((3, 1, 2, 64), (512, 128, 64, 1), (512, 512, 64, 1))):
+        with pytest.raises(B.RavelError):     # (by the library: the handle is null)
+            append(shape, k, v)
+    for shape, k, v in (((1, 5, 2, 64), (640, 128, 64, 1), (640, 512, 64, 1)), ((3, 1, 2, 64), (128, 128, 64, 1), (512, 128, 64, 1))):
+        with pytest.raises(ValueError):
+            append(shape, k, v)
+    assert c.arguments.rows(_Gpu((1, 1, 2, 64), torch.bfloat16, (7, 3, 64, 1)), 2, "k") == (0, 0)

@@ -568,3 +568,19 @@ def test_eviction_keeps_the_largest_finite_values(dtype):
             with np.errstate(over="ignore"):
                 np.testing.assert_array_equal(_np(g), w[:, :, :keep].astype(np.float32).astype(np.float64))
         cache, mass, lengths = to, mass64.astype(np.float32), list(lengths)
+
+
+def test_a_decoded_token_whose_key_and_value_lie_apart():
+    from paper_2609_34170_gb300 import ContextCache
+    c, want = (ContextCache(1, 4, 2, 64, 32, 1, 1) for _ in range(2))
+    qkv = _rand((1, 1, 8, 64), 1, "bf16")
+    q, k, v = qkv[:, :, :4], _rand((1, 1, 2, 64), 4, "bf16"), qkv[:, :, 6:]
+    assert k.stride() != v.stride()
+    for cache in (c, want):
+        cache.append(0, _rand((1, 9, 2, 64), 2, "bf16"), _rand((1, 9, 2, 64), 3, "bf16"))
+    c.append(0, k, v, _ints([9]))
+    want.append(0, k, torch.empty_like(k).copy_(v), _ints([9]))
+    for a, b in zip(c.read(0, 1, 10), want.read(0, 1, 10)):
+        assert torch.equal(a, b)
+    out = torch.empty((1, 3, 4, 64), dtype=torch.bfloat16, device="cuda")[:, 1:2]
+    assert torch.equal(c.attend(0, q, _ints([10]), out=out), want.attend(0, torch.empty((1, 1, 4, 64), dtype=q.dtype, device="cuda").copy_(q), _ints([10])))
