@@ -54,7 +54,9 @@ typedef struct {
   int max_batch;    /* robots */
   int max_queries;  /* largest n of ravel_cache_attend */
   int dtype;        /* RAVEL_BF16 or RAVEL_FP32: type of the keys, values, queries and outputs of every call.
-                       RAVEL_FP32 results are fp32-accurate for the keys and values held */
+                       RAVEL_FP32 results are fp32-accurate for the keys and values held.  RAVEL_BF16: weights have
+                       11 bits; of more than 16 query rows per KV head, a query's elements below 2^-13 of its
+                       largest are held to within 2^-21 of the largest */
 } ravel_cache_config;
 
 typedef struct ravel_cache_ctx ravel_cache_t;

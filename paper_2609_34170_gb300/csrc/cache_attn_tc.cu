@@ -5,7 +5,7 @@
 // head) and a share (split) of the 128-token tiles that they see; CTAs, one per SM,
 // walk the items of their launch:
 //   S = Q K^T        tcgen05.mma kind::f8f6f4, M = 128, N = 128, into TMEM: the codes
-//                    of K as they are, Q in two e4m3 pieces
+//                    of K as they are, Q in two 8-bit pieces
 //   P = 2^(S - m)    softmax warps: TMEM -> registers -> f16 P over S in TMEM
 //   O += P V         tcgen05.mma kind::f16, M = 128, N = head dim, 16 tokens at a time
 // Warp roles (640 threads): warps 0-7 softmax and output (see TcShape::own); warps
@@ -17,9 +17,9 @@
 // What bounds it at head dim 256 is shared memory: per tile (2048 cycles of MMA) its
 // 128 bytes a cycle carry 192 KB of MMA operands, and every code that is widened to
 // f16 costs 4 bytes more of TMA, reading and writing.  So K is not widened: bf16's 8
-// significant bits are two e4m3 pieces of 4 (a rounded one and the rest, exactly,
-// down to 2^-18 of the row's largest), whose two MMAs at twice the rate cost what
-// one in f16 does.  V is: 2^-9 is the least P that e4m3 holds, and a long flat tail
+// significant bits are 4 in e4m3 and the rest in e5m2 (see stage_q8: exactly, down to
+// 2^-13 of the row's largest, and within 2^-21 of it below), whose two MMAs at twice the
+// rate cost what one in f16 does.  V is: 2^-9 is the least P that e4m3 holds, and a long flat tail
 // of smaller ones carries weight.  The codes of V come by TMA and are widened in
 // shared memory to f16 (exact), into the 128-byte swizzled layout of a TMA load of
 // f16 rows.  (Widening K as well, in units of 64 head dims, 448 KB a tile, took 3600
@@ -384,7 +384,7 @@ __global__ void __launch_bounds__(TCT, 1) cache_tc_kernel(const __grid_constant_
             const uint64_t bd = kd0 + (uint32_t)sk * (KU >> 4);
 #pragma unroll
             for (int k = 0; k < 4; ++k)   // both pieces of Q
-              umma_e4m3(sd, ad + (k >> 1) * (NB * QB >> 4) + 2 * (k & 1), bd + 2 * (k & 1), idesc_s, (blk > 0 || k > 0) ? 1u : 0u, el);
+              umma_f8(sd, ad + (k >> 1) * (NB * QB >> 4) + 2 * (k & 1), bd + 2 * (k & 1), k < 2 ? idesc_s : idesc_s | kE5m2A, (blk > 0 || k > 0) ? 1u : 0u, el);
             umma_commit(&k_empty[sk], el);
             if (++sk == KS) {
               sk = 0;

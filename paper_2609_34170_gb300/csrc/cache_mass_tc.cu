@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(MT, 1) cache_mass_tc_kernel(const __grid_const
           const uint64_t kd = kd0 + (uint32_t)sk * (KU >> 4), qb = qd + (uint32_t)blk * (QB >> 4);
 #pragma unroll
           for (int k = 0; k < 4; ++k)   // both pieces of Q, the low one first: less is cut off the sums
-            umma_e4m3(sd, kd + 2 * (k & 1), qb + (1 - (k >> 1)) * (NB * QB >> 4) + 2 * (k & 1), idesc, (blk > 0 || k > 0) ? 1u : 0u, el);
+            umma_f8(sd, kd + 2 * (k & 1), qb + (1 - (k >> 1)) * (NB * QB >> 4) + 2 * (k & 1), k < 2 ? idesc | kE5m2B : idesc, (blk > 0 || k > 0) ? 1u : 0u, el);
           umma_commit(&k_empty[sk], el);
           if (++sk == KS) {
             sk = 0;

@@ -1,5 +1,5 @@
-// What the tensor-core kernels of the 8-bit context cache share: operands in e4m3,
-// waits, and Q laid out in e4m3 pieces.
+// What the tensor-core kernels of the 8-bit context cache share: operands in 8 bits,
+// waits, and Q laid out in two pieces.
 #pragma once
 
 #include <cuda.h>
@@ -21,8 +21,8 @@ __device__ __forceinline__ uint64_t sw64_desc(uint32_t saddr) {
          (uint64_t)4 << 61;
 }
 
-// D += A B of e4m3 operands (K = 32), issued by the elected lane of a converged warp
-__device__ __forceinline__ void umma_e4m3(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc, uint32_t el) {
+// D += A B of 8-bit operands (K = 32), issued by the elected lane of a converged warp
+__device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc, uint32_t el) {
   asm volatile(
       "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.b32 q, %5, 0;\n\t"
@@ -31,7 +31,8 @@ __device__ __forceinline__ void umma_e4m3(uint32_t d_tmem, uint64_t a, uint64_t 
       "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(el));
 }
 
-// f16 A and B (kind::f16) or e4m3 ones (kind::f8f6f4), fp32 D
+// f16 A and B (kind::f16) or e4m3 ones (kind::f8f6f4, of which one may be e5m2), fp32 D
+constexpr uint32_t kE5m2A = 1u << 7, kE5m2B = 1u << 10;
 __device__ __forceinline__ uint32_t idesc_f16(int m, int n) {
   return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
@@ -56,6 +57,12 @@ __device__ __forceinline__ void sts_u2(uint32_t a, uint32_t x, uint32_t y) {
 __device__ __forceinline__ uint32_t f16_to_e4m3(uint32_t h) {
   uint16_t r;
   asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(h));
+  return r;
+}
+// and two e5m2
+__device__ __forceinline__ uint32_t f16_to_e5m2(uint32_t h) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e5m2x2.f16x2 %0, %1;" : "=h"(r) : "r"(h));
   return r;
 }
 __device__ __forceinline__ uint32_t f16_sub(uint32_t a, uint32_t b) {
@@ -149,8 +156,12 @@ __device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, 
 
 // Q rows rb .. rb + 7 of the tile of rows from r0 on of robot b, KV head h (8 NB lanes
 // with 8 dims each to a row), scaled by the row's power of two to a largest magnitude
-// in [2^kQExp, 2^(kQExp + 1)), in two e4m3 pieces: y rounded and what is left.  64-byte
-// rows of 64 dims, 64-byte swizzled, blocks of QB bytes, the second piece NB blocks
+// in [2^kQExp, 2^(kQExp + 1)), in two pieces: y rounded to e4m3, and what is left, in e5m2.
+// Of a y from 2^-6 on (2^-13 of the row's largest) that is at most 8 units of bf16's last
+// place, three bits: the pieces are y.  Below, what is left is rounded to e5m2 by at most
+// 2^-14: an element is never off by more than 2^-21 of the row's largest magnitude.  (An e4m3
+// rest would end at 2^-9, 2^-17 of the largest: small dims beside a large one that the keys do
+// not use were lost.)  64-byte rows of 64 dims, 64-byte swizzled, blocks of QB bytes, the second piece NB blocks
 // behind the first: into shared memory at q0 or, where `to` is given, there.  row_done:
 // called by one lane with each row's place in the tile and its exponent bits.
 template <int NB, typename F>
@@ -214,7 +225,7 @@ __device__ __forceinline__ void stage_q8(const CacheAttnArgs& a, const Sight& s,
       const uint32_t h0 = pack_f16x2(__uint_as_float(y[2 * z] << 16) * f, __uint_as_float(y[2 * z] & 0xffff0000u) * f);
       const uint32_t h1 = pack_f16x2(__uint_as_float(y[2 * z + 1] << 16) * f, __uint_as_float(y[2 * z + 1] & 0xffff0000u) * f);
       hi[z] = f16_to_e4m3(h0) | f16_to_e4m3(h1) << 16;
-      lo[z] = f16_to_e4m3(f16_sub(h0, e4m3_lo(hi[z]))) | f16_to_e4m3(f16_sub(h1, e4m3_hi(hi[z]))) << 16;
+      lo[z] = f16_to_e5m2(f16_sub(h0, e4m3_lo(hi[z]))) | f16_to_e5m2(f16_sub(h1, e4m3_hi(hi[z]))) << 16;
     }
     const int lr = rb + p * RPW + sub;
     if (mine) {

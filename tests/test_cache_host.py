@@ -223,3 +223,16 @@ def test_strides_of_a_single_robot_or_token_mean_nothing(lib):
         with pytest.raises(ValueError):
             append(shape, k, v)
     assert c.arguments.rows(_Gpu((1, 1, 2, 64), torch.bfloat16, (7, 3, 64, 1)), 2, "k") == (0, 0)
+
+
+def test_two_pieces_hold_what_the_prompts_kernels_claim():
+    """y = e4m3(y) + e5m2(rest) for bf16 values of a row whose largest lies in [2^7, 2^8): exact from
+    2^-6 on, off by at most 2^-14 below."""
+    bits = torch.arange(1 << 15, dtype=torch.int32)
+    y = bits.to(torch.int16).view(torch.bfloat16).double()
+    y = y[(y < 2.0 ** 8) & (y > 2.0 ** -60)]
+    half = y.to(torch.float16)        # (a subnormal's rounding, below 2^-14)
+    hi = half.to(torch.float8_e4m3fn)
+    lo = (half - hi.half()).to(torch.float8_e5m2)
+    off = (y - hi.double() - lo.double()).abs()
+    assert (off[y >= 2.0 ** -6] == 0).all() and off.max() <= 2.0 ** -14

@@ -584,3 +584,47 @@ def test_a_decoded_token_whose_key_and_value_lie_apart():
         assert torch.equal(a, b)
     out = torch.empty((1, 3, 4, 64), dtype=torch.bfloat16, device="cuda")[:, 1:2]
     assert torch.equal(c.attend(0, q, _ints([10]), out=out), want.attend(0, torch.empty((1, 1, 4, 64), dtype=q.dtype, device="cuda").copy_(q), _ints([10])))
+
+
+def _within(pair, got, q, n, causal=True, window=0, sinks=0, mass=None, counts=None):
+    """bf16 attention of many rows against the reference, with a score's error as it is there: 2^-18
+    of scale sum |q k| for the sums, and each element of q off by up to 2^-21 of the row's largest;
+    scores off by d change weights by a factor of up to e^2d."""
+    counts = [n] * pair.batch if counts is None else counts
+    o, ms, W, size = ref.attend(_np(q), pair.held, pair.lengths, counts, causal, window, sinks)
+    hq, hkv, hd = pair.layout
+    keys = np.abs(pair.held.k).sum(-1).max(-1).repeat(hq // hkv, 1)            # [B, Hq]: the largest sum of |k|
+    d = 2.0 ** -18 * size + 2.0 ** -21 / np.sqrt(hd) * np.abs(_np(q)).max(-1) * keys[:, None]
+    tol = 2.0 ** -8 * np.abs(o) + (2.0 ** -10 + np.expm1(2 * d[..., None])) * W
+    err = np.abs(_np(got) - o)
+    assert (err <= tol + 1e-37).all(), (err.max(), (err / (tol + 1e-37)).max())
+    if mass is not None:
+        m = _np(mass)[:, :, :ms.shape[2]]
+        ms = ms[:, :, :m.shape[2]]
+        assert (np.abs(m - ms) <= (2.0 ** -18 + np.expm1(2 * d.max())) * ms + 1e-37).all()
+
+
+@pytest.mark.parametrize("layout,n", [((2, 1, 40), 20), ((4, 1, 64), 40), ((2, 2, 128), 140), ((3, 1, 192), 30), ((8, 1, 256), 5)])
+@pytest.mark.parametrize("big", [2.0 ** 7, 2.0 ** 12, 2.0 ** 15])
+def test_small_dims_beside_a_large_one_keep_their_weight(layout, n, big):
+    """A query's first dim is far above the others, and the keys do not use it."""
+    hq, hkv, hd = layout
+    p = Pair(layout, "bf16", 300, 2, queries=n)
+    p.lengths = [300, 201]
+    rng = np.random.default_rng(1)
+    sign = rng.choice([-1.0, -0.5, 0.5, 1.0], (2, 300, hkv, 1))
+    for same in (True, False):        # dims that add up, and dims of any size
+        k = np.ones((2, 300, hkv, hd)) * sign if same else rng.standard_normal((2, 300, hkv, hd))
+        k[..., 0] = 0.0
+        # (just below half a unit of what e4m3 holds beside the largest)
+        q = np.full((2, n, hq, hd), 0.97) if same else 2.0 ** rng.uniform(-12, 6, (2, n, hq, hd)) * rng.choice([-1, 1], (2, n, hq, hd))
+        q *= 2.0 ** -17 * big
+        q[..., 0] = big
+        k, q = (torch.from_numpy(x).to(torch.bfloat16).cuda() for x in (k, q))
+        v = _rand((2, 300, hkv, hd), 2, "bf16")
+        p.cache.append(0, k, v, counts=_ints(p.lengths))
+        p.held.append(_np(k), _np(v), [0, 0], p.lengths)
+        for causal, window, sinks in ((False, 0, 0), (True, 60, 4)):
+            mass = torch.zeros((2, hkv, 300), device="cuda")
+            out = p.cache.attend(0, q, _ints(p.lengths), causal=causal, window=window, sinks=sinks, mass=mass)
+            _within(p, out, q, n, causal, window, sinks, mass)
