@@ -75,8 +75,10 @@ class ContextCache:
         causal: query i sees up to its own position, with `window` the last
         `window` of those and the first `sinks`.  mass (float32 [B, Hkv, tokens]):
         receives, or with add_mass is increased by, the attention mass that each
-        token drew.  max_length: a bound of the lengths, if one below the
-        cache's room is known; launches are planned for it."""
+        token drew.  max_length: a bound of the lengths (None: the cache's
+        room).  Launches are planned for it, so that a bound near the lengths is
+        worth giving: one token over 816 takes 8 us with it, 39 in a cache with
+        room for 8192 without."""
         qr, qt = self._rows(q, self.n_q_heads, "q")
         shape = q.shape
         batch, n = shape[0], shape[1]

@@ -20,10 +20,12 @@
 // to work on.  Few rows take K as the A operand, 16 tokens by 8 rows, and P transposed
 // in registers: half the MMAs and exponentials of a tile of 16 rows that is half empty.
 //
-// Measured (one query per robot, bf16): one robot of 816 tokens, head dim 256: 10.0 us,
-// a chain of launch, Q, one unit per warp, two joins; 64 robots of 1024 to 2048: 18.6 us
-// for 50 MB (2.7 TB/s; a round of unequal robots); 4 robots of 131071, 4 heads of 64:
-// 56 us for 269 MB (4.8 TB/s).  3 robots, 37 queries, 301 tokens in fp32: 9.7 us.
+// Measured (one query per robot, bf16; alone / in a chain of calls): one robot of 816 tokens,
+// head dim 256: 10.1 / 8.1 us, a chain of launch, Q, one unit per warp, two joins; 64 robots of
+// 1024 to 2048: 19.3 / 17.2 us for 50 MB (2.9 TB/s; a round of unequal robots); 4 robots of
+// 131071, 4 heads of 64: 56.5 / 51.7 us for 269 MB (5.2 TB/s; alone, CTAs are on the SMs for
+// three quarters of the time: arithmetic 48 % busy meanwhile, tensor pipe 17, exponentials 9, and
+// what warps wait for most is their units).  3 robots, 37 queries, 301 tokens in fp32: 9.4 / 8.0.
 //
 // Numbers: q is scaled by a power of two per row to a maximum in [2^14, 2^15) and
 // held in f16 -- exactly for bf16 inputs (8 significant bits; what lies 2^38
@@ -842,8 +844,9 @@ __global__ void __launch_bounds__(RW * 32, 2) cache_rows_kernel(const __grid_con
 // Attention mass: token j's softmax weights summed over the rows of its KV head, from the
 // scores that the attention kept and the rows' (max, 1 / sum): a thread per two tokens
 // and, of many queries, every 8th, 16th or 64th of them, summed in a fixed order.  Bound by
-// reading them, 4 bytes per row and token (4 robots x 16 rows x 131071 tokens: 34 MB, in
-// L2, 13.6 us); computing them again would read the keys' 134 MB from HBM.
+// reading them, 4 bytes per row and token, on the way of few loads per thread (4 robots x 16
+// rows x 131071 tokens: 34 MB, in L2, 17 us behind the attention, 18.7 alone); computing them
+// again would read the keys' 134 MB from HBM.
 __global__ void __launch_bounds__(1024) cache_mass_scores_kernel(CacheAttnArgs a, int groups) {
   __shared__ float2 sums[1024];
   const int per = (int)blockDim.x / groups, group = threadIdx.x / per, at = threadIdx.x % per;
@@ -919,8 +922,12 @@ cudaError_t launch_part(CacheAttnArgs a, int batch, cudaStream_t st) {
                                       cluster, maps, a);
   if (e != cudaSuccess || !a.scores) return e;
   // groups of a token's queries, and with them threads: as many as the queries fill, 1024 where
-  // the tokens are few CTAs otherwise (1 robot's 816 queries and tokens, one KV head of fp32: 232
-  // us with 8 groups, 36 with 64; 26 robots' 23 queries, two heads of 1465 tokens: 10 and 19)
+  // the tokens are few CTAs otherwise.  Measured, us with 1 / 8 / 16 / 64 groups: 1 robot of 816
+  // tokens (8 heads on one), 16 queries 29 / 6.0 / 4.0 / 5.0, 64: 111 / 18 / 11 / 5.3, 512: 871 /
+  // 118 / 66 / 22; 26 robots of 1465 (6 heads on each of 2), 16: 35 / 14 / 20 / 58, 64: 243 / 50 /
+  // 57 / 78, 128: 900 / 184 / 158 / 160, 512: 19674 / 3132 / 1869 / 879.  (Below 16 queries 8 groups
+  // would be the faster ones from four on: 8 of 1 robot 15.4 / 3.7, of 26 robots 19 / 9; at 64 of
+  // many robots 8 or 16.)
   const int queries = a.i1 - a.i0;
   const bool few = (long long)((a.max_length + 63) / 64) * a.c.Hkv * batch < 2 * a.num_sms;
   const int groups = queries >= 64 ? 64 : (queries < 16 ? 1 : (few ? 16 : 8)), threads = groups >= 16 ? 1024 : 256;
@@ -933,6 +940,12 @@ template <int HDP, int NP, typename T>
 cudaError_t launch_rows(CacheAttnArgs a, cudaStream_t st) {
   const Overlap overlap;
   const bool mass = a.mass && a.max_length > 0;
+  // From 17 rows per KV head on, bf16 goes to the tensor cores' kernel.  Measured without the mass,
+  // us here / there: 8 heads of 256 on one, 64 robots of 816 tokens, 16 rows 14.7 / 15.7, 24 rows
+  // 19.0 / 16.4, 64 rows 24.6 / 17.2; 16 robots, 16 rows 11.5 / 13.0, 64 rows 14.6 / 15.2, 128 rows
+  // 19.0 / 18.3; 16 heads of 64 on 4, 64 robots, 16 rows 10.1 / 21.8, 32 rows 19.4 / 21.8, 64 rows
+  // 37.6 / 21.9.  (The line fits many robots; of one, whose rows fill few CTAs, this kernel is the
+  // faster one up to 128 rows: 10.3 / 20.8 over 816 tokens, 42 / 216 over 8192.)
   if (NP == 1 && a.n * a.G > 16) {
     const cudaError_t e = launch_cache_attend_tc(a, st);
     return e != cudaSuccess || !mass ? e : launch_cache_mass_tc(a, st);

@@ -32,9 +32,9 @@
 // a grown one waits for its rescaling of O (only growth by more than 2^8 rescales);
 // what contributes less than 2^-31 of the row's largest is dropped.
 //
-// Measured: 16 prompts of 816 tokens (8 heads of 256, one KV head) 88.5 us, 985 TFLOP/s;
-// 2 of 8191 with a window of 1024 (16 heads of 64) 193 us, without the window 426; 50 slots of
-// 16 robots over 816 tokens, 20 us.  A tile of 128 x 128 takes 1570 cycles at head dim 64, 1940
+// Measured: 16 prompts of 816 tokens (8 heads of 256, one KV head) 88.5 us, 985 TFLOP/s
+// (causal 71); 2 of 8191 with a window of 1024 (16 heads of 64) 193 us, without the window
+// 425; 50 slots of 16 robots over 816 tokens, 20 us.  A tile of 128 x 128 takes 1570 cycles at head dim 64, 1940
 // at 128, 2190 at 192 and 2550 at 256 (MMAs alone: 512, 1024, 1536, 2048), an item's begin and
 // end 7500 to 12000 more.  Up to 128 the softmax bounds it; of a tile that two threads a row
 // share, one after the other: scores in 130, maxima 250, their exchange 250, exponentials 700,

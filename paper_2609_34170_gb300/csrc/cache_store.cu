@@ -73,11 +73,12 @@ __device__ __forceinline__ void store_block(BlockShared& s, float* kx, float* vx
   }
 }
 
-// Bandwidth-bound for prompts, a launch's latency for single tokens.  A CTA per
-// block: its exponent needs the whole block's maximum before the first value
-// is rounded, and 16 tokens x 16 values per thread hold it in registers, so
-// the inputs are read once.  Measured: a token of 64 robots 4.3 us; 816 tokens of 16 robots
-// (one KV head of 256) 8.1 us, 20 MB (2.5 TB/s).
+// Bandwidth-bound for many tokens, latency for few (a launch, the loads, three
+// barriers).  A CTA per block: its exponent needs the whole block's maximum
+// before the first value is rounded, and 16 tokens x 16 values per thread hold
+// it in registers, so the inputs are read once.  Measured (alone / in a chain, inputs then in
+// L2): a token of 64 robots 4.3 / 2.2 us; 816 tokens of 16 robots (one KV head of 256), 20 MB,
+// 8.2 / 4.6; 4096 of 64, 403 MB, 79 (5.1 TB/s).
 template <typename T>
 __global__ void __launch_bounds__(256) cache_append_kernel(AppendArgs a) {
   __shared__ BlockShared s;
@@ -129,8 +130,9 @@ __device__ __forceinline__ void store16(T* row, int d, int hd, int vec, const fl
   }
 }
 
-// Bandwidth-bound: a thread takes 16 values of a token's key row and of its value row.
-// Measured: 816 tokens of 16 robots, one KV head of 256: 6.8 us, 20 MB (2.9 TB/s).
+// Bandwidth-bound for many tokens, a launch and dependent loads for few: a thread takes 16
+// values of a token's key row and of its value row.  Measured (one KV head of 256; alone / in a
+// chain): 816 tokens of 16 robots, 20 MB, 6.8 / 5.4 us; 4096 of 64, 403 MB, 71 (5.7 TB/s).
 template <typename T>
 __global__ void __launch_bounds__(256) cache_read_kernel(ReadArgs a) {
   const CacheLayer& c = a.c;
@@ -187,10 +189,10 @@ __device__ __forceinline__ uint32_t mass_key(float x) {
 //
 // A cluster per (robot, KV head), each of its CTAs with a run of the tokens; the
 // histograms and the counts are added up through distributed shared memory.  The
-// masses are read five times, from L2 after the first: one CTA took 66 us for 65537
-// tokens, 64 dependent turns of the loop per pass.  Measured: 4 heads of 65537 tokens 21 us
-// (latency: three to four passes of loads, cluster barrier, remote reads and scan at 4 us),
-// 64 robots of 816 tokens 7.2 us.
+// masses are read up to six times (four histograms, the counts of the runs before, the
+// places), from L2 after the first: one CTA took 66 us for 65537 tokens, 64 dependent turns of
+// the loop per pass.  Measured: 4 heads of 65537 tokens 22 us (latency: three to four passes of
+// loads, cluster barrier, remote reads and scan at 4 us), 64 robots of 816 tokens 7.6 us.
 __global__ void __launch_bounds__(kSelThreads) cache_select_kernel(EvictArgs a, int ctas) {
   __shared__ unsigned hist[2][256], sums[256];
   __shared__ uint32_t sel_bin, sel_left, sel_all;
@@ -390,7 +392,7 @@ __global__ void __launch_bounds__(kSelThreads) cache_select_kernel(EvictArgs a, 
 constexpr int kMoveUp = 8;
 
 // The kept rows into the other cache: a CTA per block of 16, as in append.  Bound by the
-// dependent loads (index, block exponent, row): 256 of 816 tokens of 64 robots 8.2 us for 17 MB.
+// dependent loads (index, block exponent, row): 256 of 816 tokens of 64 robots 7.8 us for 17 MB.
 __global__ void __launch_bounds__(256) cache_move_kernel(EvictArgs a) {
   __shared__ BlockShared s;
   const CacheLayer &from = a.from, &to = a.to;
