@@ -44,6 +44,12 @@ class RavelCacheConfig(C.Structure):
         "layers", "n_q_heads", "n_kv_heads", "head_dim", "max_tokens", "max_batch", "max_queries", "dtype")]
 
 
+class RavelRotaryConfig(C.Structure):
+    _fields_ = ([("dims", C.c_int), ("interleaved", C.c_int)]
+                + [(n, C.c_double) for n in ("base", "factor", "original_length", "low", "high", "amplitude")]
+                + [("frequencies", C.POINTER(C.c_double))])
+
+
 class RavelError(RuntimeError):
     def __init__(self, status: int, msg: str):
         self.status = status
@@ -98,6 +104,18 @@ def load(path: str | None = None):
         "ravel_cache_evict": (i, [vp, i, vp, i, i, vp, vp, ll, i, i, i, vp, vp, vp, vp]),
         "ravel_cache_read": (i, [vp, i, i, i, vp, vp, vp, vp, vp]),
         "ravel_cache_last_error": (C.c_char_p, [vp]),
+        "ravel_rotary_create": (i, [C.POINTER(RavelRotaryConfig), i, pp]),
+        "ravel_rotary_destroy": (None, [vp]),
+        "ravel_rotary_apply": (i, [vp, i, i, i, i, i, vp, ll, ll, vp, ll, ll, vp, vp, vp, vp]),
+        "ravel_cache_append_rotary": (i, [vp, i, vp, i, i, vp, ll, ll, vp, ll, ll, vp, ll, ll, vp, ll, ll, vp, vp, vp, vp]),
+        "ravel_w4_create": (i, [i, i, i, i, pp]),
+        "ravel_w4_destroy": (None, [vp]),
+        "ravel_w4_load": (i, [vp, vp, vp, vp, vp]),
+        "ravel_w4_quantize": (i, [vp, i, i, i, i, i, vp, vp, vp, vp]),
+        "ravel_w4_read": (i, [vp, vp, i, i, vp]),
+        "ravel_w4_gemm": (i, [vp, vp, i, i, i, vp, i, i, vp, vp]),
+        "ravel_draw_tokens": (i, [vp, i, i, ll, i, vp, vp, vp, vp, vp, vp, vp, vp]),
+        "ravel_decode_last_error": (C.c_char_p, []),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -313,6 +331,18 @@ def current_stream_getter():
     return get if get is not None else lambda device: torch.cuda.current_stream(device).cuda_stream
 
 
+def new_tensor(shape, dtype, device, stream, zeros=False):
+    """A new tensor of the stream that is going to write it."""
+    import torch
+    make = torch.zeros if zeros else torch.empty
+    if stream is None:
+        return make(shape, dtype=dtype, device=device)
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream), device=device)
+    with torch.cuda.stream(stream):
+        return make(shape, dtype=dtype, device=device)
+
+
 def _check_cache(c, status: int, what: str):
     if status != 0:
         raise RavelError(status, f"{what}: {load().ravel_cache_last_error(c).decode()}")
@@ -451,3 +481,209 @@ def ravel_cache_read(c, layer: int, k, v, firsts=None, lengths=None, stream=None
     _check_cache(c, load().ravel_cache_read(c, layer, B, n, a.ints(firsts, B, "firsts"), a.ints(lengths, B, "lengths"),
                                             a.dense(k, held, a.dtype, "k"), a.dense(v, held, a.dtype, "v"),
                                             _stream_ptr(stream)), "ravel_cache_read")
+
+
+def ravel_cache_append_rotary(c, layer: int, rotary, q, q_out, k, v, starts=None, positions=None, counts=None, stream=None):
+    """q, q_out [B, n, Hq, hd] (or None), k, v [B, n, Hkv, hd]; positions int32 [B, n]; see ravel_decode.h."""
+    a = _arguments(c)
+    if getattr(rotary, "rotary", None) is None:
+        raise ValueError("not a handle that ravel_rotary_create returned")
+    krs, kts = a.rows(k, a.n_kv_heads, "k")
+    vrs, vts = a.rows(v, a.n_kv_heads, "v")
+    shape = k.shape
+    if v.shape != shape:
+        raise ValueError("k and v must have the same shape")
+    B, n = shape[0], shape[1]
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    qp = qop = None
+    qrs = qts = qors = qots = 0
+    if q is not None:
+        qrs, qts = a.rows(q, a.n_q_heads, "q")
+        qors, qots = a.rows(q_out, a.n_q_heads, "q_out")
+        if q.shape[:2] != shape[:2] or q_out.shape != q.shape:
+            raise ValueError("q and q_out must have as many tokens as k")
+        qp, qop = q.data_ptr(), q_out.data_ptr()
+    _check_cache(c, load().ravel_cache_append_rotary(
+        c, layer, rotary, B, n, qp, qrs, qts, qop, qors, qots, k.data_ptr(), krs, kts, v.data_ptr(), vrs, vts,
+        a.ints(starts, B, "starts"), a.dense(positions, (B, n), a.int32, "positions"), a.ints(counts, B, "counts"),
+        _stream_ptr(stream)), "ravel_cache_append_rotary")
+
+
+# ---- rotary positions, 4-bit products, drawing tokens (include/ravel_decode.h)
+
+
+def _check_decode(status: int, what: str):
+    if status != 0:
+        raise RavelError(status, f"{what}: {load().ravel_decode_last_error().decode()}")
+
+
+def _row_dtype(t, name: str) -> int:
+    import torch
+    if t.dtype is torch.bfloat16:
+        return RAVEL_BF16
+    if t.dtype is torch.float32:
+        return RAVEL_FP32
+    raise ValueError(f"{name} must be bfloat16 or float32, got {t.dtype}")
+
+
+def _flat(t, shape: tuple, dtype, device: int, name: str):
+    """Address of a contiguous CUDA tensor of that shape, or None."""
+    if t is None:
+        return None
+    if not hasattr(t, "data_ptr") or t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        got = f"{tuple(t.shape)} of {t.dtype} on {t.device}" if hasattr(t, "data_ptr") else repr(t)
+        raise ValueError(f"{name} must be a contiguous tensor {list(shape)} of {dtype} on cuda:{device}, got {got}")
+    return t.data_ptr()
+
+
+def _matrix(t, rows: int, cols: int, device: int, name: str) -> int:
+    """Row stride of a [rows, cols] tensor whose rows are contiguous; of a single row, whose
+    stride means nothing, the next multiple of 8."""
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or t.get_device() != device or (cols > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be [{rows}, {cols}] on cuda:{device} with contiguous rows, got {tuple(t.shape)} on {t.device}")
+    if rows > 1 and t.stride(0) < cols:
+        raise ValueError(f"{name}: rows overlap")
+    return t.stride(0) if rows > 1 else -(-cols // 8) * 8
+
+
+def ravel_rotary_create(dims: int, base: float = 10000.0, interleaved: bool = False, factor: float = 1.0,
+                        original_length: float = 0.0, low: float = 1.0, high: float = 32.0, amplitude: float = 1.0,
+                        frequencies=None, device: int = 0):
+    f = None
+    if frequencies is not None:
+        f = np.ascontiguousarray(frequencies, dtype=np.float64)
+        if f.shape != (dims // 2,):
+            raise ValueError(f"frequencies must be [{dims // 2}], got {f.shape}")
+    c = RavelRotaryConfig(dims, int(interleaved), base, factor, original_length, low, high, amplitude,
+                          None if f is None else f.ctypes.data_as(C.POINTER(C.c_double)))
+    h = C.c_void_p()
+    _check_decode(load().ravel_rotary_create(C.byref(c), device, C.byref(h)), "ravel_rotary_create")
+    h.rotary = (dims, device)
+    return h
+
+
+def ravel_rotary_destroy(r):
+    load().ravel_rotary_destroy(r)
+
+
+def _heads(x, device: int, name: str):
+    """Strides (robot, token) of a [batch, n, heads, hd] tensor whose heads are contiguous."""
+    if x.dim() != 4 or x.get_device() != device:
+        raise ValueError(f"{name} must be [batch, n, heads, head_dim] on cuda:{device}, got {tuple(x.shape)} on {x.device}")
+    shape = x.shape
+    robot, token, head, dim = x.stride()
+    if (dim != 1 and shape[3] > 1) or (head != shape[3] and shape[2] > 1):
+        raise ValueError(f"{name}: the heads of a token must be contiguous")
+    return robot if shape[0] > 1 else 0, token if shape[1] > 1 else 0
+
+
+def ravel_rotary_apply(r, x, out, starts=None, positions=None, counts=None, stream=None):
+    """x, out [B, n, heads, hd]; see ravel_decode.h."""
+    import torch
+    if getattr(r, "rotary", None) is None:
+        raise ValueError("not a handle that ravel_rotary_create returned")
+    device = r.rotary[1]
+    xr, xt = _heads(x, device, "x")
+    if out is x:
+        outr, outt = xr, xt
+    else:
+        outr, outt = _heads(out, device, "out")
+        if out.shape != x.shape or out.dtype is not x.dtype:
+            raise ValueError("out must have x's shape and dtype")
+    B, n, heads, hd = x.shape
+    i32 = torch.int32
+    _check_decode(load().ravel_rotary_apply(
+        r, B, n, heads, hd, _row_dtype(x, "x"), x.data_ptr(), xr, xt, out.data_ptr(), outr, outt,
+        _flat(starts, (B,), i32, device, "starts"), _flat(positions, (B, n), i32, device, "positions"),
+        _flat(counts, (B,), i32, device, "counts"), _stream_ptr(stream)), "ravel_rotary_apply")
+
+
+def ravel_w4_create(N: int, K: int, group: int = 128, device: int = 0):
+    h = C.c_void_p()
+    _check_decode(load().ravel_w4_create(N, K, group, device, C.byref(h)), "ravel_w4_create")
+    h.w4 = (N, K, group, device)
+    return h
+
+
+def ravel_w4_destroy(w):
+    load().ravel_w4_destroy(w)
+
+
+def _w4(w):
+    a = getattr(w, "w4", None)
+    if a is None:
+        raise ValueError("not a handle that ravel_w4_create returned")
+    return a
+
+
+def ravel_w4_load(w, codes, scales, zeros, stream=None):
+    """codes uint8 [N, (K + 1) // 2], scales bfloat16 and zeros uint8 [N, groups]; see ravel_decode.h."""
+    import torch
+    N, K, group, device = _w4(w)
+    groups = -(-K // group)
+    _check_decode(load().ravel_w4_load(
+        w, _flat(codes, (N, (K + 1) // 2), torch.uint8, device, "codes"), _flat(scales, (N, groups), torch.bfloat16, device, "scales"),
+        _flat(zeros, (N, groups), torch.uint8, device, "zeros"), _stream_ptr(stream)), "ravel_w4_load")
+
+
+def ravel_w4_quantize(W, group: int, codes, scales, zeros, stream=None):
+    """Nearest codes of W [N, K]; see ravel_decode.h."""
+    import torch
+    device = W.get_device()
+    if W.dim() != 2 or device < 0:
+        raise ValueError(f"W must be a CUDA tensor [N, K], got {tuple(W.shape)} on {W.device}")
+    N, K = W.shape
+    ldw = _matrix(W, N, K, device, "W")
+    groups = -(-K // group)
+    with torch.cuda.device(device):
+        _check_decode(load().ravel_w4_quantize(
+            W.data_ptr(), N, K, ldw, _row_dtype(W, "W"), group, _flat(codes, (N, (K + 1) // 2), torch.uint8, device, "codes"),
+            _flat(scales, (N, groups), torch.bfloat16, device, "scales"), _flat(zeros, (N, groups), torch.uint8, device, "zeros"),
+            _stream_ptr(stream)), "ravel_w4_quantize")
+
+
+def ravel_w4_read(w, out, stream=None):
+    """out [N, K], written; see ravel_decode.h."""
+    N, K, _, device = _w4(w)
+    ldo = _matrix(out, N, K, device, "out")
+    _check_decode(load().ravel_w4_read(w, out.data_ptr(), ldo, _row_dtype(out, "out"), _stream_ptr(stream)), "ravel_w4_read")
+
+
+W4_EPILOGUES = {"store": 0, "silu": 1, "add": 2, "geglu": 3}
+
+
+def ravel_w4_gemm(w, X, epi: int, out, bias=None, stream=None):
+    """out (op)= X [M, K] times the matrix's rows (+ bias); see ravel_decode.h."""
+    import torch
+    N, K, _, device = _w4(w)
+    if X.dtype is not torch.bfloat16:
+        raise ValueError(f"X must be bfloat16, got {X.dtype}")
+    M = X.shape[0]
+    lda = _matrix(X, M, K, device, "X")
+    ldo = _matrix(out, M, N // 2 if epi == 3 else N, device, "out")
+    _check_decode(load().ravel_w4_gemm(w, X.data_ptr(), M, lda, epi, out.data_ptr(), ldo, _row_dtype(out, "out"),
+                                       _flat(bias, (N,), torch.float32, device, "bias"), _stream_ptr(stream)), "ravel_w4_gemm")
+
+
+def ravel_draw_tokens(logits, u, temperature, top_k, top_p, min_p, tokens, log_probs=None, stream=None):
+    """logits [B, V]; the others [B] or None; tokens int32 and log_probs float32 [B], written; see ravel_decode.h."""
+    import torch
+    device = logits.get_device()
+    if logits.dim() != 2 or device < 0:
+        raise ValueError(f"logits must be a CUDA tensor [batch, vocab], got {tuple(logits.shape)} on {logits.device}")
+    B, V = logits.shape
+    row = _matrix(logits, B, V, device, "logits")
+    f32, i32, one = torch.float32, torch.int32, (B,)
+    if u is None or tokens is None:
+        raise ValueError("u and tokens must be given")
+    args = (logits.data_ptr(), B, V, row, _row_dtype(logits, "logits"), _flat(u, one, f32, device, "u"),
+            _flat(temperature, one, f32, device, "temperature"), _flat(top_k, one, i32, device, "top_k"),
+            _flat(top_p, one, f32, device, "top_p"), _flat(min_p, one, f32, device, "min_p"), _flat(tokens, one, i32, device, "tokens"),
+            _flat(log_probs, one, f32, device, "log_probs"))
+    if torch.cuda.current_device() == device:
+        status = load().ravel_draw_tokens(*args, _stream_ptr(stream))
+    else:
+        with torch.cuda.device(device):
+            status = load().ravel_draw_tokens(*args, _stream_ptr(stream))
+    _check_decode(status, "ravel_draw_tokens")

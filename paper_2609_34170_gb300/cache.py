@@ -43,15 +43,8 @@ class ContextCache:
             return self._current_stream(self._index)
         return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
-    def _empty(self, shape, dtype, stream):
-        """A new tensor of the stream that is going to write it."""
-        t = self.torch
-        if stream is None:
-            return t.empty(shape, dtype=dtype, device=self.device)
-        if not hasattr(stream, "cuda_stream"):
-            stream = t.cuda.ExternalStream(int(stream), device=self.device)
-        with t.cuda.stream(stream):
-            return t.empty(shape, dtype=dtype, device=self.device)
+    def _empty(self, shape, dtype, stream, zeros=False):
+        return B.new_tensor(shape, dtype, self.device, stream, zeros)
 
     # -- calls
     def append(self, layer: int, k, v, starts=None, counts=None, stream=None):
@@ -67,6 +60,17 @@ class ContextCache:
                                               self._stream(stream))
         if status:
             B._check_cache(self.handle, status, "ravel_cache_append")
+
+    def append_rotary(self, layer: int, rotary, q, k, v, starts=None, counts=None, positions=None, q_out=None, stream=None):
+        """``append`` of keys turned by a ``Rotary`` to their positions (int32 [B, n]; None:
+        starts[b] + i), and the queries q [B, n, Hq, hd] turned with them: returned, or written to
+        q_out, which may be q itself (rows from counts[b] on are not written; of a new tensor they are
+        zeros).  q None: keys alone."""
+        if q is not None and q_out is None:
+            q_out = self._empty(q.shape, q.dtype, stream, zeros=counts is not None)
+        B.ravel_cache_append_rotary(self.handle, layer, rotary.handle, q, q_out, k, v, starts, positions, counts,
+                                    self._stream(stream))
+        return q_out
 
     def attend(self, layer: int, q, lengths, counts=None, causal: bool = True, window: int = 0, sinks: int = 0,
                scale: float = 0.0, max_length: int | None = None, out=None, mass=None, add_mass: bool = False, stream=None):

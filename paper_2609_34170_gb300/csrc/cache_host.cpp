@@ -11,6 +11,7 @@
 
 #include "../../include/ravel_cache.h"
 #include "cache.h"
+#include "rotary_host.h"
 
 using namespace ravel;
 
@@ -205,6 +206,34 @@ ravel_status ravel_cache_append(ravel_cache_t* c, int layer, int batch, int n, c
   a.vec = aligned16(k, robot_stride, token_stride, c->esize) && aligned16(v, 0, 0, 1);
   const cudaError_t e = launch_cache_append(a, c->dt, (cudaStream_t)stream);
   return e == cudaSuccess ? RAVEL_OK : cuda_fail(c, e, "append");
+}
+
+ravel_status ravel_cache_append_rotary(ravel_cache_t* c, int layer, const ravel_rotary_t* r, int batch, int n, const void* q,
+                                       long long q_robot_stride, long long q_token_stride, void* q_out,
+                                       long long q_out_robot_stride, long long q_out_token_stride, const void* k,
+                                       long long k_robot_stride, long long k_token_stride, const void* v,
+                                       long long v_robot_stride, long long v_token_stride, const int* starts,
+                                       const int* positions, const int* counts, void* stream) {
+  if (!c || !r || !k || !v) return fail(c, RAVEL_EINVAL, "append_rotary: null argument");
+  if (!q != !q_out) return fail(c, RAVEL_EINVAL, "append_rotary: q and q_out go together");
+  if (q_robot_stride < 0 || q_token_stride < 0 || q_out_robot_stride < 0 || q_out_token_stride < 0 || k_robot_stride < 0 ||
+      k_token_stride < 0 || v_robot_stride < 0 || v_token_stride < 0)
+    return fail(c, RAVEL_EINVAL, "append_rotary: negative stride");
+  if (q && q == q_out && (q_robot_stride != q_out_robot_stride || q_token_stride != q_out_token_stride))
+    return fail(c, RAVEL_EINVAL, "append_rotary: in place, q and q_out need the same strides");
+  ravel_status s = check_call(c, layer, batch, "append_rotary");
+  if (s != RAVEL_OK) return s;
+  if (n < 1 || n > c->cfg.max_tokens) return fail(c, RAVEL_ESHAPE, "append_rotary: n outside [1, max_tokens]");
+  if (r->table.dims > c->cfg.head_dim) return fail(c, RAVEL_ESHAPE, "append_rotary: the table has more dims than a head");
+  if (r->device != c->device) return fail(c, RAVEL_EINVAL, "append_rotary: the table is on another device");
+  AppendRotaryArgs a{c->layer(layer), r->table, q, k, v, q_out, q_robot_stride, q_token_stride, q_out_robot_stride,
+                     q_out_token_stride, k_robot_stride, k_token_stride, v_robot_stride, v_token_stride, batch, n,
+                     c->cfg.n_q_heads / c->cfg.n_kv_heads, c->cfg.max_tokens, starts, positions, counts, 0, 0, &c->err->bits};
+  a.kv_vec = aligned16(k, k_robot_stride, k_token_stride, c->esize) && aligned16(v, v_robot_stride, v_token_stride, c->esize);
+  a.q_vec = aligned16(q, q_robot_stride, q_token_stride, c->esize) &&
+            aligned16(q_out, q_out_robot_stride, q_out_token_stride, c->esize);
+  const cudaError_t e = launch_cache_append_rotary(a, c->dt, (cudaStream_t)stream);
+  return e == cudaSuccess ? RAVEL_OK : cuda_fail(c, e, "append_rotary");
 }
 
 ravel_status ravel_cache_attend(ravel_cache_t* c, int layer, int batch, int n, const void* q, long long q_robot_stride,

@@ -4,6 +4,7 @@
 
 #include "cache.cuh"
 #include "launch.h"
+#include "rotary.cuh"
 #include "tc_common.cuh"
 
 namespace ravel {
@@ -127,6 +128,113 @@ __device__ __forceinline__ void store16(T* row, int d, int hd, int vec, const fl
 #pragma unroll
       for (int i = 0; i < 8; ++i) row[d8 + i] = y[i];
     }
+  }
+}
+
+// 16 values from dim d on of a row of heads, turned.  cs: the token's cosines and sines by pair.
+// The pair of a dim may be anywhere in the row where the halves are not whole multiples of 16: then
+// both are loaded one by one.
+template <typename T>
+__device__ __forceinline__ void load16_turned(const T* row, int d, int hd, int vec, const RotaryTable& r, const float2* cs, float* x) {
+  const int half = r.dims / 2;
+  if (d >= r.dims) {
+    load16(row, d, hd, vec, x);
+  } else if (r.interleaved && r.dims % 16 == 0) {
+    float y[16];
+    load16(row, d, hd, vec, y);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float2 t = cs[d / 2 + i];
+      x[2 * i] = turned(y[2 * i], y[2 * i + 1], t, true);
+      x[2 * i + 1] = turned(y[2 * i + 1], y[2 * i], t, false);
+    }
+  } else if (!r.interleaved && half % 16 == 0) {
+    const bool first = d < half;
+    const int pair = first ? d : d - half;
+    float y[16], z[16];
+    load16(row, d, hd, vec, y);
+    load16(row, first ? d + half : pair, hd, vec, z);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      x[i] = turned(y[i], z[i], cs[pair + i], first);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int at = d + i;
+      x[i] = at < hd ? to_f32(row[at]) : 0.f;
+      if (at < r.dims) {
+        const bool first = r.interleaved ? at % 2 == 0 : at < half;
+        const int other = r.interleaved ? at ^ 1 : first ? at + half : at - half;
+        const float2 t = cs[r.interleaved ? at / 2 : first ? at : at - half];
+        x[i] = turned(x[i], to_f32(row[other]), t, first);
+      }
+    }
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void store16(T* row, int d, int hd, int vec, const float* x);
+
+// cache_append_kernel with the keys turned on their way in, and the G query heads of the KV head
+// turned beside them: a launch and the keys' way through memory less than turning first.  The CTA's
+// 16 tokens share one table of cosines and sines.
+template <typename T>
+__global__ void __launch_bounds__(256) cache_append_rotary_kernel(AppendRotaryArgs a) {
+  __shared__ BlockShared s;
+  __shared__ float2 cs[kCacheBlock * 128];   // [token][pair]
+  pdl_trigger();
+  pdl_wait();
+  const CacheLayer& c = a.c;
+  const int b = blockIdx.z, h = blockIdx.y;
+  const int start = a.starts ? a.starts[b] : 0, count = a.counts ? a.counts[b] : a.n;
+  if (start < 0 || count < 0 || count > a.n || start > a.max_tokens - count) {
+    if (threadIdx.x == 0 && blockIdx.x == 0 && h == 0) raise_error(a.err, ERR_SHAPE);
+    return;
+  }
+  const int blk = start / kCacheBlock + blockIdx.x, end = start + count;
+  if (count == 0 || blk * kCacheBlock >= end) return;
+  const int half = a.r.dims / 2;
+  const int p0 = max(blk * kCacheBlock, start), tokens = min((blk + 1) * kCacheBlock, end) - p0;   // the new ones here
+  for (int i = threadIdx.x; i < tokens * half; i += blockDim.x) {
+    const int t = i / half, pair = i % half, at = p0 - start + t;
+    const long long position = a.positions ? a.positions[(long long)b * a.n + at] : (long long)p0 + t;
+    cs[t * half + pair] = turn_of(a.r.f[pair], position, a.r.amplitude);
+  }
+  const int tpt = c.hdp / 16;   // threads per token
+  const int token = threadIdx.x / tpt, d = (threadIdx.x % tpt) * 16;
+  const int pos = blk * kCacheBlock + token;
+  const bool fresh = pos >= start && pos < end, stay = pos < start;
+  __syncthreads();
+  float kx[16], vx[16];
+  if (fresh) {
+    const T* k = (const T*)a.k + (long long)b * a.k_robot + (long long)(pos - start) * a.k_token + (long long)h * c.hd;
+    const T* v = (const T*)a.v + (long long)b * a.v_robot + (long long)(pos - start) * a.v_token + (long long)h * c.hd;
+    load16_turned(k, d, c.hd, a.kv_vec, a.r, cs + (pos - p0) * half, kx);
+    load16(v, d, c.hd, a.kv_vec, vx);
+  }
+  const size_t head = (size_t)b * c.Hkv + h;
+  store_block<0>(s, kx, vx, fresh, stay, blk * kCacheBlock < start, token, c, (head * c.T + pos) * c.hdp,
+                 head * (c.T / kCacheBlock) + blk, d);
+  if (!a.q) return;
+  // queries: 16 dims of one head and token per turn.  A thread's 16 dims may be read by others as
+  // their pairs' other halves, so where q is written in place all of a token's heads that are at
+  // hand are read before any is written.
+  const int items = tokens * a.G * tpt;
+  for (int i0 = 0; i0 < items; i0 += blockDim.x) {
+    const int i = i0 + threadIdx.x;
+    float x[16];
+    T* to = nullptr;
+    int at = 0;
+    if (i < items) {
+      const int th = i / tpt, t = th / a.G, g = th % a.G;
+      at = (i % tpt) * 16;
+      const long long tok = p0 - start + t, head_at = (long long)(h * a.G + g) * c.hd;
+      load16_turned((const T*)a.q + (long long)b * a.q_robot + tok * a.q_token + head_at, at, c.hd, a.q_vec, a.r, cs + t * half, x);
+      to = (T*)a.q_out + (long long)b * a.qo_robot + tok * a.qo_token + head_at;
+    }
+    __syncthreads();   // (blockDim.x is a whole number of heads: 16 threads per token, tpt to a head)
+    if (to) store16(to, at, c.hd, a.q_vec, x);
   }
 }
 
@@ -425,6 +533,13 @@ cudaError_t launch_cache_append(const AppendArgs& a, Dtype dt, cudaStream_t st) 
   const dim3 grid((a.n + 2 * kCacheBlock - 2) / kCacheBlock, a.c.Hkv, a.batch);
   const Overlap overlap;
   return launch_kernel(dt == DT_BF16 ? cache_append_kernel<bf16> : cache_append_kernel<float>, grid, dim3(a.c.hdp), 0, st, 1, a);
+}
+
+cudaError_t launch_cache_append_rotary(const AppendRotaryArgs& a, Dtype dt, cudaStream_t st) {
+  const dim3 grid((a.n + 2 * kCacheBlock - 2) / kCacheBlock, a.c.Hkv, a.batch);
+  const Overlap overlap;
+  return launch_kernel(dt == DT_BF16 ? cache_append_rotary_kernel<bf16> : cache_append_rotary_kernel<float>, grid, dim3(a.c.hdp), 0,
+                       st, 1, a);
 }
 
 cudaError_t launch_cache_read(const ReadArgs& a, Dtype dt, cudaStream_t st) {

@@ -1,0 +1,84 @@
+// Internal launch API of what a decode step needs beside the context cache
+// (host side): rotary positions, products with 4-bit weights, drawing tokens.
+// Every launcher enqueues on `st` and returns the launch's cudaError_t.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "cache.h"
+#include "kernels.h"
+
+namespace ravel {
+
+// Angles as whole numbers: `f` holds f_i / (2 pi) of a turn in units of 2^-64, so that
+// position * f[i], modulo 2^64, is the fraction of a turn, whatever the position.
+struct RotaryTable {
+  const unsigned long long* f;   // device [dims / 2]
+  int dims, interleaved;
+  float amplitude;
+};
+
+struct RotaryArgs {
+  RotaryTable r;
+  const void* x;
+  void* out;
+  long long x_robot, x_token, out_robot, out_token;   // strides in elements
+  int batch, n, heads, hd;
+  const int *starts, *positions, *counts;
+  int align;   // largest power of two, up to 16, that divides every row's address and stride in bytes
+  int num_sms;
+};
+cudaError_t launch_rotary(const RotaryArgs& a, Dtype dt, cudaStream_t st);
+
+struct AppendRotaryArgs {
+  CacheLayer c;
+  RotaryTable r;
+  const void *q, *k, *v;
+  void* q_out;
+  long long q_robot, q_token, qo_robot, qo_token, k_robot, k_token, v_robot, v_token;
+  int batch, n, G, max_tokens;
+  const int *starts, *positions, *counts;
+  int kv_vec, q_vec;   // rows of k and v, of q and q_out are 16-byte aligned
+  int* err;
+};
+cudaError_t launch_cache_append_rotary(const AppendRotaryArgs& a, Dtype dt, cudaStream_t st);
+
+// A matrix of 4-bit weights in the order in which the tensor cores' fragments
+// take it (w4.cu): tiles of 16 rows, blocks of 64 columns.
+struct W4Matrix {
+  uint4* codes;       // [tiles][kblocks][32 lanes]
+  uint2* sz;          // [tiles][groups][8]: (scale, 128 + zero) of rows g and g + 8
+  int N, K, group;
+  int tiles, kblocks, groups;   // tiles: an even number
+};
+struct W4Args {
+  W4Matrix w;
+  const void* x;
+  void* out;
+  const float* bias;
+  int M, lda, ldo, epi, out_bf16;
+  int vec;            // rows of x are 16-byte aligned
+  int num_sms;
+};
+cudaError_t launch_w4_gemm(const W4Args& a, cudaStream_t st);
+cudaError_t launch_w4_load(const W4Matrix& w, const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, cudaStream_t st);
+cudaError_t launch_w4_read(const W4Matrix& w, void* out, int ldo, Dtype dt, cudaStream_t st);
+cudaError_t launch_w4_quantize(const void* W, int N, int K, int ldw, Dtype dt, int group, uint8_t* codes, uint16_t* scales,
+                               uint8_t* zeros, cudaStream_t st);
+cudaError_t init_w4_kernels();
+
+struct DrawArgs {
+  const void* logits;
+  int batch, vocab;
+  long long row;
+  const float *u, *temperature, *top_p, *min_p;
+  const int* top_k;
+  int* tokens;
+  float* log_probs;
+  int vec;            // rows are 16-byte aligned
+  int num_sms;
+};
+cudaError_t launch_draw(const DrawArgs& a, Dtype dt, cudaStream_t st);
+
+}  // namespace ravel
