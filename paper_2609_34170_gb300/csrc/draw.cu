@@ -2,10 +2,16 @@
 //
 // Weights are whole numbers, 2^43 exp((x - max) / T) rounded, so that their sums are exact and
 // the same in any order; a row is at most 2^20 long, its sum below 2^64.  The order of the tokens (by
-// logit, equal ones by index) is never made: each limit is a border in it, a key and how many of the
-// tokens with that key stay, found by a radix selection over the keys, whose histograms count tokens
-// (top-k) or add weights (top-p).  The draw sums what stays in the order of the index: sums of runs
-// first, then a walk through the run that holds the token.
+// logit, equal ones by index) is not made: a limit is a border in it, a key and how many of the
+// tokens with that key stay.
+//
+// A cluster of CTAs per row.  The row's maximum first; then a histogram of 512 bins between the
+// maximum and the least logit that has a weight, of counts and, where top-p alone limits, of weights: the
+// bin that holds the border.  Where the tokens up to that bin are at most 2048, they are brought
+// together in one CTA, which sorts them and does the rest by itself.  Where they are more, the
+// bin's own tokens are, which gives the border, and the cluster sums what stays in the order of the index: by
+// warps' runs first, then within the run that holds the token.  Where even the bin holds more
+// (thousands of nearly equal logits), a radix selection over the keys' four bytes finds the border.
 #include <algorithm>
 
 #include "common.cuh"
@@ -16,7 +22,8 @@
 namespace ravel {
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kThreads = 1024, kWarps = kThreads / 32;
+constexpr int kBins = 512, kCap = 2048;
 constexpr int kRanks = 8;        // CTAs of a row at most
 constexpr int kBits = 43;        // weight of the likeliest token: 2^43
 
@@ -110,6 +117,12 @@ __device__ __forceinline__ u64 ld_cluster_u64(uint32_t a) {
   return v;
 }
 
+__device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+
 __device__ __forceinline__ u64 warp_max_u64(u64 v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
@@ -126,21 +139,31 @@ __device__ __forceinline__ u64 warp_sum_u64(u64 v) {
 
 struct DrawShared {
   u64 table[1024];
-  u64 hist[2][256], sums[256];
-  u64 slot[2][2];             // what this CTA gives to a reduction
+  union {
+    uint32_t bins[3][kBins];    // of a CTA: counts, weights' low and high words
+    u64 hist[2][256];           // radix selection
+  };
+  u64 list[kCap];               // (key, ~index), in the order of the index
+  union {
+    u64 sorted[kCap];           // the same, from the largest down
+    float keep[kWarps][64];     // a warp's logits that wait for their weights
+  };
+  u64 slot[2][2];               // what this CTA gives to a reduction
   u64 warp_a[kWarps], warp_b[kWarps];
-  u64 all_a, all_b;           // of a reduction
-  u64 sel_left;
-  uint32_t sel_bin;
+  u64 sel_left, sel_before, sel_in;
+  uint32_t sel_bin, sel_key, listed, found_run;
+  u64 run_at, run_equal;
 };
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
   __shared__ DrawShared s;
   constexpr int V = 16 / sizeof(T);
+  constexpr uint32_t kAll = 0xffffffffu;
   const int ranks = (int)gridDim.x, rank = ranks > 1 ? (int)cluster_ctarank() : 0, b = blockIdx.y;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  for (int i = tid; i < 1024; i += kThreads) s.table[i] = kExp.v[i];
+  const float inf = __uint_as_float(0x7f800000u);
+  s.table[tid] = kExp.v[tid];
   pdl_trigger();
   pdl_wait();
   const T* row = (const T*)a.logits + (long long)b * a.row;
@@ -158,247 +181,494 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
       for (int j = 0; j < V; ++j) x[j] = to_f32(t[j]);
     } else {
 #pragma unroll
-      for (int j = 0; j < V; ++j) x[j] = i + j < a.vocab ? to_f32(row[i + j]) : __uint_as_float(0xff800000u);
+      for (int j = 0; j < V; ++j) x[j] = i + j < a.vocab ? to_f32(row[i + j]) : -inf;
     }
   };
+  auto index_of = [&](int step, int j) { return (step * 32 + lane) * V + j; };
   int turn = 0;
   auto barrier = [&] {
     if (ranks > 1) cluster_sync();
     else __syncthreads();
   };
-  // maximum (or sum) of x and sum of y over the row's threads, for every thread
+  auto from_rank = [&](const u64* p, int i) { return ranks > 1 ? ld_cluster_u64(mapa_shared(smem_u32(p), (uint32_t)i)) : *p; };
+  // maxima or sums of x and of y over the row's threads, for every thread
   auto reduce = [&](u64 x, u64 y, bool maximum, u64& rx, u64& ry) {
     x = maximum ? warp_max_u64(x) : warp_sum_u64(x);
-    y = warp_sum_u64(y);
+    y = maximum ? warp_max_u64(y) : warp_sum_u64(y);
     if (lane == 0) s.warp_a[warp] = x, s.warp_b[warp] = y;
     __syncthreads();
     if (warp == 0) {
-      u64 p = lane < kWarps ? s.warp_a[lane] : 0ull, r = lane < kWarps ? s.warp_b[lane] : 0ull;
+      u64 p = s.warp_a[lane], r = s.warp_b[lane];
       p = maximum ? warp_max_u64(p) : warp_sum_u64(p);
-      r = warp_sum_u64(r);
+      r = maximum ? warp_max_u64(r) : warp_sum_u64(r);
       if (lane == 0) s.slot[turn][0] = p, s.slot[turn][1] = r;
     }
     barrier();
     rx = ry = 0ull;
     for (int i = 0; i < ranks; ++i) {
-      u64 p, r;
-      if (ranks > 1) {
-        const uint32_t at = mapa_shared(smem_u32(&s.slot[turn][0]), (uint32_t)i);
-        p = ld_cluster_u64(at);
-        r = ld_cluster_u64(at + 8);
-      } else {
-        p = s.slot[turn][0], r = s.slot[turn][1];
-      }
-      rx = maximum ? (p > rx ? p : rx) : rx + p;
-      ry += r;
+      const u64 p = from_rank(&s.slot[turn][0], i), r = from_rank(&s.slot[turn][1], i);
+      rx = maximum ? max(p, rx) : rx + p;
+      ry = maximum ? max(r, ry) : ry + r;
     }
     turn ^= 1;
   };
-
-  // the first of the order, and what is no number
-  u64 best = 0, bad = 0;
-  for (int step = step0; step < step1; ++step) {
-    float x[V];
-    load(step, x);
+  // sum of x over the threads before this one and, in all, over the CTA
+  auto block_scan = [&](u64 x, u64& all) {
+    u64 upto = x;
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      bad += !(x[j] < __uint_as_float(0x7f800000u));
-      const u64 c = (u64)key_of(x[j]) << 32 | (0xffffffffu - (uint32_t)((step * 32 + lane) * V + j));
-      best = c > best ? c : best;
+    for (int o = 1; o < 32; o <<= 1) {
+      const u64 up = __shfl_up_sync(kAll, upto, o);
+      if (lane >= o) upto += up;
     }
-  }
-  reduce(best, bad, true, best, bad);
-  const float top = value_of((uint32_t)(best >> 32));
-  const float u = a.u[b], t = a.temperature ? a.temperature[b] : 1.f, p = a.top_p ? a.top_p[b] : 1.f, mp = a.min_p ? a.min_p[b] : 0.f;
-  const int k = a.top_k ? a.top_k[b] : 0;
-  const float inf = __uint_as_float(0x7f800000u);
-  if (bad || !(top > -inf) || !(u >= 0.f && u < 1.f) || !(t < inf) || p != p || mp != mp) {
-    if (rank == 0 && tid == 0) {
-      a.tokens[b] = -1;
-      if (a.log_probs) a.log_probs[b] = -inf;
+    __syncthreads();
+    if (lane == 31) s.warp_a[warp] = upto;
+    __syncthreads();
+    u64 w = s.warp_a[lane], ws = w;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const u64 up = __shfl_up_sync(kAll, ws, o);
+      if (lane >= o) ws += up;
     }
-    barrier();   // (nobody leaves while its slot is read)
-    return;
-  }
-  if (t < 0x1p-20f) {
-    if (rank == 0 && tid == 0) {
-      a.tokens[b] = (int)(0xffffffffu - (uint32_t)best);
-      if (a.log_probs) a.log_probs[b] = 0.f;
-    }
-    barrier();
-    return;
-  }
-  Weigher weigh;
-  weigh.set(top, (double)t);
-
-  // Key of the token at which the sum over the tokens of keys above `above`, from the first of the
-  // order on, reaches `target`; left: what of the target its key's tokens have to give.
-  auto select = [&](u64 target, uint32_t above, bool weights, u64& left) -> uint32_t {
-    uint32_t prefix = 0u, mask = 0u;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      u64* hist = s.hist[turn];
-      if (tid < 256) hist[tid] = 0ull;
-      __syncthreads();
-      for (int step = step0; step < step1; ++step) {
-        float x[V];
-        load(step, x);
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          const uint32_t key = key_of(x[j]);
-          if (key > above && (key & mask) == prefix && (step * 32 + lane) * V + j < a.vocab) {
-            const u64 w = weights ? weigh(x[j], s.table) : 1ull;
-            if (w) atomicAdd(&hist[(key >> shift) & 255u], w);
-          }
-        }
-      }
-      barrier();
-      if (tid < 256) {
-        u64 n = 0;
-        for (int i = 0; i < ranks; ++i) n += ranks > 1 ? ld_cluster_u64(mapa_shared(smem_u32(&hist[tid]), (uint32_t)i)) : hist[tid];
-        s.sums[tid] = n;
-      }
-      __syncthreads();
-      if (warp == 0) {
-        // lane i holds bins 255 - 8i .. 248 - 8i, from the first of the order down
-        u64 n[8], sum = 0;
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          n[q] = s.sums[255 - 8 * lane - q];
-          sum += n[q];
-        }
-        u64 before = sum;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const u64 up = __shfl_up_sync(0xffffffffu, before, o);
-          if (lane >= o) before += up;
-        }
-        before -= sum;
-        if (before < target && before + sum >= target) {
-          bool found = false;
-#pragma unroll
-          for (int q = 0; q < 8; ++q) {
-            if (!found && before + n[q] >= target) {
-              s.sel_bin = (uint32_t)(255 - 8 * lane - q);
-              s.sel_left = target - before;
-              found = true;
-            }
-            before += n[q];
-          }
-        }
-      }
-      __syncthreads();
-      prefix |= s.sel_bin << shift;
-      mask |= 255u << shift;
-      target = s.sel_left;
-      turn ^= 1;
-    }
-    left = target;
-    return prefix;
+    all = __shfl_sync(kAll, ws, 31);
+    return __shfl_sync(kAll, ws - w, warp) + upto - x;
   };
 
-  // The border: tokens of keys above it stay, and of those with its key the first `ties`.
-  uint32_t border = 0u;   // (below every key)
-  u64 ties = 0ull;
-  if (k > 0 && k < a.vocab) border = select((u64)k, 0u, false, ties);
-  if (p < 1.f) {
-    u64 all = 0, none;
-    for (int step = step0; step < step1; ++step) {
-      float x[V];
-      load(step, x);
-#pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (key_of(x[j]) > border) all += weigh(x[j], s.table);
-    }
-    reduce(all, 0ull, false, all, none);
-    const u64 one = ties ? weigh(value_of(border), s.table) : 0ull;
-    const u64 want = max(1ull, p > 0.f ? times_fraction(all + ties * one, p, true) : 0ull);
-    u64 left;
-    if (want <= all) {
-      border = select(want, border, true, left);
-      const u64 w = weigh(value_of(border), s.table);
-      ties = (left + w - 1) / w;
-    } else {   // the tokens that top-k left at its border
-      ties = min(ties, (want - all + one - 1) / max(one, 1ull));
-    }
-  }
-  if (mp > 0.f) {
-    const double least = (double)top + (double)t * log((double)fminf(mp, 1.f));
-    float f = (float)least;
-    if ((double)f < least) f = nextafterf(f, inf);
-    const uint32_t key = key_of(f);
-    if (key > border) {
-      border = key - 1u;
-      ties = 0ull;
-    }
-  }
-
-  // What stays, summed by warps' runs.
-  const u64 one = ties ? weigh(value_of(border), s.table) : 0ull;
-  u64 sum = 0, equal = 0;
+  // the first of the order, the least finite logit, and what is no number
+  u64 best = 0, low = 0;
+#pragma unroll 2
   for (int step = step0; step < step1; ++step) {
     float x[V];
     load(step, x);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       const uint32_t key = key_of(x[j]);
-      if (key > border) sum += weigh(x[j], s.table);
-      equal += key == border && (step * 32 + lane) * V + j < a.vocab;
+      const u64 c = (u64)key << 32 | (kAll - (uint32_t)index_of(step, j));
+      best = c > best ? c : best;
+      if (!(x[j] < inf)) low |= 1ull << 32;
+      else if (x[j] > -inf) low = (low & 1ull << 32) | max((uint32_t)low, ~key);
     }
   }
-  u64 all, all_equal;
-  reduce(sum, equal, false, all, all_equal);
-  sum = warp_sum_u64(sum);
-  equal = warp_sum_u64(equal);
-  const u64 total = all + min(ties, all_equal) * one;
-  const u64 at = times_fraction(total, u, false);   // the token's run of the sum holds this
-  // before this warp's run: the ranks before, the warps before
-  u64 before = 0, equal_before = 0;
-  for (int i = 0; i < rank; ++i) {
-    const uint32_t from = mapa_shared(smem_u32(&s.slot[turn ^ 1][0]), (uint32_t)i);
-    before += ld_cluster_u64(from);
-    equal_before += ld_cluster_u64(from + 8);
+  reduce(best, low, true, best, low);
+  const float top = value_of((uint32_t)(best >> 32));
+  const float u = a.u[b], t = a.temperature ? a.temperature[b] : 1.f, p = a.top_p ? a.top_p[b] : 1.f, mp = a.min_p ? a.min_p[b] : 0.f;
+  int k = a.top_k ? a.top_k[b] : 0;
+  auto answer = [&](int token, float log_prob) {
+    a.tokens[b] = token;
+    if (a.log_probs) a.log_probs[b] = log_prob;
+  };
+  const bool none = low >> 32 || !(top > -inf) || !(u >= 0.f && u < 1.f) || !(t < inf) || p != p || mp != mp;
+  if (none || t < 0x1p-20f) {
+    if (rank == 0 && tid == 0) {
+      if (none) answer(-1, -inf);
+      else answer((int)(kAll - (uint32_t)best), 0.f);
+    }
+    barrier();   // (nobody leaves while its slot is read)
+    return;
   }
-  for (int i = 0; i < warp; ++i) before += s.warp_a[i], equal_before += s.warp_b[i];
-  auto upto = [&](u64 w, u64 n) { return w + min(ties, n) * one; };
-  if (upto(before, equal_before) <= at && at < upto(before + sum, equal_before + equal)) {
+  Weigher weigh;
+  weigh.set(top, (double)t);
+  auto log_prob = [&](float x, u64 total) {
+    return (float)(((double)x - (double)top) / (double)t - log((double)total * 0x1p-43));
+  };
+  // least key that min-p lets through
+  uint32_t least = 0u;
+  if (mp > 0.f) {
+    const double limit = (double)top + (double)t * log((double)fminf(mp, 1.f));
+    float f = (float)limit;
+    if ((double)f < limit) f = nextafterf(f, inf);
+    least = key_of(f);
+  }
+
+  // Bins of the order: equal parts of the log2 domain from the maximum down to the least logit or
+  // to 2^-44, where weights end; the last one for what has none.  Every step of the formula is
+  // monotone in x, rounding included.
+  const float y_least = fmaxf((0.5f * value_of(~(uint32_t)low) - weigh.top) * weigh.ch, -44.f);
+  const float per_bin = (float)(kBins - 1) / fmaxf(-y_least, 0x1p-40f);
+  auto bin_of = [&](float x) {
+    const float y = (0.5f * x - weigh.top) * weigh.ch;
+    return y > -44.f ? (uint32_t)min((int)(-y * per_bin), kBins - 2) : (uint32_t)(kBins - 1);
+  };
+  // The bin at which `part` 0 (counts) or 1 (weights), summed from the first on, reaches `target`, what
+  // comes before it and what is in it; target > all: the last one.  For every thread of the row.
+  auto bin_at = [&](int part, auto target_of, uint32_t& bin, u64& before, u64& in) {
+    u64 n = 0;
+    if (tid < kBins) {
+      if (part == 0) {
+        for (int i = 0; i < ranks; ++i) n += ranks > 1 ? ld_cluster_u32(mapa_shared(smem_u32(&s.bins[0][tid]), (uint32_t)i)) : s.bins[0][tid];
+      } else {
+        for (int i = 0; i < ranks; ++i) {
+          const uint32_t lo = ranks > 1 ? ld_cluster_u32(mapa_shared(smem_u32(&s.bins[1][tid]), (uint32_t)i)) : s.bins[1][tid];
+          const uint32_t hi = ranks > 1 ? ld_cluster_u32(mapa_shared(smem_u32(&s.bins[2][tid]), (uint32_t)i)) : s.bins[2][tid];
+          n += (u64)hi << 32 | lo;
+        }
+      }
+    }
+    u64 all;
+    const u64 cum = block_scan(n, all);
+    const u64 target = target_of(all);
+    if (tid == 0) s.sel_bin = kBins - 1, s.sel_before = all, s.sel_in = 0;
+    __syncthreads();
+    if (tid < kBins && cum < target && cum + n >= target) s.sel_bin = tid, s.sel_before = cum, s.sel_in = n;
+    __syncthreads();
+    bin = s.sel_bin, before = s.sel_before, in = s.sel_in;
+  };
+  // Tokens of the bins first .. last, in the order of the index, into rank 0's list; their number.
+  auto gather = [&](uint32_t first, uint32_t last) {
+    auto wanted = [&](float x, int i) {
+      const uint32_t bin = bin_of(x);
+      return bin >= first && bin <= last && i < a.vocab;
+    };
+    uint32_t n = 0;
+#pragma unroll 2
     for (int step = step0; step < step1; ++step) {
       float x[V];
       load(step, x);
-      u64 w = 0, n = 0;
+#pragma unroll
+      for (int j = 0; j < V; ++j) n += wanted(x[j], index_of(step, j));
+    }
+    n = __reduce_add_sync(kAll, n);
+    u64 all;
+    u64 at = block_scan(lane == 0 ? n : 0ull, all);
+    at = __shfl_sync(kAll, at, 0);
+    if (n) {
+      for (int step = step0; step < step1; ++step) {
+        float x[V];
+        load(step, x);
+        uint32_t mine = 0;
+#pragma unroll
+        for (int j = 0; j < V; ++j) mine += wanted(x[j], index_of(step, j));
+        if (!__any_sync(kAll, mine)) continue;
+        uint32_t upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const uint32_t up = __shfl_up_sync(kAll, upto, o);
+          if (lane >= o) upto += up;
+        }
+        uint32_t to = (uint32_t)at + upto - mine;
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+          if (wanted(x[j], index_of(step, j))) s.list[to++] = (u64)key_of(x[j]) << 32 | (kAll - (uint32_t)index_of(step, j));
+        at += __shfl_sync(kAll, upto, 31);
+      }
+    }
+    if (tid == 0) s.slot[turn][0] = all;
+    barrier();
+    int total = (int)all;
+    if (rank == 0 && ranks > 1) {
+      for (int flat = (int)all + tid; flat < kCap; flat += kThreads) {   // behind its own
+        int i = flat - (int)all, r = 1;
+        for (; r < ranks; ++r) {
+          const int of = (int)from_rank(&s.slot[turn][0], r);
+          if (i < of) break;
+          i -= of;
+        }
+        if (r < ranks) s.list[flat] = from_rank(&s.list[i], r);
+      }
+      for (int r = 1; r < ranks; ++r) total += (int)from_rank(&s.slot[turn][0], r);
+      __syncthreads();
+    }
+    turn ^= 1;
+    return total;   // (of rank 0)
+  };
+  // s.sorted: the n values of s.list from the largest down, zeros behind; a bitonic network
+  auto sort = [&](int n) {
+    int size = 64;
+    while (size < n) size *= 2;
+    for (int i = tid; i < size; i += kThreads) s.sorted[i] = i < n ? s.list[i] : 0ull;
+    __syncthreads();
+    for (int run = 2; run <= size; run *= 2)
+      for (int stride = run / 2; stride > 0; stride /= 2) {
+        if (tid < size / 2) {
+          const int i = 2 * tid - (tid & (stride - 1)), j = i + stride;
+          const u64 x = s.sorted[i], y = s.sorted[j];
+          if ((x < y) == ((i & run) == 0)) s.sorted[i] = y, s.sorted[j] = x;
+        }
+        // (up to 32 apart, a warp's pairs stay within its own 64 values)
+        if (stride > 32 || (stride == 1 && run >= 64)) __syncthreads();
+        else __syncwarp();
+      }
+    __syncthreads();
+  };
+
+  // The border: tokens of keys above it stay, and of those with its key the first `ties`.
+  uint32_t border = 0u;   // (below every key)
+  u64 ties = 0ull;
+  const bool by_count = k > 0 && k < a.vocab, by_weight = p < 1.f;
+  bool radix = false;
+  if (by_count || by_weight) {
+    for (int i = tid; i < kBins; i += kThreads) s.bins[0][i] = s.bins[1][i] = s.bins[2][i] = 0u;
+    __syncthreads();
+#pragma unroll 2
+    for (int step = step0; step < step1; ++step) {
+      float x[V];
+      load(step, x);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const uint32_t key = key_of(x[j]);
-        if (key > border) w += weigh(x[j], s.table);
-        n += key == border && (step * 32 + lane) * V + j < a.vocab;
+        const uint32_t bin = bin_of(x[j]);
+        if (bin == kBins - 1) continue;
+        atomicAdd(&s.bins[0][bin], 1u);
+        if (!by_count) {
+          const u64 w = weigh(x[j], s.table);
+          const uint32_t lo = (uint32_t)w, was = atomicAdd(&s.bins[1][bin], lo);
+          atomicAdd(&s.bins[2][bin], (uint32_t)(w >> 32) + (was + lo < was ? 1u : 0u));
+        }
       }
-      u64 wi = w, ni = n;   // up to and with this lane
+    }
+    barrier();
+    uint32_t bin, cbin;
+    u64 before = 0, in = 0, count = 0, cin = 0, want = 0;
+    if (by_count) {
+      bin_at(0, [&](u64) { return (u64)k; }, cbin, count, cin);
+      bin = cbin;
+      if (bin == kBins - 1) k = 0;   // what top-k leaves out has no weight
+      count += cin;
+    } else {
+      bin_at(1, [&](u64 all) { return want = max(1ull, p > 0.f ? times_fraction(all, p, true) : 0ull); }, bin, before, in);
+      // tokens up to that bin and in it
+      u64 n = 0;
+      if (tid <= bin)
+        for (int i = 0; i < ranks; ++i) n += ranks > 1 ? ld_cluster_u32(mapa_shared(smem_u32(&s.bins[0][tid]), (uint32_t)i)) : s.bins[0][tid];
+      block_scan(n, count);
+      block_scan(tid == bin ? n : 0ull, cin);
+    }
+    if (by_count && k == 0 && by_weight) {
+      radix = true;
+    } else if (by_count && k == 0) {
+      // nothing is left out
+    } else if (count <= kCap) {
+      // all that can stay comes together in rank 0, which goes on alone
+      const int n = gather(0u, bin);
+      if (rank == 0) {
+        sort(n);
+        const int kept = by_count ? k : n;   // (k <= n)
+        // two tokens per thread, from the first of the order on
+        u64 w[2];
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const u64 wu = __shfl_up_sync(0xffffffffu, wi, o), nu = __shfl_up_sync(0xffffffffu, ni, o);
-        if (lane >= o) wi += wu, ni += nu;
+        for (int i = 0; i < 2; ++i) w[i] = 2 * tid + i < kept ? weigh(value_of((uint32_t)(s.sorted[2 * tid + i] >> 32)), s.table) : 0ull;
+        u64 all;
+        const u64 cum = block_scan(w[0] + w[1], all);
+        if (by_count) want = by_weight ? max(1ull, p > 0.f ? times_fraction(all, p, true) : 0ull) : all;
+        if (!by_weight) want = ~0ull;   // (what stays ends with the kept)
+        if (tid == 0) s.sel_left = s.sorted[kept - 1];
+        __syncthreads();
+        if (cum < want && cum + w[0] >= want) s.sel_left = s.sorted[2 * tid];
+        else if (cum + w[0] < want && cum + w[0] + w[1] >= want) s.sel_left = s.sorted[2 * tid + 1];
+        __syncthreads();
+        const u64 last = max(s.sel_left, (u64)least << 32);
+        // the draw, in the order of the index
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const u64 c = 2 * tid + i < n ? s.list[2 * tid + i] : 0ull;
+          w[i] = 2 * tid + i < n && c >= last ? weigh(value_of((uint32_t)(c >> 32)), s.table) : 0ull;
+        }
+        u64 total;
+        const u64 sum = block_scan(w[0] + w[1], total);
+        const u64 at = times_fraction(total, u, false);
+        if (sum <= at && at < sum + w[0] + w[1]) {
+          const u64 c = s.list[2 * tid + (sum + w[0] <= at)];
+          answer((int)(kAll - (uint32_t)c), log_prob(value_of((uint32_t)(c >> 32)), total));
+        }
       }
-      const bool there = upto(before + wi, equal_before + ni) > at;
-      const unsigned mask = __ballot_sync(0xffffffffu, there);
-      if (mask) {
-        if (lane == __ffs(mask) - 1) {
-          u64 c = before + wi - w, e = equal_before + ni - n;
+      barrier();   // nobody leaves while its list is read
+      return;
+    } else if (cin <= kCap && !(by_count && by_weight)) {
+      // the border's bin alone, whose sorted tokens hold the border
+      const int n = gather(bin, bin);
+      if (rank == 0) {
+        sort(n);
+        u64 last;
+        if (by_count) {
+          last = s.sorted[k - (int)(count - cin) - 1];
+        } else {
+          u64 w[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) w[i] = 2 * tid + i < n ? weigh(value_of((uint32_t)(s.sorted[2 * tid + i] >> 32)), s.table) : 0ull;
+          u64 all;
+          const u64 cum = before + block_scan(w[0] + w[1], all);
+          if (cum < want && cum + w[0] >= want) s.sel_left = s.sorted[2 * tid];
+          else if (cum + w[0] < want && cum + w[0] + w[1] >= want) s.sel_left = s.sorted[2 * tid + 1];
+          __syncthreads();
+          last = s.sel_left;
+        }
+        u64 equal = 0;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const u64 c = 2 * tid + i < n ? s.sorted[2 * tid + i] : 0ull;
+          equal += c >> 32 == last >> 32 && c >= last;
+        }
+        u64 all;
+        block_scan(equal, all);
+        if (tid == 0) s.slot[turn][0] = last >> 32, s.slot[turn][1] = all;
+      }
+      barrier();
+      border = (uint32_t)from_rank(&s.slot[turn][0], 0);
+      ties = from_rank(&s.slot[turn][1], 0);
+      turn ^= 1;
+    } else {
+      radix = true;
+    }
+  }
+
+  if (radix) {
+    // Key of the token at which the sum over the tokens of keys above `above`, from the first of the
+    // order on, reaches `target`; left: what of the target its key's tokens have to give.
+    auto select = [&](u64 target, uint32_t above, bool weights, u64& left) -> uint32_t {
+      uint32_t prefix = 0u, mask = 0u;
+      for (int shift = 24; shift >= 0; shift -= 8) {
+        u64* hist = s.hist[turn];
+        if (tid < 256) hist[tid] = 0ull;
+        __syncthreads();
+        for (int step = step0; step < step1; ++step) {
+          float x[V];
+          load(step, x);
 #pragma unroll
           for (int j = 0; j < V; ++j) {
             const uint32_t key = key_of(x[j]);
-            const int i = (step * 32 + lane) * V + j;
-            const u64 was = upto(c, e);
-            if (key > border) c += weigh(x[j], s.table);
-            e += key == border && i < a.vocab;
-            if (was <= at && upto(c, e) > at) {
-              a.tokens[b] = i;
-              if (a.log_probs) a.log_probs[b] = (float)(((double)x[j] - (double)top) / (double)t - log((double)total * 0x1p-43));
+            if (key > above && (key & mask) == prefix && index_of(step, j) < a.vocab) {
+              const u64 w = weights ? weigh(x[j], s.table) : 1ull;
+              if (w) atomicAdd(&hist[(key >> shift) & 255u], w);
             }
           }
         }
-        break;
+        barrier();
+        // bins from the first of the order down
+        u64 n = 0;
+        if (tid < 256)
+          for (int i = 0; i < ranks; ++i) n += from_rank(&hist[255 - tid], i);
+        u64 all;
+        const u64 cum = block_scan(n, all);
+        if (tid < 256 && cum < target && cum + n >= target) s.sel_bin = 255u - tid, s.sel_left = target - cum;
+        __syncthreads();
+        prefix |= s.sel_bin << shift;
+        mask |= 255u << shift;
+        target = s.sel_left;
+        turn ^= 1;
       }
-      before += __shfl_sync(0xffffffffu, wi, 31);
-      equal_before += __shfl_sync(0xffffffffu, ni, 31);
+      left = target;
+      return prefix;
+    };
+    barrier();   // (the histograms lie where the bins are read)
+    if (k > 0 && by_count) border = select((u64)k, 0u, false, ties);
+    if (by_weight) {
+      u64 all = 0, nothing;
+      for (int step = step0; step < step1; ++step) {
+        float x[V];
+        load(step, x);
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+          if (key_of(x[j]) > border) all += weigh(x[j], s.table);
+      }
+      reduce(all, 0ull, false, all, nothing);
+      const u64 one = ties ? weigh(value_of(border), s.table) : 0ull;
+      const u64 want = max(1ull, p > 0.f ? times_fraction(all + ties * one, p, true) : 0ull);
+      if (want <= all) {
+        u64 left;
+        border = select(want, border, true, left);
+        const u64 w = weigh(value_of(border), s.table);
+        ties = (left + w - 1) / w;
+      } else {   // the tokens that top-k left at its border
+        ties = min(ties, (want - all + one - 1) / max(one, 1ull));
+      }
+    }
+  }
+  if (least > border) {
+    border = least - 1u;
+    ties = 0ull;
+  }
+
+  // What stays, summed by warps' runs.  Its logits are collected until there are weights for a
+  // whole warp to compute.
+  const u64 one = ties ? weigh(value_of(border), s.table) : 0ull;
+  u64 sum = 0, equal = 0;
+  if (border == 0u) {
+    for (int step = step0; step < step1; ++step) {
+      float x[V];
+      load(step, x);
+#pragma unroll
+      for (int j = 0; j < V; ++j) sum += weigh(x[j], s.table);
+    }
+  } else {
+    float* keep = s.keep[warp];
+    uint32_t n = 0;
+#pragma unroll 2
+    for (int step = step0; step < step1; ++step) {
+      float x[V];
+      load(step, x);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const uint32_t key = key_of(x[j]);
+        equal += key == border && index_of(step, j) < a.vocab;
+        const uint32_t mask = __ballot_sync(kAll, key > border);
+        if (mask == 0u) continue;
+        if (key > border) keep[n + __popc(mask & ((1u << lane) - 1u))] = x[j];
+        n += __popc(mask);
+        __syncwarp();
+        if (n >= 32u) {
+          n -= 32u;
+          sum += weigh(keep[n + lane], s.table);
+          __syncwarp();
+        }
+      }
+    }
+    if ((uint32_t)lane < n) sum += weigh(keep[lane], s.table);
+  }
+  u64 all, all_equal;
+  reduce(sum, equal, false, all, all_equal);
+  const u64 total = all + min(ties, all_equal) * one;
+  const u64 at = times_fraction(total, u, false);   // the token's part of the sum holds this
+  auto upto = [&](u64 w, u64 n) { return w + min(ties, n) * one; };
+  // before this rank
+  u64 before = 0, equal_before = 0;
+  for (int i = 0; i < rank; ++i) before += from_rank(&s.slot[turn ^ 1][0], i), equal_before += from_rank(&s.slot[turn ^ 1][1], i);
+  const u64 mine = s.slot[turn ^ 1][0], mine_equal = s.slot[turn ^ 1][1];
+  if (upto(before, equal_before) <= at && at < upto(before + mine, equal_before + mine_equal)) {
+    // the token is in this CTA: in which warp's run
+    sum = s.warp_a[warp], equal = s.warp_b[warp];
+    for (int i = 0; i < warp; ++i) before += s.warp_a[i], equal_before += s.warp_b[i];
+    if (lane == 0 && upto(before, equal_before) <= at && at < upto(before + sum, equal_before + equal))
+      s.found_run = (uint32_t)warp, s.run_at = before, s.run_equal = equal_before;
+    __syncthreads();
+    // that run again, by all warps: 32 of its steps at a time, a step to a warp
+    const int fshare = rank * kWarps + (int)s.found_run;
+    const int f0 = (int)((long long)steps_all * fshare / shares), f1 = (int)((long long)steps_all * (fshare + 1) / shares);
+    before = s.run_at, equal_before = s.run_equal;
+    for (int base = f0; base < f1; base += kWarps) {
+      const int step = base + warp;
+      float x[V];
+      u64 w[V], ws = 0, ns = 0;
+#pragma unroll
+      for (int j = 0; j < V; ++j) x[j] = -inf;
+      if (step < f1) load(step, x);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const uint32_t key = key_of(x[j]);
+        w[j] = key > border ? weigh(x[j], s.table) : 0ull;
+        ws += w[j];
+        ns += key == border && index_of(step, j) < a.vocab && step < f1;
+      }
+      u64 wi = ws, ni = ns;   // up to and with this lane
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const u64 wu = __shfl_up_sync(kAll, wi, o), nu = __shfl_up_sync(kAll, ni, o);
+        if (lane >= o) wi += wu, ni += nu;
+      }
+      __syncthreads();
+      if (lane == 31) s.warp_a[warp] = wi, s.warp_b[warp] = ni;
+      __syncthreads();
+      u64 c = before, e = equal_before;
+      for (int i = 0; i < kWarps; ++i) {
+        if (i == warp) c += wi - ws, e += ni - ns;
+        if (i < warp) c += s.warp_a[i], e += s.warp_b[i];
+        before += s.warp_a[i], equal_before += s.warp_b[i];
+      }
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const u64 was = upto(c, e);
+        c += w[j];
+        e += key_of(x[j]) == border && index_of(step, j) < a.vocab && step < f1;
+        if (was <= at && upto(c, e) > at) answer(index_of(step, j), log_prob(x[j], total));
+      }
+      if (upto(before, equal_before) > at) break;   // (all threads: the same sums)
     }
   }
   barrier();   // nobody leaves while its sums are read
@@ -411,8 +681,7 @@ cudaError_t launch_draw(const DrawArgs& a, Dtype dt, cudaStream_t st) {
   int ranks = 1;
   while (ranks < kRanks && (long long)a.batch * ranks * 2 <= a.num_sms && a.vocab >= ranks * 2 * 4096) ranks *= 2;
   const Overlap overlap;
-  return launch_kernel_cluster(dt == DT_BF16 ? draw_kernel<bf16> : draw_kernel<float>, dim3(ranks, a.batch), dim3(kThreads), 0, st,
-                               dim3(ranks, 1, 1), a);
+  return launch_kernel_cluster(dt == DT_BF16 ? draw_kernel<bf16> : draw_kernel<float>, dim3(ranks, a.batch), dim3(kThreads), 0, st, dim3(ranks, 1, 1), a);
 }
 
 }  // namespace ravel
