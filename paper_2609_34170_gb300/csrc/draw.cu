@@ -29,12 +29,12 @@ constexpr int kBits = 43;        // weight of the likeliest token: 2^43
 
 typedef unsigned long long u64;
 
-// 2^(-j / 1024) in units of 2^-62
+// 2^(j / 1024) in units of 2^-62
 struct ExpTable {
   u64 v[1024];
   constexpr ExpTable() : v() {
     for (int j = 0; j < 1024; ++j) {
-      const double x = -0.6931471805599453094 * j / 1024.0;
+      const double x = 0.6931471805599453094 * j / 1024.0;
       double term = 1.0, sum = 1.0;
       for (int i = 1; i < 22; ++i) {
         term *= x / i;
@@ -56,38 +56,33 @@ __device__ __forceinline__ float value_of(uint32_t key) {
 }
 
 // exp((x - top) / T) as a whole number.  In the log2 domain y = (x - top) * c with c = log2(e) / T
-// in two floats and the difference and its product with their rounding errors, then in units of
-// 2^-46: 2^y = 2^-n 2^(-j / 1024) 2^-g with the middle one from a table and 2^-g = 1 - r, r below 2^-10,
-// from its series (the first term as a whole number, the others in fp32).  About 2^-43 of the
+// in two floats, and the difference and its product with their rounding errors: yh + ye.  With q
+// the nearest whole number to 1024 yh, 2^y = 2^(q / 1024) 2^f, the first factor from a table, 2^f = 1 + r
+// from its series, r below 2^-11, whose first term is a product in two floats.  About 2^-43 of the
 // weight off.  (In fp32 a weight is 2^-22 off and its error grows with x: at 100000 tokens one
 // border in a hundred falls elsewhere than in 64 bits.)
 struct Weigher {
   float top, ch, cl;   // half the largest logit; twice log2(e) / T
-  __device__ __forceinline__ void set(float max, double temperature) {
-    const double c = 2.0 * 1.4426950408889634074 / temperature;
-    top = 0.5f * max;   // (halves, so that no difference overflows)
-    ch = (float)c;
-    cl = (float)(c - (double)ch);
-  }
   __device__ __forceinline__ u64 operator()(float logit, const u64* table) const {
-    const float x = 0.5f * logit;
+    const float x = 0.5f * logit;   // (halves, so that no difference overflows)
     const float dh = x - top;
     const float v = dh - x, dl = (x - (dh - v)) - (top + v);
     const float yh = dh * ch;
     if (!(yh > -44.f)) return 0ull;
     const float ye = __fmaf_rn(dh, ch, -yh) + __fmaf_rn(dh, cl, dl * ch);
-    const int i1 = __float2int_rn(yh * 0x1p24f);
-    const float rest = __fmaf_rn(-(float)i1, 0x1p-24f, yh) + ye;
-    const long long Y = ((long long)i1 << 22) + __float2int_rn(rest * 0x1p46f);
-    const u64 U = Y < 0 ? (u64)-Y : 0ull;
-    const int n = (int)(U >> 46);
-    const u64 t = table[(U >> 36) & 1023];
-    const uint32_t g = (uint32_t)((U & 0xfffffffffull) >> 4);   // 2^-42
-    const uint32_t gl = __umulhi(g, 0xb17217f8u);               // times ln 2
-    const float gf = (float)gl * 0x1p-42f;
-    const uint32_t r = gl - __float2uint_rn(gf * gf * (0.5f - gf * 0.16666667f) * 0x1p42f);
-    const u64 w = t - (((u64)(uint32_t)(t >> 32) * r + __umulhi((uint32_t)t, r)) >> 10);
-    return (w + (1ull << (62 - kBits - 1 + n))) >> (62 - kBits + n);
+    const float shifted = __fmaf_rn(yh, 1024.f, 12582912.f);   // 1.5 * 2^23: q in the low bits
+    const int q = __float_as_int(shifted) - 0x4b400000;
+    const float rest = __fmaf_rn(shifted - 12582912.f, -0x1p-10f, yh);   // exact, up to 2^-11
+    // r in units of 2^-42: ln 2 rest as a float and what it lacks, the small terms with the latter
+    const float rh = rest * 0.693147182f;
+    const float f = (rest + ye) * 0.693147182f;
+    const float rl = __fmaf_rn(rest, 0.693147182f, -rh) + __fmaf_rn(rest, -1.90465421e-9f, ye * 0.693147182f) +
+                     f * f * __fmaf_rn(f, 0.166666667f, 0.5f);
+    const int r = __float2int_rn(rh * 0x1p42f) + __float2int_rn(rl * 0x1p42f);
+    const u64 t = table[q & 1023];   // in units of 2^-62
+    const u64 w = t + (u64)((long long)(uint32_t)(t >> 31) * r >> 11);
+    const int down = 62 - kBits - (q >> 10);
+    return (w + (1ull << (down - 1))) >> down;
   }
 };
 
@@ -151,6 +146,9 @@ struct DrawShared {
   u64 slot[2][2];               // what this CTA gives to a reduction
   u64 warp_a[kWarps], warp_b[kWarps];
   u64 sel_left, sel_before, sel_in;
+  double per_t, least;          // 1 / T; T log(min_p)
+  float ch, cl;                 // Weigher's
+  uint32_t counts[kRanks];
   uint32_t sel_bin, sel_key, listed, found_run;
   u64 run_at, run_equal;
 };
@@ -166,6 +164,15 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
   s.table[tid] = kExp.v[tid];
   pdl_trigger();
   pdl_wait();
+  const float u = a.u[b], t = a.temperature ? a.temperature[b] : 1.f, p = a.top_p ? a.top_p[b] : 1.f, mp = a.min_p ? a.min_p[b] : 0.f;
+  int k = a.top_k ? a.top_k[b] : 0;
+  if (tid == kThreads - 1) {   // (one thread: 64-bit floats come two to a clock)
+    const double c = 2.0 * 1.4426950408889634074 / (double)t;
+    s.ch = (float)c;
+    s.cl = (float)(c - (double)s.ch);
+    s.per_t = 1.0 / (double)t;
+    s.least = mp > 0.f ? (double)t * log((double)fminf(mp, 1.f)) : 0.0;
+  }
   const T* row = (const T*)a.logits + (long long)b * a.row;
   // this warp's run of the row: whole steps of 32 lanes x V values
   const int steps_all = (a.vocab + 32 * V - 1) / (32 * V), shares = ranks * kWarps, share = rank * kWarps + warp;
@@ -190,8 +197,20 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
     if (ranks > 1) cluster_sync();
     else __syncthreads();
   };
+  // sum of 32-bit words of all ranks (the loads on their way together)
+  auto sum_of = [&](const uint32_t* p) {
+    if (ranks == 1) return (u64)*p;
+    uint32_t x[kRanks];
+#pragma unroll
+    for (int i = 0; i < kRanks; ++i) x[i] = ld_cluster_u32(mapa_shared(smem_u32(p), (uint32_t)min(i, ranks - 1)));
+    u64 n = 0;
+#pragma unroll
+    for (int i = 0; i < kRanks; ++i) n += i < ranks ? x[i] : 0u;
+    return n;
+  };
   auto from_rank = [&](const u64* p, int i) { return ranks > 1 ? ld_cluster_u64(mapa_shared(smem_u32(p), (uint32_t)i)) : *p; };
   // maxima or sums of x and of y over the row's threads, for every thread
+  u64 before_x, before_y;
   auto reduce = [&](u64 x, u64 y, bool maximum, u64& rx, u64& ry) {
     x = maximum ? warp_max_u64(x) : warp_sum_u64(x);
     y = maximum ? warp_max_u64(y) : warp_sum_u64(y);
@@ -204,12 +223,13 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
       if (lane == 0) s.slot[turn][0] = p, s.slot[turn][1] = r;
     }
     barrier();
-    rx = ry = 0ull;
-    for (int i = 0; i < ranks; ++i) {
-      const u64 p = from_rank(&s.slot[turn][0], i), r = from_rank(&s.slot[turn][1], i);
-      rx = maximum ? max(p, rx) : rx + p;
-      ry = maximum ? max(r, ry) : ry + r;
-    }
+    // lane i takes rank i's
+    x = lane < ranks ? from_rank(&s.slot[turn][0], lane) : 0ull;
+    y = lane < ranks ? from_rank(&s.slot[turn][1], lane) : 0ull;
+    rx = maximum ? warp_max_u64(x) : warp_sum_u64(x);
+    ry = maximum ? warp_max_u64(y) : warp_sum_u64(y);
+    before_x = warp_sum_u64(lane < rank ? x : 0ull);   // of the ranks before this one
+    before_y = warp_sum_u64(lane < rank ? y : 0ull);
     turn ^= 1;
   };
   // sum of x over the threads before this one and, in all, over the CTA
@@ -250,8 +270,6 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
   }
   reduce(best, low, true, best, low);
   const float top = value_of((uint32_t)(best >> 32));
-  const float u = a.u[b], t = a.temperature ? a.temperature[b] : 1.f, p = a.top_p ? a.top_p[b] : 1.f, mp = a.min_p ? a.min_p[b] : 0.f;
-  int k = a.top_k ? a.top_k[b] : 0;
   auto answer = [&](int token, float log_prob) {
     a.tokens[b] = token;
     if (a.log_probs) a.log_probs[b] = log_prob;
@@ -265,15 +283,16 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
     barrier();   // (nobody leaves while its slot is read)
     return;
   }
-  Weigher weigh;
-  weigh.set(top, (double)t);
+  const Weigher weigh{0.5f * top, s.ch, s.cl};
   auto log_prob = [&](float x, u64 total) {
-    return (float)(((double)x - (double)top) / (double)t - log((double)total * 0x1p-43));
+    const int e = 63 - __clzll((long long)total);
+    const float m = (float)total * exp2f((float)-e);   // total = m 2^e
+    return (float)(((double)x - (double)top) * s.per_t - (double)(e - kBits) * 0.6931471805599453094 - (double)logf(m));
   };
   // least key that min-p lets through
   uint32_t least = 0u;
   if (mp > 0.f) {
-    const double limit = (double)top + (double)t * log((double)fminf(mp, 1.f));
+    const double limit = (double)top + s.least;
     float f = (float)limit;
     if ((double)f < limit) f = nextafterf(f, inf);
     least = key_of(f);
@@ -284,25 +303,16 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
   // monotone in x, rounding included.
   const float y_least = fmaxf((0.5f * value_of(~(uint32_t)low) - weigh.top) * weigh.ch, -44.f);
   const float per_bin = (float)(kBins - 1) / fmaxf(-y_least, 0x1p-40f);
-  auto bin_of = [&](float x) {
+  // place in bins, for bin i from i up to below i + 1 (the last but one: from there on); -1: no weight
+  auto place_of = [&](float x) {
     const float y = (0.5f * x - weigh.top) * weigh.ch;
-    return y > -44.f ? (uint32_t)min((int)(-y * per_bin), kBins - 2) : (uint32_t)(kBins - 1);
+    return y > -44.f ? fminf(-y * per_bin, (float)(kBins - 2)) : -1.f;
   };
   // The bin at which `part` 0 (counts) or 1 (weights), summed from the first on, reaches `target`, what
   // comes before it and what is in it; target > all: the last one.  For every thread of the row.
   auto bin_at = [&](int part, auto target_of, uint32_t& bin, u64& before, u64& in) {
     u64 n = 0;
-    if (tid < kBins) {
-      if (part == 0) {
-        for (int i = 0; i < ranks; ++i) n += ranks > 1 ? ld_cluster_u32(mapa_shared(smem_u32(&s.bins[0][tid]), (uint32_t)i)) : s.bins[0][tid];
-      } else {
-        for (int i = 0; i < ranks; ++i) {
-          const uint32_t lo = ranks > 1 ? ld_cluster_u32(mapa_shared(smem_u32(&s.bins[1][tid]), (uint32_t)i)) : s.bins[1][tid];
-          const uint32_t hi = ranks > 1 ? ld_cluster_u32(mapa_shared(smem_u32(&s.bins[2][tid]), (uint32_t)i)) : s.bins[2][tid];
-          n += (u64)hi << 32 | lo;
-        }
-      }
-    }
+    if (tid < kBins) n = part == 0 ? sum_of(&s.bins[0][tid]) : sum_of(&s.bins[1][tid]) + (sum_of(&s.bins[2][tid]) << 32);
     u64 all;
     const u64 cum = block_scan(n, all);
     const u64 target = target_of(all);
@@ -314,9 +324,10 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
   };
   // Tokens of the bins first .. last, in the order of the index, into rank 0's list; their number.
   auto gather = [&](uint32_t first, uint32_t last) {
-    auto wanted = [&](float x, int i) {
-      const uint32_t bin = bin_of(x);
-      return bin >= first && bin <= last && i < a.vocab;
+    const float from = (float)first, to = (float)(last + 1);
+    auto wanted = [&](float x) {   // (past the end there is no weight)
+      const float place = place_of(x);
+      return place >= from && place < to;
     };
     uint32_t n = 0;
 #pragma unroll 2
@@ -324,7 +335,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
       float x[V];
       load(step, x);
 #pragma unroll
-      for (int j = 0; j < V; ++j) n += wanted(x[j], index_of(step, j));
+      for (int j = 0; j < V; ++j) n += wanted(x[j]);
     }
     n = __reduce_add_sync(kAll, n);
     u64 all;
@@ -336,7 +347,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
         load(step, x);
         uint32_t mine = 0;
 #pragma unroll
-        for (int j = 0; j < V; ++j) mine += wanted(x[j], index_of(step, j));
+        for (int j = 0; j < V; ++j) mine += wanted(x[j]);
         if (!__any_sync(kAll, mine)) continue;
         uint32_t upto = mine;
 #pragma unroll
@@ -344,10 +355,10 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
           const uint32_t up = __shfl_up_sync(kAll, upto, o);
           if (lane >= o) upto += up;
         }
-        uint32_t to = (uint32_t)at + upto - mine;
+        uint32_t put = (uint32_t)at + upto - mine;
 #pragma unroll
         for (int j = 0; j < V; ++j)
-          if (wanted(x[j], index_of(step, j))) s.list[to++] = (u64)key_of(x[j]) << 32 | (kAll - (uint32_t)index_of(step, j));
+          if (wanted(x[j])) s.list[put++] = (u64)key_of(x[j]) << 32 | (kAll - (uint32_t)index_of(step, j));
         at += __shfl_sync(kAll, upto, 31);
       }
     }
@@ -355,16 +366,14 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
     barrier();
     int total = (int)all;
     if (rank == 0 && ranks > 1) {
-      for (int flat = (int)all + tid; flat < kCap; flat += kThreads) {   // behind its own
+      if (tid < ranks) s.counts[tid] = (uint32_t)from_rank(&s.slot[turn][0], tid);
+      __syncthreads();
+      for (int r = 1; r < ranks; ++r) total += (int)s.counts[r];
+      for (int flat = (int)all + tid; flat < total; flat += kThreads) {   // behind its own
         int i = flat - (int)all, r = 1;
-        for (; r < ranks; ++r) {
-          const int of = (int)from_rank(&s.slot[turn][0], r);
-          if (i < of) break;
-          i -= of;
-        }
-        if (r < ranks) s.list[flat] = from_rank(&s.list[i], r);
+        while (i >= (int)s.counts[r]) i -= (int)s.counts[r++];
+        s.list[flat] = from_rank(&s.list[i], r);
       }
-      for (int r = 1; r < ranks; ++r) total += (int)from_rank(&s.slot[turn][0], r);
       __syncthreads();
     }
     turn ^= 1;
@@ -404,8 +413,9 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
       load(step, x);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const uint32_t bin = bin_of(x[j]);
-        if (bin == kBins - 1) continue;
+        const float place = place_of(x[j]);
+        if (place < 0.f) continue;
+        const int bin = (int)place;
         atomicAdd(&s.bins[0][bin], 1u);
         if (!by_count) {
           const u64 w = weigh(x[j], s.table);
@@ -425,9 +435,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
     } else {
       bin_at(1, [&](u64 all) { return want = max(1ull, p > 0.f ? times_fraction(all, p, true) : 0ull); }, bin, before, in);
       // tokens up to that bin and in it
-      u64 n = 0;
-      if (tid <= bin)
-        for (int i = 0; i < ranks; ++i) n += ranks > 1 ? ld_cluster_u32(mapa_shared(smem_u32(&s.bins[0][tid]), (uint32_t)i)) : s.bins[0][tid];
+      const u64 n = tid <= bin ? sum_of(&s.bins[0][tid]) : 0ull;
       block_scan(n, count);
       block_scan(tid == bin ? n : 0ull, cin);
     }
@@ -617,16 +625,24 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
   const u64 total = all + min(ties, all_equal) * one;
   const u64 at = times_fraction(total, u, false);   // the token's part of the sum holds this
   auto upto = [&](u64 w, u64 n) { return w + min(ties, n) * one; };
-  // before this rank
-  u64 before = 0, equal_before = 0;
-  for (int i = 0; i < rank; ++i) before += from_rank(&s.slot[turn ^ 1][0], i), equal_before += from_rank(&s.slot[turn ^ 1][1], i);
+  u64 before = before_x, equal_before = before_y;
   const u64 mine = s.slot[turn ^ 1][0], mine_equal = s.slot[turn ^ 1][1];
   if (upto(before, equal_before) <= at && at < upto(before + mine, equal_before + mine_equal)) {
     // the token is in this CTA: in which warp's run
-    sum = s.warp_a[warp], equal = s.warp_b[warp];
-    for (int i = 0; i < warp; ++i) before += s.warp_a[i], equal_before += s.warp_b[i];
-    if (lane == 0 && upto(before, equal_before) <= at && at < upto(before + sum, equal_before + equal))
-      s.found_run = (uint32_t)warp, s.run_at = before, s.run_equal = equal_before;
+    u64 w0, w1, e0, e1;   // before warp `lane`, and with it
+    auto scan_warps = [&] {
+      const u64 w = s.warp_a[lane], e = s.warp_b[lane];
+      w1 = w, e1 = e;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const u64 wu = __shfl_up_sync(kAll, w1, o), eu = __shfl_up_sync(kAll, e1, o);
+        if (lane >= o) w1 += wu, e1 += eu;
+      }
+      w1 += before, e1 += equal_before;
+      w0 = w1 - w, e0 = e1 - e;
+    };
+    scan_warps();
+    if (warp == 0 && upto(w0, e0) <= at && at < upto(w1, e1)) s.found_run = (uint32_t)lane, s.run_at = w0, s.run_equal = e0;
     __syncthreads();
     // that run again, by all warps: 32 of its steps at a time, a step to a warp
     const int fshare = rank * kWarps + (int)s.found_run;
@@ -655,12 +671,9 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
       __syncthreads();
       if (lane == 31) s.warp_a[warp] = wi, s.warp_b[warp] = ni;
       __syncthreads();
-      u64 c = before, e = equal_before;
-      for (int i = 0; i < kWarps; ++i) {
-        if (i == warp) c += wi - ws, e += ni - ns;
-        if (i < warp) c += s.warp_a[i], e += s.warp_b[i];
-        before += s.warp_a[i], equal_before += s.warp_b[i];
-      }
+      scan_warps();
+      u64 c = __shfl_sync(kAll, w0, warp) + wi - ws, e = __shfl_sync(kAll, e0, warp) + ni - ns;
+      before = __shfl_sync(kAll, w1, 31), equal_before = __shfl_sync(kAll, e1, 31);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const u64 was = upto(c, e);
