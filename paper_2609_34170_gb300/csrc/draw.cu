@@ -358,18 +358,19 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
         uint32_t put = (uint32_t)at + upto - mine;
 #pragma unroll
         for (int j = 0; j < V; ++j)
-          if (wanted(x[j])) s.list[put++] = (u64)key_of(x[j]) << 32 | (kAll - (uint32_t)index_of(step, j));
+          if (wanted(x[j]) && put < kCap) s.list[put++] = (u64)key_of(x[j]) << 32 | (kAll - (uint32_t)index_of(step, j));
         at += __shfl_sync(kAll, upto, 31);
       }
     }
     if (tid == 0) s.slot[turn][0] = all;
     barrier();
-    int total = (int)all;
+    int total = (int)min(all, (u64)kCap);
     if (rank == 0 && ranks > 1) {
       if (tid < ranks) s.counts[tid] = (uint32_t)from_rank(&s.slot[turn][0], tid);
       __syncthreads();
       for (int r = 1; r < ranks; ++r) total += (int)s.counts[r];
-      for (int flat = (int)all + tid; flat < total; flat += kThreads) {   // behind its own
+      total = min(total, kCap);   // (the counts said so; logits that change under the kernel must not write past the list)
+      for (int flat = (int)min(all, (u64)kCap) + tid; flat < total; flat += kThreads) {   // behind its own
         int i = flat - (int)all, r = 1;
         while (i >= (int)s.counts[r]) i -= (int)s.counts[r++];
         s.list[flat] = from_rank(&s.list[i], r);

@@ -20,6 +20,7 @@ namespace {
 // nibble i the first k of register ai and in nibble 4 + i the second, and a warp reads 16 rows x 64 ks in
 // one contiguous 512-byte load.
 constexpr int kWarps = 8;
+constexpr int kRanks = 8;    // CTAs that share the ks of a pair at most
 constexpr int kPitch = 36;   // floats of a token's 32 rows: lanes of a store land in different banks
 
 __device__ __forceinline__ void code_place(int lane, int word, int nibble, int* row, int* k) {
@@ -184,6 +185,104 @@ struct Block {
   uint2 sz[2][G32 ? 2 : 1];
 };
 
+// Tiles of a pair: side by side, or for GeGLU 16 gate rows and their 16 up rows.
+__device__ __forceinline__ int first_tile(int pair, int epi) { return epi == EPI_GEGLU ? pair / 4 * 8 + pair % 4 : 2 * pair; }
+__device__ __forceinline__ int second_tile(int pair, int epi) { return first_tile(pair, epi) + (epi == EPI_GEGLU ? 4 : 1); }
+
+// A pair's sums [token][kPitch] in shared memory, this rank's share of them, into the output: threads
+// first, first + step, ... of those that work on the pair.
+template <int NT>
+__device__ __forceinline__ void finish(const W4Args& a, const float* part, int pair, int m0, int ranks, int rank, int first, int step) {
+  const bool glu = a.epi == EPI_GEGLU;
+  const int t0 = first_tile(pair, a.epi), t1 = second_tile(pair, a.epi);
+  const int shift = glu ? 4 : 5, rows = 1 << shift, all = min(NT * 8, a.M - m0) << shift;
+  const int e0 = all * rank / ranks, e1 = all * (rank + 1) / ranks;
+  for (int e = e0 + first; e < e1; e += step) {
+    const int m = e >> shift, r = e & (rows - 1);
+    auto total = [&](int row) {
+      if (ranks == 1) return part[m * kPitch + row];
+      const uint32_t at = smem_u32(part + m * kPitch + row);
+      float x[kRanks];   // (all on their way together)
+#pragma unroll
+      for (int i = 0; i < kRanks; ++i) x[i] = ld_cluster_f(mapa_shared(at, (uint32_t)min(i, ranks - 1)));
+      float v = x[0];
+#pragma unroll
+      for (int i = 1; i < kRanks; ++i) v += i < ranks ? x[i] : 0.f;
+      return v;
+    };
+    auto with_bias = [&](int row, float v) {
+      const int n = (row < 16 ? t0 : t1) * 16 + (row & 15);
+      return a.bias && n < a.w.N ? v + a.bias[n] : v;
+    };
+    float v = with_bias(r, total(r));
+    int col = (r < 16 ? t0 : t1) * 16 + (r & 15);
+    if (glu) {
+      v = gelu_tanh_f(v) * with_bias(r + 16, total(r + 16));
+      col = pair / 4 * 64 + pair % 4 * 16 + r;
+    } else if (col >= a.w.N) {
+      continue;
+    }
+    const size_t to = (size_t)(m0 + m) * a.ldo + col;
+    if (a.epi == EPI_STORE_SILU) v = silu_f(v);
+    if (a.epi == EPI_ADD_F32) ((float*)a.out)[to] += v;
+    else if (a.out_bf16) ((bf16*)a.out)[to] = from_f32<bf16>(v);
+    else ((float*)a.out)[to] = v;
+  }
+}
+
+// A block's weights of a pair of tiles into the registers of A, and the rows' scales.
+template <bool G32>
+struct Operand {
+  uint32_t A[2][4][4];
+  float s0[2][G32 ? 2 : 1], s8[2][G32 ? 2 : 1];
+  __device__ __forceinline__ void set(const Block<G32>& b) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const uint32_t* c = (const uint32_t*)&b.codes[t];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint2 sz = b.sz[t][G32 ? i >> 1 : 0];
+        widen(c[i], __byte_perm(sz.x, 0u, 0x1010), __byte_perm(sz.y, 0u, 0x1010), A[t][i]);
+      }
+#pragma unroll
+      for (int h = 0; h < (G32 ? 2 : 1); ++h) {
+        s0[t][h] = __uint_as_float(b.sz[t][h].x & 0xffff0000u);
+        s8[t][h] = __uint_as_float(b.sz[t][h].y & 0xffff0000u);
+      }
+    }
+  }
+  // acc += the block's product with 8 tokens' values x (of its first and its second 32 ks)
+  __device__ __forceinline__ void multiply(const uint4* x, float (*acc)[4], int stride) const {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int h = 0; h < (G32 ? 2 : 1); ++h) {
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int hh = G32 ? h : 0; hh < (G32 ? h + 1 : 2); ++hh) {
+          mma_bf16(sum, A[t][2 * hh], x[hh].x, x[hh].y);
+          mma_bf16(sum, A[t][2 * hh + 1], x[hh].z, x[hh].w);
+        }
+        acc[t * stride][0] += s0[t][h] * sum[0];
+        acc[t * stride][1] += s0[t][h] * sum[1];
+        acc[t * stride][2] += s8[t][h] * sum[2];
+        acc[t * stride][3] += s8[t][h] * sum[3];
+      }
+    }
+  }
+};
+
+// The sums of a warp into [token][kPitch].
+template <int NT>
+__device__ __forceinline__ void put_sums(float* to, const float (*acc)[NT][4], int g, int q) {
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) to[(n * 8 + 2 * q + (i & 1)) * kPitch + t * 16 + g + (i >> 1) * 8] = acc[t][n][i];
+}
+
 // A CTA takes two tiles of 16 rows (GeGLU: 16 gate rows and their 16 up rows) and NT * 8 tokens; its eight
 // warps, and the CTAs of its cluster, share the ks.
 //
@@ -199,7 +298,7 @@ __global__ void __launch_bounds__(256) w4_gemm_kernel(W4Args a) {
   const int ranks = (int)gridDim.z, rank = ranks > 1 ? (int)cluster_ctarank() : 0;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
   const int pair = blockIdx.x, m0 = blockIdx.y * NT * 8;
-  const int t0 = a.epi == EPI_GEGLU ? pair / 4 * 8 + pair % 4 : 2 * pair, t1 = a.epi == EPI_GEGLU ? t0 + 4 : t0 + 1;
+  const int t0 = first_tile(pair, a.epi), t1 = second_tile(pair, a.epi);
   const int shares = ranks * kWarps, share = rank * kWarps + warp;
   const int k0 = (int)((long long)w.kblocks * share / shares), k1 = (int)((long long)w.kblocks * (share + 1) / shares);
 
@@ -236,22 +335,8 @@ __global__ void __launch_bounds__(256) w4_gemm_kernel(W4Args a) {
     for (int d = 0; d < kAhead; ++d) {
       const int kb = kb0 + d;
       if (kb >= k1) break;
-      uint32_t A[2][4][4];
-      float s0[2][G32 ? 2 : 1], s8[2][G32 ? 2 : 1];
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const uint32_t* c = (const uint32_t*)&held[d].codes[t];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint2 sz = held[d].sz[t][G32 ? i >> 1 : 0];
-          widen(c[i], __byte_perm(sz.x, 0u, 0x1010), __byte_perm(sz.y, 0u, 0x1010), A[t][i]);
-        }
-#pragma unroll
-        for (int h = 0; h < (G32 ? 2 : 1); ++h) {
-          s0[t][h] = __uint_as_float(held[d].sz[t][h].x & 0xffff0000u);
-          s8[t][h] = __uint_as_float(held[d].sz[t][h].y & 0xffff0000u);
-        }
-      }
+      Operand<G32> op;
+      op.set(held[d]);
       if (kb + kAhead < k1) fetch(held[d], kb + kAhead);
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
@@ -260,33 +345,13 @@ __global__ void __launch_bounds__(256) w4_gemm_kernel(W4Args a) {
         uint4 x[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) x[h] = load_x(row, kb * 64 + h * 32 + q * 8, w.K, m < a.M, a.vec);
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-#pragma unroll
-          for (int h = 0; h < (G32 ? 2 : 1); ++h) {
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int hh = G32 ? h : 0; hh < (G32 ? h + 1 : 2); ++hh) {
-              mma_bf16(sum, A[t][2 * hh], x[hh].x, x[hh].y);
-              mma_bf16(sum, A[t][2 * hh + 1], x[hh].z, x[hh].w);
-            }
-            acc[t][n][0] += s0[t][h] * sum[0];
-            acc[t][n][1] += s0[t][h] * sum[1];
-            acc[t][n][2] += s8[t][h] * sum[2];
-            acc[t][n][3] += s8[t][h] * sum[3];
-          }
-        }
+        op.multiply(x, &acc[0][n], NT);
       }
     }
   }
 
   float* mine = part + warp * kPart;
-#pragma unroll
-  for (int t = 0; t < 2; ++t)
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) mine[(n * 8 + 2 * q + (i & 1)) * kPitch + t * 16 + g + (i >> 1) * 8] = acc[t][n][i];
+  put_sums<NT>(mine, acc, g, q);
   __syncthreads();
   for (int e = threadIdx.x; e < NT * 8 * 32; e += 256) {
     const int at = (e >> 5) * kPitch + (e & 31);
@@ -298,38 +363,152 @@ __global__ void __launch_bounds__(256) w4_gemm_kernel(W4Args a) {
   if (ranks > 1) cluster_sync();
   else __syncthreads();
 
-  // this rank's share of the tokens' values
-  const bool glu = a.epi == EPI_GEGLU;
-  const int rows = glu ? 16 : 32, tokens = min(NT * 8, a.M - m0), all = tokens * rows;
-  const int e0 = (int)((long long)all * rank / ranks), e1 = (int)((long long)all * (rank + 1) / ranks);
-  for (int e = e0 + threadIdx.x; e < e1; e += 256) {
-    const int m = e / rows, r = e % rows;
-    auto total = [&](int row) {
-      const uint32_t at = smem_u32(part + m * kPitch + row);
-      if (ranks == 1) return part[m * kPitch + row];
-      float v = 0.f;
-      for (int i = 0; i < ranks; ++i) v += ld_cluster_f(mapa_shared(at, (uint32_t)i));
-      return v;
-    };
-    auto with_bias = [&](int row, float v) {
-      const int n = (row < 16 ? t0 : t1) * 16 + (row & 15);
-      return a.bias && n < w.N ? v + a.bias[n] : v;
-    };
-    float v = with_bias(r, total(r));
-    int col = (r < 16 ? t0 : t1) * 16 + (r & 15);
-    if (glu) {
-      v = gelu_tanh_f(v) * with_bias(r + 16, total(r + 16));
-      col = pair / 4 * 64 + pair % 4 * 16 + r;
-    } else if (col >= w.N) {
-      continue;
-    }
-    const size_t to = (size_t)(m0 + m) * a.ldo + col;
-    if (a.epi == EPI_STORE_SILU) v = silu_f(v);
-    if (a.epi == EPI_ADD_F32) ((float*)a.out)[to] += v;
-    else if (a.out_bf16) ((bf16*)a.out)[to] = from_f32<bf16>(v);
-    else ((float*)a.out)[to] = v;
-  }
+  finish<NT>(a, part, pair, m0, ranks, rank, threadIdx.x, 256);
   if (ranks > 1) cluster_sync();   // nobody leaves while its sums are read
+}
+
+// More tokens, where the rows fill the SMs: a warp takes a pair of tiles with all of the CTA's ks, so that
+// eight pairs share each token's values.  Codes, scales and values come by asynchronous copies
+// into a ring of stages of 64 ks.  A stage's tokens are rows of 128 bytes, whose halves change
+// places in odd rows: the 8 lanes that a shared-memory access serves at a time read 64 bytes of two rows.
+constexpr int kStages = 6;
+template <int NT>
+struct Stage {
+  uint4 x[NT * 8][8];
+  uint4 codes[kWarps * 2][32];
+  uint2 sz[2][kWarps * 2][8];   // by 32 ks where these are a group, otherwise the first
+};
+
+__device__ __forceinline__ void copy_async(void* to, const void* from, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
+
+template <int NT, bool G32>
+__global__ void __launch_bounds__(256, 2) w4_wide_kernel(W4Args a) {
+  extern __shared__ __align__(16) unsigned char wide_smem[];
+  Stage<NT>* ring = (Stage<NT>*)wide_smem;
+  const W4Matrix& w = a.w;
+  const int ranks = (int)gridDim.z, rank = ranks > 1 ? (int)cluster_ctarank() : 0;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q = lane & 3;
+  const int pair0 = blockIdx.x * kWarps, pair = pair0 + warp, pairs = w.tiles / 2, m0 = blockIdx.y * NT * 8;
+  const int k0 = (int)((long long)w.kblocks * rank / ranks), k1 = (int)((long long)w.kblocks * (rank + 1) / ranks);
+
+  // a stage's weights: a warp copies its own pair's; of pairs past the end nothing is copied and nothing kept
+  auto fetch_weights = [&](int kb) {
+    if (pair >= pairs) return;
+    Stage<NT>& st = ring[(kb - k0) % kStages];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int tile = t ? second_tile(pair, a.epi) : first_tile(pair, a.epi);
+      copy_async(&st.codes[warp * 2 + t][lane], w.codes + ((size_t)tile * w.kblocks + kb) * 32 + lane, true);
+    }
+    // 64 bytes of scales per tile and group: 4 lanes each
+    const int t = lane >> 2 & 1, h = lane >> 3;
+    if (h < (G32 ? 2 : 1)) {
+      const int tile = t ? second_tile(pair, a.epi) : first_tile(pair, a.epi);
+      const int group = min((kb * 64 + h * 32) / w.group, w.groups - 1);
+      copy_async(&st.sz[h][warp * 2 + t][(lane & 3) * 2], w.sz + ((size_t)tile * w.groups + group) * 8 + (lane & 3) * 2, true);
+    }
+  };
+  auto fetch_x = [&](int kb) {
+    Stage<NT>& st = ring[(kb - k0) % kStages];
+#pragma unroll
+    for (int i = 0; i < NT * 64 / 256; ++i) {
+      const int at = tid + i * 256, token = at >> 3, piece = at & 7, m = m0 + token, k = kb * 64 + piece * 8;
+      const bf16* row = (const bf16*)a.x + (long long)m * a.lda;
+      uint4* to = &st.x[token][piece ^ (token & 1) * 4];
+      if (a.vec) {
+        const bool there = m < a.M && k + 8 <= w.K;
+        if (m < a.M && k < w.K && !there) *to = load_x(row, k, w.K, true, 0);
+        else copy_async(to, there ? (const void*)(row + k) : a.x, there);
+      } else {
+        *to = load_x(row, k, w.K, m < a.M, 0);
+      }
+    }
+  };
+  auto commit = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
+
+#pragma unroll
+  for (int i = 0; i < kStages - 1; ++i)   // (weights do not change: ahead of the wait)
+    if (k0 + i < k1) fetch_weights(k0 + i);
+  pdl_trigger();
+  pdl_wait();
+#pragma unroll
+  for (int i = 0; i < kStages - 1; ++i) {
+    if (k0 + i < k1) fetch_x(k0 + i);
+    commit();   // (the first group holds all the weights so far)
+  }
+
+  float acc[2][NT][4];
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[t][n][i] = 0.f;
+
+  for (int kb = k0; kb < k1; ++kb) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+    __syncthreads();   // everybody's copies are there, and the stage before is read
+    if (kb + kStages - 1 < k1) {
+      fetch_weights(kb + kStages - 1);
+      fetch_x(kb + kStages - 1);
+    }
+    commit();
+    if (pair >= pairs) continue;
+    const Stage<NT>& st = ring[(kb - k0) % kStages];
+    Operand<G32> op;
+    {
+      Block<G32> b;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        b.codes[t] = st.codes[warp * 2 + t][lane];
+#pragma unroll
+        for (int h = 0; h < (G32 ? 2 : 1); ++h) b.sz[t][h] = st.sz[h][warp * 2 + t][g];
+      }
+      op.set(b);
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int token = n * 8 + g;
+      uint4 x[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) x[h] = st.x[token][(h ^ (token & 1)) * 4 + q];
+      op.multiply(x, &acc[0][n], NT);
+    }
+  }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  __syncthreads();
+  float* part = (float*)wide_smem + warp * NT * 8 * kPitch;
+  put_sums<NT>(part, acc, g, q);
+  if (ranks > 1) cluster_sync();
+  else __syncwarp();
+  if (pair < pairs) finish<NT>(a, part, pair, m0, ranks, rank, lane, 32);
+  if (ranks > 1) cluster_sync();   // nobody leaves while its sums are read
+}
+
+template <int NT>
+constexpr size_t wide_smem_of() {
+  return sizeof(Stage<NT>) * kStages > sizeof(float) * kWarps * NT * 8 * kPitch ? sizeof(Stage<NT>) * kStages
+                                                                                  : sizeof(float) * kWarps * NT * 8 * kPitch;
+}
+
+template <int NT>
+cudaError_t init_wide() {
+  cudaError_t e = cudaFuncSetAttribute(w4_wide_kernel<NT, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)wide_smem_of<NT>());
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(w4_wide_kernel<NT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)wide_smem_of<NT>());
+  return e;
+}
+
+template <int NT>
+cudaError_t launch_wide(const W4Args& a, cudaStream_t st) {
+  const int blocks = (a.w.tiles / 2 + kWarps - 1) / kWarps, tiles = (a.M + NT * 8 - 1) / (NT * 8);
+  int ranks = 1;
+  while (ranks < kRanks && (long long)blocks * tiles * ranks < 4 * a.num_sms && a.w.kblocks >= ranks * 2 * 4) ranks *= 2;
+  const Overlap overlap;
+  return launch_kernel_cluster(a.w.group == 32 ? w4_wide_kernel<NT, true> : w4_wide_kernel<NT, false>, dim3(blocks, tiles, ranks),
+                               dim3(256), wide_smem_of<NT>(), st, dim3(1, 1, ranks), a);
 }
 
 template <int NT>
@@ -365,10 +544,13 @@ cudaError_t init_w4_kernels() {
   if (e == cudaSuccess) e = init_nt<2>();
   if (e == cudaSuccess) e = init_nt<4>();
   if (e == cudaSuccess) e = init_nt<8>();
+  if (e == cudaSuccess) e = init_wide<4>();
+  if (e == cudaSuccess) e = init_wide<8>();
   return e;
 }
 
 cudaError_t launch_w4_gemm(const W4Args& a, cudaStream_t st) {
+  if (a.M > 16 && a.w.tiles >= 256) return a.M <= 32 ? launch_wide<4>(a, st) : launch_wide<8>(a, st);
   return a.M <= 8 ? launch_nt<1>(a, st) : a.M <= 16 ? launch_nt<2>(a, st) : a.M <= 32 ? launch_nt<4>(a, st) : launch_nt<8>(a, st);
 }
 
