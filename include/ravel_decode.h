@@ -97,6 +97,10 @@ ravel_status ravel_w4_create(int N, int K, int group, int device, ravel_w4_t** o
 /* Free the matrix (after synchronising the device).  NULL is a no-op. */
 void ravel_w4_destroy(ravel_w4_t* w);
 
+/* Clear the error word of a matrix, after waiting for the device: a product of more than 16 rows in
+ * which a bounded wait ran out (its output is not valid) makes later ones return RAVEL_ETIMEOUT. */
+ravel_status ravel_w4_reset(ravel_w4_t* w);
+
 /* Codes, scales and zeros (device, as above, contiguous) into the matrix, in the order
  * in which the products read them.  Scales are finite.  Waits until `stream` is done, because
  * products read weights ahead of their place on a stream; refused (RAVEL_EINVAL)
@@ -124,8 +128,8 @@ ravel_status ravel_w4_read(ravel_w4_t* w, void* out, int ldo, int dtype, void* s
  *           matching up rows; out[m][f] = gelu_tanh(gate + bias) * (up + bias) for f < N / 2
  *   out  device [M, ldo], out_dtype RAVEL_FP32 or RAVEL_BF16; bias device float32 [N] or NULL
  * Codes are multiplied as whole numbers and sums kept in fp32, so that the result is that of the
- * weights held, not of weights rounded to bf16.  Meant for up to some 64 rows, where the weights'
- * bytes are what a product costs; any M works, in tiles of 64 rows that each read the matrix.
+ * weights held, not of weights rounded to bf16.  Meant for few rows, where the weights' bytes are
+ * what a product costs; any M works, in tiles of 64 rows that each read the matrix.
  * out must not overlap X. */
 ravel_status ravel_w4_gemm(const ravel_w4_t* w, const void* X, int M, int lda, int epi, void* out, int ldo, int out_dtype,
                            const float* bias, void* stream);

@@ -16,7 +16,7 @@ from ._binding import (  # noqa: F401
     ravel_cache_create, ravel_cache_destroy, ravel_cache_reset, ravel_cache_append, ravel_cache_attend,
     ravel_cache_evict, ravel_cache_read,
     ravel_cache_append_rotary, ravel_rotary_create, ravel_rotary_destroy, ravel_rotary_apply, ravel_w4_create,
-    ravel_w4_destroy, ravel_w4_load, ravel_w4_quantize, ravel_w4_read, ravel_w4_gemm, ravel_draw_tokens,
+    ravel_w4_destroy, ravel_w4_reset, ravel_w4_load, ravel_w4_quantize, ravel_w4_read, ravel_w4_gemm, ravel_draw_tokens,
 )
 from .cache import ContextCache  # noqa: F401
 from .decode import Rotary, Weights4, draw_tokens  # noqa: F401

@@ -110,6 +110,7 @@ def load(path: str | None = None):
         "ravel_cache_append_rotary": (i, [vp, i, vp, i, i, vp, ll, ll, vp, ll, ll, vp, ll, ll, vp, ll, ll, vp, vp, vp, vp]),
         "ravel_w4_create": (i, [i, i, i, i, pp]),
         "ravel_w4_destroy": (None, [vp]),
+        "ravel_w4_reset": (i, [vp]),
         "ravel_w4_load": (i, [vp, vp, vp, vp, vp]),
         "ravel_w4_quantize": (i, [vp, i, i, i, i, i, vp, vp, vp, vp]),
         "ravel_w4_read": (i, [vp, vp, i, i, vp]),
@@ -608,6 +609,10 @@ def ravel_w4_create(N: int, K: int, group: int = 128, device: int = 0):
 
 def ravel_w4_destroy(w):
     load().ravel_w4_destroy(w)
+
+
+def ravel_w4_reset(w):
+    _check_decode(load().ravel_w4_reset(w), "ravel_w4_reset")
 
 
 def _w4(w):

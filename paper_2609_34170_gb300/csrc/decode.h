@@ -60,13 +60,16 @@ struct W4Args {
   int M, lda, ldo, epi, out_bf16;
   int vec;            // rows of x are 16-byte aligned
   int num_sms;
+  int* err;
 };
 cudaError_t launch_w4_gemm(const W4Args& a, cudaStream_t st);
 cudaError_t launch_w4_load(const W4Matrix& w, const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, cudaStream_t st);
 cudaError_t launch_w4_read(const W4Matrix& w, void* out, int ldo, Dtype dt, cudaStream_t st);
 cudaError_t launch_w4_quantize(const void* W, int N, int K, int ldw, Dtype dt, int group, uint8_t* codes, uint16_t* scales,
                                uint8_t* zeros, cudaStream_t st);
+cudaError_t launch_w4_tc(const W4Args& a, cudaStream_t st);   // more than 16 tokens
 cudaError_t init_w4_kernels();
+cudaError_t init_w4_tc_kernels();
 
 struct DrawArgs {
   const void* logits;

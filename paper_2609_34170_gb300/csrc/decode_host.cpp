@@ -16,6 +16,8 @@ using namespace ravel;
 struct ravel_w4_ctx {
   W4Matrix m{};
   int device = 0, num_sms = 0;
+  ErrorWord* err = nullptr;
+  int* err_host = nullptr;   // pinned, mapped: the error word's mirror
 };
 
 namespace {
@@ -62,6 +64,14 @@ cudaError_t sm_count(int* out) {
   e = cudaDeviceGetAttribute(out, cudaDevAttrMultiProcessorCount, dev);
   if (e == cudaSuccess && kept) counts[dev].store(*out, std::memory_order_relaxed);
   return e;
+}
+
+void free_matrix(ravel_w4_t* w) {
+  if (w->m.codes) cudaFree(w->m.codes);
+  if (w->m.sz) cudaFree(w->m.sz);
+  if (w->err) cudaFree(w->err);
+  if (w->err_host) cudaFreeHost(w->err_host);
+  delete w;
 }
 
 const char* rotary_fault(const ravel_rotary_config& c) {
@@ -204,12 +214,17 @@ ravel_status ravel_w4_create(int N, int K, int group, int device, ravel_w4_t** o
   if (e == cudaSuccess) e = cudaMalloc((void**)&m.sz, sz);
   if (e == cudaSuccess) e = cudaMemset(m.codes, 0, codes);
   if (e == cudaSuccess) e = cudaMemset(m.sz, 0, sz);
+  ErrorWord word{0, nullptr};
+  if (e == cudaSuccess) e = cudaMalloc((void**)&w->err, sizeof word);
+  if (e == cudaSuccess) e = cudaHostAlloc((void**)&w->err_host, sizeof(int), cudaHostAllocMapped);
+  if (e == cudaSuccess) *w->err_host = 0;
+  if (e == cudaSuccess) e = cudaHostGetDevicePointer((void**)&word.mirror, w->err_host, 0);
+  if (e == cudaSuccess) e = cudaMemcpy(w->err, &word, sizeof word, cudaMemcpyHostToDevice);
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   if (e != cudaSuccess) {
     const ravel_status s = cuda_fail(e, "w4_create");
-    if (m.codes) cudaFree(m.codes);
-    if (m.sz) cudaFree(m.sz);
-    delete w;
+    free_matrix(w);
+    cudaGetLastError();
     return s;
   }
   *out = w;
@@ -219,12 +234,19 @@ ravel_status ravel_w4_create(int N, int K, int group, int device, ravel_w4_t** o
 void ravel_w4_destroy(ravel_w4_t* w) {
   if (!w) return;
   OnDevice on(w->device);
-  if (on.e == cudaSuccess) {
-    cudaDeviceSynchronize();
-    cudaFree(w->m.codes);
-    cudaFree(w->m.sz);
-  }
-  delete w;
+  if (on.e == cudaSuccess) cudaDeviceSynchronize();
+  free_matrix(w);
+}
+
+ravel_status ravel_w4_reset(ravel_w4_t* w) {
+  if (!w) return fail(RAVEL_EINVAL, "w4_reset: null argument");
+  OnDevice on(w->device);
+  cudaError_t e = on.e;
+  if (e == cudaSuccess) e = cudaDeviceSynchronize();
+  if (e == cudaSuccess) e = cudaMemset(w->err, 0, sizeof(int));
+  if (e != cudaSuccess) return cuda_fail(e, "w4_reset");
+  *w->err_host = 0;
+  return RAVEL_OK;
 }
 
 ravel_status ravel_w4_load(ravel_w4_t* w, const void* codes, const void* scales, const void* zeros, void* stream) {
@@ -277,7 +299,12 @@ ravel_status ravel_w4_gemm(const ravel_w4_t* w, const void* X, int M, int lda, i
   if ((uintptr_t)X % 2 || (uintptr_t)out % size_of(out_dtype)) return fail(RAVEL_EINVAL, "w4_gemm: unaligned X or out");
   if (M == 0) return RAVEL_OK;
   if (!X || !out) return fail(RAVEL_EINVAL, "w4_gemm: null argument");
-  W4Args a{w->m, X, out, bias, M, lda, ldo, epi, out_dtype == RAVEL_BF16, 0, w->num_sms};
+  const int bits = *(volatile int*)w->err_host;
+  if (bits) {
+    snprintf(t_error, sizeof t_error, "device error word 0x%x", bits);
+    return bits & ERR_TIMEOUT ? RAVEL_ETIMEOUT : RAVEL_EDEVICE;
+  }
+  W4Args a{w->m, X, out, bias, M, lda, ldo, epi, out_dtype == RAVEL_BF16, 0, w->num_sms, &w->err->bits};
   a.vec = (uintptr_t)X % 16 == 0 && lda % 8 == 0;
   OnDevice on(w->device);
   cudaError_t e = on.e;

@@ -5,6 +5,7 @@
 #include "decode.h"
 #include "launch.h"
 #include "tc_common.cuh"
+#include "w4.cuh"
 
 namespace ravel {
 namespace {
@@ -20,7 +21,6 @@ namespace {
 // nibble i the first k of register ai and in nibble 4 + i the second, and a warp reads 16 rows x 64 ks in
 // one contiguous 512-byte load.
 constexpr int kWarps = 8;
-constexpr int kRanks = 8;    // CTAs that share the ks of a pair at most
 constexpr int kPitch = 36;   // floats of a token's 32 rows: lanes of a store land in different banks
 
 __device__ __forceinline__ void code_place(int lane, int word, int nibble, int* row, int* k) {
@@ -135,10 +135,12 @@ __device__ __forceinline__ void mma_bf16(float* d, const uint32_t* a, uint32_t b
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-__device__ __forceinline__ uint32_t sub_bf16x2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
+// the same from zero
+__device__ __forceinline__ void mma_bf16_first(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 
 // Eight codes as c - z in bf16, the four registers of A: 0x43 above a code is 128 + c, and 128 + c less
@@ -148,68 +150,21 @@ __device__ __forceinline__ void widen(uint32_t w, uint32_t z0, uint32_t z8, uint
   for (int i = 0; i < 4; ++i) a[i] = sub_bf16x2((w >> 4 * i & 0x000f000fu) | 0x43004300u, i & 1 ? z8 : z0);
 }
 
-// Eight values of a row from k on; what is not there is zero (a code past the end stands for
-// weight 0, but 0 times a neighbour's NaN is not).
-__device__ __forceinline__ uint4 load_x(const bf16* row, int k, int K, bool there, int vec) {
-  uint4 r = make_uint4(0u, 0u, 0u, 0u);
-  if (!there || k >= K) return r;
-  if (vec && k + 8 <= K) return *(const uint4*)(row + k);
-  uint16_t v[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = k + i < K ? ((const uint16_t*)row)[k + i] : 0;
-  memcpy(&r, v, 16);
-  return r;
-}
-
-__device__ __forceinline__ float ld_cluster_f(uint32_t a) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
-  return v;
-}
-
-__device__ __forceinline__ uint4 ld_weights(const uint4* p) {
-  uint4 v;
-  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
-}
-__device__ __forceinline__ uint2 ld_weights(const uint2* p) {
-  uint2 v;
-  asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
-  return v;
-}
-
-// What a warp holds of a block of 64 ks: codes of its two tiles and their scales.
-template <bool G32>
-struct Block {
-  uint4 codes[2];
-  uint2 sz[2][G32 ? 2 : 1];
-};
-
 // Tiles of a pair: side by side, or for GeGLU 16 gate rows and their 16 up rows.
 __device__ __forceinline__ int first_tile(int pair, int epi) { return epi == EPI_GEGLU ? pair / 4 * 8 + pair % 4 : 2 * pair; }
 __device__ __forceinline__ int second_tile(int pair, int epi) { return first_tile(pair, epi) + (epi == EPI_GEGLU ? 4 : 1); }
 
-// A pair's sums [token][kPitch] in shared memory, this rank's share of them, into the output: threads
+// A pair's outputs, or this rank's share of them: total(token, row of the pair's 32), computed by threads
 // first, first + step, ... of those that work on the pair.
-template <int NT>
-__device__ __forceinline__ void finish(const W4Args& a, const float* part, int pair, int m0, int ranks, int rank, int first, int step) {
+template <int NT, typename Total>
+__device__ __forceinline__ void finish(const W4Args& a, int pair, int m0, int ranks, int rank, int first, int step, Total total_of) {
   const bool glu = a.epi == EPI_GEGLU;
   const int t0 = first_tile(pair, a.epi), t1 = second_tile(pair, a.epi);
   const int shift = glu ? 4 : 5, rows = 1 << shift, all = min(NT * 8, a.M - m0) << shift;
   const int e0 = all * rank / ranks, e1 = all * (rank + 1) / ranks;
   for (int e = e0 + first; e < e1; e += step) {
     const int m = e >> shift, r = e & (rows - 1);
-    auto total = [&](int row) {
-      if (ranks == 1) return part[m * kPitch + row];
-      const uint32_t at = smem_u32(part + m * kPitch + row);
-      float x[kRanks];   // (all on their way together)
-#pragma unroll
-      for (int i = 0; i < kRanks; ++i) x[i] = ld_cluster_f(mapa_shared(at, (uint32_t)min(i, ranks - 1)));
-      float v = x[0];
-#pragma unroll
-      for (int i = 1; i < kRanks; ++i) v += i < ranks ? x[i] : 0.f;
-      return v;
-    };
+    auto total = [&](int row) { return total_of(m, row); };
     auto with_bias = [&](int row, float v) {
       const int n = (row < 16 ? t0 : t1) * 16 + (row & 15);
       return a.bias && n < a.w.N ? v + a.bias[n] : v;
@@ -235,20 +190,26 @@ template <bool G32>
 struct Operand {
   uint32_t A[2][4][4];
   float s0[2][G32 ? 2 : 1], s8[2][G32 ? 2 : 1];
-  __device__ __forceinline__ void set(const Block<G32>& b) {
+  __device__ __forceinline__ void set(const uint4* codes, const uint2* sz, int t) {   // sz: of the first 32, of the second
+    const uint32_t c[4] = {codes->x, codes->y, codes->z, codes->w};
+#pragma unroll
+    for (int h = 0; h < (G32 ? 2 : 1); ++h) {
+      s0[t][h] = __uint_as_float(sz[h].x & 0xffff0000u);
+      s8[t][h] = __uint_as_float(sz[h].y & 0xffff0000u);
+      const uint32_t z0 = __byte_perm(sz[h].x, 0u, 0x1010), z8 = __byte_perm(sz[h].y, 0u, 0x1010);
+#pragma unroll
+      for (int i = G32 ? 2 * h : 0; i < (G32 ? 2 * h + 2 : 4); ++i) widen(c[i], z0, z8, A[t][i]);
+    }
+  }
+  template <typename S>
+  __device__ __forceinline__ void set(const S& slot, int lane, int g) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const uint32_t* c = (const uint32_t*)&b.codes[t];
+      const uint4 c = slot.codes[t][lane];
+      uint2 sz[G32 ? 2 : 1];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint2 sz = b.sz[t][G32 ? i >> 1 : 0];
-        widen(c[i], __byte_perm(sz.x, 0u, 0x1010), __byte_perm(sz.y, 0u, 0x1010), A[t][i]);
-      }
-#pragma unroll
-      for (int h = 0; h < (G32 ? 2 : 1); ++h) {
-        s0[t][h] = __uint_as_float(b.sz[t][h].x & 0xffff0000u);
-        s8[t][h] = __uint_as_float(b.sz[t][h].y & 0xffff0000u);
-      }
+      for (int h = 0; h < (G32 ? 2 : 1); ++h) sz[h] = slot.sz[h][t][g];
+      set(&c, sz, t);
     }
   }
   // acc += the block's product with 8 tokens' values x (of its first and its second 32 ks)
@@ -257,11 +218,12 @@ struct Operand {
     for (int t = 0; t < 2; ++t) {
 #pragma unroll
       for (int h = 0; h < (G32 ? 2 : 1); ++h) {
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int hh = G32 ? h : 0; hh < (G32 ? h + 1 : 2); ++hh) {
-          mma_bf16(sum, A[t][2 * hh], x[hh].x, x[hh].y);
-          mma_bf16(sum, A[t][2 * hh + 1], x[hh].z, x[hh].w);
+        float sum[4];
+        mma_bf16_first(sum, A[t][2 * h], x[h].x, x[h].y);
+        mma_bf16(sum, A[t][2 * h + 1], x[h].z, x[h].w);
+        if constexpr (!G32) {
+          mma_bf16(sum, A[t][2], x[1].x, x[1].y);
+          mma_bf16(sum, A[t][3], x[1].z, x[1].w);
         }
         acc[t * stride][0] += s0[t][h] * sum[0];
         acc[t * stride][1] += s0[t][h] * sum[1];
@@ -284,255 +246,150 @@ __device__ __forceinline__ void put_sums(float* to, const float (*acc)[NT][4], i
 }
 
 // A CTA takes two tiles of 16 rows (GeGLU: 16 gate rows and their 16 up rows) and NT * 8 tokens; its eight
-// warps, and the CTAs of its cluster, share the ks.
+// warps, and the CTAs of its cluster, share the ks.  A CTA that has several pairs of tiles goes
+// through them one after another, and the copies of the next pair's weights run on under the end of the one
+// before: each warp has a ring of its own, filled by asynchronous copies.
 //
 // Sums: an MMA chain per group (at most 64 ks of it) starts from zero, and the group's scale
 // takes its result into an fp32 sum, so that weights enter as whole numbers and no scaled weight
 // is rounded.  Parts of the ks are joined in the order of warps and ranks.
+constexpr int kRing = 6;   // blocks of 64 ks
+// CTAs an SM holds, by shared memory and registers
 template <int NT, bool G32>
-__global__ void __launch_bounds__(256) w4_gemm_kernel(W4Args a) {
-  constexpr int kAhead = NT <= 2 ? 4 : 2;   // blocks on their way
+constexpr int kHeld = NT == 1 ? (G32 ? 2 : 3) : NT == 2 ? 2 : 1;
+template <bool G32>
+struct Slot {
+  uint4 codes[2][32];
+  uint2 sz[G32 ? 2 : 1][2][8];
+};
+
+template <int NT, bool G32>
+__global__ void __launch_bounds__(256, kHeld<NT, G32>) w4_gemm_kernel(W4Args a) {
   constexpr int kPart = NT * 8 * kPitch;
-  extern __shared__ float part[];           // [warp][token][kPitch], then the CTA's sums in the first
+  extern __shared__ __align__(16) unsigned char few_smem[];
+  Slot<G32>* ring = (Slot<G32>*)few_smem + (threadIdx.x >> 5) * kRing;
+  float* parts = (float*)((Slot<G32>*)few_smem + kWarps * kRing);   // [2][warp][token][kPitch]
   const W4Matrix& w = a.w;
   const int ranks = (int)gridDim.z, rank = ranks > 1 ? (int)cluster_ctarank() : 0;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
-  const int pair = blockIdx.x, m0 = blockIdx.y * NT * 8;
-  const int t0 = first_tile(pair, a.epi), t1 = second_tile(pair, a.epi);
+  const int pairs = w.tiles / 2, m0 = blockIdx.y * NT * 8;
   const int shares = ranks * kWarps, share = rank * kWarps + warp;
   const int k0 = (int)((long long)w.kblocks * share / shares), k1 = (int)((long long)w.kblocks * (share + 1) / shares);
 
-  Block<G32> held[kAhead];
-  auto fetch = [&](Block<G32>& b, int kb) {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int tile = t ? t1 : t0;
-      b.codes[t] = ld_weights(w.codes + ((size_t)tile * w.kblocks + kb) * 32 + lane);
-#pragma unroll
-      for (int h = 0; h < (G32 ? 2 : 1); ++h) {
-        const int group = min((kb * 64 + h * 32) / w.group, w.groups - 1);
-        b.sz[t][h] = ld_weights(w.sz + ((size_t)tile * w.groups + group) * 8 + g);
+  // the next block of the sequence (pair by pair, the warp's blocks of each) into the next slot
+  int next_pair = blockIdx.x, next_kb = k0, next_slot = 0;
+  const int per_group = w.group == 128 ? 7 : w.group == 64 ? 6 : 5;
+  auto fetch = [&] {
+    if (next_pair < pairs && k0 < k1) {
+      Slot<G32>& to = ring[next_slot];
+      const int t0 = first_tile(next_pair, a.epi), t1 = second_tile(next_pair, a.epi);
+      copy_async(&to.codes[0][lane], w.codes + ((size_t)t0 * w.kblocks + next_kb) * 32 + lane, true);
+      copy_async(&to.codes[1][lane], w.codes + ((size_t)t1 * w.kblocks + next_kb) * 32 + lane, true);
+      const int t = lane >> 2 & 1, h = lane >> 3;   // 64 bytes of scales per tile and group: 4 lanes each
+      if (h < (G32 ? 2 : 1)) {
+        const int group = min((next_kb * 64 + h * 32) >> per_group, w.groups - 1);
+        copy_async(&to.sz[h][t][q * 2], w.sz + ((size_t)(t ? t1 : t0) * w.groups + group) * 8 + q * 2, true);
       }
+      if (++next_kb == k1) next_kb = k0, next_pair += gridDim.x;
+      if (++next_slot == kRing) next_slot = 0;
     }
+    copies_commit();
   };
   // loaded weights do not change: the first blocks are on their way before the launch before has ended
 #pragma unroll
-  for (int d = 0; d < kAhead; ++d)
-    if (k0 + d < k1) fetch(held[d], k0 + d);
+  for (int i = 0; i < kRing - 1; ++i) fetch();
   pdl_trigger();
   pdl_wait();
 
-  float acc[2][NT][4];
+  auto load = [&](uint4 (*x)[2], int kb) {
 #pragma unroll
-  for (int t = 0; t < 2; ++t)
+    for (int n = 0; n < NT; ++n) {
+      const int m = m0 + n * 8 + g;
+      const bf16* row = (const bf16*)a.x + (long long)m * a.lda;
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+      for (int h = 0; h < 2; ++h) x[n][h] = load_x(row, kb * 64 + h * 32 + q * 8, w.K, m < a.M, a.vec);
+    }
+  };
+  constexpr bool kAheadX = NT <= 2;   // the next block's tokens on their way
+  uint4 x[NT][2];
+  if (kAheadX && k0 < k1) load(x, k0);
+  int slot = 0, buf = 0;
+  for (int pair = blockIdx.x; pair < pairs; pair += gridDim.x, buf ^= 1) {
+    float acc[2][NT][4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[t][n][i] = 0.f;
-
-  for (int kb0 = k0; kb0 < k1; kb0 += kAhead) {
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int d = 0; d < kAhead; ++d) {
-      const int kb = kb0 + d;
-      if (kb >= k1) break;
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[t][n][i] = 0.f;
+    for (int kb = k0; kb < k1; ++kb) {
+      copies_wait<kRing - 2>();
+      __syncwarp();
+      fetch();   // (into the slot that was read last)
       Operand<G32> op;
-      op.set(held[d]);
-      if (kb + kAhead < k1) fetch(held[d], kb + kAhead);
+      op.set(ring[slot], lane, g);
+      if (++slot == kRing) slot = 0;
+      uint4 xn[NT][2];
+      if (kAheadX) load(xn, kb + 1 < k1 ? kb + 1 : k0);
+      else load(x, kb);
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        const int m = m0 + n * 8 + g;
-        const bf16* row = (const bf16*)a.x + (long long)m * a.lda;
-        uint4 x[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) x[h] = load_x(row, kb * 64 + h * 32 + q * 8, w.K, m < a.M, a.vec);
-        op.multiply(x, &acc[0][n], NT);
+        op.multiply(x[n], &acc[0][n], NT);
+        if (kAheadX) x[n][0] = xn[n][0], x[n][1] = xn[n][1];
       }
     }
-  }
-
-  float* mine = part + warp * kPart;
-  put_sums<NT>(mine, acc, g, q);
-  __syncthreads();
-  for (int e = threadIdx.x; e < NT * 8 * 32; e += 256) {
-    const int at = (e >> 5) * kPitch + (e & 31);
-    float v = part[at];
+    float* part = parts + buf * kWarps * kPart;   // (two in turn: one barrier a pair)
+    put_sums<NT>(part + warp * kPart, acc, g, q);
+    __syncthreads();
+    auto over_warps = [&](int m, int row) {
+      const float* p = part + m * kPitch + row;
+      float v = p[0];
 #pragma unroll
-    for (int i = 1; i < kWarps; ++i) v += part[i * kPart + at];
-    part[at] = v;   // (read by this thread alone so far)
+      for (int i = 1; i < kWarps; ++i) v += p[i * kPart];
+      return v;
+    };
+    if (ranks == 1) {
+      finish<NT>(a, pair, m0, 1, 0, threadIdx.x, 256, over_warps);
+    } else {   // (one pair a CTA)
+      float* sums = parts + (buf ^ 1) * kWarps * kPart;
+      for (int e = threadIdx.x; e < NT * 8 * 32; e += 256) sums[(e >> 5) * kPitch + (e & 31)] = over_warps(e >> 5, e & 31);
+      cluster_sync();
+      finish<NT>(a, pair, m0, ranks, rank, threadIdx.x, 256, [&](int m, int row) { return over_ranks(sums + m * kPitch + row, ranks); });
+      cluster_sync();   // nobody leaves while its sums are read
+    }
   }
-  if (ranks > 1) cluster_sync();
-  else __syncthreads();
-
-  finish<NT>(a, part, pair, m0, ranks, rank, threadIdx.x, 256);
-  if (ranks > 1) cluster_sync();   // nobody leaves while its sums are read
-}
-
-// More tokens, where the rows fill the SMs: a warp takes a pair of tiles with all of the CTA's ks, so that
-// eight pairs share each token's values.  Codes, scales and values come by asynchronous copies
-// into a ring of stages of 64 ks.  A stage's tokens are rows of 128 bytes, whose halves change
-// places in odd rows: the 8 lanes that a shared-memory access serves at a time read 64 bytes of two rows.
-constexpr int kStages = 6;
-template <int NT>
-struct Stage {
-  uint4 x[NT * 8][8];
-  uint4 codes[kWarps * 2][32];
-  uint2 sz[2][kWarps * 2][8];   // by 32 ks where these are a group, otherwise the first
-};
-
-__device__ __forceinline__ void copy_async(void* to, const void* from, bool there) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(there ? 16 : 0) : "memory");
+  copies_wait<0>();
 }
 
 template <int NT, bool G32>
-__global__ void __launch_bounds__(256, 2) w4_wide_kernel(W4Args a) {
-  extern __shared__ __align__(16) unsigned char wide_smem[];
-  Stage<NT>* ring = (Stage<NT>*)wide_smem;
-  const W4Matrix& w = a.w;
-  const int ranks = (int)gridDim.z, rank = ranks > 1 ? (int)cluster_ctarank() : 0;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q = lane & 3;
-  const int pair0 = blockIdx.x * kWarps, pair = pair0 + warp, pairs = w.tiles / 2, m0 = blockIdx.y * NT * 8;
-  const int k0 = (int)((long long)w.kblocks * rank / ranks), k1 = (int)((long long)w.kblocks * (rank + 1) / ranks);
-
-  // a stage's weights: a warp copies its own pair's; of pairs past the end nothing is copied and nothing kept
-  auto fetch_weights = [&](int kb) {
-    if (pair >= pairs) return;
-    Stage<NT>& st = ring[(kb - k0) % kStages];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int tile = t ? second_tile(pair, a.epi) : first_tile(pair, a.epi);
-      copy_async(&st.codes[warp * 2 + t][lane], w.codes + ((size_t)tile * w.kblocks + kb) * 32 + lane, true);
-    }
-    // 64 bytes of scales per tile and group: 4 lanes each
-    const int t = lane >> 2 & 1, h = lane >> 3;
-    if (h < (G32 ? 2 : 1)) {
-      const int tile = t ? second_tile(pair, a.epi) : first_tile(pair, a.epi);
-      const int group = min((kb * 64 + h * 32) / w.group, w.groups - 1);
-      copy_async(&st.sz[h][warp * 2 + t][(lane & 3) * 2], w.sz + ((size_t)tile * w.groups + group) * 8 + (lane & 3) * 2, true);
-    }
-  };
-  auto fetch_x = [&](int kb) {
-    Stage<NT>& st = ring[(kb - k0) % kStages];
-#pragma unroll
-    for (int i = 0; i < NT * 64 / 256; ++i) {
-      const int at = tid + i * 256, token = at >> 3, piece = at & 7, m = m0 + token, k = kb * 64 + piece * 8;
-      const bf16* row = (const bf16*)a.x + (long long)m * a.lda;
-      uint4* to = &st.x[token][piece ^ (token & 1) * 4];
-      if (a.vec) {
-        const bool there = m < a.M && k + 8 <= w.K;
-        if (m < a.M && k < w.K && !there) *to = load_x(row, k, w.K, true, 0);
-        else copy_async(to, there ? (const void*)(row + k) : a.x, there);
-      } else {
-        *to = load_x(row, k, w.K, m < a.M, 0);
-      }
-    }
-  };
-  auto commit = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
-
-#pragma unroll
-  for (int i = 0; i < kStages - 1; ++i)   // (weights do not change: ahead of the wait)
-    if (k0 + i < k1) fetch_weights(k0 + i);
-  pdl_trigger();
-  pdl_wait();
-#pragma unroll
-  for (int i = 0; i < kStages - 1; ++i) {
-    if (k0 + i < k1) fetch_x(k0 + i);
-    commit();   // (the first group holds all the weights so far)
-  }
-
-  float acc[2][NT][4];
-#pragma unroll
-  for (int t = 0; t < 2; ++t)
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc[t][n][i] = 0.f;
-
-  for (int kb = k0; kb < k1; ++kb) {
-    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
-    __syncthreads();   // everybody's copies are there, and the stage before is read
-    if (kb + kStages - 1 < k1) {
-      fetch_weights(kb + kStages - 1);
-      fetch_x(kb + kStages - 1);
-    }
-    commit();
-    if (pair >= pairs) continue;
-    const Stage<NT>& st = ring[(kb - k0) % kStages];
-    Operand<G32> op;
-    {
-      Block<G32> b;
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        b.codes[t] = st.codes[warp * 2 + t][lane];
-#pragma unroll
-        for (int h = 0; h < (G32 ? 2 : 1); ++h) b.sz[t][h] = st.sz[h][warp * 2 + t][g];
-      }
-      op.set(b);
-    }
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const int token = n * 8 + g;
-      uint4 x[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) x[h] = st.x[token][(h ^ (token & 1)) * 4 + q];
-      op.multiply(x, &acc[0][n], NT);
-    }
-  }
-  asm volatile("cp.async.wait_group 0;" ::: "memory");
-  __syncthreads();
-  float* part = (float*)wide_smem + warp * NT * 8 * kPitch;
-  put_sums<NT>(part, acc, g, q);
-  if (ranks > 1) cluster_sync();
-  else __syncwarp();
-  if (pair < pairs) finish<NT>(a, part, pair, m0, ranks, rank, lane, 32);
-  if (ranks > 1) cluster_sync();   // nobody leaves while its sums are read
-}
-
-template <int NT>
-constexpr size_t wide_smem_of() {
-  return sizeof(Stage<NT>) * kStages > sizeof(float) * kWarps * NT * 8 * kPitch ? sizeof(Stage<NT>) * kStages
-                                                                                  : sizeof(float) * kWarps * NT * 8 * kPitch;
-}
-
-template <int NT>
-cudaError_t init_wide() {
-  cudaError_t e = cudaFuncSetAttribute(w4_wide_kernel<NT, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)wide_smem_of<NT>());
-  if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(w4_wide_kernel<NT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)wide_smem_of<NT>());
-  return e;
-}
-
-template <int NT>
-cudaError_t launch_wide(const W4Args& a, cudaStream_t st) {
-  const int blocks = (a.w.tiles / 2 + kWarps - 1) / kWarps, tiles = (a.M + NT * 8 - 1) / (NT * 8);
-  int ranks = 1;
-  while (ranks < kRanks && (long long)blocks * tiles * ranks < 4 * a.num_sms && a.w.kblocks >= ranks * 2 * 4) ranks *= 2;
-  const Overlap overlap;
-  return launch_kernel_cluster(a.w.group == 32 ? w4_wide_kernel<NT, true> : w4_wide_kernel<NT, false>, dim3(blocks, tiles, ranks),
-                               dim3(256), wide_smem_of<NT>(), st, dim3(1, 1, ranks), a);
-}
-
-template <int NT>
 constexpr size_t smem_of() {
-  return sizeof(float) * kWarps * NT * 8 * kPitch;
+  return sizeof(Slot<G32>) * kWarps * kRing + sizeof(float) * 2 * kWarps * NT * 8 * kPitch;
 }
 
 template <int NT>
 cudaError_t init_nt() {
-  cudaError_t e = cudaFuncSetAttribute(w4_gemm_kernel<NT, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_of<NT>());
+  cudaError_t e = cudaFuncSetAttribute(w4_gemm_kernel<NT, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_of<NT, false>());
   if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(w4_gemm_kernel<NT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_of<NT>());
+    e = cudaFuncSetAttribute(w4_gemm_kernel<NT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_of<NT, true>());
   return e;
 }
 
+template <int NT, bool G32>
+cudaError_t launch_few(const W4Args& a, cudaStream_t st) {
+  const int pairs = a.w.tiles / 2, tiles = (a.M + NT * 8 - 1) / (NT * 8);
+  // the ks of a pair over as many CTAs (1, 2, 4) as there are SMs for and blocks for the warps
+  int ranks = 1;
+  while (ranks < 4 && (long long)pairs * tiles * ranks * 2 <= a.num_sms && a.w.kblocks >= ranks * 2 * kWarps) ranks *= 2;
+  // pairs beyond what the SMs hold at once follow one another in a CTA
+  const int held = kHeld<NT, G32> * a.num_sms;
+  const int across = ranks > 1 || pairs <= held ? pairs : std::max(1, held / std::min(tiles, held));
+  const Overlap overlap;
+  return launch_kernel_cluster(w4_gemm_kernel<NT, G32>, dim3(across, tiles, ranks), dim3(256), smem_of<NT, G32>(), st,
+                               dim3(1, 1, ranks), a);
+}
 template <int NT>
 cudaError_t launch_nt(const W4Args& a, cudaStream_t st) {
-  const int pairs = a.w.tiles / 2, tiles = (a.M + NT * 8 - 1) / (NT * 8);
-  // the ks of a pair over as many CTAs (1, 2, 4, 8) as there are SMs for and blocks for the warps
-  int ranks = 1;
-  while (ranks < 8 && (long long)pairs * tiles * ranks * 2 <= 2 * a.num_sms && a.w.kblocks >= ranks * 2 * kWarps) ranks *= 2;
-  const Overlap overlap;
-  return launch_kernel_cluster(a.w.group == 32 ? w4_gemm_kernel<NT, true> : w4_gemm_kernel<NT, false>, dim3(pairs, tiles, ranks),
-                               dim3(256), smem_of<NT>(), st, dim3(1, 1, ranks), a);
+  return a.w.group == 32 ? launch_few<NT, true>(a, st) : launch_few<NT, false>(a, st);
 }
 
 unsigned blocks_of(long long threads) { return (unsigned)((threads + 255) / 256); }
@@ -542,16 +399,12 @@ unsigned blocks_of(long long threads) { return (unsigned)((threads + 255) / 256)
 cudaError_t init_w4_kernels() {
   cudaError_t e = init_nt<1>();
   if (e == cudaSuccess) e = init_nt<2>();
-  if (e == cudaSuccess) e = init_nt<4>();
-  if (e == cudaSuccess) e = init_nt<8>();
-  if (e == cudaSuccess) e = init_wide<4>();
-  if (e == cudaSuccess) e = init_wide<8>();
+  if (e == cudaSuccess) e = init_w4_tc_kernels();
   return e;
 }
 
 cudaError_t launch_w4_gemm(const W4Args& a, cudaStream_t st) {
-  if (a.M > 16 && a.w.tiles >= 256) return a.M <= 32 ? launch_wide<4>(a, st) : launch_wide<8>(a, st);
-  return a.M <= 8 ? launch_nt<1>(a, st) : a.M <= 16 ? launch_nt<2>(a, st) : a.M <= 32 ? launch_nt<4>(a, st) : launch_nt<8>(a, st);
+  return a.M <= 8 ? launch_nt<1>(a, st) : a.M <= 16 ? launch_nt<2>(a, st) : launch_w4_tc(a, st);
 }
 
 cudaError_t launch_w4_load(const W4Matrix& w, const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, cudaStream_t st) {

@@ -85,6 +85,10 @@ class Weights4(_Handle):
         [n, groups].  Waits for the stream; no product may be running."""
         B.ravel_w4_load(self.handle, codes, scales, zeros, self._stream(stream))
 
+    def reset(self):
+        """Clear a device error (a bounded wait that ran out)."""
+        B.ravel_w4_reset(self.handle)
+
     def read(self, dtype=None, out=None, stream=None):
         """The weights held, [n, k] in bf16 or fp32, for example for products of whole prompts."""
         if out is None:
