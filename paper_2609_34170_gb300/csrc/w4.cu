@@ -404,7 +404,8 @@ cudaError_t init_w4_kernels() {
 }
 
 cudaError_t launch_w4_gemm(const W4Args& a, cudaStream_t st) {
-  return a.M <= 8 ? launch_nt<1>(a, st) : a.M <= 16 ? launch_nt<2>(a, st) : launch_w4_tc(a, st);
+  if (a.M <= 8) return launch_nt<1>(a, st);
+  return a.M <= 16 || !a.vec ? launch_nt<2>(a, st) : launch_w4_tc(a, st);   // (TMA takes aligned rows only)
 }
 
 cudaError_t launch_w4_load(const W4Matrix& w, const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, cudaStream_t st) {

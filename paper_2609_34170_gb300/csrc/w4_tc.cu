@@ -1,6 +1,10 @@
 // Products with 4-bit weights for more tokens than a warp's MMAs carry at the pace of memory: tcgen05, with
 // the weights widened into tensor memory.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
 #include <algorithm>
+#include <atomic>
 
 #include "common.cuh"
 #include "decode.h"
@@ -14,7 +18,7 @@ namespace {
 // A CTA takes 128 rows of weights, the MMAs' M, and NTOK tokens, their N.  Per block of 64 ks:
 //   four of 12 warps widen: a thread takes a row's 64 codes out of a ring of its warp (asynchronous copies),
 //     makes them c - z in bf16 and stores them as the row's 32 columns of A in tensor memory;
-//   four warps copy the tokens' values into a swizzled tile, which is B;
+//   one warp loads the tokens' values by TMA into a swizzled tile, which is B;
 //   one warp issues the MMAs.  A group's products are summed into an accumulator of their own, in turn;
 //   eight warps take the accumulators, scale them by the group's scale and add them up in fp32 registers, half
 //     of a row's tokens to a thread, and at the end of the ks store the outputs.
@@ -23,7 +27,7 @@ namespace {
 // An MMA of 128 x NTOK x 16 occupies the tensor core for 71 cycles at any NTOK up to 128, a block of 128 x
 // 64 weights (4 KB) for 284: 14 bytes a cycle, two thirds of what memory delivers.  MEASURED
 constexpr int kSets = 3;        // of four warps that widen a block
-constexpr int kSumWarp = 4 * kSets, kXWarp = kSumWarp + 8, kMmaWarp = kXWarp + 4;
+constexpr int kSumWarp = 4 * kSets, kXWarp = kSumWarp + 8, kMmaWarp = kXWarp + 1;
 constexpr int kTcThreads = 32 * (kMmaWarp + 1);
 constexpr int kBlocks = 4;      // blocks of A in tensor memory
 constexpr int kXBlocks = 8;     // blocks of B, most of them on their way (their latency is that of four blocks' MMAs)
@@ -46,7 +50,7 @@ struct TcShared {
 
 // GS: 32s of ks in a group
 template <int NTOK, int GS>
-__global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(W4Args a) {
+__global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_constant__ CUtensorMap x_map, W4Args a) {
   typedef TcShared<NTOK, GS> Shared;
   constexpr int kAccs = Shared::kAccs;
   extern __shared__ __align__(1024) unsigned char tc_smem[];
@@ -69,23 +73,33 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(W4Args a) {
   // codes of the sequence of blocks (unit by unit), every kSets-th of them, into the warp's ring
   const int blocks_here = k1 - k0, quarter = warp & 3;
   int next_unit = blockIdx.x, next_kb = k0, next_slot = 0;
-  auto skip = [&](int n) {
+  const uint4 *from0 = nullptr, *from1 = nullptr;   // this lane's pieces of the next block, by tile
+  const uint2* from_sz = nullptr;                   // this lane's piece of the tile's scales
+  const int sz_t = lane >> 2 & 1, sz_h = lane >> 3;
+  auto skip = [&](int n) {   // n blocks on
+    const int unit = next_unit;
     next_kb += n;
     while (next_kb >= k1 && next_unit < units) next_kb -= blocks_here, next_unit += gridDim.x;
+    if (unit != next_unit || !from0) {
+      const int tile0 = next_unit % row_tiles * 8 + 2 * quarter;   // (past the end: anything that is finite)
+      const int t0 = min(tile0, w.tiles - 1), t1 = min(tile0 + 1, w.tiles - 1);
+      from0 = w.codes + ((size_t)t0 * w.kblocks + next_kb) * 32 + lane;
+      from1 = w.codes + ((size_t)t1 * w.kblocks + next_kb) * 32 + lane;
+      from_sz = w.sz + (size_t)(sz_t ? t1 : t0) * w.groups * 8 + (lane & 3) * 2;
+    } else {
+      from0 += n * 32;
+      from1 += n * 32;
+    }
   };
+  // pieces change places with the rows, so that eight lanes that read a piece of eight rows hit all banks
+  const int put = (lane >> 2) * 4 + ((lane & 3) ^ (lane >> 3));
   auto fetch = [&] {
     if (next_unit < units) {
-      const int tile0 = next_unit % row_tiles * 8 + 2 * quarter, g = lane >> 2, q = lane & 3;
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int tile = min(tile0 + t, w.tiles - 1);   // (past the end: anything that is finite)
-        // pieces change places with the rows, so that eight lanes that read a piece of eight rows hit all banks
-        copy_async(&s.codes[warp][next_slot][t][g * 4 + (q ^ (g >> 1))], w.codes + ((size_t)tile * w.kblocks + next_kb) * 32 + lane, true);
-      }
-      const int t = lane >> 2 & 1, h = lane >> 3;
-      if (h < (GS == 1 ? 2 : 1)) {
-        const int group = min((next_kb * 64 + h * 32) >> per_group, w.groups - 1);
-        copy_async(&s.sz[warp][next_slot][h][t][q * 2], w.sz + ((size_t)min(tile0 + t, w.tiles - 1) * w.groups + group) * 8 + q * 2, true);
+      copy_async(&s.codes[warp][next_slot][0][put], from0, true);
+      copy_async(&s.codes[warp][next_slot][1][put], from1, true);
+      if (sz_h < (GS == 1 ? 2 : 1)) {
+        const int group = min((next_kb * 64 + sz_h * 32) >> per_group, w.groups - 1);
+        copy_async(&s.sz[warp][next_slot][sz_h][sz_t][(lane & 3) * 2], from_sz + (size_t)group * 8, true);
       }
       if (++next_slot == kCodeRing) next_slot = 0;
       skip(kSets);
@@ -93,15 +107,20 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(W4Args a) {
     copies_commit();
   };
   // scales of the sequence of groups, a thread its row's
-  const int srow = quarter * 32 + lane, sthread = (tid - 32 * kSumWarp) & 255, sg = srow & 7, shi = srow >> 3 & 1;
-  int scale_unit = blockIdx.x, scale_at = k0 * 2, scale_slot = 0;
+  const int srow = quarter * 32 + lane, sthread = (tid - 32 * kSumWarp) & 255;
+  const int group0 = k0 * 2 / GS, groups_here = (blocks_here * 2 + GS - 1) / GS;
+  int scale_unit = blockIdx.x, scale_at = 0, scale_slot = 0;
+  const uint32_t* from_scale = nullptr;
   auto fetch_scale = [&] {
     if (scale_unit < units) {
-      const int tile = min(scale_unit % row_tiles * 8 + (srow >> 4), w.tiles - 1), group = min(scale_at / GS, w.groups - 1);
-      const uint32_t* from = (const uint32_t*)w.sz + (((size_t)tile * w.groups + group) * 8 + sg) * 2 + shi;
+      if (scale_at == 0) {
+        const int tile = min(scale_unit % row_tiles * 8 + (srow >> 4), w.tiles - 1);
+        from_scale = (const uint32_t*)w.sz + (((size_t)tile * w.groups + group0) * 8 + (srow & 7)) * 2 + (srow >> 3 & 1);
+      }
+      // (past the last group there are no values: its scale will do)
+      const uint32_t* from = from_scale + 16 * (size_t)min(scale_at, w.groups - 1 - group0);
       asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(&s.scale[scale_slot][sthread])), "l"(from) : "memory");
-      scale_at += GS;
-      if (scale_at >= k1 * 2) scale_at = k0 * 2, scale_unit += gridDim.x;
+      if (++scale_at == groups_here) scale_at = 0, scale_unit += gridDim.x;
       if (++scale_slot == kScaleRing) scale_slot = 0;
     }
     copies_commit();
@@ -120,7 +139,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(W4Args a) {
       mbar_init(&s.empty[i], 1);
     }
     for (int i = 0; i < kXBlocks; ++i) {
-      mbar_init(&s.x_full[i], 4);
+      mbar_init(&s.x_full[i], 1);
       mbar_init(&s.x_empty[i], 1);
     }
     for (int i = 0; i < kAccs; ++i) {
@@ -194,7 +213,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(W4Args a) {
     int acc_at = 0, slot = 0;
     uint32_t parity = 0u, up_parity = 0u;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-    const int groups_here = (k1 * 2 - k0 * 2 + GS - 1) / GS;
     for (int unit = blockIdx.x; unit < units && ok; unit += gridDim.x) {
       const int m0 = unit / row_tiles * NTOK, tile = unit % row_tiles, row = tile * 128 + srow, tokens = min(NTOK, a.M - m0);
       float sum[kTok];
@@ -262,53 +280,24 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(W4Args a) {
       }
     }
   } else if (warp < kMmaWarp) {
-    // tokens: a piece of 16 bytes of every sixteenth row per thread; copied six blocks ahead of where they are handed on
-    constexpr int kLag = kXBlocks - 2, kPieces = NTOK / 16;
-    const int t128 = tid - 32 * kXWarp, piece = t128 & 7, token0 = t128 >> 3;
-    const uint32_t to0 = (uint32_t)(token0 * 128 + ((piece ^ (token0 & 7)) << 4));   // (16 rows further the place is the same)
-    int block = 0, done = 0;
+    const uint32_t el = elect_one();
+    uint64_t keep;   // (every CTA reads them)
+    asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(keep));
+    int block = 0, issued = 0;
     uint32_t parity = 1u;
-    int pending = 0;
-    auto hand_on = [&] {
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&s.x_full[done]);
-      if (++done == kXBlocks) done = 0;
-    };
     for (int unit = blockIdx.x; unit < units && ok; unit += gridDim.x) {
       const int m0 = unit / row_tiles * NTOK;
-      const bf16* row[kPieces];
-      uint32_t there = 0u;
-#pragma unroll
-      for (int i = 0; i < kPieces; ++i) {
-        const int m = m0 + token0 + 16 * i;
-        row[i] = (const bf16*)a.x + (long long)min(m, a.M - 1) * a.lda;
-        there |= (m < a.M ? 1u : 0u) << i;
-      }
       for (int kb = k0; kb < k1; ++kb) {
         ok = mbar_wait_warp(&s.x_empty[block], parity);
         if (!ok) break;
-        const int k = kb * 64 + piece * 8;
-        uint8_t* to = s.x[block] + to0;
-        if (a.vec && (k + 8 <= w.K || k >= w.K)) {
-          const bool in = k < w.K;
-#pragma unroll
-          for (int i = 0; i < kPieces; ++i) copy_async(to + i * 2048, row[i] + (in ? k : 0), in && (there >> i & 1u));
-        } else {
-#pragma unroll
-          for (int i = 0; i < kPieces; ++i) *(uint4*)(to + i * 2048) = load_x(row[i], k, w.K, there >> i & 1u, 0);
-        }
-        copies_commit();
+        mbar_expect_tx_el(&s.x_full[block], NTOK * 128, el);
+        tma_load_2d_el(&x_map, smem_u32(&s.x_full[block]), smem_u32(s.x[block]), kb * 64, m0, keep, el);
+        ++issued;
         if (++block == kXBlocks) block = 0, parity ^= 1u;
-        if (++pending > kLag) {
-          copies_wait<kLag>();
-          hand_on();
-          --pending;
-        }
       }
     }
-    copies_wait<0>();
-    for (; ok && pending > 0; --pending) hand_on();
+    // nobody leaves with loads in flight, not even where a wait ran out
+    for (int n = max(0, issued - kXBlocks); n < issued; ++n) ok = mbar_wait_warp(&s.x_full[n % kXBlocks], (n / kXBlocks) & 1u) && ok;
   } else {
     const uint32_t el = elect_one();
     const uint32_t idesc = idesc_bf16(128, NTOK);
@@ -392,15 +381,36 @@ cudaError_t init_gs() {
   return cudaFuncSetAttribute(w4_tc_kernel<NTOK, GS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tc_smem_of<NTOK, GS>());
 }
 
+std::atomic<void*> g_encode{nullptr};
+
+cudaError_t get_encoder() {
+  if (g_encode.load()) return cudaSuccess;
+  cudaDriverEntryPointQueryResult q;
+  void* fn = nullptr;
+  const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q);
+  if (e != cudaSuccess) return e;
+  if (q != cudaDriverEntryPointSuccess || !fn) return cudaErrorSymbolNotFound;
+  g_encode.store(fn);
+  return cudaSuccess;
+}
+
 template <int NTOK, int GS>
 cudaError_t launch_gs(const W4Args& a, cudaStream_t st) {
+  CUtensorMap map;   // boxes of NTOK tokens x 64 ks, zeros past the ends
+  cuuint64_t dims[2] = {(cuuint64_t)a.w.K, (cuuint64_t)a.M};
+  cuuint64_t strides[1] = {(cuuint64_t)a.lda * 2};
+  cuuint32_t box[2] = {64, NTOK}, steps[2] = {1, 1};
+  const auto encode = (PFN_cuTensorMapEncodeTiled_v12000)g_encode.load();
+  if (encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(a.x), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return cudaErrorInvalidValue;
   const int units = (a.w.tiles + 7) / 8 * ((a.M + NTOK - 1) / NTOK);
   // the ks of a unit over as many CTAs (1, 2, 4, 8) as there are SMs for and four blocks for each
   int ranks = 1;
   while (ranks < kRanks && units * ranks * 2 <= a.num_sms && a.w.kblocks >= ranks * 2 * 4) ranks *= 2;
   const Overlap overlap;
   return launch_kernel_cluster(w4_tc_kernel<NTOK, GS>, dim3(ranks > 1 ? units : std::min(units, a.num_sms), 1, ranks), dim3(kTcThreads),
-                               tc_smem_of<NTOK, GS>(), st, dim3(1, 1, ranks), a);
+                               tc_smem_of<NTOK, GS>(), st, dim3(1, 1, ranks), map, a);
 }
 
 template <int NTOK>
@@ -411,7 +421,8 @@ cudaError_t launch_ntok(const W4Args& a, cudaStream_t st) {
 }  // namespace
 
 cudaError_t init_w4_tc_kernels() {
-  cudaError_t e = init_gs<32, 1>();
+  cudaError_t e = get_encoder();
+  if (e == cudaSuccess) e = init_gs<32, 1>();
   if (e == cudaSuccess) e = init_gs<32, 2>();
   if (e == cudaSuccess) e = init_gs<32, 4>();
   if (e == cudaSuccess) e = init_gs<64, 1>();
