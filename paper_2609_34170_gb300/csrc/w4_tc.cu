@@ -1,5 +1,5 @@
 // Products with 4-bit weights for more tokens than a warp's MMAs carry at the pace of memory: tcgen05, with
-// the weights widened into tensor memory.
+// the weights widened into shared memory.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -17,7 +17,7 @@ namespace {
 
 // A CTA takes 128 rows of weights, the MMAs' M, and NTOK tokens, their N.  Per block of 64 ks:
 //   four of 12 warps widen: a thread takes a row's 64 codes out of a ring of its warp (asynchronous copies),
-//     makes them c - z in bf16 and stores them as the row's 32 columns of A in tensor memory;
+//     makes them c - z in bf16 and stores them as the row's 128 bytes of A, in a swizzled tile;
 //   one warp loads the tokens' values by TMA into a swizzled tile, which is B;
 //   one warp issues the MMAs.  A group's products are summed into an accumulator of their own, in turn;
 //   eight warps take the accumulators, scale them by the group's scale and add them up in fp32 registers, half
@@ -29,24 +29,40 @@ namespace {
 constexpr int kSets = 3;        // of four warps that widen a block
 constexpr int kSumWarp = 4 * kSets, kXWarp = kSumWarp + 8, kMmaWarp = kXWarp + 1;
 constexpr int kTcThreads = 32 * (kMmaWarp + 1);
-constexpr int kBlocks = 4;      // blocks of A in tensor memory
-constexpr int kXBlocks = 8;     // blocks of B, most of them on their way (their latency is that of four blocks' MMAs)
-constexpr int kCodeRing = 5;    // blocks of codes on their way to a warp
-constexpr int kScaleRing = 16;  // groups' scales on their way to a thread
+constexpr int kBlocks = 3;      // blocks of A
+constexpr int kXBlocks = 6;     // blocks of B, most of them on their way (their latency is that of four blocks' MMAs)
+constexpr int kCodeRing = 4;    // blocks of codes on their way to a warp
+constexpr int kScaleHalf = 4;   // groups' scales that come to a thread together, while as many are used
 constexpr uint32_t kTcCols = 256;
 constexpr int kSumPitch = 132;  // floats of a token's 128 rows
 
 template <int NTOK, int GS>
 struct TcShared {
-  static constexpr int kAccs = 128 / NTOK;
+  static constexpr int kAccs = (int)kTcCols / NTOK;
+  uint8_t a[kBlocks][128 * 128];                        // swizzled rows of 128 bytes, as x
   uint8_t x[kXBlocks][NTOK * 128];                      // swizzled rows of 128 bytes
   uint4 codes[4 * kSets][kCodeRing][2][32];
   uint2 sz[4 * kSets][kCodeRing][GS == 1 ? 2 : 1][2][8];
-  uint32_t scale[kScaleRing][256];
+  uint32_t scale[2 * kScaleHalf][256];
   float sums[NTOK * kSumPitch];                         // GeGLU's up rows, or the sums for the other ranks
   uint64_t full[kBlocks], empty[kBlocks], x_full[kXBlocks], x_empty[kXBlocks], acc_full[kAccs], acc_empty[kAccs], up_full, up_free, ended;
   uint32_t tmem;
 };
+
+// x += a s, y += b s in one instruction
+__device__ __forceinline__ void fma_pair(float& x, float& y, uint32_t a, uint32_t b, float s) {
+  asm("{\n\t.reg .b64 p, q, r;\n\tmov.b64 p, {%2, %3};\n\tmov.b64 q, {%4, %4};\n\tmov.b64 r, {%0, %1};\n\t"
+      "fma.rn.f32x2 r, p, q, r;\n\tmov.b64 {%0, %1}, r;\n\t}"
+      : "+f"(x), "+f"(y)
+      : "r"(a), "r"(b), "f"(s));
+}
+
+// A wait that tries some times before it looks at the clock.
+__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity) {
+  for (int i = 0; i < 64; ++i)
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  return mbar_wait_warp(bar, parity);
+}
 
 // GS: 32s of ks in a group
 template <int NTOK, int GS>
@@ -109,19 +125,21 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
   // scales of the sequence of groups, a thread its row's
   const int srow = quarter * 32 + lane, sthread = (tid - 32 * kSumWarp) & 255;
   const int group0 = k0 * 2 / GS, groups_here = (blocks_here * 2 + GS - 1) / GS;
-  int scale_unit = blockIdx.x, scale_at = 0, scale_slot = 0;
-  const uint32_t* from_scale = nullptr;
-  auto fetch_scale = [&] {
+  int scale_unit = blockIdx.x, scale_at = 0;
+  const uint32_t scale_to = smem_u32(&s.scale[0][sthread]);
+  // half of the ring: the next kScaleHalf groups of the unit (past the last one there are no values, and its
+  // scale will do: every unit takes whole halves)
+  auto fetch_scales = [&](int half) {
     if (scale_unit < units) {
-      if (scale_at == 0) {
-        const int tile = min(scale_unit % row_tiles * 8 + (srow >> 4), w.tiles - 1);
-        from_scale = (const uint32_t*)w.sz + (((size_t)tile * w.groups + group0) * 8 + (srow & 7)) * 2 + (srow >> 3 & 1);
-      }
-      // (past the last group there are no values: its scale will do)
-      const uint32_t* from = from_scale + 16 * (size_t)min(scale_at, w.groups - 1 - group0);
-      asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(&s.scale[scale_slot][sthread])), "l"(from) : "memory");
-      if (++scale_at == groups_here) scale_at = 0, scale_unit += gridDim.x;
-      if (++scale_slot == kScaleRing) scale_slot = 0;
+      const int tile = min(scale_unit % row_tiles * 8 + (srow >> 4), w.tiles - 1);
+      const uint32_t* from = (const uint32_t*)w.sz + (((size_t)tile * w.groups + group0) * 8 + (srow & 7)) * 2 + (srow >> 3 & 1);
+#pragma unroll
+      for (int i = 0; i < kScaleHalf; ++i)
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(scale_to + (half * kScaleHalf + i) * 1024),
+                     "l"(from + 16 * (size_t)min(scale_at + i, w.groups - 1 - group0))
+                     : "memory");
+      scale_at += kScaleHalf;
+      if (scale_at >= groups_here) scale_at = 0, scale_unit += gridDim.x;
     }
     copies_commit();
   };
@@ -131,7 +149,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
     skip(warp / 4);
     for (int i = 0; i < kCodeRing - 1; ++i) fetch();
   } else if (warp < kXWarp) {
-    for (int i = 0; i < kScaleRing - 1; ++i) fetch_scale();
+    fetch_scales(0);
+    fetch_scales(1);
   }
   if (tid == 0) {
     for (int i = 0; i < kBlocks; ++i) {
@@ -160,12 +179,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
   tc_fence_before();
   cta_sync();
   tc_fence_after();
-  const uint32_t tmem = s.tmem, tmem_a = tmem, tmem_d = tmem + kBlocks * 32;
+  const uint32_t tmem = s.tmem;
   bool ok = true;
 
   if (warp < kSumWarp) {
     const int t = lane >> 4, g = lane & 7, hi = lane >> 3 & 1;
-    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     int slot = 0, block = warp / 4;   // the warp's first block of the sequence, in the ring of blocks
     uint32_t parity = 1u;             // of empty[block]
     if (block >= kBlocks) block -= kBlocks, parity ^= 1u;
@@ -195,13 +213,15 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
           }
         }
         if (++slot == kCodeRing) slot = 0;
-        ok = mbar_wait_warp(&s.empty[block], parity);
+        ok = wait_for(&s.empty[block], parity);
         if (!ok) break;
-        tc_fence_after();
-        tmem_st16u(tmem_a + lanes + block * 32, out[0]);
-        tmem_st16u(tmem_a + lanes + block * 32 + 16, out[1]);
-        tmem_wait_st();
-        tc_fence_before();
+        // pieces of 16 bytes change places with the rows
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const uint32_t* v = &out[j >> 2][(j & 3) * 4];
+          *(uint4*)(s.a[block] + srow * 128 + ((j ^ (srow & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(&s.full[block]);
         block += kSets;
@@ -210,7 +230,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
   } else if (warp < kXWarp) {
     constexpr int kTok = NTOK / 2;   // of a thread
     const int first = (warp - kSumWarp) / 4 * kTok;
-    int acc_at = 0, slot = 0;
+    int acc_at = 0, half = 0;
     uint32_t parity = 0u, up_parity = 0u;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     for (int unit = blockIdx.x; unit < units && ok; unit += gridDim.x) {
@@ -219,16 +239,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
 #pragma unroll
       for (int i = 0; i < kTok; ++i) sum[i] = 0.f;
       for (int group = 0; group < groups_here; ++group) {
-        copies_wait<kScaleRing - 2>();
-        const float scale = __uint_as_float(s.scale[slot][sthread] & 0xffff0000u);
-        fetch_scale();   // (into a slot that this thread has read)
-        if (++slot == kScaleRing) slot = 0;
-        ok = mbar_wait_warp(&s.acc_full[acc_at], parity);
+        if (group % kScaleHalf == 0) copies_wait<1>();
+        const float scale = __uint_as_float(s.scale[half * kScaleHalf + group % kScaleHalf][sthread] & 0xffff0000u);
+        if (group % kScaleHalf == kScaleHalf - 1 || group + 1 == groups_here) {   // (this half is read)
+          fetch_scales(half);
+          half ^= 1;
+        }
+        ok = wait_for(&s.acc_full[acc_at], parity);
         if (!ok) break;
         tc_fence_after();
         uint32_t v[kTok / 16][16];
 #pragma unroll
-        for (int i = 0; i < kTok / 16; ++i) tmem_ld16_async(tmem_d + lanes + acc_at * NTOK + first + i * 16, v[i]);
+        for (int i = 0; i < kTok / 16; ++i) tmem_ld16_async(tmem + lanes + acc_at * NTOK + first + i * 16, v[i]);
         tmem_wait_ld();
 #pragma unroll
         for (int i = 0; i < kTok / 16; ++i) tmem_reg_fence16(v[i]);
@@ -237,7 +259,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
         if (lane == 0) mbar_arrive(&s.acc_empty[acc_at]);
         if (++acc_at == kAccs) acc_at = 0, parity ^= 1u;
 #pragma unroll
-        for (int i = 0; i < kTok; ++i) sum[i] += scale * __uint_as_float(v[i / 16][i % 16]);
+        for (int i = 0; i < kTok; i += 2) fma_pair(sum[i], sum[i + 1], v[i / 16][i % 16], v[i / 16][i % 16 + 1], scale);
       }
       if (!ok) break;
       if (ranks > 1) {   // (the only unit)
@@ -248,14 +270,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
       const float bias = a.bias && row < w.N ? a.bias[row] : 0.f;
       if (a.epi == EPI_GEGLU) {   // (bounded waits: a warp that gave up does not come)
         if (quarter >= 2) {
-          ok = mbar_wait_warp(&s.up_free, up_parity ^ 1u);
+          ok = wait_for(&s.up_free, up_parity ^ 1u);
           if (!ok) break;
 #pragma unroll
           for (int i = 0; i < kTok; ++i) s.sums[(first + i) * kSumPitch + srow] = sum[i] + bias;
           __syncwarp();
           if (lane == 0) mbar_arrive(&s.up_full);
         } else {
-          ok = mbar_wait_warp(&s.up_full, up_parity);
+          ok = wait_for(&s.up_full, up_parity);
           if (!ok) break;
           bf16* out = (bf16*)a.out + (size_t)(m0 + first) * a.ldo + tile * 64 + srow;
 #pragma unroll
@@ -288,7 +310,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
     for (int unit = blockIdx.x; unit < units && ok; unit += gridDim.x) {
       const int m0 = unit / row_tiles * NTOK;
       for (int kb = k0; kb < k1; ++kb) {
-        ok = mbar_wait_warp(&s.x_empty[block], parity);
+        ok = wait_for(&s.x_empty[block], parity);
         if (!ok) break;
         mbar_expect_tx_el(&s.x_full[block], NTOK * 128, el);
         tma_load_2d_el(&x_map, smem_u32(&s.x_full[block]), smem_u32(s.x[block]), kb * 64, m0, keep, el);
@@ -297,43 +319,50 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
       }
     }
     // nobody leaves with loads in flight, not even where a wait ran out
-    for (int n = max(0, issued - kXBlocks); n < issued; ++n) ok = mbar_wait_warp(&s.x_full[n % kXBlocks], (n / kXBlocks) & 1u) && ok;
+    for (int n = max(0, issued - kXBlocks); n < issued; ++n) ok = wait_for(&s.x_full[n % kXBlocks], (n / kXBlocks) & 1u) && ok;
   } else {
     const uint32_t el = elect_one();
     const uint32_t idesc = idesc_bf16(128, NTOK);
-    const uint64_t xd0 = sw128_desc(smem_u32(s.x[0]));
-    int block = 0, x_block = 0, acc_at = 0;
+    const uint64_t xd0 = sw128_desc(smem_u32(s.x[0])), ad0 = sw128_desc(smem_u32(s.a[0]));
+    constexpr int kAccsOf = GS == 1 ? 2 : 1;   // accumulators that a block begins
+    int block = 0, x_block = 0, acc_at = 0, in_unit = 0;
     uint32_t parity = 0u, x_parity = 0u, acc_parity = 1u;
-    for (int unit = blockIdx.x; unit < units && ok; unit += gridDim.x)
-      for (int kb = k0; kb < k1 && ok; ++kb) {
-        ok = mbar_wait_warp(&s.x_full[x_block], x_parity) && mbar_wait_warp(&s.full[block], parity);
+    const int mine = blockIdx.x < units ? (units - 1 - (int)blockIdx.x) / (int)gridDim.x + 1 : 0;
+    for (long long left = (long long)mine * blocks_here; left > 0; --left) {
+      // GS 4: a group is two blocks, or one at the end
+      const bool first = GS < 4 || (in_unit & 1) == 0, last = GS < 4 || (in_unit & 1) || in_unit + 1 == blocks_here;
+      ok = wait_for(&s.x_full[x_block], x_parity);
+      if (!ok) break;
+      ok = wait_for(&s.full[block], parity);
+      if (!ok) break;
+      if (first) {
+        ok = wait_for(&s.acc_empty[acc_at], acc_parity);
         if (!ok) break;
-        const uint32_t ta = tmem_a + block * 32;
-        const uint64_t xd = xd0 + (uint64_t)(x_block * (NTOK * 128 >> 4));
-#pragma unroll
-        for (int part = 0; part < (GS == 1 ? 2 : 1); ++part) {
-          const bool first = GS < 4 || ((kb - k0) & 1) == 0, last = GS < 4 || ((kb - k0) & 1) || kb + 1 == k1;
-          if (first) {
-            ok = ok && mbar_wait_warp(&s.acc_empty[acc_at], acc_parity);
-            if (!ok) break;
-          }
-          tc_fence_after();
-          const uint32_t td = tmem_d + acc_at * NTOK;
-#pragma unroll
-          for (int j = (GS == 1 ? 2 * part : 0); j < (GS == 1 ? 2 * part + 2 : 4); ++j)
-            umma_bf16_ts(td, ta + 8 * j, xd + 2 * j, idesc, j > (GS == 1 ? 2 * part : 0) || !first ? 1u : 0u, el);
-          if (last) {
-            umma_commit(&s.acc_full[acc_at], el);
-            if (++acc_at == kAccs) acc_at = 0, acc_parity ^= 1u;
-          }
+        if (kAccsOf == 2) {   // (the accumulators are an even number)
+          ok = wait_for(&s.acc_empty[acc_at + 1], acc_parity);
+          if (!ok) break;
         }
-        umma_commit(&s.empty[block], el);
-        umma_commit(&s.x_empty[x_block], el);
-        if (++x_block == kXBlocks) x_block = 0, x_parity ^= 1u;
-        if (++block == kBlocks) block = 0, parity ^= 1u;
       }
+      tc_fence_after();
+      const uint64_t ad = ad0 + (uint32_t)(block * (128 * 128 >> 4)), xd = xd0 + (uint32_t)(x_block * (NTOK * 128 >> 4));
+      const uint32_t td = tmem + acc_at * NTOK, more = first ? 0u : 1u;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        umma_bf16(td + (kAccsOf == 2 ? (j >> 1) * NTOK : 0), ad + 2 * j, xd + 2 * j, idesc, j % (4 / kAccsOf) > 0 ? 1u : more, el);
+      if (last) {
+        umma_commit(&s.acc_full[acc_at], el);
+        if (kAccsOf == 2) umma_commit(&s.acc_full[acc_at + 1], el);
+        acc_at += kAccsOf;
+        if (acc_at == kAccs) acc_at = 0, acc_parity ^= 1u;
+      }
+      umma_commit(&s.empty[block], el);
+      umma_commit(&s.x_empty[x_block], el);
+      if (++block == kBlocks) block = 0, parity ^= 1u;
+      if (++x_block == kXBlocks) x_block = 0, x_parity ^= 1u;
+      if (++in_unit == blocks_here) in_unit = 0;
+    }
     umma_commit(&s.ended, el);   // nothing is in flight when the columns are given back
-    ok = mbar_wait_warp(&s.ended, 0u) && ok;
+    ok = wait_for(&s.ended, 0u) && ok;
   }
   copies_wait<0>();
   if (!ok && lane == 0) raise_error(a.err, ERR_TIMEOUT);
