@@ -143,6 +143,8 @@ def _dptr(t, dtype=None, name="tensor"):
 
 
 def _stream_ptr(stream):
+    if type(stream) is int:
+        return stream
     import torch
     if stream is None:
         stream = torch.cuda.current_stream()
@@ -519,11 +521,27 @@ def _check_decode(status: int, what: str):
         raise RavelError(status, f"{what}: {load().ravel_decode_last_error().decode()}")
 
 
+class _Types:
+    """torch's types, looked up once (an import statement takes 0.5 us of a call)."""
+    bf16 = f32 = i32 = u8 = get_device = None
+
+    @classmethod
+    def look_up(cls):
+        import torch
+        cls.bf16, cls.f32, cls.i32, cls.u8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
+        cls.get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+        return cls
+
+
+def _types():
+    return _Types if _Types.bf16 is not None else _Types.look_up()
+
+
 def _row_dtype(t, name: str) -> int:
-    import torch
-    if t.dtype is torch.bfloat16:
+    types = _types()
+    if t.dtype is types.bf16:
         return RAVEL_BF16
-    if t.dtype is torch.float32:
+    if t.dtype is types.f32:
         return RAVEL_FP32
     raise ValueError(f"{name} must be bfloat16 or float32, got {t.dtype}")
 
@@ -532,20 +550,26 @@ def _flat(t, shape: tuple, dtype, device: int, name: str):
     """Address of a contiguous CUDA tensor of that shape, or None."""
     if t is None:
         return None
-    if not hasattr(t, "data_ptr") or t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
-        got = f"{tuple(t.shape)} of {t.dtype} on {t.device}" if hasattr(t, "data_ptr") else repr(t)
-        raise ValueError(f"{name} must be a contiguous tensor {list(shape)} of {dtype} on cuda:{device}, got {got}")
-    return t.data_ptr()
+    try:
+        if t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
+            return t.data_ptr()
+        got = f"{tuple(t.shape)} of {t.dtype} on {t.device}"
+    except AttributeError:
+        got = repr(t)
+    raise ValueError(f"{name} must be a contiguous tensor {list(shape)} of {dtype} on cuda:{device}, got {got}")
 
 
 def _matrix(t, rows: int, cols: int, device: int, name: str) -> int:
     """Row stride of a [rows, cols] tensor whose rows are contiguous; of a single row, whose
     stride means nothing, the next multiple of 8."""
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or t.get_device() != device or (cols > 1 and t.stride(1) != 1):
+    stride = t.stride()
+    if len(stride) != 2 or t.shape != (rows, cols) or t.get_device() != device or (stride[1] != 1 and cols > 1):
         raise ValueError(f"{name} must be [{rows}, {cols}] on cuda:{device} with contiguous rows, got {tuple(t.shape)} on {t.device}")
-    if rows > 1 and t.stride(0) < cols:
+    if rows < 2:
+        return -(-cols // 8) * 8
+    if stride[0] < cols:
         raise ValueError(f"{name}: rows overlap")
-    return t.stride(0) if rows > 1 else -(-cols // 8) * 8
+    return stride[0]
 
 
 def ravel_rotary_create(dims: int, base: float = 10000.0, interleaved: bool = False, factor: float = 1.0,
@@ -570,10 +594,10 @@ def ravel_rotary_destroy(r):
 
 def _heads(x, device: int, name: str):
     """Strides (robot, token) of a [batch, n, heads, hd] tensor whose heads are contiguous."""
-    if x.dim() != 4 or x.get_device() != device:
-        raise ValueError(f"{name} must be [batch, n, heads, head_dim] on cuda:{device}, got {tuple(x.shape)} on {x.device}")
-    shape = x.shape
-    robot, token, head, dim = x.stride()
+    shape, stride = x.shape, x.stride()
+    if len(shape) != 4 or x.get_device() != device:
+        raise ValueError(f"{name} must be [batch, n, heads, head_dim] on cuda:{device}, got {tuple(shape)} on {x.device}")
+    robot, token, head, dim = stride
     if (dim != 1 and shape[3] > 1) or (head != shape[3] and shape[2] > 1):
         raise ValueError(f"{name}: the heads of a token must be contiguous")
     return robot if shape[0] > 1 else 0, token if shape[1] > 1 else 0
@@ -581,7 +605,6 @@ def _heads(x, device: int, name: str):
 
 def ravel_rotary_apply(r, x, out, starts=None, positions=None, counts=None, stream=None):
     """x, out [B, n, heads, hd]; see ravel_decode.h."""
-    import torch
     if getattr(r, "rotary", None) is None:
         raise ValueError("not a handle that ravel_rotary_create returned")
     device = r.rotary[1]
@@ -593,11 +616,13 @@ def ravel_rotary_apply(r, x, out, starts=None, positions=None, counts=None, stre
         if out.shape != x.shape or out.dtype is not x.dtype:
             raise ValueError("out must have x's shape and dtype")
     B, n, heads, hd = x.shape
-    i32 = torch.int32
-    _check_decode(load().ravel_rotary_apply(
+    i32 = _types().i32
+    status = load().ravel_rotary_apply(
         r, B, n, heads, hd, _row_dtype(x, "x"), x.data_ptr(), xr, xt, out.data_ptr(), outr, outt,
         _flat(starts, (B,), i32, device, "starts"), _flat(positions, (B, n), i32, device, "positions"),
-        _flat(counts, (B,), i32, device, "counts"), _stream_ptr(stream)), "ravel_rotary_apply")
+        _flat(counts, (B,), i32, device, "counts"), _stream_ptr(stream))
+    if status:
+        _check_decode(status, "ravel_rotary_apply")
 
 
 def ravel_w4_create(N: int, K: int, group: int = 128, device: int = 0):
@@ -624,12 +649,11 @@ def _w4(w):
 
 def ravel_w4_load(w, codes, scales, zeros, stream=None):
     """codes uint8 [N, (K + 1) // 2], scales bfloat16 and zeros uint8 [N, groups]; see ravel_decode.h."""
-    import torch
     N, K, group, device = _w4(w)
-    groups = -(-K // group)
+    groups, types = -(-K // group), _types()
     _check_decode(load().ravel_w4_load(
-        w, _flat(codes, (N, (K + 1) // 2), torch.uint8, device, "codes"), _flat(scales, (N, groups), torch.bfloat16, device, "scales"),
-        _flat(zeros, (N, groups), torch.uint8, device, "zeros"), _stream_ptr(stream)), "ravel_w4_load")
+        w, _flat(codes, (N, (K + 1) // 2), types.u8, device, "codes"), _flat(scales, (N, groups), types.bf16, device, "scales"),
+        _flat(zeros, (N, groups), types.u8, device, "zeros"), _stream_ptr(stream)), "ravel_w4_load")
 
 
 def ravel_w4_quantize(W, group: int, codes, scales, zeros, stream=None):
@@ -660,35 +684,39 @@ W4_EPILOGUES = {"store": 0, "silu": 1, "add": 2, "geglu": 3}
 
 def ravel_w4_gemm(w, X, epi: int, out, bias=None, stream=None):
     """out (op)= X [M, K] times the matrix's rows (+ bias); see ravel_decode.h."""
-    import torch
     N, K, _, device = _w4(w)
-    if X.dtype is not torch.bfloat16:
+    types = _types()
+    if X.dtype is not types.bf16:
         raise ValueError(f"X must be bfloat16, got {X.dtype}")
     M = X.shape[0]
     lda = _matrix(X, M, K, device, "X")
     ldo = _matrix(out, M, N // 2 if epi == 3 else N, device, "out")
-    _check_decode(load().ravel_w4_gemm(w, X.data_ptr(), M, lda, epi, out.data_ptr(), ldo, _row_dtype(out, "out"),
-                                       _flat(bias, (N,), torch.float32, device, "bias"), _stream_ptr(stream)), "ravel_w4_gemm")
+    status = load().ravel_w4_gemm(w, X.data_ptr(), M, lda, epi, out.data_ptr(), ldo, _row_dtype(out, "out"),
+                                       _flat(bias, (N,), types.f32, device, "bias"), _stream_ptr(stream))
+    if status:
+        _check_decode(status, "ravel_w4_gemm")
 
 
 def ravel_draw_tokens(logits, u, temperature, top_k, top_p, min_p, tokens, log_probs=None, stream=None):
     """logits [B, V]; the others [B] or None; tokens int32 and log_probs float32 [B], written; see ravel_decode.h."""
-    import torch
+    types = _types()
     device = logits.get_device()
     if logits.dim() != 2 or device < 0:
         raise ValueError(f"logits must be a CUDA tensor [batch, vocab], got {tuple(logits.shape)} on {logits.device}")
     B, V = logits.shape
     row = _matrix(logits, B, V, device, "logits")
-    f32, i32, one = torch.float32, torch.int32, (B,)
+    f32, i32, one = types.f32, types.i32, (B,)
     if u is None or tokens is None:
         raise ValueError("u and tokens must be given")
     args = (logits.data_ptr(), B, V, row, _row_dtype(logits, "logits"), _flat(u, one, f32, device, "u"),
             _flat(temperature, one, f32, device, "temperature"), _flat(top_k, one, i32, device, "top_k"),
             _flat(top_p, one, f32, device, "top_p"), _flat(min_p, one, f32, device, "min_p"), _flat(tokens, one, i32, device, "tokens"),
-            _flat(log_probs, one, f32, device, "log_probs"))
-    if torch.cuda.current_device() == device:
-        status = load().ravel_draw_tokens(*args, _stream_ptr(stream))
+            _flat(log_probs, one, f32, device, "log_probs"), _stream_ptr(stream))
+    if types.get_device() == device:
+        status = load().ravel_draw_tokens(*args)
     else:
+        import torch
         with torch.cuda.device(device):
-            status = load().ravel_draw_tokens(*args, _stream_ptr(stream))
-    _check_decode(status, "ravel_draw_tokens")
+            status = load().ravel_draw_tokens(*args)
+    if status:
+        _check_decode(status, "ravel_draw_tokens")

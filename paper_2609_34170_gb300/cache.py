@@ -33,7 +33,7 @@ class ContextCache:
                                            B.RAVEL_BF16 if dtype == "bf16" else B.RAVEL_FP32, device)
         self._lib = B.load()
         arguments = self.handle.arguments
-        self._rows, self._ints, self._mass = arguments.rows, arguments.ints, arguments.mass
+        self._rows, self._ints, self._mass, self._dense = arguments.rows, arguments.ints, arguments.mass, arguments.dense
         self._int32, self._float32 = torch.int32, torch.float32
         self._index, self._current_stream = self.device.index, B.current_stream_getter()
 
@@ -66,10 +66,40 @@ class ContextCache:
         starts[b] + i), and the queries q [B, n, Hq, hd] turned with them: returned, or written to
         q_out, which may be q itself (rows from counts[b] on are not written; of a new tensor they are
         zeros).  q None: keys alone."""
-        if q is not None and q_out is None:
-            q_out = self._empty(q.shape, q.dtype, stream, zeros=counts is not None)
-        B.ravel_cache_append_rotary(self.handle, layer, rotary.handle, q, q_out, k, v, starts, positions, counts,
-                                    self._stream(stream))
+        r = rotary.handle
+        if getattr(r, "rotary", None) is None:
+            raise ValueError("rotary must be an open Rotary")
+        rows, ints = self._rows, self._ints
+        shape = k.shape
+        krs, kts = rows(k, self.n_kv_heads, "k")
+        if v.shape != shape:
+            raise ValueError("k and v must have the same shape")
+        vrs, vts = rows(v, self.n_kv_heads, "v")
+        batch, n = shape[0], shape[1]
+        q_at = out_at = None
+        qrs = qts = ors = ots = 0
+        if q is not None:
+            qrs, qts = rows(q, self.n_q_heads, "q")
+            shape = q.shape
+            if shape[0] != batch or shape[1] != n:
+                raise ValueError("q must have as many tokens as k")
+            if q_out is None:
+                q_out = self._empty(shape, q.dtype, stream, zeros=counts is not None)
+            elif q_out.shape != shape:
+                raise ValueError("q_out must have q's shape")
+            if q_out is q:
+                ors, ots = qrs, qts
+            else:
+                ors, ots = rows(q_out, self.n_q_heads, "q_out")
+            q_at, out_at = q.data_ptr(), q_out.data_ptr()
+        elif q_out is not None:
+            raise ValueError("q and q_out go together")
+        status = self._lib.ravel_cache_append_rotary(
+            self.handle, layer, r, batch, n, q_at, qrs, qts, out_at, ors, ots, k.data_ptr(), krs, kts, v.data_ptr(), vrs, vts,
+            ints(starts, batch, "starts"), self._dense(positions, (batch, n), self._int32, "positions") if positions is not None else None,
+            ints(counts, batch, "counts"), self._stream(stream))
+        if status:
+            B._check_cache(self.handle, status, "ravel_cache_append_rotary")
         return q_out
 
     def attend(self, layer: int, q, lengths, counts=None, causal: bool = True, window: int = 0, sinks: int = 0,

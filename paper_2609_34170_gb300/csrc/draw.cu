@@ -3,15 +3,15 @@
 // Weights are whole numbers, 2^43 exp((x - max) / T) rounded, so that their sums are exact and
 // the same in any order; a row is at most 2^20 long, its sum below 2^64.  The order of the tokens (by
 // logit, equal ones by index) is not made: a limit is a border in it, a key and how many of the
-// tokens with that key stay.
+// tokens with that key stay; as one number, (key, ~index) of the last token that stays.
 //
 // A cluster of CTAs per row.  The row's maximum first; then a histogram of 512 bins between the
 // maximum and the least logit that has a weight, of counts and, where top-p alone limits, of weights: the
 // bin that holds the border.  Where the tokens up to that bin are at most 2048, they are brought
-// together in one CTA, which sorts them and does the rest by itself.  Where they are more, the
-// bin's own tokens are, which gives the border, and the cluster sums what stays in the order of the index: by
-// warps' runs first, then within the run that holds the token.  Where even the bin holds more
-// (thousands of nearly equal logits), a radix selection over the keys' four bytes finds the border.
+// together in one CTA, which does the rest by itself.  Where they are more, the bin's own tokens are, which gives
+// the border, while the weights before it are summed by warps' runs of the row; the run that holds the
+// token is gone through again.  Where even the bin holds more (thousands of nearly equal logits), a
+// radix selection over the keys' four bytes finds the border.
 #include <algorithm>
 
 #include "common.cuh"
@@ -63,6 +63,13 @@ __device__ __forceinline__ float value_of(uint32_t key) {
 // border in a hundred falls elsewhere than in 64 bits.)
 struct Weigher {
   float top, ch, cl;   // half the largest logit; twice log2(e) / T
+  // (in two floats: 64-bit ones come two to a clock)
+  __device__ __forceinline__ Weigher(float max, float temperature) {
+    const float c = 2.88539004f, less = 3.851925982e-08f;   // 2 log2(e) = c + less
+    top = 0.5f * max;
+    ch = __fdiv_rn(c, temperature);
+    cl = __fdiv_rn(__fmaf_rn(-ch, temperature, c) + less, temperature);
+  }
   __device__ __forceinline__ u64 operator()(float logit, const u64* table) const {
     const float x = 0.5f * logit;   // (halves, so that no difference overflows)
     const float dh = x - top;
@@ -85,6 +92,20 @@ struct Weigher {
     return (w + (1ull << (down - 1))) >> down;
   }
 };
+
+// ln(p) for 0 < p < 1 in two floats, off by some 2^-43: ln of p's mantissa m from logf, corrected by what
+// m lacks of exp of that, and its exponent.
+__device__ __forceinline__ float2 log_of(float p, const u64* table) {
+  int e;
+  const float m = frexpf(p, &e);   // 1/2 <= m < 1
+  const float y = logf(m);
+  const Weigher weigh(0.f, 1.f);
+  const u64 w = weigh(y, table);
+  const float more = (float)((long long)(u64)(m * 0x1p24f) * (1ll << (kBits - 24)) - (long long)w) / (float)w;
+  const float a = (float)e * 0.693147182f, al = __fmaf_rn((float)e, 0.693147182f, -a) + (float)e * -1.90465421e-9f;
+  const float h = a + y, v = h - a, hl = (a - (h - v)) + (y - v);
+  return make_float2(h, hl + al + more);
+}
 
 // floor(f * s), or the next whole number at or above, for a finite f >= 0
 __device__ __forceinline__ u64 times_fraction(u64 s, float f, bool up) {
@@ -138,19 +159,15 @@ struct DrawShared {
     uint32_t bins[3][kBins];    // of a CTA: counts, weights' low and high words
     u64 hist[2][256];           // radix selection
   };
-  u64 list[kCap];               // (key, ~index), in the order of the index
+  u64 list[kCap];               // (key, ~index)
   union {
     u64 sorted[kCap];           // the same, from the largest down
     float keep[kWarps][64];     // a warp's logits that wait for their weights
   };
   u64 slot[2][2];               // what this CTA gives to a reduction
-  u64 warp_a[kWarps], warp_b[kWarps];
-  u64 sel_left, sel_before, sel_in;
-  double per_t, least;          // 1 / T; T log(min_p)
-  float ch, cl;                 // Weigher's
-  uint32_t counts[kRanks];
-  uint32_t sel_bin, sel_key, listed, found_run;
-  u64 run_at, run_equal;
+  u64 warp_a[kWarps], runs[kWarps];
+  u64 sel, sel_before, sel_in;
+  uint32_t sel_bin, listed, counts[kRanks], found_run;
 };
 
 template <typename T>
@@ -162,21 +179,17 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const float inf = __uint_as_float(0x7f800000u);
   s.table[tid] = kExp.v[tid];
+  for (int i = tid; i < 3 * kBins; i += kThreads) (&s.bins[0][0])[i] = 0u;
+  if (tid == 0) s.listed = 0u;
   pdl_trigger();
   pdl_wait();
   const float u = a.u[b], t = a.temperature ? a.temperature[b] : 1.f, p = a.top_p ? a.top_p[b] : 1.f, mp = a.min_p ? a.min_p[b] : 0.f;
   int k = a.top_k ? a.top_k[b] : 0;
-  if (tid == kThreads - 1) {   // (one thread: 64-bit floats come two to a clock)
-    const double c = 2.0 * 1.4426950408889634074 / (double)t;
-    s.ch = (float)c;
-    s.cl = (float)(c - (double)s.ch);
-    s.per_t = 1.0 / (double)t;
-    s.least = mp > 0.f ? (double)t * log((double)fminf(mp, 1.f)) : 0.0;
-  }
   const T* row = (const T*)a.logits + (long long)b * a.row;
   // this warp's run of the row: whole steps of 32 lanes x V values
   const int steps_all = (a.vocab + 32 * V - 1) / (32 * V), shares = ranks * kWarps, share = rank * kWarps + warp;
-  const int step0 = (int)((long long)steps_all * share / shares), step1 = (int)((long long)steps_all * (share + 1) / shares);
+  auto first_step = [&](int share) { return (int)((long long)steps_all * share / shares); };
+  const int step0 = first_step(share), step1 = first_step(share + 1);
 
   auto load = [&](int step, float* x) {   // values past the end: -inf
     const int i = (step * 32 + lane) * V;
@@ -192,6 +205,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
     }
   };
   auto index_of = [&](int step, int j) { return (step * 32 + lane) * V + j; };
+  auto order_of = [&](float x, int i) { return (u64)key_of(x) << 32 | (kAll - (uint32_t)i); };
   int turn = 0;
   auto barrier = [&] {
     if (ranks > 1) cluster_sync();
@@ -209,27 +223,21 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
     return n;
   };
   auto from_rank = [&](const u64* p, int i) { return ranks > 1 ? ld_cluster_u64(mapa_shared(smem_u32(p), (uint32_t)i)) : *p; };
-  // maxima or sums of x and of y over the row's threads, for every thread
-  u64 before_x, before_y;
-  auto reduce = [&](u64 x, u64 y, bool maximum, u64& rx, u64& ry) {
-    x = maximum ? warp_max_u64(x) : warp_sum_u64(x);
-    y = maximum ? warp_max_u64(y) : warp_sum_u64(y);
-    if (lane == 0) s.warp_a[warp] = x, s.warp_b[warp] = y;
+  // maxima of x and of y over the row's threads, for every thread
+  auto reduce_max = [&](u64& x, u64& y) {
+    x = warp_max_u64(x);
+    y = warp_max_u64(y);
+    if (lane == 0) s.warp_a[warp] = x, s.runs[warp] = y;
     __syncthreads();
     if (warp == 0) {
-      u64 p = s.warp_a[lane], r = s.warp_b[lane];
-      p = maximum ? warp_max_u64(p) : warp_sum_u64(p);
-      r = maximum ? warp_max_u64(r) : warp_sum_u64(r);
-      if (lane == 0) s.slot[turn][0] = p, s.slot[turn][1] = r;
+      x = warp_max_u64(s.warp_a[lane]);
+      y = warp_max_u64(s.runs[lane]);
+      if (lane == 0) s.slot[turn][0] = x, s.slot[turn][1] = y;
     }
     barrier();
     // lane i takes rank i's
-    x = lane < ranks ? from_rank(&s.slot[turn][0], lane) : 0ull;
-    y = lane < ranks ? from_rank(&s.slot[turn][1], lane) : 0ull;
-    rx = maximum ? warp_max_u64(x) : warp_sum_u64(x);
-    ry = maximum ? warp_max_u64(y) : warp_sum_u64(y);
-    before_x = warp_sum_u64(lane < rank ? x : 0ull);   // of the ranks before this one
-    before_y = warp_sum_u64(lane < rank ? y : 0ull);
+    x = warp_max_u64(lane < ranks ? from_rank(&s.slot[turn][0], lane) : 0ull);
+    y = warp_max_u64(lane < ranks ? from_rank(&s.slot[turn][1], lane) : 0ull);
     turn ^= 1;
   };
   // sum of x over the threads before this one and, in all, over the CTA
@@ -261,46 +269,52 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
     load(step, x);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const uint32_t key = key_of(x[j]);
-      const u64 c = (u64)key << 32 | (kAll - (uint32_t)index_of(step, j));
+      const u64 c = order_of(x[j], index_of(step, j));
       best = c > best ? c : best;
       if (!(x[j] < inf)) low |= 1ull << 32;
-      else if (x[j] > -inf) low = (low & 1ull << 32) | max((uint32_t)low, ~key);
+      else if (x[j] > -inf) low = (low & 1ull << 32) | max((uint32_t)low, ~(uint32_t)(c >> 32));
     }
   }
-  reduce(best, low, true, best, low);
+  reduce_max(best, low);
   const float top = value_of((uint32_t)(best >> 32));
-  auto answer = [&](int token, float log_prob) {
+  const Weigher weigh(top, t);
+  // log of the share of a token of logit x: x's part in the log2 domain and the sum's, in two floats
+  auto answer = [&](int token, float x, u64 total) {
     a.tokens[b] = token;
-    if (a.log_probs) a.log_probs[b] = log_prob;
+    if (!a.log_probs) return;
+    const float d = 0.5f * x - weigh.top, yh = d * weigh.ch, yl = __fmaf_rn(d, weigh.ch, -yh) + d * weigh.cl;
+    const int e = 63 - __clzll((long long)total);
+    const float m = (float)total * exp2f((float)-e);   // total = m 2^e
+    const float h = yh - (float)(e - kBits), v = h - yh, l = (yh - (h - v)) + (-(float)(e - kBits) - v) + yl;
+    a.log_probs[b] = __fmaf_rn(h, 0.693147182f, __fmaf_rn(l, 0.693147182f, h * -1.90465421e-9f) - logf(m));
   };
   const bool none = low >> 32 || !(top > -inf) || !(u >= 0.f && u < 1.f) || !(t < inf) || p != p || mp != mp;
   if (none || t < 0x1p-20f) {
     if (rank == 0 && tid == 0) {
-      if (none) answer(-1, -inf);
-      else answer((int)(kAll - (uint32_t)best), 0.f);
+      a.tokens[b] = none ? -1 : (int)(kAll - (uint32_t)best);
+      if (a.log_probs) a.log_probs[b] = none ? -inf : 0.f;
     }
     barrier();   // (nobody leaves while its slot is read)
     return;
   }
-  const Weigher weigh{0.5f * top, s.ch, s.cl};
-  auto log_prob = [&](float x, u64 total) {
-    const int e = 63 - __clzll((long long)total);
-    const float m = (float)total * exp2f((float)-e);   // total = m 2^e
-    return (float)(((double)x - (double)top) * s.per_t - (double)(e - kBits) * 0.6931471805599453094 - (double)logf(m));
-  };
-  // least key that min-p lets through
-  uint32_t least = 0u;
+  // the last of the order that min-p lets through: key of the least logit that is not below
+  // top + T ln(min_p), any index
+  u64 last = 0ull;
   if (mp > 0.f) {
-    const double limit = (double)top + s.least;
-    float f = (float)limit;
-    if ((double)f < limit) f = nextafterf(f, inf);
-    least = key_of(f);
+    float limit = top;
+    if (mp < 1.f) {
+      const float2 l = log_of(mp, s.table);
+      const float h = t * l.x, hl = __fmaf_rn(t, l.x, -h) + t * l.y;
+      limit = top + h;
+      const float v = limit - top, rest = (top - (limit - v)) + (h - v) + hl;
+      if (rest > 0.f) limit = nextafterf(limit, inf);
+      limit = fminf(limit, top);
+    }
+    last = (u64)key_of(limit) << 32;
   }
 
   // Bins of the order: equal parts of the log2 domain from the maximum down to the least logit or
-  // to 2^-44, where weights end; the last one for what has none.  Every step of the formula is
-  // monotone in x, rounding included.
+  // to 2^-44, where weights end.  Every step of the formula is monotone in x, rounding included.
   const float y_least = fmaxf((0.5f * value_of(~(uint32_t)low) - weigh.top) * weigh.ch, -44.f);
   const float per_bin = (float)(kBins - 1) / fmaxf(-y_least, 0x1p-40f);
   // place in bins, for bin i from i up to below i + 1 (the last but one: from there on); -1: no weight
@@ -308,83 +322,63 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
     const float y = (0.5f * x - weigh.top) * weigh.ch;
     return y > -44.f ? fminf(-y * per_bin, (float)(kBins - 2)) : -1.f;
   };
-  // The bin at which `part` 0 (counts) or 1 (weights), summed from the first on, reaches `target`, what
-  // comes before it and what is in it; target > all: the last one.  For every thread of the row.
-  auto bin_at = [&](int part, auto target_of, uint32_t& bin, u64& before, u64& in) {
-    u64 n = 0;
-    if (tid < kBins) n = part == 0 ? sum_of(&s.bins[0][tid]) : sum_of(&s.bins[1][tid]) + (sum_of(&s.bins[2][tid]) << 32);
-    u64 all;
-    const u64 cum = block_scan(n, all);
-    const u64 target = target_of(all);
+  // The bin at which the counts or the weights, summed from the first on, reach `target`, what comes
+  // before it and what is in it; target > all: the last one.  For every thread of the row.
+  auto bin_at = [&](u64 n, u64 target, u64 cum, u64 all, uint32_t& bin, u64& before, u64& in) {
     if (tid == 0) s.sel_bin = kBins - 1, s.sel_before = all, s.sel_in = 0;
     __syncthreads();
     if (tid < kBins && cum < target && cum + n >= target) s.sel_bin = tid, s.sel_before = cum, s.sel_in = n;
     __syncthreads();
     bin = s.sel_bin, before = s.sel_before, in = s.sel_in;
   };
-  // Tokens of the bins first .. last, in the order of the index, into rank 0's list; their number.
-  auto gather = [&](uint32_t first, uint32_t last) {
-    const float from = (float)first, to = (float)(last + 1);
-    auto wanted = [&](float x) {   // (past the end there is no weight)
-      const float place = place_of(x);
-      return place >= from && place < to;
-    };
-    uint32_t n = 0;
-#pragma unroll 2
-    for (int step = step0; step < step1; ++step) {
-      float x[V];
-      load(step, x);
-#pragma unroll
-      for (int j = 0; j < V; ++j) n += wanted(x[j]);
-    }
-    n = __reduce_add_sync(kAll, n);
-    u64 all;
-    u64 at = block_scan(lane == 0 ? n : 0ull, all);
-    at = __shfl_sync(kAll, at, 0);
-    if (n) {
-      for (int step = step0; step < step1; ++step) {
-        float x[V];
-        load(step, x);
-        uint32_t mine = 0;
-#pragma unroll
-        for (int j = 0; j < V; ++j) mine += wanted(x[j]);
-        if (!__any_sync(kAll, mine)) continue;
-        uint32_t upto = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const uint32_t up = __shfl_up_sync(kAll, upto, o);
-          if (lane >= o) upto += up;
-        }
-        uint32_t put = (uint32_t)at + upto - mine;
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-          if (wanted(x[j]) && put < kCap) s.list[put++] = (u64)key_of(x[j]) << 32 | (kAll - (uint32_t)index_of(step, j));
-        at += __shfl_sync(kAll, upto, 31);
-      }
-    }
-    if (tid == 0) s.slot[turn][0] = all;
+  // The lists of the ranks one behind the other in rank 0; their number there.
+  auto bring_together = [&] {
     barrier();
-    int total = (int)min(all, (u64)kCap);
+    int own = (int)min(s.listed, (uint32_t)kCap), total = own;   // (the counts said that all fit)
     if (rank == 0 && ranks > 1) {
-      if (tid < ranks) s.counts[tid] = (uint32_t)from_rank(&s.slot[turn][0], tid);
+      if (tid < ranks) s.counts[tid] = ld_cluster_u32(mapa_shared(smem_u32(&s.listed), (uint32_t)tid));
       __syncthreads();
       for (int r = 1; r < ranks; ++r) total += (int)s.counts[r];
-      total = min(total, kCap);   // (the counts said so; logits that change under the kernel must not write past the list)
-      for (int flat = (int)min(all, (u64)kCap) + tid; flat < total; flat += kThreads) {   // behind its own
-        int i = flat - (int)all, r = 1;
+      total = min(total, kCap);
+      for (int flat = own + tid; flat < total; flat += kThreads) {
+        int i = flat - own, r = 1;
         while (i >= (int)s.counts[r]) i -= (int)s.counts[r++];
         s.list[flat] = from_rank(&s.list[i], r);
       }
       __syncthreads();
     }
-    turn ^= 1;
-    return total;   // (of rank 0)
+    return total;
   };
-  // s.sorted: the n values of s.list from the largest down, zeros behind; a bitonic network
+  // a warp's tokens (those of lanes whose `in` is set) behind those that are listed
+  auto list_up = [&](bool in, u64 order) {
+    const uint32_t mask = __ballot_sync(kAll, in);
+    if (mask == 0u) return;
+    uint32_t at = 0;
+    if (lane == 0) at = atomicAdd(&s.listed, (uint32_t)__popc(mask));
+    at = __shfl_sync(kAll, at, 0) + __popc(mask & ((1u << lane) - 1u));
+    if (in && at < (uint32_t)kCap) s.list[at] = order;
+  };
+  // s.sorted: the n values of s.list from the largest down, zeros behind.  Few: each value's place is the number of
+  // larger ones.  Many: a bitonic network.
   auto sort = [&](int n) {
-    int size = 64;
-    while (size < n) size *= 2;
+    if (n <= 512) {
+      for (int i = n + tid; i < kCap; i += kThreads) s.sorted[i] = 0ull;
+      // four threads to a value up to 256 of them, two up to 512
+      const int parts = n <= 256 ? 4 : 2, i = tid / parts, part = tid % parts;
+      const u64 x = i < n ? s.list[i] : 0ull;
+      uint32_t larger = 0;
+      if (i - lane / parts < n)   // (whole warps)
+        for (int j = part; j < n; j += parts) larger += s.list[j] > x;
+      larger += __shfl_xor_sync(kAll, larger, 1);
+      if (parts == 4) larger += __shfl_xor_sync(kAll, larger, 2);
+      if (part == 0 && i < n) s.sorted[larger] = x;
+      __syncthreads();
+      return;
+    }
+    int size = 1024;
+    if (size < n) size = kCap;
     for (int i = tid; i < size; i += kThreads) s.sorted[i] = i < n ? s.list[i] : 0ull;
+    if (size < kCap) s.sorted[size + tid] = 0ull;
     __syncthreads();
     for (int run = 2; run <= size; run *= 2)
       for (int stride = run / 2; stride > 0; stride /= 2) {
@@ -399,15 +393,126 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
       }
     __syncthreads();
   };
+  auto weight_at = [&](u64 order) { return weigh(value_of((uint32_t)(order >> 32)), s.table); };
+  // Of s.sorted's first n the one at which the weights from the first on, `before` being those before them, reach
+  // `want` (the last one if they do not).  two: this thread's two weights.
+  auto reach = [&](int n, u64 before, const u64* two, u64 want) {
+    u64 all;
+    const u64 cum = before + block_scan(two[0] + two[1], all);
+    if (tid == 0) s.sel = s.sorted[n - 1];
+    __syncthreads();
+    if (cum < want && cum + two[0] >= want) s.sel = s.sorted[2 * tid];
+    else if (cum + two[0] < want && cum + two[0] + two[1] >= want) s.sel = s.sorted[2 * tid + 1];
+    __syncthreads();
+    return s.sel;
+  };
+  auto share_of = [&](u64 all) { return max(1ull, p > 0.f ? times_fraction(all, p, true) : 0ull); };   // top-p's
 
-  // The border: tokens of keys above it stay, and of those with its key the first `ties`.
-  uint32_t border = 0u;   // (below every key)
-  u64 ties = 0ull;
+  // The token at which the sum of value_at(x, order) in the order of the index exceeds target_of(all): given
+  // the warps' sums, `sum` of each lane's, the run that holds it is gone through once more, by all warps of its CTA,
+  // a step to a warp.  found(index, x, all) is called by the thread that has it.
+  auto locate = [&](u64 sum, auto value_at, auto target_of, auto found) {
+    sum = warp_sum_u64(sum);
+    __syncthreads();
+    if (lane == 0) s.runs[warp] = sum;
+    __syncthreads();
+    u64 w0, w1;   // before warp `lane` of this CTA, and with it
+    auto scan = [&](const u64* of, u64 before) {
+      const u64 w = of[lane];
+      w1 = w;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const u64 up = __shfl_up_sync(kAll, w1, o);
+        if (lane >= o) w1 += up;
+      }
+      w1 += before;
+      w0 = w1 - w;
+      return __shfl_sync(kAll, w1, 31);
+    };
+    const u64 mine = scan(s.runs, 0ull);
+    if (tid == 0) s.slot[turn][0] = mine;
+    barrier();
+    const u64 of_rank = lane < ranks ? from_rank(&s.slot[turn][0], lane) : 0ull;
+    turn ^= 1;
+    const u64 all = warp_sum_u64(of_rank), at = target_of(all);
+    u64 before = warp_sum_u64(lane < rank ? of_rank : 0ull);
+    if (before <= at && at < before + mine) {   // (all of the CTA)
+      w0 += before, w1 += before;
+      if (warp == 0 && w0 <= at && at < w1) s.found_run = (uint32_t)lane, s.sel = w0;
+      __syncthreads();
+      const int f0 = first_step(rank * kWarps + (int)s.found_run), f1 = first_step(rank * kWarps + (int)s.found_run + 1);
+      before = s.sel;
+      for (int base = f0; base < f1; base += kWarps) {
+        const int step = base + warp;
+        float x[V];
+        u64 w[V], ws = 0;
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] = -inf;
+        if (step < f1) load(step, x);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          w[j] = step < f1 && index_of(step, j) < a.vocab ? value_at(x[j], order_of(x[j], index_of(step, j))) : 0ull;
+          ws += w[j];
+        }
+        u64 wi = ws;   // up to and with this lane
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const u64 up = __shfl_up_sync(kAll, wi, o);
+          if (lane >= o) wi += up;
+        }
+        __syncthreads();
+        if (lane == 31) s.warp_a[warp] = wi;
+        __syncthreads();
+        before = scan(s.warp_a, before);
+        u64 c = __shfl_sync(kAll, w0, warp) + wi - ws;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          if (c <= at && at < c + w[j]) found(index_of(step, j), x[j], all);
+          c += w[j];
+        }
+        if (before > at) break;   // (all threads: the same sums)
+      }
+    }
+  };
+  auto weight_from = [&](float x, u64 order) { return order >= last ? weigh(x, s.table) : 0ull; };
+  auto draw = [&](u64 sum) {
+    locate(sum, weight_from, [&](u64 all) { return times_fraction(all, u, false); },
+           [&](int i, float x, u64 all) { answer(i, x, all); });
+    barrier();   // nobody leaves while its sums are read
+  };
+  // this lane's share of the weights of tokens that `takes` says yes to: their logits are collected until there are
+  // weights for a whole warp to compute
+  auto sum_weights = [&](auto takes) {
+    float* keep = s.keep[warp];
+    uint32_t n = 0;
+    u64 sum = 0;
+#pragma unroll 2
+    for (int step = step0; step < step1; ++step) {
+      float x[V];
+      load(step, x);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const bool in = takes(x[j], order_of(x[j], index_of(step, j)));
+        const uint32_t mask = __ballot_sync(kAll, in);
+        if (mask == 0u) continue;
+        if (in) keep[n + __popc(mask & ((1u << lane) - 1u))] = x[j];
+        n += __popc(mask);
+        __syncwarp();
+        if (n >= 32u) {
+          n -= 32u;
+          sum += weigh(keep[n + lane], s.table);
+          __syncwarp();
+        }
+      }
+    }
+    if ((uint32_t)lane < n) sum += weigh(keep[lane], s.table);
+    __syncwarp();
+    return sum;
+  };
+
   const bool by_count = k > 0 && k < a.vocab, by_weight = p < 1.f;
   bool radix = false;
   if (by_count || by_weight) {
-    for (int i = tid; i < kBins; i += kThreads) s.bins[0][i] = s.bins[1][i] = s.bins[2][i] = 0u;
-    __syncthreads();
 #pragma unroll 2
     for (int step = step0; step < step1; ++step) {
       float x[V];
@@ -426,93 +531,125 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
       }
     }
     barrier();
-    uint32_t bin, cbin;
-    u64 before = 0, in = 0, count = 0, cin = 0, want = 0;
+    uint32_t bin;
+    u64 before = 0, in = 0, want = 0, all;
+    const u64 n = tid < kBins ? sum_of(&s.bins[0][tid]) : 0ull;
+    u64 upto = block_scan(n, all), count, cin;   // tokens up to the bin, in it
     if (by_count) {
-      bin_at(0, [&](u64) { return (u64)k; }, cbin, count, cin);
-      bin = cbin;
+      bin_at(n, (u64)k, upto, all, bin, before, in);
       if (bin == kBins - 1) k = 0;   // what top-k leaves out has no weight
-      count += cin;
+      cin = in, count = before + in;
     } else {
-      bin_at(1, [&](u64 all) { return want = max(1ull, p > 0.f ? times_fraction(all, p, true) : 0ull); }, bin, before, in);
-      // tokens up to that bin and in it
-      const u64 n = tid <= bin ? sum_of(&s.bins[0][tid]) : 0ull;
-      block_scan(n, count);
-      block_scan(tid == bin ? n : 0ull, cin);
+      const u64 w = tid < kBins ? sum_of(&s.bins[1][tid]) + (sum_of(&s.bins[2][tid]) << 32) : 0ull;
+      const u64 cum = block_scan(w, all);
+      want = share_of(all);
+      bin_at(w, want, cum, all, bin, before, in);
+      __syncthreads();
+      if (tid == (int)bin) s.sel = upto + n, s.sel_in = n;
+      __syncthreads();
+      count = s.sel, cin = s.sel_in;
     }
-    if (by_count && k == 0 && by_weight) {
-      radix = true;
-    } else if (by_count && k == 0) {
-      // nothing is left out
+    const float from = (float)bin, to = (float)(bin + 1);
+    if (by_count && k == 0) {
+      radix = by_weight;   // (without top-p nothing is left out)
     } else if (count <= kCap) {
       // all that can stay comes together in rank 0, which goes on alone
-      const int n = gather(0u, bin);
+#pragma unroll 1
+      for (int step = step0; step < step1; ++step) {
+        float x[V];
+        load(step, x);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          const float place = place_of(x[j]);
+          list_up(place >= 0.f && place < to, order_of(x[j], index_of(step, j)));
+        }
+      }
+      const int n = bring_together();
       if (rank == 0) {
         sort(n);
-        const int kept = by_count ? k : n;   // (k <= n)
+        const int kept = by_count ? min(k, n) : n;
         // two tokens per thread, from the first of the order on
         u64 w[2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) w[i] = 2 * tid + i < kept ? weigh(value_of((uint32_t)(s.sorted[2 * tid + i] >> 32)), s.table) : 0ull;
-        u64 all;
-        const u64 cum = block_scan(w[0] + w[1], all);
-        if (by_count) want = by_weight ? max(1ull, p > 0.f ? times_fraction(all, p, true) : 0ull) : all;
-        if (!by_weight) want = ~0ull;   // (what stays ends with the kept)
-        if (tid == 0) s.sel_left = s.sorted[kept - 1];
-        __syncthreads();
-        if (cum < want && cum + w[0] >= want) s.sel_left = s.sorted[2 * tid];
-        else if (cum + w[0] < want && cum + w[0] + w[1] >= want) s.sel_left = s.sorted[2 * tid + 1];
-        __syncthreads();
-        const u64 last = max(s.sel_left, (u64)least << 32);
-        // the draw, in the order of the index
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const u64 c = 2 * tid + i < n ? s.list[2 * tid + i] : 0ull;
-          w[i] = 2 * tid + i < n && c >= last ? weigh(value_of((uint32_t)(c >> 32)), s.table) : 0ull;
+        for (int i = 0; i < 2; ++i) w[i] = 2 * tid + i < kept ? weight_at(s.sorted[2 * tid + i]) : 0ull;
+        if (by_weight) {
+          u64 all;
+          if (by_count) {
+            block_scan(w[0] + w[1], all);
+            want = share_of(all);
+          }
+          last = max(last, reach(kept, 0ull, w, want));
+        } else {
+          last = max(last, s.sorted[kept - 1]);
         }
+        // the draw, in the order of the index: what stays, sorted by ~index
+        int stay = 0;   // tokens that do
+#pragma unroll
+        for (int i = 0; i < 2; ++i) stay += 2 * tid + i < kept && s.sorted[2 * tid + i] >= last;
+        u64 left;
+        block_scan((u64)stay, left);
+        const int m = (int)left;
+        __syncthreads();
+        for (int i = tid; i < m; i += kThreads) {
+          const u64 c = s.sorted[i];
+          s.list[i] = c << 32 | c >> 32;   // (~index, key): the first token has the largest
+        }
+        __syncthreads();
+        sort(m);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) w[i] = 2 * tid + i < m ? weigh(value_of((uint32_t)s.sorted[2 * tid + i]), s.table) : 0ull;
         u64 total;
         const u64 sum = block_scan(w[0] + w[1], total);
         const u64 at = times_fraction(total, u, false);
         if (sum <= at && at < sum + w[0] + w[1]) {
-          const u64 c = s.list[2 * tid + (sum + w[0] <= at)];
-          answer((int)(kAll - (uint32_t)c), log_prob(value_of((uint32_t)(c >> 32)), total));
+          const u64 c = s.sorted[2 * tid + (sum + w[0] <= at)];
+          answer((int)(kAll - (uint32_t)(c >> 32)), value_of((uint32_t)c), total);
         }
       }
       barrier();   // nobody leaves while its list is read
       return;
     } else if (cin <= kCap && !(by_count && by_weight)) {
-      // the border's bin alone, whose sorted tokens hold the border
-      const int n = gather(bin, bin);
+      // the border's bin alone, whose sorted tokens hold the border; meanwhile the weights before it
+      u64 sum = sum_weights([&](float x, u64 order) {
+        const float place = place_of(x);
+        list_up(place >= from && place < to, order);
+        return place >= 0.f && place < from && order >= last;
+      });
+      const int n = bring_together();
       if (rank == 0) {
         sort(n);
-        u64 last;
+        u64 border;
         if (by_count) {
-          last = s.sorted[k - (int)(count - cin) - 1];
+          border = s.sorted[min(max(k - (int)before - 1, 0), kCap - 1)];
         } else {
           u64 w[2];
 #pragma unroll
-          for (int i = 0; i < 2; ++i) w[i] = 2 * tid + i < n ? weigh(value_of((uint32_t)(s.sorted[2 * tid + i] >> 32)), s.table) : 0ull;
-          u64 all;
-          const u64 cum = before + block_scan(w[0] + w[1], all);
-          if (cum < want && cum + w[0] >= want) s.sel_left = s.sorted[2 * tid];
-          else if (cum + w[0] < want && cum + w[0] + w[1] >= want) s.sel_left = s.sorted[2 * tid + 1];
-          __syncthreads();
-          last = s.sel_left;
+          for (int i = 0; i < 2; ++i) w[i] = 2 * tid + i < n ? weight_at(s.sorted[2 * tid + i]) : 0ull;
+          border = reach(n, before, w, want);
         }
-        u64 equal = 0;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const u64 c = 2 * tid + i < n ? s.sorted[2 * tid + i] : 0ull;
-          equal += c >> 32 == last >> 32 && c >= last;
-        }
-        u64 all;
-        block_scan(equal, all);
-        if (tid == 0) s.slot[turn][0] = last >> 32, s.slot[turn][1] = all;
+        if (tid == 0) s.slot[turn][0] = border;
       }
       barrier();
-      border = (uint32_t)from_rank(&s.slot[turn][0], 0);
-      ties = from_rank(&s.slot[turn][1], 0);
+      last = max(last, from_rank(&s.slot[turn][0], 0));
       turn ^= 1;
+      // the bin's tokens that stay, into the sums of their runs: this CTA's, in its list
+      if (lane == 0) s.runs[warp] = 0ull;
+      const int own = rank == 0 && ranks > 1 ? (int)s.counts[0] : (int)min(s.listed, (uint32_t)kCap);
+      __syncthreads();
+      for (int i = tid; i < own; i += kThreads) {
+        const u64 c = s.list[i];
+        if (c < last) continue;
+        const int step = (int)((kAll - (uint32_t)c) / (32 * V));
+        int w = (int)(((long long)step * shares + shares - 1) / steps_all) - rank * kWarps;   // its run, or one beside it
+        w = min(max(w, 0), kWarps - 1);
+        while (w > 0 && first_step(rank * kWarps + w) > step) --w;
+        while (w < kWarps - 1 && first_step(rank * kWarps + w + 1) <= step) ++w;
+        atomicAdd(&s.runs[w], weight_at(c));
+      }
+      __syncthreads();
+      if (lane == 0) sum += s.runs[warp];
+      draw(sum);
+      return;
     } else {
       radix = true;
     }
@@ -546,50 +683,63 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
           for (int i = 0; i < ranks; ++i) n += from_rank(&hist[255 - tid], i);
         u64 all;
         const u64 cum = block_scan(n, all);
-        if (tid < 256 && cum < target && cum + n >= target) s.sel_bin = 255u - tid, s.sel_left = target - cum;
+        if (tid < 256 && cum < target && cum + n >= target) s.sel_bin = 255u - tid, s.sel = target - cum;
         __syncthreads();
         prefix |= s.sel_bin << shift;
         mask |= 255u << shift;
-        target = s.sel_left;
+        target = s.sel;
         turn ^= 1;
       }
       left = target;
       return prefix;
     };
+    uint32_t border = 0u;   // tokens of keys above it stay, and of those with its key the first `ties`
+    u64 ties = 0ull;
     barrier();   // (the histograms lie where the bins are read)
     if (k > 0 && by_count) border = select((u64)k, 0u, false, ties);
     if (by_weight) {
-      u64 all = 0, nothing;
-      for (int step = step0; step < step1; ++step) {
-        float x[V];
-        load(step, x);
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-          if (key_of(x[j]) > border) all += weigh(x[j], s.table);
-      }
-      reduce(all, 0ull, false, all, nothing);
+      u64 all = sum_weights([&](float x, u64 order) { return (uint32_t)(order >> 32) > border; }), ignored;
+      all = warp_sum_u64(all);
+      block_scan(lane == 0 ? all : 0ull, ignored);
+      if (tid == 0) s.slot[turn][0] = ignored;
+      barrier();
+      all = warp_sum_u64(lane < ranks ? from_rank(&s.slot[turn][0], lane) : 0ull);
+      turn ^= 1;
       const u64 one = ties ? weigh(value_of(border), s.table) : 0ull;
-      const u64 want = max(1ull, p > 0.f ? times_fraction(all + ties * one, p, true) : 0ull);
+      const u64 want = share_of(all + ties * one);
       if (want <= all) {
         u64 left;
         border = select(want, border, true, left);
         const u64 w = weigh(value_of(border), s.table);
-        ties = (left + w - 1) / w;
+        ties = (left + w - 1) / max(w, 1ull);
       } else {   // the tokens that top-k left at its border
         ties = min(ties, (want - all + one - 1) / max(one, 1ull));
       }
     }
-  }
-  if (least > border) {
-    border = least - 1u;
-    ties = 0ull;
+    if (border > 0u) {
+      // the last of the ties that stay
+      auto tie = [&](float x, u64 order) { return (uint32_t)(order >> 32) == border ? 1ull : 0ull; };
+      u64 n = 0;
+      for (int step = step0; step < step1; ++step) {
+        float x[V];
+        load(step, x);
+#pragma unroll
+        for (int j = 0; j < V; ++j) n += index_of(step, j) < a.vocab ? tie(x[j], order_of(x[j], index_of(step, j))) : 0ull;
+      }
+      if (tid == 0) s.sel_in = 0ull;
+      locate(n, tie, [&](u64 all) { return min(ties, all) - 1ull; }, [&](int i, float x, u64 all) { s.sel_in = order_of(x, i); });
+      __syncthreads();
+      if (tid == 0) s.slot[turn][0] = s.sel_in;
+      barrier();
+      last = max(last, warp_max_u64(lane < ranks ? from_rank(&s.slot[turn][0], lane) : 0ull));
+      turn ^= 1;
+    }
   }
 
-  // What stays, summed by warps' runs.  Its logits are collected until there are weights for a
-  // whole warp to compute.
-  const u64 one = ties ? weigh(value_of(border), s.table) : 0ull;
-  u64 sum = 0, equal = 0;
-  if (border == 0u) {
+  // What stays, summed by warps' runs.
+  u64 sum = 0;
+  if (last == 0ull) {
+#pragma unroll 2
     for (int step = step0; step < step1; ++step) {
       float x[V];
       load(step, x);
@@ -597,95 +747,9 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
       for (int j = 0; j < V; ++j) sum += weigh(x[j], s.table);
     }
   } else {
-    float* keep = s.keep[warp];
-    uint32_t n = 0;
-#pragma unroll 2
-    for (int step = step0; step < step1; ++step) {
-      float x[V];
-      load(step, x);
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const uint32_t key = key_of(x[j]);
-        equal += key == border && index_of(step, j) < a.vocab;
-        const uint32_t mask = __ballot_sync(kAll, key > border);
-        if (mask == 0u) continue;
-        if (key > border) keep[n + __popc(mask & ((1u << lane) - 1u))] = x[j];
-        n += __popc(mask);
-        __syncwarp();
-        if (n >= 32u) {
-          n -= 32u;
-          sum += weigh(keep[n + lane], s.table);
-          __syncwarp();
-        }
-      }
-    }
-    if ((uint32_t)lane < n) sum += weigh(keep[lane], s.table);
+    sum = sum_weights([&](float x, u64 order) { return order >= last; });
   }
-  u64 all, all_equal;
-  reduce(sum, equal, false, all, all_equal);
-  const u64 total = all + min(ties, all_equal) * one;
-  const u64 at = times_fraction(total, u, false);   // the token's part of the sum holds this
-  auto upto = [&](u64 w, u64 n) { return w + min(ties, n) * one; };
-  u64 before = before_x, equal_before = before_y;
-  const u64 mine = s.slot[turn ^ 1][0], mine_equal = s.slot[turn ^ 1][1];
-  if (upto(before, equal_before) <= at && at < upto(before + mine, equal_before + mine_equal)) {
-    // the token is in this CTA: in which warp's run
-    u64 w0, w1, e0, e1;   // before warp `lane`, and with it
-    auto scan_warps = [&] {
-      const u64 w = s.warp_a[lane], e = s.warp_b[lane];
-      w1 = w, e1 = e;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const u64 wu = __shfl_up_sync(kAll, w1, o), eu = __shfl_up_sync(kAll, e1, o);
-        if (lane >= o) w1 += wu, e1 += eu;
-      }
-      w1 += before, e1 += equal_before;
-      w0 = w1 - w, e0 = e1 - e;
-    };
-    scan_warps();
-    if (warp == 0 && upto(w0, e0) <= at && at < upto(w1, e1)) s.found_run = (uint32_t)lane, s.run_at = w0, s.run_equal = e0;
-    __syncthreads();
-    // that run again, by all warps: 32 of its steps at a time, a step to a warp
-    const int fshare = rank * kWarps + (int)s.found_run;
-    const int f0 = (int)((long long)steps_all * fshare / shares), f1 = (int)((long long)steps_all * (fshare + 1) / shares);
-    before = s.run_at, equal_before = s.run_equal;
-    for (int base = f0; base < f1; base += kWarps) {
-      const int step = base + warp;
-      float x[V];
-      u64 w[V], ws = 0, ns = 0;
-#pragma unroll
-      for (int j = 0; j < V; ++j) x[j] = -inf;
-      if (step < f1) load(step, x);
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const uint32_t key = key_of(x[j]);
-        w[j] = key > border ? weigh(x[j], s.table) : 0ull;
-        ws += w[j];
-        ns += key == border && index_of(step, j) < a.vocab && step < f1;
-      }
-      u64 wi = ws, ni = ns;   // up to and with this lane
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const u64 wu = __shfl_up_sync(kAll, wi, o), nu = __shfl_up_sync(kAll, ni, o);
-        if (lane >= o) wi += wu, ni += nu;
-      }
-      __syncthreads();
-      if (lane == 31) s.warp_a[warp] = wi, s.warp_b[warp] = ni;
-      __syncthreads();
-      scan_warps();
-      u64 c = __shfl_sync(kAll, w0, warp) + wi - ws, e = __shfl_sync(kAll, e0, warp) + ni - ns;
-      before = __shfl_sync(kAll, w1, 31), equal_before = __shfl_sync(kAll, e1, 31);
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const u64 was = upto(c, e);
-        c += w[j];
-        e += key_of(x[j]) == border && index_of(step, j) < a.vocab && step < f1;
-        if (was <= at && upto(c, e) > at) answer(index_of(step, j), log_prob(x[j], total));
-      }
-      if (upto(before, equal_before) > at) break;   // (all threads: the same sums)
-    }
-  }
-  barrier();   // nobody leaves while its sums are read
+  draw(sum);
 }
 
 }  // namespace

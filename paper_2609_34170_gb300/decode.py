@@ -12,6 +12,13 @@ from __future__ import annotations
 from . import _binding as B
 
 
+def _current_stream(device: int) -> int:
+    """Address of a device's current stream."""
+    global _current_stream
+    _current_stream = B.current_stream_getter()
+    return _current_stream(device)
+
+
 class _Handle:
     """Owns a handle of the library on one device."""
 
@@ -122,7 +129,7 @@ def quantize4(w, group: int = 128, stream=None):
     codes = B.new_tensor((n, (k + 1) // 2), torch.uint8, w.device, stream)
     scales, zeros = (B.new_tensor((n, groups), t, w.device, stream) for t in (torch.bfloat16, torch.uint8))
     if stream is None:
-        stream = B.current_stream_getter()(w.get_device())
+        stream = _current_stream(w.get_device())
     B.ravel_w4_quantize(w, group, codes, scales, zeros, stream)
     return codes, scales, zeros
 
@@ -132,12 +139,15 @@ def draw_tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=None,
     < 1), and with log_probs its log-probability.  temperature, top_p, min_p (fp32 [B]) and top_k (int32
     [B]) are settings of each row or None; see ravel_decode.h for their order and what they leave.  A row that
     cannot be drawn from (nothing but -inf, a NaN, a setting out of range) gives -1."""
-    import torch
+    types = B._types()
+    index = logits.get_device()
+    if index < 0:
+        raise ValueError(f"logits must be a CUDA tensor, got one on {logits.device}")
     shape, device = (logits.shape[0],), logits.device
     if tokens is None:
-        tokens = B.new_tensor(shape, torch.int32, device, stream)
-    logs = B.new_tensor(shape, torch.float32, device, stream) if log_probs else None
+        tokens = B.new_tensor(shape, types.i32, device, stream)
+    logs = B.new_tensor(shape, types.f32, device, stream) if log_probs else None
     if stream is None:
-        stream = B.current_stream_getter()(logits.get_device())
+        stream = _current_stream(index)
     B.ravel_draw_tokens(logits, u, temperature, top_k, top_p, min_p, tokens, logs, stream)
     return (tokens, logs) if log_probs else tokens
