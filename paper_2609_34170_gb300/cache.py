@@ -44,6 +44,9 @@ class ContextCache:
         return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
     def _empty(self, shape, dtype, stream, zeros=False):
+        """A new tensor of the stream that is going to write it."""
+        if stream is None:
+            return (self.torch.zeros if zeros else self.torch.empty)(shape, dtype=dtype, device=self.device)
         return B.new_tensor(shape, dtype, self.device, stream, zeros)
 
     # -- calls

@@ -349,48 +349,68 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
     }
     return total;
   };
-  // a warp's tokens (those of lanes whose `in` is set) behind those that are listed
-  auto list_up = [&](bool in, u64 order) {
-    const uint32_t mask = __ballot_sync(kAll, in);
-    if (mask == 0u) return;
+  // of a step's V values per lane those whose bit is set in `in`, behind those that are listed
+  auto list_up = [&](uint32_t in, const float* x, int step) {
+    if (!__any_sync(kAll, in != 0u)) return;
+    uint32_t upto = __popc(in);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t up = __shfl_up_sync(kAll, upto, o);
+      if (lane >= o) upto += up;
+    }
     uint32_t at = 0;
-    if (lane == 0) at = atomicAdd(&s.listed, (uint32_t)__popc(mask));
-    at = __shfl_sync(kAll, at, 0) + __popc(mask & ((1u << lane) - 1u));
-    if (in && at < (uint32_t)kCap) s.list[at] = order;
+    if (lane == 31) at = atomicAdd(&s.listed, upto);
+    at = __shfl_sync(kAll, at, 31) + upto - __popc(in);
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (in >> j & 1u) {
+        if (at < (uint32_t)kCap) s.list[at] = order_of(x[j], index_of(step, j));
+        ++at;
+      }
   };
   // s.sorted: the n values of s.list from the largest down, zeros behind.  Few: each value's place is the number of
-  // larger ones.  Many: a bitonic network.
+  // larger ones, counted by four threads.  Many: a bitonic network, two values to a thread, that exchanges within a
+  // warp by shuffles and beyond through s.sorted.
   auto sort = [&](int n) {
-    if (n <= 512) {
+    if (n <= 256) {
       for (int i = n + tid; i < kCap; i += kThreads) s.sorted[i] = 0ull;
-      // four threads to a value up to 256 of them, two up to 512
-      const int parts = n <= 256 ? 4 : 2, i = tid / parts, part = tid % parts;
+      const int i = tid / 4, part = tid % 4;
       const u64 x = i < n ? s.list[i] : 0ull;
       uint32_t larger = 0;
-      if (i - lane / parts < n)   // (whole warps)
-        for (int j = part; j < n; j += parts) larger += s.list[j] > x;
+      if (i - lane / 4 < n)   // (whole warps)
+        for (int j = part; j < n; j += 4) larger += s.list[j] > x;
       larger += __shfl_xor_sync(kAll, larger, 1);
-      if (parts == 4) larger += __shfl_xor_sync(kAll, larger, 2);
+      larger += __shfl_xor_sync(kAll, larger, 2);
       if (part == 0 && i < n) s.sorted[larger] = x;
       __syncthreads();
       return;
     }
-    int size = 1024;
-    if (size < n) size = kCap;
-    for (int i = tid; i < size; i += kThreads) s.sorted[i] = i < n ? s.list[i] : 0ull;
-    if (size < kCap) s.sorted[size + tid] = 0ull;
-    __syncthreads();
-    for (int run = 2; run <= size; run *= 2)
-      for (int stride = run / 2; stride > 0; stride /= 2) {
-        if (tid < size / 2) {
-          const int i = 2 * tid - (tid & (stride - 1)), j = i + stride;
-          const u64 x = s.sorted[i], y = s.sorted[j];
-          if ((x < y) == ((i & run) == 0)) s.sorted[i] = y, s.sorted[j] = x;
+    int size = 512;
+    while (size < n) size *= 2;
+    u64 x = 2 * tid < n ? s.list[2 * tid] : 0ull, y = 2 * tid + 1 < n ? s.list[2 * tid + 1] : 0ull;
+    for (int run = 2; run <= size; run *= 2) {
+      const bool down = (2 * tid & run) == 0;
+      for (int apart = run / 4; apart > 0; apart /= 2) {   // in threads
+        u64 px, py;
+        if (apart >= 32) {
+          __syncthreads();
+          s.sorted[2 * tid] = x, s.sorted[2 * tid + 1] = y;
+          __syncthreads();
+          px = s.sorted[2 * (tid ^ apart)], py = s.sorted[2 * (tid ^ apart) + 1];
+        } else {
+          px = __shfl_xor_sync(kAll, x, apart), py = __shfl_xor_sync(kAll, y, apart);
         }
-        // (up to 32 apart, a warp's pairs stay within its own 64 values)
-        if (stride > 32 || (stride == 1 && run >= 64)) __syncthreads();
-        else __syncwarp();
+        const bool larger = ((tid & apart) == 0) == down;
+        x = larger == (px > x) ? px : x;
+        y = larger == (py > y) ? py : y;
       }
+      if ((x < y) == down) {
+        const u64 z = x;
+        x = y, y = z;
+      }
+    }
+    __syncthreads();
+    s.sorted[2 * tid] = x, s.sorted[2 * tid + 1] = y;   // (threads past `size` hold zeros throughout)
     __syncthreads();
   };
   auto weight_at = [&](u64 order) { return weigh(value_of((uint32_t)(order >> 32)), s.table); };
@@ -482,7 +502,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
   };
   // this lane's share of the weights of tokens that `takes` says yes to: their logits are collected until there are
   // weights for a whole warp to compute
-  auto sum_weights = [&](auto takes) {
+  auto sum_weights = [&](auto takes, auto lists) {
     float* keep = s.keep[warp];
     uint32_t n = 0;
     u64 sum = 0;
@@ -490,6 +510,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
     for (int step = step0; step < step1; ++step) {
       float x[V];
       load(step, x);
+      lists(x, step);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const bool in = takes(x[j], order_of(x[j], index_of(step, j)));
@@ -510,6 +531,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
     return sum;
   };
 
+  auto no_list = [](const float*, int) {};
   const bool by_count = k > 0 && k < a.vocab, by_weight = p < 1.f;
   bool radix = false;
   if (by_count || by_weight) {
@@ -558,11 +580,13 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
       for (int step = step0; step < step1; ++step) {
         float x[V];
         load(step, x);
+        uint32_t in = 0u;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           const float place = place_of(x[j]);
-          list_up(place >= 0.f && place < to, order_of(x[j], index_of(step, j)));
+          in |= (place >= 0.f && place < to ? 1u : 0u) << j;
         }
+        list_up(in, x, step);
       }
       const int n = bring_together();
       if (rank == 0) {
@@ -610,11 +634,20 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
       return;
     } else if (cin <= kCap && !(by_count && by_weight)) {
       // the border's bin alone, whose sorted tokens hold the border; meanwhile the weights before it
-      u64 sum = sum_weights([&](float x, u64 order) {
-        const float place = place_of(x);
-        list_up(place >= from && place < to, order);
-        return place >= 0.f && place < from && order >= last;
-      });
+      u64 sum = sum_weights(
+          [&](float x, u64 order) {
+            const float place = place_of(x);
+            return place >= 0.f && place < from && order >= last;
+          },
+          [&](const float* x, int step) {
+            uint32_t in = 0u;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+              const float place = place_of(x[j]);
+              in |= (place >= from && place < to ? 1u : 0u) << j;
+            }
+            list_up(in, x, step);
+          });
       const int n = bring_together();
       if (rank == 0) {
         sort(n);
@@ -698,7 +731,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
     barrier();   // (the histograms lie where the bins are read)
     if (k > 0 && by_count) border = select((u64)k, 0u, false, ties);
     if (by_weight) {
-      u64 all = sum_weights([&](float x, u64 order) { return (uint32_t)(order >> 32) > border; }), ignored;
+      u64 all = sum_weights([&](float x, u64 order) { return (uint32_t)(order >> 32) > border; }, no_list), ignored;
       all = warp_sum_u64(all);
       block_scan(lane == 0 ? all : 0ull, ignored);
       if (tid == 0) s.slot[turn][0] = ignored;
@@ -747,7 +780,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
       for (int j = 0; j < V; ++j) sum += weigh(x[j], s.table);
     }
   } else {
-    sum = sum_weights([&](float x, u64 order) { return order >= last; });
+    sum = sum_weights([&](float x, u64 order) { return order >= last; }, no_list);
   }
   draw(sum);
 }
