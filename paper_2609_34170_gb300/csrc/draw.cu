@@ -158,16 +158,22 @@ struct DrawShared {
   union {
     uint32_t bins[3][kBins];    // of a CTA: counts, weights' low and high words
     u64 hist[2][256];           // radix selection
+    struct {
+      u64 hist[kBins];          // selection within the list
+      u64 few[256];
+    } pick;
   };
   u64 list[kCap];               // (key, ~index)
   union {
     u64 sorted[kCap];           // the same, from the largest down
+    u64 few_weights[256];
+    ulonglong2 pairs[256];      // values and weights
     float keep[kWarps][64];     // a warp's logits that wait for their weights
   };
   u64 slot[2][2];               // what this CTA gives to a reduction
   u64 warp_a[kWarps], runs[kWarps];
   u64 sel, sel_before, sel_in;
-  uint32_t sel_bin, listed, counts[kRanks], found_run;
+  uint32_t sel_bin, few_n, listed, counts[kRanks], found_run;
 };
 
 template <typename T>
@@ -426,6 +432,48 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
     __syncthreads();
     return s.sel;
   };
+  // Of the list's first n values c that at which value_of_it(c), summed from the largest order_in(c) down, reaches
+  // `target`: a histogram by bin_in (of kBins, monotone), then the values of the bin that holds it, each with the sum of
+  // those before it.  false: the bin has more than 256 of them.
+  auto pick = [&](int n, u64 target, auto bin_in, auto value_of_it, auto order_in, u64& found) {
+    __syncthreads();
+    if (tid < kBins) s.pick.hist[tid] = 0ull;
+    if (tid == 0) s.few_n = 0u;
+    __syncthreads();
+    u64 c[2], w[2];
+    int bin[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int at = tid + i * kThreads;
+      c[i] = at < n ? s.list[at] : 0ull;
+      w[i] = at < n ? value_of_it(c[i]) : 0ull;
+      bin[i] = w[i] ? bin_in(c[i]) : -1;
+      if (w[i]) atomicAdd(&s.pick.hist[bin[i]], w[i]);
+    }
+    __syncthreads();
+    u64 all;
+    const u64 in = tid < kBins ? s.pick.hist[tid] : 0ull, cum = block_scan(in, all);
+    if (cum < target && cum + in >= target) s.sel_bin = tid, s.sel_before = cum;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (bin[i] == (int)s.sel_bin) {
+        const uint32_t at = atomicAdd(&s.few_n, 1u);
+        if (at < 256u) s.pick.few[at] = c[i], s.few_weights[at] = w[i];
+      }
+    __syncthreads();
+    const int few = (int)s.few_n;
+    if (few > 256) return false;
+    if (tid < few) {
+      const u64 mine = s.pick.few[tid], order = order_in(mine);
+      u64 before = s.sel_before;
+      for (int j = 0; j < few; ++j) before += order_in(s.pick.few[j]) > order ? s.few_weights[j] : 0ull;
+      if (before < target && before + s.few_weights[tid] >= target) s.sel = mine;
+    }
+    __syncthreads();
+    found = s.sel;
+    return true;
+  };
   auto share_of = [&](u64 all) { return max(1ull, p > 0.f ? times_fraction(all, p, true) : 0ull); };   // top-p's
 
   // The token at which the sum of value_at(x, order) in the order of the index exceeds target_of(all): given
@@ -589,7 +637,8 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
         list_up(in, x, step);
       }
       const int n = bring_together();
-      if (rank == 0) {
+      // by sorting
+      auto by_sort = [&] {
         sort(n);
         const int kept = by_count ? min(k, n) : n;
         // two tokens per thread, from the first of the order on
@@ -629,6 +678,80 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
           const u64 c = s.sorted[2 * tid + (sum + w[0] <= at)];
           answer((int)(kAll - (uint32_t)(c >> 32)), value_of((uint32_t)c), total);
         }
+      };
+      // by histograms of the list
+      auto by_picks = [&] {
+        const float per = (float)kBins / to;
+        auto bin_in = [&](u64 c) { return min((int)(place_of(value_of((uint32_t)(c >> 32))) * per), kBins - 1); };
+        auto order_in = [](u64 c) { return c; };
+        u64 border = 0ull, sum[2];
+        if (by_count && !pick(n, (u64)min(k, n), bin_in, [](u64) { return 1ull; }, order_in, border)) return false;
+        auto sums = [&](u64 from) {   // this thread's weights of what stays
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const u64 c = tid + i * kThreads < n ? s.list[tid + i * kThreads] : 0ull;
+            sum[i] = c > 0ull && c >= from ? weight_at(c) : 0ull;
+          }
+          u64 all;
+          block_scan(sum[0] + sum[1], all);
+          return all;
+        };
+        if (by_weight) {
+          if (by_count) want = share_of(sums(border));
+          if (!pick(n, want, bin_in, [&](u64 c) { return c >= border ? weight_at(c) : 0ull; }, order_in, border)) return false;
+        }
+        const u64 from = max(last, border), total = sums(from);
+        const float per_index = (float)kBins / (float)a.vocab;
+        u64 c;
+        if (!pick(n, times_fraction(total, u, false) + 1ull,
+                  [&](u64 c) { return min((int)((float)(kAll - (uint32_t)c) * per_index), kBins - 1); },
+                  [&](u64 c) { return c >= from ? weight_at(c) : 0ull; }, [](u64 c) { return c << 32 | c >> 32; }, c))
+          return false;
+        if (tid == 0) answer((int)(kAll - (uint32_t)c), value_of((uint32_t)(c >> 32)), total);
+        return true;
+      };
+      // few: a thread per value goes through all of them, and knows how many and what weights come before its own
+      auto by_all = [&] {
+        u64 c = 0ull, w = 0ull;
+        if (tid < n) {
+          c = s.list[tid];
+          w = weight_at(c);
+          s.pairs[tid] = make_ulonglong2(c, w);
+        }
+        __syncthreads();
+        const bool mine = tid < n;
+        if (by_count || by_weight) {
+          int place = 0;
+          u64 cum = 0ull;
+          if (warp * 32 < n)
+            for (int j = 0; j < n; ++j) {
+              const ulonglong2 of = s.pairs[j];
+              if (of.x > c) ++place, cum += of.y;
+            }
+          const int kept = by_count ? min(k, n) : n;
+          if (mine && place == kept - 1) s.sel = c, s.sel_in = cum + w;   // the last one, and the sum of all
+          if (by_weight) {
+            __syncthreads();
+            if (by_count) want = share_of(s.sel_in);
+            if (mine && place < kept && cum < want && cum + w >= want) s.sel = c;   // (the last one again, or an earlier one)
+          }
+          __syncthreads();
+          last = max(last, s.sel);
+        }
+        u64 cum = 0ull, total = 0ull;
+        if (warp * 32 < n)
+          for (int j = 0; j < n; ++j) {
+            const ulonglong2 of = s.pairs[j];
+            if (of.x < last) continue;
+            total += of.y;
+            if ((uint32_t)of.x > (uint32_t)c) cum += of.y;   // (~index: the earlier ones are larger)
+          }
+        const u64 at = times_fraction(total, u, false);
+        if (mine && c >= last && cum <= at && at < cum + w) answer((int)(kAll - (uint32_t)c), value_of((uint32_t)(c >> 32)), total);
+      };
+      if (rank == 0) {
+        if (n <= 256) by_all();
+        else if (!by_picks()) by_sort();
       }
       barrier();   // nobody leaves while its list is read
       return;
