@@ -256,14 +256,15 @@ __device__ __forceinline__ void put_sums(float* to, const float (*acc)[NT][4], i
 constexpr int kRing = 6;   // blocks of 64 ks
 // CTAs an SM holds, by shared memory and registers
 template <int NT, bool G32>
-constexpr int kHeld = NT == 1 ? (G32 ? 2 : 3) : NT == 2 ? 2 : 1;
+constexpr int kHeld = 2;
 template <bool G32>
 struct Slot {
   uint4 codes[2][32];
   uint2 sz[G32 ? 2 : 1][2][8];
 };
 
-template <int NT, bool G32>
+// FAST: rows of x are 16-byte aligned and K a multiple of 8, so that a lane's eight values are there or not.
+template <int NT, bool G32, bool FAST>
 __global__ void __launch_bounds__(256, kHeld<NT, G32>) w4_gemm_kernel(W4Args a) {
   constexpr int kPart = NT * 8 * kPitch;
   extern __shared__ __align__(16) unsigned char few_smem[];
@@ -277,66 +278,95 @@ __global__ void __launch_bounds__(256, kHeld<NT, G32>) w4_gemm_kernel(W4Args a) 
   const int k0 = (int)((long long)w.kblocks * share / shares), k1 = (int)((long long)w.kblocks * (share + 1) / shares);
 
   // the next block of the sequence (pair by pair, the warp's blocks of each) into the next slot
-  int next_pair = blockIdx.x, next_kb = k0, next_slot = 0;
+  int next_pair = blockIdx.x, next_kb = k1, next_slot = 0;
   const int per_group = w.group == 128 ? 7 : w.group == 64 ? 6 : 5;
+  const int sz_t = lane >> 2 & 1, sz_h = lane >> 3;   // 64 bytes of scales per tile and group: 4 lanes each
+  const uint4 *from0 = nullptr, *from1 = nullptr;
+  const uint2* from_sz = nullptr;
+  if (k0 == k1) next_pair = pairs;
+  else next_pair -= (int)gridDim.x;
   auto fetch = [&] {
-    if (next_pair < pairs && k0 < k1) {
+    if (next_kb == k1 && next_pair < pairs) {
+      next_pair += (int)gridDim.x;
+      next_kb = k0;
+      const int t0 = first_tile(min(next_pair, pairs - 1), a.epi), t1 = second_tile(min(next_pair, pairs - 1), a.epi);
+      from0 = w.codes + ((size_t)t0 * w.kblocks + k0) * 32 + lane;
+      from1 = w.codes + ((size_t)t1 * w.kblocks + k0) * 32 + lane;
+      from_sz = w.sz + (size_t)(sz_t ? t1 : t0) * w.groups * 8 + q * 2;
+    }
+    if (next_pair < pairs) {
       Slot<G32>& to = ring[next_slot];
-      const int t0 = first_tile(next_pair, a.epi), t1 = second_tile(next_pair, a.epi);
-      copy_async(&to.codes[0][lane], w.codes + ((size_t)t0 * w.kblocks + next_kb) * 32 + lane, true);
-      copy_async(&to.codes[1][lane], w.codes + ((size_t)t1 * w.kblocks + next_kb) * 32 + lane, true);
-      const int t = lane >> 2 & 1, h = lane >> 3;   // 64 bytes of scales per tile and group: 4 lanes each
-      if (h < (G32 ? 2 : 1)) {
-        const int group = min((next_kb * 64 + h * 32) >> per_group, w.groups - 1);
-        copy_async(&to.sz[h][t][q * 2], w.sz + ((size_t)(t ? t1 : t0) * w.groups + group) * 8 + q * 2, true);
-      }
-      if (++next_kb == k1) next_kb = k0, next_pair += gridDim.x;
+      copy_async(&to.codes[0][lane], from0, true);
+      copy_async(&to.codes[1][lane], from1, true);
+      if (sz_h < (G32 ? 2 : 1))
+        copy_async(&to.sz[sz_h][sz_t][q * 2], from_sz + (size_t)min((next_kb * 64 + sz_h * 32) >> per_group, w.groups - 1) * 8, true);
+      from0 += 32;
+      from1 += 32;
+      ++next_kb;
       if (++next_slot == kRing) next_slot = 0;
     }
     copies_commit();
   };
   // loaded weights do not change: the first blocks are on their way before the launch before has ended
-#pragma unroll
+#pragma unroll 1
   for (int i = 0; i < kRing - 1; ++i) fetch();
   pdl_trigger();
   pdl_wait();
 
+  const bf16* rows[NT];
+  bool there[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    there[n] = m0 + n * 8 + g < a.M;
+    rows[n] = (const bf16*)a.x + (long long)min(m0 + n * 8 + g, a.M - 1) * a.lda + q * 8;
+  }
   auto load = [&](uint4 (*x)[2], int kb) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const int m = m0 + n * 8 + g;
-      const bf16* row = (const bf16*)a.x + (long long)m * a.lda;
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) x[n][h] = load_x(row, kb * 64 + h * 32 + q * 8, w.K, m < a.M, a.vec);
-    }
+      for (int h = 0; h < 2; ++h) {
+        const int k = kb * 64 + h * 32;
+        if constexpr (FAST) {
+          x[n][h] = make_uint4(0u, 0u, 0u, 0u);
+          if (there[n] && k + q * 8 < w.K) x[n][h] = *(const uint4*)(rows[n] + k);
+        } else {
+          x[n][h] = load_x(rows[n] - q * 8, k + q * 8, w.K, there[n], 0);
+        }
+      }
   };
-  constexpr bool kAheadX = NT <= 2;   // the next block's tokens on their way
-  uint4 x[NT][2];
-  if (kAheadX && k0 < k1) load(x, k0);
   int slot = 0, buf = 0;
+  float acc[2][NT][4];
+  // a block with its tokens in x, while the next one's come into xn
+  auto block = [&](int kb, uint4 (*x)[2], uint4 (*xn)[2]) {
+    copies_wait<kRing - 2>();
+    __syncwarp();
+    fetch();   // (into the slot that was read last)
+    load(xn, kb + 1 < k1 ? kb + 1 : k0);
+    Operand<G32> op;
+    op.set(ring[slot], lane, g);
+    if (++slot == kRing) slot = 0;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) op.multiply(x[n], &acc[0][n], NT);
+  };
+  uint4 xa[NT][2], xb[NT][2];
+  if (k0 < k1) load(xa, k0);
   for (int pair = blockIdx.x; pair < pairs; pair += gridDim.x, buf ^= 1) {
-    float acc[2][NT][4];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[t][n][i] = 0.f;
-    for (int kb = k0; kb < k1; ++kb) {
-      copies_wait<kRing - 2>();
-      __syncwarp();
-      fetch();   // (into the slot that was read last)
-      Operand<G32> op;
-      op.set(ring[slot], lane, g);
-      if (++slot == kRing) slot = 0;
-      uint4 xn[NT][2];
-      if (kAheadX) load(xn, kb + 1 < k1 ? kb + 1 : k0);
-      else load(x, kb);
+    int kb = k0;
+#pragma unroll 1
+    for (; kb + 1 < k1; kb += 2) {
+      block(kb, xa, xb);
+      block(kb + 1, xb, xa);
+    }
+    if (kb < k1) {
+      block(kb, xa, xb);
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        op.multiply(x[n], &acc[0][n], NT);
-        if (kAheadX) x[n][0] = xn[n][0], x[n][1] = xn[n][1];
-      }
+      for (int n = 0; n < NT; ++n) xa[n][0] = xb[n][0], xa[n][1] = xb[n][1];
     }
     float* part = parts + buf * kWarps * kPart;   // (two in turn: one barrier a pair)
     put_sums<NT>(part + warp * kPart, acc, g, q);
@@ -368,9 +398,11 @@ constexpr size_t smem_of() {
 
 template <int NT>
 cudaError_t init_nt() {
-  cudaError_t e = cudaFuncSetAttribute(w4_gemm_kernel<NT, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_of<NT, false>());
-  if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(w4_gemm_kernel<NT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_of<NT, true>());
+  auto set = [](auto kernel, size_t bytes) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); };
+  cudaError_t e = set(w4_gemm_kernel<NT, false, false>, smem_of<NT, false>());
+  if (e == cudaSuccess) e = set(w4_gemm_kernel<NT, false, true>, smem_of<NT, false>());
+  if (e == cudaSuccess) e = set(w4_gemm_kernel<NT, true, false>, smem_of<NT, true>());
+  if (e == cudaSuccess) e = set(w4_gemm_kernel<NT, true, true>, smem_of<NT, true>());
   return e;
 }
 
@@ -384,7 +416,7 @@ cudaError_t launch_few(const W4Args& a, cudaStream_t st) {
   const int held = kHeld<NT, G32> * a.num_sms;
   const int across = ranks > 1 || pairs <= held ? pairs : std::max(1, held / std::min(tiles, held));
   const Overlap overlap;
-  return launch_kernel_cluster(w4_gemm_kernel<NT, G32>, dim3(across, tiles, ranks), dim3(256), smem_of<NT, G32>(), st,
+  return launch_kernel_cluster(a.vec && a.w.K % 8 == 0 ? w4_gemm_kernel<NT, G32, true> : w4_gemm_kernel<NT, G32, false>, dim3(across, tiles, ranks), dim3(256), smem_of<NT, G32>(), st,
                                dim3(1, 1, ranks), a);
 }
 template <int NT>
