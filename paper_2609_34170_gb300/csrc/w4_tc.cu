@@ -39,7 +39,7 @@ struct TcShape {
   static constexpr int kSets = GS == 1 ? 2 : 3;          // of four warps that widen a piece (as many as have room for codes)
   static constexpr int kSumWarp = 4 * kSets, kXWarp = kSumWarp + 8, kMmaWarp = kXWarp + 1, kThreads = 32 * (kMmaWarp + 1);
   static constexpr int kGroups = 4 / GS;                 // of a piece
-  static constexpr int kAccs = (int)kTcCols / NTOK;
+  static constexpr int kSlots = (int)kTcCols / NTOK / kGroups;   // pieces whose accumulators there are
   struct Piece {
     uint8_t a[2][128 * 128], x[2][NTOK * 128];           // swizzled rows of 128 bytes
   };
@@ -53,9 +53,9 @@ struct TcShape {
       float sums[NTOK * kSumPitch];                      // for the other ranks, once every MMA is done
     };
     Codes ring[4 * kSets][kCodeRing];
-    uint32_t scale[2 * kScaleHalf][256];
+    uint32_t scale[2][256][kScaleHalf];
     float up[NTOK * kUpPitch];                           // GeGLU's up rows
-    uint64_t full[kPieces], empty[kPieces], acc_full[kAccs], acc_empty[kAccs], up_full, up_free, ended;
+    uint64_t full[kPieces], empty[kPieces], acc_full[kSlots], acc_empty[kSlots], up_full, up_free, ended;
     uint32_t tmem;
   };
 };
@@ -79,7 +79,7 @@ template <int NTOK, int GS>
 __global__ void __launch_bounds__(TcShape<NTOK, GS>::kThreads, 1) w4_tc_kernel(const __grid_constant__ CUtensorMap x_map, W4Args a) {
   typedef TcShape<NTOK, GS> Shape;
   constexpr int kSets = Shape::kSets, kSumWarp = Shape::kSumWarp, kXWarp = Shape::kXWarp, kMmaWarp = Shape::kMmaWarp;
-  constexpr int kGroups = Shape::kGroups, kAccs = Shape::kAccs;
+  constexpr int kGroups = Shape::kGroups, kSlots = Shape::kSlots;
   extern __shared__ __align__(1024) unsigned char tc_smem[];
   typename Shape::Shared& s = *(typename Shape::Shared*)tc_smem;
   const W4Matrix& w = a.w;
@@ -134,7 +134,7 @@ __global__ void __launch_bounds__(TcShape<NTOK, GS>::kThreads, 1) w4_tc_kernel(c
   const int srow = quarter * 32 + lane, sthread = (tid - 32 * kSumWarp) & 255;
   const int group0 = p0 * kGroups, groups_here = pieces_here * kGroups;
   int scale_unit = blockIdx.x, scale_at = 0;
-  const uint32_t scale_to = smem_u32(&s.scale[0][sthread]);
+  const uint32_t scale_to = smem_u32(&s.scale[0][sthread][0]);
   // half of the ring: the next kScaleHalf groups of the unit (past the last one there are no values, and its
   // scale will do: every unit takes whole halves)
   auto fetch_scales = [&](int half) {
@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(TcShape<NTOK, GS>::kThreads, 1) w4_tc_kernel(c
       const uint32_t* from = (const uint32_t*)w.sz + ((size_t)tile * w.groups * 8 + (srow & 7)) * 2 + (srow >> 3 & 1);
 #pragma unroll
       for (int i = 0; i < kScaleHalf; ++i)
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(scale_to + (half * kScaleHalf + i) * 1024),
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(scale_to + half * (256 * kScaleHalf * 4) + i * 4),
                      "l"(from + 16 * (size_t)min(group0 + scale_at + i, w.groups - 1))
                      : "memory");
       scale_at += kScaleHalf;
@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(TcShape<NTOK, GS>::kThreads, 1) w4_tc_kernel(c
       mbar_init(&s.full[i], 5);   // four warps that widen, and the tokens' bytes
       mbar_init(&s.empty[i], 1);
     }
-    for (int i = 0; i < kAccs; ++i) {
+    for (int i = 0; i < kSlots; ++i) {
       mbar_init(&s.acc_full[i], 1);
       mbar_init(&s.acc_empty[i], 8);
     }
@@ -241,28 +241,36 @@ __global__ void __launch_bounds__(TcShape<NTOK, GS>::kThreads, 1) w4_tc_kernel(c
       float sum[kTok];
 #pragma unroll
       for (int i = 0; i < kTok; ++i) sum[i] = 0.f;
-      for (int group = 0; group < groups_here; ++group) {
-        if (group % kScaleHalf == 0) copies_wait<1>();
-        const float scale = __uint_as_float(s.scale[half * kScaleHalf + group % kScaleHalf][sthread] & 0xffff0000u);
-        if (group % kScaleHalf == kScaleHalf - 1 || group + 1 == groups_here) {   // (this half is read)
+      for (int piece = 0; piece < pieces_here; ++piece) {
+        const int in_half = piece * kGroups % kScaleHalf;
+        if (in_half == 0) copies_wait<1>();
+        float scale[kGroups];
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i) scale[i] = __uint_as_float(s.scale[half][sthread][in_half + i] & 0xffff0000u);
+        if (in_half + kGroups == kScaleHalf || piece + 1 == pieces_here) {   // (this half is read)
           fetch_scales(half);
           half ^= 1;
         }
         ok = wait_for(&s.acc_full[acc_at], parity);
         if (!ok) break;
         tc_fence_after();
-        uint32_t v[kTok / 16][16];
 #pragma unroll
-        for (int i = 0; i < kTok / 16; ++i) tmem_ld16_async(tmem + lanes + acc_at * NTOK + first + i * 16, v[i]);
-        tmem_wait_ld();
+        for (int group = 0; group < kGroups; ++group) {
+          uint32_t v[kTok / 16][16];
 #pragma unroll
-        for (int i = 0; i < kTok / 16; ++i) tmem_reg_fence16(v[i]);
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&s.acc_empty[acc_at]);
-        if (++acc_at == kAccs) acc_at = 0, parity ^= 1u;
+          for (int i = 0; i < kTok / 16; ++i) tmem_ld16_async(tmem + lanes + (acc_at * kGroups + group) * NTOK + first + i * 16, v[i]);
+          tmem_wait_ld();
 #pragma unroll
-        for (int i = 0; i < kTok; i += 2) fma_pair(sum[i], sum[i + 1], v[i / 16][i % 16], v[i / 16][i % 16 + 1], scale);
+          for (int i = 0; i < kTok / 16; ++i) tmem_reg_fence16(v[i]);
+          if (group == kGroups - 1) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&s.acc_empty[acc_at]);
+          }
+#pragma unroll
+          for (int i = 0; i < kTok; i += 2) fma_pair(sum[i], sum[i + 1], v[i / 16][i % 16], v[i / 16][i % 16 + 1], scale[group]);
+        }
+        if (++acc_at == kSlots) acc_at = 0, parity ^= 1u;
       }
       if (!ok) break;
       if (ranks > 1) {   // (the only unit, and its last MMA is done: the pieces are free)
@@ -335,26 +343,21 @@ __global__ void __launch_bounds__(TcShape<NTOK, GS>::kThreads, 1) w4_tc_kernel(c
     for (long long left = (long long)mine * pieces_here; left > 0; --left) {
       ok = wait_for(&s.full[at], parity);
       if (!ok) break;
-#pragma unroll
-      for (int i = 0; i < kGroups; ++i) {   // (the accumulators are a multiple of a piece's groups)
-        ok = wait_for(&s.acc_empty[acc_at + i], acc_parity);
-        if (!ok) break;
-      }
+      ok = wait_for(&s.acc_empty[acc_at], acc_parity);
       if (!ok) break;
       tc_fence_after();
       const uint32_t ahead = (uint32_t)(at * (sizeof(typename Shape::Piece) >> 4));
       const uint64_t ad = ad0 + ahead, xd = xd0 + ahead;
-      const uint32_t td = tmem + acc_at * NTOK;
+      const uint32_t td = tmem + acc_at * kGroups * NTOK;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {   // 16 ks each
         const int group = j / (2 * GS);
         umma_bf16(td + group * NTOK, ad + (j / 4) * (128 * 128 >> 4) + 2 * (j % 4), xd + (j / 4) * (NTOK * 128 >> 4) + 2 * (j % 4), idesc,
                   j % (2 * GS) > 0 ? 1u : 0u, el);
-        if (j % (2 * GS) == 2 * GS - 1) umma_commit(&s.acc_full[acc_at + group], el);
       }
+      umma_commit(&s.acc_full[acc_at], el);
       umma_commit(&s.empty[at], el);
-      acc_at += kGroups;
-      if (acc_at == kAccs) acc_at = 0, acc_parity ^= 1u;
+      if (++acc_at == kSlots) acc_at = 0, acc_parity ^= 1u;
       if (++at == kPieces) at = 0, parity ^= 1u;
     }
     umma_commit(&s.ended, el);   // nothing is in flight when the columns are given back
