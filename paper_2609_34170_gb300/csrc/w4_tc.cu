@@ -16,8 +16,8 @@ namespace ravel {
 namespace {
 
 // A CTA takes 128 rows of weights, the MMAs' M, and NTOK tokens, their N.  Per piece of 128 ks:
-//   four of the warps that widen do so: a thread takes a row's 128 codes out of a ring of its warp (asynchronous
-//     copies), makes them c - z in bf16 and stores them as the row's part of A, two swizzled tiles of 64 ks;
+//   four of the warps that widen do so: a thread takes half of the codes of two rows out of a ring of its warp
+//     (asynchronous copies), makes them c - z in bf16 and stores them into A, two swizzled tiles of 64 ks;
 //   one warp loads the tokens' values by TMA, two tiles of B;
 //   one warp issues the MMAs.  A group's products are summed into an accumulator of their own, in turn;
 //   eight warps take the accumulators, scale them by the group's scale and add them up in fp32 registers, half
@@ -39,7 +39,11 @@ struct TcShape {
   static constexpr int kSets = GS == 1 ? 2 : 3;          // of four warps that widen a piece (as many as have room for codes)
   static constexpr int kSumWarp = 4 * kSets, kXWarp = kSumWarp + 8, kMmaWarp = kXWarp + 1, kThreads = 32 * (kMmaWarp + 1);
   static constexpr int kGroups = 4 / GS;                 // of a piece
-  static constexpr int kSlots = (int)kTcCols / NTOK / kGroups;   // pieces whose accumulators there are
+  // pieces whose accumulators there are; where they are as many as the pieces in the making, one barrier says of a
+  // piece that its operands are free and its accumulators full (who waits for it is never a round behind: a piece is made,
+  // and its accumulators written, only when both waits for the one three before have ended)
+  static constexpr bool kOne = (int)kTcCols / NTOK / kGroups >= kPieces;
+  static constexpr int kSlots = kOne ? kPieces : (int)kTcCols / NTOK / kGroups;
   struct Piece {
     uint8_t a[2][128 * 128], x[2][NTOK * 128];           // swizzled rows of 128 bytes
   };
@@ -135,16 +139,20 @@ __global__ void __launch_bounds__(TcShape<NTOK, GS>::kThreads, 1) w4_tc_kernel(c
   const int group0 = p0 * kGroups, groups_here = pieces_here * kGroups;
   int scale_unit = blockIdx.x, scale_at = 0;
   const uint32_t scale_to = smem_u32(&s.scale[0][sthread][0]);
+  const uint32_t* from_scale = nullptr;   // of the unit's first group
   // half of the ring: the next kScaleHalf groups of the unit (past the last one there are no values, and its
   // scale will do: every unit takes whole halves)
   auto fetch_scales = [&](int half) {
     if (scale_unit < units) {
-      const int tile = min(scale_unit % row_tiles * 8 + (srow >> 4), w.tiles - 1);
-      const uint32_t* from = (const uint32_t*)w.sz + ((size_t)tile * w.groups * 8 + (srow & 7)) * 2 + (srow >> 3 & 1);
+      if (scale_at == 0) {
+        const int tile = min(scale_unit % row_tiles * 8 + (srow >> 4), w.tiles - 1);
+        from_scale = (const uint32_t*)w.sz + ((size_t)tile * w.groups * 8 + (srow & 7)) * 2 + (srow >> 3 & 1);
+      }
+      const int at = group0 + scale_at, most = w.groups - 1;
 #pragma unroll
       for (int i = 0; i < kScaleHalf; ++i)
         asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(scale_to + half * (256 * kScaleHalf * 4) + i * 4),
-                     "l"(from + 16 * (size_t)min(group0 + scale_at + i, w.groups - 1))
+                     "l"(from_scale + 16 * (size_t)(uint32_t)min(at + i, most))
                      : "memory");
       scale_at += kScaleHalf;
       if (scale_at >= groups_here) scale_at = 0, scale_unit += gridDim.x;
@@ -199,27 +207,40 @@ __global__ void __launch_bounds__(TcShape<NTOK, GS>::kThreads, 1) w4_tc_kernel(c
       typename Shape::Piece& to = s.pieces[at];
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        uint32_t z[2];
+        uint32_t z0[2], z8[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) z[h] = __byte_perm(((const uint32_t*)&from.sz[(2 * half + h) / GS][t][g])[hi], 0u, 0x1010);
-        uint4 c[4];
+        for (int h = 0; h < 2; ++h) {
+          const uint2 sz = from.sz[(2 * half + h) / GS][t][g];
+          z0[h] = __byte_perm(sz.x, 0u, 0x1010);
+          z8[h] = __byte_perm(sz.y, 0u, 0x1010);
+        }
+        uint4 c[2];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) c[q] = from.codes[half][t][g * 4 + (q ^ (g >> 1))];
+        for (int i = 0; i < 2; ++i) c[i] = from.codes[half][t][g * 4 + ((2 * hi + i) ^ (g >> 1))];
         if (half == 0) {
           ok = wait_for(&s.empty[at], parity);
           if (!ok) break;
         }
-        uint8_t* row = to.a[half] + srow * 128;
-        // word 2h + s of part q: ks 32h + 8q + 4s ..; the row's 16 bytes 4h + q change places with the row
+        // word 2h + s of part q: ks 32h + 8q + 4s .., nibbles 0, 2 of row g and 1, 3 of row g + 8; a row's 16 bytes 4h + q
+        // change places with the row (by the same for both)
+        uint8_t* row = to.a[half] + (quarter * 32 + t * 16 + g) * 128;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const uint32_t word[4] = {c[q].x, c[q].y, c[q].z, c[q].w};
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t word[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const uint32_t v0 = word[2 * h] >> 4 * hi, v1 = word[2 * h + 1] >> 4 * hi;
-            *(uint4*)(row + (((4 * h + q) ^ (srow & 7)) << 4)) =
-                make_uint4(sub_bf16x2((v0 & 0x000f000fu) | 0x43004300u, z[h]), sub_bf16x2((v0 >> 8 & 0x000f000fu) | 0x43004300u, z[h]),
-                           sub_bf16x2((v1 & 0x000f000fu) | 0x43004300u, z[h]), sub_bf16x2((v1 >> 8 & 0x000f000fu) | 0x43004300u, z[h]));
+            uint32_t r0[4], r8[4];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const uint32_t v = word[2 * h + e];
+              r0[2 * e] = sub_bf16x2((v & 0x000f000fu) | 0x43004300u, z0[h]);
+              r8[2 * e] = sub_bf16x2((v >> 4 & 0x000f000fu) | 0x43004300u, z8[h]);
+              r0[2 * e + 1] = sub_bf16x2((v >> 8 & 0x000f000fu) | 0x43004300u, z0[h]);
+              r8[2 * e + 1] = sub_bf16x2((v >> 12 & 0x000f000fu) | 0x43004300u, z8[h]);
+            }
+            uint8_t* piece = row + (((4 * h + 2 * hi + i) ^ g) << 4);
+            *(uint4*)piece = make_uint4(r0[0], r0[1], r0[2], r0[3]);
+            *(uint4*)(piece + 8 * 128) = make_uint4(r8[0], r8[1], r8[2], r8[3]);
           }
         }
       }
@@ -251,7 +272,7 @@ __global__ void __launch_bounds__(TcShape<NTOK, GS>::kThreads, 1) w4_tc_kernel(c
           fetch_scales(half);
           half ^= 1;
         }
-        ok = wait_for(&s.acc_full[acc_at], parity);
+        ok = wait_for(Shape::kOne ? &s.empty[acc_at] : &s.acc_full[acc_at], parity);
         if (!ok) break;
         tc_fence_after();
 #pragma unroll
@@ -355,7 +376,7 @@ __global__ void __launch_bounds__(TcShape<NTOK, GS>::kThreads, 1) w4_tc_kernel(c
         umma_bf16(td + group * NTOK, ad + (j / 4) * (128 * 128 >> 4) + 2 * (j % 4), xd + (j / 4) * (NTOK * 128 >> 4) + 2 * (j % 4), idesc,
                   j % (2 * GS) > 0 ? 1u : 0u, el);
       }
-      umma_commit(&s.acc_full[acc_at], el);
+      if (!Shape::kOne) umma_commit(&s.acc_full[acc_at], el);
       umma_commit(&s.empty[at], el);
       if (++acc_at == kSlots) acc_at = 0, acc_parity ^= 1u;
       if (++at == kPieces) at = 0, parity ^= 1u;
