@@ -437,7 +437,14 @@ cudaError_t init_w4_kernels() {
 
 cudaError_t launch_w4_gemm(const W4Args& a, cudaStream_t st) {
   if (a.M <= 8) return launch_nt<1>(a, st);
-  return a.M <= 16 || !a.vec ? launch_nt<2>(a, st) : launch_w4_tc(a, st);   // (TMA takes aligned rows only)
+  // More than 16 rows: tiles of 16 go through the matrix each, from L2 after the first, and win while that is little
+  // work, the tcgen05 kernel (an SM a CTA, with a longer start) from there on.  us, tiles / tcgen05, groups of 128: 64 rows x
+  // 2560 x 1024 5.9 / 8.8; 64 x 4096 x 1024 7.0 / 9.3, 96 x 4096 x 1024 10.4 / 9.1; 32 x 8192 x 1024 7.1 / 7.9, 48 rows
+  // 10.3 / 9.0; 32 x 4096 x 4096 8.8 / 9.9, 48 rows 13.6 / 11.0; 17 x 4096 x 8192 15.6 / 12.5; 64 x 2048 x 4096 8.8 / 14.3.
+  // (TMA takes aligned rows only.)
+  const long long tiles = (a.M + 15) / 16;
+  const bool little = a.w.tiles / 2 * tiles * 3 <= 10 * a.num_sms && (long long)a.w.N * a.w.K * tiles <= 36ll << 20;
+  return a.M <= 16 || !a.vec || little ? launch_nt<2>(a, st) : launch_w4_tc(a, st);
 }
 
 cudaError_t launch_w4_load(const W4Matrix& w, const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, cudaStream_t st) {

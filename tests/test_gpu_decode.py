@@ -292,25 +292,26 @@ def test_products(n, k, group):
 
 
 @pytest.mark.parametrize("group", [32, 64, 128])
-@pytest.mark.parametrize("n,k", [(4113, 70), (5000, 1003), (4097, 2056), (9000, 512)])
+@pytest.mark.parametrize("n,k", [(4113, 70), (5000, 1003), (4097, 2056), (9000, 512), (17000, 1000), (700, 20000)])
 def test_products_of_many_rows_of_weights(n, k, group):
     """Where pairs of tiles share the tokens' values: ends inside a tile, a stage, a group and a cluster's share."""
     w, held = _held(n, k, group, n)
-    flat = _rand((70 * 2070,), 1, "bf16")
-    for m, lda, offset in ((17, k, 0), (32, k + 1, 0), (33, -(-k // 8) * 8, 0), (64, -(-k // 8) * 8 + 8, 8), (70, k, 1)):
+    flat = _rand((130 * (k + 16),), 1, "bf16")
+    up = -(-k // 8) * 8
+    for m, lda, offset in ((17, up, 0), (32, k + 1, 0), (33, up, 0), (64, up + 8, 8), (70, k, 1), (129, up, 16)):
         x = flat[offset:].as_strided((m, k), (lda, 1))
         bias = _rand((n,), 3)
         _product_close(_np(w.product(x, dtype=torch.float32, bias=bias)), _np(x), held, "store", "fp32", _np(bias))
-    before = _rand((70, n), 2)
+    before = _rand((129, n), 2)
     _product_close(_np(w.product(x, out=before.clone(), epi="add")), _np(x), held, "add", "fp32", None, _np(before))
 
 
 @pytest.mark.parametrize("group", [32, 128])
-@pytest.mark.parametrize("n,k", [(128, 64), (384, 333), (8192, 1024), (4224, 1500)])
+@pytest.mark.parametrize("n,k", [(128, 64), (384, 333), (8192, 1024), (4224, 1500), (16384, 1096)])
 def test_geglu_products(n, k, group):
     w, held = _held(n, k, group, n)
     bias = _rand((n,), 4)
-    for m in (1, 4, 12, 50, 70):
+    for m in (1, 4, 12, 32, 50, 72, 200):
         x = _rand((m, k), m, "bf16")
         _product_close(_np(w.product(x, epi="geglu")), _np(x), held, "geglu", "bf16")
         _product_close(_np(w.product(x, epi="geglu", bias=bias)), _np(x), held, "geglu", "bf16", _np(bias))
