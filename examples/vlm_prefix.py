@@ -5,6 +5,11 @@ the attention mass that its tokens drew, and what stays becomes the context of
 the rolling step.
 
     python examples/vlm_prefix.py [--robots 4] [--prompt 200] [--decode 8] [--keep 96]
+                                  [--rotary] [--four-bit] [--temperature 0.8]
+
+--rotary turns queries and keys to their positions, --four-bit holds the decoder's
+matrices in 4-bit codes (decoded tokens' products read those; the prompt's take the values that the
+codes stand for), and a temperature draws tokens among the likeliest 40 in the place of the first.
 
 The decoder's attention shape is the expert's (its layers, heads and head dim),
 as the expert reads the VLM's keys and values layer by layer."""
@@ -18,14 +23,14 @@ import torch
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
 import synth  # noqa: E402
-from paper_2609_34170_gb300 import ContextCache, RollingSession  # noqa: E402
+from paper_2609_34170_gb300 import ContextCache, RollingSession, Rotary, Weights4, draw_tokens  # noqa: E402
 
 
 class Decoder:
-    """Pre-norm attention and MLP layers, weights ~ N(0, 1 / fan-in); rotary
-    positions are left out: the cache holds whatever keys it is given."""
+    """Pre-norm attention and MLP layers, weights ~ N(0, 1 / fan-in), without rotary
+    positions (the cache holds whatever keys it is given) or with them."""
 
-    def __init__(self, layers, width, hq, hkv, hd, vocab, seed=0):
+    def __init__(self, layers, width, hq, hkv, hd, vocab, seed=0, rotary=False, four_bit=False):
         g = torch.Generator("cuda").manual_seed(seed)
         self.hq, self.hkv, self.hd = hq, hkv, hd
 
@@ -35,6 +40,19 @@ class Decoder:
         self.embed = w(vocab, width) * math.sqrt(vocab)
         self.layers = [dict(qkv=w(width, (hq + 2 * hkv) * hd), o=w(hq * hd, width), up=w(width, 2 * width), down=w(2 * width, width))
                        for _ in range(layers)]
+        self.rotary = Rotary(hd) if rotary else None
+        if four_bit:
+            self.layers = [{name: Weights4.quantize(m.t().contiguous(), 64) for name, m in layer.items()} for layer in self.layers]
+            self.values = [{name: m.read().t() for name, m in layer.items()} for layer in self.layers]
+
+    def times(self, x, layer, name):
+        """x [B, n, k] times a matrix of a layer."""
+        w = self.layers[layer][name]
+        if not isinstance(w, Weights4):
+            return x @ w
+        if x.shape[0] * x.shape[1] > 64:   # a prompt: the values once for all rows
+            return x @ self.values[layer][name]
+        return w.product(x.flatten(0, 1)).unflatten(0, x.shape[:2])
 
     @staticmethod
     def norm(x):
@@ -46,14 +64,17 @@ class Decoder:
         l's attention mass."""
         x = self.embed[tokens]
         lengths = starts + counts
-        for index, w in enumerate(self.layers):
-            qkv = (self.norm(x) @ w["qkv"]).unflatten(-1, (self.hq + 2 * self.hkv, self.hd))
+        for index in range(len(self.layers)):
+            qkv = self.times(self.norm(x), index, "qkv").unflatten(-1, (self.hq + 2 * self.hkv, self.hd))
             # columns of one projection, as they are
             q, k, v = qkv[:, :, :self.hq], qkv[:, :, self.hq:self.hq + self.hkv], qkv[:, :, self.hq + self.hkv:]
-            cache.append(index, k, v, starts, counts)
+            if self.rotary is None:
+                cache.append(index, k, v, starts, counts)
+            else:
+                cache.append_rotary(index, self.rotary, q, k, v, starts, counts, q_out=q)
             att = cache.attend(index, q, lengths, counts, causal=causal, mass=mass[index], add_mass=True)
-            x = x + att.flatten(2) @ w["o"]
-            x = x + torch.nn.functional.silu(self.norm(x) @ w["up"]) @ w["down"]
+            x = x + self.times(att.flatten(2), index, "o")
+            x = x + self.times(torch.nn.functional.silu(self.times(self.norm(x), index, "up")), index, "down")
         last = (counts - 1).clamp(min=0).long()
         return self.norm(x[torch.arange(len(x), device=x.device), last]) @ self.embed.t()
 
@@ -62,11 +83,15 @@ def main(argv=None):
     p = argparse.ArgumentParser()
     for name, value in (("robots", 4), ("prompt", 200), ("decode", 8), ("keep", 96), ("layers", 4), ("width", 256)):
         p.add_argument("--" + name, type=int, default=value)
+    p.add_argument("--rotary", action="store_true")
+    p.add_argument("--four-bit", action="store_true")
+    p.add_argument("--temperature", type=float, default=0.0)
     a = p.parse_args(argv)
     cfg = synth.ExpertConfig(layers=a.layers, width=a.width, n_q_heads=8, n_kv_heads=1, head_dim=64, mlp_dim=4 * a.width, slots=10,
                              action_dim=7, prefix=a.keep, fop_tokens=0, batch=a.robots, dtype="bf16")
     room = a.prompt + a.decode
-    model = Decoder(cfg.layers, cfg.width, cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim, vocab=512)
+    model = Decoder(cfg.layers, cfg.width, cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim, vocab=512, rotary=a.rotary,
+                    four_bit=a.four_bit)
     shape = dict(layers=cfg.layers, n_q_heads=cfg.n_q_heads, n_kv_heads=cfg.n_kv_heads, head_dim=cfg.head_dim, max_batch=a.robots)
     cache = ContextCache(**shape, max_tokens=room, max_queries=a.prompt)
     small = ContextCache(**shape, max_tokens=a.keep)
@@ -77,13 +102,22 @@ def main(argv=None):
     tokens = torch.randint(0, 512, (a.robots, a.prompt), generator=g, device="cuda")
     counts = torch.tensor([a.prompt - 7 * b % (a.prompt // 2) for b in range(a.robots)], dtype=torch.int32, device="cuda")
     starts = torch.zeros_like(counts)
-    nxt = model.run(cache, tokens, starts, counts, causal=False, mass=mass).argmax(-1)
+    random = torch.Generator("cuda").manual_seed(2)
+    temperature, most = torch.full((a.robots,), a.temperature, device="cuda"), torch.full_like(counts, 40)
+
+    def next_token(logits):
+        if not a.temperature:
+            return logits.argmax(-1)
+        u = torch.rand((a.robots,), generator=random, device="cuda")
+        return draw_tokens(logits, u, temperature=temperature, top_k=most).long()
+
+    nxt = next_token(model.run(cache, tokens, starts, counts, causal=False, mass=mass))
     # decoded tokens see what came before them
     lengths, one = counts.clone(), torch.ones_like(counts)
     said = []
     for _ in range(a.decode):
         said.append(nxt)
-        nxt = model.run(cache, nxt[:, None], lengths, one, causal=True, mass=mass).argmax(-1)
+        nxt = next_token(model.run(cache, nxt[:, None], lengths, one, causal=True, mass=mass))
         lengths += one
 
     # the prefix down to its budget, layer by layer, and into the expert's context

@@ -129,7 +129,7 @@ ravel_status ravel_w4_read(ravel_w4_t* w, void* out, int ldo, int dtype, void* s
  *   out  device [M, ldo], out_dtype RAVEL_FP32 or RAVEL_BF16; bias device float32 [N] or NULL
  * Codes are multiplied as whole numbers and sums kept in fp32, so that the result is that of the
  * weights held, not of weights rounded to bf16.  Meant for few rows, where the weights' bytes are
- * what a product costs; any M works, in tiles of 64 rows that each read the matrix.
+ * what a product costs; M up to 2^19 works, in tiles of 16 to 64 rows that each go through the matrix.
  * out must not overlap X. */
 ravel_status ravel_w4_gemm(const ravel_w4_t* w, const void* X, int M, int lda, int epi, void* out, int ldo, int out_dtype,
                            const float* bias, void* stream);

@@ -294,8 +294,8 @@ ravel_status ravel_w4_gemm(const ravel_w4_t* w, const void* X, int M, int lda, i
   if (epi == EPI_ADD_F32 && out_dtype != RAVEL_FP32) return fail(RAVEL_EINVAL, "w4_gemm: epilogue 2 adds to float32");
   if (epi == EPI_GEGLU && (w->m.N % 128 || out_dtype != RAVEL_BF16))
     return fail(RAVEL_EINVAL, "w4_gemm: epilogue 3 takes N % 128 == 0 and a bf16 out");
-  if (M < 0 || M > (1 << 20) || lda < w->m.K || ldo < (epi == EPI_GEGLU ? w->m.N / 2 : w->m.N))
-    return fail(RAVEL_ESHAPE, "w4_gemm: M outside [0, 2^20], lda below K or ldo below the outputs");
+  if (M < 0 || M > (1 << 19) || lda < w->m.K || ldo < (epi == EPI_GEGLU ? w->m.N / 2 : w->m.N))
+    return fail(RAVEL_ESHAPE, "w4_gemm: M outside [0, 2^19], lda below K or ldo below the outputs");
   if ((uintptr_t)X % 2 || (uintptr_t)out % size_of(out_dtype)) return fail(RAVEL_EINVAL, "w4_gemm: unaligned X or out");
   if (M == 0) return RAVEL_OK;
   if (!X || !out) return fail(RAVEL_EINVAL, "w4_gemm: null argument");

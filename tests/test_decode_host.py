@@ -91,6 +91,7 @@ def test_null_arguments_are_refused(lib):
     assert lib.ravel_w4_load(n, n, n, n, n) == 1
     assert lib.ravel_w4_quantize(n, 1, 1, 1, 0, 32, n, n, n, n) == 1
     assert lib.ravel_w4_read(n, n, 1, 0, n) == 1
+    assert lib.ravel_w4_reset(n) == 1
     assert lib.ravel_w4_gemm(n, n, 1, 1, 0, n, 1, 0, n, n) == 1
     assert lib.ravel_draw_tokens(n, 1, 1, 1, 0, n, n, n, n, n, n, n, n) == 1
     assert b"draw_tokens" in lib.ravel_decode_last_error()
@@ -231,8 +232,22 @@ def test_kernels_that_overlap_their_predecessors_read_nothing_as_constant():
     import os
 
     from paper_2609_34170_gb300.build import CSRC
-    for name in ("rotary.cu", "rotary.cuh", "w4.cu", "draw.cu"):
+    for name in ("rotary.cu", "rotary.cuh", "w4.cu", "w4.cuh", "w4_tc.cu", "draw.cu"):
         with open(os.path.join(CSRC, name)) as f:
             text = f.read()
         for word in ("__ldg(", "__ldcg(", "__ldcs(", "__ldca(", "ld.global.nc", "__restrict__"):
             assert word not in text, (name, word)
+
+
+def test_waits_of_the_tensor_core_kernel_are_bounded():
+    """Every wait goes through the helper that tries and then looks at the clock."""
+    import os
+    import re
+
+    from paper_2609_34170_gb300.build import CSRC
+    with open(os.path.join(CSRC, "w4_tc.cu")) as f:
+        text = f.read()
+    helper = text[text.index("bool wait_for("):text.index("template <int NTOK, int GS>\n__global__")]
+    rest = text.replace(helper, "")
+    assert "mbar_wait_warp" in helper and "wait_for(" in rest
+    assert not re.search(r"mbar_(try_|test_)?wait", rest) and "while (!" not in rest and "bar.sync" not in rest

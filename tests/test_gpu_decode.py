@@ -417,7 +417,7 @@ def test_draws_under_every_mix_of_limits(vocab, dtype):
             _draws(x, u, t, k, p, q)
 
 
-@pytest.mark.parametrize("vocab", [64, 40000])
+@pytest.mark.parametrize("vocab", [64, 1500, 40000])
 def test_draws_among_ties_by_index(vocab):
     """Equal logits: sums of equal weights, limits in the middle of them."""
     u = np.array([0.0, 0.25, 0.5, 0.999, 0.3, 0.8])
@@ -429,6 +429,18 @@ def test_draws_among_ties_by_index(vocab):
         _draws(steps, u, p=p, k=k)
     signs = torch.where(torch.arange(vocab, device="cuda")[None] % 2 == 0, 0.0, -0.0).repeat(6, 1)   # -0 is 0
     _draws(signs, u, k=[vocab // 2] * 6)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("vocab,spread", [(20000, 3.0), (20000, 0.01), (100003, 1.0), (1 << 20, 2.0)])
+def test_draws_where_more_stays_than_a_list_holds(vocab, spread, dtype):
+    """Limits of thousands of tokens, alone and together, and rows so flat that one bin of the order holds thousands."""
+    mixes = [(1.0, 3000, 1.0, 0.0), (1.0, 3000, 0.9, 0.0), (1.0, 3000, 1.0, 0.001), (0.9, 9000, 0.999, 1e-5), (1.0, 0, 0.97, 0.0),
+             (1.0, 0, 0.97, 0.01), (1.0, 2047, 0.5, 0.0), (1.0, 2048, 1.0, 0.0), (3.0, 2049, 0.7, 0.0), (1.0, 0, 0.999999, 0.0)]
+    x = _rand((len(mixes), vocab), vocab, dtype, spread)
+    t, k, p, q = zip(*mixes)
+    for seed in range(3):
+        _draws(x, np.random.default_rng(seed).random(len(mixes), dtype=np.float32), t, k, p, q)
 
 
 def test_masks_and_rows_that_cannot_be_drawn_from():
@@ -570,6 +582,49 @@ def test_replayed_and_chained_steps_equal_eager_ones():
 
     eager = run(False)
     assert torch.equal(eager, run(False)) and torch.equal(eager, run(True))
+
+
+FIRST_CALLS = """
+import sys; sys.path.insert(0, sys.argv[1])
+import torch
+from paper_2609_34170_gb300 import Rotary, Weights4, draw_tokens
+w, r = Weights4(4200, 512, 64), Rotary(32)
+x = torch.randn((40, 512), device="cuda").to(torch.bfloat16)
+u, starts = torch.full((40,), 0.5, device="cuda"), torch.arange(40, dtype=torch.int32, device="cuda")
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    got = w.product(x), r.apply(x.view(40, 1, 16, 32), starts=starts), draw_tokens(x, u), w.product(x[:5]), draw_tokens(x.float(), u)
+graph.replay()
+torch.cuda.synchronize()
+again = w.product(x), r.apply(x.view(40, 1, 16, 32), starts=starts), draw_tokens(x, u), w.product(x[:5]), draw_tokens(x.float(), u)
+assert all(torch.equal(a, b) for a, b in zip(got, again))
+print("the same")
+"""
+
+
+def test_first_calls_may_be_captured():
+    """In a process of its own, where nothing has run before the capture."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", FIRST_CALLS, root], capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0 and "the same" in done.stdout, done.stderr[-2000:]
+
+
+def test_a_matrix_can_be_reset_and_loaded_again():
+    from paper_2609_34170_gb300 import Weights4
+    x = _rand((3, 96), 0, "bf16")
+    w = Weights4(40, 96, 32)
+    for seed in (1, 2):
+        codes, scales, zeros = _weights(40, 96, 32, seed)
+        w.load(torch.from_numpy(ref.pack(codes)).cuda(), torch.from_numpy(scales).to(torch.bfloat16).cuda(), torch.from_numpy(zeros).cuda())
+        w.reset()
+        _product_close(_np(w.product(x, dtype=torch.float32)), _np(x), ref.weights(ref.pack(codes), scales, zeros, 96, 32), "store", "fp32")
+    w.close()
+    with pytest.raises(ValueError):
+        w.product(x)
 
 
 def test_two_streams_share_weights_and_a_table():
