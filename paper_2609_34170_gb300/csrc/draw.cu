@@ -267,22 +267,26 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
     return __shfl_sync(kAll, ws - w, warp) + upto - x;
   };
 
-  // the first of the order, the least finite logit, and what is no number
-  u64 best = 0, low = 0;
-#pragma unroll 2
+  // the largest logit, the least finite one, and what is no number: +inf and NaN are the largest as signed words, or, with
+  // the sign set, the largest as unsigned ones
+  float most = -inf, least = inf;
+  int words = 0;
+  uint32_t uwords = 0u;
+#pragma unroll 4
   for (int step = step0; step < step1; ++step) {
     float x[V];
     load(step, x);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const u64 c = order_of(x[j], index_of(step, j));
-      best = c > best ? c : best;
-      if (!(x[j] < inf)) low |= 1ull << 32;
-      else if (x[j] > -inf) low = (low & 1ull << 32) | max((uint32_t)low, ~(uint32_t)(c >> 32));
+      most = fmaxf(most, x[j]);
+      least = fminf(least, x[j] == -inf ? inf : x[j]);
+      words = max(words, __float_as_int(x[j]));
+      uwords = max(uwords, __float_as_uint(x[j]));
     }
   }
+  u64 best = key_of(most), low = words >= 0x7f800000 || uwords > 0xff800000u ? 1ull << 32 : (u64)~key_of(least);
   reduce_max(best, low);
-  const float top = value_of((uint32_t)(best >> 32));
+  const float top = value_of((uint32_t)best);
   const Weigher weigh(top, t);
   // log of the share of a token of logit x: x's part in the log2 domain and the sum's, in two floats
   auto answer = [&](int token, float x, u64 total) {
@@ -296,8 +300,19 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
   };
   const bool none = low >> 32 || !(top > -inf) || !(u >= 0.f && u < 1.f) || !(t < inf) || p != p || mp != mp;
   if (none || t < 0x1p-20f) {
+    // (the first of the largest)
+    u64 first = 0ull, ignored = 0ull;
+    if (!none)
+      for (int step = step0; step < step1; ++step) {
+        float x[V];
+        load(step, x);
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+          if (x[j] == top) first = max(first, (u64)(kAll - (uint32_t)index_of(step, j)));
+      }
+    reduce_max(first, ignored);
     if (rank == 0 && tid == 0) {
-      a.tokens[b] = none ? -1 : (int)(kAll - (uint32_t)best);
+      a.tokens[b] = none ? -1 : (int)(kAll - (uint32_t)first);
       if (a.log_probs) a.log_probs[b] = none ? -inf : 0.f;
     }
     barrier();   // (nobody leaves while its slot is read)
@@ -321,13 +336,12 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
 
   // Bins of the order: equal parts of the log2 domain from the maximum down to the least logit or
   // to 2^-44, where weights end.  Every step of the formula is monotone in x, rounding included.
-  const float y_least = fmaxf((0.5f * value_of(~(uint32_t)low) - weigh.top) * weigh.ch, -44.f);
-  const float per_bin = (float)(kBins - 1) / fmaxf(-y_least, 0x1p-40f);
-  // place in bins, for bin i from i up to below i + 1 (the last but one: from there on); -1: no weight
-  auto place_of = [&](float x) {
-    const float y = (0.5f * x - weigh.top) * weigh.ch;
-    return y > -44.f ? fminf(-y * per_bin, (float)(kBins - 2)) : -1.f;
-  };
+  const float d_least = 0.5f * value_of(~(uint32_t)low) - weigh.top, y_least = fmaxf(d_least * weigh.ch, -44.f);
+  const float to_place = -weigh.ch * ((float)(kBins - 1) / fmaxf(-y_least, 0x1p-40f));
+  // place in bins, for bin i from i up to below i + 1 (the last but one: from there on)
+  auto place_of = [&](float x) { return (0.5f * x - weigh.top) * to_place; };
+  auto weighs = [&](float x) { return (0.5f * x - weigh.top) * weigh.ch > -44.f; };
+  auto bin_of = [&](float x) { return min((int)place_of(x), kBins - 2); };
   // The bin at which the counts or the weights, summed from the first on, reach `target`, what comes
   // before it and what is in it; target > all: the last one.  For every thread of the row.
   auto bin_at = [&](u64 n, u64 target, u64 cum, u64 all, uint32_t& bin, u64& before, u64& in) {
@@ -589,9 +603,8 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
       load(step, x);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const float place = place_of(x[j]);
-        if (place < 0.f) continue;
-        const int bin = (int)place;
+        if (!weighs(x[j])) continue;
+        const int bin = bin_of(x[j]);
         atomicAdd(&s.bins[0][bin], 1u);
         if (!by_count) {
           const u64 w = weigh(x[j], s.table);
@@ -619,7 +632,8 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
       __syncthreads();
       count = s.sel, cin = s.sel_in;
     }
-    const float from = (float)bin, to = (float)(bin + 1);
+    // (before the last but one nothing is without weight)
+    const float from = (float)bin, to = bin == kBins - 2 ? inf : (float)(bin + 1);
     if (by_count && k == 0) {
       radix = by_weight;   // (without top-p nothing is left out)
     } else if (count <= kCap) {
@@ -631,8 +645,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
         uint32_t in = 0u;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-          const float place = place_of(x[j]);
-          in |= (place >= 0.f && place < to ? 1u : 0u) << j;
+          in |= (place_of(x[j]) < to && weighs(x[j]) ? 1u : 0u) << j;
         }
         list_up(in, x, step);
       }
@@ -681,8 +694,8 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
       };
       // by histograms of the list
       auto by_picks = [&] {
-        const float per = (float)kBins / to;
-        auto bin_in = [&](u64 c) { return min((int)(place_of(value_of((uint32_t)(c >> 32))) * per), kBins - 1); };
+        const float per = (float)kBins / (float)(bin + 1);
+        auto bin_in = [&](u64 c) { return min((int)(fminf(place_of(value_of((uint32_t)(c >> 32))), (float)kBins) * per), kBins - 1); };
         auto order_in = [](u64 c) { return c; };
         u64 border = 0ull, sum[2];
         if (by_count && !pick(n, (u64)min(k, n), bin_in, [](u64) { return 1ull; }, order_in, border)) return false;
@@ -759,8 +772,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
       // the border's bin alone, whose sorted tokens hold the border; meanwhile the weights before it
       u64 sum = sum_weights(
           [&](float x, u64 order) {
-            const float place = place_of(x);
-            return place >= 0.f && place < from && order >= last;
+            return place_of(x) < from && (last == 0ull || order >= last);
           },
           [&](const float* x, int step) {
             uint32_t in = 0u;
@@ -768,6 +780,10 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
             for (int j = 0; j < V; ++j) {
               const float place = place_of(x[j]);
               in |= (place >= from && place < to ? 1u : 0u) << j;
+            }
+            if (bin == kBins - 2) {
+#pragma unroll
+              for (int j = 0; j < V; ++j) in &= ~((weighs(x[j]) ? 0u : 1u) << j);
             }
             list_up(in, x, step);
           });
