@@ -197,17 +197,33 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
   auto first_step = [&](int share) { return (int)((long long)steps_all * share / shares); };
   const int step0 = first_step(share), step1 = first_step(share + 1);
 
-  auto load = [&](int step, float* x) {   // values past the end: -inf
+  auto fetch = [&](int step) {   // V values; past the end -inf
     const int i = (step * 32 + lane) * V;
-    if (a.vec && i + V <= a.vocab) {
-      const uint4 w = *(const uint4*)(row + i);
-      T t[V];
-      memcpy(t, &w, 16);
+    if (a.vec && i + V <= a.vocab) return *(const uint4*)(row + i);
+    T t[V];
 #pragma unroll
-      for (int j = 0; j < V; ++j) x[j] = to_f32(t[j]);
-    } else {
+    for (int j = 0; j < V; ++j) t[j] = i + j < a.vocab ? row[i + j] : from_f32<T>(-inf);
+    uint4 w;
+    memcpy(&w, t, 16);
+    return w;
+  };
+  auto widen = [&](const uint4& w, float* x) {
+    T t[V];
+    memcpy(t, &w, 16);
 #pragma unroll
-      for (int j = 0; j < V; ++j) x[j] = i + j < a.vocab ? to_f32(row[i + j]) : -inf;
+    for (int j = 0; j < V; ++j) x[j] = to_f32(t[j]);
+  };
+  auto load = [&](int step, float* x) { widen(fetch(step), x); };
+  // f(step, values) for the steps of this warp's run, a step's values on their way while the one before is worked on
+  auto for_steps = [&](auto f) {
+    if (step0 >= step1) return;
+    uint4 next = fetch(step0);
+#pragma unroll 1
+    for (int step = step0; step < step1; ++step) {
+      float x[V];
+      widen(next, x);
+      if (step + 1 < step1) next = fetch(step + 1);
+      f(step, x);
     }
   };
   auto index_of = [&](int step, int j) { return (step * 32 + lane) * V + j; };
@@ -568,17 +584,18 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
     float* keep = s.keep[warp];
     uint32_t n = 0;
     u64 sum = 0;
-#pragma unroll 2
-    for (int step = step0; step < step1; ++step) {
-      float x[V];
-      load(step, x);
+    for_steps([&](int step, const float* x) {
       lists(x, step);
+      uint32_t in = 0u;
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const bool in = takes(x[j], order_of(x[j], index_of(step, j)));
-        const uint32_t mask = __ballot_sync(kAll, in);
-        if (mask == 0u) continue;
-        if (in) keep[n + __popc(mask & ((1u << lane) - 1u))] = x[j];
+      for (int j = 0; j < V; ++j) in |= (takes(x[j], order_of(x[j], index_of(step, j))) ? 1u : 0u) << j;
+      while (const uint32_t mask = __ballot_sync(kAll, in != 0u)) {   // one of each lane's at a time
+        const int at = __ffs(in) - 1;
+        float of = x[0];
+#pragma unroll
+        for (int j = 1; j < V; ++j) of = at == j ? x[j] : of;
+        if (in) keep[n + __popc(mask & ((1u << lane) - 1u))] = of;
+        in &= in - 1u;
         n += __popc(mask);
         __syncwarp();
         if (n >= 32u) {
@@ -587,7 +604,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
           __syncwarp();
         }
       }
-    }
+    });
     if ((uint32_t)lane < n) sum += weigh(keep[lane], s.table);
     __syncwarp();
     return sum;
@@ -597,10 +614,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
   const bool by_count = k > 0 && k < a.vocab, by_weight = p < 1.f;
   bool radix = false;
   if (by_count || by_weight) {
-#pragma unroll 2
-    for (int step = step0; step < step1; ++step) {
-      float x[V];
-      load(step, x);
+    for_steps([&](int step, const float* x) {
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         if (!weighs(x[j])) continue;
@@ -612,7 +626,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
           atomicAdd(&s.bins[2][bin], (uint32_t)(w >> 32) + (was + lo < was ? 1u : 0u));
         }
       }
-    }
+    });
     barrier();
     uint32_t bin;
     u64 before = 0, in = 0, want = 0, all;
@@ -638,17 +652,12 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
       radix = by_weight;   // (without top-p nothing is left out)
     } else if (count <= kCap) {
       // all that can stay comes together in rank 0, which goes on alone
-#pragma unroll 1
-      for (int step = step0; step < step1; ++step) {
-        float x[V];
-        load(step, x);
+      for_steps([&](int step, const float* x) {
         uint32_t in = 0u;
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-          in |= (place_of(x[j]) < to && weighs(x[j]) ? 1u : 0u) << j;
-        }
+        for (int j = 0; j < V; ++j) in |= (place_of(x[j]) < to && weighs(x[j]) ? 1u : 0u) << j;
         list_up(in, x, step);
-      }
+      });
       const int n = bring_together();
       // by sorting
       auto by_sort = [&] {
@@ -911,13 +920,10 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
   // What stays, summed by warps' runs.
   u64 sum = 0;
   if (last == 0ull) {
-#pragma unroll 2
-    for (int step = step0; step < step1; ++step) {
-      float x[V];
-      load(step, x);
+    for_steps([&](int step, const float* x) {
 #pragma unroll
       for (int j = 0; j < V; ++j) sum += weigh(x[j], s.table);
-    }
+    });
   } else {
     sum = sum_weights([&](float x, u64 order) { return order >= last; }, no_list);
   }
