@@ -228,10 +228,14 @@ ravel_status ravel_cache_append_rotary(ravel_cache_t* c, int layer, const ravel_
   if (r->device != c->device) return fail(c, RAVEL_EINVAL, "append_rotary: the table is on another device");
   AppendRotaryArgs a{c->layer(layer), r->table, q, k, v, q_out, q_robot_stride, q_token_stride, q_out_robot_stride,
                      q_out_token_stride, k_robot_stride, k_token_stride, v_robot_stride, v_token_stride, batch, n,
-                     c->cfg.n_q_heads / c->cfg.n_kv_heads, c->cfg.max_tokens, starts, positions, counts, 0, 0, &c->err->bits};
+                     c->cfg.n_q_heads / c->cfg.n_kv_heads, c->cfg.max_tokens, starts, positions, counts, 0, 0, 16, c->num_sms, &c->err->bits};
   a.kv_vec = aligned16(k, k_robot_stride, k_token_stride, c->esize) && aligned16(v, v_robot_stride, v_token_stride, c->esize);
   a.q_vec = aligned16(q, q_robot_stride, q_token_stride, c->esize) &&
             aligned16(q_out, q_out_robot_stride, q_out_token_stride, c->esize);
+  const long long es = (long long)c->esize;
+  const uintptr_t all = (uintptr_t)q | (uintptr_t)q_out | (uintptr_t)(q_robot_stride * es) | (uintptr_t)(q_token_stride * es) |
+                        (uintptr_t)(q_out_robot_stride * es) | (uintptr_t)(q_out_token_stride * es);
+  while (all % a.q_align) a.q_align /= 2;
   const cudaError_t e = launch_cache_append_rotary(a, c->dt, (cudaStream_t)stream);
   return e == cudaSuccess ? RAVEL_OK : cuda_fail(c, e, "append_rotary");
 }

@@ -176,9 +176,8 @@ __device__ __forceinline__ void load16_turned(const T* row, int d, int hd, int v
 template <typename T>
 __device__ __forceinline__ void store16(T* row, int d, int hd, int vec, const float* x);
 
-// cache_append_kernel with the keys turned on their way in, and the G query heads of the KV head
-// turned beside them: a launch and the keys' way through memory less than turning first.  The CTA's
-// 16 tokens share one table of cosines and sines.
+// cache_append_kernel with the keys turned on their way in and, by CTAs of their own, the G query heads of
+// the KV head turned beside them.  A CTA's 16 tokens share one table of cosines and sines.
 template <typename T>
 __global__ void __launch_bounds__(256) cache_append_rotary_kernel(AppendRotaryArgs a) {
   __shared__ BlockShared s;
@@ -186,10 +185,11 @@ __global__ void __launch_bounds__(256) cache_append_rotary_kernel(AppendRotaryAr
   pdl_trigger();
   pdl_wait();
   const CacheLayer& c = a.c;
-  const int b = blockIdx.z, h = blockIdx.y;
+  const bool queries = (int)blockIdx.y >= c.Hkv;
+  const int b = blockIdx.z, h = queries ? blockIdx.y - c.Hkv : blockIdx.y;
   const int start = a.starts ? a.starts[b] : 0, count = a.counts ? a.counts[b] : a.n;
   if (start < 0 || count < 0 || count > a.n || start > a.max_tokens - count) {
-    if (threadIdx.x == 0 && blockIdx.x == 0 && h == 0) raise_error(a.err, ERR_SHAPE);
+    if (threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0) raise_error(a.err, ERR_SHAPE);
     return;
   }
   const int blk = start / kCacheBlock + blockIdx.x, end = start + count;
@@ -201,11 +201,32 @@ __global__ void __launch_bounds__(256) cache_append_rotary_kernel(AppendRotaryAr
     const long long position = a.positions ? a.positions[(long long)b * a.n + at] : (long long)p0 + t;
     cs[t * half + pair] = turn_of(a.r.f[pair], position, a.r.amplitude);
   }
+  __syncthreads();
   const int tpt = c.hdp / 16;   // threads per token
+  if (queries) {
+    // 16 dims of one head and token per turn.  A thread's 16 dims may be read by others as their pairs'
+    // other halves, so where q is written in place a turn's heads are read before any is written.
+    const int items = tokens * a.G * tpt;
+    for (int i0 = 0; i0 < items; i0 += blockDim.x) {
+      const int i = i0 + threadIdx.x;
+      float x[16];
+      T* to = nullptr;
+      int at = 0;
+      if (i < items) {
+        const int th = i / tpt, t = th / a.G, g = th % a.G;
+        at = (i % tpt) * 16;
+        const long long tok = p0 - start + t, head_at = (long long)(h * a.G + g) * c.hd;
+        load16_turned((const T*)a.q + (long long)b * a.q_robot + tok * a.q_token + head_at, at, c.hd, a.q_vec, a.r, cs + t * half, x);
+        to = (T*)a.q_out + (long long)b * a.qo_robot + tok * a.qo_token + head_at;
+      }
+      __syncthreads();   // (blockDim.x is a whole number of heads: 16 threads per token, tpt to a head)
+      if (to) store16(to, at, c.hd, a.q_vec, x);
+    }
+    return;
+  }
   const int token = threadIdx.x / tpt, d = (threadIdx.x % tpt) * 16;
   const int pos = blk * kCacheBlock + token;
   const bool fresh = pos >= start && pos < end, stay = pos < start;
-  __syncthreads();
   float kx[16], vx[16];
   if (fresh) {
     const T* k = (const T*)a.k + (long long)b * a.k_robot + (long long)(pos - start) * a.k_token + (long long)h * c.hd;
@@ -216,26 +237,6 @@ __global__ void __launch_bounds__(256) cache_append_rotary_kernel(AppendRotaryAr
   const size_t head = (size_t)b * c.Hkv + h;
   store_block<0>(s, kx, vx, fresh, stay, blk * kCacheBlock < start, token, c, (head * c.T + pos) * c.hdp,
                  head * (c.T / kCacheBlock) + blk, d);
-  if (!a.q) return;
-  // queries: 16 dims of one head and token per turn.  A thread's 16 dims may be read by others as
-  // their pairs' other halves, so where q is written in place all of a token's heads that are at
-  // hand are read before any is written.
-  const int items = tokens * a.G * tpt;
-  for (int i0 = 0; i0 < items; i0 += blockDim.x) {
-    const int i = i0 + threadIdx.x;
-    float x[16];
-    T* to = nullptr;
-    int at = 0;
-    if (i < items) {
-      const int th = i / tpt, t = th / a.G, g = th % a.G;
-      at = (i % tpt) * 16;
-      const long long tok = p0 - start + t, head_at = (long long)(h * a.G + g) * c.hd;
-      load16_turned((const T*)a.q + (long long)b * a.q_robot + tok * a.q_token + head_at, at, c.hd, a.q_vec, a.r, cs + t * half, x);
-      to = (T*)a.q_out + (long long)b * a.qo_robot + tok * a.qo_token + head_at;
-    }
-    __syncthreads();   // (blockDim.x is a whole number of heads: 16 threads per token, tpt to a head)
-    if (to) store16(to, at, c.hd, a.q_vec, x);
-  }
 }
 
 // Bandwidth-bound for many tokens, a launch and dependent loads for few: a thread takes 16
@@ -536,7 +537,15 @@ cudaError_t launch_cache_append(const AppendArgs& a, Dtype dt, cudaStream_t st) 
 }
 
 cudaError_t launch_cache_append_rotary(const AppendRotaryArgs& a, Dtype dt, cudaStream_t st) {
-  const dim3 grid((a.n + 2 * kCacheBlock - 2) / kCacheBlock, a.c.Hkv, a.batch);
+  // queries of few tokens in the same launch, of many in one that streams them; FEWSTORE
+  const bool apart = a.q && a.n > 16;
+  if (apart) {
+    RotaryArgs r{a.r, a.q, a.q_out, a.q_robot, a.q_token, a.qo_robot, a.qo_token, a.batch, a.n, a.c.Hkv * a.G, a.c.hd,
+                 a.starts, a.positions, a.counts, a.q_align, a.num_sms, a.max_tokens};
+    const cudaError_t e = launch_rotary(r, dt, st);
+    if (e != cudaSuccess) return e;
+  }
+  const dim3 grid((a.n + 2 * kCacheBlock - 2) / kCacheBlock, a.q && !apart ? 2 * a.c.Hkv : a.c.Hkv, a.batch);
   const Overlap overlap;
   return launch_kernel(dt == DT_BF16 ? cache_append_rotary_kernel<bf16> : cache_append_rotary_kernel<float>, grid, dim3(a.c.hdp), 0,
                        st, 1, a);

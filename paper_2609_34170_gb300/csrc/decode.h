@@ -28,6 +28,7 @@ struct RotaryArgs {
   const int *starts, *positions, *counts;
   int align;   // largest power of two, up to 16, that divides every row's address and stride in bytes
   int num_sms;
+  int room;    // > 0: a robot whose count is not 0 .. n or whose tokens from starts on would pass `room` is left out
 };
 cudaError_t launch_rotary(const RotaryArgs& a, Dtype dt, cudaStream_t st);
 
@@ -40,6 +41,7 @@ struct AppendRotaryArgs {
   int batch, n, G, max_tokens;
   const int *starts, *positions, *counts;
   int kv_vec, q_vec;   // rows of k and v, of q and q_out are 16-byte aligned
+  int q_align, num_sms;   // as RotaryArgs, of q and q_out
   int* err;
 };
 cudaError_t launch_cache_append_rotary(const AppendRotaryArgs& a, Dtype dt, cudaStream_t st);

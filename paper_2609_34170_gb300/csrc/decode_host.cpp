@@ -179,7 +179,7 @@ ravel_status ravel_rotary_apply(ravel_rotary_t* r, int batch, int n, int heads, 
   if (batch == 0 || n == 0 || heads == 0) return RAVEL_OK;
   if (!x || !out) return fail(RAVEL_EINVAL, "rotary_apply: null argument");
   RotaryArgs a{r->table, x,     out, x_robot_stride, x_token_stride, out_robot_stride, out_token_stride, batch, n, heads, hd,
-               starts,   positions, counts, 16, r->num_sms};
+               starts,   positions, counts, 16, r->num_sms, 0};
   const long long es = size_of(dtype);
   const uintptr_t all = (uintptr_t)x | (uintptr_t)out | (uintptr_t)(x_robot_stride * es) | (uintptr_t)(x_token_stride * es) |
                         (uintptr_t)(out_robot_stride * es) | (uintptr_t)(out_token_stride * es);

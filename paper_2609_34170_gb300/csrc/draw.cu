@@ -611,13 +611,15 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
   };
 
   auto no_list = [](const float*, int) {};
-  const bool by_count = k > 0 && k < a.vocab, by_weight = p < 1.f;
-  bool radix = false;
-  if (by_count || by_weight) {
+  const bool by_weight = p < 1.f;
+  bool by_count = k > 0 && k < a.vocab, radix = false;
+  u64 stays = 0ull;   // the last of the order that top-k lets through, once it is known by itself
+  // (twice where top-k's border has to be found before top-p's sum: its tokens are more than a list holds)
+  while (by_count || by_weight) {
     for_steps([&](int step, const float* x) {
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        if (!weighs(x[j])) continue;
+        if (!weighs(x[j]) || (stays != 0ull && order_of(x[j], index_of(step, j)) < stays)) continue;
         const int bin = bin_of(x[j]);
         atomicAdd(&s.bins[0][bin], 1u);
         if (!by_count) {
@@ -634,7 +636,6 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
     u64 upto = block_scan(n, all), count, cin;   // tokens up to the bin, in it
     if (by_count) {
       bin_at(n, (u64)k, upto, all, bin, before, in);
-      if (bin == kBins - 1) k = 0;   // what top-k leaves out has no weight
       cin = in, count = before + in;
     } else {
       const u64 w = tid < kBins ? sum_of(&s.bins[1][tid]) + (sum_of(&s.bins[2][tid]) << 32) : 0ull;
@@ -648,14 +649,43 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
     }
     // (before the last but one nothing is without weight)
     const float from = (float)bin, to = bin == kBins - 2 ? inf : (float)(bin + 1);
-    if (by_count && k == 0) {
-      radix = by_weight;   // (without top-p nothing is left out)
-    } else if (count <= kCap) {
+    auto again = [&] {   // (nobody reads this CTA's any more)
+      for (int i = tid; i < 3 * kBins; i += kThreads) (&s.bins[0][0])[i] = 0u;
+      if (tid == 0) s.listed = 0u;
+      __syncthreads();
+    };
+    if (by_count && bin == kBins - 1) {   // what top-k leaves out has no weight
+      by_count = false;
+      k = 0;
+      barrier();
+      again();
+      continue;
+    }
+    // a step's tokens of the border's bin
+    auto in_bin = [&](const float* x, int step) {
+      uint32_t in = 0u;
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float place = place_of(x[j]);
+        in |= (place >= from && place < to ? 1u : 0u) << j;
+      }
+      if (bin == kBins - 2) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) in &= ~((weighs(x[j]) ? 0u : 1u) << j);
+      }
+      if (stays != 0ull) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) in &= ~((order_of(x[j], index_of(step, j)) < stays ? 1u : 0u) << j);
+      }
+      return in;
+    };
+    if (count <= kCap) {
       // all that can stay comes together in rank 0, which goes on alone
       for_steps([&](int step, const float* x) {
         uint32_t in = 0u;
 #pragma unroll
-        for (int j = 0; j < V; ++j) in |= (place_of(x[j]) < to && weighs(x[j]) ? 1u : 0u) << j;
+        for (int j = 0; j < V; ++j)
+          in |= (place_of(x[j]) < to && weighs(x[j]) && (stays == 0ull || order_of(x[j], index_of(step, j)) >= stays) ? 1u : 0u) << j;
         list_up(in, x, step);
       });
       const int n = bring_together();
@@ -777,25 +807,16 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
       }
       barrier();   // nobody leaves while its list is read
       return;
-    } else if (cin <= kCap && !(by_count && by_weight)) {
+    } else if (cin <= kCap) {
       // the border's bin alone, whose sorted tokens hold the border; meanwhile the weights before it
-      u64 sum = sum_weights(
-          [&](float x, u64 order) {
-            return place_of(x) < from && (last == 0ull || order >= last);
-          },
-          [&](const float* x, int step) {
-            uint32_t in = 0u;
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-              const float place = place_of(x[j]);
-              in |= (place >= from && place < to ? 1u : 0u) << j;
-            }
-            if (bin == kBins - 2) {
-#pragma unroll
-              for (int j = 0; j < V; ++j) in &= ~((weighs(x[j]) ? 0u : 1u) << j);
-            }
-            list_up(in, x, step);
-          });
+      u64 sum = 0ull;
+      if (by_count && by_weight) {
+        for_steps([&](int step, const float* x) { list_up(in_bin(x, step), x, step); });
+      } else {
+        last = max(last, stays);
+        sum = sum_weights([&](float x, u64 order) { return place_of(x) < from && (last == 0ull || order >= last); },
+                          [&](const float* x, int step) { list_up(in_bin(x, step), x, step); });
+      }
       const int n = bring_together();
       if (rank == 0) {
         sort(n);
@@ -811,8 +832,15 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
         if (tid == 0) s.slot[turn][0] = border;
       }
       barrier();
-      last = max(last, from_rank(&s.slot[turn][0], 0));
+      const u64 border = from_rank(&s.slot[turn][0], 0);
       turn ^= 1;
+      if (by_count && by_weight) {
+        stays = border;
+        by_count = false;
+        again();
+        continue;
+      }
+      last = max(last, border);
       // the bin's tokens that stay, into the sums of their runs: this CTA's, in its list
       if (lane == 0) s.runs[warp] = 0ull;
       const int own = rank == 0 && ranks > 1 ? (int)s.counts[0] : (int)min(s.listed, (uint32_t)kCap);
@@ -831,9 +859,9 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
       if (lane == 0) sum += s.runs[warp];
       draw(sum);
       return;
-    } else {
-      radix = true;
     }
+    radix = true;
+    break;
   }
 
   if (radix) {
@@ -851,10 +879,16 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
 #pragma unroll
           for (int j = 0; j < V; ++j) {
             const uint32_t key = key_of(x[j]);
-            if (key > above && (key & mask) == prefix && index_of(step, j) < a.vocab) {
-              const u64 w = weights ? weigh(x[j], s.table) : 1ull;
-              if (w) atomicAdd(&hist[(key >> shift) & 255u], w);
-            }
+            u64 w = 0ull;
+            if (key > above && (key & mask) == prefix && index_of(step, j) < a.vocab) w = weights ? weigh(x[j], s.table) : 1ull;
+            // lanes of the first one's digit together (many equal logits would queue up at one address)
+            const uint32_t digit = (key >> shift) & 255u, active = __ballot_sync(kAll, w != 0ull);
+            if (!active) continue;
+            const uint32_t lead = __shfl_sync(kAll, digit, __ffs(active) - 1);
+            const bool with = w != 0ull && digit == lead;
+            const u64 sum = warp_sum_u64(with ? w : 0ull);
+            if (lane == 0) atomicAdd(&hist[lead], sum);
+            if (w && !with) atomicAdd(&hist[digit], w);
           }
         }
         barrier();
@@ -877,7 +911,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
     uint32_t border = 0u;   // tokens of keys above it stay, and of those with its key the first `ties`
     u64 ties = 0ull;
     barrier();   // (the histograms lie where the bins are read)
-    if (k > 0 && by_count) border = select((u64)k, 0u, false, ties);
+    if (k > 0 && k < a.vocab) border = select((u64)k, 0u, false, ties);
     if (by_weight) {
       u64 all = sum_weights([&](float x, u64 order) { return (uint32_t)(order >> 32) > border; }, no_list), ignored;
       all = warp_sum_u64(all);

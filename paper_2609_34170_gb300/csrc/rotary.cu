@@ -64,7 +64,12 @@ __global__ void __launch_bounds__(256) rotary_kernel(RotaryArgs a, int tokens, L
   const int threads = blockDim.x * blockDim.y, tid = threadIdx.y * blockDim.x + threadIdx.x;
   pdl_trigger();
   pdl_wait();
-  const int count = min(a.counts ? a.counts[b] : a.n, a.n), i0 = blockIdx.x * tokens, here = min(tokens, count - i0);
+  int count = min(a.counts ? a.counts[b] : a.n, a.n);
+  if (a.room > 0) {
+    const int first = a.starts ? a.starts[b] : 0;
+    if (first < 0 || (a.counts && a.counts[b] > a.n) || first > a.room - count) count = 0;
+  }
+  const int i0 = blockIdx.x * tokens, here = min(tokens, count - i0);
   if (here <= 0) return;
   const long long start = (a.starts ? (long long)a.starts[b] : 0ll) + i0;
   for (int at = tid; at < here * half; at += threads) {

@@ -220,6 +220,17 @@ def test_append_rotary_reports_positions_out_of_range():
     cache.append_rotary(0, Rotary(64), q, k, k, _ints([30, 0]), q_out=out)
     torch.cuda.synchronize()
     assert (out[0] == 3).all() and not (out[1] == 3).all()
+    cache.reset()
+    k20, q20 = _rand((2, 20, 1, 64), 0, "bf16"), _rand((2, 20, 2, 64), 1, "bf16")
+    for starts, counts in (([13, 0], None), ([-1, 0], None), ([0, 0], [21, 20]), ([0, 0], [-1, 20]), ([30, 0], [3, 20])):
+        out20 = torch.full_like(q20, 3.0)
+        cache.append_rotary(0, Rotary(64), q20, k20, k20, _ints(starts), counts=None if counts is None else _ints(counts), q_out=out20)
+        torch.cuda.synchronize()
+        assert (out20[0] == 3).all() and not (out20[1] == 3).any()
+        cache.reset()
+    cache = ContextCache(1, 2, 1, 64, 32, 2)
+    cache.append_rotary(0, Rotary(64), q, k, k, _ints([30, 0]), q_out=out)
+    torch.cuda.synchronize()
     with pytest.raises(RavelError) as ei:
         cache.append_rotary(0, Rotary(64), q, k, k, _ints([0, 0]))
     assert ei.value.status == 7
