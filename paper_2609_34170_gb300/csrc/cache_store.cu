@@ -131,7 +131,15 @@ __device__ __forceinline__ void store16(T* row, int d, int hd, int vec, const fl
   }
 }
 
-// 16 values from dim d on of a row of heads, turned.  cs: the token's cosines and sines by pair.
+// Where a token's cosine and sine of a pair lie: the w = 2^log pairs that a thread of load16_turned takes are
+// half / w apart, so that threads side by side read side by side (with a thread's pairs side by side their reads
+// fell into one bank: 816 tokens of 16 robots with one head of 256 14.6 us, now KEYS).
+__device__ __forceinline__ int turn_log(const RotaryTable& r) {
+  return r.interleaved ? (r.dims % 16 == 0 ? 3 : 0) : r.dims % 32 == 0 ? 4 : 0;
+}
+__device__ __forceinline__ int turn_at(int pair, int half, int log) { return (pair & ((1 << log) - 1)) * (half >> log) + (pair >> log); }
+
+// 16 values from dim d on of a row of heads, turned.  cs: the token's cosines and sines, see turn_at.
 // The pair of a dim may be anywhere in the row where the halves are not whole multiples of 16: then
 // both are loaded one by one.
 template <typename T>
@@ -144,7 +152,7 @@ __device__ __forceinline__ void load16_turned(const T* row, int d, int hd, int v
     load16(row, d, hd, vec, y);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float2 t = cs[d / 2 + i];
+      const float2 t = cs[i * (half >> 3) + d / 16];
       x[2 * i] = turned(y[2 * i], y[2 * i + 1], t, true);
       x[2 * i + 1] = turned(y[2 * i + 1], y[2 * i], t, false);
     }
@@ -156,7 +164,7 @@ __device__ __forceinline__ void load16_turned(const T* row, int d, int hd, int v
     load16(row, first ? d + half : pair, hd, vec, z);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      x[i] = turned(y[i], z[i], cs[pair + i], first);
+      x[i] = turned(y[i], z[i], cs[i * (half >> 4) + pair / 16], first);
     }
   } else {
 #pragma unroll
@@ -196,13 +204,21 @@ __global__ void __launch_bounds__(256) cache_append_rotary_kernel(AppendRotaryAr
   if (count == 0 || blk * kCacheBlock >= end) return;
   const int half = a.r.dims / 2;
   const int p0 = max(blk * kCacheBlock, start), tokens = min((blk + 1) * kCacheBlock, end) - p0;   // the new ones here
+  const int tpt = c.hdp / 16, log = turn_log(a.r);   // threads per token
+  const int token = threadIdx.x / tpt, d = (threadIdx.x % tpt) * 16;
+  const int pos = blk * kCacheBlock + token;
+  const bool fresh = pos >= start && pos < end, stay = pos < start;
+  const T* k = (const T*)a.k + (long long)b * a.k_robot + (long long)(pos - start) * a.k_token + (long long)h * c.hd;
+  const T* v = (const T*)a.v + (long long)b * a.v_robot + (long long)(pos - start) * a.v_token + (long long)h * c.hd;
+  float kx[16], vx[16];
+  if (!queries && fresh) load16(v, d, c.hd, a.kv_vec, vx);   // (on its way while the sines are computed)
+#pragma unroll 4
   for (int i = threadIdx.x; i < tokens * half; i += blockDim.x) {
-    const int t = i / half, pair = i % half, at = p0 - start + t;
+    const int t = i / half, pair = i - t * half, at = p0 - start + t;
     const long long position = a.positions ? a.positions[(long long)b * a.n + at] : (long long)p0 + t;
-    cs[t * half + pair] = turn_of(a.r.f[pair], position, a.r.amplitude);
+    cs[t * half + turn_at(pair, half, log)] = turn_of(a.r.f[pair], position, a.r.amplitude);
   }
   __syncthreads();
-  const int tpt = c.hdp / 16;   // threads per token
   if (queries) {
     // 16 dims of one head and token per turn.  A thread's 16 dims may be read by others as their pairs'
     // other halves, so where q is written in place a turn's heads are read before any is written.
@@ -224,16 +240,7 @@ __global__ void __launch_bounds__(256) cache_append_rotary_kernel(AppendRotaryAr
     }
     return;
   }
-  const int token = threadIdx.x / tpt, d = (threadIdx.x % tpt) * 16;
-  const int pos = blk * kCacheBlock + token;
-  const bool fresh = pos >= start && pos < end, stay = pos < start;
-  float kx[16], vx[16];
-  if (fresh) {
-    const T* k = (const T*)a.k + (long long)b * a.k_robot + (long long)(pos - start) * a.k_token + (long long)h * c.hd;
-    const T* v = (const T*)a.v + (long long)b * a.v_robot + (long long)(pos - start) * a.v_token + (long long)h * c.hd;
-    load16_turned(k, d, c.hd, a.kv_vec, a.r, cs + (pos - p0) * half, kx);
-    load16(v, d, c.hd, a.kv_vec, vx);
-  }
+  if (fresh) load16_turned(k, d, c.hd, a.kv_vec, a.r, cs + (pos - p0) * half, kx);
   const size_t head = (size_t)b * c.Hkv + h;
   store_block<0>(s, kx, vx, fresh, stay, blk * kCacheBlock < start, token, c, (head * c.T + pos) * c.hdp,
                  head * (c.T / kCacheBlock) + blk, d);
