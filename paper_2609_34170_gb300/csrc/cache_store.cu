@@ -131,7 +131,7 @@ __device__ __forceinline__ void store16(T* row, int d, int hd, int vec, const fl
   }
 }
 
-// Where a token's cosine and sine of a pair lie: the w = 2^log pairs that a thread of load16_turned takes are
+// Where a token's cosine and sine of a pair lie: the w = 2^log pairs that a thread of Turned16 takes are
 // half / w apart, so that threads side by side read side by side (with a thread's pairs side by side their reads
 // fell into one bank: 816 tokens of 16 robots with one head of 256 14.6 us, now KEYS).
 __device__ __forceinline__ int turn_log(const RotaryTable& r) {
@@ -139,47 +139,80 @@ __device__ __forceinline__ int turn_log(const RotaryTable& r) {
 }
 __device__ __forceinline__ int turn_at(int pair, int half, int log) { return (pair & ((1 << log) - 1)) * (half >> log) + (pair >> log); }
 
-// 16 values from dim d on of a row of heads, turned.  cs: the token's cosines and sines, see turn_at.
-// The pair of a dim may be anywhere in the row where the halves are not whole multiples of 16: then
-// both are loaded one by one.
+// 16 values of a row as they lie in memory (zeros from hd on): to be on their way while something else is done.
 template <typename T>
-__device__ __forceinline__ void load16_turned(const T* row, int d, int hd, int vec, const RotaryTable& r, const float2* cs, float* x) {
-  const int half = r.dims / 2;
-  if (d >= r.dims) {
-    load16(row, d, hd, vec, x);
-  } else if (r.interleaved && r.dims % 16 == 0) {
-    float y[16];
-    load16(row, d, hd, vec, y);
+struct Raw16 {
+  uint4 w[sizeof(T)];
+  __device__ __forceinline__ void load(const T* row, int d, int hd, int vec) {
+    constexpr int NV = sizeof(T) / 2;   // of 8 values
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float2 t = cs[i * (half >> 3) + d / 16];
-      x[2 * i] = turned(y[2 * i], y[2 * i + 1], t, true);
-      x[2 * i + 1] = turned(y[2 * i + 1], y[2 * i], t, false);
-    }
-  } else if (!r.interleaved && half % 16 == 0) {
-    const bool first = d < half;
-    const int pair = first ? d : d - half;
-    float y[16], z[16];
-    load16(row, d, hd, vec, y);
-    load16(row, first ? d + half : pair, hd, vec, z);
+    for (int h = 0; h < 2; ++h) {
+      const int d8 = d + 8 * h;
+      T y[8];
+      if (d8 < hd && !vec) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      x[i] = turned(y[i], z[i], cs[i * (half >> 4) + pair / 16], first);
-    }
-  } else {
+        for (int i = 0; i < 8; ++i) y[i] = row[d8 + i];
+        memcpy(&w[h * NV], y, sizeof y);
+      } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int at = d + i;
-      x[i] = at < hd ? to_f32(row[at]) : 0.f;
-      if (at < r.dims) {
-        const bool first = r.interleaved ? at % 2 == 0 : at < half;
-        const int other = r.interleaved ? at ^ 1 : first ? at + half : at - half;
-        const float2 t = cs[r.interleaved ? at / 2 : first ? at : at - half];
-        x[i] = turned(x[i], to_f32(row[other]), t, first);
+        for (int i = 0; i < NV; ++i) w[h * NV + i] = d8 < hd ? *((const uint4*)(row + d8) + i) : make_uint4(0u, 0u, 0u, 0u);
       }
     }
   }
-}
+  __device__ __forceinline__ void values(float* x) const {
+    T y[16];
+    memcpy(y, w, sizeof y);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = to_f32(y[i]);
+  }
+};
+
+// 16 values from dim d on of a row of heads, turned: loaded first, then (behind the cosines and sines cs of the
+// token, see turn_at) turned.  The pair of a dim may be anywhere in the row where the halves are not whole multiples
+// of 16: then both are loaded one by one.
+template <typename T>
+struct Turned16 {
+  Raw16<T> own, other;
+  __device__ __forceinline__ static int kind(int d, const RotaryTable& r) {
+    return d >= r.dims ? 0 : r.interleaved && r.dims % 16 == 0 ? 1 : !r.interleaved && r.dims % 32 == 0 ? 2 : 3;
+  }
+  __device__ __forceinline__ void load(const T* row, int d, int hd, int vec, const RotaryTable& r) {
+    const int of = kind(d, r), half = r.dims / 2;
+    if (of < 3) own.load(row, d, hd, vec);
+    if (of == 2) other.load(row, d < half ? d + half : d - half, hd, vec);
+  }
+  __device__ __forceinline__ void values(const T* row, int d, int hd, const RotaryTable& r, const float2* cs, float* x) const {
+    const int of = kind(d, r), half = r.dims / 2;
+    if (of < 3) own.values(x);
+    if (of == 1) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float2 t = cs[i * (half >> 3) + d / 16];
+        const float p = x[2 * i], q = x[2 * i + 1];
+        x[2 * i] = turned(p, q, t, true);
+        x[2 * i + 1] = turned(q, p, t, false);
+      }
+    } else if (of == 2) {
+      const bool first = d < half;
+      const int pair = first ? d : d - half;
+      float z[16];
+      other.values(z);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = turned(x[i], z[i], cs[i * (half >> 4) + pair / 16], first);
+    } else if (of == 3) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int at = d + i;
+        x[i] = at < hd ? to_f32(row[at]) : 0.f;
+        if (at < r.dims) {
+          const bool first = r.interleaved ? at % 2 == 0 : at < half;
+          const int pair = r.interleaved ? at ^ 1 : first ? at + half : at - half;
+          x[i] = turned(x[i], to_f32(row[pair]), cs[r.interleaved ? at / 2 : first ? at : at - half], first);
+        }
+      }
+    }
+  }
+};
 
 template <typename T>
 __device__ __forceinline__ void store16(T* row, int d, int hd, int vec, const float* x);
@@ -210,13 +243,18 @@ __global__ void __launch_bounds__(256) cache_append_rotary_kernel(AppendRotaryAr
   const bool fresh = pos >= start && pos < end, stay = pos < start;
   const T* k = (const T*)a.k + (long long)b * a.k_robot + (long long)(pos - start) * a.k_token + (long long)h * c.hd;
   const T* v = (const T*)a.v + (long long)b * a.v_robot + (long long)(pos - start) * a.v_token + (long long)h * c.hd;
-  float kx[16], vx[16];
-  if (!queries && fresh) load16(v, d, c.hd, a.kv_vec, vx);   // (on its way while the sines are computed)
-#pragma unroll 4
-  for (int i = threadIdx.x; i < tokens * half; i += blockDim.x) {
-    const int t = i / half, pair = i - t * half, at = p0 - start + t;
-    const long long position = a.positions ? a.positions[(long long)b * a.n + at] : (long long)p0 + t;
+  Turned16<T> key;
+  Raw16<T> value;
+  if (!queries && fresh) {   // (on their way while the sines are computed)
+    key.load(k, d, c.hd, a.kv_vec, a.r);
+    value.load(v, d, c.hd, a.kv_vec);
+  }
+  const int on_t = blockDim.x / half, on_pair = blockDim.x - on_t * half;
+  for (int t = threadIdx.x / half, pair = threadIdx.x - t * half; t < tokens;) {
+    const long long position = a.positions ? a.positions[(long long)b * a.n + p0 - start + t] : (long long)p0 + t;
     cs[t * half + turn_at(pair, half, log)] = turn_of(a.r.f[pair], position, a.r.amplitude);
+    t += on_t, pair += on_pair;
+    if (pair >= half) pair -= half, ++t;
   }
   __syncthreads();
   if (queries) {
@@ -232,7 +270,10 @@ __global__ void __launch_bounds__(256) cache_append_rotary_kernel(AppendRotaryAr
         const int th = i / tpt, t = th / a.G, g = th % a.G;
         at = (i % tpt) * 16;
         const long long tok = p0 - start + t, head_at = (long long)(h * a.G + g) * c.hd;
-        load16_turned((const T*)a.q + (long long)b * a.q_robot + tok * a.q_token + head_at, at, c.hd, a.q_vec, a.r, cs + t * half, x);
+        const T* q = (const T*)a.q + (long long)b * a.q_robot + tok * a.q_token + head_at;
+        Turned16<T> query;
+        query.load(q, at, c.hd, a.q_vec, a.r);
+        query.values(q, at, c.hd, a.r, cs + t * half, x);
         to = (T*)a.q_out + (long long)b * a.qo_robot + tok * a.qo_token + head_at;
       }
       __syncthreads();   // (blockDim.x is a whole number of heads: 16 threads per token, tpt to a head)
@@ -240,7 +281,11 @@ __global__ void __launch_bounds__(256) cache_append_rotary_kernel(AppendRotaryAr
     }
     return;
   }
-  if (fresh) load16_turned(k, d, c.hd, a.kv_vec, a.r, cs + (pos - p0) * half, kx);
+  float kx[16], vx[16];
+  if (fresh) {
+    key.values(k, d, c.hd, a.r, cs + (pos - p0) * half, kx);
+    value.values(vx);
+  }
   const size_t head = (size_t)b * c.Hkv + h;
   store_block<0>(s, kx, vx, fresh, stay, blk * kCacheBlock < start, token, c, (head * c.T + pos) * c.hdp,
                  head * (c.T / kCacheBlock) + blk, d);

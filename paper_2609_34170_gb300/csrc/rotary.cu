@@ -72,11 +72,13 @@ __global__ void __launch_bounds__(256) rotary_kernel(RotaryArgs a, int tokens, L
   const int i0 = blockIdx.x * tokens, here = min(tokens, count - i0);
   if (here <= 0) return;
   const long long start = (a.starts ? (long long)a.starts[b] : 0ll) + i0;
-  for (int at = tid; at < here * half; at += threads) {
-    const int token = at / half, pair = at - token * half;
+  const int on_token = threads / half, on_pair = threads - on_token * half;
+  for (int token = tid / half, pair = tid - token * half; token < here;) {
     const long long position = a.positions ? a.positions[(long long)b * a.n + i0 + token] : start + token;
-    const int place = pair / P, j = pair - place * P;
+    const int place = pair / P, j = pair - place * P;   // (P is a power of two)
     cs[token * half + (j / kVec * turning + place) * kVec + j % kVec] = turn_of(a.r.f[pair], position, a.r.amplitude);
+    token += on_token, pair += on_pair;
+    if (pair >= half) pair -= half, ++token;
   }
   __syncthreads();
   const bool stays = (int)threadIdx.x >= turning;
