@@ -133,7 +133,7 @@ __device__ __forceinline__ void store16(T* row, int d, int hd, int vec, const fl
 
 // Where a token's cosine and sine of a pair lie: the w = 2^log pairs that a thread of Turned16 takes are
 // half / w apart, so that threads side by side read side by side (with a thread's pairs side by side their reads
-// fell into one bank: 816 tokens of 16 robots with one head of 256 14.6 us, now KEYS).
+// fell into one bank: keys alone of 816 tokens of 16 robots, one head of 256, 14.6 us, so 11.9).
 __device__ __forceinline__ int turn_log(const RotaryTable& r) {
   return r.interleaved ? (r.dims % 16 == 0 ? 3 : 0) : r.dims % 32 == 0 ? 4 : 0;
 }
@@ -218,7 +218,9 @@ template <typename T>
 __device__ __forceinline__ void store16(T* row, int d, int hd, int vec, const float* x);
 
 // cache_append_kernel with the keys turned on their way in and, by CTAs of their own, the G query heads of
-// the KV head turned beside them.  A CTA's 16 tokens share one table of cosines and sines.
+// the KV head turned beside them.  A CTA's 16 tokens share one table of cosines and sines.  Keys alone of 816
+// tokens of 16 robots, one head of 256: 11.3 us where cache_append_kernel takes 4.8, for one and a third rounds of
+// CTAs (64 registers; 48 or 40 spill and cost more) that compute 2048 sines each before anything is stored.
 template <typename T>
 __global__ void __launch_bounds__(256) cache_append_rotary_kernel(AppendRotaryArgs a) {
   __shared__ BlockShared s;
@@ -589,7 +591,9 @@ cudaError_t launch_cache_append(const AppendArgs& a, Dtype dt, cudaStream_t st) 
 }
 
 cudaError_t launch_cache_append_rotary(const AppendRotaryArgs& a, Dtype dt, cudaStream_t st) {
-  // queries of few tokens in the same launch, of many in one that streams them; FEWSTORE
+  // Queries of few tokens in the same launch: a token of 64 robots (8 query heads on one of 256) 2.9 us, turned and
+  // stored by two calls 3.7.  Of many in one that streams them: 816 tokens of 16 robots 31 us (81 in one launch;
+  // two calls, whose keys are rounded to bf16 in between, 27).
   const bool apart = a.q && a.n > 16;
   if (apart) {
     RotaryArgs r{a.r, a.q, a.q_out, a.q_robot, a.q_token, a.qo_robot, a.qo_token, a.batch, a.n, a.c.Hkv * a.G, a.c.hd,

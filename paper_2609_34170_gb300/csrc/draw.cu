@@ -12,6 +12,12 @@
 // the border, while the weights before it are summed by warps' runs of the row; the run that holds the
 // token is gone through again.  Where even the bin holds more (thousands of nearly equal logits), a
 // radix selection over the keys' four bytes finds the border.
+//
+// Measured (replays from a graph): one row of 65536 bf16 logits under top-k 40, top-p and min-p 12.2 us, a chain of four
+// barriers of the cluster (800 to 1500 cycles each) and what lies between; 64 rows of 128001 fp32 logits under top-p 0.9 61
+// us, of which the histogram takes 21 (84 instructions a logit, 50 of them its weight, at two thirds of the issue
+// rate), the list and the sums 14, the first pass 5.5; the same without limits 33, with top-k 50 28, with top-k 3000
+// and top-p 75, all logits equal 467.
 #include <algorithm>
 
 #include "common.cuh"

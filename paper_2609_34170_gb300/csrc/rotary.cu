@@ -50,7 +50,7 @@ constexpr int kTable = 2048;   // cosines and sines of a CTA's tokens
 // either half) per turn, kAhead rows of heads at a time.  threadIdx.x: the vector's place in the head, of
 // the dims that turn and, where out is not x, of those that stay.  Nothing but bytes bounds it for many
 // tokens; for few a launch, a load and the sines.  Measured: 816 tokens of 16 robots, 9 of 10 heads of 256 in
-// bf16, half layout, 120 MB, 21.6 us (5.6 TB/s; two turns' vectors on their way 24.6, four 34); 65536 tokens of
+// bf16, half layout, 120 MB, 20.9 us (5.8 TB/s; two turns' vectors on their way 24.6, four 34); 65536 tokens of
 // 20 heads of 64 in fp32, 32 dims interleaved, 671 MB, 98 us (6.8 TB/s; one turn's 102).  With the sines in
 // registers, a thread taking one head after another, 25.8 and 124 to 144.
 template <typename T, int V, bool IL>
