@@ -468,21 +468,16 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
     __syncthreads();
     return s.sel;
   };
-  // Of the list's first n values c that at which value_of_it(c), summed from the largest order_in(c) down, reaches
-  // `target`: a histogram by bin_in (of kBins, monotone), then the values of the bin that holds it, each with the sum of
-  // those before it.  false: the bin has more than 256 of them.
-  auto pick = [&](int n, u64 target, auto bin_in, auto value_of_it, auto order_in, u64& found) {
-    __syncthreads();
+  // Of values c with weights w, two to a thread, that at which the weights, summed from the largest order_in(c) down,
+  // reach `target`: a histogram by bin_in (of kBins, monotone), then the values of the bin that holds it, each with
+  // the sum of those before it.  false: the bin has more than 256 of them.
+  auto pick = [&](const u64* c, const u64* w, u64 target, auto bin_in, auto order_in, u64& found) {
     if (tid < kBins) s.pick.hist[tid] = 0ull;
     if (tid == 0) s.few_n = 0u;
     __syncthreads();
-    u64 c[2], w[2];
     int bin[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int at = tid + i * kThreads;
-      c[i] = at < n ? s.list[at] : 0ull;
-      w[i] = at < n ? value_of_it(c[i]) : 0ull;
       bin[i] = w[i] ? bin_in(c[i]) : -1;
       if (w[i]) atomicAdd(&s.pick.hist[bin[i]], w[i]);
     }
@@ -742,30 +737,38 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
         const float per = (float)kBins / (float)(bin + 1);
         auto bin_in = [&](u64 c) { return min((int)(fminf(place_of(value_of((uint32_t)(c >> 32))), (float)kBins) * per), kBins - 1); };
         auto order_in = [](u64 c) { return c; };
-        u64 border = 0ull, sum[2];
-        if (by_count && !pick(n, (u64)min(k, n), bin_in, [](u64) { return 1ull; }, order_in, border)) return false;
-        auto sums = [&](u64 from) {   // this thread's weights of what stays
+        u64 border = 0ull, c[2], w[2], of[2], found;
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const u64 c = tid + i * kThreads < n ? s.list[tid + i * kThreads] : 0ull;
-            sum[i] = c > 0ull && c >= from ? weight_at(c) : 0ull;
-          }
+        for (int i = 0; i < 2; ++i) {
+          const int at = tid + i * kThreads;
+          c[i] = at < n ? s.list[at] : 0ull;
+          w[i] = at < n ? weight_at(c[i]) : 0ull;
+        }
+        __syncthreads();   // (the histograms of the row are read)
+        if (by_count) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) of[i] = tid + i * kThreads < n;
+          if (!pick(c, of, (u64)min(k, n), bin_in, order_in, border)) return false;
+        }
+        auto sums = [&](u64 from) {   // of: the weights of what stays; their sum
+#pragma unroll
+          for (int i = 0; i < 2; ++i) of[i] = c[i] >= from ? w[i] : 0ull;
           u64 all;
-          block_scan(sum[0] + sum[1], all);
+          block_scan(of[0] + of[1], all);
           return all;
         };
         if (by_weight) {
-          if (by_count) want = share_of(sums(border));
-          if (!pick(n, want, bin_in, [&](u64 c) { return c >= border ? weight_at(c) : 0ull; }, order_in, border)) return false;
+          const u64 all = sums(border);
+          if (by_count) want = share_of(all);
+          if (!pick(c, of, want, bin_in, order_in, border)) return false;
         }
-        const u64 from = max(last, border), total = sums(from);
+        const u64 total = sums(max(last, border));
         const float per_index = (float)kBins / (float)a.vocab;
-        u64 c;
-        if (!pick(n, times_fraction(total, u, false) + 1ull,
+        if (!pick(c, of, times_fraction(total, u, false) + 1ull,
                   [&](u64 c) { return min((int)((float)(kAll - (uint32_t)c) * per_index), kBins - 1); },
-                  [&](u64 c) { return c >= from ? weight_at(c) : 0ull; }, [](u64 c) { return c << 32 | c >> 32; }, c))
+                  [](u64 c) { return c << 32 | c >> 32; }, found))
           return false;
-        if (tid == 0) answer((int)(kAll - (uint32_t)c), value_of((uint32_t)(c >> 32)), total);
+        if (tid == 0) answer((int)(kAll - (uint32_t)found), value_of((uint32_t)(found >> 32)), total);
         return true;
       };
       // few: a thread per value goes through all of them, and knows how many and what weights come before its own
