@@ -13,11 +13,11 @@
 // token is gone through again.  Where even the bin holds more (thousands of nearly equal logits), a
 // radix selection over the keys' four bytes finds the border.
 //
-// Measured (replays from a graph): one row of 65536 bf16 logits under top-k 40, top-p and min-p 12.2 us, a chain of four
-// barriers of the cluster (800 to 1500 cycles each) and what lies between; 64 rows of 128001 fp32 logits under top-p 0.9 61
-// us, of which the histogram takes 21 (84 instructions a logit, 50 of them its weight, at two thirds of the issue
-// rate), the list and the sums 14, the first pass 5.5; the same without limits 33, with top-k 50 28, with top-k 3000
-// and top-p 75, all logits equal 467.
+// Measured (replays from a graph): one row of 65536 bf16 logits under top-k 40, top-p and min-p 13 us, a chain of four
+// barriers of the cluster (1000 cycles each) and what lies between, a thousand here and there; 24 rows of 32003 under
+// settings of their own 30; 64 rows of 128001 fp32 logits under top-p 0.9 65 us, of which the histogram takes 21 (84
+// instructions a logit, 50 of them its weight, at two thirds of the issue rate), the list and the sums 14, the first
+// pass 5.5; the same without limits 33, with top-k 50 29, with top-k 3000 and top-p 75, all logits equal 467.
 #include <algorithm>
 
 #include "common.cuh"
@@ -114,7 +114,7 @@ __device__ __forceinline__ float2 log_of(float p, const u64* table) {
 }
 
 // floor(f * s), or the next whole number at or above, for a finite f >= 0
-__device__ __forceinline__ u64 times_fraction(u64 s, float f, bool up) {
+__device__ __noinline__ u64 times_fraction(u64 s, float f, bool up) {
   const uint32_t bits = __float_as_uint(f), e = bits >> 23;
   const u64 mant = e ? (bits & 0x7fffffu) | 0x800000u : bits & 0x7fffffu;
   const int shift = 150 - (int)(e ? e : 1u);   // f = mant * 2^-shift
@@ -181,6 +181,71 @@ struct DrawShared {
   u64 sel, sel_before, sel_in;
   uint32_t sel_bin, few_n, listed, counts[kRanks], found_run;
 };
+
+// What is not in a loop over the row is called, not inlined: it runs a few times a launch, and its instructions are
+// fetched once (the times are the same, the code a third less).
+
+// Sum of x over the threads before this one, and over the CTA.
+__device__ __noinline__ ulonglong2 scan_block(DrawShared& s, u64 x) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  u64 upto = x;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const u64 up = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += up;
+  }
+  __syncthreads();
+  if (lane == 31) s.warp_a[warp] = upto;
+  __syncthreads();
+  const u64 w = s.warp_a[lane];
+  u64 ws = w;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const u64 up = __shfl_up_sync(0xffffffffu, ws, o);
+    if (lane >= o) ws += up;
+  }
+  return make_ulonglong2(__shfl_sync(0xffffffffu, ws - w, warp) + upto - x, __shfl_sync(0xffffffffu, ws, 31));
+}
+
+__device__ __noinline__ u64 weight_of(const Weigher& weigh, u64 order, const u64* table) {
+  return weigh(value_of((uint32_t)(order >> 32)), table);
+}
+
+// Of values c with weights w, two to a thread, that at which the weights, summed from the largest down in the order
+// of c (or, by_index, of their index), reach `target`: a histogram by bins (of kBins, monotone), then the values of the
+// bin that holds it, each with the sum of those before it.  0: the bin has more than 256 of them.
+__device__ __noinline__ u64 pick(DrawShared& s, ulonglong2 c, ulonglong2 w, u64 target, int bin0, int bin1, bool by_index) {
+  const int tid = threadIdx.x;
+  if (tid < kBins) s.pick.hist[tid] = 0ull;
+  if (tid == 0) s.few_n = 0u;
+  __syncthreads();
+  if (w.x) atomicAdd(&s.pick.hist[bin0], w.x);
+  if (w.y) atomicAdd(&s.pick.hist[bin1], w.y);
+  __syncthreads();
+  const u64 in = tid < kBins ? s.pick.hist[tid] : 0ull, cum = scan_block(s, in).x;
+  if (cum < target && cum + in >= target) s.sel_bin = tid, s.sel_before = cum;
+  __syncthreads();
+#pragma unroll 1
+  for (int i = 0; i < 2; ++i)
+    if ((i ? w.y : w.x) && (i ? bin1 : bin0) == (int)s.sel_bin) {
+      const uint32_t at = atomicAdd(&s.few_n, 1u);
+      if (at < 256u) s.pick.few[at] = i ? c.y : c.x, s.few_weights[at] = i ? w.y : w.x;
+    }
+  __syncthreads();
+  const int few = (int)s.few_n;
+  if (few > 256) return 0ull;
+  if (tid < few) {
+    const u64 mine = s.pick.few[tid], order = by_index ? mine << 32 : mine;
+    u64 before = s.sel_before;
+    for (int j = 0; j < few; ++j) {
+      const u64 other = s.pick.few[j];
+      before += (by_index ? other << 32 : other) > order ? s.few_weights[j] : 0ull;
+    }
+    if (before < target && before + s.few_weights[tid] >= target) s.sel = mine;
+  }
+  __syncthreads();
+  return s.sel;
+}
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
@@ -270,23 +335,9 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
   };
   // sum of x over the threads before this one and, in all, over the CTA
   auto block_scan = [&](u64 x, u64& all) {
-    u64 upto = x;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const u64 up = __shfl_up_sync(kAll, upto, o);
-      if (lane >= o) upto += up;
-    }
-    __syncthreads();
-    if (lane == 31) s.warp_a[warp] = upto;
-    __syncthreads();
-    u64 w = s.warp_a[lane], ws = w;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const u64 up = __shfl_up_sync(kAll, ws, o);
-      if (lane >= o) ws += up;
-    }
-    all = __shfl_sync(kAll, ws, 31);
-    return __shfl_sync(kAll, ws - w, warp) + upto - x;
+    const ulonglong2 r = scan_block(s, x);
+    all = r.y;
+    return r.x;
   };
 
   // the largest logit, the least finite one, and what is no number: +inf and NaN are the largest as signed words, or, with
@@ -455,7 +506,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
     s.sorted[2 * tid] = x, s.sorted[2 * tid + 1] = y;   // (threads past `size` hold zeros throughout)
     __syncthreads();
   };
-  auto weight_at = [&](u64 order) { return weigh(value_of((uint32_t)(order >> 32)), s.table); };
+  auto weight_at = [&](u64 order) { return weight_of(weigh, order, s.table); };
   // Of s.sorted's first n the one at which the weights from the first on, `before` being those before them, reach
   // `want` (the last one if they do not).  two: this thread's two weights.
   auto reach = [&](int n, u64 before, const u64* two, u64 want) {
@@ -467,43 +518,6 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
     else if (cum + two[0] < want && cum + two[0] + two[1] >= want) s.sel = s.sorted[2 * tid + 1];
     __syncthreads();
     return s.sel;
-  };
-  // Of values c with weights w, two to a thread, that at which the weights, summed from the largest order_in(c) down,
-  // reach `target`: a histogram by bin_in (of kBins, monotone), then the values of the bin that holds it, each with
-  // the sum of those before it.  false: the bin has more than 256 of them.
-  auto pick = [&](const u64* c, const u64* w, u64 target, auto bin_in, auto order_in, u64& found) {
-    if (tid < kBins) s.pick.hist[tid] = 0ull;
-    if (tid == 0) s.few_n = 0u;
-    __syncthreads();
-    int bin[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      bin[i] = w[i] ? bin_in(c[i]) : -1;
-      if (w[i]) atomicAdd(&s.pick.hist[bin[i]], w[i]);
-    }
-    __syncthreads();
-    u64 all;
-    const u64 in = tid < kBins ? s.pick.hist[tid] : 0ull, cum = block_scan(in, all);
-    if (cum < target && cum + in >= target) s.sel_bin = tid, s.sel_before = cum;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      if (bin[i] == (int)s.sel_bin) {
-        const uint32_t at = atomicAdd(&s.few_n, 1u);
-        if (at < 256u) s.pick.few[at] = c[i], s.few_weights[at] = w[i];
-      }
-    __syncthreads();
-    const int few = (int)s.few_n;
-    if (few > 256) return false;
-    if (tid < few) {
-      const u64 mine = s.pick.few[tid], order = order_in(mine);
-      u64 before = s.sel_before;
-      for (int j = 0; j < few; ++j) before += order_in(s.pick.few[j]) > order ? s.few_weights[j] : 0ull;
-      if (before < target && before + s.few_weights[tid] >= target) s.sel = mine;
-    }
-    __syncthreads();
-    found = s.sel;
-    return true;
   };
   auto share_of = [&](u64 all) { return max(1ull, p > 0.f ? times_fraction(all, p, true) : 0ull); };   // top-p's
 
@@ -734,21 +748,25 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
       };
       // by histograms of the list
       auto by_picks = [&] {
-        const float per = (float)kBins / (float)(bin + 1);
-        auto bin_in = [&](u64 c) { return min((int)(fminf(place_of(value_of((uint32_t)(c >> 32))), (float)kBins) * per), kBins - 1); };
-        auto order_in = [](u64 c) { return c; };
-        u64 border = 0ull, c[2], w[2], of[2], found;
+        const float per = (float)kBins / (float)(bin + 1), per_index = (float)kBins / (float)a.vocab;
+        u64 border = 0ull, c[2], w[2], of[2];
+        int by_key[2], by_index[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int at = tid + i * kThreads;
           c[i] = at < n ? s.list[at] : 0ull;
           w[i] = at < n ? weight_at(c[i]) : 0ull;
+          by_key[i] = min((int)(fminf(place_of(value_of((uint32_t)(c[i] >> 32))), (float)kBins) * per), kBins - 1);
+          by_index[i] = min((int)((float)(kAll - (uint32_t)c[i]) * per_index), kBins - 1);
         }
         __syncthreads();   // (the histograms of the row are read)
+        auto pick_of = [&](u64 target, const int* bins, bool index) {
+          return pick(s, make_ulonglong2(c[0], c[1]), make_ulonglong2(of[0], of[1]), target, bins[0], bins[1], index);
+        };
         if (by_count) {
 #pragma unroll
           for (int i = 0; i < 2; ++i) of[i] = tid + i * kThreads < n;
-          if (!pick(c, of, (u64)min(k, n), bin_in, order_in, border)) return false;
+          if (!(border = pick_of((u64)min(k, n), by_key, false))) return false;
         }
         auto sums = [&](u64 from) {   // of: the weights of what stays; their sum
 #pragma unroll
@@ -760,14 +778,11 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
         if (by_weight) {
           const u64 all = sums(border);
           if (by_count) want = share_of(all);
-          if (!pick(c, of, want, bin_in, order_in, border)) return false;
+          if (!(border = pick_of(want, by_key, false))) return false;
         }
         const u64 total = sums(max(last, border));
-        const float per_index = (float)kBins / (float)a.vocab;
-        if (!pick(c, of, times_fraction(total, u, false) + 1ull,
-                  [&](u64 c) { return min((int)((float)(kAll - (uint32_t)c) * per_index), kBins - 1); },
-                  [](u64 c) { return c << 32 | c >> 32; }, found))
-          return false;
+        const u64 found = pick_of(times_fraction(total, u, false) + 1ull, by_index, true);
+        if (!found) return false;
         if (tid == 0) answer((int)(kAll - (uint32_t)found), value_of((uint32_t)(found >> 32)), total);
         return true;
       };
