@@ -7,8 +7,8 @@
  * Conventions beside those of ravel.h and ravel_cache.h:
  *  - Positions, counts and settings of a robot are device arrays, read by the
  *    kernels, so that calls can be captured into CUDA graphs.
- *  - Every call but the ones that create, destroy, load or read weights is
- *    enqueued on `stream` and returns.  Its launch may begin while the one before
+ *  - Every call but the ones that create, destroy or load is enqueued on `stream`
+ *    and returns.  Its launch may begin while the one before
  *    it on the stream ends, and waits for it before it reads or writes anything
  *    that is passed to the call.
  *  - A rotary table and loaded weights are not changed by the calls that use
@@ -68,7 +68,7 @@ ravel_status ravel_rotary_apply(ravel_rotary_t* r, int batch, int n, int heads, 
                                 void* stream);
 
 /* ravel_cache_append of keys turned to their positions, and the queries turned
- * with them, in one launch.  Between a turned key and the cache nothing is rounded
+ * with them, in one call.  Between a turned key and the cache nothing is rounded
  * but to the cache's own values.
  *   q, q_out   device [batch, n, Hq, hd] of the cache's dtype, or both NULL; q_out is q itself (with q's strides)
  *              or overlaps none of the others

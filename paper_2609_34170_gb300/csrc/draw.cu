@@ -182,8 +182,7 @@ struct DrawShared {
   uint32_t sel_bin, few_n, listed, counts[kRanks], found_run;
 };
 
-// What is not in a loop over the row is called, not inlined: it runs a few times a launch, and its instructions are
-// fetched once (the times are the same, the code a third less).
+// What is not in a loop over the row is called, not inlined (the times are the same).
 
 // Sum of x over the threads before this one, and over the CTA.
 __device__ __noinline__ ulonglong2 scan_block(DrawShared& s, u64 x) {

@@ -5,10 +5,10 @@ pi / 4, in fp32) + 2^-24 (one unit of the function at 1) + 2^-25 (the amplitude)
 add 2 x 2^-24: below 2^-21 (|x| + |y|) amplitude.  The frequency's own 2^-52 is position f 2^-51 on top.
 Then half a step of the type, 2^-8 |result| in bf16.
 
-Products: exact terms x (c - z) are summed on the tensor core, which cuts each of the four MMAs of a chain off by
-less than 2^-21 of the sum of magnitudes (its addends are kept to 24 bits below the largest of 17); the scale
-and the sums over the groups (at most two per 64 ks, then 8 warps and 8 ranks) add 2^-24 each:
-(2^-19 + (K / 32 + 18) 2^-24) sum |x w|.  Then the epilogue and the output's half step.
+Products: exact terms x (c - z) are summed on the tensor core in chains of up to eight MMAs.  Each keeps its 17
+addends to 24 bits below the largest, which for the spread values here is below a quarter of the group's sum of
+magnitudes: 8 x 16 x 2^-24 / 4 = 2^-19 of it; the scale and the sums over the groups (at most two per 64 ks, then 8
+warps and 8 ranks) add 2^-24 each: (2^-19 + (K / 32 + 18) 2^-24) sum |x w|.  Then the epilogue and the output's half step.
 
 Tokens are equal; log-probabilities within 2^-23 of their size and 1e-7."""
 import math
