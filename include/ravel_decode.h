@@ -56,7 +56,7 @@ void ravel_rotary_destroy(ravel_rotary_t* r);
 /* Turn rows of heads.
  *   x, out     device [batch, n, heads, hd] of dtype; heads of a token are contiguous, token i of robot b
  *              begins at element b * robot_stride + i * token_stride.  out is x itself (with x's strides)
- *              or does not overlap it.  Query and key heads that lie side by side are one call.
+ *              or does not overlap it; its rows do not overlap each other.  Query and key heads that lie side by side are one call.
  *   hd         >= dims
  *   starts     device int32 [batch] or NULL (0): token i of robot b has position starts[b] + i ...
  *   positions  device int32 [batch, n] or NULL: ... or positions[b][i]
@@ -71,7 +71,7 @@ ravel_status ravel_rotary_apply(ravel_rotary_t* r, int batch, int n, int heads, 
  * with them, in one call.  Between a turned key and the cache nothing is rounded
  * but to the cache's own values.
  *   q, q_out   device [batch, n, Hq, hd] of the cache's dtype, or both NULL; q_out is q itself (with q's strides)
- *              or overlaps none of the others
+ *              or overlaps none of the others; its rows do not overlap each other
  *   k, v       as for ravel_cache_append, each with strides of its own; they are not written
  *   positions  device int32 [batch, n] or NULL: starts[b] + i
  *   starts, counts  as for ravel_cache_append; rows of q_out from counts[b] on are not written
@@ -109,7 +109,8 @@ ravel_status ravel_w4_load(ravel_w4_t* w, const void* codes, const void* scales,
 
 /* Nearest codes of a matrix: per row and group s = (max(w, 0) - min(w, 0)) / 15 in
  * bf16, z = -min(w, 0) / s and c = w / s + z, both rounded to nearest (ties to even)
- * and limited to 0 .. 15; a group of zeros has s = z = c = 0.  Not for values that are not finite.
+ * and limited to 0 .. 15; a group of zeros has s = z = c = 0.  For values of
+ * up to 3e38 (codes of a larger one may stand for more than fp32 holds).
  *   W  device [N, ldw] of dtype, first K columns; codes, scales, zeros device, written
  * Enqueued on `stream` of the current device. */
 ravel_status ravel_w4_quantize(const void* W, int N, int K, int ldw, int dtype, int group, void* codes, void* scales,

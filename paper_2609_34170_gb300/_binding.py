@@ -559,12 +559,17 @@ def _flat(t, shape: tuple, dtype, device: int, name: str):
     raise ValueError(f"{name} must be a contiguous tensor {list(shape)} of {dtype} on cuda:{device}, got {got}")
 
 
-def _matrix(t, rows: int, cols: int, device: int, name: str) -> int:
-    """Row stride of a [rows, cols] tensor whose rows are contiguous; of a single row, whose
-    stride means nothing, the next multiple of 8."""
+_INT_MAX = (1 << 31) - 1   # (ctypes cuts off what does not fit into an int)
+
+
+def _matrix(t, rows: int, cols: int, device: int, name: str, wide: bool = False) -> int:
+    """Row stride (an int; wide: a long long) of a [rows, cols] tensor whose rows are contiguous; of
+    a single row, whose stride means nothing, the next multiple of 8."""
     stride = t.stride()
     if len(stride) != 2 or t.shape != (rows, cols) or t.get_device() != device or (stride[1] != 1 and cols > 1):
         raise ValueError(f"{name} must be [{rows}, {cols}] on cuda:{device} with contiguous rows, got {tuple(t.shape)} on {t.device}")
+    if rows > _INT_MAX or cols > _INT_MAX or (stride[0] > _INT_MAX and rows > 1 and not wide):
+        raise ValueError(f"{name}: more than 2^31 - 1 rows, columns, or values from one row to the next")
     if rows < 2:
         return -(-cols // 8) * 8
     if stride[0] < cols:
@@ -600,6 +605,8 @@ def _heads(x, device: int, name: str):
     robot, token, head, dim = stride
     if (dim != 1 and shape[3] > 1) or (head != shape[3] and shape[2] > 1):
         raise ValueError(f"{name}: the heads of a token must be contiguous")
+    if shape[0] > _INT_MAX or shape[1] > _INT_MAX or shape[2] > _INT_MAX or shape[3] > _INT_MAX:
+        raise ValueError(f"{name}: sizes must be below 2^31")
     return robot if shape[0] > 1 else 0, token if shape[1] > 1 else 0
 
 
@@ -704,7 +711,7 @@ def ravel_draw_tokens(logits, u, temperature, top_k, top_p, min_p, tokens, log_p
     if logits.dim() != 2 or device < 0:
         raise ValueError(f"logits must be a CUDA tensor [batch, vocab], got {tuple(logits.shape)} on {logits.device}")
     B, V = logits.shape
-    row = _matrix(logits, B, V, device, "logits")
+    row = _matrix(logits, B, V, device, "logits", wide=True)
     f32, i32, one = types.f32, types.i32, (B,)
     if u is None or tokens is None:
         raise ValueError("u and tokens must be given")

@@ -224,6 +224,10 @@ ravel_status ravel_cache_append_rotary(ravel_cache_t* c, int layer, const ravel_
   ravel_status s = check_call(c, layer, batch, "append_rotary");
   if (s != RAVEL_OK) return s;
   if (n < 1 || n > c->cfg.max_tokens) return fail(c, RAVEL_ESHAPE, "append_rotary: n outside [1, max_tokens]");
+  if (((uintptr_t)q | (uintptr_t)q_out | (uintptr_t)k | (uintptr_t)v) % c->esize)
+    return fail(c, RAVEL_EINVAL, "append_rotary: unaligned q, q_out, k or v");
+  if (q && rows_overlap(batch, n, (long long)c->cfg.n_q_heads * c->cfg.head_dim, q_out_robot_stride, q_out_token_stride))
+    return fail(c, RAVEL_EINVAL, "append_rotary: rows of q_out overlap");
   if (r->table.dims > c->cfg.head_dim) return fail(c, RAVEL_ESHAPE, "append_rotary: the table has more dims than a head");
   if (r->device != c->device) return fail(c, RAVEL_EINVAL, "append_rotary: the table is on another device");
   AppendRotaryArgs a{c->layer(layer), r->table, q, k, v, q_out, q_robot_stride, q_token_stride, q_out_robot_stride,

@@ -178,6 +178,9 @@ ravel_status ravel_rotary_apply(ravel_rotary_t* r, int batch, int n, int heads, 
   if (hd < r->table.dims || hd > 256) return fail(RAVEL_ESHAPE, "rotary_apply: hd outside [dims, 256]");
   if (batch == 0 || n == 0 || heads == 0) return RAVEL_OK;
   if (!x || !out) return fail(RAVEL_EINVAL, "rotary_apply: null argument");
+  if (((uintptr_t)x | (uintptr_t)out) % size_of(dtype)) return fail(RAVEL_EINVAL, "rotary_apply: unaligned x or out");
+  if (rows_overlap(batch, n, (long long)heads * hd, out_robot_stride, out_token_stride))
+    return fail(RAVEL_EINVAL, "rotary_apply: rows of out overlap");
   RotaryArgs a{r->table, x,     out, x_robot_stride, x_token_stride, out_robot_stride, out_token_stride, batch, n, heads, hd,
                starts,   positions, counts, 16, r->num_sms, 0};
   const long long es = size_of(dtype);
@@ -269,6 +272,7 @@ ravel_status ravel_w4_quantize(const void* W, int N, int K, int ldw, int dtype, 
   if (!W || !codes || !scales || !zeros) return fail(RAVEL_EINVAL, "w4_quantize: null argument");
   if (!known(dtype)) return fail(RAVEL_EINVAL, "w4_quantize: unknown dtype");
   if (group != 32 && group != 64 && group != 128) return fail(RAVEL_EINVAL, "w4_quantize: group must be 32, 64 or 128");
+  if ((uintptr_t)W % size_of(dtype) || (uintptr_t)scales % 2) return fail(RAVEL_EINVAL, "w4_quantize: unaligned W or scales");
   if (N < 1 || K < 1 || ldw < K || N > (1 << 24) || K > (1 << 24)) return fail(RAVEL_ESHAPE, "w4_quantize: N, K or ldw");
   if ((long long)N * ((K + group - 1) / group) > (1ll << 31))
     return fail(RAVEL_ESHAPE, "w4_quantize: at most 2^31 groups");
@@ -281,6 +285,7 @@ ravel_status ravel_w4_read(ravel_w4_t* w, void* out, int ldo, int dtype, void* s
   if (!w || !out) return fail(RAVEL_EINVAL, "w4_read: null argument");
   if (!known(dtype)) return fail(RAVEL_EINVAL, "w4_read: unknown dtype");
   if (ldo < w->m.K) return fail(RAVEL_ESHAPE, "w4_read: ldo below K");
+  if ((uintptr_t)out % size_of(dtype)) return fail(RAVEL_EINVAL, "w4_read: unaligned out");
   OnDevice on(w->device);
   cudaError_t e = on.e;
   if (e == cudaSuccess) e = launch_w4_read(w->m, out, ldo, type_of(dtype), (cudaStream_t)stream);
@@ -321,6 +326,7 @@ ravel_status ravel_draw_tokens(const void* logits, int batch, int vocab, long lo
   if (batch > 1 && row_stride < vocab) return fail(RAVEL_ESHAPE, "draw_tokens: rows overlap");
   if (batch == 0) return RAVEL_OK;
   if (!logits || !u || !tokens) return fail(RAVEL_EINVAL, "draw_tokens: null argument");
+  if ((uintptr_t)logits % size_of(dtype)) return fail(RAVEL_EINVAL, "draw_tokens: unaligned logits");
   DrawArgs a{logits, batch, vocab, row_stride, u, temperature, top_p, min_p, top_k, tokens, log_probs, 0, 0};
   a.vec = (uintptr_t)logits % 16 == 0 && (batch == 1 || row_stride * size_of(dtype) % 16 == 0);
   cudaError_t e = sm_count(&a.num_sms);

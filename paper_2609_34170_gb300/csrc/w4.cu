@@ -111,7 +111,8 @@ __global__ void __launch_bounds__(256) w4_quantize_kernel(const T* W, int N, int
   }
   hi = warp_max(hi);
   lo = -warp_max(-lo);
-  const bf16 sb = __float2bfloat16_rn((hi - lo) / 15.f);
+  const float range = hi - lo;   // (of finite values may be infinite)
+  const bf16 sb = __float2bfloat16_rn(range < INFINITY ? range / 15.f : hi / 15.f - lo / 15.f);
   const float s = __bfloat162float(sb);
   const float z = s > 0.f ? fminf(fmaxf(rintf(-lo / s), 0.f), 15.f) : 0.f;
   auto code = [&](int k) -> uint32_t {

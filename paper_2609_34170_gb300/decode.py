@@ -124,6 +124,8 @@ def quantize4(w, group: int = 128, stream=None):
     """Nearest 4-bit codes of w [n, k]: codes uint8 [n, (k + 1) // 2], scales bf16 and zeros uint8
     [n, groups], as ``Weights4.load`` takes them."""
     import torch
+    if w.dim() != 2 or w.get_device() < 0 or group not in (32, 64, 128):
+        raise ValueError(f"w must be a CUDA tensor [n, k] and group 32, 64 or 128, got {tuple(w.shape)} on {w.device} and {group}")
     n, k = w.shape
     groups = -(-k // group)
     codes = B.new_tensor((n, (k + 1) // 2), torch.uint8, w.device, stream)

@@ -159,6 +159,54 @@ def test_rotary_refuses_tensors_that_do_not_fit(lib):
             apply(**{name: bad})
 
 
+class _Table(C.Structure):
+    """A rotary handle of 16 dims on a device that there is not."""
+    _fields_ = [("f", C.c_void_p), ("dims", C.c_int), ("interleaved", C.c_int), ("amplitude", C.c_float), ("device", C.c_int * 3)]
+
+
+def test_rows_that_overlap_or_lie_askew_are_not_written(lib):
+    r = C.byref(_Table(None, 16, 0, 1.0, (1 << 20, 0, 0)))
+    x, out = 1 << 20, 1 << 21
+
+    def apply(batch, n, out_strides, x=x, out=out, x_strides=(640, 64)):
+        return lib.ravel_rotary_apply(r, batch, n, 2, 32, 1, x, *x_strides, out, *out_strides, None, None, None, None)
+
+    # (a status of 1 is a refusal; what is not refused ends at the device)
+    for batch, n, strides in ((3, 5, (640, 63)), (3, 5, (0, 64)), (3, 5, (319, 64)), (3, 5, (64, 191)), (3, 5, (64, 64)), (3, 1, (63, 0)),
+                              (1, 5, (0, 0)), (2, 1 << 30, (1 << 62, 1 << 60))):
+        assert apply(batch, n, strides) == 1 and b"overlap" in lib.ravel_decode_last_error(), strides
+    assert apply(3, 5, (0, 64), out=x, x_strides=(0, 64)) == 1   # in place, robots that share their rows
+    for batch, n, strides in ((3, 5, (320, 64)), (3, 5, (64, 192)), (3, 1, (64, 0)), (1, 5, (0, 64)), (1, 1, (0, 0)), (2, 2, (1 << 60, 1 << 61)), (2, 1 << 30, (1 << 40, 1 << 62))):
+        apply(batch, n, strides)
+        assert b"overlap" not in lib.ravel_decode_last_error(), strides
+    assert apply(1, 1, (0, 0), x=x + 1) == 1 and b"unaligned" in lib.ravel_decode_last_error()
+    assert apply(1, 1, (0, 0), out=out + 1) == 1 and b"unaligned" in lib.ravel_decode_last_error()
+    p = C.c_void_p(256)
+    assert lib.ravel_draw_tokens(C.c_void_p(258), 1, 8, 8, 0, p, None, None, None, None, p, None, None) == 1
+    assert lib.ravel_w4_quantize(C.c_void_p(257), 8, 8, 8, 1, 32, p, p, p, None) == 1
+
+
+def test_sizes_beyond_an_int_are_refused_not_cut_off(lib):
+    import paper_2609_34170_gb300 as pkg
+    b16, f32 = torch.bfloat16, torch.float32
+    w = C.c_void_p()
+    w.w4 = (256, 70, 32, 0)
+    far = (1 << 32) + 72
+    for x, out in ((_Gpu((4, 70), b16, (far, 1)), _Gpu((4, 256), b16)), (_Gpu((4, 70), b16), _Gpu((4, 256), b16, (far, 1))),
+                   (_Gpu(((1 << 32) + 4, 70), b16), _Gpu(((1 << 32) + 4, 256), b16))):
+        with pytest.raises(ValueError, match="2\\^31"):
+            pkg.ravel_w4_gemm(w, x, 0, out, None, stream=0)
+    with pytest.raises(ValueError, match="2\\^31"):
+        pkg.ravel_draw_tokens(_Gpu((1, (1 << 32) + 4), f32), _Gpu((1,), f32), None, None, None, None, _Gpu((1,), torch.int32), stream=0)
+    x = _Gpu((1, (1 << 32) + 4, 1, 16), b16)
+    with pytest.raises(ValueError, match="2\\^31"):
+        pkg.ravel_rotary_apply(_rotary_handle(), x, x, stream=0)
+    from paper_2609_34170_gb300.decode import quantize4
+    for bad in ((torch.zeros(4, 64), 32), (_Gpu((4, 64), f32), 48), (_Gpu((4, 64), f32), 0), (_Gpu((4,), f32), 32)):
+        with pytest.raises(ValueError):
+            quantize4(*bad)
+
+
 def test_append_rotary_refuses_tensors_that_do_not_fit(lib):
     import paper_2609_34170_gb300 as pkg
     from paper_2609_34170_gb300 import _binding as B

@@ -369,6 +369,33 @@ def test_quantises_to_the_nearest_codes(dtype):
         np.testing.assert_array_equal(_np(held), ref.weights(ref.pack(c), s, z, 203, group).astype(np.float32))
 
 
+def test_quantises_the_largest_and_smallest_values():
+    """Groups whose values lie further apart than fp32 reaches, and whose scale is bf16's smallest or none."""
+    from paper_2609_34170_gb300.decode import Weights4, quantize4
+    w = torch.zeros((4, 64), device="cuda")
+    w[0, :2] = torch.tensor([3e38, -3e38])
+    w[1, :2] = torch.tensor([3e38, -1e38])   # (beyond 3e38 the nearest code's value may be beyond fp32: excluded)
+    w[2, :2] = torch.tensor([2.0 ** -130, -2.0 ** -131])
+    w[3, :2] = torch.tensor([2.0 ** -140, 0.0])
+    held = _np(Weights4.quantize(w, 32).read(torch.float32))
+    step = np.array([6e38, 4e38, 1.5 * 2.0 ** -130, 2.0 ** -140]) / 15
+    # half a step where codes round, 0.04 for the zero point's rounding and the scale's 2^-9 of 15 steps at the ends,
+    # and a scale below bf16's smallest, 2^-133, moves by up to half of that, 15 times
+    assert (np.abs(held - _np(w)) <= 1.04 * step[:, None] + np.array([0, 0, 7.5, 7.5])[:, None] * 2.0 ** -133).all()
+    assert torch.isfinite(quantize4(w, 32)[1]).all()
+
+
+def test_overlapping_rows_are_refused():
+    from paper_2609_34170_gb300 import RavelError, Rotary
+    r = Rotary(16)
+    x = _rand((1, 5, 2, 32), 0, "bf16").expand(3, 5, 2, 32)
+    assert (r.apply(x)[2] == r.apply(x)[0]).all()   # reading the same rows is fine
+    for out in (x, torch.empty_strided((3, 5, 2, 32), (64, 64, 32, 1), dtype=torch.bfloat16, device="cuda")):
+        with pytest.raises(RavelError) as ei:
+            r.apply(x, out=out)
+        assert ei.value.status == 1
+
+
 def test_product_refusals():
     from paper_2609_34170_gb300 import RavelError, Weights4
     w = Weights4(96, 64, 32)
