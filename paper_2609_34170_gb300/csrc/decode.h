@@ -48,9 +48,10 @@ cudaError_t launch_cache_append_rotary(const AppendRotaryArgs& a, Dtype dt, cuda
 
 // A matrix of 4-bit weights in the order in which the tensor cores' fragments
 // take it (w4.cu): tiles of 16 rows, blocks of 64 columns.
+constexpr int kPadGroups = 8;
 struct W4Matrix {
   uint4* codes;       // [tiles][kblocks][32 lanes]
-  uint2* sz;          // [tiles][groups][8]: (scale, 128 + zero) of rows g and g + 8
+  uint2* sz;          // [tiles][groups][8]: (scale, 128 + zero) of rows g and g + 8; kPadGroups groups of zeros behind
   int N, K, group;
   int tiles, kblocks, groups;   // tiles: an even number
 };

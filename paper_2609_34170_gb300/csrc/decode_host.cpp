@@ -208,7 +208,7 @@ ravel_status ravel_w4_create(int N, int K, int group, int device, ravel_w4_t** o
   m.tiles = (N + 31) / 32 * 2;
   m.kblocks = (K + 63) / 64;
   m.groups = (K + group - 1) / group;
-  const size_t codes = (size_t)m.tiles * m.kblocks * 512, sz = (size_t)m.tiles * m.groups * 64;
+  const size_t codes = (size_t)m.tiles * m.kblocks * 512, sz = ((size_t)m.tiles * m.groups + kPadGroups) * 64;
   OnDevice on(device);
   cudaError_t e = on.e;
   if (e == cudaSuccess) e = sm_count(&w->num_sms);

@@ -17,7 +17,7 @@ namespace {
 // piece of a token's row is 16 contiguous bytes, and no operand of B passes through shared memory to be
 // put into order.  Two MMAs (s = 0, 1) take the 32: of the lane's eight ks, 4s and 4s + 1 are the k
 // pair of the registers a0 (row g), a1 (row g + 8) and b0, and 4s + 2, 4s + 3 that of a2, a3 and b1.
-// So a lane's weights of two rows and two 32s are 32 codes, one uint4: word 2 * (which 32) + s holds in
+// So a lane's weights of two rows and two 32s are 32 codes, one uint4: word 2s + (which 32) holds in
 // nibble i the first k of register ai and in nibble 4 + i the second, and a warp reads 16 rows x 64 ks in
 // one contiguous 512-byte load.
 constexpr int kWarps = 8;
@@ -26,7 +26,7 @@ constexpr int kPitch = 36;   // floats of a token's 32 rows: lanes of a store la
 __device__ __forceinline__ void code_place(int lane, int word, int nibble, int* row, int* k) {
   const int g = lane >> 2, q = lane & 3, i = nibble & 3;
   *row = g + (i & 1) * 8;
-  *k = (word >> 1) * 32 + q * 8 + (word & 1) * 4 + (i >> 1) * 2 + (nibble >> 2);
+  *k = (word & 1) * 32 + q * 8 + (word >> 1) * 4 + (i >> 1) * 2 + (nibble >> 2);
 }
 
 // A thread per word: 8 codes from wherever they are.
@@ -192,7 +192,7 @@ struct Operand {
   uint32_t A[2][4][4];
   float s0[2][G32 ? 2 : 1], s8[2][G32 ? 2 : 1];
   __device__ __forceinline__ void set(const uint4* codes, const uint2* sz, int t) {   // sz: of the first 32, of the second
-    const uint32_t c[4] = {codes->x, codes->y, codes->z, codes->w};
+    const uint32_t c[4] = {codes->x, codes->z, codes->y, codes->w};
 #pragma unroll
     for (int h = 0; h < (G32 ? 2 : 1); ++h) {
       s0[t][h] = __uint_as_float(sz[h].x & 0xffff0000u);

@@ -31,30 +31,35 @@ namespace {
 // piece, and a warp that sums 500 on scales and 250 on a piece's sums.  On the way here: tokens by asynchronous copies of
 // four warps 225 (their addresses took longer than the MMAs), pieces of 64 ks 185, A in tensor memory the
 // same as in shared memory, mma.sync with eight pairs of tiles sharing the tokens 267 (its MMAs alone are 113).
-constexpr int kPieces = 3;      // pieces of A and B in the making
-constexpr int kCodeRing = 2;    // pieces of codes on their way to a warp
-constexpr int kScaleHalf = 4;   // groups' scales that come to a thread together, while as many are used
+constexpr int kSets = 3;        // of four warps that widen a piece
+constexpr int kScaleBatch = kPadGroups, kScaleBufs = 3;   // groups of a unit whose scales come together; batches there is room for
+constexpr int kScalePitch = kScaleBatch * 64 + 64;         // bytes of a tile's: rows of two tiles in different banks
 constexpr uint32_t kTcCols = 512;
 constexpr int kSumPitch = 132;  // floats of a token's 128 rows
 constexpr int kUpPitch = 68;    // of its 64 up rows
 constexpr size_t kTcSmem = 227 * 1024;   // the SM's, as its tensor memory: CTAs of a cluster wait for one another with both taken
+constexpr int kSumWarp = 4 * kSets, kXWarp = kSumWarp + 8, kMmaWarp = kXWarp + 1, kTcThreads = 32 * (kMmaWarp + 1);
 
 // GS: 32s of ks in a group
 template <int NTOK, int GS>
 struct TcShape {
-  static constexpr int kSets = GS == 1 ? 2 : 3;          // of four warps that widen a piece (as many as have room for codes)
-  static constexpr int kSumWarp = 4 * kSets, kXWarp = kSumWarp + 8, kMmaWarp = kXWarp + 1, kThreads = 32 * (kMmaWarp + 1);
-  static constexpr int kGroups = 4 / GS;                 // of a piece
-  // pieces whose accumulators there are; where they are as many as the pieces in the making, one barrier says of a
-  // piece that its operands are free and its accumulators full (who waits for it is never a round behind: a piece is made,
-  // and its accumulators written, only when both waits for the one three before have ended)
-  static constexpr bool kOne = (int)kTcCols / NTOK / kGroups >= kPieces;
-  static constexpr int kSlots = kOne ? kPieces : (int)kTcCols / NTOK / kGroups;
+  static constexpr int kBlocks = 2;                      // of 64 ks in a piece
+  static constexpr int kGroups = 2 * kBlocks / GS;       // of a piece
+  static constexpr int kColsA = 32 * kBlocks, kColsAcc = kGroups * NTOK;   // of tensor memory
+  // pieces in the making, and pieces whose accumulators there are; where they are as many, one barrier says of a
+  // piece that its operands are free and its accumulators full, and one that its operands are there and its accumulators
+  // free (who waits for them is never a round behind: a piece is made, and its accumulators written, only when both
+  // waits for the one before it in its place have ended)
+  static constexpr int kFit = (int)kTcCols / (kColsA + kColsAcc);
+  static constexpr bool kOne = kFit >= 3;
+  static constexpr int kPieces = kOne ? (kFit < 4 ? kFit : 4) : 3;
+  static constexpr int kSlots = kOne ? kPieces : ((int)kTcCols - kPieces * kColsA) / kColsAcc;
+  static constexpr int kCodeRing = 4;                     // pieces of codes on their way to a warp
   struct Piece {
-    uint8_t a[2][128 * 128], x[2][NTOK * 128];           // swizzled rows of 128 bytes
+    uint8_t x[kBlocks][NTOK * 128];                      // swizzled rows of 128 bytes
   };
   struct Codes {
-    uint4 codes[2][2][32];                               // [64 ks][tile]
+    uint4 codes[kBlocks][2][32];                         // [64 ks][tile]
     uint2 sz[kGroups][2][8];
   };
   struct Shared {
@@ -63,9 +68,9 @@ struct TcShape {
       float sums[NTOK * kSumPitch];                      // for the other ranks, once every MMA is done
     };
     Codes ring[4 * kSets][kCodeRing];
-    uint32_t scale[2][256][kScaleHalf];
     float up[NTOK * kUpPitch];                           // GeGLU's up rows
-    uint64_t full[kPieces], empty[kPieces], acc_full[kSlots], acc_empty[kSlots], up_full, up_free, ended;
+    alignas(16) uint8_t scales[kScaleBufs][8][kScalePitch];
+    uint64_t scale_full[kScaleBufs], scale_empty[kScaleBufs], full[kPieces], empty[kPieces], acc_full[kSlots], acc_empty[kSlots], up_full, up_free, ended;
     uint32_t tmem;
   };
 };
@@ -78,6 +83,15 @@ __device__ __forceinline__ void fma_pair(float& x, float& y, uint32_t a, uint32_
       : "r"(a), "r"(b), "f"(s));
 }
 
+// 16 rows x 64 ks of A (lanes from those of at on): lane 4g + q's columns 2q, 2q + 1 of each 8 of rows g and g + 8.
+__device__ __forceinline__ void store_a(uint32_t at, const uint32_t (&v)[4][4]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.16x256b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(at),
+      "r"(v[0][0]), "r"(v[0][1]), "r"(v[0][2]), "r"(v[0][3]), "r"(v[1][0]), "r"(v[1][1]), "r"(v[1][2]), "r"(v[1][3]), "r"(v[2][0]),
+      "r"(v[2][1]), "r"(v[2][2]), "r"(v[2][3]), "r"(v[3][0]), "r"(v[3][1]), "r"(v[3][2]), "r"(v[3][3])
+      : "memory");
+}
+
 // A wait that tries some times before it looks at the clock.
 __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity) {
   for (int i = 0; i < 64; ++i)
@@ -86,10 +100,10 @@ __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity) {
 }
 
 template <int NTOK, int GS>
-__global__ void __launch_bounds__(TcShape<NTOK, GS>::kThreads, 1) w4_tc_kernel(const __grid_constant__ CUtensorMap x_map, W4Args a) {
+__global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_constant__ CUtensorMap x_map, W4Args a) {
   typedef TcShape<NTOK, GS> Shape;
-  constexpr int kSets = Shape::kSets, kSumWarp = Shape::kSumWarp, kXWarp = Shape::kXWarp, kMmaWarp = Shape::kMmaWarp;
-  constexpr int kGroups = Shape::kGroups, kSlots = Shape::kSlots;
+  constexpr int kPieces = Shape::kPieces, kSlots = Shape::kSlots, kBlocks = Shape::kBlocks, kGroups = Shape::kGroups;
+  constexpr int kCodeRing = Shape::kCodeRing;
   extern __shared__ __align__(1024) unsigned char tc_smem[];
   typename Shape::Shared& s = *(typename Shape::Shared*)tc_smem;
   const W4Matrix& w = a.w;
@@ -101,7 +115,7 @@ __global__ void __launch_bounds__(TcShape<NTOK, GS>::kThreads, 1) w4_tc_kernel(c
   const int ranks = (int)gridDim.z, rank = ranks > 1 ? (int)cluster_ctarank() : 0;
   const int row_tiles = (w.tiles + 7) / 8, units = row_tiles * ((a.M + NTOK - 1) / NTOK);
   // this rank's pieces
-  const int pieces = (w.kblocks + 1) / 2;
+  const int pieces = (w.kblocks + kBlocks - 1) / kBlocks;
   const int p0 = (int)((long long)pieces * rank / ranks), p1 = (int)((long long)pieces * (rank + 1) / ranks), pieces_here = p1 - p0;
   const int mine = (int)blockIdx.x < units ? (units - 1 - (int)blockIdx.x) / (int)gridDim.x + 1 : 0;   // units
 
@@ -122,17 +136,17 @@ __global__ void __launch_bounds__(TcShape<NTOK, GS>::kThreads, 1) w4_tc_kernel(c
       from_sz = w.sz + (size_t)(sz_t ? t1 : t0) * w.groups * 8 + (lane & 3) * 2;
     }
   };
-  // parts change places with the rows, so that eight lanes that read a part of eight rows hit all banks
-  const int put = (lane >> 2) * 4 + ((lane & 3) ^ (lane >> 3));
+  // parts change places with the rows, so that four rows' halves of parts hit all banks
+  const int put = lane ^ (lane >> 2 & 2);
   auto fetch = [&] {
     if (next_unit < units) {
       typename Shape::Codes& to = s.ring[warp][next_slot];
-      // (past the last block there are no values, and its codes will do)
-      const size_t b0 = (size_t)(2 * next_piece) * 32, b1 = (size_t)min(2 * next_piece + 1, w.kblocks - 1) * 32;
-      copy_async(&to.codes[0][0][put], from0 + b0, true);
-      copy_async(&to.codes[0][1][put], from1 + b0, true);
-      copy_async(&to.codes[1][0][put], from0 + b1, true);
-      copy_async(&to.codes[1][1][put], from1 + b1, true);
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) {   // (past the last block there are no values, and its codes will do)
+        const size_t at = (size_t)min(kBlocks * next_piece + b, w.kblocks - 1) * 32;
+        copy_async(&to.codes[b][0][put], from0 + at, true);
+        copy_async(&to.codes[b][1][put], from1 + at, true);
+      }
       if (sz_g < kGroups)
         copy_async(&to.sz[sz_g][sz_t][(lane & 3) * 2], from_sz + (size_t)min(next_piece * kGroups + sz_g, w.groups - 1) * 8, true);
       if (++next_slot == kCodeRing) next_slot = 0;
@@ -140,48 +154,23 @@ __global__ void __launch_bounds__(TcShape<NTOK, GS>::kThreads, 1) w4_tc_kernel(c
     }
     copies_commit();
   };
-  // scales of the sequence of groups, a thread its row's
-  const int srow = quarter * 32 + lane, sthread = (tid - 32 * kSumWarp) & 255;
-  const int group0 = p0 * kGroups, groups_here = pieces_here * kGroups;
-  int scale_unit = blockIdx.x, scale_at = 0;
-  const uint32_t scale_to = smem_u32(&s.scale[0][sthread][0]);
-  const uint32_t* from_scale = nullptr;   // of the unit's first group
-  // half of the ring: the next kScaleHalf groups of the unit (past the last one there are no values, and its
-  // scale will do: every unit takes whole halves)
-  auto fetch_scales = [&](int half) {
-    if (scale_unit < units) {
-      if (scale_at == 0) {
-        const int tile = min(scale_unit % row_tiles * 8 + (srow >> 4), w.tiles - 1);
-        from_scale = (const uint32_t*)w.sz + ((size_t)tile * w.groups * 8 + (srow & 7)) * 2 + (srow >> 3 & 1);
-      }
-      const int at = group0 + scale_at, most = w.groups - 1;
-#pragma unroll
-      for (int i = 0; i < kScaleHalf; ++i)
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(scale_to + half * (256 * kScaleHalf * 4) + i * 4),
-                     "l"(from_scale + 16 * (size_t)(uint32_t)min(at + i, most))
-                     : "memory");
-      scale_at += kScaleHalf;
-      if (scale_at >= groups_here) scale_at = 0, scale_unit += gridDim.x;
-    }
-    copies_commit();
-  };
-
   // loaded weights do not change: on their way before the launch before has ended
   if (warp < kSumWarp) {
     skip(warp / 4);
     for (int i = 0; i < kCodeRing - 1; ++i) fetch();
-  } else if (warp < kXWarp) {
-    fetch_scales(0);
-    fetch_scales(1);
   }
   if (tid == 0) {
     for (int i = 0; i < kPieces; ++i) {
-      mbar_init(&s.full[i], 5);   // four warps that widen, and the tokens' bytes
+      mbar_init(&s.full[i], Shape::kOne ? 13 : 5);   // four warps that widen, the tokens' bytes and, kOne, eight warps that sum
       mbar_init(&s.empty[i], 1);
     }
     for (int i = 0; i < kSlots; ++i) {
       mbar_init(&s.acc_full[i], 1);
       mbar_init(&s.acc_empty[i], 8);
+    }
+    for (int i = 0; i < kScaleBufs; ++i) {
+      mbar_init(&s.scale_full[i], 1);
+      mbar_init(&s.scale_empty[i], 8);
     }
     mbar_init(&s.up_full, 4);
     mbar_init(&s.up_free, 4);
@@ -201,103 +190,103 @@ __global__ void __launch_bounds__(TcShape<NTOK, GS>::kThreads, 1) w4_tc_kernel(c
   bool ok = true;
 
   if (warp < kSumWarp) {
-    const int t = lane >> 4, g = lane & 7, hi = lane >> 3 & 1, set = warp / 4;
+    const int g = lane >> 2, q = lane & 3, set = warp / 4;
     int slot = 0, at = set % kPieces;                    // the warp's first piece of the sequence, in the ring of pieces
     uint32_t parity = 1u ^ (uint32_t)(set / kPieces);    // of empty[at]
+    const uint32_t a_at = tmem + Shape::kSlots * Shape::kColsAcc + ((uint32_t)(quarter * 32) << 16);
     for (long long left = (long long)mine * pieces_here - set; left > 0; left -= kSets) {
       copies_wait<kCodeRing - 2>();
       __syncwarp();
       fetch();   // (into the slot that was read last)
       const typename Shape::Codes& from = s.ring[warp][slot];
       if (++slot == kCodeRing) slot = 0;
-      typename Shape::Piece& to = s.pieces[at];
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        uint32_t z0[2], z8[2];
+      for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint2 sz = from.sz[(2 * half + h) / GS][t][g];
-          z0[h] = __byte_perm(sz.x, 0u, 0x1010);
-          z8[h] = __byte_perm(sz.y, 0u, 0x1010);
-        }
-        uint4 c[2];
+        for (int t = 0; t < 2; ++t) {
+          // what rows g and g + 8 of a tile give to an MMA's columns 2q and 2q + 1 of A: ks 4q .. 4q + 3 of 16
+          uint32_t made[4][4];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) c[i] = from.codes[half][t][g * 4 + ((2 * hi + i) ^ (g >> 1))];
-        if (half == 0) {
-          ok = wait_for(&s.empty[at], parity);
-          if (!ok) break;
-        }
-        // word 2h + s of part q: ks 32h + 8q + 4s .., nibbles 0, 2 of row g and 1, 3 of row g + 8; a row's 16 bytes 4h + q
-        // change places with the row (by the same for both)
-        uint8_t* row = to.a[half] + (quarter * 32 + t * 16 + g) * 128;
+          for (int e = 0; e < 2; ++e) {
+            const uint2 c = *((const uint2*)&from.codes[b][t][g * 4 + ((2 * e + (q >> 1)) ^ (g & 2))] + (q & 1));
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint32_t word[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t r0[4], r8[4];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const uint32_t v = word[2 * h + e];
-              r0[2 * e] = sub_bf16x2((v & 0x000f000fu) | 0x43004300u, z0[h]);
-              r8[2 * e] = sub_bf16x2((v >> 4 & 0x000f000fu) | 0x43004300u, z8[h]);
-              r0[2 * e + 1] = sub_bf16x2((v >> 8 & 0x000f000fu) | 0x43004300u, z0[h]);
-              r8[2 * e + 1] = sub_bf16x2((v >> 12 & 0x000f000fu) | 0x43004300u, z8[h]);
+            for (int h = 0; h < 2; ++h) {
+              const uint2 sz = from.sz[(2 * b + h) / GS][t][g];
+              const uint32_t z0 = __byte_perm(sz.x, 0u, 0x1010), z8 = __byte_perm(sz.y, 0u, 0x1010), v = h ? c.y : c.x;
+              made[2 * h + e][0] = sub_bf16x2((v & 0x000f000fu) | 0x43004300u, z0);
+              made[2 * h + e][1] = sub_bf16x2((v >> 8 & 0x000f000fu) | 0x43004300u, z0);
+              made[2 * h + e][2] = sub_bf16x2((v >> 4 & 0x000f000fu) | 0x43004300u, z8);
+              made[2 * h + e][3] = sub_bf16x2((v >> 12 & 0x000f000fu) | 0x43004300u, z8);
             }
-            uint8_t* piece = row + (((4 * h + 2 * hi + i) ^ g) << 4);
-            *(uint4*)piece = make_uint4(r0[0], r0[1], r0[2], r0[3]);
-            *(uint4*)(piece + 8 * 128) = make_uint4(r8[0], r8[1], r8[2], r8[3]);
           }
+          if (b == 0 && t == 0) {   // (the piece's place is taken only once there is something to store)
+            ok = wait_for(&s.empty[at], parity);
+            if (!ok) goto widened;
+            tc_fence_after();
+          }
+          store_a(a_at + at * Shape::kColsA + b * 32 + ((uint32_t)(t * 16) << 16), made);
         }
-      }
-      if (!ok) break;
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      tmem_wait_st();
+      tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&s.full[at]);
       at += kSets;
       if (at >= kPieces) at -= kPieces, parity ^= 1u;
     }
+  widened:;
   } else if (warp < kXWarp) {
     constexpr int kTok = NTOK / 2;   // of a thread
     const int first = (warp - kSumWarp) / 4 * kTok;
-    int acc_at = 0, half = 0;
-    uint32_t parity = 0u, up_parity = 0u;
+    int at = 0, scale_at = 0;
+    const int srow = quarter * 32 + lane;
+    uint32_t parity = 0u, up_parity = 0u, scale_parity = 0u;
+    // this row's scale of the next group (sz: row g's and row g + 8's side by side)
+    const uint32_t my_scales = smem_u32(&s.scales[0][srow >> 4][(srow & 7) * 8 + (srow >> 1 & 4)]);
+    uint32_t from_scale = my_scales;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    if (Shape::kOne && lane == 0)
+      for (int i = 0; i < kPieces; ++i) mbar_arrive(&s.full[i]);   // (no accumulator holds anything yet)
     for (int unit = blockIdx.x; unit < units && ok; unit += gridDim.x) {
       const int m0 = unit / row_tiles * NTOK, tile = unit % row_tiles, row = tile * 128 + srow, tokens = min(NTOK, a.M - m0);
       float sum[kTok];
 #pragma unroll
       for (int i = 0; i < kTok; ++i) sum[i] = 0.f;
       for (int piece = 0; piece < pieces_here; ++piece) {
-        const int in_half = piece * kGroups % kScaleHalf;
-        if (in_half == 0) copies_wait<1>();
-        float scale[kGroups];
-#pragma unroll
-        for (int i = 0; i < kGroups; ++i) scale[i] = __uint_as_float(s.scale[half][sthread][in_half + i] & 0xffff0000u);
-        if (in_half + kGroups == kScaleHalf || piece + 1 == pieces_here) {   // (this half is read)
-          fetch_scales(half);
-          half ^= 1;
+        if (piece % (kScaleBatch / kGroups) == 0) {
+          ok = wait_for(&s.scale_full[scale_at], scale_parity);
+          if (!ok) break;
         }
-        ok = wait_for(Shape::kOne ? &s.empty[acc_at] : &s.acc_full[acc_at], parity);
+        uint32_t scale[kGroups];
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(scale[i]) : "r"(from_scale + i * 64));
+        from_scale += kGroups * 64;
+        const bool batch_read = (piece + 1) % (kScaleBatch / kGroups) == 0 || piece + 1 == pieces_here;
+        ok = wait_for(Shape::kOne ? &s.empty[at] : &s.acc_full[at], parity);
         if (!ok) break;
         tc_fence_after();
 #pragma unroll
         for (int group = 0; group < kGroups; ++group) {
-          uint32_t v[kTok / 16][16];
 #pragma unroll
-          for (int i = 0; i < kTok / 16; ++i) tmem_ld16_async(tmem + lanes + (acc_at * kGroups + group) * NTOK + first + i * 16, v[i]);
-          tmem_wait_ld();
+          for (int i = 0; i < kTok; i += 16) {
+            uint32_t v[16];
+            tmem_ld16_async(tmem + lanes + (at * kGroups + group) * NTOK + first + i, v);
+            tmem_wait_ld();
+            tmem_reg_fence16(v);
+            if (group == kGroups - 1 && i + 16 == kTok) {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(Shape::kOne ? &s.full[at] : &s.acc_empty[at]);
+              if (lane == 0 && batch_read) mbar_arrive(&s.scale_empty[scale_at]);
+            }
 #pragma unroll
-          for (int i = 0; i < kTok / 16; ++i) tmem_reg_fence16(v[i]);
-          if (group == kGroups - 1) {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&s.acc_empty[acc_at]);
+            for (int j = 0; j < 16; j += 2) fma_pair(sum[i + j], sum[i + j + 1], v[j], v[j + 1], __uint_as_float(scale[group] & 0xffff0000u));
           }
-#pragma unroll
-          for (int i = 0; i < kTok; i += 2) fma_pair(sum[i], sum[i + 1], v[i / 16][i % 16], v[i / 16][i % 16 + 1], scale[group]);
         }
-        if (++acc_at == kSlots) acc_at = 0, parity ^= 1u;
+        if (++at == kSlots) at = 0, parity ^= 1u;
+        if (batch_read) {
+          if (++scale_at == kScaleBufs) scale_at = 0, scale_parity ^= 1u;
+          from_scale = my_scales + scale_at * (8 * kScalePitch);
+        }
       }
       if (!ok) break;
       if (ranks > 1) {   // (the only unit, and its last MMA is done: the pieces are free)
@@ -339,21 +328,40 @@ __global__ void __launch_bounds__(TcShape<NTOK, GS>::kThreads, 1) w4_tc_kernel(c
         }
       }
     }
-  } else if (warp < kMmaWarp) {
+  } else {
+    if (warp == kXWarp) {
     const uint32_t el = elect_one();
     uint64_t keep;   // (every CTA reads them)
     asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(keep));
-    int at = 0;
-    uint32_t parity = 1u;
-    long long issued = 0;
+    int at = 0, scale_at = 0;
+    uint32_t parity = 1u, scale_parity = 1u;
+    long long issued = 0, batches = 0;
     for (int unit = blockIdx.x; unit < units && ok; unit += gridDim.x) {
       const int m0 = unit / row_tiles * NTOK;
+      // (past the last tile: any that is finite; past the last group of a tile: the next one's, or zeros)
+      const uint2* sz = w.sz + ((size_t)min(unit % row_tiles * 8 + (lane & 7), w.tiles - 1) * w.groups + p0 * kGroups) * 8;
       for (int piece = p0; piece < p1; ++piece) {
+        const int group = (piece - p0) * kGroups;
+        if (group % kScaleBatch == 0) {
+          ok = wait_for(&s.scale_empty[scale_at], scale_parity);
+          if (!ok) break;
+          mbar_expect_tx_el(&s.scale_full[scale_at], 8 * kScaleBatch * 64, el);
+          __syncwarp();
+          if (lane < 8)
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                             smem_u32(s.scales[scale_at][lane])),
+                         "l"(sz + (size_t)group * 8), "r"(kScaleBatch * 64), "r"(smem_u32(&s.scale_full[scale_at]))
+                         : "memory");
+          __syncwarp();
+          ++batches;
+          if (++scale_at == kScaleBufs) scale_at = 0, scale_parity ^= 1u;
+        }
         ok = wait_for(&s.empty[at], parity);
         if (!ok) break;
-        mbar_expect_tx_el(&s.full[at], 2 * NTOK * 128, el);
-        tma_load_2d_el(&x_map, smem_u32(&s.full[at]), smem_u32(s.pieces[at].x[0]), piece * 128, m0, keep, el);
-        tma_load_2d_el(&x_map, smem_u32(&s.full[at]), smem_u32(s.pieces[at].x[1]), piece * 128 + 64, m0, keep, el);
+        mbar_expect_tx_el(&s.full[at], kBlocks * NTOK * 128, el);
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+          tma_load_2d_el(&x_map, smem_u32(&s.full[at]), smem_u32(s.pieces[at].x[b]), (piece * kBlocks + b) * 64, m0, keep, el);
         ++issued;
         if (++at == kPieces) at = 0, parity ^= 1u;
       }
@@ -361,34 +369,37 @@ __global__ void __launch_bounds__(TcShape<NTOK, GS>::kThreads, 1) w4_tc_kernel(c
     // nobody leaves with loads in flight, not even where a wait ran out
     for (long long n = issued > kPieces ? issued - kPieces : 0; n < issued; ++n)
       ok = wait_for(&s.full[n % kPieces], (uint32_t)(n / kPieces) & 1u) && ok;
-  } else {
+    for (long long n = batches > kScaleBufs ? batches - kScaleBufs : 0; n < batches; ++n)
+      ok = wait_for(&s.scale_full[n % kScaleBufs], (uint32_t)(n / kScaleBufs) & 1u) && ok;
+    } else if (warp == kMmaWarp) {
     const uint32_t el = elect_one();
     const uint32_t idesc = idesc_bf16(128, NTOK);
-    const uint64_t ad0 = sw128_desc(smem_u32(s.pieces[0].a[0])), xd0 = sw128_desc(smem_u32(s.pieces[0].x[0]));
+    const uint64_t xd0 = sw128_desc(smem_u32(s.pieces[0].x[0]));
     int at = 0, acc_at = 0;
     uint32_t parity = 0u, acc_parity = 1u;
-    for (long long left = (long long)mine * pieces_here; left > 0; --left) {
-      ok = wait_for(&s.full[at], parity);
-      if (!ok) break;
-      ok = wait_for(&s.acc_empty[acc_at], acc_parity);
-      if (!ok) break;
-      tc_fence_after();
-      const uint32_t ahead = (uint32_t)(at * (sizeof(typename Shape::Piece) >> 4));
-      const uint64_t ad = ad0 + ahead, xd = xd0 + ahead;
-      const uint32_t td = tmem + acc_at * kGroups * NTOK;
+    for (int unit = blockIdx.x; unit < units && ok; unit += gridDim.x) {
+      for (int piece = p0; piece < p1; ++piece) {
+        ok = wait_for(&s.full[at], parity);
+        if (!ok) break;
+        if (!Shape::kOne) {
+          ok = wait_for(&s.acc_empty[acc_at], acc_parity);
+          if (!ok) break;
+        }
+        tc_fence_after();
+        const uint64_t xd = xd0 + (uint32_t)(at * (sizeof(typename Shape::Piece) >> 4));
+        const uint32_t td = tmem + acc_at * Shape::kColsAcc, ta = tmem + kSlots * Shape::kColsAcc + at * Shape::kColsA;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {   // 16 ks each
-        const int group = j / (2 * GS);
-        umma_bf16(td + group * NTOK, ad + (j / 4) * (128 * 128 >> 4) + 2 * (j % 4), xd + (j / 4) * (NTOK * 128 >> 4) + 2 * (j % 4), idesc,
-                  j % (2 * GS) > 0 ? 1u : 0u, el);
+        for (int j = 0; j < 4 * kBlocks; ++j)   // 16 ks each
+          umma_bf16_ts(td + j / (2 * GS) * NTOK, ta + 8 * j, xd + (j / 4) * (NTOK * 128 >> 4) + 2 * (j % 4), idesc, j % (2 * GS) > 0 ? 1u : 0u, el);
+        if (!Shape::kOne) umma_commit(&s.acc_full[acc_at], el);
+        umma_commit(&s.empty[at], el);
+        if (++acc_at == kSlots) acc_at = 0, acc_parity ^= 1u;
+        if (++at == kPieces) at = 0, parity ^= 1u;
       }
-      if (!Shape::kOne) umma_commit(&s.acc_full[acc_at], el);
-      umma_commit(&s.empty[at], el);
-      if (++acc_at == kSlots) acc_at = 0, acc_parity ^= 1u;
-      if (++at == kPieces) at = 0, parity ^= 1u;
     }
     umma_commit(&s.ended, el);   // nothing is in flight when the columns are given back
     ok = wait_for(&s.ended, 0u) && ok;
+  }
   }
   copies_wait<0>();
   if (!ok && lane == 0) raise_error(a.err, ERR_TIMEOUT);
@@ -397,7 +408,7 @@ __global__ void __launch_bounds__(TcShape<NTOK, GS>::kThreads, 1) w4_tc_kernel(c
     const int unit = blockIdx.x, m0 = unit / row_tiles * NTOK, tile = unit % row_tiles, tokens = min(NTOK, a.M - m0);
     const bool glu = a.epi == EPI_GEGLU;
     const int shift = glu ? 6 : 7, all = tokens << shift, e0 = all * rank / ranks, e1 = all * (rank + 1) / ranks;
-    for (int e = e0 + tid; e < e1; e += Shape::kThreads) {
+    for (int e = e0 + tid; e < e1; e += kTcThreads) {
       const int m = e >> shift, r = e & ((1 << shift) - 1), row = tile * 128 + r;
       auto value = [&](int r) {
         const int n = tile * 128 + r;
@@ -427,6 +438,7 @@ template <int NTOK, int GS>
 cudaError_t init_gs() {
   static_assert(sizeof(typename TcShape<NTOK, GS>::Shared) <= kTcSmem, "shared memory");
   static_assert(sizeof(typename TcShape<NTOK, GS>::Piece) % 1024 == 0, "swizzled tiles");
+  static_assert(TcShape<NTOK, GS>::kPieces * TcShape<NTOK, GS>::kColsA + TcShape<NTOK, GS>::kSlots * TcShape<NTOK, GS>::kColsAcc <= (int)kTcCols, "tensor memory");
   return cudaFuncSetAttribute(w4_tc_kernel<NTOK, GS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kTcSmem);
 }
 
@@ -459,7 +471,7 @@ cudaError_t launch_gs(const W4Args& a, cudaStream_t st) {
   while (ranks < kRanks && units * ranks * 2 <= a.num_sms && a.w.kblocks >= ranks * 2 * 4) ranks *= 2;
   const Overlap overlap;
   return launch_kernel_cluster(w4_tc_kernel<NTOK, GS>, dim3(ranks > 1 ? units : std::min(units, a.num_sms), 1, ranks),
-                               dim3(TcShape<NTOK, GS>::kThreads), kTcSmem, st, dim3(1, 1, ranks), map, a);
+                               dim3(kTcThreads), kTcSmem, st, dim3(1, 1, ranks), map, a);
 }
 
 template <int NTOK>
