@@ -100,7 +100,7 @@ __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity) {
 }
 
 template <int NTOK, int GS>
-__global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_constant__ CUtensorMap x_map, W4Args a) {
+__global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_constant__ CUtensorMap x_map, W4Args a, int ranks) {
   typedef TcShape<NTOK, GS> Shape;
   constexpr int kPieces = Shape::kPieces, kSlots = Shape::kSlots, kBlocks = Shape::kBlocks, kGroups = Shape::kGroups;
   constexpr int kCodeRing = Shape::kCodeRing;
@@ -112,24 +112,32 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
     if (tid == 0) raise_error(a.err, ERR_SHAPE);
     return;
   }
-  const int ranks = (int)gridDim.z, rank = ranks > 1 ? (int)cluster_ctarank() : 0;
+  const int rank = ranks > 1 ? (int)cluster_ctarank() : 0;
   const int row_tiles = (w.tiles + 7) / 8, units = row_tiles * ((a.M + NTOK - 1) / NTOK);
-  // this rank's pieces
   const int pieces = (w.kblocks + kBlocks - 1) / kBlocks;
-  const int p0 = (int)((long long)pieces * rank / ranks), p1 = (int)((long long)pieces * (rank + 1) / ranks), pieces_here = p1 - p0;
-  const int mine = (int)blockIdx.x < units ? (units - 1 - (int)blockIdx.x) / (int)gridDim.x + 1 : 0;   // units
+  // Units go round the CTAs.  With ranks > 1 the units of the round that is not full go to a cluster each, whose CTAs share
+  // its pieces.
+  const int full = ranks > 1 ? units / (int)gridDim.x : (int)blockIdx.x < units ? (units - 1 - (int)blockIdx.x) / (int)gridDim.x + 1 : 0;
+  const int last_unit = full * (int)gridDim.x + (int)blockIdx.x / ranks;
+  const bool joint = ranks > 1 && last_unit < units;
+  const int rounds = full + joint, p0 = (int)((long long)pieces * rank / ranks), p1 = (int)((long long)pieces * (rank + 1) / ranks);
+  auto unit_of = [&](int round) { return round < full ? (int)blockIdx.x + round * (int)gridDim.x : last_unit; };
+  auto first_of = [&](int round) { return round < full ? 0 : p0; };
+  auto end_of = [&](int round) { return round < full ? pieces : p1; };
 
   // codes of the sequence of pieces (unit by unit), every kSets-th of them, into the warp's ring
-  int next_unit = blockIdx.x, next_piece = p0, next_slot = 0;
+  int next_round = 0, next_piece = first_of(0), next_end = end_of(0), next_slot = 0;
   const uint4 *from0 = nullptr, *from1 = nullptr;   // this lane's part of a block of 64 ks, by tile
   const uint2* from_sz = nullptr;                   // this lane's part of a tile's scales
   const int sz_t = lane >> 2 & 1, sz_g = lane >> 3;
   auto skip = [&](int n) {   // n pieces on
-    const int unit = next_unit;
     next_piece += n;
-    while (next_piece >= p1 && next_unit < units) next_piece -= pieces_here, next_unit += gridDim.x;
-    if (unit != next_unit || !from0) {
-      const int tile0 = next_unit % row_tiles * 8 + 2 * quarter;   // (past the end: anything that is finite)
+    if (next_piece >= next_end || !from0) {
+      while (next_round < rounds && next_piece >= next_end) {
+        next_piece += first_of(++next_round) - next_end;
+        next_end = end_of(next_round);
+      }
+      const int tile0 = unit_of(next_round) % row_tiles * 8 + 2 * quarter;   // (past the end: anything that is finite)
       const int t0 = min(tile0, w.tiles - 1), t1 = min(tile0 + 1, w.tiles - 1);
       from0 = w.codes + (size_t)t0 * w.kblocks * 32 + lane;
       from1 = w.codes + (size_t)t1 * w.kblocks * 32 + lane;
@@ -139,7 +147,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
   // parts change places with the rows, so that four rows' halves of parts hit all banks
   const int put = lane ^ (lane >> 2 & 2);
   auto fetch = [&] {
-    if (next_unit < units) {
+    if (next_round < rounds) {
       typename Shape::Codes& to = s.ring[warp][next_slot];
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b) {   // (past the last block there are no values, and its codes will do)
@@ -194,7 +202,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
     int slot = 0, at = set % kPieces;                    // the warp's first piece of the sequence, in the ring of pieces
     uint32_t parity = 1u ^ (uint32_t)(set / kPieces);    // of empty[at]
     const uint32_t a_at = tmem + Shape::kSlots * Shape::kColsAcc + ((uint32_t)(quarter * 32) << 16);
-    for (long long left = (long long)mine * pieces_here - set; left > 0; left -= kSets) {
+    for (long long left = (long long)full * pieces + (joint ? p1 - p0 : 0) - set; left > 0; left -= kSets) {
       copies_wait<kCodeRing - 2>();
       __syncwarp();
       fetch();   // (into the slot that was read last)
@@ -246,7 +254,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     if (Shape::kOne && lane == 0)
       for (int i = 0; i < kPieces; ++i) mbar_arrive(&s.full[i]);   // (no accumulator holds anything yet)
-    for (int unit = blockIdx.x; unit < units && ok; unit += gridDim.x) {
+    for (int round = 0; round < rounds && ok; ++round) {
+      const int unit = unit_of(round), pieces_here = end_of(round) - first_of(round);
       const int m0 = unit / row_tiles * NTOK, tile = unit % row_tiles, row = tile * 128 + srow, tokens = min(NTOK, a.M - m0);
       float sum[kTok];
 #pragma unroll
@@ -289,7 +298,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
         }
       }
       if (!ok) break;
-      if (ranks > 1) {   // (the only unit, and its last MMA is done: the pieces are free)
+      if (round == full) {   // (joint: the last unit, and its last MMA is done, the pieces are free)
 #pragma unroll
         for (int i = 0; i < kTok; ++i) s.sums[(first + i) * kSumPitch + srow] = sum[i];
         continue;
@@ -316,15 +325,34 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
         up_parity ^= 1u;
       } else if (row < w.N) {
         const size_t at = (size_t)(m0 + first) * a.ldo + row;
+        const int here = tokens - first;
 #pragma unroll
-        for (int i = 0; i < kTok; ++i) {
-          if (first + i >= tokens) break;
-          const size_t to = at + (size_t)i * a.ldo;
-          float v = sum[i] + bias;
-          if (a.epi == EPI_STORE_SILU) v = silu_f(v);
-          if (a.epi == EPI_ADD_F32) ((float*)a.out)[to] += v;
-          else if (a.out_bf16) ((bf16*)a.out)[to] = from_f32<bf16>(v);
-          else ((float*)a.out)[to] = v;
+        for (int i = 0; i < kTok; ++i) sum[i] += bias;
+        if (a.epi == EPI_STORE_SILU) {
+#pragma unroll
+          for (int i = 0; i < kTok; ++i) sum[i] = silu_f(sum[i]);
+        }
+        if (a.out_bf16) {
+          bf16* to = (bf16*)a.out + at;
+#pragma unroll
+          for (int i = 0; i < kTok; ++i, to += a.ldo)
+            if (i < here) *to = from_f32<bf16>(sum[i]);
+        } else if (a.epi == EPI_ADD_F32) {
+          float* to = (float*)a.out + at;
+#pragma unroll
+          for (int i0 = 0; i0 < kTok; i0 += 4, to += (size_t)4 * a.ldo) {   // (four loads on their way at a time)
+            float was[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) was[i] = i0 + i < here ? to[(size_t)i * a.ldo] : 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (i0 + i < here) to[(size_t)i * a.ldo] = was[i] + sum[i0 + i];
+          }
+        } else {
+          float* to = (float*)a.out + at;
+#pragma unroll
+          for (int i = 0; i < kTok; ++i, to += a.ldo)
+            if (i < here) *to = sum[i];
         }
       }
     }
@@ -336,12 +364,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
     int at = 0, scale_at = 0;
     uint32_t parity = 1u, scale_parity = 1u;
     long long issued = 0, batches = 0;
-    for (int unit = blockIdx.x; unit < units && ok; unit += gridDim.x) {
-      const int m0 = unit / row_tiles * NTOK;
+    for (int round = 0; round < rounds && ok; ++round) {
+      const int unit = unit_of(round), m0 = unit / row_tiles * NTOK, first = first_of(round), end = end_of(round);
       // (past the last tile: any that is finite; past the last group of a tile: the next one's, or zeros)
-      const uint2* sz = w.sz + ((size_t)min(unit % row_tiles * 8 + (lane & 7), w.tiles - 1) * w.groups + p0 * kGroups) * 8;
-      for (int piece = p0; piece < p1; ++piece) {
-        const int group = (piece - p0) * kGroups;
+      const uint2* sz = w.sz + ((size_t)min(unit % row_tiles * 8 + (lane & 7), w.tiles - 1) * w.groups + first * kGroups) * 8;
+      for (int piece = first; piece < end; ++piece) {
+        const int group = (piece - first) * kGroups;
         if (group % kScaleBatch == 0) {
           ok = wait_for(&s.scale_empty[scale_at], scale_parity);
           if (!ok) break;
@@ -377,8 +405,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
     const uint64_t xd0 = sw128_desc(smem_u32(s.pieces[0].x[0]));
     int at = 0, acc_at = 0;
     uint32_t parity = 0u, acc_parity = 1u;
-    for (int unit = blockIdx.x; unit < units && ok; unit += gridDim.x) {
-      for (int piece = p0; piece < p1; ++piece) {
+    for (int round = 0; round < rounds && ok; ++round) {
+      for (int left = end_of(round) - first_of(round); left > 0; --left) {
         ok = wait_for(&s.full[at], parity);
         if (!ok) break;
         if (!Shape::kOne) {
@@ -403,9 +431,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
   }
   copies_wait<0>();
   if (!ok && lane == 0) raise_error(a.err, ERR_TIMEOUT);
-  if (ranks > 1) {
+  if (joint) {
     cluster_sync();
-    const int unit = blockIdx.x, m0 = unit / row_tiles * NTOK, tile = unit % row_tiles, tokens = min(NTOK, a.M - m0);
+    const int unit = last_unit, m0 = unit / row_tiles * NTOK, tile = unit % row_tiles, tokens = min(NTOK, a.M - m0);
     const bool glu = a.epi == EPI_GEGLU;
     const int shift = glu ? 6 : 7, all = tokens << shift, e0 = all * rank / ranks, e1 = all * (rank + 1) / ranks;
     for (int e = e0 + tid; e < e1; e += kTcThreads) {
@@ -466,12 +494,15 @@ cudaError_t launch_gs(const W4Args& a, cudaStream_t st) {
              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return cudaErrorInvalidValue;
   const int units = (a.w.tiles + 7) / 8 * ((a.M + NTOK - 1) / NTOK);
-  // the ks of a unit over as many CTAs (1, 2, 4, 8) as there are SMs for and two pieces for each
+  // the ks of the last round's units over as many CTAs (1, 2, 4, 8; after full rounds, whose CTAs all have to be there
+  // at once, 2) as there are SMs for and four pieces for each
+  const int sms = a.num_sms / 2 * 2, most = units < a.num_sms ? kRanks : 2;
+  const int last = units < a.num_sms ? units : units % sms;
   int ranks = 1;
-  while (ranks < kRanks && units * ranks * 2 <= a.num_sms && a.w.kblocks >= ranks * 2 * 4) ranks *= 2;
+  while (last > 0 && ranks < most && last * ranks * 2 <= sms && a.w.kblocks >= ranks * 2 * 4) ranks *= 2;
+  const int grid = units < a.num_sms ? units * ranks : ranks > 1 ? sms : a.num_sms;
   const Overlap overlap;
-  return launch_kernel_cluster(w4_tc_kernel<NTOK, GS>, dim3(ranks > 1 ? units : std::min(units, a.num_sms), 1, ranks),
-                               dim3(kTcThreads), kTcSmem, st, dim3(1, 1, ranks), map, a);
+  return launch_kernel_cluster(w4_tc_kernel<NTOK, GS>, dim3(grid), dim3(kTcThreads), kTcSmem, st, dim3(ranks, 1, 1), map, a, ranks);
 }
 
 template <int NTOK>

@@ -328,6 +328,22 @@ def test_geglu_products(n, k, group):
         _product_close(_np(w.product(x, epi="geglu", bias=bias)), _np(x), held, "geglu", "bf16", _np(bias))
 
 
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_products_whose_last_round_is_shared(group):
+    """More tiles than SMs, and few in the last round: pairs of CTAs share those, every epilogue."""
+    w, held = _held(20480, 1100, group, 5)
+    flat, bias = _rand((70, 1104), 1, "bf16"), _rand((20480,), 4)
+    for m in (31, 58, 70):
+        x = flat[:m, :1100]
+        _product_close(_np(w.product(x, epi="geglu", bias=bias)), _np(x), held, "geglu", "bf16", _np(bias))
+        _product_close(_np(w.product(x, epi="silu", dtype=torch.float32)), _np(x), held, "silu", "fp32")
+        before = _rand((m, 20480), 2)
+        _product_close(_np(w.product(x, out=before.clone(), epi="add", bias=bias)), _np(x), held, "add", "fp32", _np(bias), _np(before))
+    w, held = _held(20449, 1101, group, 6)
+    x = flat[:33, :1101]
+    _product_close(_np(w.product(x)), _np(x), held, "store", "bf16")
+
+
 def test_products_of_strided_and_unaligned_rows_touch_nothing_else():
     w, held = _held(50, 104, 32)
     flat = _rand((20 * 131 + 40,), 5, "bf16")
