@@ -162,6 +162,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
     }
     copies_commit();
   };
+  if (tid == 32 * kXWarp) asm volatile("prefetch.tensormap [%0];" ::"l"(&x_map) : "memory");
   // loaded weights do not change: on their way before the launch before has ended
   if (warp < kSumWarp) {
     skip(warp / 4);
@@ -433,26 +434,42 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
   if (!ok && lane == 0) raise_error(a.err, ERR_TIMEOUT);
   if (joint) {
     cluster_sync();
-    const int unit = last_unit, m0 = unit / row_tiles * NTOK, tile = unit % row_tiles, tokens = min(NTOK, a.M - m0);
-    const bool glu = a.epi == EPI_GEGLU;
-    const int shift = glu ? 6 : 7, all = tokens << shift, e0 = all * rank / ranks, e1 = all * (rank + 1) / ranks;
-    for (int e = e0 + tid; e < e1; e += kTcThreads) {
-      const int m = e >> shift, r = e & ((1 << shift) - 1), row = tile * 128 + r;
-      auto value = [&](int r) {
-        const int n = tile * 128 + r;
-        return over_ranks(&s.sums[m * kSumPitch + r], ranks) + (a.bias && n < w.N ? a.bias[n] : 0.f);
-      };
-      float v = value(r);
-      if (glu) {
-        ((bf16*)a.out)[(size_t)(m0 + m) * a.ldo + tile * 64 + r] = from_f32<bf16>(gelu_tanh_f(v) * value(r + 64));
+    const int m0 = last_unit / row_tiles * NTOK, tile = last_unit % row_tiles, tokens = min(NTOK, a.M - m0);
+    // a warp per token: four of its rows' sums to a lane, of all ranks in their order (the loads on their way together)
+    for (int m = tokens * rank / ranks + warp; m < tokens * (rank + 1) / ranks; m += kTcThreads / 32) {
+      float x[kRanks][4], v[4];
+#pragma unroll
+      for (int i = 0; i < kRanks; ++i)
+        if (i < ranks) {
+          const uint32_t from = mapa_shared(smem_u32(&s.sums[m * kSumPitch + lane]), (uint32_t)i);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[i][j] = ld_cluster_f(from + 128 * j);
+        }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        v[j] = x[0][j];
+#pragma unroll
+        for (int i = 1; i < kRanks; ++i)
+          if (i < ranks) v[j] += x[i][j];
+        const int n = tile * 128 + lane + 32 * j;
+        if (a.bias && n < w.N) v[j] += a.bias[n];
+      }
+      if (a.epi == EPI_GEGLU) {
+        bf16* to = (bf16*)a.out + (size_t)(m0 + m) * a.ldo + tile * 64 + lane;
+        to[0] = from_f32<bf16>(gelu_tanh_f(v[0]) * v[2]);
+        to[32] = from_f32<bf16>(gelu_tanh_f(v[1]) * v[3]);
         continue;
       }
-      if (row >= w.N) continue;
-      const size_t to = (size_t)(m0 + m) * a.ldo + row;
-      if (a.epi == EPI_STORE_SILU) v = silu_f(v);
-      if (a.epi == EPI_ADD_F32) ((float*)a.out)[to] += v;
-      else if (a.out_bf16) ((bf16*)a.out)[to] = from_f32<bf16>(v);
-      else ((float*)a.out)[to] = v;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int row = tile * 128 + lane + 32 * j;
+        if (row >= w.N) continue;
+        const size_t to = (size_t)(m0 + m) * a.ldo + row;
+        if (a.epi == EPI_STORE_SILU) v[j] = silu_f(v[j]);
+        if (a.epi == EPI_ADD_F32) ((float*)a.out)[to] += v[j];
+        else if (a.out_bf16) ((bf16*)a.out)[to] = from_f32<bf16>(v[j]);
+        else ((float*)a.out)[to] = v[j];
+      }
     }
     cluster_sync();   // nobody leaves while its sums are read
   }
