@@ -97,7 +97,7 @@ ravel_status ravel_w4_create(int N, int K, int group, int device, ravel_w4_t** o
 /* Free the matrix (after synchronising the device).  NULL is a no-op. */
 void ravel_w4_destroy(ravel_w4_t* w);
 
-/* Clear the error word of a matrix, after waiting for the device: a product of more than 16 rows in
+/* Clear the error word of a matrix, after waiting for the device: a product of more than 8 rows in
  * which a bounded wait ran out (its output is not valid) makes later ones return RAVEL_ETIMEOUT. */
 ravel_status ravel_w4_reset(ravel_w4_t* w);
 

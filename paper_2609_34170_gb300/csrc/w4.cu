@@ -416,9 +416,7 @@ cudaError_t init_nt() {
 template <int NT, bool G32>
 cudaError_t launch_few(const W4Args& a, cudaStream_t st) {
   const int pairs = a.w.tiles / 2, tiles = (a.M + NT * 8 - 1) / (NT * 8);
-  // the ks of a pair over as many CTAs (1, 2, 4) as there are SMs for and blocks for the warps
-  int ranks = 1;
-  while (ranks < 4 && (long long)pairs * tiles * ranks * 2 <= a.num_sms && a.w.kblocks >= ranks * 2 * kWarps) ranks *= 2;
+  const int ranks = w4_ranks((long long)pairs * tiles, a.w.kblocks, kWarps, kRanks, a.num_sms);
   // pairs beyond what the SMs hold at once follow one another in a CTA
   const int held = kHeld<NT, G32> * a.num_sms;
   const int across = ranks > 1 || pairs <= held ? pairs : std::max(1, held / std::min(tiles, held));
@@ -444,14 +442,18 @@ cudaError_t init_w4_kernels() {
 
 cudaError_t launch_w4_gemm(const W4Args& a, cudaStream_t st) {
   if (a.M <= 8) return launch_nt<1>(a, st);
-  // More than 16 rows: tiles of 16 go through the matrix each, from L2 after the first, and win while that is little
-  // work, the tcgen05 kernel (an SM a CTA, with a longer start) from there on.  us, tiles / tcgen05, groups of 128: 64 rows x
-  // 2560 x 1024 5.9 / 8.8; 64 x 4096 x 1024 7.0 / 9.3, 96 x 4096 x 1024 10.4 / 9.1; 32 x 8192 x 1024 7.1 / 7.9, 48 rows
-  // 10.3 / 9.0; 32 x 4096 x 4096 8.8 / 9.9, 48 rows 13.6 / 11.0; 17 x 4096 x 8192 15.6 / 12.5; 64 x 2048 x 4096 8.8 / 14.3.
-  // (TMA takes aligned rows only.)
-  const long long tiles = (a.M + 15) / 16;
-  const bool little = a.w.tiles / 2 * tiles * 3 <= 10 * a.num_sms && (long long)a.w.N * a.w.K * tiles <= 36ll << 20;
-  return a.M <= 16 || !a.vec || little ? launch_nt<2>(a, st) : launch_w4_tc(a, st);
+  // Tiles of 16 rows go through the matrix each, from L2 after the first, in about 2.5 us and 0.8 to 1 for each block of 64 ks of
+  // a warp; the tcgen05 kernel (an SM a CTA, a longer start) takes 5.5 and 0.4 for each piece of 128 ks of a CTA, 0.7 where its
+  // sums are many.  us, tiles / tcgen05, groups of 128: 16 rows x 4096 x 8192 15.1 / 10.7, x 8192 x 8192 15.7 / 16.4, x 65536 x
+  // 2048 31.6 / 26.3, x 1024 x 16384 9.6 / 15.3; 32 rows x 2048 x 4096 8.3 / 6.7, x 1024 x 4096 5.7 / 6.7, x 8192 x 1024 7.0 /
+  // 6.6; 64 x 4096 x 1024 7.0 / 6.9, x 2048 x 2048 5.3 / 6.5; 96 x 4096 x 1024 10.3 / 7.1; groups of 32, 64 rows x 512 x 8192
+  // 10.2 / 15.3.  (TMA takes aligned rows only.)
+  const long long tiles = (a.M + 15) / 16, ctas = a.w.tiles / 2 * tiles;
+  const int ranks = w4_ranks(ctas, a.w.kblocks, kWarps, kRanks, a.num_sms);
+  const long long blocks = (a.w.kblocks + kWarps * ranks - 1) / (kWarps * ranks) * ((ctas * ranks + 2 * a.num_sms - 1) / (2 * a.num_sms));
+  const W4TcPlan plan(a, a.M <= 32 ? 32 : 64);
+  const bool tc = 10 * blocks > 33 + (a.w.group == 32 && a.M > 32 ? 7ll : 4ll) * plan.pieces;
+  return a.vec && tc ? launch_w4_tc(a, st) : launch_nt<2>(a, st);
 }
 
 cudaError_t launch_w4_load(const W4Matrix& w, const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, cudaStream_t st) {

@@ -1,5 +1,5 @@
 // Products with 4-bit weights for more tokens than a warp's MMAs carry at the pace of memory: tcgen05, with
-// the weights widened into shared memory.
+// the weights widened into tensor memory.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -16,21 +16,24 @@ namespace ravel {
 namespace {
 
 // A CTA takes 128 rows of weights, the MMAs' M, and NTOK tokens, their N.  Per piece of 128 ks:
-//   four of the warps that widen do so: a thread takes half of the codes of two rows out of a ring of its warp
-//     (asynchronous copies), makes them c - z in bf16 and stores them into A, two swizzled tiles of 64 ks;
-//   one warp loads the tokens' values by TMA, two tiles of B;
+//   four of the warps that widen do so: a thread takes the codes of two rows out of a ring of its warp (asynchronous
+//     copies), makes them c - z in bf16 and stores them into A, in tensor memory, as the fragments that they are;
+//   one warp loads the tokens' values by TMA, two swizzled tiles of B, and every eight groups the rows' scales;
 //   one warp issues the MMAs.  A group's products are summed into an accumulator of their own, in turn;
 //   eight warps take the accumulators, scale them by the group's scale and add them up in fp32 registers, half
 //     of a row's tokens to a thread, and at the end of the ks store the outputs.
 // So weights enter as whole numbers, as in the other kernels; no scaled weight is rounded.
 //
-// 64 rows x 65536 x 8192 with groups of 128 (268 MB of codes) 124 us: 2.4 TB/s, 0.55 PFLOP/s.  What bounds it is
-// neither memory (44 us) nor the tensor core (an MMA of 128 x NTOK x 16 takes 71 cycles at any NTOK up to
-// 128: 63 us) but the roles' own instructions: of the 1000 cycles a piece takes, the MMA warp spends 240 on its
-// MMAs and the rest on waits that have mostly ended, commits and the loop, a warp that widens 2000 on every third
-// piece, and a warp that sums 500 on scales and 250 on a piece's sums.  On the way here: tokens by asynchronous copies of
-// four warps 225 (their addresses took longer than the MMAs), pieces of 64 ks 185, A in tensor memory the
-// same as in shared memory, mma.sync with eight pairs of tiles sharing the tokens 267 (its MMAs alone are 113).
+// 64 rows x 65536 x 8192 with groups of 128 (268 MB of codes) 93 us: 3.0 TB/s, 0.74 PFLOP/s.  What bounds it is
+// neither memory (44 us) nor the tensor core (a fifth of its cycles; an MMA of 128 x NTOK x 16 takes 71 at any NTOK up to
+// 128: 55 us) but the roles' own instructions, some ten cycles each with 22 warps on four schedulers: of the 800
+// cycles that a piece takes, the warps that sum need all for some 100 of them, the MMA warp 700 for its wait, eight MMAs and
+// a commit, a warp that widens 1800 on every third piece.  Measured on the way here (same product, us): mma.sync with eight
+// pairs of tiles sharing the tokens 267; tokens by asynchronous copies of four warps 225; pieces of 64 ks 185; A in shared
+// memory, three pieces in the making, scales by copies of each thread 124; A in tensor memory and scales by bulk copies
+// 111; the last of 3.4 rounds shared by pairs of CTAs and outputs without a branch each 98; units joined a token to a
+// warp 93.  Warps that sum in turn, all of a row's tokens to a thread that has more registers, are no
+// faster.
 constexpr int kSets = 3;        // of four warps that widen a piece
 constexpr int kScaleBatch = kPadGroups, kScaleBufs = 3;   // groups of a unit whose scales come together; batches there is room for
 constexpr int kScalePitch = kScaleBatch * 64 + 64;         // bytes of a tile's: rows of two tiles in different banks
@@ -257,7 +260,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
       for (int i = 0; i < kPieces; ++i) mbar_arrive(&s.full[i]);   // (no accumulator holds anything yet)
     for (int round = 0; round < rounds && ok; ++round) {
       const int unit = unit_of(round), pieces_here = end_of(round) - first_of(round);
-      const int m0 = unit / row_tiles * NTOK, tile = unit % row_tiles, row = tile * 128 + srow, tokens = min(NTOK, a.M - m0);
       float sum[kTok];
 #pragma unroll
       for (int i = 0; i < kTok; ++i) sum[i] = 0.f;
@@ -304,6 +306,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
         for (int i = 0; i < kTok; ++i) s.sums[(first + i) * kSumPitch + srow] = sum[i];
         continue;
       }
+      const int m0 = unit / row_tiles * NTOK, tile = unit % row_tiles, row = tile * 128 + srow;
+      const int here = min(kTok, a.M - m0 - first);   // tokens that there are
       const float bias = a.bias && row < w.N ? a.bias[row] : 0.f;
       if (a.epi == EPI_GEGLU) {   // (bounded waits: a warp that gave up does not come)
         if (quarter >= 2) {
@@ -318,15 +322,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
           if (!ok) break;
           bf16* out = (bf16*)a.out + (size_t)(m0 + first) * a.ldo + tile * 64 + srow;
 #pragma unroll
-          for (int i = 0; i < kTok; ++i)
-            if (first + i < tokens) out[(size_t)i * a.ldo] = from_f32<bf16>(gelu_tanh_f(sum[i] + bias) * s.up[(first + i) * kUpPitch + srow]);
+          for (int i = 0; i < kTok; ++i, out += a.ldo)
+            if (i < here) *out = from_f32<bf16>(gelu_tanh_f(sum[i] + bias) * s.up[(first + i) * kUpPitch + srow]);
           __syncwarp();
           if (lane == 0) mbar_arrive(&s.up_free);
         }
         up_parity ^= 1u;
       } else if (row < w.N) {
         const size_t at = (size_t)(m0 + first) * a.ldo + row;
-        const int here = tokens - first;
 #pragma unroll
         for (int i = 0; i < kTok; ++i) sum[i] += bias;
         if (a.epi == EPI_STORE_SILU) {
@@ -510,16 +513,9 @@ cudaError_t launch_gs(const W4Args& a, cudaStream_t st) {
   if (encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(a.x), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return cudaErrorInvalidValue;
-  const int units = (a.w.tiles + 7) / 8 * ((a.M + NTOK - 1) / NTOK);
-  // the ks of the last round's units over as many CTAs (1, 2, 4, 8; after full rounds, whose CTAs all have to be there
-  // at once, 2) as there are SMs for and four pieces for each
-  const int sms = a.num_sms / 2 * 2, most = units < a.num_sms ? kRanks : 2;
-  const int last = units < a.num_sms ? units : units % sms;
-  int ranks = 1;
-  while (last > 0 && ranks < most && last * ranks * 2 <= sms && a.w.kblocks >= ranks * 2 * 4) ranks *= 2;
-  const int grid = units < a.num_sms ? units * ranks : ranks > 1 ? sms : a.num_sms;
+  const W4TcPlan plan(a, NTOK);
   const Overlap overlap;
-  return launch_kernel_cluster(w4_tc_kernel<NTOK, GS>, dim3(grid), dim3(kTcThreads), kTcSmem, st, dim3(ranks, 1, 1), map, a, ranks);
+  return launch_kernel_cluster(w4_tc_kernel<NTOK, GS>, dim3(plan.grid), dim3(kTcThreads), kTcSmem, st, dim3(plan.ranks, 1, 1), map, a, plan.ranks);
 }
 
 template <int NTOK>
