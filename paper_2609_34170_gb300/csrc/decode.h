@@ -82,9 +82,9 @@ struct DrawArgs {
   const int* top_k;
   int* tokens;
   float* log_probs;
-  int vec;            // rows are 16-byte aligned
   int num_sms;
 };
+cudaError_t init_draw_kernels();
 cudaError_t launch_draw(const DrawArgs& a, Dtype dt, cudaStream_t st);
 
 }  // namespace ravel

@@ -53,6 +53,7 @@ bool known(int dtype) { return dtype == RAVEL_FP32 || dtype == RAVEL_BF16; }
 Dtype type_of(int dtype) { return dtype == RAVEL_BF16 ? DT_BF16 : DT_F32; }
 int size_of(int dtype) { return dtype == RAVEL_BF16 ? 2 : 4; }
 
+// The current device's SMs; once per device before anything is launched on it.
 cudaError_t sm_count(int* out) {
   static std::atomic<int> counts[64];
   int dev = 0;
@@ -62,6 +63,7 @@ cudaError_t sm_count(int* out) {
   *out = kept ? counts[dev].load(std::memory_order_relaxed) : 0;
   if (*out) return cudaSuccess;
   e = cudaDeviceGetAttribute(out, cudaDevAttrMultiProcessorCount, dev);
+  if (e == cudaSuccess) e = init_draw_kernels();
   if (e == cudaSuccess && kept) counts[dev].store(*out, std::memory_order_relaxed);
   return e;
 }
@@ -327,8 +329,7 @@ ravel_status ravel_draw_tokens(const void* logits, int batch, int vocab, long lo
   if (batch == 0) return RAVEL_OK;
   if (!logits || !u || !tokens) return fail(RAVEL_EINVAL, "draw_tokens: null argument");
   if ((uintptr_t)logits % size_of(dtype)) return fail(RAVEL_EINVAL, "draw_tokens: unaligned logits");
-  DrawArgs a{logits, batch, vocab, row_stride, u, temperature, top_p, min_p, top_k, tokens, log_probs, 0, 0};
-  a.vec = (uintptr_t)logits % 16 == 0 && (batch == 1 || row_stride * size_of(dtype) % 16 == 0);
+  DrawArgs a{logits, batch, vocab, row_stride, u, temperature, top_p, min_p, top_k, tokens, log_probs, 0};
   cudaError_t e = sm_count(&a.num_sms);
   if (e == cudaSuccess) e = launch_draw(a, type_of(dtype), (cudaStream_t)stream);
   return e == cudaSuccess ? RAVEL_OK : cuda_fail(e, "draw_tokens");

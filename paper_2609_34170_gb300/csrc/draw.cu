@@ -32,6 +32,7 @@ constexpr int kThreads = 1024, kWarps = kThreads / 32;
 constexpr int kBins = 512, kCap = 2048;
 constexpr int kRanks = 8;        // CTAs of a row at most
 constexpr int kBits = 43;        // weight of the likeliest token: 2^43
+constexpr int kWarpBins = 2 * kWarps * kBins * 4;   // bytes of the weights of warps' runs by bin
 
 typedef unsigned long long u64;
 
@@ -162,7 +163,10 @@ __device__ __forceinline__ u64 warp_sum_u64(u64 v) {
 struct DrawShared {
   u64 table[1024];
   union {
-    uint32_t bins[3][kBins];    // of a CTA: counts, weights' low and high words
+    struct {
+      uint32_t bins[kBins];     // of a CTA: counts
+      u64 weights[kBins];       // and weights
+    };
     u64 hist[2][256];           // radix selection
     struct {
       u64 hist[kBins];          // selection within the list
@@ -249,30 +253,38 @@ __device__ __noinline__ u64 pick(DrawShared& s, ulonglong2 c, ulonglong2 w, u64 
 template <typename T>
 __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
   __shared__ DrawShared s;
+  extern __shared__ uint4 draw_smem[];
+  uint32_t* warp_bins = (uint32_t*)draw_smem;   // weights of a warp's run by bin: [low, high word][warp][bin]
   constexpr int V = 16 / sizeof(T);
   constexpr uint32_t kAll = 0xffffffffu;
   const int ranks = (int)gridDim.x, rank = ranks > 1 ? (int)cluster_ctarank() : 0, b = blockIdx.y;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const float inf = __uint_as_float(0x7f800000u);
   s.table[tid] = kExp.v[tid];
-  for (int i = tid; i < 3 * kBins; i += kThreads) (&s.bins[0][0])[i] = 0u;
+  auto clear_warp_bins = [&] {
+    for (int i = tid; i < 2 * kWarps * kBins / 4; i += kThreads) draw_smem[i] = make_uint4(0u, 0u, 0u, 0u);
+  };
+  if (a.top_p) clear_warp_bins();
+  if (tid < kBins) s.bins[tid] = 0u;
   if (tid == 0) s.listed = 0u;
   pdl_trigger();
   pdl_wait();
   const float u = a.u[b], t = a.temperature ? a.temperature[b] : 1.f, p = a.top_p ? a.top_p[b] : 1.f, mp = a.min_p ? a.min_p[b] : 0.f;
   int k = a.top_k ? a.top_k[b] : 0;
   const T* row = (const T*)a.logits + (long long)b * a.row;
-  // this warp's run of the row: whole steps of 32 lanes x V values
-  const int steps_all = (a.vocab + 32 * V - 1) / (32 * V), shares = ranks * kWarps, share = rank * kWarps + warp;
+  // this warp's run of the row: whole steps of 32 lanes x V values, from the 16 bytes on in which the row begins
+  const int shift = (int)((uintptr_t)row % 16 / sizeof(T)), past = shift + a.vocab;
+  const T* from16 = row - shift;
+  const int steps_all = (past + 32 * V - 1) / (32 * V), shares = ranks * kWarps, share = rank * kWarps + warp;
   auto first_step = [&](int share) { return (int)((long long)steps_all * share / shares); };
   const int step0 = first_step(share), step1 = first_step(share + 1);
 
-  auto fetch = [&](int step) {   // V values; past the end -inf
+  auto fetch = [&](int step) {   // V values; before the row and past it -inf
     const int i = (step * 32 + lane) * V;
-    if (a.vec && i + V <= a.vocab) return *(const uint4*)(row + i);
+    if (i >= shift && i + V <= past) return *(const uint4*)(from16 + i);
     T t[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) t[j] = i + j < a.vocab ? row[i + j] : from_f32<T>(-inf);
+    for (int j = 0; j < V; ++j) t[j] = i + j >= shift && i + j < past ? from16[i + j] : from_f32<T>(-inf);
     uint4 w;
     memcpy(&w, t, 16);
     return w;
@@ -296,20 +308,23 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
       f(step, x);
     }
   };
-  auto index_of = [&](int step, int j) { return (step * 32 + lane) * V + j; };
+  auto index_of = [&](int step, int j) { return (step * 32 + lane) * V + j - shift; };
+  auto there = [&](int i) { return (uint32_t)i < (uint32_t)a.vocab; };
   auto order_of = [&](float x, int i) { return (u64)key_of(x) << 32 | (kAll - (uint32_t)i); };
   int turn = 0;
   auto barrier = [&] {
     if (ranks > 1) cluster_sync();
     else __syncthreads();
   };
-  // sum of 32-bit words of all ranks (the loads on their way together)
-  auto sum_of = [&](const uint32_t* p) {
+  // sum of a word of all ranks (the loads on their way together)
+  auto sum_of = [&](const auto* p) {
     if (ranks == 1) return (u64)*p;
-    uint32_t x[kRanks];
+    u64 x[kRanks], n = 0;
 #pragma unroll
-    for (int i = 0; i < kRanks; ++i) x[i] = ld_cluster_u32(mapa_shared(smem_u32(p), (uint32_t)min(i, ranks - 1)));
-    u64 n = 0;
+    for (int i = 0; i < kRanks; ++i) {
+      const uint32_t at = mapa_shared(smem_u32(p), (uint32_t)min(i, ranks - 1));
+      x[i] = sizeof(*p) == 8 ? ld_cluster_u64(at) : ld_cluster_u32(at);
+    }
 #pragma unroll
     for (int i = 0; i < kRanks; ++i) n += i < ranks ? x[i] : 0u;
     return n;
@@ -563,7 +578,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
         if (step < f1) load(step, x);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-          w[j] = step < f1 && index_of(step, j) < a.vocab ? value_at(x[j], order_of(x[j], index_of(step, j))) : 0ull;
+          w[j] = step < f1 && there(index_of(step, j)) ? value_at(x[j], order_of(x[j], index_of(step, j))) : 0ull;
           ws += w[j];
         }
         u64 wi = ws;   // up to and with this lane
@@ -630,29 +645,43 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
   u64 stays = 0ull;   // the last of the order that top-k lets through, once it is known by itself
   // (twice where top-k's border has to be found before top-p's sum: its tokens are more than a list holds)
   while (by_count || by_weight) {
-    for_steps([&](int step, const float* x) {
+    if (by_count) {
+      for_steps([&](int step, const float* x) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        if (!weighs(x[j]) || (stays != 0ull && order_of(x[j], index_of(step, j)) < stays)) continue;
-        const int bin = bin_of(x[j]);
-        atomicAdd(&s.bins[0][bin], 1u);
-        if (!by_count) {
+        for (int j = 0; j < V; ++j)
+          if (weighs(x[j])) atomicAdd(&s.bins[bin_of(x[j])], 1u);
+      });
+    } else {
+      uint32_t *low = warp_bins + warp * kBins, *high = low + kWarps * kBins;
+      for_steps([&](int step, const float* x) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          if (!weighs(x[j]) || (stays != 0ull && order_of(x[j], index_of(step, j)) < stays)) continue;
+          const int bin = bin_of(x[j]);
           const u64 w = weigh(x[j], s.table);
-          const uint32_t lo = (uint32_t)w, was = atomicAdd(&s.bins[1][bin], lo);
-          atomicAdd(&s.bins[2][bin], (uint32_t)(w >> 32) + (was + lo < was ? 1u : 0u));
+          atomicAdd(&s.bins[bin], 1u);
+          const uint32_t lo = (uint32_t)w, was = atomicAdd(low + bin, lo);
+          atomicAdd(high + bin, (uint32_t)(w >> 32) + (was + lo < was ? 1u : 0u));
         }
+      });
+      __syncthreads();
+      if (tid < kBins) {
+        u64 lo = 0ull, hi = 0ull;
+#pragma unroll 8
+        for (int i = 0; i < kWarps; ++i) lo += warp_bins[i * kBins + tid], hi += warp_bins[(kWarps + i) * kBins + tid];
+        s.weights[tid] = lo + (hi << 32);
       }
-    });
+    }
     barrier();
     uint32_t bin;
     u64 before = 0, in = 0, want = 0, all;
-    const u64 n = tid < kBins ? sum_of(&s.bins[0][tid]) : 0ull;
+    const u64 n = tid < kBins ? sum_of(&s.bins[tid]) : 0ull;
     u64 upto = block_scan(n, all), count, cin;   // tokens up to the bin, in it
     if (by_count) {
       bin_at(n, (u64)k, upto, all, bin, before, in);
       cin = in, count = before + in;
     } else {
-      const u64 w = tid < kBins ? sum_of(&s.bins[1][tid]) + (sum_of(&s.bins[2][tid]) << 32) : 0ull;
+      const u64 w = tid < kBins ? sum_of(&s.weights[tid]) : 0ull;
       const u64 cum = block_scan(w, all);
       want = share_of(all);
       bin_at(w, want, cum, all, bin, before, in);
@@ -664,7 +693,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
     // (before the last but one nothing is without weight)
     const float from = (float)bin, to = bin == kBins - 2 ? inf : (float)(bin + 1);
     auto again = [&] {   // (nobody reads this CTA's any more)
-      for (int i = tid; i < 3 * kBins; i += kThreads) (&s.bins[0][0])[i] = 0u;
+      if (tid < kBins) s.bins[tid] = 0u;
       if (tid == 0) s.listed = 0u;
       __syncthreads();
     };
@@ -748,7 +777,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
       // by histograms of the list
       auto by_picks = [&] {
         const float per = (float)kBins / (float)(bin + 1), per_index = (float)kBins / (float)a.vocab;
-        u64 border = 0ull, c[2], w[2], of[2];
+        u64 border = 0ull, c[2], w[2], of[2] = {};
         int by_key[2], by_index[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -837,8 +866,15 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
         for_steps([&](int step, const float* x) { list_up(in_bin(x, step), x, step); });
       } else {
         last = max(last, stays);
-        sum = sum_weights([&](float x, u64 order) { return place_of(x) < from && (last == 0ull || order >= last); },
-                          [&](const float* x, int step) { list_up(in_bin(x, step), x, step); });
+        if (by_count || place_of(value_of((uint32_t)(last >> 32))) < from) {
+          // (no sums by bin, or min-p's border before the bin's)
+          sum = sum_weights([&](float x, u64 order) { return place_of(x) < from && (last == 0ull || order >= last); },
+                            [&](const float* x, int step) { list_up(in_bin(x, step), x, step); });
+        } else {
+          const uint32_t *low = warp_bins + warp * kBins, *high = low + kWarps * kBins;
+          for (int i = lane; i < (int)bin; i += 32) sum += (u64)low[i] + ((u64)high[i] << 32);
+          for_steps([&](int step, const float* x) { list_up(in_bin(x, step), x, step); });
+        }
       }
       const int n = bring_together();
       if (rank == 0) {
@@ -871,7 +907,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
       for (int i = tid; i < own; i += kThreads) {
         const u64 c = s.list[i];
         if (c < last) continue;
-        const int step = (int)((kAll - (uint32_t)c) / (32 * V));
+        const int step = (int)((kAll - (uint32_t)c + shift) / (32 * V));
         int w = (int)(((long long)step * shares + shares - 1) / steps_all) - rank * kWarps;   // its run, or one beside it
         w = min(max(w, 0), kWarps - 1);
         while (w > 0 && first_step(rank * kWarps + w) > step) --w;
@@ -903,7 +939,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
           for (int j = 0; j < V; ++j) {
             const uint32_t key = key_of(x[j]);
             u64 w = 0ull;
-            if (key > above && (key & mask) == prefix && index_of(step, j) < a.vocab) w = weights ? weigh(x[j], s.table) : 1ull;
+            if (key > above && (key & mask) == prefix && there(index_of(step, j))) w = weights ? weigh(x[j], s.table) : 1ull;
             // lanes of the first one's digit together (many equal logits would queue up at one address)
             const uint32_t digit = (key >> shift) & 255u, active = __ballot_sync(kAll, w != 0ull);
             if (!active) continue;
@@ -962,7 +998,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
         float x[V];
         load(step, x);
 #pragma unroll
-        for (int j = 0; j < V; ++j) n += index_of(step, j) < a.vocab ? tie(x[j], order_of(x[j], index_of(step, j))) : 0ull;
+        for (int j = 0; j < V; ++j) n += there(index_of(step, j)) ? tie(x[j], order_of(x[j], index_of(step, j))) : 0ull;
       }
       if (tid == 0) s.sel_in = 0ull;
       locate(n, tie, [&](u64 all) { return min(ties, all) - 1ull; }, [&](int i, float x, u64 all) { s.sel_in = order_of(x, i); });
@@ -989,12 +1025,17 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
 
 }  // namespace
 
+cudaError_t init_draw_kernels() {
+  const cudaError_t e = cudaFuncSetAttribute(draw_kernel<bf16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kWarpBins);
+  return e != cudaSuccess ? e : cudaFuncSetAttribute(draw_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, kWarpBins);
+}
+
 cudaError_t launch_draw(const DrawArgs& a, Dtype dt, cudaStream_t st) {
   // CTAs of a row: up to 8 while there are SMs for all, and work for their warps
   int ranks = 1;
   while (ranks < kRanks && (long long)a.batch * ranks * 2 <= a.num_sms && a.vocab >= ranks * 2 * 4096) ranks *= 2;
   const Overlap overlap;
-  return launch_kernel_cluster(dt == DT_BF16 ? draw_kernel<bf16> : draw_kernel<float>, dim3(ranks, a.batch), dim3(kThreads), 0, st, dim3(ranks, 1, 1), a);
+  return launch_kernel_cluster(dt == DT_BF16 ? draw_kernel<bf16> : draw_kernel<float>, dim3(ranks, a.batch), dim3(kThreads), kWarpBins, st, dim3(ranks, 1, 1), a);
 }
 
 }  // namespace ravel
