@@ -6,18 +6,20 @@
 // tokens with that key stay; as one number, (key, ~index) of the last token that stays.
 //
 // A cluster of CTAs per row.  The row's maximum first; then a histogram of 512 bins between the
-// maximum and the least logit that has a weight, of counts and, where top-p alone limits, of weights: the
-// bin that holds the border.  Where the tokens up to that bin are at most 2048, they are brought
+// maximum and the least logit that has a weight, of counts or, where top-p alone limits, of weights too (of each warp's
+// run of the row): the bin that holds the border.  Where the tokens up to that bin are at most 2048, they are brought
 // together in one CTA, which does the rest by itself.  Where they are more, the bin's own tokens are, which gives
-// the border, while the weights before it are summed by warps' runs of the row; the run that holds the
+// the border, and the weights before it are summed by warps' runs; the run that holds the
 // token is gone through again.  Where even the bin holds more (thousands of nearly equal logits), a
 // radix selection over the keys' four bytes finds the border.
 //
 // Measured (replays from a graph): one row of 65536 bf16 logits under top-k 40, top-p and min-p 13 us, a chain of four
 // barriers of the cluster (1000 cycles each) and what lies between, a thousand here and there; 24 rows of 32003 under
-// settings of their own 30; 64 rows of 128001 fp32 logits under top-p 0.9 65 us, of which the histogram takes 21 (84
-// instructions a logit, 50 of them its weight, at two thirds of the issue rate), the list and the sums 14, the first
-// pass 5.5; the same without limits 33, with top-k 50 29, with top-k 3000 and top-p 75, all logits equal 467.
+// settings of their own 27; 64 rows of 128001 fp32 logits under top-p 0.9 53 us, of which the histogram takes 26 (80
+// instructions a logit, 50 of them its weight, and three atomics), the list 7, the first
+// pass 3 (66 with the weights before the border computed once more, and rows that begin between 16 bytes read value by
+// value); the same without limits 30, with top-k 50 24, with top-k 3000 and top-p 71, all logits equal 458.  Weights two
+// at a time in packed operations, and 64-bit atomics, are no faster.
 #include <algorithm>
 
 #include "common.cuh"

@@ -19,14 +19,15 @@ inline int w4_ranks(long long units, int kblocks, int blocks, int most, int sms)
 // there are few, are shared (after full rounds, whose CTAs all have to be there at once, by 2 CTAs).  Clusters of 8 of CTAs
 // that fill an SM start late: 64 rows x 2048 x 8192 16.7 us with them, 10.8 with 4.
 struct W4TcPlan {
-  int grid, ranks, pieces;   // pieces: of 128 ks, of the CTA that has most
+  int grid, ranks;
+  long long pieces;   // of 128 ks, of the CTA that has most
   W4TcPlan(const W4Args& a, int tokens) {
     const int units = (a.w.tiles + 7) / 8 * ((a.M + tokens - 1) / tokens), sms = a.num_sms / 2 * 2, all = (a.w.kblocks + 1) / 2;
     const bool rounds = units >= a.num_sms;
     const int last = rounds ? units % sms : units;
     ranks = last > 0 ? w4_ranks(last, a.w.kblocks, 4, rounds ? 2 : kRanks, sms) : 1;
     grid = !rounds ? units * ranks : ranks > 1 ? sms : a.num_sms;
-    pieces = (rounds ? units / sms * all : 0) + (last > 0 ? (all + ranks - 1) / ranks : 0);
+    pieces = (rounds ? (long long)(units / sms) * all : 0) + (last > 0 ? (all + ranks - 1) / ranks : 0);
   }
 };
 
