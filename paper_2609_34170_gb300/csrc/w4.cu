@@ -186,54 +186,44 @@ __device__ __forceinline__ void finish(const W4Args& a, int pair, int m0, int ra
   }
 }
 
-// A block's weights of a pair of tiles into the registers of A, and the rows' scales.
-template <bool G32>
-struct Operand {
-  uint32_t A[2][4][4];
-  float s0[2][G32 ? 2 : 1], s8[2][G32 ? 2 : 1];
-  __device__ __forceinline__ void set(const uint4* codes, const uint2* sz, int t) {   // sz: of the first 32, of the second
-    const uint32_t c[4] = {codes->x, codes->z, codes->y, codes->w};
+// Two blocks of a warp's codes and their groups' scales; GS: 32s of ks in a group.
+template <int GS>
+struct Slot {
+  uint4 codes[2][2][32];    // [block][tile]
+  uint2 sz[4 / GS][2][8];   // [group][tile]
+};
+
+// sum += a block's product with NT * 8 tokens' values x, chains of a group from zero; at a group's end acc += scale sum
+template <int NT, int GS, int B>
+__device__ __forceinline__ void multiply(const Slot<GS>& slot, int lane, int g, const uint4 (*x)[2], float (*sum)[NT][4], float (*acc)[NT][4]) {
 #pragma unroll
-    for (int h = 0; h < (G32 ? 2 : 1); ++h) {
-      s0[t][h] = __uint_as_float(sz[h].x & 0xffff0000u);
-      s8[t][h] = __uint_as_float(sz[h].y & 0xffff0000u);
-      const uint32_t z0 = __byte_perm(sz[h].x, 0u, 0x1010), z8 = __byte_perm(sz[h].y, 0u, 0x1010);
+  for (int t = 0; t < 2; ++t) {
+    const uint4 codes = slot.codes[B][t][lane];
+    const uint32_t c[4] = {codes.x, codes.z, codes.y, codes.w};
 #pragma unroll
-      for (int i = G32 ? 2 * h : 0; i < (G32 ? 2 * h + 2 : 4); ++i) widen(c[i], z0, z8, A[t][i]);
-    }
-  }
-  template <typename S>
-  __device__ __forceinline__ void set(const S& slot, int lane, int g) {
+    for (int h = 0; h < 2; ++h) {
+      const int at = 2 * B + h;   // of four 32s
+      const uint2 sz = slot.sz[at / GS][t][g];
+      const uint32_t z0 = __byte_perm(sz.x, 0u, 0x1010), z8 = __byte_perm(sz.y, 0u, 0x1010);
+      uint32_t A[2][4];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const uint4 c = slot.codes[t][lane];
-      uint2 sz[G32 ? 2 : 1];
+      for (int i = 0; i < 2; ++i) widen(c[2 * h + i], z0, z8, A[i]);
 #pragma unroll
-      for (int h = 0; h < (G32 ? 2 : 1); ++h) sz[h] = slot.sz[h][t][g];
-      set(&c, sz, t);
-    }
-  }
-  // acc += the block's product with 8 tokens' values x (of its first and its second 32 ks)
-  __device__ __forceinline__ void multiply(const uint4* x, float (*acc)[4], int stride) const {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-#pragma unroll
-      for (int h = 0; h < (G32 ? 2 : 1); ++h) {
-        float sum[4];
-        mma_bf16_first(sum, A[t][2 * h], x[h].x, x[h].y);
-        mma_bf16(sum, A[t][2 * h + 1], x[h].z, x[h].w);
-        if constexpr (!G32) {
-          mma_bf16(sum, A[t][2], x[1].x, x[1].y);
-          mma_bf16(sum, A[t][3], x[1].z, x[1].w);
+      for (int n = 0; n < NT; ++n) {
+        if (at % GS == 0) mma_bf16_first(sum[t][n], A[0], x[n][h].x, x[n][h].y);
+        else mma_bf16(sum[t][n], A[0], x[n][h].x, x[n][h].y);
+        mma_bf16(sum[t][n], A[1], x[n][h].z, x[n][h].w);
+        if (at % GS == GS - 1) {
+          const float s0 = __uint_as_float(sz.x & 0xffff0000u), s8 = __uint_as_float(sz.y & 0xffff0000u);
+          acc[t][n][0] += s0 * sum[t][n][0];
+          acc[t][n][1] += s0 * sum[t][n][1];
+          acc[t][n][2] += s8 * sum[t][n][2];
+          acc[t][n][3] += s8 * sum[t][n][3];
         }
-        acc[t * stride][0] += s0[t][h] * sum[0];
-        acc[t * stride][1] += s0[t][h] * sum[1];
-        acc[t * stride][2] += s8[t][h] * sum[2];
-        acc[t * stride][3] += s8[t][h] * sum[3];
       }
     }
   }
-};
+}
 
 // The sums of a warp into [token][kPitch].
 template <int NT>
@@ -255,66 +245,62 @@ __device__ __forceinline__ void put_sums(float* to, const float (*acc)[NT][4], i
 // takes its result into an fp32 sum, so that weights enter as whole numbers and no scaled weight
 // is rounded.  Parts of the ks are joined in the order of warps and ranks.
 //
-// Small matrices are a chain's latency: 1 row x 2560 x 1024 2.1 us (replays from a graph), 16 x 1024 x 4096 4.4.
-// Large ones are bound by the codes' widening: 226 instructions a block of 2048 codes, 11 of every 8 codes'
-// on the half-rate integer pipe, 56 % busy: 1 row x 65536 x 2048 22.4 us (3.2 TB/s of 6.7), x 8192 x 8192 12.3;
-// 16 rows 31.4 and 15.7.  With three CTAs an SM and 80 registers 23 and 18.5, with a division and 64-bit addresses a
-// block 27.5 and 23.
-constexpr int kRing = 6;   // blocks of 64 ks
-// CTAs an SM holds, by shared memory and registers
-template <int NT, bool G32>
-constexpr int kHeld = 2;
-template <bool G32>
-struct Slot {
-  uint4 codes[2][32];
-  uint2 sz[G32 ? 2 : 1][2][8];
-};
+// Small matrices are a chain's latency: 1 row x 2560 x 1024 2.1 us (replays from a graph), 16 x 1024 x 4096 4.7 in fp32 to a
+// residual.  Large ones are bound by the codes' widening, 11 instructions for every 8 codes, most of them on the half-rate
+// integer pipe: 1 row x 65536 x 2048 19.8 us (3.6 TB/s of 6.7), x 8192 x 8192 11.0; 16 rows x 8192 x 8192 13.5.  With
+// pieces of 64 ks 22.4, 12.3 and 15.7 (the copies' instructions and waits twice as often); those with three CTAs an SM and 80
+// registers 23 and 18.5, with a division and 64-bit addresses a piece 27.5 and 23.
+constexpr int kRing = 3;   // pieces of 128 ks
+constexpr int kHeld = 2;   // CTAs an SM holds, by registers
 
 // FAST: rows of x are 16-byte aligned and K a multiple of 8, so that a lane's eight values are there or not.
-template <int NT, bool G32, bool FAST>
-__global__ void __launch_bounds__(256, kHeld<NT, G32>) w4_gemm_kernel(W4Args a) {
+template <int NT, int GS, bool FAST>
+__global__ void __launch_bounds__(256, kHeld) w4_gemm_kernel(W4Args a) {
   constexpr int kPart = NT * 8 * kPitch;
   extern __shared__ __align__(16) unsigned char few_smem[];
-  Slot<G32>* ring = (Slot<G32>*)few_smem + (threadIdx.x >> 5) * kRing;
-  float* parts = (float*)((Slot<G32>*)few_smem + kWarps * kRing);   // [2][warp][token][kPitch]
+  Slot<GS>* ring = (Slot<GS>*)few_smem + (threadIdx.x >> 5) * kRing;
+  float* parts = (float*)((Slot<GS>*)few_smem + kWarps * kRing);   // [2][warp][token][kPitch]
   const W4Matrix& w = a.w;
   const int ranks = (int)gridDim.z, rank = ranks > 1 ? (int)cluster_ctarank() : 0;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
   const int pairs = w.tiles / 2, m0 = blockIdx.y * NT * 8;
   const int shares = ranks * kWarps, share = rank * kWarps + warp;
-  const int k0 = (int)((long long)w.kblocks * share / shares), k1 = (int)((long long)w.kblocks * (share + 1) / shares);
+  const int pieces = (w.kblocks + 1) / 2;
+  const int k0 = (int)((long long)pieces * share / shares), k1 = (int)((long long)pieces * (share + 1) / shares);
 
-  // the next block of the sequence (pair by pair, the warp's blocks of each) into the next slot
-  int next_pair = blockIdx.x, next_kb = k1, next_slot = 0;
-  const int per_group = w.group == 128 ? 7 : w.group == 64 ? 6 : 5;
-  const int sz_t = lane >> 2 & 1, sz_h = lane >> 3;   // 64 bytes of scales per tile and group: 4 lanes each
+  // the next piece of the sequence (pair by pair, the warp's pieces of each) into the next slot
+  int next_pair = blockIdx.x, next_piece = k1, next_slot = 0;
+  const int sz_t = lane >> 2 & 1, sz_g = lane >> 3;   // 64 bytes of scales per tile and group: 4 lanes each
   const uint4 *from0 = nullptr, *from1 = nullptr;
   const uint2* from_sz = nullptr;
   if (k0 == k1) next_pair = pairs;
   else next_pair -= (int)gridDim.x;
   auto fetch = [&] {
-    if (next_kb == k1 && next_pair < pairs) {
+    if (next_piece == k1 && next_pair < pairs) {
       next_pair += (int)gridDim.x;
-      next_kb = k0;
+      next_piece = k0;
       const int t0 = first_tile(min(next_pair, pairs - 1), a.epi), t1 = second_tile(min(next_pair, pairs - 1), a.epi);
-      from0 = w.codes + ((size_t)t0 * w.kblocks + k0) * 32 + lane;
-      from1 = w.codes + ((size_t)t1 * w.kblocks + k0) * 32 + lane;
+      from0 = w.codes + ((size_t)t0 * w.kblocks + 2 * k0) * 32 + lane;
+      from1 = w.codes + ((size_t)t1 * w.kblocks + 2 * k0) * 32 + lane;
       from_sz = w.sz + (size_t)(sz_t ? t1 : t0) * w.groups * 8 + q * 2;
     }
     if (next_pair < pairs) {
-      Slot<G32>& to = ring[next_slot];
-      copy_async(&to.codes[0][lane], from0, true);
-      copy_async(&to.codes[1][lane], from1, true);
-      if (sz_h < (G32 ? 2 : 1))
-        copy_async(&to.sz[sz_h][sz_t][q * 2], from_sz + (size_t)min((next_kb * 64 + sz_h * 32) >> per_group, w.groups - 1) * 8, true);
-      from0 += 32;
-      from1 += 32;
-      ++next_kb;
+      Slot<GS>& to = ring[next_slot];
+      const int second = 2 * next_piece + 1 < w.kblocks ? 32 : 0;   // (past the last block there are no values, and its codes will do)
+      copy_async(&to.codes[0][0][lane], from0, true);
+      copy_async(&to.codes[0][1][lane], from1, true);
+      copy_async(&to.codes[1][0][lane], from0 + second, true);
+      copy_async(&to.codes[1][1][lane], from1 + second, true);
+      if (sz_g < 4 / GS)
+        copy_async(&to.sz[sz_g][sz_t][q * 2], from_sz + (size_t)min(next_piece * (4 / GS) + sz_g, w.groups - 1) * 8, true);
+      from0 += 64;
+      from1 += 64;
+      ++next_piece;
       if (++next_slot == kRing) next_slot = 0;
     }
     copies_commit();
   };
-  // loaded weights do not change: the first blocks are on their way before the launch before has ended
+  // loaded weights do not change: the first pieces are on their way before the launch before has ended
 #pragma unroll 1
   for (int i = 0; i < kRing - 1; ++i) fetch();
   pdl_trigger();
@@ -342,21 +328,9 @@ __global__ void __launch_bounds__(256, kHeld<NT, G32>) w4_gemm_kernel(W4Args a) 
       }
   };
   int slot = 0, buf = 0;
-  float acc[2][NT][4];
-  // a block with its tokens in x, while the next one's come into xn
-  auto block = [&](int kb, uint4 (*x)[2], uint4 (*xn)[2]) {
-    copies_wait<kRing - 2>();
-    __syncwarp();
-    fetch();   // (into the slot that was read last)
-    load(xn, kb + 1 < k1 ? kb + 1 : k0);
-    Operand<G32> op;
-    op.set(ring[slot], lane, g);
-    if (++slot == kRing) slot = 0;
-#pragma unroll
-    for (int n = 0; n < NT; ++n) op.multiply(x[n], &acc[0][n], NT);
-  };
-  uint4 xa[NT][2], xb[NT][2];
-  if (k0 < k1) load(xa, k0);
+  float acc[2][NT][4], sum[2][NT][4];
+  uint4 xa[NT][2], xb[NT][2];   // a block's tokens, while the next one's are on their way
+  if (k0 < k1) load(xa, 2 * k0);
   for (int pair = blockIdx.x; pair < pairs; pair += gridDim.x, buf ^= 1) {
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -364,16 +338,16 @@ __global__ void __launch_bounds__(256, kHeld<NT, G32>) w4_gemm_kernel(W4Args a) 
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[t][n][i] = 0.f;
-    int kb = k0;
 #pragma unroll 1
-    for (; kb + 1 < k1; kb += 2) {
-      block(kb, xa, xb);
-      block(kb + 1, xb, xa);
-    }
-    if (kb < k1) {
-      block(kb, xa, xb);
-#pragma unroll
-      for (int n = 0; n < NT; ++n) xa[n][0] = xb[n][0], xa[n][1] = xb[n][1];
+    for (int piece = k0; piece < k1; ++piece) {
+      copies_wait<kRing - 2>();
+      __syncwarp();
+      fetch();   // (into the slot that was read last)
+      load(xb, 2 * piece + 1);
+      multiply<NT, GS, 0>(ring[slot], lane, g, xa, sum, acc);
+      load(xa, piece + 1 < k1 ? 2 * piece + 2 : 2 * k0);
+      multiply<NT, GS, 1>(ring[slot], lane, g, xb, sum, acc);
+      if (++slot == kRing) slot = 0;
     }
     float* part = parts + buf * kWarps * kPart;   // (two in turn: one barrier a pair)
     put_sums<NT>(part + warp * kPart, acc, g, q);
@@ -398,35 +372,38 @@ __global__ void __launch_bounds__(256, kHeld<NT, G32>) w4_gemm_kernel(W4Args a) 
   copies_wait<0>();
 }
 
-template <int NT, bool G32>
+template <int NT, int GS>
 constexpr size_t smem_of() {
-  return sizeof(Slot<G32>) * kWarps * kRing + sizeof(float) * 2 * kWarps * NT * 8 * kPitch;
+  return sizeof(Slot<GS>) * kWarps * kRing + sizeof(float) * 2 * kWarps * NT * 8 * kPitch;
 }
 
-template <int NT>
-cudaError_t init_nt() {
-  auto set = [](auto kernel, size_t bytes) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); };
-  cudaError_t e = set(w4_gemm_kernel<NT, false, false>, smem_of<NT, false>());
-  if (e == cudaSuccess) e = set(w4_gemm_kernel<NT, false, true>, smem_of<NT, false>());
-  if (e == cudaSuccess) e = set(w4_gemm_kernel<NT, true, false>, smem_of<NT, true>());
-  if (e == cudaSuccess) e = set(w4_gemm_kernel<NT, true, true>, smem_of<NT, true>());
-  return e;
+template <int NT, int GS>
+cudaError_t init_gs() {
+  static_assert(kHeld * (smem_of<NT, GS>() + 1024) <= 228 * 1024, "shared memory");
+  const cudaError_t e = cudaFuncSetAttribute(w4_gemm_kernel<NT, GS, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_of<NT, GS>());
+  return e != cudaSuccess ? e : cudaFuncSetAttribute(w4_gemm_kernel<NT, GS, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_of<NT, GS>());
 }
 
-template <int NT, bool G32>
+// CTAs that share a pair of tiles.  Their join costs a microsecond: 1 row x 2048 x 2048 2.7 us, by two CTAs 3.2; 1 x 1024 x 4096
+// by four 3.2, by two 3.7.
+int few_ranks(const W4Args& a, long long ctas) {
+  return a.w.kblocks < 6 * kWarps ? 1 : w4_ranks(ctas, a.w.kblocks, 2 * kWarps, kRanks, a.num_sms);
+}
+
+template <int NT, int GS>
 cudaError_t launch_few(const W4Args& a, cudaStream_t st) {
   const int pairs = a.w.tiles / 2, tiles = (a.M + NT * 8 - 1) / (NT * 8);
-  const int ranks = w4_ranks((long long)pairs * tiles, a.w.kblocks, kWarps, kRanks, a.num_sms);
+  const int ranks = few_ranks(a, (long long)pairs * tiles);
   // pairs beyond what the SMs hold at once follow one another in a CTA
-  const int held = kHeld<NT, G32> * a.num_sms;
+  const int held = kHeld * a.num_sms;
   const int across = ranks > 1 || pairs <= held ? pairs : std::max(1, held / std::min(tiles, held));
   const Overlap overlap;
-  return launch_kernel_cluster(a.vec && a.w.K % 8 == 0 ? w4_gemm_kernel<NT, G32, true> : w4_gemm_kernel<NT, G32, false>, dim3(across, tiles, ranks), dim3(256), smem_of<NT, G32>(), st,
-                               dim3(1, 1, ranks), a);
+  return launch_kernel_cluster(a.vec && a.w.K % 8 == 0 ? w4_gemm_kernel<NT, GS, true> : w4_gemm_kernel<NT, GS, false>, dim3(across, tiles, ranks), dim3(256),
+                               smem_of<NT, GS>(), st, dim3(1, 1, ranks), a);
 }
 template <int NT>
 cudaError_t launch_nt(const W4Args& a, cudaStream_t st) {
-  return a.w.group == 32 ? launch_few<NT, true>(a, st) : launch_few<NT, false>(a, st);
+  return a.w.group == 128 ? launch_few<NT, 4>(a, st) : a.w.group == 64 ? launch_few<NT, 2>(a, st) : launch_few<NT, 1>(a, st);
 }
 
 unsigned blocks_of(long long threads) { return (unsigned)((threads + 255) / 256); }
@@ -434,8 +411,12 @@ unsigned blocks_of(long long threads) { return (unsigned)((threads + 255) / 256)
 }  // namespace
 
 cudaError_t init_w4_kernels() {
-  cudaError_t e = init_nt<1>();
-  if (e == cudaSuccess) e = init_nt<2>();
+  cudaError_t e = init_gs<1, 1>();
+  if (e == cudaSuccess) e = init_gs<1, 2>();
+  if (e == cudaSuccess) e = init_gs<1, 4>();
+  if (e == cudaSuccess) e = init_gs<2, 1>();
+  if (e == cudaSuccess) e = init_gs<2, 2>();
+  if (e == cudaSuccess) e = init_gs<2, 4>();
   if (e == cudaSuccess) e = init_w4_tc_kernels();
   return e;
 }
@@ -449,7 +430,7 @@ cudaError_t launch_w4_gemm(const W4Args& a, cudaStream_t st) {
   // 6.6; 64 x 4096 x 1024 7.0 / 6.9, x 2048 x 2048 5.3 / 6.5; 96 x 4096 x 1024 10.3 / 7.1; groups of 32, 64 rows x 512 x 8192
   // 10.2 / 15.3.  (TMA takes aligned rows only.)
   const long long tiles = (a.M + 15) / 16, ctas = a.w.tiles / 2 * tiles;
-  const int ranks = w4_ranks(ctas, a.w.kblocks, kWarps, kRanks, a.num_sms);
+  const int ranks = few_ranks(a, ctas);
   const long long blocks = (a.w.kblocks + kWarps * ranks - 1) / (kWarps * ranks) * ((ctas * ranks + 2 * a.num_sms - 1) / (2 * a.num_sms));
   const W4TcPlan plan(a, a.M <= 32 ? 32 : 64);
   const bool tc = 10 * blocks > 33 + (a.w.group == 32 && a.M > 32 ? 7ll : 4ll) * plan.pieces;
