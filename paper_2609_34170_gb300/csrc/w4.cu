@@ -423,17 +423,20 @@ cudaError_t init_w4_kernels() {
 
 cudaError_t launch_w4_gemm(const W4Args& a, cudaStream_t st) {
   if (a.M <= 8) return launch_nt<1>(a, st);
-  // Tiles of 16 rows go through the matrix each, from L2 after the first, in about 2.5 us and 0.8 to 1 for each block of 64 ks of
-  // a warp; the tcgen05 kernel (an SM a CTA, a longer start) takes 5.5 and 0.4 for each piece of 128 ks of a CTA, 0.7 where its
-  // sums are many.  us, tiles / tcgen05, groups of 128: 16 rows x 4096 x 8192 15.1 / 10.7, x 8192 x 8192 15.7 / 16.4, x 65536 x
-  // 2048 31.6 / 26.3, x 1024 x 16384 9.6 / 15.3; 32 rows x 2048 x 4096 8.3 / 6.7, x 1024 x 4096 5.7 / 6.7, x 8192 x 1024 7.0 /
-  // 6.6; 64 x 4096 x 1024 7.0 / 6.9, x 2048 x 2048 5.3 / 6.5; 96 x 4096 x 1024 10.3 / 7.1; groups of 32, 64 rows x 512 x 8192
-  // 10.2 / 15.3.  (TMA takes aligned rows only.)
+  // Tiles of 16 rows that go through the matrix each, from L2 after the first, or the tcgen05 kernel (an SM a CTA, a longer
+  // start), whichever takes less by these times, in 10 ns: of tiles a start, rounds, blocks of 64 ks of a warp (faster where an
+  // SM has one CTA) and a cluster's join; of tcgen05 a start and pieces of 128 ks of a CTA, longer where its sums are many.  us,
+  // tiles / tcgen05, groups of 128: 16 rows x 4096 x 4096 5.8 / 7.7, x 8192 x 8192 13.5 / 16.3, x 65536 x 2048 26.7 / 26.1; 32 x
+  // 2048 x 4096 5.8 / 6.7, x 3000 x 5000 9.3 / 8.2, x 8192 x 8192 25.6 / 16.7, x 1024 x 16384 13.3 / 15.6; 64 x 4096 x 1024
+  // 6.4 / 6.7, x 1024 x 4096 5.8 / 7.4, x 2048 x 8192 13.5 / 10.6; 96 x 4096 x 1024 9.3 / 6.8; groups of 32, 16 x 4096 x 8192
+  // 14.3 / 12.1, 64 x 512 x 8192 9.2 / 15.2, 48 x 8192 x 1024 9.9 / 8.2.  (TMA takes aligned rows only.)
   const long long tiles = (a.M + 15) / 16, ctas = a.w.tiles / 2 * tiles;
   const int ranks = few_ranks(a, ctas);
-  const long long blocks = (a.w.kblocks + kWarps * ranks - 1) / (kWarps * ranks) * ((ctas * ranks + 2 * a.num_sms - 1) / (2 * a.num_sms));
-  const W4TcPlan plan(a, a.M <= 32 ? 32 : 64);
-  const bool tc = 10 * blocks > 33 + (a.w.group == 32 && a.M > 32 ? 7ll : 4ll) * plan.pieces;
+  const long long rounds = (ctas * ranks + kHeld * a.num_sms - 1) / (kHeld * a.num_sms), blocks = (a.w.kblocks + kWarps * ranks - 1) / (kWarps * ranks);
+  const bool g32 = a.w.group == 32, alone = !g32 && ctas * ranks <= a.num_sms;
+  const long long as_tiles = 150 + rounds * (100 + blocks * (alone ? 45 : 70)) + (ranks > 1 ? 200 : 0);
+  const long long as_tc = 500 + W4TcPlan(a, a.M <= 32 ? 32 : 64).pieces * (a.M <= 32 ? (g32 ? 45 : 35) : g32 ? 70 : 40);
+  const bool tc = as_tc < as_tiles;
   return a.vec && tc ? launch_w4_tc(a, st) : launch_nt<2>(a, st);
 }
 
