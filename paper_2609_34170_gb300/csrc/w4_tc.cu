@@ -486,6 +486,9 @@ template <int NTOK, int GS>
 cudaError_t init_gs() {
   static_assert(sizeof(typename TcShape<NTOK, GS>::Shared) <= kTcSmem, "shared memory");
   static_assert(sizeof(typename TcShape<NTOK, GS>::Piece) % 1024 == 0, "swizzled tiles");
+  // (a set's last wait was kSets pieces ago; the round before the one that it waits for now has to have ended by then, for a
+  // barrier's parity does not tell a round from the second next one)
+  static_assert(TcShape<NTOK, GS>::kPieces >= kSets, "places");
   static_assert(TcShape<NTOK, GS>::kPieces * TcShape<NTOK, GS>::kColsA + TcShape<NTOK, GS>::kSlots * TcShape<NTOK, GS>::kColsAcc <= (int)kTcCols, "tensor memory");
   return cudaFuncSetAttribute(w4_tc_kernel<NTOK, GS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kTcSmem);
 }
