@@ -18,7 +18,7 @@
 // settings of their own 27; 64 rows of 128001 fp32 logits under top-p 0.9 53 us, of which the histogram takes 26 (80
 // instructions a logit, 50 of them its weight, and three atomics), the list 7, the first
 // pass 3 (66 with the weights before the border computed once more, and rows that begin between 16 bytes read value by
-// value); the same without limits 30, with top-k 50 24, with top-k 3000 and top-p 71, all logits equal 458.  Weights two
+// value); the same without limits 30, with top-k 50 24, with top-k 3000 and top-p 71, all logits equal 457.  Weights two
 // at a time in packed operations, and 64-bit atomics, are no faster.
 #include <algorithm>
 
@@ -38,9 +38,9 @@ constexpr int kWarpBins = 2 * kWarps * kBins * 4;   // bytes of the weights of w
 
 typedef unsigned long long u64;
 
-// 2^(j / 1024) in units of 2^-62
+// 2^(j / 1024) = h 2^-30 (1 + d): h, a whole number, and d in units of 2^-42, as a float's bits
 struct ExpTable {
-  u64 v[1024];
+  uint2 v[1024];
   constexpr ExpTable() : v() {
     for (int j = 0; j < 1024; ++j) {
       const double x = 0.6931471805599453094 * j / 1024.0;
@@ -49,7 +49,9 @@ struct ExpTable {
         term *= x / i;
         sum += term;
       }
-      v[j] = (u64)(sum * 4611686018427387904.0);
+      const double h = sum * 1073741824.0;
+      v[j].x = (uint32_t)(h + 0.5);
+      v[j].y = __builtin_bit_cast(uint32_t, (float)((h / v[j].x - 1.0) * 4398046511104.0));
     }
   }
 };
@@ -79,7 +81,7 @@ struct Weigher {
     ch = __fdiv_rn(c, temperature);
     cl = __fdiv_rn(__fmaf_rn(-ch, temperature, c) + less, temperature);
   }
-  __device__ __forceinline__ u64 operator()(float logit, const u64* table) const {
+  __device__ __forceinline__ u64 operator()(float logit, const uint2* table) const {
     const float x = 0.5f * logit;   // (halves, so that no difference overflows)
     const float dh = x - top;
     const float v = dh - x, dl = (x - (dh - v)) - (top + v);
@@ -88,23 +90,23 @@ struct Weigher {
     const float ye = __fmaf_rn(dh, ch, -yh) + __fmaf_rn(dh, cl, dl * ch);
     const float shifted = __fmaf_rn(yh, 1024.f, 12582912.f);   // 1.5 * 2^23: q in the low bits
     const int q = __float_as_int(shifted) - 0x4b400000;
+    const uint2 t = table[__float_as_int(shifted) & 1023];
     const float rest = __fmaf_rn(shifted - 12582912.f, -0x1p-10f, yh);   // exact, up to 2^-11
     // r in units of 2^-42: ln 2 rest as a float and what it lacks, the small terms with the latter
     const float rh = rest * 0.693147182f;
     const float f = (rest + ye) * 0.693147182f;
     const float rl = __fmaf_rn(rest, 0.693147182f, -rh) + __fmaf_rn(rest, -1.90465421e-9f, ye * 0.693147182f) +
                      f * f * __fmaf_rn(f, 0.166666667f, 0.5f);
-    const int r = __float2int_rn(rh * 0x1p42f) + __float2int_rn(rl * 0x1p42f);
-    const u64 t = table[q & 1023];   // in units of 2^-62
-    const u64 w = t + (u64)((long long)(uint32_t)(t >> 31) * r >> 11);
-    const int down = 62 - kBits - (q >> 10);
-    return (w + (1ull << (down - 1))) >> down;
+    const int r = __float2int_rn(rh * 0x1p42f) + __float2int_rn(__fmaf_rn(rl, 0x1p42f, __uint_as_float(t.y)));
+    // h (1 + r 2^-42), in units of 2^-52, and rounded to 2^-43
+    const long long v52 = (long long)(int)t.x * (1 << 22) + ((long long)(int)t.x * r >> 20);
+    return (((u64)v52 >> (51 - kBits - (q >> 10))) + 1ull) >> 1;
   }
 };
 
 // ln(p) for 0 < p < 1 in two floats, off by some 2^-43: ln of p's mantissa m from logf, corrected by what
 // m lacks of exp of that, and its exponent.
-__device__ __forceinline__ float2 log_of(float p, const u64* table) {
+__device__ __forceinline__ float2 log_of(float p, const uint2* table) {
   int e;
   const float m = frexpf(p, &e);   // 1/2 <= m < 1
   const float y = logf(m);
@@ -163,7 +165,7 @@ __device__ __forceinline__ u64 warp_sum_u64(u64 v) {
 }
 
 struct DrawShared {
-  u64 table[1024];
+  uint2 table[1024];
   union {
     struct {
       uint32_t bins[kBins];     // of a CTA: counts
@@ -212,7 +214,7 @@ __device__ __noinline__ ulonglong2 scan_block(DrawShared& s, u64 x) {
   return make_ulonglong2(__shfl_sync(0xffffffffu, ws - w, warp) + upto - x, __shfl_sync(0xffffffffu, ws, 31));
 }
 
-__device__ __noinline__ u64 weight_of(const Weigher& weigh, u64 order, const u64* table) {
+__device__ __noinline__ u64 weight_of(const Weigher& weigh, u64 order, const uint2* table) {
   return weigh(value_of((uint32_t)(order >> 32)), table);
 }
 
