@@ -41,8 +41,9 @@ typedef struct {
                            frequency makes over that length: in full for t <= low, not at all for t >= high,
                            and in between f_i (g + (1 - g) / factor) with g = (t - low) / (high - low) */
   double low, high;     /* 0 <= low < high, read where original_length > 0 */
-  double amplitude;     /* of the turned dims, finite (1: lengths stay) */
-  const double* frequencies; /* host [dims / 2] or NULL: the f_i themselves, in the place of base to high; finite */
+  double amplitude;     /* of the turned dims, finite in fp32 (1: lengths stay) */
+  const double* frequencies; /* host [dims / 2] or NULL: the f_i themselves, in the place of base to high; given or made,
+                           they are finite */
 } ravel_rotary_config;
 
 typedef struct ravel_rotary_ctx ravel_rotary_t;

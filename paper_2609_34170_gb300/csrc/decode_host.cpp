@@ -3,6 +3,7 @@
 #include <cuda_runtime.h>
 
 #include <atomic>
+#include <cfloat>
 #include <cmath>
 #include <cstdio>
 #include <new>
@@ -76,19 +77,32 @@ void free_matrix(ravel_w4_t* w) {
   delete w;
 }
 
+const double kTwoPi = 6.283185307179586476925;
+
+// f_i
+double rotary_frequency(const ravel_rotary_config& c, int i) {
+  if (c.frequencies) return c.frequencies[i];
+  const double f = std::pow(c.base, -2.0 * i / c.dims);
+  double g = 0.0;
+  if (c.original_length > 0) {
+    g = (c.original_length * f / kTwoPi - c.low) / (c.high - c.low);
+    g = g < 0.0 ? 0.0 : g > 1.0 ? 1.0 : g;
+  }
+  return g >= 1.0 ? f : f * (g + (1.0 - g) / c.factor);
+}
+
 const char* rotary_fault(const ravel_rotary_config& c) {
   if (c.dims < 2 || c.dims % 2 || c.dims > 256) return "dims must be even, 2 to 256";
   if (c.interleaved != 0 && c.interleaved != 1) return "interleaved must be 0 or 1";
-  if (!std::isfinite(c.amplitude)) return "amplitude must be finite";
-  if (c.frequencies) {
-    for (int i = 0; i < c.dims / 2; ++i)
-      if (!std::isfinite(c.frequencies[i])) return "frequencies must be finite";
-    return nullptr;
+  if (!(std::fabs(c.amplitude) <= FLT_MAX)) return "amplitude must be finite in fp32";
+  if (!c.frequencies) {
+    if (!(c.base > 0) || !std::isfinite(c.base)) return "base must be positive";
+    if (!(c.factor > 0) || !std::isfinite(c.factor)) return "factor must be positive";
+    if (!(c.original_length >= 0) || !std::isfinite(c.original_length)) return "original_length must not be negative";
+    if (c.original_length > 0 && !(c.low >= 0 && c.low < c.high && std::isfinite(c.high))) return "0 <= low < high is wanted";
   }
-  if (!(c.base > 0) || !std::isfinite(c.base)) return "base must be positive";
-  if (!(c.factor > 0) || !std::isfinite(c.factor)) return "factor must be positive";
-  if (!(c.original_length >= 0) || !std::isfinite(c.original_length)) return "original_length must not be negative";
-  if (c.original_length > 0 && !(c.low >= 0 && c.low < c.high && std::isfinite(c.high))) return "0 <= low < high is wanted";
+  for (int i = 0; i < c.dims / 2; ++i)   // (a small base or factor makes large ones)
+    if (!std::isfinite(rotary_frequency(c, i))) return "frequencies must be finite";
   return nullptr;
 }
 
@@ -97,21 +111,8 @@ const char* rotary_fault(const ravel_rotary_config& c) {
 namespace ravel {
 
 unsigned long long rotary_turns(const ravel_rotary_config& c, int i) {
-  const double two_pi = 6.283185307179586476925;
-  double f;
-  if (c.frequencies) {
-    f = c.frequencies[i];
-  } else {
-    f = std::pow(c.base, -2.0 * i / c.dims);
-    double g = 0.0;
-    if (c.original_length > 0) {
-      g = (c.original_length * f / two_pi - c.low) / (c.high - c.low);
-      g = g < 0.0 ? 0.0 : g > 1.0 ? 1.0 : g;
-    }
-    f = g >= 1.0 ? f : f * (g + (1.0 - g) / c.factor);
-  }
   // turns per position modulo 1: whole turns do nothing at whole positions
-  double turns = f / two_pi;
+  double turns = rotary_frequency(c, i) / kTwoPi;
   turns -= std::floor(turns);
   // (two halves: 2^64 itself is no uint64)
   const double high = std::floor(turns * 4294967296.0);
