@@ -486,6 +486,16 @@ def ravel_cache_read(c, layer: int, k, v, firsts=None, lengths=None, stream=None
                                             _stream_ptr(stream)), "ravel_cache_read")
 
 
+_INT_MAX = (1 << 31) - 1
+
+
+def _fit_ints(what: str, *values):
+    """ctypes passes the low 32 bits of what does not fit into an int."""
+    for x in values:
+        if not -_INT_MAX <= x <= _INT_MAX:
+            raise ValueError(f"{what}: {x} is beyond 2^31 - 1")
+
+
 def ravel_cache_append_rotary(c, layer: int, rotary, q, q_out, k, v, starts=None, positions=None, counts=None, stream=None):
     """q, q_out [B, n, Hq, hd] (or None), k, v [B, n, Hkv, hd]; positions int32 [B, n]; see ravel_decode.h."""
     a = _arguments(c)
@@ -497,6 +507,7 @@ def ravel_cache_append_rotary(c, layer: int, rotary, q, q_out, k, v, starts=None
     if v.shape != shape:
         raise ValueError("k and v must have the same shape")
     B, n = shape[0], shape[1]
+    _fit_ints("ravel_cache_append_rotary", layer, B, n)
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out go together")
     qp = qop = None
@@ -559,9 +570,6 @@ def _flat(t, shape: tuple, dtype, device: int, name: str):
     raise ValueError(f"{name} must be a contiguous tensor {list(shape)} of {dtype} on cuda:{device}, got {got}")
 
 
-_INT_MAX = (1 << 31) - 1   # (ctypes cuts off what does not fit into an int)
-
-
 def _matrix(t, rows: int, cols: int, device: int, name: str, wide: bool = False) -> int:
     """Row stride (an int; wide: a long long) of a [rows, cols] tensor whose rows are contiguous; of
     a single row, whose stride means nothing, the next multiple of 8."""
@@ -581,6 +589,7 @@ def ravel_rotary_create(dims: int, base: float = 10000.0, interleaved: bool = Fa
                         original_length: float = 0.0, low: float = 1.0, high: float = 32.0, amplitude: float = 1.0,
                         frequencies=None, device: int = 0):
     f = None
+    _fit_ints("ravel_rotary_create", dims, device)
     if frequencies is not None:
         f = np.ascontiguousarray(frequencies, dtype=np.float64)
         if f.shape != (dims // 2,):
@@ -634,6 +643,7 @@ def ravel_rotary_apply(r, x, out, starts=None, positions=None, counts=None, stre
 
 def ravel_w4_create(N: int, K: int, group: int = 128, device: int = 0):
     h = C.c_void_p()
+    _fit_ints("ravel_w4_create", N, K, group, device)
     _check_decode(load().ravel_w4_create(N, K, group, device, C.byref(h)), "ravel_w4_create")
     h.w4 = (N, K, group, device)
     return h
@@ -670,6 +680,7 @@ def ravel_w4_quantize(W, group: int, codes, scales, zeros, stream=None):
     if W.dim() != 2 or device < 0:
         raise ValueError(f"W must be a CUDA tensor [N, K], got {tuple(W.shape)} on {W.device}")
     N, K = W.shape
+    _fit_ints("ravel_w4_quantize", group)
     ldw = _matrix(W, N, K, device, "W")
     groups = -(-K // group)
     with torch.cuda.device(device):
@@ -695,6 +706,8 @@ def ravel_w4_gemm(w, X, epi: int, out, bias=None, stream=None):
     types = _types()
     if X.dtype is not types.bf16:
         raise ValueError(f"X must be bfloat16, got {X.dtype}")
+    if not 0 <= epi <= 3:
+        raise ValueError(f"unknown epilogue {epi}")
     M = X.shape[0]
     lda = _matrix(X, M, K, device, "X")
     ldo = _matrix(out, M, N // 2 if epi == 3 else N, device, "out")

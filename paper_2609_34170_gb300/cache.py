@@ -79,6 +79,8 @@ class ContextCache:
             raise ValueError("k and v must have the same shape")
         vrs, vts = rows(v, self.n_kv_heads, "v")
         batch, n = shape[0], shape[1]
+        if (layer | batch | n) >> 31:
+            B._fit_ints("append_rotary", layer, batch, n)
         q_at = out_at = None
         qrs = qts = ors = ots = 0
         if q is not None:

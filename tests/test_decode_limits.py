@@ -22,3 +22,51 @@ def test_rotary_refuses_settings_whose_table_is_not_finite(lib, bad):
     with pytest.raises(RavelError) as ei:
         ravel_rotary_create(**{**dict(dims=16), **bad})
     assert ei.value.status == 1 and "finite" in str(ei.value)
+
+
+def _wide(of: int) -> int:
+    """What an int of 32 bits makes `of` from."""
+    return of + (1 << 32)
+
+
+def test_settings_beyond_an_int_are_refused_not_cut_off(lib):
+    """ctypes passes the low 32 bits of a Python int: a matrix of other sizes than the handle's, a group of 32 for scales
+    of one group a row (read past their end)."""
+    import paper_2609_34170_gb300 as pkg
+    from tests.test_decode_host import _Gpu
+    for args in ((_wide(96), 64, 32), (96, _wide(64), 32), (96, 64, _wide(32)), (96, 64, 32, _wide(0)), (96, 64, 32 - (1 << 32))):
+        with pytest.raises(ValueError, match="2\\^31"):
+            pkg.ravel_w4_create(*args)
+    with pytest.raises(ValueError, match="2\\^31"):
+        pkg.ravel_rotary_create(_wide(16))
+    with pytest.raises(ValueError, match="2\\^31"):
+        pkg.ravel_rotary_create(16, device=_wide(0))
+    f32, b16, u8 = torch.float32, torch.bfloat16, torch.uint8
+    with pytest.raises(ValueError, match="2\\^31"):
+        pkg.ravel_w4_quantize(_Gpu((4, 64), f32), _wide(32), _Gpu((4, 32), u8), _Gpu((4, 1), b16), _Gpu((4, 1), u8), stream=0)
+    w = C.c_void_p()
+    w.w4 = (256, 70, 32, 0)
+    with pytest.raises(ValueError, match="epilogue"):
+        pkg.ravel_w4_gemm(w, _Gpu((4, 70), b16), _wide(3), _Gpu((4, 256), b16), None, stream=0)
+
+
+def test_append_rotary_refuses_sizes_beyond_an_int(lib):
+    """(k of one robot seen 2^32 + 1 times would be stored once)"""
+    import paper_2609_34170_gb300 as pkg
+    from paper_2609_34170_gb300 import _binding as B
+    from tests.test_decode_host import _Gpu, _rotary_handle
+    c = C.c_void_p()
+    c.arguments = B.CacheArguments(n_q_heads=4, n_kv_heads=2, head_dim=64, dtype=B.RAVEL_BF16, device=0)
+    cache = pkg.ContextCache.__new__(pkg.ContextCache)
+    cache.handle, cache._lib, cache._rows, cache._ints, cache._dense = c, lib, c.arguments.rows, c.arguments.ints, c.arguments.dense
+    cache.n_q_heads, cache.n_kv_heads, cache._stream = 4, 2, lambda stream: 0
+    rotary = pkg.Rotary.__new__(pkg.Rotary)
+    rotary.handle = _rotary_handle()
+    for layer, shape, stride in ((0, (_wide(1), 3, 2, 64), (0, 128, 64, 1)), (0, (3, _wide(1), 2, 64), (128, 0, 64, 1)),
+                                 (_wide(0), (3, 5, 2, 64), None)):
+        k = _Gpu(shape, torch.bfloat16, stride)
+        with pytest.raises(ValueError, match="2\\^31"):
+            pkg.ravel_cache_append_rotary(c, layer, rotary.handle, None, None, k, k, stream=0)
+        with pytest.raises(ValueError, match="2\\^31"):
+            cache.append_rotary(layer, rotary, None, k, k)
+    rotary.handle = cache.handle = None   # (nothing to close)
