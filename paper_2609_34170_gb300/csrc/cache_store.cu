@@ -593,8 +593,8 @@ cudaError_t launch_cache_append(const AppendArgs& a, Dtype dt, cudaStream_t st) 
 cudaError_t launch_cache_append_rotary(const AppendRotaryArgs& a, Dtype dt, cudaStream_t st) {
   // Queries of few tokens in the same launch: a token of 64 robots (8 query heads on one of 256) 2.9 us, turned and
   // stored by two calls 3.7.  Of many in one that streams them: 816 tokens of 16 robots 31 us (81 in one launch;
-  // two calls, whose keys are rounded to bf16 in between, 27).
-  const bool apart = a.q && a.n > 16;
+  // two calls, whose keys are rounded to bf16 in between, 27).  (A grid has 65535 rows of CTAs, a cache up to as many heads.)
+  const bool apart = a.q && (a.n > 16 || a.c.Hkv > 65535 / 2);
   if (apart) {
     RotaryArgs r{a.r, a.q, a.q_out, a.q_robot, a.q_token, a.qo_robot, a.qo_token, a.batch, a.n, a.c.Hkv * a.G, a.c.hd,
                  a.starts, a.positions, a.counts, a.q_align, a.num_sms, a.max_tokens};

@@ -1,0 +1,23 @@
+"""Rotary positions, 4-bit products and drawing tokens at the ends of what their headers allow."""
+import pytest
+
+from tests.test_gpu_decode import _ints, _lib, _rand  # noqa: F401
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dims,interleaved", [(8, False), (4, True)])
+def test_append_rotary_of_more_heads_than_half_a_grid(dims, interleaved):
+    """As apply and append with fp32 between them; keys and queries of one launch would be 2 x 40000 rows of CTAs."""
+    from paper_2609_34170_gb300 import ContextCache, Rotary
+    heads, hd = 40000, 8
+    r = Rotary(dims, interleaved=interleaved)
+    cache, plain = (ContextCache(1, heads, heads, hd, 16, 1, 1, dtype) for dtype in ("bf16", "fp32"))
+    q, k, v = (_rand((1, 3, heads, hd), s, "bf16") for s in (1, 2, 3))
+    starts = _ints([5])
+    got = cache.append_rotary(0, r, q, k, v, starts)
+    plain.append(0, r.apply(k.float(), starts=starts), v.float(), starts)
+    assert torch.equal(got, r.apply(q, starts=starts))
+    for a, b in zip(cache.read(0, 1, 8), plain.read(0, 1, 8)):
+        assert torch.equal(a.float(), b)
