@@ -72,7 +72,8 @@ ravel_status ravel_rotary_apply(ravel_rotary_t* r, int batch, int n, int heads, 
  * with them, in one call.  Between a turned key and the cache nothing is rounded
  * but to the cache's own values.
  *   q, q_out   device [batch, n, Hq, hd] of the cache's dtype, or both NULL; q_out is q itself (with q's strides)
- *              or overlaps none of the others; its rows do not overlap each other
+ *              or overlaps none of the others; its rows do not overlap each other.  Hq * (hd rounded up to 64) is at
+ *              most 2^30
  *   k, v       as for ravel_cache_append, each with strides of its own; they are not written
  *   positions  device int32 [batch, n] or NULL: starts[b] + i
  *   starts, counts  as for ravel_cache_append; rows of q_out from counts[b] on are not written

@@ -226,6 +226,8 @@ ravel_status ravel_cache_append_rotary(ravel_cache_t* c, int layer, const ravel_
   if (n < 1 || n > c->cfg.max_tokens) return fail(c, RAVEL_ESHAPE, "append_rotary: n outside [1, max_tokens]");
   if (((uintptr_t)q | (uintptr_t)q_out | (uintptr_t)k | (uintptr_t)v) % c->esize)
     return fail(c, RAVEL_EINVAL, "append_rotary: unaligned q, q_out, k or v");
+  if (q && (long long)c->cfg.n_q_heads * c->hdp > (1 << 30))   // (places in a token's queries are counted in 32 bits)
+    return fail(c, RAVEL_ESHAPE, "append_rotary: more than 2^30 values in the query heads of a token");
   if (q && rows_overlap(batch, n, (long long)c->cfg.n_q_heads * c->cfg.head_dim, q_out_robot_stride, q_out_token_stride))
     return fail(c, RAVEL_EINVAL, "append_rotary: rows of q_out overlap");
   if (r->table.dims > c->cfg.head_dim) return fail(c, RAVEL_ESHAPE, "append_rotary: the table has more dims than a head");

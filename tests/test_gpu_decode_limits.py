@@ -21,3 +21,18 @@ def test_append_rotary_of_more_heads_than_half_a_grid(dims, interleaved):
     assert torch.equal(got, r.apply(q, starts=starts))
     for a, b in zip(cache.read(0, 1, 8), plain.read(0, 1, 8)):
         assert torch.equal(a.float(), b)
+
+
+def test_append_rotary_refuses_queries_beyond_what_it_counts():
+    """Places in a token's queries are counted in 32 bits.  (The addresses are never looked at.)"""
+    from paper_2609_34170_gb300 import ContextCache, Rotary, load
+    heads, hd = 1 << 23, 256
+    cache, r = ContextCache(1, heads, 1, hd, 16, 1), Rotary(hd)
+    k = _rand((1, 1, 1, hd), 0, "bf16")
+    assert load().ravel_cache_append_rotary(cache.handle, 0, r.handle, 1, 1, 1 << 20, 0, 0, 1 << 20, 0, 0, k.data_ptr(), 0, 0, k.data_ptr(), 0,
+                                            0, None, None, None, 0) == 2
+    assert cache.append_rotary(0, r, None, k, k) is None   # keys alone are not limited
+    held = cache.read(0, 1, 1)[0]
+    other = ContextCache(1, 1, 1, hd, 16, 1)
+    other.append_rotary(0, r, None, k, k)
+    assert torch.equal(held, other.read(0, 1, 1)[0])
