@@ -72,17 +72,21 @@ __device__ __forceinline__ float value_of(uint32_t key) {
 // from its series, r below 2^-11, whose first term is a product in two floats.  About 2^-43 of the
 // weight off.  (In fp32 a weight is 2^-22 off and its error grows with x: at 100000 tokens one
 // border in a hundred falls elsewhere than in 64 bits.)
+// Logits are halved, so that no difference overflows, and where T is above 2^64 taken by 2^-65 (as T by 2^-64), or
+// c's second float, from 10^32 on, and its first, from 2 10^38 on, would lack bits.
 struct Weigher {
-  float top, ch, cl;   // half the largest logit; twice log2(e) / T
+  float scale, top, ch, cl;   // of the logits; the largest one's share of it; twice log2(e) / T
   // (in two floats: 64-bit ones come two to a clock)
   __device__ __forceinline__ Weigher(float max, float temperature) {
     const float c = 2.88539004f, less = 3.851925982e-08f;   // 2 log2(e) = c + less
-    top = 0.5f * max;
+    scale = temperature > 0x1p64f ? 0x1p-65f : 0.5f;
+    temperature *= 2.f * scale;
+    top = scale * max;
     ch = __fdiv_rn(c, temperature);
     cl = __fdiv_rn(__fmaf_rn(-ch, temperature, c) + less, temperature);
   }
   __device__ __forceinline__ u64 operator()(float logit, const uint2* table) const {
-    const float x = 0.5f * logit;   // (halves, so that no difference overflows)
+    const float x = scale * logit;
     const float dh = x - top;
     const float v = dh - x, dl = (x - (dh - v)) - (top + v);
     const float yh = dh * ch;
@@ -383,7 +387,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
   auto answer = [&](int token, float x, u64 total) {
     a.tokens[b] = token;
     if (!a.log_probs) return;
-    const float d = 0.5f * x - weigh.top, yh = d * weigh.ch, yl = __fmaf_rn(d, weigh.ch, -yh) + d * weigh.cl;
+    const float d = weigh.scale * x - weigh.top, yh = d * weigh.ch, yl = __fmaf_rn(d, weigh.ch, -yh) + d * weigh.cl;
     const int e = 63 - __clzll((long long)total);
     const float m = (float)total * exp2f((float)-e);   // total = m 2^e
     const float h = yh - (float)(e - kBits), v = h - yh, l = (yh - (h - v)) + (-(float)(e - kBits) - v) + yl;
@@ -427,11 +431,11 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
 
   // Bins of the order: equal parts of the log2 domain from the maximum down to the least logit or
   // to 2^-44, where weights end.  Every step of the formula is monotone in x, rounding included.
-  const float d_least = 0.5f * value_of(~(uint32_t)low) - weigh.top, y_least = fmaxf(d_least * weigh.ch, -44.f);
+  const float d_least = weigh.scale * value_of(~(uint32_t)low) - weigh.top, y_least = fmaxf(d_least * weigh.ch, -44.f);
   const float to_place = -weigh.ch * ((float)(kBins - 1) / fmaxf(-y_least, 0x1p-40f));
   // place in bins, for bin i from i up to below i + 1 (the last but one: from there on)
-  auto place_of = [&](float x) { return (0.5f * x - weigh.top) * to_place; };
-  auto weighs = [&](float x) { return (0.5f * x - weigh.top) * weigh.ch > -44.f; };
+  auto place_of = [&](float x) { return (weigh.scale * x - weigh.top) * to_place; };
+  auto weighs = [&](float x) { return (weigh.scale * x - weigh.top) * weigh.ch > -44.f; };
   auto bin_of = [&](float x) { return min((int)place_of(x), kBins - 2); };
   // The bin at which the counts or the weights, summed from the first on, reach `target`, what comes
   // before it and what is in it; target > all: the last one.  For every thread of the row.

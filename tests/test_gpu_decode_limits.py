@@ -1,7 +1,10 @@
 """Rotary positions, 4-bit products and drawing tokens at the ends of what their headers allow."""
+import math
+
+import numpy as np
 import pytest
 
-from tests.test_gpu_decode import _ints, _lib, _rand  # noqa: F401
+from tests.test_gpu_decode import _draws, _ints, _lib, _rand  # noqa: F401
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -36,3 +39,18 @@ def test_append_rotary_refuses_queries_beyond_what_it_counts():
     other = ContextCache(1, 1, 1, hd, 16, 1)
     other.append_rotary(0, r, None, k, k)
     assert torch.equal(held, other.read(0, 1, 1)[0])
+
+
+@pytest.mark.parametrize("low,high", [(2.0 ** -20, 1.0), (1.0, 2.0 ** 64), (2.0 ** 64, 2.0 ** 110), (2.0 ** 110, 3.4e38)])
+def test_weights_at_every_temperature(low, high):
+    """Two tokens, and u the float next to the share of the first: which one is drawn says on which side of u the share
+    lies.  Weights are good to 2^-42 (1e-12 from there on is decided), u and shares to 2^-25."""
+    rng = np.random.default_rng(1)
+    t = np.exp(rng.uniform(math.log(low), math.log(high), 4000)).astype(np.float32)
+    first = (rng.uniform(0.0, 1.0, 4000) * np.minimum(8.0 * t.astype(np.float64), 3.4e38)).astype(np.float32)
+    second = np.maximum(first.astype(np.float64) - rng.uniform(0.2, 3.0, 4000) * t, -3.4e38).astype(np.float32)
+    share = 1 / (1 + np.exp((second.astype(np.float64) - first) / t))
+    u = share.astype(np.float32)
+    clear = (np.abs(u - share) > 1e-12) & (u < 1)
+    assert clear.sum() > 3900
+    _draws(torch.from_numpy(np.stack([first, second], 1)[clear]).cuda(), u[clear], t=t[clear])
