@@ -419,12 +419,14 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(DrawArgs a) {
   if (mp > 0.f) {
     float limit = top;
     if (mp < 1.f) {
+      // (logits and T by a power of two, as Weigher takes them: T ln(min_p) may be beyond fp32 where the limit is not)
       const float2 l = log_of(mp, s.table);
-      const float h = t * l.x, hl = __fmaf_rn(t, l.x, -h) + t * l.y;
-      limit = top + h;
-      const float v = limit - top, rest = (top - (limit - v)) + (h - v) + hl;
+      const float by = 2.f * weigh.scale, tt = by * t, most = by * top;
+      const float h = tt * l.x, hl = __fmaf_rn(tt, l.x, -h) + tt * l.y;
+      limit = most + h;
+      const float v = limit - most, rest = (most - (limit - v)) + (h - v) + hl;
       if (rest > 0.f) limit = nextafterf(limit, inf);
-      limit = fminf(limit, top);
+      limit = fminf(limit * (by < 1.f ? 0x1p64f : 1.f), top);
     }
     last = (u64)key_of(limit) << 32;
   }

@@ -54,3 +54,16 @@ def test_weights_at_every_temperature(low, high):
     clear = (np.abs(u - share) > 1e-12) & (u < 1)
     assert clear.sum() > 3900
     _draws(torch.from_numpy(np.stack([first, second], 1)[clear]).cuda(), u[clear], t=t[clear])
+
+
+def test_min_p_at_temperatures_whose_border_is_far_below_the_row():
+    """T ln(min_p) is beyond fp32, the border that it makes is not: 3.4e38 - 4e38 lies within the row."""
+    rng = np.random.default_rng(0)
+    x = torch.from_numpy(rng.uniform(-3.39e38, 3.39e38, (8, 5000)).astype(np.float32)).cuda()
+    x[:, 7] = 3.4e38
+    t = [1e38, 1e38, 2e38, 2e38, 3.3e38, 3.3e38, 1.5e38, 1e20]
+    q = [math.exp(-4), 0.03, 0.15, 0.2, 0.17, 0.3, 0.07, 0.5]
+    for u in (0.0, 0.3, 0.7, 1 - 2.0 ** -24):
+        _draws(x, [u] * 8, t=t, q=q)
+        _draws(x, [u] * 8, t=t, q=q, p=[0.9] * 8)
+        _draws(x, [u] * 8, t=t, q=q, k=[400] * 8)
