@@ -539,8 +539,9 @@ class _Types:
     @classmethod
     def look_up(cls):
         import torch
-        cls.bf16, cls.f32, cls.i32, cls.u8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
+        cls.f32, cls.i32, cls.u8 = torch.float32, torch.int32, torch.uint8
         cls.get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+        cls.bf16 = torch.bfloat16   # (the last: says that all are there)
         return cls
 
 

@@ -70,3 +70,30 @@ def test_append_rotary_refuses_sizes_beyond_an_int(lib):
         with pytest.raises(ValueError, match="2\\^31"):
             cache.append_rotary(layer, rotary, None, k, k)
     rotary.handle = cache.handle = None   # (nothing to close)
+
+
+def test_types_are_looked_up_before_another_thread_may_use_them():
+    """Two threads' first calls: whoever finds the look-up done finds all of it.  (Looked at after each instruction.)"""
+    import sys
+
+    from paper_2609_34170_gb300 import _binding as B
+
+    class Fresh(B._Types):
+        bf16 = f32 = i32 = u8 = get_device = None
+
+    seen = []
+
+    def watch(frame, event, arg):
+        if frame.f_code.co_name != "look_up":
+            return None
+        frame.f_trace_opcodes = True
+        if Fresh.bf16 is not None:
+            seen.append(None not in (Fresh.f32, Fresh.i32, Fresh.u8, Fresh.get_device))
+        return watch
+
+    sys.settrace(watch)
+    try:
+        Fresh.look_up()
+    finally:
+        sys.settrace(None)
+    assert seen and all(seen) and Fresh.bf16 is torch.bfloat16
