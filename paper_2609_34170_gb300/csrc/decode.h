@@ -54,7 +54,17 @@ struct W4Matrix {
   uint2* sz;          // [tiles][groups][8]: (scale, 128 + zero) of rows g and g + 8; kPadGroups groups of zeros behind
   int N, K, group;
   int tiles, kblocks, groups;   // tiles: an even number
+  W4Matrix() = default;
+  W4Matrix(int n, int k, int g)
+      : codes(nullptr), sz(nullptr), N(n), K(k), group(g), tiles((n + 31) / 32 * 2), kblocks((k + 63) / 64), groups((k + g - 1) / g) {}
 };
+// Which kernel takes a product.
+enum W4Kernel { W4_FEW = 0 /* up to 8 tokens */, W4_TILES = 1 /* tiles of 16 */, W4_TC = 2 /* tcgen05, tiles of 32 or 64 */ };
+// What a test sets for its thread's products of more than 8 aligned tokens (ravel_debug_w4); -1: by the rule.
+inline int& w4_forced() {
+  static thread_local int kernel = -1;
+  return kernel;
+}
 struct W4Args {
   W4Matrix w;
   const void* x;
@@ -65,12 +75,13 @@ struct W4Args {
   int num_sms;
   int* err;
 };
+W4Kernel w4_kernel(const W4Args& a);
 cudaError_t launch_w4_gemm(const W4Args& a, cudaStream_t st);
 cudaError_t launch_w4_load(const W4Matrix& w, const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, cudaStream_t st);
 cudaError_t launch_w4_read(const W4Matrix& w, void* out, int ldo, Dtype dt, cudaStream_t st);
 cudaError_t launch_w4_quantize(const void* W, int N, int K, int ldw, Dtype dt, int group, uint8_t* codes, uint16_t* scales,
                                uint8_t* zeros, cudaStream_t st);
-cudaError_t launch_w4_tc(const W4Args& a, cudaStream_t st);   // more than 16 tokens
+cudaError_t launch_w4_tc(const W4Args& a, cudaStream_t st);   // aligned rows of tokens, any number
 cudaError_t init_w4_kernels();
 cudaError_t init_w4_tc_kernels();
 

@@ -203,14 +203,8 @@ ravel_status ravel_w4_create(int N, int K, int group, int device, ravel_w4_t** o
   if (N < 1 || K < 1 || N > (1 << 24) || K > (1 << 24)) return fail(RAVEL_ESHAPE, "w4_create: N and K must be 1 to 2^24");
   ravel_w4_t* w = new (std::nothrow) ravel_w4_t();
   if (!w) return fail(RAVEL_ENOMEM, "w4_create: no memory");
-  W4Matrix& m = w->m;
+  W4Matrix& m = w->m = W4Matrix(N, K, group);
   w->device = device;
-  m.N = N;
-  m.K = K;
-  m.group = group;
-  m.tiles = (N + 31) / 32 * 2;
-  m.kblocks = (K + 63) / 64;
-  m.groups = (K + group - 1) / group;
   const size_t codes = (size_t)m.tiles * m.kblocks * 512, sz = ((size_t)m.tiles * m.groups + kPadGroups) * 64;
   OnDevice on(device);
   cudaError_t e = on.e;

@@ -421,23 +421,47 @@ cudaError_t init_w4_kernels() {
   return e;
 }
 
-cudaError_t launch_w4_gemm(const W4Args& a, cudaStream_t st) {
-  if (a.M <= 8) return launch_nt<1>(a, st);
+W4Kernel w4_kernel(const W4Args& a) {
+  if (a.M <= 8) return W4_FEW;
+  if (!a.vec) return W4_TILES;   // (TMA takes aligned rows only)
+  if (w4_forced() >= 0) return (W4Kernel)w4_forced();
   // Tiles of 16 rows that go through the matrix each, from L2 after the first, or the tcgen05 kernel (an SM a CTA, a longer
   // start), whichever takes less by these times, in 10 ns: of tiles a start, rounds, blocks of 64 ks of a warp (faster where an
   // SM has one CTA) and a cluster's join; of tcgen05 a start and pieces of 128 ks of a CTA, longer where its sums are many.  us,
   // tiles / tcgen05, groups of 128: 16 rows x 4096 x 4096 5.8 / 7.7, x 8192 x 8192 13.5 / 16.3, x 65536 x 2048 26.7 / 26.1; 32 x
   // 2048 x 4096 5.8 / 6.7, x 3000 x 5000 9.3 / 8.2, x 8192 x 8192 25.6 / 16.7, x 1024 x 16384 13.3 / 15.6; 64 x 4096 x 1024
   // 6.4 / 6.7, x 1024 x 4096 5.8 / 7.4, x 2048 x 8192 13.5 / 10.6; 96 x 4096 x 1024 9.3 / 6.8; groups of 32, 16 x 4096 x 8192
-  // 14.3 / 12.1, 64 x 512 x 8192 9.2 / 15.2, 48 x 8192 x 1024 9.9 / 8.2.  (TMA takes aligned rows only.)
+  // 14.3 / 12.1, 64 x 512 x 8192 9.2 / 15.2, 48 x 8192 x 1024 9.9 / 8.2.
   const long long tiles = (a.M + 15) / 16, ctas = a.w.tiles / 2 * tiles;
   const int ranks = few_ranks(a, ctas);
   const long long rounds = (ctas * ranks + kHeld * a.num_sms - 1) / (kHeld * a.num_sms), blocks = (a.w.kblocks + kWarps * ranks - 1) / (kWarps * ranks);
   const bool g32 = a.w.group == 32, alone = !g32 && ctas * ranks <= a.num_sms;
   const long long as_tiles = 150 + rounds * (100 + blocks * (alone ? 45 : 70)) + (ranks > 1 ? 200 : 0);
-  const long long as_tc = 500 + W4TcPlan(a, a.M <= 32 ? 32 : 64).pieces * (a.M <= 32 ? (g32 ? 45 : 35) : g32 ? 70 : 40);
-  const bool tc = as_tc < as_tiles;
-  return a.vec && tc ? launch_w4_tc(a, st) : launch_nt<2>(a, st);
+  const long long as_tc = 500 + W4TcPlan(a, w4_tc_tokens(a.M)).pieces * (a.M <= 32 ? (g32 ? 45 : 35) : g32 ? 70 : 40);
+  return as_tc < as_tiles ? W4_TC : W4_TILES;
+}
+
+cudaError_t launch_w4_gemm(const W4Args& a, cudaStream_t st) {
+  switch (w4_kernel(a)) {
+    case W4_FEW: return launch_nt<1>(a, st);
+    case W4_TILES: return launch_nt<2>(a, st);
+    default: return launch_w4_tc(a, st);
+  }
+}
+
+// For tests: the kernel of this thread's products of more than 8 aligned tokens (else: by the rule), and what a product is
+// planned to be: its kernel and, on tcgen05, the tokens of a unit, CTAs, those that share a unit of the last round, and
+// whether there are full rounds before it.
+extern "C" void ravel_debug_w4(int kernel) { w4_forced() = kernel == W4_TILES || kernel == W4_TC ? kernel : -1; }
+extern "C" void ravel_debug_w4_plan(int N, int K, int group, int M, int aligned, int sms, int* out) {
+  W4Args a{W4Matrix(N, K, group), nullptr, nullptr, nullptr, M, K, N, EPI_STORE, 0, aligned, sms, nullptr};
+  out[0] = w4_kernel(a);
+  if (out[0] != W4_TC) return;
+  out[1] = w4_tc_tokens(M);
+  const W4TcPlan plan(a, out[1]);
+  out[2] = plan.grid;
+  out[3] = plan.ranks;
+  out[4] = (a.w.tiles + 7) / 8 * ((M + out[1] - 1) / out[1]) >= sms;
 }
 
 cudaError_t launch_w4_load(const W4Matrix& w, const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, cudaStream_t st) {

@@ -15,6 +15,7 @@ inline int w4_ranks(long long units, int kblocks, int blocks, int most, int sms)
   while (ranks < most && units * ranks * 2 <= sms && kblocks >= ranks * 2 * blocks) ranks *= 2;
   return ranks;
 }
+inline int w4_tc_tokens(int M) { return M <= 32 ? 32 : 64; }   // of a unit of the tcgen05 kernel
 // How the tcgen05 kernel goes through a matrix: the units (128 rows of weights x 32 or 64 tokens) of the last round, if
 // there are few, are shared (after full rounds, whose CTAs all have to be there at once, by 2 CTAs).  Clusters of 8 of CTAs
 // that fill an SM start late: 64 rows x 2048 x 8192 16.7 us with them, 10.8 with 4.

@@ -540,7 +540,7 @@ cudaError_t init_w4_tc_kernels() {
 }
 
 cudaError_t launch_w4_tc(const W4Args& a, cudaStream_t st) {
-  return a.M <= 32 ? launch_ntok<32>(a, st) : launch_ntok<64>(a, st);
+  return w4_tc_tokens(a.M) == 32 ? launch_ntok<32>(a, st) : launch_ntok<64>(a, st);
 }
 
 }  // namespace ravel
