@@ -65,6 +65,11 @@ inline int& w4_forced() {
   static thread_local int kernel = -1;
   return kernel;
 }
+// Launches of the tcgen05 kernel by this thread that are left to run with its tokens withheld (ravel_debug_w4_withhold).
+inline int& w4_withheld() {
+  static thread_local int launches = 0;
+  return launches;
+}
 struct W4Args {
   W4Matrix w;
   const void* x;
@@ -74,6 +79,7 @@ struct W4Args {
   int vec;            // rows of x are 16-byte aligned
   int num_sms;
   int* err;
+  int withhold = 0;   // fault injection (tests): no tokens are loaded, so that bounded waits run out
 };
 W4Kernel w4_kernel(const W4Args& a);
 cudaError_t launch_w4_gemm(const W4Args& a, cudaStream_t st);

@@ -453,6 +453,9 @@ cudaError_t launch_w4_gemm(const W4Args& a, cudaStream_t st) {
 // planned to be: its kernel and, on tcgen05, the tokens of a unit, CTAs, those that share a unit of the last round, and
 // whether there are full rounds before it.
 extern "C" void ravel_debug_w4(int kernel) { w4_forced() = kernel == W4_TILES || kernel == W4_TC ? kernel : -1; }
+// Fault injection for tests: this thread's next `launches` of the tcgen05 kernel load no tokens; every wait for them gives up
+// after a second, the CTAs give back what they hold and raise ERR_TIMEOUT, and outputs are not valid (no fault, no hang).
+extern "C" void ravel_debug_w4_withhold(int launches) { w4_withheld() = launches; }
 extern "C" void ravel_debug_w4_plan(int N, int K, int group, int M, int aligned, int sms, int* out) {
   W4Args a{W4Matrix(N, K, group), nullptr, nullptr, nullptr, M, K, N, EPI_STORE, 0, aligned, sms, nullptr};
   out[0] = w4_kernel(a);

@@ -368,7 +368,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
     int at = 0, scale_at = 0;
     uint32_t parity = 1u, scale_parity = 1u;
     long long issued = 0, batches = 0;
-    for (int round = 0; round < rounds && ok; ++round) {
+    for (int round = a.withhold ? rounds : 0; round < rounds && ok; ++round) {
       const int unit = unit_of(round), m0 = unit / row_tiles * NTOK, first = first_of(round), end = end_of(round);
       // (past the last tile: any that is finite; past the last group of a tile: the next one's, or zeros)
       const uint2* sz = w.sz + ((size_t)min(unit % row_tiles * 8 + (lane & 7), w.tiles - 1) * w.groups + first * kGroups) * 8;
@@ -540,7 +540,9 @@ cudaError_t init_w4_tc_kernels() {
 }
 
 cudaError_t launch_w4_tc(const W4Args& a, cudaStream_t st) {
-  return w4_tc_tokens(a.M) == 32 ? launch_ntok<32>(a, st) : launch_ntok<64>(a, st);
+  W4Args b = a;
+  b.withhold = w4_withheld() > 0 && w4_withheld()-- > 0;
+  return w4_tc_tokens(a.M) == 32 ? launch_ntok<32>(b, st) : launch_ntok<64>(b, st);
 }
 
 }  // namespace ravel

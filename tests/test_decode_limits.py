@@ -97,3 +97,22 @@ def test_types_are_looked_up_before_another_thread_may_use_them():
     finally:
         sys.settrace(None)
     assert seen and all(seen) and Fresh.bf16 is torch.bfloat16
+
+
+class _Matrix(C.Structure):
+    """A handle of a 4-bit matrix as far as its error word's mirror, on a device that there is not."""
+    _fields_ = [("codes", C.c_void_p), ("sz", C.c_void_p), ("sizes", C.c_int * 6), ("device", C.c_int * 2), ("err", C.c_void_p),
+                ("err_host", C.POINTER(C.c_int))]
+
+
+def test_an_error_of_earlier_work_is_reported_before_a_device_is_touched(lib):
+    word = C.c_int(0)
+    w = C.byref(_Matrix(None, None, (96, 64, 32, 6, 1, 2), (1 << 20, 0), None, C.pointer(word)))
+    for bits, status in ((1 << 1, 8), (1 << 2, 7), (3 << 1, 8)):   # a wait that ran out; any other
+        word.value = bits
+        assert lib.ravel_w4_gemm(w, 1 << 20, 3, 64, 0, 1 << 21, 96, 0, None, None) == status
+        assert b"error word" in lib.ravel_decode_last_error()
+        assert lib.ravel_w4_gemm(w, 1 << 20, 0, 64, 0, 1 << 21, 96, 0, None, None) == 0   # nothing to do
+    word.value = 0
+    lib.ravel_w4_gemm(w, 1 << 20, 3, 64, 0, 1 << 21, 96, 0, None, None)   # (ends at the device)
+    assert b"error word" not in lib.ravel_decode_last_error()

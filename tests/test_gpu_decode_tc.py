@@ -178,3 +178,27 @@ def test_first_calls_may_be_captured(which):
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     done = subprocess.run([sys.executable, "-c", FIRST_CALLS, root, str(which)], capture_output=True, text=True, timeout=300)
     assert done.returncode == 0 and "the same" in done.stdout, done.stderr[-2000:]
+
+
+@pytest.mark.parametrize("kernel", [TC], indirect=True)
+@pytest.mark.parametrize("n,k,m,group", [(256, 260, 20, 128), (384, 1100, 40, 64), (20480, 600, 58, 32)])
+def test_a_wait_that_runs_out_is_reported_until_a_reset(kernel, n, k, m, group):
+    """Tokens that are not loaded: the roles' waits give up after a second, later products of the matrix (of any number of
+    rows) are refused, others are not, and after a reset they are what they were."""
+    from paper_2609_34170_gb300 import RavelError, load
+    w, held = _held(n, k, group, n)
+    other, _ = _held(256, 260, 128, 1)
+    x, y = _tokens(m, k, 1), _tokens(20, 260, 2)
+    want, untouched = w.product(x, dtype=torch.float32), other.product(y)
+    _product_close(_np(want), _np(x), held, "store", "fp32")
+    load().ravel_debug_w4_withhold(1)
+    w.product(x, dtype=torch.float32)
+    torch.cuda.synchronize()
+    for rows in (x, x[:3]):
+        with pytest.raises(RavelError) as ei:
+            w.product(rows)
+        assert ei.value.status == 8   # RAVEL_ETIMEOUT
+    assert torch.equal(other.product(y), untouched)
+    np.testing.assert_array_equal(_np(w.read(torch.float32)), held.astype(np.float32))
+    w.reset()
+    assert torch.equal(w.product(x, dtype=torch.float32), want)
