@@ -67,3 +67,29 @@ def test_min_p_at_temperatures_whose_border_is_far_below_the_row():
         _draws(x, [u] * 8, t=t, q=q)
         _draws(x, [u] * 8, t=t, q=q, p=[0.9] * 8)
         _draws(x, [u] * 8, t=t, q=q, k=[400] * 8)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("layout,dims,interleaved", [((8, 1, 256), 256, False), ((16, 4, 64), 64, True), ((6, 2, 40), 16, True),
+                                                     ((4, 4, 128), 34, False), ((20, 1, 64), 64, False)])
+@pytest.mark.parametrize("n", [1, 5, 16, 17, 40])
+def test_append_rotary_in_place_leaves_the_rest_of_the_projection(layout, dims, interleaved, dtype, n):
+    """Queries turned in place, columns of one projection: its keys and values stay as they were, and so do query rows from
+    counts[b] on and those of a robot that is left out."""
+    from paper_2609_34170_gb300 import ContextCache, Rotary
+    hq, hkv, hd = layout
+    r = Rotary(dims, interleaved=interleaved)
+    cache = ContextCache(1, hq, hkv, hd, 64, 4, 1, dtype)
+    qkv = _rand((4, n, hq + 2 * hkv, hd), n, dtype, 2.0)
+    was = qkv.clone()
+    counts = [n, n // 2, 0, n]
+    starts = [3, 20, 9, 65 - n]   # (the last robot's tokens would pass the cache's end)
+    q, k, v = qkv[:, :, :hq], qkv[:, :, hq:hq + hkv], qkv[:, :, hq + hkv:]
+    assert cache.append_rotary(0, r, q, k, v, _ints(starts), counts=_ints(counts), q_out=q) is q
+    torch.cuda.synchronize()
+    cache.reset()
+    turned = r.apply(was[:, :, :hq], starts=_ints(starts))
+    for b in range(4):
+        c = counts[b] if b < 3 else 0
+        assert torch.equal(q[b, :c], turned[b, :c]) and torch.equal(q[b, c:], was[b, c:, :hq])
+    assert torch.equal(qkv[:, :, hq:], was[:, :, hq:])
