@@ -214,9 +214,6 @@ struct Turned16 {
   }
 };
 
-template <typename T>
-__device__ __forceinline__ void store16(T* row, int d, int hd, int vec, const float* x);
-
 // cache_append_kernel with the keys turned on their way in and, by CTAs of their own, the G query heads of
 // the KV head turned beside them.  A CTA's 16 tokens share one table of cosines and sines.  Keys alone of 816
 // tokens of 16 robots, one head of 256: 11.3 us where cache_append_kernel takes 4.8, for one and a third rounds of

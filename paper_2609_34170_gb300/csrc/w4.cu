@@ -287,12 +287,12 @@ __global__ void __launch_bounds__(256, kHeld) w4_gemm_kernel(W4Args a) {
     if (next_pair < pairs) {
       Slot<GS>& to = ring[next_slot];
       const int second = 2 * next_piece + 1 < w.kblocks ? 32 : 0;   // (past the last block there are no values, and its codes will do)
-      copy_async(&to.codes[0][0][lane], from0, true);
-      copy_async(&to.codes[0][1][lane], from1, true);
-      copy_async(&to.codes[1][0][lane], from0 + second, true);
-      copy_async(&to.codes[1][1][lane], from1 + second, true);
+      copy_async(&to.codes[0][0][lane], from0);
+      copy_async(&to.codes[0][1][lane], from1);
+      copy_async(&to.codes[1][0][lane], from0 + second);
+      copy_async(&to.codes[1][1][lane], from1 + second);
       if (sz_g < 4 / GS)
-        copy_async(&to.sz[sz_g][sz_t][q * 2], from_sz + (size_t)min(next_piece * (4 / GS) + sz_g, w.groups - 1) * 8, true);
+        copy_async(&to.sz[sz_g][sz_t][q * 2], from_sz + (size_t)min(next_piece * (4 / GS) + sz_g, w.groups - 1) * 8);
       from0 += 64;
       from1 += 64;
       ++next_piece;
@@ -323,7 +323,7 @@ __global__ void __launch_bounds__(256, kHeld) w4_gemm_kernel(W4Args a) {
           x[n][h] = make_uint4(0u, 0u, 0u, 0u);
           if (there[n] && k + q * 8 < w.K) x[n][h] = *(const uint4*)(rows[n] + k);
         } else {
-          x[n][h] = load_x(rows[n] - q * 8, k + q * 8, w.K, there[n], 0);
+          x[n][h] = load_x(rows[n] - q * 8, k + q * 8, w.K, there[n]);
         }
       }
   };

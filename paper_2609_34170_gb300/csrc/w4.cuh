@@ -40,10 +40,9 @@ __device__ __forceinline__ uint32_t sub_bf16x2(uint32_t a, uint32_t b) {
 
 // Eight values of a row from k on; what is not there is zero (a code past the end stands for
 // weight 0, but 0 times a neighbour's NaN is not).
-__device__ __forceinline__ uint4 load_x(const bf16* row, int k, int K, bool there, int vec) {
+__device__ __forceinline__ uint4 load_x(const bf16* row, int k, int K, bool there) {
   uint4 r = make_uint4(0u, 0u, 0u, 0u);
   if (!there || k >= K) return r;
-  if (vec && k + 8 <= K) return *(const uint4*)(row + k);
   uint16_t v[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = k + i < K ? ((const uint16_t*)row)[k + i] : 0;
@@ -69,8 +68,8 @@ __device__ __forceinline__ float over_ranks(const float* p, int ranks) {
   return v;
 }
 
-__device__ __forceinline__ void copy_async(void* to, const void* from, bool there) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(there ? 16 : 0) : "memory");
+__device__ __forceinline__ void copy_async(void* to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>

@@ -155,11 +155,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b) {   // (past the last block there are no values, and its codes will do)
         const size_t at = (size_t)min(kBlocks * next_piece + b, w.kblocks - 1) * 32;
-        copy_async(&to.codes[b][0][put], from0 + at, true);
-        copy_async(&to.codes[b][1][put], from1 + at, true);
+        copy_async(&to.codes[b][0][put], from0 + at);
+        copy_async(&to.codes[b][1][put], from1 + at);
       }
       if (sz_g < kGroups)
-        copy_async(&to.sz[sz_g][sz_t][(lane & 3) * 2], from_sz + (size_t)min(next_piece * kGroups + sz_g, w.groups - 1) * 8, true);
+        copy_async(&to.sz[sz_g][sz_t][(lane & 3) * 2], from_sz + (size_t)min(next_piece * kGroups + sz_g, w.groups - 1) * 8);
       if (++next_slot == kCodeRing) next_slot = 0;
       skip(kSets);
     }
