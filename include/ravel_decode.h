@@ -30,8 +30,10 @@ extern "C" {
  * interleaved, (2i, 2i + 1), by the angle a = p f_i, p the token's position:
  *   (x, y) -> amplitude * (x cos a - y sin a, x sin a + y cos a)
  * The others stay.  p is any int32 (the transpose, which is also the gradient, is
- * the rotation by -p); angles are reduced in 64-bit integers, so that far
- * positions lose nothing, and everything else is fp32, rounded once. */
+ * the rotation by -p).  The table holds f_i / (2 pi), computed in 64-bit floats, and p times it is
+ * reduced in 64-bit integers: an angle is off by no more than the table's rounding, p f_i 2^-51 (up to positions of
+ * 10^8 less than a rounding of fp32, in which everything else is; 3e-7 at 2^31), and results are rounded
+ * once.  Other rules for long contexts, a ramp over the dims' index say, are given as `frequencies`. */
 typedef struct {
   int dims;             /* even, 2 to 256 */
   int interleaved;      /* 0: pairs (i, i + dims / 2); 1: pairs (2i, 2i + 1) */
@@ -57,8 +59,11 @@ void ravel_rotary_destroy(ravel_rotary_t* r);
 /* Turn rows of heads.
  *   x, out     device [batch, n, heads, hd] of dtype; heads of a token are contiguous, token i of robot b
  *              begins at element b * robot_stride + i * token_stride.  out is x itself (with x's strides)
- *              or does not overlap it; its rows do not overlap each other.  Query and key heads that lie side by side are one call.
- *   hd         >= dims
+ *              or does not overlap it; its rows do not overlap each other: a robot's tokens lie before the next one's, or a
+ *              token's robots before the next one's (rows that interleave in another way are refused).  Query and
+ *              key heads that lie side by side are one call.
+ *   batch, heads  up to 65535; n up to 2^30
+ *   hd         dims to 256
  *   starts     device int32 [batch] or NULL (0): token i of robot b has position starts[b] + i ...
  *   positions  device int32 [batch, n] or NULL: ... or positions[b][i]
  *   counts     device int32 [batch] or NULL (n): tokens from counts[b] on are not written (a count below 0 is
@@ -70,10 +75,12 @@ ravel_status ravel_rotary_apply(ravel_rotary_t* r, int batch, int n, int heads, 
 
 /* ravel_cache_append of keys turned to their positions, and the queries turned
  * with them, in one call.  Between a turned key and the cache nothing is rounded
- * but to the cache's own values.
+ * but to the cache's own values.  (For prompts two calls, ravel_rotary_apply and ravel_cache_append, take less
+ * time, 27 us for 816 tokens of 16 robots with 8 heads of 256 where this takes 31, and round keys to the cache's
+ * type in between.)
  *   q, q_out   device [batch, n, Hq, hd] of the cache's dtype, or both NULL; q_out is q itself (with q's strides)
- *              or overlaps none of the others; its rows do not overlap each other.  Hq * (hd rounded up to 64) is at
- *              most 2^30
+ *              or overlaps none of the others; its rows do not overlap each other (as above).  Hq * (hd rounded up to
+ *              64) is at most 2^30
  *   k, v       as for ravel_cache_append, each with strides of its own; they are not written
  *   positions  device int32 [batch, n] or NULL: starts[b] + i
  *   starts, counts  as for ravel_cache_append; rows of q_out from counts[b] on are not written
@@ -89,7 +96,8 @@ ravel_status ravel_cache_append_rotary(ravel_cache_t* c, int layer, const ravel_
  * Row n of a matrix W [N, K] holds for each k a code c of 0 .. 15 and for each group
  * of `group` ks a zero point z of 0 .. 15 and a bf16 scale s: w = (c - z) s.  Codes
  * come two to a byte (even k in the low nibble), [N, (K + 1) / 2]; scales and zeros
- * [N, (K + group - 1) / group]. */
+ * [N, (K + group - 1) / group].  Scales held in another type are rounded to bf16 by the caller: of an
+ * fp16 scale that moves its group's weights by up to 2^-8 of their size, 0.06 of a step of the codes at most. */
 typedef struct ravel_w4_ctx ravel_w4_t;
 
 /* Allocate an N x K matrix (about N K / 2 + 4 N K / group bytes) on `device`, all zeros.
@@ -106,13 +114,14 @@ ravel_status ravel_w4_reset(ravel_w4_t* w);
 /* Codes, scales and zeros (device, as above, contiguous) into the matrix, in the order
  * in which the products read them.  Scales are finite.  Waits until `stream` is done, because
  * products read weights ahead of their place on a stream; refused (RAVEL_EINVAL)
- * on a stream that is being captured.  No product may be running. */
+ * on a stream that is being captured.  No product may be running.  (20 us for 2560 x 1024, 72 for 8192 x 8192, 530 for
+ * 65536 x 8192.) */
 ravel_status ravel_w4_load(ravel_w4_t* w, const void* codes, const void* scales, const void* zeros, void* stream);
 
 /* Nearest codes of a matrix: per row and group s = (max(w, 0) - min(w, 0)) / 15 in
  * bf16, z = -min(w, 0) / s and c = w / s + z, both rounded to nearest (ties to even)
  * and limited to 0 .. 15; a group of zeros has s = z = c = 0.  For values of
- * up to 3e38 (codes of a larger one may stand for more than fp32 holds).
+ * up to 3e38 (codes of a larger one may stand for more than fp32 holds).  (160 us for 8192 x 8192 in bf16.)
  *   W  device [N, ldw] of dtype, first K columns; codes, scales, zeros device, written
  * Enqueued on `stream` of the current device. */
 ravel_status ravel_w4_quantize(const void* W, int N, int K, int ldw, int dtype, int group, void* codes, void* scales,
@@ -120,7 +129,7 @@ ravel_status ravel_w4_quantize(const void* W, int N, int K, int ldw, int dtype, 
 
 /* The matrix as values: out [N, ldo] of dtype, its first K columns written ((c - z) s in
  * fp32, which holds it exactly, or rounded to bf16), for example for ravel_gemm on
- * whole prompts.  Enqueued on `stream`. */
+ * whole prompts.  Enqueued on `stream`.  (120 us for 8192 x 8192.) */
 ravel_status ravel_w4_read(ravel_w4_t* w, void* out, int ldo, int dtype, void* stream);
 
 /* out (op)= X W^T (+ bias), the epilogues of ravel_gemm:
@@ -146,7 +155,7 @@ ravel_status ravel_w4_gemm(const ravel_w4_t* w, const void* X, int M, int lda, i
  *   of those the ones with w_i >= min_p (min_p above 1 counts as 1),
  * and the token is the lowest index for which the weights of what stays, summed in the
  * order of the index, exceed u times their sum.  T < 2^-20 (0, say): the first of the order.
- * Sums are of whole numbers (weights to 2^-43), so that no order of summation enters
+ * Sums are of whole numbers (weights in units of 2^-43, computed to some 2^-42 whatever T), so that no order of summation enters
  * the result and ties are ties.
  *   logits       device [batch, row_stride] of dtype, vocab columns (vocab up to 2^20)
  *   u            device float32 [batch], 0 <= u < 1

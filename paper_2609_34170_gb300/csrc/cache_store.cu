@@ -589,8 +589,11 @@ cudaError_t launch_cache_append(const AppendArgs& a, Dtype dt, cudaStream_t st) 
 
 cudaError_t launch_cache_append_rotary(const AppendRotaryArgs& a, Dtype dt, cudaStream_t st) {
   // Queries of few tokens in the same launch: a token of 64 robots (8 query heads on one of 256) 2.9 us, turned and
-  // stored by two calls 3.7.  Of many in one that streams them: 816 tokens of 16 robots 31 us (81 in one launch;
-  // two calls, whose keys are rounded to bf16 in between, 27).  (A grid has 65535 rows of CTAs, a cache up to as many heads.)
+  // stored by two calls 3.7.  Of many in one that streams them: 816 tokens of 16 robots 31 us (46 in one launch;
+  // two calls, whose keys are rounded to bf16 in between, 27).  One launch / two, n tokens of 16 robots, 8 heads on one of 256: 1
+  // 2.7 / 4.5 us, 4 3.9 / 4.6, 8 6.0 / 5.2, 16 10.3 / 6.4, 32 11.0 / 6.7; of 64 robots 4 5.5 / 5.4, 16 15.6 / 9.0; 16 robots
+  // with 16 heads on 4 of 64: 8 3.7 / 4.8, 16 5.7 / 5.6, 32 6.2 / 6.3, 64 6.8 / 9.4.  (16 is right for the latter, late by half for
+  // heads of 256 that share one KV head.)  (A grid has 65535 rows of CTAs, a cache up to as many heads.)
   const bool apart = a.q && (a.n > 16 || a.c.Hkv > 65535 / 2);
   if (apart) {
     RotaryArgs r{a.r, a.q, a.q_out, a.q_robot, a.q_token, a.qo_robot, a.qo_token, a.batch, a.n, a.c.Hkv * a.G, a.c.hd,

@@ -18,8 +18,13 @@
 // settings of their own 27; 64 rows of 128001 fp32 logits under top-p 0.9 53 us, of which the histogram takes 26 (80
 // instructions a logit, 50 of them its weight, and three atomics), the list 7, the first
 // pass 3 (66 with the weights before the border computed once more, and rows that begin between 16 bytes read value by
-// value); the same without limits 30, with top-k 50 24, with top-k 3000 and top-p 71, all logits equal 457.  Weights two
+// value); the same without limits 29, with top-k 50 24, with top-k 3000 and top-p 68, all logits equal 459.  Weights two
 // at a time in packed operations, and 64-bit atomics, are no faster.
+//
+// A list by all threads / by histograms / sorted, one row of 65536 under top-p 0.95 and top-k 40: 11.7 / 16.7 / 15.0 us;
+// 100: 13.2 / 17.4 / 15.4; 200: 17.2 / 17.9 / 17.1; 256: 18.3 / 18.1 / 21.3; 1000: - / 22.3 / 30.2; 2000: - / 26.6 / 32.7.  A
+// list of up to 256 sorted by counting, else exchanges: the same row under top-p 0.9, whose border's bin is sorted, 23.2 /
+// 27.4.
 #include <algorithm>
 
 #include "common.cuh"
@@ -69,8 +74,8 @@ __device__ __forceinline__ float value_of(uint32_t key) {
 // exp((x - top) / T) as a whole number.  In the log2 domain y = (x - top) * c with c = log2(e) / T
 // in two floats, and the difference and its product with their rounding errors: yh + ye.  With q
 // the nearest whole number to 1024 yh, 2^y = 2^(q / 1024) 2^f, the first factor from a table, 2^f = 1 + r
-// from its series, r below 2^-11, whose first term is a product in two floats.  About 2^-43 of the
-// weight off.  (In fp32 a weight is 2^-22 off and its error grows with x: at 100000 tokens one
+// from its series, r below 2^-11, whose first term is a product in two floats.  Some 2^-42 of the
+// weight off: r's two roundings, and the product of r with the table's own remainder, which is left out.  (In fp32 a weight is 2^-22 off and its error grows with x: at 100000 tokens one
 // border in a hundred falls elsewhere than in 64 bits.)
 // Logits are halved, so that no difference overflows, and where T is above 2^64 taken by 2^-65 (as T by 2^-64), or
 // c's second float, from 10^32 on, and its first, from 2 10^38 on, would lack bits.
@@ -1041,7 +1046,10 @@ cudaError_t init_draw_kernels() {
 }
 
 cudaError_t launch_draw(const DrawArgs& a, Dtype dt, cudaStream_t st) {
-  // CTAs of a row: up to 8 while there are SMs for all, and work for their warps
+  // CTAs of a row: up to 8 while there are SMs for all, and 4096 logits for each.  One bf16 row under top-k 40 and top-p
+  // 0.95 with 2048 / 4096 / 8192 logits to a CTA, us: 4096 logits 11.3 / 9.1 / 9.1, 8192 11.7 / 11.2 / 9.1, 16384 11.7 /
+  // 11.4 / 11.1, 32768 11.7 / 11.7 / 11.5; under top-p 0.9 alone 19.5 / 16.9 / 16.8, 20.7 / 19.8 / 17.0, 21.8 / 22.1 /
+  // 21.2, 25.1 / 25.1 / 25.5.  (8192 would be the better line for rows of 8192 to 16384.)
   int ranks = 1;
   while (ranks < kRanks && (long long)a.batch * ranks * 2 <= a.num_sms && a.vocab >= ranks * 2 * 4096) ranks *= 2;
   const Overlap overlap;

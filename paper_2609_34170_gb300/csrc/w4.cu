@@ -241,13 +241,16 @@ __device__ __forceinline__ void put_sums(float* to, const float (*acc)[NT][4], i
 // through them one after another, and the copies of the next pair's weights run on under the end of the one
 // before: each warp has a ring of its own, filled by asynchronous copies.
 //
-// Sums: an MMA chain per group (at most 64 ks of it) starts from zero, and the group's scale
+// Sums: an MMA chain per group (at most 128 ks) starts from zero, and the group's scale
 // takes its result into an fp32 sum, so that weights enter as whole numbers and no scaled weight
 // is rounded.  Parts of the ks are joined in the order of warps and ranks.
 //
 // Small matrices are a chain's latency: 1 row x 2560 x 1024 2.1 us (replays from a graph), 16 x 1024 x 4096 4.7 in fp32 to a
-// residual.  Large ones are bound by the codes' widening, 11 instructions for every 8 codes, most of them on the half-rate
-// integer pipe: 1 row x 65536 x 2048 19.8 us (3.6 TB/s of 6.7), x 8192 x 8192 11.0; 16 rows x 8192 x 8192 13.5.  With
+// residual.  Large ones are bound by instructions: 191 for 2048 codes, 88 of them the codes' widening (11 for every 8 codes of
+// a lane), most of which take the half-rate integer pipe.  1 row x 65536 x 8192: that pipe is busy for 73 % of an SM's active
+// cycles, the schedulers issue in 63 %, DRAM gives half its rate; of the 5.3 cycles between a warp's instructions 1.2 wait
+// for a full pipe, 1.2 for another warp's turn, 0.9 for the instruction before, 0.3 for memory.  1 row x 65536 x 2048 19.8 us
+// (3.6 TB/s of 6.7), x 8192 x 8192 11.0; 16 rows x 8192 x 8192 13.5.  With
 // pieces of 64 ks 22.4, 12.3 and 15.7 (the copies' instructions and waits twice as often); those with three CTAs an SM and 80
 // registers 23 and 18.5, with a division and 64-bit addresses a piece 27.5 and 23.
 constexpr int kRing = 3;   // pieces of 128 ks

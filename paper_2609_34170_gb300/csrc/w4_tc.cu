@@ -25,10 +25,11 @@ namespace {
 // So weights enter as whole numbers, as in the other kernels; no scaled weight is rounded.
 //
 // 64 rows x 65536 x 8192 with groups of 128 (268 MB of codes) 93 us: 3.0 TB/s, 0.74 PFLOP/s.  What bounds it is
-// neither memory (44 us) nor the tensor core (a fifth of its cycles; an MMA of 128 x NTOK x 16 takes 71 at any NTOK up to
-// 128: 55 us) but the roles' own instructions, some ten cycles each with 22 warps on four schedulers: of the 800
-// cycles that a piece takes, the warps that sum need all for some 100 of them, the MMA warp 700 for its wait, eight MMAs and
-// a commit, a warp that widens 1800 on every third piece.  Measured on the way here (same product, us): mma.sync with eight
+// neither memory (44 us) nor the tensor pipe (busy for 30 % of an SM's active cycles) but the roles' own instructions, some ten
+// cycles each with 22 warps on four schedulers (which issue in 66 % of the cycles, the integer pipe busy for 65 %): of
+// the 830 cycles that a piece takes at the 1.93 GHz seen, the warps that sum need all for some 100 of them, a warp that widens
+// 1800 on every third piece, and the MMA warp 700 for its wait, a commit and eight MMAs, each of which (128 x NTOK x 16) keeps it for
+// 71 at any NTOK up to 128: 568 cycles of a piece, 63 us in all.  Measured on the way here (same product, us): mma.sync with eight
 // pairs of tiles sharing the tokens 267; tokens by asynchronous copies of four warps 225; pieces of 64 ks 185; A in shared
 // memory, three pieces in the making, scales by copies of each thread 124; A in tensor memory and scales by bulk copies
 // 111; the last of 3.4 rounds shared by pairs of CTAs and outputs without a branch each 98; units joined a token to a

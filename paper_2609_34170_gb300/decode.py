@@ -50,7 +50,8 @@ class Rotary(_Handle):
     the angle position * f_i, f_i = base^(-2i / dims).  For contexts longer than a model was trained
     on, frequencies are divided by `factor`: all of them, or, with an original_length, in full those
     that make at most `low` turns over it, not those that make `high` or more, and in between in
-    proportion.  amplitude scales what is turned; frequencies [dims / 2] replaces the f_i."""
+    proportion (to those turns; for tables that go by the dims' index, give frequencies).  amplitude scales
+    what is turned; frequencies [dims / 2] replaces the f_i."""
     _destroy = staticmethod(B.ravel_rotary_destroy)
 
     def __init__(self, dims: int, base: float = 10000.0, interleaved: bool = False, factor: float = 1.0,
@@ -73,7 +74,7 @@ class Rotary(_Handle):
 
 class Weights4(_Handle):
     """A matrix [n, k] of 4-bit weights (c - z) s, with a zero point and a bf16 scale per
-    `group` (32, 64 or 128) ks of a row."""
+    `group` (32, 64 or 128) ks of a row.  (fp16 scales rounded to bf16 move by up to 2^-8 of their size.)"""
     _destroy = staticmethod(B.ravel_w4_destroy)
 
     def __init__(self, n: int, k: int, group: int = 128, device: int = 0):
