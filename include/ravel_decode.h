@@ -31,9 +31,9 @@ extern "C" {
  *   (x, y) -> amplitude * (x cos a - y sin a, x sin a + y cos a)
  * The others stay.  p is any int32 (the transpose, which is also the gradient, is
  * the rotation by -p).  The table holds f_i / (2 pi), computed in 64-bit floats, and p times it is
- * reduced in 64-bit integers: an angle is off by no more than the table's rounding, p f_i 2^-51 (up to positions of
- * 10^8 less than a rounding of fp32, in which everything else is; 3e-7 at 2^31), and results are rounded
- * once.  Other rules for long contexts, a ramp over the dims' index say, are given as `frequencies`. */
+ * reduced in 64-bit integers: an angle is off by no more than p times the table's rounding, f_i 2^-51 (of frequencies
+ * between low and high their formula's): up to positions of 10^8 less than a rounding of fp32, in which everything else
+ * is, 3e-7 at 2^31.  Results are rounded once.  Other rules for long contexts, a ramp over the dims' index say, are given as `frequencies`. */
 typedef struct {
   int dims;             /* even, 2 to 256 */
   int interleaved;      /* 0: pairs (i, i + dims / 2); 1: pairs (2i, 2i + 1) */

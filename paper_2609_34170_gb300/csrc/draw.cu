@@ -75,8 +75,9 @@ __device__ __forceinline__ float value_of(uint32_t key) {
 // in two floats, and the difference and its product with their rounding errors: yh + ye.  With q
 // the nearest whole number to 1024 yh, 2^y = 2^(q / 1024) 2^f, the first factor from a table, 2^f = 1 + r
 // from its series, r below 2^-11, whose first term is a product in two floats.  Some 2^-42 of the
-// weight off: r's two roundings, and the product of r with the table's own remainder, which is left out.  (In fp32 a weight is 2^-22 off and its error grows with x: at 100000 tokens one
-// border in a hundred falls elsewhere than in 64 bits.)
+// weight off: r's two roundings, and the product of r with the table's own remainder, which is left out.  (In fp32 a
+// weight is 2^-22 off and its error grows with x: at 100000 tokens one border in a hundred falls elsewhere than in
+// 64 bits.)
 // Logits are halved, so that no difference overflows, and where T is above 2^64 taken by 2^-65 (as T by 2^-64), or
 // c's second float, from 10^32 on, and its first, from 2 10^38 on, would lack bits.
 struct Weigher {
